@@ -16,16 +16,20 @@
  *   gist_gcn_layer_bwd_sgd     the backward pass with the SGD step fused   (device)
  *   gist_gat_layer_fwd/_bwd    the graph attention layer GIST also trains (device)
  *   gist_softmax_xent          loss and its gradient                    (device)
+ *   gist_log_probs/_bwd        log probabilities, entropy, best classes (device)
+ *   gist_embed_*               learned input rows and their gradient    (device)
  *   gist_sgd_update            one SGD step                             (device)
  *   gist_adam_update           one Adam step (the experiments' optimizer) (device)
  *   gist_adam_update_dev       the same, coefficients read from the device (device)
+ *   gist_muon_update           momentum step along an orthogonal factor (device)
  *   gist_subagg                subAgg: Theta[D_in, D_out] <- Theta^(i)  (device)
  *   gist_subagg_gather         subAgg of one round + gather of the next (device)
  *   gist_subagg_mean           subAgg of an unsplit parameter: mean of copies (device)
  *   gist_capture_* / replay_*  record library calls once, replay them      (device)
  *
  * Conventions
- *  - Every matrix is row-major fp32 with the leading dimension stated.
+ *  - Every matrix is row-major fp32 with the leading dimension stated (the
+ *    calls that take a gist_store also read or write 16-bit elements).
  *  - "device" pointers are HIP device memory on the context's device; the
  *    caller owns every buffer.  The library never frees caller memory and
  *    never allocates device memory inside these calls: scratch space is
@@ -224,9 +228,17 @@ typedef enum gist_layer_kind { GIST_LAYER_GCN = 0, GIST_LAYER_SAGE_MEAN = 1 } gi
 typedef enum gist_act { GIST_ACT_NONE = 0, GIST_ACT_RELU = 1 } gist_act;
 typedef enum gist_dtype {
   GIST_DTYPE_F32 = 0,      /* fp32 operands, fp32 MFMA                        */
-  GIST_DTYPE_BF16_IN = 1   /* GEMM operands rounded to bf16 (nearest-even),    */
+  GIST_DTYPE_BF16_IN = 1,  /* GEMM operands rounded to bf16 (nearest-even),    */
                            /* fp32 accumulation; aggregation stays fp32        */
+  GIST_DTYPE_F16_IN = 2    /* operands rounded to fp16: gist_orthogonalize and */
+                           /* gist_muon_update only                            */
 } gist_dtype;
+/* How the elements of a table or of logits are stored. */
+typedef enum gist_store {
+  GIST_STORE_F32 = 0,
+  GIST_STORE_BF16 = 1,
+  GIST_STORE_F16 = 2
+} gist_store;
 typedef enum gist_order {
   GIST_ORDER_AUTO = 0,        /* GCN: aggregate at min(s_in, s_out)        */
   GIST_ORDER_AGG_FIRST = 1,   /* (Abar H) W                                 */
@@ -434,6 +446,42 @@ gist_status gist_gat_layer_bwd(gist_ctx* ctx, const gist_gat_desc* D, const gist
                                float* da_src, float* da_dst, float* dH, void* ws,
                                size_t ws_bytes);
 
+/* ---- learned input rows --------------------------------------------- */
+
+/* out[i][:] = scale * table[ids[i]][:], i < n: rows of a learned table (node
+ * embeddings of a graph without features, ids the mini-batch's node map; or
+ * tokens), or of a frozen one kept in 16 bits.  table is V x d, stored as
+ * `store` (gist_store) with leading dimension ldt; out is fp32 with leading
+ * dimension ldo.  One product and one rounding per element.  An id outside
+ * [0, V) is padding: its row of out is zero and nothing is read for it.
+ * Errors: GIST_E_INVAL (negative n or V, d < 1, ldt < d, ldo < d, unknown
+ * store, non-finite scale, NULL pointers with n > 0; V == 0 needs no table),
+ * GIST_E_UNSUPPORTED (n or V >= 2^31 - 1, d above 2^22). */
+gist_status gist_embed_lookup(gist_ctx* ctx, int64_t n, int64_t V, int32_t d, const void* table,
+                              int64_t ldt, int32_t store, const int32_t* ids, float scale,
+                              float* out, int64_t ldo);
+
+/* The gradient of the table: dTable[v][:] = scale * sum over i with
+ * ids[i] == v of dY[i][:], for every v < V; a row that no id names is zero.
+ * dY is n x d (leading dimension ldy), dTable V x d (ldg, overwritten), both
+ * fp32.  The ids are sorted (stably) and every row's terms summed in fp32 in
+ * a fixed order, so results are deterministic: no floating-point atomics.
+ * Ids outside [0, V) contribute nothing.  Columns past d are left as they
+ * were.  `ws` needs gist_embed_grad_workspace(n, V, d) bytes (0 for
+ * arguments the calls reject).  Errors as gist_embed_lookup, and
+ * GIST_E_NOMEM for a small workspace. */
+size_t gist_embed_grad_workspace(int64_t n, int64_t V, int32_t d);
+gist_status gist_embed_grad(gist_ctx* ctx, int64_t n, int64_t V, int32_t d, const int32_t* ids,
+                            float scale, const float* dY, int64_t ldy, float* dTable, int64_t ldg,
+                            void* ws, size_t ws_bytes);
+/* The same with the SGD step fused in: table[v] <- table[v] - lr dTable[v]
+ * for the rows that ids name, in place; no other row is read or written.
+ * Bitwise gist_embed_grad followed by gist_sgd_update on those rows.  lr = -1
+ * adds the gradient to a dense accumulator. */
+gist_status gist_embed_grad_sgd(gist_ctx* ctx, int64_t n, int64_t V, int32_t d,
+                                const int32_t* ids, float scale, const float* dY, int64_t ldy,
+                                float lr, float* table, int64_t ldt, void* ws, size_t ws_bytes);
+
 /* ---- loss (Section 2.1: the sub-GCN output keeps the global width, so the
  *      loss is the usual one) ---------------------------------------- */
 
@@ -473,6 +521,48 @@ gist_status gist_softmax_xent_padded(gist_ctx* ctx, int64_t n, int32_t C,
 gist_status gist_softmax_xent_noalloc(gist_ctx* ctx, int64_t n, int32_t C,
                                       const float* logits, const int32_t* labels,
                                       float* loss_dev, float* dlogits);
+
+/* ---- log probabilities ------------------------------------------------ */
+
+/* Per row v < n of logits z (n x C, stored as `store`, leading dimension
+ * ldz), all outputs fp32 and any of them NULL when not wanted:
+ *   lse[v]     = log sum_j exp z_j
+ *   logp[v]    = z_y - lse, y = tokens[v] the row's given class
+ *   entropy[v] = - sum_j p_j log p_j,  p = softmax(z)
+ *   top_logp[v][k], top_idx[v][k], k < K (both n x K, or both NULL with
+ *              K == 0): the K largest z_j - lse, descending, equal logits by
+ *              ascending class.  K <= min(C, GIST_LOG_PROBS_MAX_TOP).
+ * Sums and maxima are fp32; a row is read once.
+ * Masked classes: a logit of -Inf has probability 0 and adds nothing; its
+ * log probability is -Inf.  A row that is -Inf throughout has lse -Inf,
+ * logp and top_logp -Inf, entropy 0 and the classes 0 .. K-1.  A row that
+ * holds a NaN or +Inf has NaN outputs and top_idx -1.
+ * Tokens: a negative one means no given class (logp 0; its gradient has no
+ * log-probability term); one >= C is the caller's error, reported as a NaN
+ * logp (and gradient row).  logp != NULL requires tokens.
+ * `ws` needs gist_log_probs_workspace(n, C, K) bytes, which may be 0.
+ * Errors: GIST_E_INVAL (n < 0, C < 1, ldz < C, unknown store, K out of
+ * range, top outputs not matching K, NULL logits with n > 0, logp without
+ * tokens), GIST_E_UNSUPPORTED (n or C >= 2^31 - 1), GIST_E_NOMEM. */
+#define GIST_LOG_PROBS_MAX_TOP 64
+size_t gist_log_probs_workspace(int64_t n, int64_t C, int32_t K);
+gist_status gist_log_probs(gist_ctx* ctx, int64_t n, int64_t C, const void* logits, int64_t ldz,
+                           int32_t store, const int32_t* tokens, float* logp, float* entropy,
+                           float* lse, int32_t K, float* top_logp, int32_t* top_idx, void* ws,
+                           size_t ws_bytes);
+/* Gradient of sum_v (g_logp[v] logp[v] + g_entropy[v] entropy[v]) with
+ * respect to the logits:
+ *   dz_j = g_logp (1[j = y] - p_j) - g_entropy p_j (log p_j + entropy),
+ * formed in fp32 from the logits, the lse and entropy of the forward call,
+ * and rounded once to `store`.  dlogits is n x C (leading dimension ldd,
+ * stored as the logits) and may be the logits themselves.  g_logp (then
+ * tokens) or g_entropy (then entropy) may be NULL, meaning zero.  A row that
+ * is -Inf throughout has gradient 0; a row with a NaN lse, a NaN gradient.
+ * Errors as gist_log_probs. */
+gist_status gist_log_probs_bwd(gist_ctx* ctx, int64_t n, int64_t C, const void* logits,
+                               int64_t ldz, int32_t store, const int32_t* tokens,
+                               const float* lse, const float* entropy, const float* g_logp,
+                               const float* g_entropy, void* dlogits, int64_t ldd);
 
 /* ---- subGCNs slice gather (Section 2.1) ----------------------------- */
 
@@ -523,6 +613,60 @@ gist_status gist_adam_coefficients(float lr, float beta1, float beta2, float eps
 gist_status gist_adam_update_dev(gist_ctx* ctx, float* W, const float* dW, float* m, float* v,
                                  int64_t n, float beta1, float beta2, float eps,
                                  const float* coef_dev);
+
+/* ---- orthogonalised updates ------------------------------------------- */
+
+/* Newton-Schulz orthogonalisation of `groups` matrices (rows x cols, row-major,
+ * one after another: a layer's [W_self; W_neigh], or stacked slices):
+ *   X = U / max(||U||_F, eps), then `steps` times, with the smaller of the two
+ *   sides as rows (X transposed otherwise):
+ *   A = X X^T,  B = b A + c A A,  X = a X + B X,   (a, b, c) = coef.
+ * With the usual coefficients (3.4445, -4.7750, 2.0315) and five steps the
+ * singular values end between about 0.7 and 1.2 (Jordan et al., the Muon
+ * optimiser); singular vectors are kept.  The norm is summed in double.
+ *   dtype GIST_DTYPE_F32      every operand of a product is held in two fp16
+ *         parts (22 to 23 significant bits), sums in fp32; output fp32;
+ *   dtype GIST_DTYPE_F16_IN   operands are rounded once to fp16 (scaled by
+ *         2^12, so that entries down to 2^-26 keep all 11 bits), sums in fp32:
+ *         a third of the matrix work.  gist_orthogonalize then writes fp16.
+ * Entries are held up to 15 in magnitude, so the coefficients must not let a
+ * singular value of [0, 1] (or its square, or |b s^2 + c s^4|) grow past 8 in
+ * any step (checked; GIST_E_INVAL).  A zero matrix gives zero; a matrix holding NaN or
+ * Inf gives NaN throughout, in its own group only. */
+typedef struct gist_muon_desc {
+  int64_t rows, cols;
+  int32_t groups;  /* matrices (0 means 1)                                */
+  int32_t dtype;   /* GIST_DTYPE_F32 or GIST_DTYPE_F16_IN                 */
+  int32_t steps;   /* Newton-Schulz steps, 1 .. 32                        */
+  uint32_t flags;  /* GIST_MUON_NESTEROV | GIST_MUON_FRESH (update only)  */
+  float coef[3];   /* a, b, c                                             */
+  float eps;       /* > 0: smallest divisor                               */
+} gist_muon_desc;
+enum {
+  GIST_MUON_NESTEROV = 1,
+  GIST_MUON_FRESH = 2      /* the incoming momentum counts as zero        */
+};
+/* Device bytes both calls need. */
+gist_status gist_muon_workspace_size(const gist_muon_desc* D, size_t* bytes);
+/* O = the orthogonalised G (groups x rows x cols): fp32, or fp16 with
+ * GIST_DTYPE_F16_IN.  The update's flags are ignored.  Errors: GIST_E_INVAL
+ * (NULL pointers, rows, cols or groups out of range, unknown dtype or flags,
+ * steps, eps or coefficients out of range), GIST_E_UNSUPPORTED (rows or cols
+ * above 65,536), GIST_E_NOMEM.  rows == 0 or cols == 0 is a no-op. */
+gist_status gist_orthogonalize(gist_ctx* ctx, const gist_muon_desc* D, const float* G, void* O,
+                               void* ws, size_t ws_bytes);
+/* One step of momentum with an orthogonalised direction (Muon), for the
+ * weight matrices gist_sgd_update and gist_adam_update step element by element:
+ *   M <- momentum M + (1 - momentum) dW
+ *   U  = M, or with GIST_MUON_NESTEROV (1 - momentum) dW + momentum M
+ *   W <- (1 - lr weight_decay) W - lr scale X,  X = U orthogonalised.
+ * W and M (groups x rows x cols fp32) are updated in place, dW is read.  `scale`
+ * sizes the update: sqrt(max(1, cols / rows)), or 0.2 sqrt(max(rows, cols))
+ * for steps the size of Adam's.  Errors as gist_orthogonalize, and GIST_E_INVAL
+ * for momentum outside [0, 1) or a non-finite lr, weight_decay or scale. */
+gist_status gist_muon_update(gist_ctx* ctx, const gist_muon_desc* D, float* W, const float* dW,
+                             float* M, float lr, float momentum, float weight_decay, float scale,
+                             void* ws, size_t ws_bytes);
 
 /* ---- subAgg (Section 2.2) ------------------------------------------- */
 

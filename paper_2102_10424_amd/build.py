@@ -15,7 +15,7 @@ OUT = os.path.join(PKG, "libgist.so")
 BUILD = os.path.join(PKG, "_build")
 
 HIP_SOURCES = ["api.hip", "spmm.hip", "spmm_tile.hip", "gemm.hip",
-               "elementwise.hip", "gat.hip"]
+               "elementwise.hip", "gat.hip", "embed.hip", "logprob.hip", "muon.hip"]
 HOST_SOURCES = ["host_partition.cpp", "host_minibatch.cpp", "host_ladies.cpp"]
 
 ARCH = "gfx950"

@@ -7,6 +7,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <climits>
 #include <cmath>
 #include <cstdio>
@@ -961,6 +962,255 @@ extern "C" gist_status gist_subagg_gather(gist_ctx* ctx, float* Wg, int64_t rows
   if (done) bytes += 4.0 * slice_elems(done);
   if (next) bytes += 4.0 * slice_elems(next);
   return gist::subagg_gather(ctx->stream, Wg, rows, cols, ldg, m, done, next, bytes);
+}
+
+// ---------------------------------------------------------------------------
+// Learned input rows, log probabilities, orthogonalised updates
+// ---------------------------------------------------------------------------
+
+namespace {
+gist_status bad(const char* what, gist_status s, const char* msg) {
+  return set_error(s, std::string(what) + msg);
+}
+
+bool known_store(int32_t s) {
+  return s == GIST_STORE_F32 || s == GIST_STORE_BF16 || s == GIST_STORE_F16;
+}
+
+gist_status check_embed(const char* what, int64_t n, int64_t V, int32_t d, const int32_t* ids,
+                        float scale, int64_t ld_rows, int64_t ld_table) {
+  if (n < 0 || V < 0 || d < 1) return bad(what, GIST_E_INVAL, ": bad sizes");
+  if (ld_rows < d || ld_table < d)
+    return bad(what, GIST_E_INVAL, ": leading dimension below d");
+  if (!std::isfinite(scale)) return bad(what, GIST_E_INVAL, ": non-finite scale");
+  if (n >= INT32_MAX || V >= INT32_MAX)
+    return bad(what, GIST_E_UNSUPPORTED, ": n or V exceeds int32");
+  if (d > (1 << 22)) return bad(what, GIST_E_UNSUPPORTED, ": d above 4194304");
+  if (n > 0 && !ids) return bad(what, GIST_E_INVAL, ": NULL ids");
+  return GIST_OK;
+}
+}  // namespace
+
+extern "C" gist_status gist_embed_lookup(gist_ctx* ctx, int64_t n, int64_t V, int32_t d,
+                                         const void* table, int64_t ldt, int32_t store,
+                                         const int32_t* ids, float scale, float* out,
+                                         int64_t ldo) {
+  gist::clear_error();
+  if (!ctx) return set_error(GIST_E_INVAL, "embed_lookup: NULL ctx");
+  gist::ProfBind pb(ctx);
+  GIST_TRY(check_embed("embed_lookup", n, V, d, ids, scale, ldo, ldt));
+  if (!known_store(store)) return set_error(GIST_E_INVAL, "embed_lookup: unknown store");
+  if (n == 0) return GIST_OK;
+  if (!out || (V > 0 && !table)) return set_error(GIST_E_INVAL, "embed_lookup: NULL pointer");
+  gist::DeviceGuard dg(ctx->device);
+  return gist::embed_lookup(ctx->stream, n, V, d, table, ldt, store, ids, scale, out, ldo);
+}
+
+extern "C" size_t gist_embed_grad_workspace(int64_t n, int64_t V, int32_t d) {
+  if (n < 0 || V < 0 || d < 1 || d > (1 << 22) || n >= INT32_MAX || V >= INT32_MAX) return 0;
+  return gist::embed_grad_workspace(n, V, d);
+}
+
+namespace {
+gist_status embed_grad_call(const char* what, gist_ctx* ctx, int64_t n, int64_t V, int32_t d,
+                            const int32_t* ids, float scale, const float* dY, int64_t ldy,
+                            bool sgd, float lr, float* out, int64_t ldo, void* ws,
+                            size_t ws_bytes) {
+  if (!ctx) return bad(what, GIST_E_INVAL, ": NULL ctx");
+  gist::ProfBind pb(ctx);
+  GIST_TRY(check_embed(what, n, V, d, ids, scale, ldy, ldo));
+  if (sgd && !std::isfinite(lr)) return bad(what, GIST_E_INVAL, ": non-finite lr");
+  if (V == 0 || (sgd && n == 0)) return GIST_OK;
+  if (!out || (n > 0 && !dY)) return bad(what, GIST_E_INVAL, ": NULL pointer");
+  const size_t need = gist::embed_grad_workspace(n, V, d);
+  if (ws_bytes < need || (need > 0 && !ws))
+    return bad(what, GIST_E_NOMEM, ": workspace too small");
+  if (reinterpret_cast<uintptr_t>(ws) & 15u)
+    return bad(what, GIST_E_INVAL, ": workspace not aligned to 16 bytes");
+  gist::DeviceGuard dg(ctx->device);
+  return gist::embed_grad(ctx->stream, n, V, d, ids, scale, dY, ldy, sgd, lr, out, ldo, ws);
+}
+}  // namespace
+
+extern "C" gist_status gist_embed_grad(gist_ctx* ctx, int64_t n, int64_t V, int32_t d,
+                                       const int32_t* ids, float scale, const float* dY,
+                                       int64_t ldy, float* dTable, int64_t ldg, void* ws,
+                                       size_t ws_bytes) {
+  gist::clear_error();
+  return embed_grad_call("embed_grad", ctx, n, V, d, ids, scale, dY, ldy, false, 0.f, dTable, ldg,
+                         ws, ws_bytes);
+}
+
+extern "C" gist_status gist_embed_grad_sgd(gist_ctx* ctx, int64_t n, int64_t V, int32_t d,
+                                           const int32_t* ids, float scale, const float* dY,
+                                           int64_t ldy, float lr, float* table, int64_t ldt,
+                                           void* ws, size_t ws_bytes) {
+  gist::clear_error();
+  return embed_grad_call("embed_grad_sgd", ctx, n, V, d, ids, scale, dY, ldy, true, lr, table,
+                         ldt, ws, ws_bytes);
+}
+
+namespace {
+gist_status check_logits(const char* what, int64_t n, int64_t C, const void* logits, int64_t ldz,
+                         int32_t store) {
+  if (n < 0 || C < 1 || ldz < C) return bad(what, GIST_E_INVAL, ": bad sizes");
+  if (!known_store(store)) return bad(what, GIST_E_INVAL, ": unknown store");
+  if (n >= INT32_MAX || C >= INT32_MAX)
+    return bad(what, GIST_E_UNSUPPORTED, ": n or C exceeds int32");
+  if (n > 0 && !logits) return bad(what, GIST_E_INVAL, ": NULL logits");
+  return GIST_OK;
+}
+}  // namespace
+
+extern "C" size_t gist_log_probs_workspace(int64_t n, int64_t C, int32_t K) {
+  if (n < 0 || C < 1 || n >= INT32_MAX || C >= INT32_MAX || K < 0 || K > C ||
+      K > GIST_LOG_PROBS_MAX_TOP)
+    return 0;
+  return gist::log_probs_workspace(n, C, K);
+}
+
+extern "C" gist_status gist_log_probs(gist_ctx* ctx, int64_t n, int64_t C, const void* logits,
+                                      int64_t ldz, int32_t store, const int32_t* tokens,
+                                      float* logp, float* entropy, float* lse, int32_t K,
+                                      float* top_logp, int32_t* top_idx, void* ws,
+                                      size_t ws_bytes) {
+  gist::clear_error();
+  if (!ctx) return set_error(GIST_E_INVAL, "log_probs: NULL ctx");
+  gist::ProfBind pb(ctx);
+  GIST_TRY(check_logits("log_probs", n, C, logits, ldz, store));
+  if (K < 0 || K > C || K > GIST_LOG_PROBS_MAX_TOP)
+    return set_error(GIST_E_INVAL, "log_probs: K outside [0, min(C, 64)]");
+  if (n == 0) return GIST_OK;
+  if (K > 0 && (!top_logp || !top_idx))
+    return set_error(GIST_E_INVAL, "log_probs: K > 0 needs top_logp and top_idx");
+  if (logp && !tokens) return set_error(GIST_E_INVAL, "log_probs: logp needs tokens");
+  const size_t need = gist::log_probs_workspace(n, C, K);
+  if (ws_bytes < need || (need > 0 && !ws))
+    return set_error(GIST_E_NOMEM, "log_probs: workspace too small");
+  if (need > 0 && (reinterpret_cast<uintptr_t>(ws) & 15u))
+    return set_error(GIST_E_INVAL, "log_probs: workspace not aligned to 16 bytes");
+  if (!logp && !entropy && !lse && K == 0) return GIST_OK;
+  gist::DeviceGuard dg(ctx->device);
+  return gist::log_probs(ctx->stream, n, C, logits, ldz, store, tokens, logp, entropy, lse, K,
+                         top_logp, top_idx, ws);
+}
+
+extern "C" gist_status gist_log_probs_bwd(gist_ctx* ctx, int64_t n, int64_t C, const void* logits,
+                                          int64_t ldz, int32_t store, const int32_t* tokens,
+                                          const float* lse, const float* entropy,
+                                          const float* g_logp, const float* g_entropy,
+                                          void* dlogits, int64_t ldd) {
+  gist::clear_error();
+  if (!ctx) return set_error(GIST_E_INVAL, "log_probs_bwd: NULL ctx");
+  gist::ProfBind pb(ctx);
+  GIST_TRY(check_logits("log_probs_bwd", n, C, logits, ldz, store));
+  if (ldd < C) return set_error(GIST_E_INVAL, "log_probs_bwd: bad sizes");
+  if (n == 0) return GIST_OK;
+  if (!lse || !dlogits) return set_error(GIST_E_INVAL, "log_probs_bwd: NULL pointer");
+  if (g_logp && !tokens) return set_error(GIST_E_INVAL, "log_probs_bwd: g_logp needs tokens");
+  if (g_entropy && !entropy)
+    return set_error(GIST_E_INVAL, "log_probs_bwd: g_entropy needs entropy");
+  if (dlogits == logits && ldd != ldz)
+    return set_error(GIST_E_INVAL, "log_probs_bwd: in place needs one leading dimension");
+  gist::DeviceGuard dg(ctx->device);
+  return gist::log_probs_bwd(ctx->stream, n, C, logits, ldz, store, tokens, lse, entropy, g_logp,
+                             g_entropy, dlogits, ldd);
+}
+
+namespace {
+gist_status check_muon(const char* what, const gist_muon_desc* D) {
+  if (!D) return bad(what, GIST_E_INVAL, ": NULL descriptor");
+  if (D->rows < 0 || D->cols < 0 || D->groups < 0)
+    return bad(what, GIST_E_INVAL, ": bad sizes");
+  if (D->rows > 65536 || D->cols > 65536 || D->groups > 65535)
+    return bad(what, GIST_E_UNSUPPORTED, ": rows or cols above 65536, or groups above 65535");
+  if (D->dtype != GIST_DTYPE_F32 && D->dtype != GIST_DTYPE_F16_IN)
+    return bad(what, GIST_E_INVAL, ": dtype is F32 or F16_IN");
+  if (D->flags & ~static_cast<uint32_t>(GIST_MUON_NESTEROV | GIST_MUON_FRESH))
+    return bad(what, GIST_E_INVAL, ": unknown flags");
+  if (D->steps < 1 || D->steps > 32) return bad(what, GIST_E_INVAL, ": steps outside 1..32");
+  if (!(D->eps >= FLT_MIN) || !std::isfinite(D->eps))
+    return bad(what, GIST_E_INVAL, ": eps must be positive");
+  const double a = D->coef[0], b = D->coef[1], c = D->coef[2];
+  if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c))
+    return bad(what, GIST_E_INVAL, ": non-finite coefficient");
+  // r bounds the singular values, and so the entries, of X: one step takes it
+  // to the largest |a s + b s^3 + c s^5| over [0, r], at r or at a stationary
+  // point (q = s^2); B has at most the largest |b q + c q^2| over [0, r^2].
+  double r = 1.0;
+  for (int k = 0; k < D->steps; ++k) {
+    double next = 0.0, poly = 0.0;
+    auto at = [&](double q) {
+      if (!(q >= 0.0 && q <= r * r)) return;
+      poly = std::max(poly, std::fabs(b * q + c * q * q));
+      next = std::max(next, std::sqrt(q) * std::fabs(a + b * q + c * q * q));
+    };
+    at(r * r);
+    if (c != 0.0) {
+      at(-b / (2.0 * c));
+      const double disc = 9.0 * b * b - 20.0 * a * c;
+      if (disc >= 0.0) {
+        at((-3.0 * b + std::sqrt(disc)) / (10.0 * c));
+        at((-3.0 * b - std::sqrt(disc)) / (10.0 * c));
+      }
+    } else if (b != 0.0) {
+      at(-a / (3.0 * b));
+    }
+    if (!(poly <= 8.0) || !(next <= 8.0) || !(r * r <= 8.0))
+      return bad(what, GIST_E_INVAL, ": the coefficients let a singular value grow past the range");
+    r = next;
+  }
+  return GIST_OK;
+}
+
+gist_status muon_ws(const char* what, const gist_muon_desc* D, void* ws, size_t ws_bytes) {
+  const size_t need = gist::muon_workspace(D);
+  if (ws_bytes < need || !ws)
+    return bad(what, GIST_E_NOMEM, ": workspace too small");
+  if (reinterpret_cast<uintptr_t>(ws) & 15u)
+    return bad(what, GIST_E_INVAL, ": workspace not aligned to 16 bytes");
+  return GIST_OK;
+}
+}  // namespace
+
+extern "C" gist_status gist_muon_workspace_size(const gist_muon_desc* D, size_t* bytes) {
+  gist::clear_error();
+  if (!bytes) return set_error(GIST_E_INVAL, "muon_workspace_size: NULL out");
+  GIST_TRY(check_muon("muon_workspace_size", D));
+  *bytes = D->rows == 0 || D->cols == 0 ? 0 : gist::muon_workspace(D);
+  return GIST_OK;
+}
+
+extern "C" gist_status gist_orthogonalize(gist_ctx* ctx, const gist_muon_desc* D, const float* G,
+                                          void* O, void* ws, size_t ws_bytes) {
+  gist::clear_error();
+  if (!ctx) return set_error(GIST_E_INVAL, "orthogonalize: NULL ctx");
+  gist::ProfBind pb(ctx);
+  GIST_TRY(check_muon("orthogonalize", D));
+  if (D->rows == 0 || D->cols == 0) return GIST_OK;
+  if (!G || !O) return set_error(GIST_E_INVAL, "orthogonalize: NULL pointer");
+  GIST_TRY(muon_ws("orthogonalize", D, ws, ws_bytes));
+  gist::DeviceGuard dg(ctx->device);
+  return gist::muon(ctx->stream, D, G, O, nullptr, nullptr, 0.f, 0.f, 0.f, 0.f, ws);
+}
+
+extern "C" gist_status gist_muon_update(gist_ctx* ctx, const gist_muon_desc* D, float* W,
+                                        const float* dW, float* M, float lr, float momentum,
+                                        float weight_decay, float scale, void* ws,
+                                        size_t ws_bytes) {
+  gist::clear_error();
+  if (!ctx) return set_error(GIST_E_INVAL, "muon_update: NULL ctx");
+  gist::ProfBind pb(ctx);
+  GIST_TRY(check_muon("muon_update", D));
+  if (!(momentum >= 0.f && momentum < 1.f))
+    return set_error(GIST_E_INVAL, "muon_update: momentum outside [0, 1)");
+  if (!std::isfinite(lr) || !std::isfinite(weight_decay) || !std::isfinite(scale))
+    return set_error(GIST_E_INVAL, "muon_update: non-finite lr, weight_decay or scale");
+  if (D->rows == 0 || D->cols == 0) return GIST_OK;
+  if (!W || !dW || !M) return set_error(GIST_E_INVAL, "muon_update: NULL pointer");
+  GIST_TRY(muon_ws("muon_update", D, ws, ws_bytes));
+  gist::DeviceGuard dg(ctx->device);
+  return gist::muon(ctx->stream, D, dW, nullptr, W, M, lr, momentum, weight_decay, scale, ws);
 }
 
 // ---------------------------------------------------------------------------

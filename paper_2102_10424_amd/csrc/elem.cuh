@@ -1,0 +1,128 @@
+// Vectors of stored elements (gist_store) as floats: loads that widen, stores
+// that round once to nearest even.
+#pragma once
+
+#include "common.cuh"
+#include "gist_internal.h"
+
+namespace gist {
+
+typedef float fx4 __attribute__((ext_vector_type(4)));
+typedef float fx2 __attribute__((ext_vector_type(2)));
+typedef unsigned short us8 __attribute__((ext_vector_type(8)));
+typedef unsigned short us4 __attribute__((ext_vector_type(4)));
+typedef unsigned short us2 __attribute__((ext_vector_type(2)));
+
+// ---- stored elements as floats ------------------------------------------------
+
+template <int STORE>
+__device__ __forceinline__ float widen(unsigned short u) {
+  if constexpr (STORE == GIST_STORE_BF16) return __uint_as_float(static_cast<unsigned>(u) << 16);
+  return static_cast<float>(__builtin_bit_cast(_Float16, u));
+}
+
+template <int STORE, int V>
+__device__ __forceinline__ void load_vec(const void* base, int64_t e, float (&x)[V]) {
+  if constexpr (STORE == GIST_STORE_F32) {
+    const float* p = static_cast<const float*>(base) + e;
+    if constexpr (V == 4) {
+      const fx4 t = *reinterpret_cast<const fx4*>(p);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) x[q] = t[q];
+    } else if constexpr (V == 2) {
+      const fx2 t = *reinterpret_cast<const fx2*>(p);
+      x[0] = t[0];
+      x[1] = t[1];
+    } else {
+      x[0] = *p;
+    }
+  } else {
+    const unsigned short* p = static_cast<const unsigned short*>(base) + e;
+    if constexpr (V == 8) {
+      const us8 t = *reinterpret_cast<const us8*>(p);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) x[q] = widen<STORE>(t[q]);
+    } else if constexpr (V == 4) {
+      const us4 t = *reinterpret_cast<const us4*>(p);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) x[q] = widen<STORE>(t[q]);
+    } else if constexpr (V == 2) {
+      const us2 t = *reinterpret_cast<const us2*>(p);
+      x[0] = widen<STORE>(t[0]);
+      x[1] = widen<STORE>(t[1]);
+    } else {
+      x[0] = widen<STORE>(*p);
+    }
+  }
+}
+
+template <int V>
+__device__ __forceinline__ void store_vec(float* p, const float (&x)[V]) {
+  if constexpr (V >= 4) {
+#pragma unroll
+    for (int h = 0; h < V; h += 4) {
+      fx4 t;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) t[q] = x[h + q];
+      *reinterpret_cast<fx4*>(p + h) = t;
+    }
+  } else if constexpr (V == 2) {
+    fx2 t;
+    t[0] = x[0];
+    t[1] = x[1];
+    *reinterpret_cast<fx2*>(p) = t;
+  } else {
+    *p = x[0];
+  }
+}
+
+template <int STORE>
+__device__ __forceinline__ unsigned short narrow(float x) {
+  if constexpr (STORE == GIST_STORE_BF16) return __builtin_bit_cast(unsigned short, static_cast<__bf16>(x));
+  return __builtin_bit_cast(unsigned short, static_cast<_Float16>(x));
+}
+
+template <int STORE, int V>
+__device__ __forceinline__ void store_as(void* base, int64_t e, const float (&x)[V]) {
+  if constexpr (STORE == GIST_STORE_F32) {
+    store_vec<V>(static_cast<float*>(base) + e, x);
+  } else {
+    unsigned short* p = static_cast<unsigned short*>(base) + e;
+    if constexpr (V == 8) {
+      us8 t;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) t[q] = narrow<STORE>(x[q]);
+      *reinterpret_cast<us8*>(p) = t;
+    } else if constexpr (V == 4) {
+      us4 t;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) t[q] = narrow<STORE>(x[q]);
+      *reinterpret_cast<us4*>(p) = t;
+    } else if constexpr (V == 2) {
+      us2 t;
+      t[0] = narrow<STORE>(x[0]);
+      t[1] = narrow<STORE>(x[1]);
+      *reinterpret_cast<us2*>(p) = t;
+    } else {
+      *p = narrow<STORE>(x[0]);
+    }
+  }
+}
+
+inline int ceil_log2(int64_t x) {
+  int l = 0;
+  while ((int64_t{1} << l) < x) ++l;
+  return l;
+}
+
+// Elements per access: as many as divide the width and the leading dimension
+// and leave every row's address aligned to the access.
+inline int vec_of(int most, int64_t width, int64_t ld, const void* p, int elem_bytes) {
+  int v = most;
+  while (v > 1 && (width % v != 0 || ld % v != 0 ||
+                   reinterpret_cast<uintptr_t>(p) % static_cast<uintptr_t>(v * elem_bytes > 16 ? 16 : v * elem_bytes) != 0))
+    v /= 2;
+  return v;
+}
+
+}  // namespace gist

@@ -1,0 +1,414 @@
+// Learned input rows: out[i] = scale table[ids[i]], and the table's gradient.
+//
+// The gradient adds the rows of dY whose ids are equal.  Adding them with
+// floating-point atomics would make the sum's order, and its result, change
+// from run to run, and would serialise a frequent id on one row; so the ids
+// are sorted (stably, by a radix sort of (id, position)) and equal ids, now
+// neighbours, are summed in position order: chunks of sorted positions in
+// parallel, partial sums of ids that cross a chunk's border joined by a
+// second kernel in chunk order.
+
+#include <algorithm>
+
+#include "elem.cuh"
+
+namespace gist {
+
+namespace {
+
+constexpr int kBlock = 256;
+
+// ---- lookup --------------------------------------------------------------------
+
+// One group of TPR threads per row (TPR a power of two up to the block), V
+// elements a thread and step.
+template <int STORE, int V>
+__global__ __launch_bounds__(kBlock) void lookup_kernel(int n, int64_t V_rows, int d, int tpr_log2,
+                                                        const void* __restrict__ table,
+                                                        int64_t ldt, const int* __restrict__ ids,
+                                                        float scale, float* __restrict__ out,
+                                                        int64_t ldo) {
+  const int lane = threadIdx.x & ((1 << tpr_log2) - 1);
+  const int step = V << tpr_log2;
+  for (int64_t row = (static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x) >> tpr_log2; row < n;
+       row += (static_cast<int64_t>(gridDim.x) * kBlock) >> tpr_log2) {
+    const int64_t id = ids[row];
+    float* o = out + row * ldo;
+    const bool in = id >= 0 && id < V_rows;
+    const int64_t base = id * ldt;
+    for (int j = V * lane; j < d; j += step) {
+      float x[V] = {};
+      if (in) load_vec<STORE, V>(table, base + j, x);
+#pragma unroll
+      for (int q = 0; q < V; ++q) x[q] *= scale;
+      store_vec<V>(o + j, x);
+    }
+  }
+}
+
+// ---- sort -----------------------------------------------------------------------
+
+constexpr int kDigit = 8, kBins = 1 << kDigit;
+constexpr int kItems = 16;                  // keys per thread and tile
+constexpr int kTile = kBlock * kItems;      // 4,096
+
+__device__ __forceinline__ int key_of(int id, int V) {   // padding sorts last
+  return id >= 0 && id < V ? id : V;
+}
+
+// Digit counts of every tile, digit-major: hist[digit * tiles + tile].
+template <bool FIRST>
+__global__ __launch_bounds__(kBlock) void hist_kernel(int n, int V, const int* __restrict__ keys,
+                                                      int shift, int tiles,
+                                                      int* __restrict__ hist) {
+  __shared__ int cnt[kBins];
+  cnt[threadIdx.x] = 0;
+  __syncthreads();
+  const int64_t base = static_cast<int64_t>(blockIdx.x) * kTile;
+#pragma unroll
+  for (int i = 0; i < kItems; ++i) {
+    const int64_t e = base + i * kBlock + threadIdx.x;
+    if (e < n) {
+      const int k = FIRST ? key_of(keys[e], V) : keys[e];
+      atomicAdd(&cnt[(k >> shift) & (kBins - 1)], 1);
+    }
+  }
+  __syncthreads();
+  hist[static_cast<int64_t>(threadIdx.x) * tiles + blockIdx.x] = cnt[threadIdx.x];
+}
+
+// In-place exclusive scan of `count` ints by one workgroup.
+__global__ __launch_bounds__(1024) void scan_kernel(int64_t count, int* __restrict__ v) {
+  __shared__ int wsum[16];
+  __shared__ int carry_s;
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  if (t == 0) carry_s = 0;
+  __syncthreads();
+  for (int64_t base = 0; base < count; base += 4096) {
+    const int64_t e = base + 4 * t;
+    int x[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) x[q] = e + q < count ? v[e + q] : 0;
+    const int mine = x[0] + x[1] + x[2] + x[3];
+    int inc = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int u = __shfl_up(inc, o, 64);
+      if (lane >= o) inc += u;
+    }
+    if (lane == 63) wsum[wave] = inc;
+    __syncthreads();
+    int before = carry_s;
+    for (int w = 0; w < wave; ++w) before += wsum[w];
+    int run = before + inc - mine;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if (e + q < count) v[e + q] = run;
+      run += x[q];
+    }
+    __syncthreads();   // everyone has read carry_s and wsum
+    if (t == 1023) carry_s = before + inc;
+    __syncthreads();
+  }
+}
+
+// Stable scatter of every tile's (key, position) pairs by one digit.  A wave
+// holds kItems * 64 consecutive keys, 64 at a time; equal digits among a
+// wave's 64 keys are found by matching the digit's bits with ballots.
+template <bool FIRST>
+__global__ __launch_bounds__(kBlock) void scatter_digit_kernel(
+    int n, int V, const int* __restrict__ kin, const int* __restrict__ pin, int shift, int tiles,
+    const int* __restrict__ offs, int* __restrict__ kout, int* __restrict__ pout) {
+  constexpr int kWaves = kBlock / 64;
+  __shared__ int cnt[kWaves][kBins];
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) cnt[w][t] = 0;
+  __syncthreads();
+  const int64_t base = static_cast<int64_t>(blockIdx.x) * kTile + wave * (kItems * 64);
+  int key[kItems], rank[kItems];
+#pragma unroll
+  for (int i = 0; i < kItems; ++i) {
+    const int64_t e = base + i * 64 + lane;
+    const bool in = e < n;
+    key[i] = in ? (FIRST ? key_of(kin[e], V) : kin[e]) : 0;
+    const int dg = (key[i] >> shift) & (kBins - 1);
+    unsigned long long m = __ballot(in);
+#pragma unroll
+    for (int b = 0; b < kDigit; ++b) {
+      const unsigned long long s = __ballot((dg >> b) & 1);
+      m &= (dg >> b) & 1 ? s : ~s;
+    }
+    const int before = __popcll(m & ((1ull << lane) - 1));
+    const int had = cnt[wave][dg];   // the wave's keys of this digit so far
+    rank[i] = had + before;
+    __builtin_amdgcn_wave_barrier();
+    if (in && before == 0) cnt[wave][dg] = had + __popcll(m);
+    __builtin_amdgcn_wave_barrier();
+  }
+  __syncthreads();
+  {   // thread t turns digit t's counts into the waves' first places
+    int run = offs[static_cast<int64_t>(t) * tiles + blockIdx.x];
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const int c = cnt[w][t];
+      cnt[w][t] = run;
+      run += c;
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kItems; ++i) {
+    const int64_t e = base + i * 64 + lane;
+    if (e < n) {
+      const int to = cnt[wave][(key[i] >> shift) & (kBins - 1)] + rank[i];
+      kout[to] = key[i];
+      pout[to] = FIRST ? static_cast<int>(e) : pin[e];
+    }
+  }
+}
+
+// ---- sums over equal ids -----------------------------------------------------------
+
+// A row's finished sum: the dense gradient, or the SGD step on the table.
+template <bool SGD, int V>
+__device__ __forceinline__ void finish(float* p, const float (&acc)[V], float scale, float lr) {
+  float x[V];
+  if constexpr (SGD) {
+    load_vec<GIST_STORE_F32, V>(p, 0, x);
+#pragma unroll
+    for (int q = 0; q < V; ++q) x[q] = fmaf(-lr, scale * acc[q], x[q]);
+  } else {
+#pragma unroll
+    for (int q = 0; q < V; ++q) x[q] = scale * acc[q];
+  }
+  store_vec<V>(p, x);
+}
+
+// Chunks of `len` sorted positions, one group of threads each; blockIdx.y:
+// slab of columns.  part[2 c] is the sum of chunk c's first id where that id
+// began in an earlier chunk, part[2 c + 1] that of its last id where it
+// began in this chunk and goes on in the next.
+template <bool SGD, int V>
+__global__ __launch_bounds__(kBlock) void sum_kernel(int n, int Vn, int d, int tpr_log2, int len,
+                                                     const int* __restrict__ keys,
+                                                     const int* __restrict__ pos, float scale,
+                                                     const float* __restrict__ dY, int64_t ldy,
+                                                     float lr, float* __restrict__ out,
+                                                     int64_t ldo, float* __restrict__ part,
+                                                     int64_t ldp) {
+  const int lane = threadIdx.x & ((1 << tpr_log2) - 1);
+  const int64_t c = (static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x) >> tpr_log2;
+  const int64_t b64 = c * len;
+  if (b64 >= n) return;
+  const int b = static_cast<int>(b64), e = static_cast<int>(min<int64_t>(n, b64 + len));
+  const int j = V * (lane + (static_cast<int>(blockIdx.y) << tpr_log2));
+  if (j >= d) return;
+  int cur = keys[b];
+  if (cur == Vn) return;   // padding only
+  bool head = b > 0 && keys[b - 1] == cur;
+  float acc[V] = {};
+  for (int i = b; i < e; ++i) {
+    const int k = keys[i];
+    if (k != cur) {
+      if (head) store_vec<V>(part + 2 * c * ldp + j, acc);
+      else finish<SGD, V>(out + cur * ldo + j, acc, scale, lr);
+      head = false;
+      cur = k;
+#pragma unroll
+      for (int q = 0; q < V; ++q) acc[q] = 0.f;
+      if (k == Vn) return;
+    }
+    float x[V];
+    load_vec<GIST_STORE_F32, V>(dY, pos[i] * ldy + j, x);
+#pragma unroll
+    for (int q = 0; q < V; ++q) acc[q] += x[q];
+  }
+  if (head) store_vec<V>(part + 2 * c * ldp + j, acc);
+  else if (e < n && keys[e] == cur) store_vec<V>(part + (2 * c + 1) * ldp + j, acc);
+  else finish<SGD, V>(out + cur * ldo + j, acc, scale, lr);
+}
+
+// Ids that cross chunk borders: the group of the chunk where such an id begins
+// adds its parts in chunk order.
+template <bool SGD, int V>
+__global__ __launch_bounds__(kBlock) void join_kernel(int n, int Vn, int d, int tpr_log2, int len,
+                                                      const int* __restrict__ keys, float scale,
+                                                      float lr, float* __restrict__ out,
+                                                      int64_t ldo, const float* __restrict__ part,
+                                                      int64_t ldp) {
+  const int lane = threadIdx.x & ((1 << tpr_log2) - 1);
+  int64_t c = (static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x) >> tpr_log2;
+  int64_t b = c * len, e = b + len;
+  if (e >= n) return;   // the last chunk: nothing goes on
+  const int j = V * (lane + (static_cast<int>(blockIdx.y) << tpr_log2));
+  if (j >= d) return;
+  const int cur = keys[e - 1];
+  if (cur == Vn || keys[e] != cur) return;
+  if (keys[b] == cur && b > 0 && keys[b - 1] == cur) return;   // began earlier
+  float acc[V];
+  load_vec<GIST_STORE_F32, V>(part, (2 * c + 1) * ldp + j, acc);
+  for (;;) {
+    ++c;
+    b = e;
+    e = min<int64_t>(n, e + len);
+    float x[V];
+    load_vec<GIST_STORE_F32, V>(part, 2 * c * ldp + j, x);
+#pragma unroll
+    for (int q = 0; q < V; ++q) acc[q] += x[q];
+    if (e >= n || keys[e - 1] != cur || keys[e] != cur) break;
+  }
+  finish<SGD, V>(out + cur * ldo + j, acc, scale, lr);
+}
+
+// Zero rows that no id names (dense gradient): a wave per 64 rows, each lane
+// looking its row up in the sorted ids.
+__global__ __launch_bounds__(kBlock) void zero_rows_kernel(int n, int Vn, int d,
+                                                           const int* __restrict__ keys,
+                                                           float* __restrict__ out, int64_t ldo) {
+  const int lane = threadIdx.x & 63;
+  const int64_t r0 = ((static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x) >> 6) * 64;
+  if (r0 >= Vn) return;
+  const int64_t r = r0 + lane;
+  int lo = 0, hi = n;
+  while (lo < hi) {
+    const int mid = lo + ((hi - lo) >> 1);
+    if (keys[mid] < r) lo = mid + 1;
+    else hi = mid;
+  }
+  const bool missing = r < Vn && (lo >= n || keys[lo] != r);
+  unsigned long long m = __ballot(missing);
+  while (m) {
+    const int q = __ffsll(m) - 1;
+    m &= m - 1;
+    float* p = out + (r0 + q) * ldo;
+    for (int j = lane; j < d; j += 64) p[j] = 0.f;
+  }
+}
+
+size_t up256(size_t x) { return (x + 255) & ~size_t(255); }
+
+struct GradPlan {
+  int64_t tiles, chunks, ldp;
+  int len, passes;
+  size_t keys, hist, part;
+  size_t total() const { return 4 * keys + hist + part; }
+};
+
+GradPlan plan(int64_t n, int64_t V, int d) {
+  GradPlan p;
+  p.tiles = (n + kTile - 1) / kTile;
+  p.passes = (ceil_log2(V + 1) + kDigit - 1) / kDigit;
+  p.len = 32;
+  p.chunks = (n + p.len - 1) / p.len;
+  p.ldp = (d + 3) / 4 * 4;
+  p.keys = up256(static_cast<size_t>(n) * 4);
+  p.hist = up256(static_cast<size_t>(p.tiles) * kBins * 4);
+  p.part = up256(static_cast<size_t>(p.chunks) * 2 * p.ldp * 4);
+  return p;
+}
+
+}  // namespace
+
+gist_status embed_lookup(hipStream_t st, int64_t n, int64_t V, int d, const void* table,
+                         int64_t ldt, int store, const int32_t* ids, float scale, float* out,
+                         int64_t ldo) {
+  const int eb = store == GIST_STORE_F32 ? 4 : 2;
+  const int most = store == GIST_STORE_F32 ? 4 : 8;
+  // eight values go out as two 16-byte stores, so the rows of out need no more
+  const int vt = vec_of(most, d, ldt, table, eb), vo = vec_of(4, d, ldo, out, 4);
+  const int v = vo == 4 ? vt : std::min(vt, vo);
+  const int tl = std::min(8, ceil_log2((d + v - 1) / v));
+  const int64_t blocks = std::min<int64_t>(((n << tl) + kBlock - 1) / kBlock, 1 << 22);
+  ProfScope ps(st, "embed_lookup", static_cast<double>(n) * d,
+               4.0 * n + static_cast<double>(n) * d * (eb + 4));
+#define LOOKUP(S, W)                                                                         \
+  lookup_kernel<S, W><<<dim3(static_cast<unsigned>(blocks)), kBlock, 0, st>>>(               \
+      static_cast<int>(n), V, d, tl, table, ldt, ids, scale, out, ldo)
+  if (store == GIST_STORE_F32) {
+    if (v == 4) LOOKUP(GIST_STORE_F32, 4);
+    else if (v == 2) LOOKUP(GIST_STORE_F32, 2);
+    else LOOKUP(GIST_STORE_F32, 1);
+  } else if (store == GIST_STORE_BF16) {
+    if (v == 8) LOOKUP(GIST_STORE_BF16, 8);
+    else if (v == 4) LOOKUP(GIST_STORE_BF16, 4);
+    else if (v == 2) LOOKUP(GIST_STORE_BF16, 2);
+    else LOOKUP(GIST_STORE_BF16, 1);
+  } else {
+    if (v == 8) LOOKUP(GIST_STORE_F16, 8);
+    else if (v == 4) LOOKUP(GIST_STORE_F16, 4);
+    else if (v == 2) LOOKUP(GIST_STORE_F16, 2);
+    else LOOKUP(GIST_STORE_F16, 1);
+  }
+#undef LOOKUP
+  return check_launch("embed_lookup");
+}
+
+size_t embed_grad_workspace(int64_t n, int64_t V, int d) { return plan(n, V, d).total(); }
+
+gist_status embed_grad(hipStream_t st, int64_t n, int64_t V, int d, const int32_t* ids,
+                       float scale, const float* dY, int64_t ldy, bool sgd, float lr, float* out,
+                       int64_t ldo, void* ws) {
+  const GradPlan p = plan(n, V, d);
+  char* c = static_cast<char*>(ws);
+  int* k[2] = {reinterpret_cast<int*>(c), reinterpret_cast<int*>(c + p.keys)};
+  int* q[2] = {reinterpret_cast<int*>(c + 2 * p.keys), reinterpret_cast<int*>(c + 3 * p.keys)};
+  int* hist = reinterpret_cast<int*>(c + 4 * p.keys);
+  float* part = reinterpret_cast<float*>(c + 4 * p.keys + p.hist);
+  const int ni = static_cast<int>(n), vi = static_cast<int>(V), tiles = static_cast<int>(p.tiles);
+  int cur = 0;
+  if (n > 0) {
+    ProfScope ps(st, "embed_sort", 0.0, 8.0 * n * p.passes);
+    for (int i = 0; i < p.passes; ++i) {
+      const int* kin = i == 0 ? ids : k[cur ^ 1];
+      const int shift = i * kDigit;
+      const dim3 g(static_cast<unsigned>(tiles));
+      if (i == 0) hist_kernel<true><<<g, kBlock, 0, st>>>(ni, vi, kin, shift, tiles, hist);
+      else hist_kernel<false><<<g, kBlock, 0, st>>>(ni, vi, kin, shift, tiles, hist);
+      scan_kernel<<<1, 1024, 0, st>>>(p.tiles * kBins, hist);
+      if (i == 0)
+        scatter_digit_kernel<true><<<g, kBlock, 0, st>>>(ni, vi, kin, nullptr, shift, tiles, hist,
+                                                         k[cur], q[cur]);
+      else
+        scatter_digit_kernel<false><<<g, kBlock, 0, st>>>(ni, vi, kin, q[cur ^ 1], shift, tiles,
+                                                          hist, k[cur], q[cur]);
+      cur ^= 1;
+    }
+    cur ^= 1;
+  }
+  if (!sgd) {
+    ProfScope ps(st, "embed_zero_rows", 0.0, 4.0 * V * d);
+    const int64_t blocks = (V + kBlock - 1) / kBlock;
+    zero_rows_kernel<<<dim3(static_cast<unsigned>(blocks)), kBlock, 0, st>>>(ni, vi, d, k[cur],
+                                                                            out, ldo);
+  }
+  if (n > 0) {
+    const int v = std::min(vec_of(4, d, ldy, dY, 4), vec_of(4, d, ldo, out, 4));
+    const int tl = std::min(8, ceil_log2((d + v - 1) / v));
+    if ((p.chunks << tl) >= (int64_t{1} << 32) - kBlock)
+      return set_error(GIST_E_UNSUPPORTED, "embed_grad: n * d exceeds the grid");
+    const dim3 g(static_cast<unsigned>(((p.chunks << tl) + kBlock - 1) / kBlock),
+                 static_cast<unsigned>((d + (v << tl) - 1) / (v << tl)));
+    ProfScope ps(st, "embed_sum", static_cast<double>(n) * d, 8.0 * n * d);
+#define SUMS(S, W)                                                                             \
+  do {                                                                                         \
+    sum_kernel<S, W><<<g, kBlock, 0, st>>>(ni, vi, d, tl, p.len, k[cur], q[cur], scale, dY, ldy, \
+                                           lr, out, ldo, part, p.ldp);                         \
+    join_kernel<S, W><<<g, kBlock, 0, st>>>(ni, vi, d, tl, p.len, k[cur], scale, lr, out, ldo, \
+                                            part, p.ldp);                                      \
+  } while (0)
+    if (sgd) {
+      if (v == 4) SUMS(true, 4);
+      else if (v == 2) SUMS(true, 2);
+      else SUMS(true, 1);
+    } else {
+      if (v == 4) SUMS(false, 4);
+      else if (v == 2) SUMS(false, 2);
+      else SUMS(false, 1);
+    }
+#undef SUMS
+  }
+  return check_launch("embed_grad");
+}
+
+}  // namespace gist

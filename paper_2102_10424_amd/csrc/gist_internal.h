@@ -208,4 +208,31 @@ gist_status softmax_xent(hipStream_t st, int64_t n, int C, const float* logits,
                          const int32_t* labels, float* loss, float* dlogits,
                          float* partials, const int32_t* n_dev = nullptr);
 
+
+// ---- learned rows (embed.hip) ----
+gist_status embed_lookup(hipStream_t st, int64_t n, int64_t V, int d, const void* table,
+                         int64_t ldt, int store, const int32_t* ids, float scale, float* out,
+                         int64_t ldo);
+size_t embed_grad_workspace(int64_t n, int64_t V, int d);
+// dense (sgd false): out = dTable, every row written; else out = table, lr applied.
+gist_status embed_grad(hipStream_t st, int64_t n, int64_t V, int d, const int32_t* ids,
+                       float scale, const float* dY, int64_t ldy, bool sgd, float lr, float* out,
+                       int64_t ldo, void* ws);
+
+// ---- log probabilities (logprob.hip) ----
+size_t log_probs_workspace(int64_t n, int64_t C, int K);
+gist_status log_probs(hipStream_t st, int64_t n, int64_t C, const void* Z, int64_t ldz, int store,
+                      const int32_t* tokens, float* logp, float* entropy, float* lse, int K,
+                      float* top_logp, int32_t* top_idx, void* ws);
+gist_status log_probs_bwd(hipStream_t st, int64_t n, int64_t C, const void* Z, int64_t ldz,
+                          int store, const int32_t* tokens, const float* lse,
+                          const float* entropy, const float* g_logp, const float* g_entropy,
+                          void* dZ, int64_t ldd);
+
+// ---- orthogonalised updates (muon.hip) ----
+size_t muon_workspace(const gist_muon_desc* D);
+// W == nullptr: O receives the factor of G; else one update of W and M.
+gist_status muon(hipStream_t st, const gist_muon_desc* D, const float* G, void* O, float* W,
+                 float* M, float lr, float momentum, float decay, float scale, void* ws);
+
 }  // namespace gist

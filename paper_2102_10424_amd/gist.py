@@ -43,7 +43,10 @@ GIST_PART_CATEGORICAL = 1
 GIST_NORM_GCN_SYM, GIST_NORM_SAGE_MEAN, GIST_NORM_THEORY = 0, 1, 2
 GIST_LAYER_GCN, GIST_LAYER_SAGE_MEAN = 0, 1
 GIST_ACT_NONE, GIST_ACT_RELU = 0, 1
-GIST_DTYPE_F32, GIST_DTYPE_BF16_IN = 0, 1
+GIST_DTYPE_F32, GIST_DTYPE_BF16_IN, GIST_DTYPE_F16_IN = 0, 1, 2
+GIST_STORE_F32, GIST_STORE_BF16, GIST_STORE_F16 = 0, 1, 2
+GIST_LOG_PROBS_MAX_TOP = 64
+GIST_MUON_NESTEROV, GIST_MUON_FRESH = 1, 2
 GIST_ORDER_AUTO, GIST_ORDER_AGG_FIRST, GIST_ORDER_XFORM_FIRST = 0, 1, 2
 GIST_SUBAGG_CHECK_FINITE = 1
 GIST_ADAM_FRESH = 1
@@ -63,6 +66,9 @@ EXPORTED = (
     "gist_gat_workspace_size", "gist_gat_layer_fwd", "gist_gat_layer_bwd", "gist_gat_scores",
     "gist_softmax_xent_workspace", "gist_softmax_xent", "gist_softmax_xent_padded",
     "gist_softmax_xent_noalloc",
+    "gist_embed_lookup", "gist_embed_grad_workspace", "gist_embed_grad", "gist_embed_grad_sgd",
+    "gist_log_probs_workspace", "gist_log_probs", "gist_log_probs_bwd",
+    "gist_muon_workspace_size", "gist_orthogonalize", "gist_muon_update",
     "gist_gather_slice",
     "gist_sgd_update", "gist_adam_update", "gist_adam_coefficients", "gist_adam_update_dev",
     "gist_subagg", "gist_partition_inverse",
@@ -117,6 +123,12 @@ class gist_gat_desc(C.Structure):
     _fields_ = [("n", C.c_int64), ("nnz", C.c_int64), ("s_in", C.c_int32), ("s_out", C.c_int32),
                 ("act", C.c_int32), ("dtype", C.c_int32), ("slope", C.c_float),
                 ("flags", C.c_uint32)]
+
+
+class gist_muon_desc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int64), ("groups", C.c_int32),
+                ("dtype", C.c_int32), ("steps", C.c_int32), ("flags", C.c_uint32),
+                ("coef", C.c_float * 3), ("eps", C.c_float)]
 
 
 class gist_slice_set(C.Structure):
@@ -178,6 +190,22 @@ _sigs = {
     "gist_softmax_xent_padded": (C.c_int, [_P, C.c_int64, C.c_int32, _P, _P, _P, _P, _P, _P,
                                            C.c_size_t]),
     "gist_softmax_xent_noalloc": (C.c_int, [_P, C.c_int64, C.c_int32, _P, _P, _P, _P]),
+    "gist_embed_lookup": (C.c_int, [_P, C.c_int64, C.c_int64, C.c_int32, _P, C.c_int64, C.c_int32,
+                                    _P, C.c_float, _P, C.c_int64]),
+    "gist_embed_grad_workspace": (C.c_size_t, [C.c_int64, C.c_int64, C.c_int32]),
+    "gist_embed_grad": (C.c_int, [_P, C.c_int64, C.c_int64, C.c_int32, _P, C.c_float, _P,
+                                  C.c_int64, _P, C.c_int64, _P, C.c_size_t]),
+    "gist_embed_grad_sgd": (C.c_int, [_P, C.c_int64, C.c_int64, C.c_int32, _P, C.c_float, _P,
+                                      C.c_int64, C.c_float, _P, C.c_int64, _P, C.c_size_t]),
+    "gist_log_probs_workspace": (C.c_size_t, [C.c_int64, C.c_int64, C.c_int32]),
+    "gist_log_probs": (C.c_int, [_P, C.c_int64, C.c_int64, _P, C.c_int64, C.c_int32, _P, _P, _P,
+                                 _P, C.c_int32, _P, _P, _P, C.c_size_t]),
+    "gist_log_probs_bwd": (C.c_int, [_P, C.c_int64, C.c_int64, _P, C.c_int64, C.c_int32, _P, _P,
+                                     _P, _P, _P, _P, C.c_int64]),
+    "gist_muon_workspace_size": (C.c_int, [C.POINTER(gist_muon_desc), C.POINTER(C.c_size_t)]),
+    "gist_orthogonalize": (C.c_int, [_P, C.POINTER(gist_muon_desc), _P, _P, _P, C.c_size_t]),
+    "gist_muon_update": (C.c_int, [_P, C.POINTER(gist_muon_desc), _P, _P, _P, C.c_float,
+                                   C.c_float, C.c_float, C.c_float, _P, C.c_size_t]),
     "gist_gather_slice": (C.c_int, [_P, _P, C.c_int64, _P, C.c_int32, _P, C.c_int32, _P,
                                     C.c_int64]),
     "gist_sgd_update": (C.c_int, [_P, _P, _P, C.c_int64, C.c_float]),
@@ -462,6 +490,77 @@ def gist_softmax_xent_padded(ctx, n, C_, logits, labels, n_valid_dev, loss_dev, 
 def gist_softmax_xent_noalloc(ctx, n, C_, logits, labels, loss_dev, dlogits):
     _check(_lib.gist_softmax_xent_noalloc(ctx.handle, int(n), int(C_), _ptr(logits), _ptr(labels),
                                           _ptr(loss_dev), _ptr(dlogits)))
+
+
+def gist_embed_lookup(ctx, n, V, d, table, ldt, store, ids, scale, out, ldo):
+    """out[i] = scale * table[ids[i]]; an id outside [0, V) gives a zero row."""
+    _check(_lib.gist_embed_lookup(ctx.handle, int(n), int(V), int(d), _ptr(table), int(ldt),
+                                  int(store), _ptr(ids), float(scale), _ptr(out), int(ldo)))
+
+
+def gist_embed_grad_workspace(n, V, d):
+    return int(_lib.gist_embed_grad_workspace(int(n), int(V), int(d)))
+
+
+def gist_embed_grad(ctx, n, V, d, ids, scale, dY, ldy, dTable, ldg, ws):
+    """Dense gradient of ``gist_embed_lookup``'s table (overwritten)."""
+    _check(_lib.gist_embed_grad(ctx.handle, int(n), int(V), int(d), _ptr(ids), float(scale),
+                                _ptr(dY), int(ldy), _ptr(dTable), int(ldg), _ptr(ws),
+                                _nbytes(ws)))
+
+
+def gist_embed_grad_sgd(ctx, n, V, d, ids, scale, dY, ldy, lr, table, ldt, ws):
+    """The SGD step on the rows that ``ids`` name, in place."""
+    _check(_lib.gist_embed_grad_sgd(ctx.handle, int(n), int(V), int(d), _ptr(ids), float(scale),
+                                    _ptr(dY), int(ldy), float(lr), _ptr(table), int(ldt),
+                                    _ptr(ws), _nbytes(ws)))
+
+
+def gist_log_probs_workspace(n, C_, K):
+    return int(_lib.gist_log_probs_workspace(int(n), int(C_), int(K)))
+
+
+def gist_log_probs(ctx, n, C_, logits, ldz, store, tokens, logp, entropy, lse, K, top_logp,
+                   top_idx, ws):
+    """Log probabilities of the given classes, entropy, log-sum-exp and the K best classes of
+    each row (outputs may be None)."""
+    _check(_lib.gist_log_probs(ctx.handle, int(n), int(C_), _ptr(logits), int(ldz), int(store),
+                               _ptr(tokens), _ptr(logp), _ptr(entropy), _ptr(lse), int(K),
+                               _ptr(top_logp), _ptr(top_idx), _ptr(ws), _nbytes(ws)))
+
+
+def gist_log_probs_bwd(ctx, n, C_, logits, ldz, store, tokens, lse, entropy, g_logp, g_entropy,
+                       dlogits, ldd):
+    """Gradient of sum(g_logp * logp + g_entropy * entropy) with respect to the logits."""
+    _check(_lib.gist_log_probs_bwd(ctx.handle, int(n), int(C_), _ptr(logits), int(ldz),
+                                   int(store), _ptr(tokens), _ptr(lse), _ptr(entropy),
+                                   _ptr(g_logp), _ptr(g_entropy), _ptr(dlogits), int(ldd)))
+
+
+def muon_desc(rows, cols, groups=1, dtype=GIST_DTYPE_F32, steps=5, flags=0,
+              coef=(3.4445, -4.7750, 2.0315), eps=1e-7):
+    """``flags``: GIST_MUON_NESTEROV, GIST_MUON_FRESH."""
+    return gist_muon_desc(int(rows), int(cols), int(groups), int(dtype), int(steps), int(flags),
+                          (C.c_float * 3)(*coef), float(eps))
+
+
+def gist_muon_workspace_size(desc):
+    b = C.c_size_t()
+    _check(_lib.gist_muon_workspace_size(C.byref(desc), C.byref(b)))
+    return int(b.value)
+
+
+def gist_orthogonalize(ctx, desc, G_, O, ws):
+    """O = the matrices of ``G_`` orthogonalised (fp16 with GIST_DTYPE_F16_IN)."""
+    _check(_lib.gist_orthogonalize(ctx.handle, C.byref(desc), _ptr(G_), _ptr(O), _ptr(ws),
+                                   _nbytes(ws)))
+
+
+def gist_muon_update(ctx, desc, W, dW, M, lr, momentum, weight_decay, scale, ws):
+    """One Muon step on W with its momentum M, in place."""
+    _check(_lib.gist_muon_update(ctx.handle, C.byref(desc), _ptr(W), _ptr(dW), _ptr(M),
+                                 float(lr), float(momentum), float(weight_decay), float(scale),
+                                 _ptr(ws), _nbytes(ws)))
 
 
 def gist_gather_slice(ctx, Wg, ldg, rows, nr, cols, nc, Ws, lds):

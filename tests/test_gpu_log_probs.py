@@ -1,0 +1,287 @@
+"""GPU parity of the log probabilities, entropy, best classes and their
+gradient against 64 bits, at one class and many, one row and many, masked
+rows and classes, missing and wrong tokens, non-finite logits, ties, strides
+and offsets, within bounds derived in ops_ref."""
+
+import numpy as np
+import pytest
+
+import ops_ref as R
+from gpu_util import log, to_dev, to_host
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def G():
+    from paper_2102_10424_amd import gist
+    return gist
+
+
+@pytest.fixture(scope="module")
+def ctx(G):
+    return G.Context(0)
+
+
+def logits(n, C, store, rng, kind="plain"):
+    """Values as stored (float32 array of them) and the padded device tensor's source."""
+    import torch
+    z = (rng.standard_normal((n, C)) * 3).astype(np.float32)
+    if kind == "masked":
+        z[rng.random((n, C)) < 0.4] = -np.inf
+        z[::3] = -np.inf
+        if n > 4:
+            z[4, C // 2] = 1.5            # one class left
+    elif kind == "lowest":
+        low = dict(f32=np.finfo(np.float32).min, bf16=-3.3895e38, f16=-65504.0)[store]
+        z[rng.random((n, C)) < 0.5] = low
+        z[::4] = low
+    elif kind == "offset":
+        z += np.float32(400.0) * np.where(np.arange(n) % 2, 1, -1)[:, None].astype(np.float32)
+    elif kind == "ties":
+        z = np.round(z)
+        z[z == 0] = np.where(rng.random((n, C)) < 0.5, -0.0, 0.0).astype(np.float32)[z == 0]
+    elif kind == "ascending":
+        z = np.sort(z, axis=1)
+    return torch.from_numpy(z).to(R.torch_type(store))
+
+
+def forward(G, ctx, t, store, y, K, ldz=None, want_all=True):
+    import torch
+    n, C = t.shape
+    ldz = ldz or C
+    dev = torch.full((n, ldz), float("nan"), dtype=t.dtype, device="cuda")
+    dev[:, :C] = t.cuda()
+    o = lambda *s: torch.full(s, 9.0, device="cuda")
+    lp, H, l, top = o(n + 1), o(n + 1), o(n + 1), o(n + 1, max(K, 1))
+    idx = torch.full((n + 1, max(K, 1)), 77, dtype=torch.int32, device="cuda")
+    ws = torch.empty(max(16, G.gist_log_probs_workspace(n, C, K)), dtype=torch.uint8, device="cuda")
+    G.gist_log_probs(ctx, n, C, dev, ldz, R.store_of(G, store), to_dev(y), lp, H, l, K,
+                     top if K else None, idx if K else None, ws)
+    for x in (lp, H, l, top):
+        assert (to_host(x)[n:] == 9).all()       # nothing behind the rows
+    assert (to_host(idx)[n:] == 77).all()
+    return dev, lp[:n], H[:n], l[:n], top[:n, :K], idx[:n, :K]
+
+
+def close(got, want, bound):
+    """Equal where not finite, else within the bound."""
+    got, want = np.asarray(got, np.float64), np.asarray(want, np.float64)
+    fin = np.isfinite(want)
+    assert np.array_equal(np.isnan(got), np.isnan(want))
+    assert np.array_equal(got[~fin & ~np.isnan(want)], want[~fin & ~np.isnan(want)])
+    err = np.where(fin, np.abs(np.where(fin, got, 0) - np.where(fin, want, 0)), 0)
+    bound = np.broadcast_to(bound, err.shape)
+    worst = float(np.max(err / bound)) if err.size else 0.0
+    assert (err <= bound).all(), worst
+    return worst
+
+
+SHAPES = [(1, 1, 1), (5, 2, 2), (7, 7, 3), (300, 41, 5), (64, 47, 47), (33, 64, 64), (20, 65, 20),
+          (9, 130, 0), (6, 1000, 32), (3, 4096, 8), (2, 5003, 20), (1, 32000, 20), (1, 100003, 64),
+          (2, 131072, 5), (1100, 129, 4), (40, 8192, 1), (2000, 16, 2)]
+
+
+@pytest.mark.parametrize("store", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("n,C,K", SHAPES)
+def test_forward(G, ctx, store, n, C, K):
+    rng = np.random.default_rng(n * 13 + C + K)
+    kinds = ["plain", "masked", "lowest", "offset", "ties", "ascending"] if C <= 8192 else \
+        ["plain", "masked", "ties"]
+    for kind in kinds:
+        t = logits(n, C, store, rng, kind)
+        z = t.float().numpy()
+        y = rng.integers(-1, C, n).astype(np.int32)
+        y[0] = C - 1
+        ldz = C + (n + C) % 3 * 4
+        _, lp, H, l, top, idx = forward(G, ctx, t, store, y, K, ldz)
+        wl, wlp, wH = R.log_probs(z, y)
+        lb = R.lse_bound(z)
+        a = close(to_host(l), wl, lb)
+        b = close(to_host(lp), wlp, lb + R.U32 * np.abs(np.where(np.isfinite(wlp), wlp, 0)))
+        c = close(to_host(H), wH, R.entropy_bound(z))
+        wi = R.top_classes(z, K)
+        assert np.array_equal(to_host(idx), wi), kind
+        if K:
+            zt = np.take_along_axis(z.astype(np.float64), wi.astype(np.int64), 1)
+            with np.errstate(invalid="ignore"):
+                wt = np.where(zt == -np.inf, -np.inf, zt - wl[:, None])
+            close(to_host(top), wt, lb[:, None] + R.U32 * np.abs(np.where(np.isfinite(wt), wt, 0)))
+        log(f"log_probs {store} n={n} C={C} K={K} {kind}: error / bound lse {a:.2f} logp {b:.2f} H {c:.2f}")
+
+
+@pytest.mark.parametrize("store", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("n,C,K", [(8, 5, 5), (9, 47, 4), (4, 300, 8), (2, 20000, 6), (8, 16, 3)])
+def test_nonfinite_and_wrong_tokens(G, ctx, store, n, C, K):
+    rng = np.random.default_rng(C)
+    t = logits(n, C, store, rng)
+    t[0, C // 2] = float("nan")
+    t[1, C - 1] = float("inf")
+    if n > 5:
+        t[2] = -float("inf")
+        t[2, 0] = float("nan")
+        t[5] = -float("inf")
+        t[5, C - 1] = float("inf")
+    y = rng.integers(0, C, n).astype(np.int32)
+    y[n - 1] = C                       # the caller's mistake
+    y[n - 2] = -5                      # no given class
+    _, lp, H, l, top, idx = forward(G, ctx, t, store, y, K)
+    z = t.float().numpy()
+    wl, wlp, wH = R.log_probs(z, y)
+    close(to_host(l), wl, R.lse_bound(z))
+    close(to_host(lp), wlp, R.lse_bound(z) * 2)
+    close(to_host(H), wH, R.entropy_bound(z))
+    assert np.array_equal(to_host(idx), R.top_classes(z, K))
+    assert np.isnan(to_host(top)[:2]).all() and np.isfinite(to_host(top)[3:4]).all()
+
+
+def test_outputs_not_wanted(G, ctx):
+    """Any output may be left out; the others are what they are with all."""
+    import torch
+    n, C, K = 50, 77, 3
+    rng = np.random.default_rng(1)
+    t = logits(n, C, "f32", rng)
+    y = rng.integers(0, C, n).astype(np.int32)
+    dev, lp, H, l, top, idx = forward(G, ctx, t, "f32", y, K)
+    ws = torch.empty(16, dtype=torch.uint8, device="cuda")
+    e = torch.empty(n, device="cuda")
+    G.gist_log_probs(ctx, n, C, dev, C, 0, None, None, e, None, 0, None, None, ws)
+    assert torch.equal(e, H)
+    G.gist_log_probs(ctx, n, C, dev, C, 0, None, None, None, e, 0, None, None, None)
+    assert torch.equal(e, l)
+    G.gist_log_probs(ctx, n, C, dev, C, 0, to_dev(y), e, None, None, 0, None, None, ws)
+    assert torch.equal(e, lp)
+    i2, t2 = torch.empty_like(idx), torch.empty_like(top)
+    t2, i2 = t2.contiguous(), i2.contiguous()
+    G.gist_log_probs(ctx, n, C, dev, C, 0, None, None, None, None, K, t2, i2, ws)
+    assert torch.equal(i2, idx) and torch.equal(t2, top)
+    G.gist_log_probs(ctx, n, C, dev, C, 0, None, None, None, None, 0, None, None, ws)
+    G.gist_log_probs(ctx, 0, C, None, C, 0, None, None, None, None, 0, None, None, ws)
+
+
+@pytest.mark.parametrize("store", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("n,C", [(1, 1), (5, 2), (300, 41), (64, 47), (33, 64), (20, 130), (6, 1000),
+                                 (2, 5003), (1, 32000), (1, 100003), (3, 16384), (1500, 12)])
+def test_backward(G, ctx, store, n, C):
+    import torch
+    rng = np.random.default_rng(n + C)
+    for kind in ("plain", "masked", "lowest", "offset"):
+        t = logits(n, C, store, rng, kind)
+        z = t.float().numpy()
+        y = rng.integers(-1, C, n).astype(np.int32)
+        y[0] = C - 1
+        ldz = C + (n + C) % 3 * 4
+        dev, _, H, l, _, _ = forward(G, ctx, t, store, y, 0, ldz)
+        glh, ghh = (rng.standard_normal(n).astype(np.float32) for _ in range(2))
+        for gl, gh in ((glh, ghh), (glh, None), (None, ghh)):
+            ldd = C + 3
+            dz = torch.full((n + 1, ldd), 5.0, dtype=t.dtype, device="cuda")
+            G.gist_log_probs_bwd(ctx, n, C, dev, ldz, R.store_of(G, store), to_dev(y), l, H,
+                                 None if gl is None else to_dev(gl),
+                                 None if gh is None else to_dev(gh), dz, ldd)
+            got = to_host(dz.float())
+            want = R.log_probs_grad(z, y, gl, gh)
+            w = close(got[:n, :C], want, R.grad_bound(z, y, gl, gh, store) + 1e-45)
+            assert (got[n:] == 5).all() and (got[:, C:] == 5).all()
+        log(f"log_probs_bwd {store} n={n} C={C} {kind}: error / bound {w:.2f}")
+
+
+@pytest.mark.parametrize("C", [40, 3000])
+def test_backward_special_rows(G, ctx, C):
+    """In place; a masked row has gradient 0, a row with a NaN or a token past the classes
+    NaN, a row without a token no log-probability term."""
+    n = 6
+    rng = np.random.default_rng(C)
+    t = logits(n, C, "f32", rng)
+    t[0], t[1, 3] = -float("inf"), float("nan")
+    y = rng.integers(0, C, n).astype(np.int32)
+    y[2], y[3] = C, -1
+    dev, _, H, l, _, _ = forward(G, ctx, t, "f32", y, 0)
+    gl, gh = (rng.standard_normal(n).astype(np.float32) for _ in range(2))
+    G.gist_log_probs_bwd(ctx, n, C, dev, C, 0, to_dev(y), l, H, to_dev(gl), to_dev(gh), dev, C)
+    z = t.numpy()
+    close(to_host(dev), R.log_probs_grad(z, y, gl, gh),
+          np.nan_to_num(R.grad_bound(z, y, gl, gh, "f32")) + 1e-45)
+
+
+def test_gradient_against_differences(G, ctx):
+    """The gradient against differences of the library's own values: a change h of one logit
+    changes logp and entropy by h g + O(h^2); with h = 2^-6 the second-order term is below
+    h^2 (curvatures below 2 for these logits), the values' errors two bounds over h."""
+    import torch
+    n, C = 4, 50
+    rng = np.random.default_rng(2)
+    t = logits(n, C, "f32", rng)
+    y = rng.integers(0, C, n).astype(np.int32)
+    dev, _, H, l, _, _ = forward(G, ctx, t, "f32", y, 0)
+    one = to_dev(np.ones(n, np.float32))
+    h = 2.0 ** -6
+    for gl, gh, pick in ((one, None, 0), (None, one, 1)):
+        dz = torch.empty(n, C, device="cuda")
+        G.gist_log_probs_bwd(ctx, n, C, dev, C, 0, to_dev(y), l, H, gl, gh, dz, C)
+        got = to_host(dz)
+        for j in range(0, C, 7):
+            f = []
+            for s in (h, -h):
+                u = t.clone()
+                u[:, j] += s
+                f.append(to_host(forward(G, ctx, u, "f32", y, 0)[1 + pick]).astype(np.float64))
+            diff = (f[0] - f[1]) / (2 * h)
+            tol = h * h + (R.lse_bound(t.numpy()) + R.entropy_bound(t.numpy())) / h
+            assert (np.abs(diff - got[:, j]) <= tol).all()
+
+
+def test_logits_beyond_32_bit_offsets(G, ctx):
+    """Rows whose elements lie past 2^31."""
+    import torch
+    n, C = 17000, 131072            # 2.2e9 elements, 4.5 GB
+    dev = torch.zeros(n, C, dtype=torch.bfloat16, device="cuda")
+    dev[n - 1, 70000] = 20.0
+    y = torch.zeros(n, dtype=torch.int32, device="cuda")
+    y[n - 1] = 70000
+    o = lambda *s: torch.empty(*s, device="cuda")
+    lp, H, l, top = o(n), o(n), o(n), o(n, 1)
+    idx = torch.empty(n, 1, dtype=torch.int32, device="cuda")
+    G.gist_log_probs(ctx, n, C, dev, C, G.GIST_STORE_BF16, y, lp, H, l, 1, top, idx, None)
+    want = -np.log1p((C - 1) * np.exp(-20.0))
+    assert abs(to_host(lp)[-1] - want) < 1e-5 and to_host(idx)[-1, 0] == 70000
+    assert np.allclose(to_host(lp)[:-1], -np.log(C), rtol=1e-6) and (to_host(idx)[:-1] == 0).all()
+    g = torch.ones(n, device="cuda")
+    G.gist_log_probs_bwd(ctx, n, C, dev, C, G.GIST_STORE_BF16, y, l, None, g, None, dev, C)
+    assert abs(float(dev[n - 1, 70000]) - (1 - np.exp(want))) < 2 ** -8
+    assert abs(float(dev[n - 2, 0]) - 1) < 2 ** -8 and float(dev[n - 2, 1]) < 0
+
+
+@pytest.mark.parametrize("n,C,K", [(200, 47, 5), (2, 40000, 20)])
+def test_replays(G, n, C, K):
+    """Forward and gradient recorded once; every replay on new logits equals the eager
+    calls."""
+    import torch
+    st = torch.cuda.Stream()
+    cctx, ectx = G.Context(0, stream=st.cuda_stream), G.Context(0)
+    rng = np.random.default_rng(3)
+    z = torch.empty(n, C, device="cuda")
+    y = to_dev(rng.integers(0, C, n).astype(np.int32))
+    gl = to_dev(rng.standard_normal(n).astype(np.float32))
+    sets = []
+    for _ in range(2):
+        o = lambda *s: torch.zeros(*s, device="cuda")
+        sets.append((o(n), o(n), o(n), o(n, K), torch.zeros(n, K, dtype=torch.int32, device="cuda"),
+                     torch.empty(max(16, G.gist_log_probs_workspace(n, C, K)), dtype=torch.uint8,
+                                 device="cuda"), o(n, C)))
+
+    def calls(c, s):
+        G.gist_log_probs(c, n, C, z, C, 0, y, s[0], s[1], s[2], K, s[3], s[4], s[5])
+        G.gist_log_probs_bwd(c, n, C, z, C, 0, y, s[2], s[1], gl, gl, s[6], C)
+
+    torch.cuda.synchronize()
+    G.gist_capture_begin(cctx)
+    calls(cctx, sets[0])
+    r = G.gist_capture_end(cctx)
+    for k in range(4):
+        z.copy_(logits(n, C, "f32", rng, "masked" if k % 2 else "plain"))
+        calls(ectx, sets[1])
+        G.gist_replay_launch(ectx, r)
+        torch.cuda.synchronize()
+        for a, b in zip(sets[0][:5] + sets[0][6:], sets[1][:5] + sets[1][6:]):
+            assert torch.equal(a.nan_to_num(7.0), b.nan_to_num(7.0)), k

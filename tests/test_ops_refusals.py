@@ -1,0 +1,219 @@
+"""Arguments that the learned-row, log-probability and orthogonalised-update
+calls refuse, and their workspace sizes.  No GPU needed: every check runs on
+the host before anything touches the device."""
+
+import ctypes
+
+import numpy as np
+import pytest
+
+import ops_ref as R
+
+G = pytest.importorskip("paper_2102_10424_amd.gist",
+                        reason="libgist.so not built (python -m paper_2102_10424_amd.build)")
+
+
+class NoDevice:
+    """A context handle over zeroed memory: device 0, the default stream.  A refused call
+    reads no more of it."""
+
+    def __init__(self):
+        self.mem = ctypes.create_string_buffer(256)
+        self.handle = ctypes.cast(self.mem, ctypes.c_void_p)
+
+
+ctx = NoDevice()
+A = np.zeros(64, dtype=np.float32)     # stands for device memory; never read
+I = np.zeros(64, dtype=np.int32)
+INVAL, NOMEM, UNSUP = G.GIST_E_INVAL, G.GIST_E_NOMEM, G.GIST_E_UNSUPPORTED
+
+
+class Ws:
+    def __init__(self, nbytes, addr=None):
+        self.n, self.a = nbytes, addr if addr is not None else 4096
+
+    def numel(self):
+        return self.n
+
+    def element_size(self):
+        return 1
+
+    def data_ptr(self):
+        return self.a
+
+
+def refused(status, fn, *args, **kw):
+    with pytest.raises(G.GistError) as e:
+        fn(*args, **kw)
+    assert e.value.status == status, e.value
+
+
+def test_null_context():
+    class Null:
+        handle = None
+    refused(INVAL, G.gist_embed_lookup, Null, 1, 1, 1, A, 1, 0, I, 1.0, A, 1)
+    refused(INVAL, G.gist_embed_grad, Null, 1, 1, 1, I, 1.0, A, 1, A, 1, Ws(1 << 20))
+    refused(INVAL, G.gist_embed_grad_sgd, Null, 1, 1, 1, I, 1.0, A, 1, 0.1, A, 1, Ws(1 << 20))
+    refused(INVAL, G.gist_log_probs, Null, 1, 1, A, 1, 0, I, A, A, A, 0, None, None, None)
+    refused(INVAL, G.gist_log_probs_bwd, Null, 1, 1, A, 1, 0, I, A, A, A, A, A, 1)
+    d = G.muon_desc(4, 4)
+    refused(INVAL, G.gist_orthogonalize, Null, d, A, A, Ws(1 << 20))
+    refused(INVAL, G.gist_muon_update, Null, d, A, A, A, 0.1, 0.9, 0.0, 1.0, Ws(1 << 20))
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(n=-1), INVAL), (dict(V=-1), INVAL), (dict(d=0), INVAL), (dict(d=(1 << 22) + 1, ldt=1 << 23, ldo=1 << 23), UNSUP),
+    (dict(n=2**31 - 1), UNSUP), (dict(V=2**31 - 1), UNSUP), (dict(ldt=3), INVAL),
+    (dict(ldo=3), INVAL), (dict(store=3), INVAL), (dict(store=-1), INVAL),
+    (dict(scale=float("nan")), INVAL), (dict(scale=float("inf")), INVAL),
+    (dict(table=None), INVAL), (dict(ids=None), INVAL), (dict(out=None), INVAL)])
+def test_embed_lookup(change, status):
+    a = dict(n=2, V=5, d=4, table=A, ldt=4, store=0, ids=I, scale=1.0, out=A, ldo=4)
+    refused(status, G.gist_embed_lookup, ctx, **{**a, **change})
+
+
+@pytest.mark.parametrize("sgd", [False, True])
+@pytest.mark.parametrize("change,status", [
+    (dict(n=-1), INVAL), (dict(V=-1), INVAL), (dict(d=0), INVAL),
+    (dict(n=2**31 - 1), UNSUP), (dict(V=2**31 - 1), UNSUP),
+    (dict(ldy=3), INVAL), (dict(ldt=3), INVAL), (dict(scale=float("nan")), INVAL),
+    (dict(ids=None), INVAL), (dict(dY=None), INVAL), (dict(out=None), INVAL),
+    (dict(ws=None), NOMEM), (dict(ws="small"), NOMEM), (dict(ws="odd"), INVAL),
+    (dict(lr=float("inf")), INVAL)])
+def test_embed_grad(sgd, change, status):
+    a = dict(n=2, V=5, d=4, ids=I, scale=1.0, dY=A, ldy=4, out=A, ldt=4, lr=0.1,
+             ws=Ws(G.gist_embed_grad_workspace(2, 5, 4)))
+    a.update(change)
+    if a["ws"] == "small":
+        a["ws"] = Ws(G.gist_embed_grad_workspace(2, 5, 4) - 1)
+    if a["ws"] == "odd":
+        a["ws"] = Ws(1 << 20, 4100)
+    if sgd:
+        refused(status, G.gist_embed_grad_sgd, ctx, a["n"], a["V"], a["d"], a["ids"], a["scale"],
+                a["dY"], a["ldy"], a["lr"], a["out"], a["ldt"], a["ws"])
+    elif "lr" not in change:
+        refused(status, G.gist_embed_grad, ctx, a["n"], a["V"], a["d"], a["ids"], a["scale"],
+                a["dY"], a["ldy"], a["out"], a["ldt"], a["ws"])
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(n=-1), INVAL), (dict(C_=0), INVAL), (dict(ldz=6), INVAL), (dict(store=7), INVAL),
+    (dict(n=2**31 - 1), UNSUP), (dict(C_=2**31 - 1, ldz=2**31), UNSUP),
+    (dict(logits=None), INVAL), (dict(K=-1), INVAL), (dict(K=8), INVAL),
+    (dict(C_=100, ldz=100, K=65), INVAL), (dict(K=2, top_logp=None), INVAL),
+    (dict(K=2, top_idx=None), INVAL), (dict(tokens=None), INVAL)])
+def test_log_probs(change, status):
+    a = dict(n=2, C_=7, logits=A, ldz=7, store=0, tokens=I, logp=A, entropy=A, lse=A, K=0,
+             top_logp=A, top_idx=I, ws=Ws(1 << 20))
+    refused(status, G.gist_log_probs, ctx, **{**a, **change})
+
+
+def test_log_probs_workspace():
+    assert G.gist_log_probs_workspace(0, 5, 0) >= 0
+    need = G.gist_log_probs_workspace(1, 1 << 20, 8)     # one long row is split
+    assert need > 0
+    a = dict(n=1, C_=1 << 20, logits=A, ldz=1 << 20, store=0, tokens=I, logp=A, entropy=A, lse=A,
+             K=8, top_logp=A, top_idx=I)
+    refused(NOMEM, G.gist_log_probs, ctx, **a, ws=Ws(need - 1))
+    refused(NOMEM, G.gist_log_probs, ctx, **a, ws=None)
+    refused(INVAL, G.gist_log_probs, ctx, **a, ws=Ws(need, 4104))
+    for bad in ((-1, 5, 0), (2, 0, 0), (2, 5, 6), (2, 100, 65), (2, 5, -1), (2**31, 5, 0)):
+        assert G.gist_log_probs_workspace(*bad) == 0
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(n=-1), INVAL), (dict(C_=0), INVAL), (dict(ldz=6), INVAL), (dict(ldd=6), INVAL),
+    (dict(store=3), INVAL), (dict(logits=None), INVAL), (dict(lse=None), INVAL),
+    (dict(dlogits=None), INVAL), (dict(tokens=None), INVAL), (dict(entropy=None), INVAL),
+    (dict(dlogits=A, ldd=8), INVAL)])
+def test_log_probs_bwd(change, status):
+    a = dict(n=2, C_=7, logits=A, ldz=7, store=0, tokens=I, lse=A, entropy=A, g_logp=A,
+             g_entropy=A, dlogits=A.copy(), ldd=7)
+    refused(status, G.gist_log_probs_bwd, ctx, **{**a, **change})
+
+
+DESC = [(dict(rows=-1), INVAL), (dict(cols=-1), INVAL), (dict(groups=-1), INVAL),
+        (dict(rows=65537), UNSUP), (dict(cols=65537), UNSUP), (dict(groups=65536), UNSUP),
+        (dict(dtype=G.GIST_DTYPE_BF16_IN), INVAL), (dict(dtype=9), INVAL), (dict(flags=4), INVAL),
+        (dict(steps=0), INVAL), (dict(steps=33), INVAL), (dict(eps=0.0), INVAL),
+        (dict(eps=float("nan")), INVAL), (dict(eps=-1.0), INVAL),
+        (dict(coef=(float("nan"), 0, 0)), INVAL), (dict(coef=(9.0, 0, 0)), INVAL),
+        (dict(coef=(3.0, 1.0, 1.0)), INVAL), (dict(coef=(1.5, 10.0, -10.0)), INVAL),
+        (dict(coef=(2.0, 0.0, 0.0), steps=4), INVAL)]
+
+
+@pytest.mark.parametrize("change,status", DESC)
+def test_muon_desc(change, status):
+    d = G.muon_desc(**{**dict(rows=8, cols=6), **change})
+    refused(status, G.gist_muon_workspace_size, d)
+    refused(status, G.gist_orthogonalize, ctx, d, A, A, Ws(1 << 30))
+    refused(status, G.gist_muon_update, ctx, d, A, A, A, 0.1, 0.9, 0.0, 1.0, Ws(1 << 30))
+
+
+@pytest.mark.parametrize("coef", [R.COEF, (1.5, -0.5, 0.0), (15 / 8, -10 / 8, 3 / 8), (1.0, 0, 0)])
+def test_muon_coefficients_in_use_are_accepted(coef):
+    for steps in (1, 5, 32):
+        assert G.gist_muon_workspace_size(G.muon_desc(8, 6, coef=coef, steps=steps)) > 0
+
+
+def test_muon_calls():
+    d = G.muon_desc(8, 6)
+    need = G.gist_muon_workspace_size(d)
+    w = Ws(need)
+    refused(INVAL, G.gist_orthogonalize, ctx, d, None, A, w)
+    refused(INVAL, G.gist_orthogonalize, ctx, d, A, None, w)
+    refused(NOMEM, G.gist_orthogonalize, ctx, d, A, A, Ws(need - 1))
+    refused(NOMEM, G.gist_orthogonalize, ctx, d, A, A, None)
+    refused(INVAL, G.gist_orthogonalize, ctx, d, A, A, Ws(need, 4097))
+    ok = dict(W=A, dW=A, M=A, lr=0.1, momentum=0.9, weight_decay=0.0, scale=1.0, ws=w)
+    for change in (dict(W=None), dict(dW=None), dict(M=None), dict(lr=float("nan")),
+                   dict(momentum=1.0), dict(momentum=-0.1), dict(momentum=float("nan")),
+                   dict(weight_decay=float("inf")), dict(scale=float("nan"))):
+        refused(INVAL, G.gist_muon_update, ctx, d, **{**ok, **change})
+    refused(NOMEM, G.gist_muon_update, ctx, d, **{**ok, "ws": Ws(need - 1)})
+
+
+def test_layers_refuse_fp16_operands():
+    refused(INVAL, G.gist_layer_workspace_size,
+            G.layer_desc(G.GIST_LAYER_GCN, G.GIST_ACT_NONE, 8, 4, 4, G.GIST_DTYPE_F16_IN))
+    refused(INVAL, G.gist_gat_workspace_size,
+            G.gat_desc(8, 8, 4, 4, G.GIST_ACT_NONE, G.GIST_DTYPE_F16_IN))
+
+
+# ---- the references ---------------------------------------------------------------
+def test_log_probs_grad_reference_against_differences():
+    """The gradient formula against central differences of the 64-bit objective: with step
+    h the difference is off by h^2 / 6 of the third derivative (below 10 here) and 2^-52 / h
+    of the value."""
+    rng = np.random.default_rng(3)
+    z = rng.standard_normal((4, 9))
+    z[1, 3] = -np.inf
+    y = np.array([2, 0, -1, 8])
+    gl, gh = rng.standard_normal(4), rng.standard_normal(4)
+
+    def f(zz):
+        lse, lp, H = R.log_probs(zz, y)
+        return float((gl * np.where(y >= 0, lp, 0.0) + gh * H).sum())
+
+    d = R.log_probs_grad(z, y, gl, gh)
+    h = 1e-4
+    for v in range(4):
+        for j in range(9):
+            if z[v, j] == -np.inf:
+                assert d[v, j] == 0
+                continue
+            a, b = z.copy(), z.copy()
+            a[v, j] += h
+            b[v, j] -= h
+            assert abs((f(a) - f(b)) / (2 * h) - d[v, j]) < 10 * h * h + 1e-10
+
+
+def test_orthogonal_reference_forms_agree():
+    """The factor by singular values and by the iteration without noise."""
+    rng = np.random.default_rng(5)
+    for shape in ((5, 9), (9, 5), (1, 7), (6, 6)):
+        a = rng.standard_normal(shape)
+        w = R.orthogonal(a)
+        x = R.orthogonal_noisy(a, 0.0, 0.0, rng)
+        # coefficients differ by their rounding to fp32 in the first
+        assert np.linalg.norm(w - x) < 1e-5 * np.linalg.norm(w)
