@@ -14,6 +14,11 @@
 //
 // All three products are row times row (K contiguous in both operands): A and
 // B are symmetric, and X is kept both as X (m x n) and as X^T (n x m), m <= n.
+// Of A and B only the tiles on and below the diagonal are computed; the others
+// are their mirror images.
+//
+// Layout: 128 bytes of a row hold 64 values, or 32 values' first and then second
+// parts, so that a step of every product takes one 128-byte line of each row.
 
 #include <algorithm>
 
@@ -25,7 +30,6 @@ namespace {
 
 constexpr int kBlock = 256;
 constexpr float kS = 4096.f, kInvS = 1.f / 4096.f;
-constexpr int kPad = 64;        // padding of both sides
 constexpr int kNormBlocks = 256;
 
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
@@ -79,11 +83,18 @@ __device__ __forceinline__ void parts_of(float v, _Float16 (&p)[NP]) {
   if constexpr (NP == 2) p[1] = static_cast<_Float16>(v - static_cast<float>(p[0]));
 }
 
-// A matrix's parts: part p of element (i, j) at p * plane + i * ld + j.
+// A matrix of ld values per row (a multiple of 64): part p of value j of row i
+// is element at<NP>(i, j, p) of its group's block.
 struct Mat {
   _Float16* p;
-  int64_t ld, plane, group;
+  int64_t ld, group;
 };
+
+template <int NP>
+__device__ __forceinline__ int64_t at(const Mat& a, int64_t i, int64_t j, int p) {
+  if constexpr (NP == 1) return i * a.ld + j;
+  return 2 * i * a.ld + (j >> 5) * 64 + p * 32 + (j & 31);
+}
 
 // U / norm, split, as it stands (D) and transposed (T); 64 x 64 tiles over the
 // padded sides.
@@ -126,7 +137,7 @@ __global__ __launch_bounds__(kBlock) void split_kernel(int64_t rows, int64_t col
     _Float16 p[NP];
     parts_of<NP>(v, p);
 #pragma unroll
-    for (int q = 0; q < NP; ++q) d[q * D.plane + (r0 + r) * D.ld + c0 + c] = p[q];
+    for (int q = 0; q < NP; ++q) d[at<NP>(D, r0 + r, c0 + c, q)] = p[q];
   }
   __syncthreads();
 #pragma unroll
@@ -135,7 +146,7 @@ __global__ __launch_bounds__(kBlock) void split_kernel(int64_t rows, int64_t col
     _Float16 p[NP];
     parts_of<NP>(tile[r][c], p);
 #pragma unroll
-    for (int q = 0; q < NP; ++q) tr[q * T.plane + (c0 + c) * T.ld + r0 + r] = p[q];
+    for (int q = 0; q < NP; ++q) tr[at<NP>(T, c0 + c, r0 + r, q)] = p[q];
   }
 }
 
@@ -155,61 +166,182 @@ struct Epi {
   int o_half;
 };
 
+// Four values of consecutive rows i..i+3 of column j, and back as values i..i+3
+// of row j (i a multiple of 4).
 template <int NP>
-__device__ __forceinline__ float value_of(const Mat& a, int64_t g, int64_t i, int64_t j) {
-  const _Float16* p = a.p + g * a.group + i * a.ld + j;
-  float v = static_cast<float>(p[0]);
-  if constexpr (NP == 2) v += static_cast<float>(p[a.plane]);
+__device__ __forceinline__ void put4(const Mat& a, int64_t g, int64_t j, int64_t i, const float (&v)[4]) {
+  half4 h[NP];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    _Float16 s[NP];
+    parts_of<NP>(v[q], s);
+#pragma unroll
+    for (int x = 0; x < NP; ++x) h[x][q] = s[x];
+  }
+#pragma unroll
+  for (int x = 0; x < NP; ++x) *reinterpret_cast<half4*>(a.p + g * a.group + at<NP>(a, j, i, x)) = h[x];
+}
+
+template <int NP>
+__device__ __forceinline__ void put1(const Mat& a, int64_t g, int64_t i, int64_t j, float v) {
+  _Float16 s[NP];
+  parts_of<NP>(v, s);
+#pragma unroll
+  for (int x = 0; x < NP; ++x) a.p[g * a.group + at<NP>(a, i, j, x)] = s[x];
+}
+
+template <int NP>
+__device__ __forceinline__ float get1(const Mat& a, int64_t g, int64_t i, int64_t j) {
+  float v = static_cast<float>(a.p[g * a.group + at<NP>(a, i, j, 0)]);
+  if constexpr (NP == 2) v += static_cast<float>(a.p[g * a.group + at<NP>(a, i, j, 1)]);
   return v;
 }
 
-// P Q^T (rows of both K contiguous): 64 x 64 tiles, a 32 x 32 block per wave,
-// fragments straight from memory.
-template <int NP, int MODE>
-__global__ __launch_bounds__(kBlock) void product_kernel(int64_t K, Mat P, Mat Q, Epi E) {
-  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+// Workgroup barrier that orders LDS only.
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// 16 bytes per lane from memory straight to LDS: base + off (per lane) to
+// dst + 16 lane.  No register is written; the caller waits for vmcnt.
+__device__ __forceinline__ void load_to_lds(unsigned dst, unsigned off, const char* base) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+               :
+               : "s"(dst), "v"(off), "s"(base));
+}
+
+// Tile t of the lower triangle, row by row.
+__device__ __forceinline__ void triangle(int t, int& ti, int& tj) {
+  ti = static_cast<int>((sqrtf(8.f * t + 1.f) - 1.f) * 0.5f);
+  while (ti * (ti + 1) / 2 > t) --ti;
+  while ((ti + 1) * (ti + 2) / 2 <= t) ++ti;
+  tj = t - ti * (ti + 1) / 2;
+}
+
+// P Q^T (rows of both K contiguous), tiles of 32 WM NWM x 32 WN NWN by NWM x NWN
+// waves.  Every step takes 128 bytes of each of the tile's rows: lines go
+// from memory to one of two LDS buffers while the matrix cores work on the
+// other; one barrier per step.  A row's eight 16-byte pieces lie in LDS in the
+// order piece ^ (row mod 8), which spreads a fragment read (one piece of 32
+// rows) over the banks; the lanes of the load pick their piece accordingly.
+template <int NP, int MODE, int WM, int WN, int NWM, int NWN>
+__global__ __launch_bounds__(64 * NWM * NWN, 2) void product_kernel(int steps, int tiles_m, int tiles_n,
+                                                                    int tiles, Mat P, Mat Q, Epi E) {
+  constexpr int BM = 32 * WM * NWM, BN = 32 * WN * NWN;
+  constexpr int ROWS = BM + BN, LOADS = ROWS / 8 / (NWM * NWN);   // 8 rows a wave's load
+  constexpr int QN = 4 / NP;                                       // MFMA depths (16 values) per step
+  __shared__ __attribute__((aligned(1024))) char lds[2][ROWS * 128];
+  const int t = threadIdx.x, lane = t & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int li = lane & 31, lh = lane >> 5;
-  const int64_t g = blockIdx.z;
-  const int64_t i0 = blockIdx.y * 64 + (wave >> 1) * 32, j0 = blockIdx.x * 64 + (wave & 1) * 32;
-  const _Float16* p = P.p + g * P.group + (i0 + li) * P.ld + 8 * lh;
-  const _Float16* q = Q.p + g * Q.group + (j0 + li) * Q.ld + 8 * lh;
-  floatx16 acc = {};
-  for (int64_t k = 0; k < K; k += 16) {
-    half8 a[NP], b[NP];
-#pragma unroll
-    for (int s = 0; s < NP; ++s) {
-      a[s] = *reinterpret_cast<const half8*>(p + s * P.plane + k);
-      b[s] = *reinterpret_cast<const half8*>(q + s * Q.plane + k);
-    }
-    if constexpr (NP == 2) {
-      acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[0], b[1], acc, 0, 0, 0);
-      acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[1], b[0], acc, 0, 0, 0);
-    }
-    acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[0], b[0], acc, 0, 0, 0);
+  const int wm = wave / NWN, wn = wave % NWN;
+  const int id = static_cast<int>(xcd_remap(blockIdx.x, gridDim.x));
+  const int64_t g = id / tiles;
+  int ti, tj;
+  if constexpr (MODE == kGram || MODE == kPoly) {
+    triangle(id - static_cast<int>(g) * tiles, ti, tj);
+  } else {
+    const int x = id - static_cast<int>(g) * tiles;
+    ti = x % tiles_m;
+    tj = x / tiles_m;
   }
+  const int64_t ldp = P.ld * (2 * NP), ldq = Q.ld * (2 * NP);   // bytes
+  const char* const pb = reinterpret_cast<const char*>(P.p + g * P.group) + ti * BM * ldp;
+  const char* const qb = reinterpret_cast<const char*>(Q.p + g * Q.group) + tj * BN * ldq;
+  const unsigned lds0 = static_cast<unsigned>(reinterpret_cast<uintptr_t>(
+      (__attribute__((address_space(3))) char*)&lds[0][0]));
+  const unsigned piece = ((lane & 7) ^ (lane >> 3)) * 16;
+  const unsigned offp = static_cast<unsigned>((lane >> 3) * ldp) + piece;
+  const unsigned offq = static_cast<unsigned>((lane >> 3) * ldq) + piece;
+  auto load = [&](int buf, int j, int i) {   // the wave's load i of step j
+    const int r = (wave * LOADS + i) * 8;    // first of its eight rows (P's, then Q's)
+    const bool p = r < BM;
+    const char* base = p ? pb + r * ldp : qb + (r - BM) * ldq;
+    load_to_lds(lds0 + buf * (ROWS * 128) + r * 128, p ? offp : offq, base + j * 128);
+  };
+  floatx16 acc[WM][WN] = {};
 #pragma unroll
-  for (int r = 0; r < 16; ++r) {
-    const int64_t i = i0 + 8 * (r >> 2) + 4 * lh + (r & 3), j = j0 + li;
-    float v = acc[r] * kInvS;   // the product times S
-    if constexpr (MODE != kGram) v = fmaf(E.alpha, value_of<NP>(E.add, g, i, j), E.beta * v);
-    if constexpr (MODE == kLast) {
-      if (i >= E.m || j >= E.n) continue;
-      const int64_t e = g * E.group + i * E.si + j * E.sj;
-      v *= kInvS;
-      if (E.W) E.W[e] = fmaf(-E.eta, v, E.keep * E.W[e]);
-      else if (E.o_half) static_cast<_Float16*>(E.O)[e] = static_cast<_Float16>(v);
-      else static_cast<float*>(E.O)[e] = v;
-    } else {
-      _Float16 s[NP];
-      parts_of<NP>(v, s);
+  for (int i = 0; i < LOADS; ++i) load(0, 0, i);
+  const char* const fa = &lds[0][0] + (wm * WM * 32 + li) * 128;
+  const char* const fb = &lds[0][0] + (BM + wn * WN * 32 + li) * 128;
+  int fo[4];
 #pragma unroll
-      for (int x = 0; x < NP; ++x) {
-        E.out.p[g * E.out.group + x * E.out.plane + i * E.out.ld + j] = s[x];
-        if constexpr (MODE == kStep)
-          E.outT.p[g * E.outT.group + x * E.outT.plane + j * E.outT.ld + i] = s[x];
+  for (int q = 0; q < 4; ++q) fo[q] = ((2 * q + lh) ^ (li & 7)) * 16;
+  for (int j = 0; j < steps; ++j) {
+    const int buf = j & 1;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    lds_barrier();
+    if (j + 1 < steps) {
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) load(buf ^ 1, j + 1, i);
+    }
+    const int bo = buf * (ROWS * 128);
+#pragma unroll
+    for (int q = 0; q < QN; ++q) {
+      half8 a[WM][NP], b[WN][NP];
+#pragma unroll
+      for (int s = 0; s < NP; ++s) {
+#pragma unroll
+        for (int x = 0; x < WM; ++x)
+          a[x][s] = *reinterpret_cast<const half8*>(fa + bo + x * 4096 + fo[2 * s + q]);
+#pragma unroll
+        for (int x = 0; x < WN; ++x)
+          b[x][s] = *reinterpret_cast<const half8*>(fb + bo + x * 4096 + fo[2 * s + q]);
       }
+      if constexpr (NP == 2) {
+#pragma unroll
+        for (int x = 0; x < WM; ++x)
+#pragma unroll
+          for (int y = 0; y < WN; ++y)
+            acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[x][0], b[y][1], acc[x][y], 0, 0, 0);
+#pragma unroll
+        for (int x = 0; x < WM; ++x)
+#pragma unroll
+          for (int y = 0; y < WN; ++y)
+            acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[x][1], b[y][0], acc[x][y], 0, 0, 0);
+      }
+#pragma unroll
+      for (int x = 0; x < WM; ++x)
+#pragma unroll
+        for (int y = 0; y < WN; ++y)
+          acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[x][0], b[y][0], acc[x][y], 0, 0, 0);
     }
   }
+  const bool mirror = (MODE == kGram || MODE == kPoly) && ti != tj;
+#pragma unroll
+  for (int x = 0; x < WM; ++x)
+#pragma unroll
+    for (int y = 0; y < WN; ++y)
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) {
+        const int64_t i0 = static_cast<int64_t>(ti) * BM + (wm * WM + x) * 32 + 8 * r4 + 4 * lh;
+        const int64_t j = static_cast<int64_t>(tj) * BN + (wn * WN + y) * 32 + li;
+        float v[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          v[q] = acc[x][y][4 * r4 + q] * kInvS;   // the product times S
+          if constexpr (MODE != kGram) v[q] = fmaf(E.alpha, get1<NP>(E.add, g, i0 + q, j), E.beta * v[q]);
+        }
+        if constexpr (MODE == kLast) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const int64_t i = i0 + q;
+            if (i >= E.m || j >= E.n) continue;
+            const int64_t e = g * E.group + i * E.si + j * E.sj;
+            const float o = v[q] * kInvS;
+            if (E.W) E.W[e] = fmaf(-E.eta, o, E.keep * E.W[e]);
+            else if (E.o_half) static_cast<_Float16*>(E.O)[e] = static_cast<_Float16>(o);
+            else static_cast<float*>(E.O)[e] = o;
+          }
+        } else {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) put1<NP>(E.out, g, i0 + q, j, v[q]);
+          if constexpr (MODE == kStep) put4<NP>(E.outT, g, j, i0, v);
+          else if (mirror) put4<NP>(E.out, g, j, i0, v);
+        }
+      }
 }
 
 size_t up256(size_t x) { return (x + 255) & ~size_t(255); }
@@ -217,6 +349,7 @@ size_t up256(size_t x) { return (x + 255) & ~size_t(255); }
 struct Plan {
   int64_t G, m, n, mp, np;    // smaller and larger side, padded
   int parts;                  // per value
+  int tile;                   // 256, 128 or 64: products' tiles; both sides are padded to it
   bool flip;                  // rows > cols
   size_t norm, x, a;          // bytes: norm partials, one X (or X^T), one A (or B)
   size_t total() const { return norm + 4 * x + 2 * a; }
@@ -228,9 +361,14 @@ Plan plan(const gist_muon_desc* D) {
   p.flip = D->rows > D->cols;
   p.m = std::min(D->rows, D->cols);
   p.n = std::max(D->rows, D->cols);
-  p.mp = (p.m + kPad - 1) / kPad * kPad;
-  p.np = (p.n + kPad - 1) / kPad * kPad;
   p.parts = D->dtype == GIST_DTYPE_F32 ? 2 : 1;
+  p.tile = 64;
+  for (int t : {256, 128}) {
+    const int64_t tiles = p.G * ((p.m + t - 1) / t) * ((p.n + t - 1) / t);
+    if (tiles >= 128 && p.m > t / 2) { p.tile = t; break; }
+  }
+  p.mp = (p.m + p.tile - 1) / p.tile * p.tile;
+  p.np = (p.n + p.tile - 1) / p.tile * p.tile;
   p.norm = up256(static_cast<size_t>(p.G) * kNormBlocks * sizeof(double));
   p.x = up256(static_cast<size_t>(p.G) * p.parts * p.mp * p.np * 2);
   p.a = up256(static_cast<size_t>(p.G) * p.parts * p.mp * p.mp * 2);
@@ -238,12 +376,18 @@ Plan plan(const gist_muon_desc* D) {
 }
 
 template <int NP, int MODE>
-void product(hipStream_t st, int64_t M, int64_t N, int64_t K, int64_t G, const Mat& P, const Mat& Q,
+void product(hipStream_t st, const Plan& p, int64_t M, int64_t N, int64_t K, const Mat& P, const Mat& Q,
              const Epi& E) {
   static const char* const names[4] = {"muon_gram", "muon_poly", "muon_step", "muon_last"};
-  ProfScope ps(st, names[MODE], 2.0 * G * M * N * K, 2.0 * NP * G * (M * K + N * K + M * N));
-  const dim3 g(static_cast<unsigned>(N / kPad), static_cast<unsigned>(M / kPad), static_cast<unsigned>(G));
-  product_kernel<NP, MODE><<<g, kBlock, 0, st>>>(K, P, Q, E);
+  constexpr bool kSym = MODE == kGram || MODE == kPoly;
+  ProfScope ps(st, names[MODE], (kSym ? 1.0 : 2.0) * p.G * M * N * K, 2.0 * NP * p.G * (M * K + N * K + M * N));
+  const int tm = static_cast<int>(M / p.tile), tn = static_cast<int>(N / p.tile);
+  const int tiles = kSym ? tm * (tm + 1) / 2 : tm * tn;
+  const int steps = static_cast<int>(K * NP / 64);
+  const dim3 g(static_cast<unsigned>(tiles * p.G));
+  if (p.tile == 256) product_kernel<NP, MODE, 4, 2, 2, 4><<<g, 512, 0, st>>>(steps, tm, tn, tiles, P, Q, E);
+  else if (p.tile == 128) product_kernel<NP, MODE, 2, 2, 2, 2><<<g, 256, 0, st>>>(steps, tm, tn, tiles, P, Q, E);
+  else product_kernel<NP, MODE, 1, 1, 2, 2><<<g, 256, 0, st>>>(steps, tm, tn, tiles, P, Q, E);
 }
 
 template <int NP>
@@ -254,7 +398,7 @@ gist_status run(hipStream_t st, const gist_muon_desc* D, const float* G, void* O
   double* part = reinterpret_cast<double*>(ws);
   ws += p.norm;
   auto mat = [&](size_t bytes, int64_t r, int64_t c) {
-    Mat x{reinterpret_cast<_Float16*>(ws), c, r * c, NP * r * c};
+    Mat x{reinterpret_cast<_Float16*>(ws), c, NP * r * c};
     ws += bytes;
     return x;
   };
@@ -284,19 +428,19 @@ gist_status run(hipStream_t st, const gist_muon_desc* D, const float* G, void* O
   for (int k = 0; k < D->steps; ++k) {
     Epi e{};
     e.out = A;
-    product<NP, kGram>(st, p.mp, p.mp, p.np, p.G, X[cur], X[cur], e);
+    product<NP, kGram>(st, p, p.mp, p.mp, p.np, X[cur], X[cur], e);
     e.out = B;
     e.add = A;
     e.alpha = D->coef[1];
     e.beta = D->coef[2];
-    product<NP, kPoly>(st, p.mp, p.mp, p.mp, p.G, A, A, e);
+    product<NP, kPoly>(st, p, p.mp, p.mp, p.mp, A, A, e);
     e.add = X[cur];
     e.alpha = D->coef[0];
     e.beta = 1.f;
     if (k + 1 < D->steps) {
       e.out = X[cur ^ 1];
       e.outT = T[cur ^ 1];
-      product<NP, kStep>(st, p.mp, p.np, p.mp, p.G, B, T[cur], e);
+      product<NP, kStep>(st, p, p.mp, p.np, p.mp, B, T[cur], e);
       cur ^= 1;
     } else {
       e.W = W;
@@ -309,7 +453,7 @@ gist_status run(hipStream_t st, const gist_muon_desc* D, const float* G, void* O
       e.keep = u.keep;
       e.eta = u.eta;
       e.o_half = NP == 1;
-      product<NP, kLast>(st, p.mp, p.np, p.mp, p.G, B, T[cur], e);
+      product<NP, kLast>(st, p, p.mp, p.np, p.mp, B, T[cur], e);
     }
   }
   return check_launch("muon");

@@ -79,6 +79,35 @@ def test_orthogonalize(G, ctx, dtype, g, r, c):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "f16"])
+@pytest.mark.parametrize("g,r,c", [(9, 300, 600), (9, 513, 260), (16, 600, 700), (15, 770, 512), (1, 3000, 2900)])
+def test_orthogonalize_many_tiles(G, ctx, dtype, g, r, c):
+    """Sizes whose products take the larger tiles; first, middle and last group checked."""
+    rng = np.random.default_rng(g * 1000 + r * 7 + c)
+    U = matrices(g, r, c, rng)
+    got = orthogonalize(G, ctx, U, dtype)
+    if r > 1024:      # the iteration itself in 64 bits on the GPU; errors as at the smaller sizes
+        import torch
+        X = to_dev(U[0]).double()
+        X = X.t() if r > c else X
+        X = X / torch.linalg.vector_norm(X)
+        a, b, q = (float(np.float32(x)) for x in R.COEF)
+        for _ in range(5):
+            A = X @ X.t()
+            X = a * X + (b * A + q * (A @ A)) @ X
+        want = to_host(X.t() if r > c else X)
+        rel = 2.0 ** -22 if dtype == "f32" else 2.0 ** -11
+        # the bound at 512 x 512 is 14 roundings of this size
+        assert np.linalg.norm(got[0] - want) <= 14 * rel * np.linalg.norm(want)
+        return
+    for i in sorted({0, g // 2, g - 1}):
+        want = R.orthogonal(U[i])
+        tol = R.muon_tolerance(U[i], dtype) + store_slack(want, dtype)
+        err = np.linalg.norm(got[i] - want)
+        log(f"orthogonalize {dtype} {r}x{c} group {i}: {err / tol:.2f} of the bound")
+        assert err <= tol
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
 @pytest.mark.parametrize("steps,coef", [(1, R.COEF), (3, R.COEF), (8, (1.5, -0.5, 0.0)),
                                         (6, (15 / 8, -10 / 8, 3 / 8)), (2, (1.0, 0.0, 0.0))])
 def test_steps_and_coefficients(G, ctx, dtype, steps, coef):
