@@ -34,6 +34,7 @@ constexpr int kNormBlocks = 256;
 
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef _Float16 half4 __attribute__((ext_vector_type(4)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
 struct Update {
@@ -204,6 +205,13 @@ __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
+// Wait until at most N of this wave's loads are out (the counter takes 6 bits).
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  static_assert(N >= 0 && N < 64, "vmcnt");
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
 // 16 bytes per lane from memory straight to LDS: base + off (per lane) to
 // dst + 16 lane.  No register is written; the caller waits for vmcnt.
 __device__ __forceinline__ void load_to_lds(unsigned dst, unsigned off, const char* base) {
@@ -211,6 +219,15 @@ __device__ __forceinline__ void load_to_lds(unsigned dst, unsigned off, const ch
                :
                : "s"(dst), "v"(off), "s"(base));
 }
+
+// Work of one product: tiles of all groups.  The first `whole` are one
+// workgroup's each; the others (`ragged` of them) are cut in K into `slices`
+// of `len` steps, slice-major, joined by a second kernel.
+struct Sched {
+  int tiles_m, tiles_n, tiles;   // of one matrix
+  int64_t whole, ragged;
+  int slices, len, steps;
+};
 
 // Tile t of the lower triangle, row by row.
 __device__ __forceinline__ void triangle(int t, int& ti, int& tj) {
@@ -220,36 +237,87 @@ __device__ __forceinline__ void triangle(int t, int& ti, int& tj) {
   tj = t - ti * (ti + 1) / 2;
 }
 
+template <int MODE>
+__device__ __forceinline__ void tile_of(const Sched& S, int64_t id, int64_t& g, int& ti, int& tj) {
+  g = static_cast<unsigned>(id) / static_cast<unsigned>(S.tiles);
+  const int x = static_cast<int>(id - g * S.tiles);
+  if constexpr (MODE == kGram || MODE == kPoly) {
+    triangle(x, ti, tj);
+  } else {
+    ti = x % S.tiles_m;
+    tj = x / S.tiles_m;
+  }
+}
+
+// One 32 x 32 block at (row, col) of group g's result.  Accumulator register r
+// of lane l: row 8 (r / 4) + 4 (l / 32) + r mod 4, column l mod 32.
+template <int NP, int MODE>
+__device__ __forceinline__ void finish_block(const floatx16& acc, const Epi& E, int64_t g, int row, int col,
+                                             int lane, bool off_diagonal) {
+  const int64_t j = col + (lane & 31);
+#pragma unroll
+  for (int r4 = 0; r4 < 4; ++r4) {
+    const int64_t i0 = row + 8 * r4 + 4 * (lane >> 5);
+    float v[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      v[q] = acc[4 * r4 + q] * kInvS;   // the product times S
+      if constexpr (MODE != kGram) v[q] = fmaf(E.alpha, get1<NP>(E.add, g, i0 + q, j), E.beta * v[q]);
+    }
+    if constexpr (MODE == kLast) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int64_t i = i0 + q;
+        if (i >= E.m || j >= E.n) continue;
+        const int64_t e = g * E.group + i * E.si + j * E.sj;
+        const float o = v[q] * kInvS;
+        if (E.W) E.W[e] = fmaf(-E.eta, o, E.keep * E.W[e]);
+        else if (E.o_half) static_cast<_Float16*>(E.O)[e] = static_cast<_Float16>(o);
+        else static_cast<float*>(E.O)[e] = o;
+      }
+    } else {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) put1<NP>(E.out, g, i0 + q, j, v[q]);
+      if constexpr (MODE == kStep) put4<NP>(E.outT, g, j, i0, v);
+      else if (off_diagonal) put4<NP>(E.out, g, j, i0, v);
+    }
+  }
+}
+
 // P Q^T (rows of both K contiguous), tiles of 32 WM NWM x 32 WN NWN by NWM x NWN
 // waves.  Every step takes 128 bytes of each of the tile's rows: lines go
 // from memory to one of two LDS buffers while the matrix cores work on the
 // other; one barrier per step.  A row's eight 16-byte pieces lie in LDS in the
 // order piece ^ (row mod 8), which spreads a fragment read (one piece of 32
 // rows) over the banks; the lanes of the load pick their piece accordingly.
-template <int NP, int MODE, int WM, int WN, int NWM, int NWN>
-__global__ __launch_bounds__(64 * NWM * NWN, 2) void product_kernel(int steps, int tiles_m, int tiles_n,
-                                                                    int tiles, Mat P, Mat Q, Epi E) {
+// NS buffers: NS - 1 steps are on their way; small tiles, whose steps are short,
+// need more of them to cover memory's latency.
+template <int NP, int MODE, int WM, int WN, int NWM, int NWN, int NS>
+__global__ __launch_bounds__(64 * NWM * NWN, 2) void product_kernel(Sched S, Mat P, Mat Q, Epi E,
+                                                                    float* __restrict__ part) {
   constexpr int BM = 32 * WM * NWM, BN = 32 * WN * NWN;
   constexpr int ROWS = BM + BN, LOADS = ROWS / 8 / (NWM * NWN);   // 8 rows a wave's load
   constexpr int QN = 4 / NP;                                       // MFMA depths (16 values) per step
-  __shared__ __attribute__((aligned(1024))) char lds[2][ROWS * 128];
+  __shared__ __attribute__((aligned(1024))) char lds[NS][ROWS * 128];
   const int t = threadIdx.x, lane = t & 63;
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int li = lane & 31, lh = lane >> 5;
   const int wm = wave / NWN, wn = wave % NWN;
-  const int id = static_cast<int>(xcd_remap(blockIdx.x, gridDim.x));
-  const int64_t g = id / tiles;
-  int ti, tj;
-  if constexpr (MODE == kGram || MODE == kPoly) {
-    triangle(id - static_cast<int>(g) * tiles, ti, tj);
+  int64_t id, u = -1, g;
+  int ti, tj, k0 = 0, steps = S.steps;
+  if (blockIdx.x < S.whole) {
+    id = xcd_remap(blockIdx.x, S.whole);
   } else {
-    const int x = id - static_cast<int>(g) * tiles;
-    ti = x % tiles_m;
-    tj = x / tiles_m;
+    u = xcd_remap(blockIdx.x - S.whole, gridDim.x - S.whole);
+    const int slice = static_cast<int>(static_cast<unsigned>(u) / static_cast<unsigned>(S.ragged));
+    id = S.whole + (u - slice * S.ragged);
+    k0 = slice * S.len;
+    steps = min(S.len, S.steps - k0);
   }
+  tile_of<MODE>(S, id, g, ti, tj);
   const int64_t ldp = P.ld * (2 * NP), ldq = Q.ld * (2 * NP);   // bytes
-  const char* const pb = reinterpret_cast<const char*>(P.p + g * P.group) + ti * BM * ldp;
-  const char* const qb = reinterpret_cast<const char*>(Q.p + g * Q.group) + tj * BN * ldq;
+  const char* const pb = reinterpret_cast<const char*>(P.p + g * P.group) + ti * BM * ldp + k0 * 128;
+  const char* const qb = reinterpret_cast<const char*>(Q.p + g * Q.group) + tj * BN * ldq + k0 * 128;
   const unsigned lds0 = static_cast<unsigned>(reinterpret_cast<uintptr_t>(
       (__attribute__((address_space(3))) char*)&lds[0][0]));
   const unsigned piece = ((lane & 7) ^ (lane >> 3)) * 16;
@@ -263,19 +331,25 @@ __global__ __launch_bounds__(64 * NWM * NWN, 2) void product_kernel(int steps, i
   };
   floatx16 acc[WM][WN] = {};
 #pragma unroll
-  for (int i = 0; i < LOADS; ++i) load(0, 0, i);
+  for (int j = 0; j < NS - 1; ++j) {
+    const int js = min(j, steps - 1);   // always NS - 1 steps' loads, so that the counts below hold
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) load(j, js, i);
+  }
   const char* const fa = &lds[0][0] + (wm * WM * 32 + li) * 128;
   const char* const fb = &lds[0][0] + (BM + wn * WN * 32 + li) * 128;
   int fo[4];
 #pragma unroll
   for (int q = 0; q < 4; ++q) fo[q] = ((2 * q + lh) ^ (li & 7)) * 16;
+  int buf = 0, free = NS - 1;
   for (int j = 0; j < steps; ++j) {
-    const int buf = j & 1;
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    // step j has arrived when at most the loads of the NS - 2 steps after it are out
+    wait_loads<LOADS * (NS - 2)>();
     lds_barrier();
-    if (j + 1 < steps) {
+    {
+      const int js = min(j + NS - 1, steps - 1);   // past the end: the last step again, never read
 #pragma unroll
-      for (int i = 0; i < LOADS; ++i) load(buf ^ 1, j + 1, i);
+      for (int i = 0; i < LOADS; ++i) load(free, js, i);
     }
     const int bo = buf * (ROWS * 128);
 #pragma unroll
@@ -308,40 +382,54 @@ __global__ __launch_bounds__(64 * NWM * NWN, 2) void product_kernel(int steps, i
         for (int y = 0; y < WN; ++y)
           acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[x][0], b[y][0], acc[x][y], 0, 0, 0);
     }
+    buf = buf + 1 == NS ? 0 : buf + 1;
+    free = free + 1 == NS ? 0 : free + 1;
   }
-  const bool mirror = (MODE == kGram || MODE == kPoly) && ti != tj;
+  wait_loads<0>();   // nothing may still be on its way to LDS when the workgroup ends
+  if (u >= 0) {   // a slice: its sums, 32 x 32 blocks in accumulator order
+    floatx4* d = reinterpret_cast<floatx4*>(part + u * static_cast<int64_t>(BM * BN)) + lane;
+#pragma unroll
+    for (int x = 0; x < WM; ++x)
+#pragma unroll
+      for (int y = 0; y < WN; ++y)
+#pragma unroll
+        for (int r4 = 0; r4 < 4; ++r4) {
+          const int blk = (wm * WM + x) * (BN / 32) + wn * WN + y;
+          d[(blk * 4 + r4) * 64] = floatx4{acc[x][y][4 * r4], acc[x][y][4 * r4 + 1], acc[x][y][4 * r4 + 2],
+                                           acc[x][y][4 * r4 + 3]};
+        }
+    return;
+  }
 #pragma unroll
   for (int x = 0; x < WM; ++x)
 #pragma unroll
     for (int y = 0; y < WN; ++y)
+      finish_block<NP, MODE>(acc[x][y], E, g, ti * BM + (wm * WM + x) * 32, tj * BN + (wn * WN + y) * 32,
+                             lane, ti != tj);
+}
+
+// Tiles that were cut in K: a wave per 32 x 32 block adds the slices in order.
+template <int NP, int MODE>
+__global__ __launch_bounds__(kBlock) void join_kernel(Sched S, int tile, const float* __restrict__ part, Epi E) {
+  const int lane = threadIdx.x & 63, bt = tile / 32;
+  const int64_t w = (static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x) >> 6;
+  const int blk = static_cast<int>(w % (bt * bt));
+  const int64_t rt = w / (bt * bt);
+  if (rt >= S.ragged) return;
+  int64_t g;
+  int ti, tj;
+  tile_of<MODE>(S, S.whole + rt, g, ti, tj);
+  floatx16 acc = {};
+  for (int s = 0; s < S.slices; ++s) {
+    const floatx4* d = reinterpret_cast<const floatx4*>(part + (s * S.ragged + rt) * tile * tile) + blk * 256 + lane;
 #pragma unroll
-      for (int r4 = 0; r4 < 4; ++r4) {
-        const int64_t i0 = static_cast<int64_t>(ti) * BM + (wm * WM + x) * 32 + 8 * r4 + 4 * lh;
-        const int64_t j = static_cast<int64_t>(tj) * BN + (wn * WN + y) * 32 + li;
-        float v[4];
+    for (int r4 = 0; r4 < 4; ++r4) {
+      const floatx4 v = d[r4 * 64];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          v[q] = acc[x][y][4 * r4 + q] * kInvS;   // the product times S
-          if constexpr (MODE != kGram) v[q] = fmaf(E.alpha, get1<NP>(E.add, g, i0 + q, j), E.beta * v[q]);
-        }
-        if constexpr (MODE == kLast) {
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const int64_t i = i0 + q;
-            if (i >= E.m || j >= E.n) continue;
-            const int64_t e = g * E.group + i * E.si + j * E.sj;
-            const float o = v[q] * kInvS;
-            if (E.W) E.W[e] = fmaf(-E.eta, o, E.keep * E.W[e]);
-            else if (E.o_half) static_cast<_Float16*>(E.O)[e] = static_cast<_Float16>(o);
-            else static_cast<float*>(E.O)[e] = o;
-          }
-        } else {
-#pragma unroll
-          for (int q = 0; q < 4; ++q) put1<NP>(E.out, g, i0 + q, j, v[q]);
-          if constexpr (MODE == kStep) put4<NP>(E.outT, g, j, i0, v);
-          else if (mirror) put4<NP>(E.out, g, j, i0, v);
-        }
-      }
+      for (int q = 0; q < 4; ++q) acc[4 * r4 + q] += v[q];
+    }
+  }
+  finish_block<NP, MODE>(acc, E, g, ti * tile + (blk / bt) * 32, tj * tile + (blk % bt) * 32, lane, ti != tj);
 }
 
 size_t up256(size_t x) { return (x + 255) & ~size_t(255); }
@@ -349,11 +437,56 @@ size_t up256(size_t x) { return (x + 255) & ~size_t(255); }
 struct Plan {
   int64_t G, m, n, mp, np;    // smaller and larger side, padded
   int parts;                  // per value
-  int tile;                   // 256, 128 or 64: products' tiles; both sides are padded to it
+  int pad;                    // 256, 128 or 64: both sides are padded to it, tiles are at most it
   bool flip;                  // rows > cols
   size_t norm, x, a;          // bytes: norm partials, one X (or X^T), one A (or B)
-  size_t total() const { return norm + 4 * x + 2 * a; }
+  size_t part;                // partial tiles
+  size_t total() const { return norm + 4 * x + 2 * a + part; }
 };
+
+struct Choice {
+  int tile;
+  Sched s;
+  size_t part_bytes() const {
+    return s.ragged ? up256(static_cast<size_t>(s.ragged) * s.slices * tile * tile * 4) : 0;
+  }
+};
+
+// Tile and K cuts of one product, by an estimate in microseconds: a round of
+// `slots` workgroups takes `step` per step of K, and a join its launch and its
+// traffic.
+Choice choose(const Plan& p, int64_t M, int64_t N, int64_t K, bool sym) {
+  Choice best{};
+  double best_us = 0;
+  for (int tile : {256, 128, 64}) {
+    if (tile > p.pad) continue;
+    const int64_t tm = M / tile, tn = N / tile;
+    Sched s{};
+    s.tiles_m = static_cast<int>(tm);
+    s.tiles_n = static_cast<int>(tn);
+    s.tiles = static_cast<int>(sym ? tm * (tm + 1) / 2 : tm * tn);
+    s.steps = static_cast<int>(K * p.parts / 64);
+    const int64_t all = s.tiles * p.G;
+    const int slots = 256 * (tile == 256 ? 1 : 2);
+    const double step = (p.parts == 2 ? 1.0 : 0.75) * (tile == 256 ? 3.0 : tile == 128 ? 1.7 : 0.6);
+    const int64_t full = all / slots * slots, left = all - full;
+    for (int slices : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
+      if (slices > 1 && (left == 0 || s.steps / slices < 4 || left * slices > slots)) continue;
+      s.len = (s.steps + slices - 1) / slices;
+      s.slices = (s.steps + s.len - 1) / s.len;
+      s.whole = slices == 1 ? all : full;
+      s.ragged = all - s.whole;
+      double us = 3.0 + (full / slots) * (s.steps * step) + (left ? s.len * step : 0.0);
+      if (slices > 1) us += 5.0 + left * slices * (tile * tile * 8.0) / 4e6;
+      if (best.tile == 0 || us < best_us) {
+        best.tile = tile;
+        best.s = s;
+        best_us = us;
+      }
+    }
+  }
+  return best;
+}
 
 Plan plan(const gist_muon_desc* D) {
   Plan p;
@@ -362,32 +495,37 @@ Plan plan(const gist_muon_desc* D) {
   p.m = std::min(D->rows, D->cols);
   p.n = std::max(D->rows, D->cols);
   p.parts = D->dtype == GIST_DTYPE_F32 ? 2 : 1;
-  p.tile = 64;
-  for (int t : {256, 128}) {
-    const int64_t tiles = p.G * ((p.m + t - 1) / t) * ((p.n + t - 1) / t);
-    if (tiles >= 128 && p.m > t / 2) { p.tile = t; break; }
-  }
-  p.mp = (p.m + p.tile - 1) / p.tile * p.tile;
-  p.np = (p.n + p.tile - 1) / p.tile * p.tile;
+  p.pad = p.m > 512 ? 256 : p.m > 128 ? 128 : 64;
+  p.mp = (p.m + p.pad - 1) / p.pad * p.pad;
+  p.np = (p.n + p.pad - 1) / p.pad * p.pad;
   p.norm = up256(static_cast<size_t>(p.G) * kNormBlocks * sizeof(double));
   p.x = up256(static_cast<size_t>(p.G) * p.parts * p.mp * p.np * 2);
   p.a = up256(static_cast<size_t>(p.G) * p.parts * p.mp * p.mp * 2);
+  p.part = 0;
+  for (const Choice& c : {choose(p, p.mp, p.mp, p.np, true), choose(p, p.mp, p.mp, p.mp, true),
+                          choose(p, p.mp, p.np, p.mp, false)})
+    p.part = std::max(p.part, c.part_bytes());
   return p;
 }
 
 template <int NP, int MODE>
 void product(hipStream_t st, const Plan& p, int64_t M, int64_t N, int64_t K, const Mat& P, const Mat& Q,
-             const Epi& E) {
+             const Epi& E, float* part) {
   static const char* const names[4] = {"muon_gram", "muon_poly", "muon_step", "muon_last"};
   constexpr bool kSym = MODE == kGram || MODE == kPoly;
-  ProfScope ps(st, names[MODE], (kSym ? 1.0 : 2.0) * p.G * M * N * K, 2.0 * NP * p.G * (M * K + N * K + M * N));
-  const int tm = static_cast<int>(M / p.tile), tn = static_cast<int>(N / p.tile);
-  const int tiles = kSym ? tm * (tm + 1) / 2 : tm * tn;
-  const int steps = static_cast<int>(K * NP / 64);
-  const dim3 g(static_cast<unsigned>(tiles * p.G));
-  if (p.tile == 256) product_kernel<NP, MODE, 4, 2, 2, 4><<<g, 512, 0, st>>>(steps, tm, tn, tiles, P, Q, E);
-  else if (p.tile == 128) product_kernel<NP, MODE, 2, 2, 2, 2><<<g, 256, 0, st>>>(steps, tm, tn, tiles, P, Q, E);
-  else product_kernel<NP, MODE, 1, 1, 2, 2><<<g, 256, 0, st>>>(steps, tm, tn, tiles, P, Q, E);
+  const Choice c = choose(p, M, N, K, kSym);
+  {
+    ProfScope ps(st, names[MODE], (kSym ? 1.0 : 2.0) * p.G * M * N * K, 2.0 * NP * p.G * (M * K + N * K + M * N));
+    const dim3 g(static_cast<unsigned>(c.s.whole + c.s.ragged * c.s.slices));
+    if (c.tile == 256) product_kernel<NP, MODE, 4, 2, 2, 4, 2><<<g, 512, 0, st>>>(c.s, P, Q, E, part);
+    else if (c.tile == 128) product_kernel<NP, MODE, 2, 2, 2, 2, 2><<<g, 256, 0, st>>>(c.s, P, Q, E, part);
+    else product_kernel<NP, MODE, 1, 1, 2, 2, 4><<<g, 256, 0, st>>>(c.s, P, Q, E, part);
+  }
+  if (c.s.ragged) {
+    ProfScope ps(st, "muon_join", 0.0, static_cast<double>(c.part_bytes()));
+    const int64_t waves = c.s.ragged * (c.tile / 32) * (c.tile / 32);
+    join_kernel<NP, MODE><<<dim3(static_cast<unsigned>((waves + 3) / 4)), kBlock, 0, st>>>(c.s, c.tile, part, E);
+  }
 }
 
 template <int NP>
@@ -408,6 +546,7 @@ gist_status run(hipStream_t st, const gist_muon_desc* D, const float* G, void* O
     T[i] = mat(p.x, p.np, p.mp);
   }
   const Mat A = mat(p.a, p.mp, p.mp), B = mat(p.a, p.mp, p.mp);
+  float* parts = reinterpret_cast<float*>(ws);
   const int nb = static_cast<int>(std::min<int64_t>(kNormBlocks, (count + kBlock - 1) / kBlock));
   {
     ProfScope ps(st, "muon_norm", 4.0 * p.G * count, (W ? 12.0 : 4.0) * p.G * count);
@@ -428,19 +567,19 @@ gist_status run(hipStream_t st, const gist_muon_desc* D, const float* G, void* O
   for (int k = 0; k < D->steps; ++k) {
     Epi e{};
     e.out = A;
-    product<NP, kGram>(st, p, p.mp, p.mp, p.np, X[cur], X[cur], e);
+    product<NP, kGram>(st, p, p.mp, p.mp, p.np, X[cur], X[cur], e, parts);
     e.out = B;
     e.add = A;
     e.alpha = D->coef[1];
     e.beta = D->coef[2];
-    product<NP, kPoly>(st, p, p.mp, p.mp, p.mp, A, A, e);
+    product<NP, kPoly>(st, p, p.mp, p.mp, p.mp, A, A, e, parts);
     e.add = X[cur];
     e.alpha = D->coef[0];
     e.beta = 1.f;
     if (k + 1 < D->steps) {
       e.out = X[cur ^ 1];
       e.outT = T[cur ^ 1];
-      product<NP, kStep>(st, p, p.mp, p.np, p.mp, B, T[cur], e);
+      product<NP, kStep>(st, p, p.mp, p.np, p.mp, B, T[cur], e, parts);
       cur ^= 1;
     } else {
       e.W = W;
@@ -453,7 +592,7 @@ gist_status run(hipStream_t st, const gist_muon_desc* D, const float* G, void* O
       e.keep = u.keep;
       e.eta = u.eta;
       e.o_half = NP == 1;
-      product<NP, kLast>(st, p, p.mp, p.np, p.mp, B, T[cur], e);
+      product<NP, kLast>(st, p, p.mp, p.np, p.mp, B, T[cur], e, parts);
     }
   }
   return check_launch("muon");
