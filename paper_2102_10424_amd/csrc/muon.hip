@@ -288,10 +288,11 @@ __device__ __forceinline__ void finish_block(const floatx16& acc, const Epi& E, 
 // waves.  Every step takes 128 bytes of each of the tile's rows: lines go
 // from memory to one of two LDS buffers while the matrix cores work on the
 // other; one barrier per step.  A row's eight 16-byte pieces lie in LDS in the
-// order piece ^ (row mod 8), which spreads a fragment read (one piece of 32
-// rows) over the banks; the lanes of the load pick their piece accordingly.
-// NS buffers: NS - 1 steps are on their way; small tiles, whose steps are short,
-// need more of them to cover memory's latency.
+// order piece ^ (row / 2 mod 8), which spreads a fragment read (one piece of 32
+// rows) over the 64 banks; the lanes of the load pick their piece accordingly.
+// (By row mod 8, right for 32 banks, half of all LDS cycles were conflicts.)
+// NS buffers; small tiles, whose steps are short, need more of them to cover
+// memory's latency.
 template <int NP, int MODE, int WM, int WN, int NWM, int NWN, int NS>
 __global__ __launch_bounds__(64 * NWM * NWN, 2) void product_kernel(Sched S, Mat P, Mat Q, Epi E,
                                                                     float* __restrict__ part) {
@@ -320,19 +321,24 @@ __global__ __launch_bounds__(64 * NWM * NWN, 2) void product_kernel(Sched S, Mat
   const char* const qb = reinterpret_cast<const char*>(Q.p + g * Q.group) + tj * BN * ldq + k0 * 128;
   const unsigned lds0 = static_cast<unsigned>(reinterpret_cast<uintptr_t>(
       (__attribute__((address_space(3))) char*)&lds[0][0]));
-  const unsigned piece = ((lane & 7) ^ (lane >> 3)) * 16;
-  const unsigned offp = static_cast<unsigned>((lane >> 3) * ldp) + piece;
-  const unsigned offq = static_cast<unsigned>((lane >> 3) * ldq) + piece;
+  static_assert(LOADS % 2 == 0, "the piece order below goes by the parity of a load");
+  unsigned offp[2], offq[2];   // of even and odd loads
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const unsigned piece = ((lane & 7) ^ ((lane >> 4) + 4 * h)) * 16;
+    offp[h] = static_cast<unsigned>((lane >> 3) * ldp) + piece;
+    offq[h] = static_cast<unsigned>((lane >> 3) * ldq) + piece;
+  }
   auto load = [&](int buf, int j, int i) {   // the wave's load i of step j
     const int r = (wave * LOADS + i) * 8;    // first of its eight rows (P's, then Q's)
     const bool p = r < BM;
     const char* base = p ? pb + r * ldp : qb + (r - BM) * ldq;
-    load_to_lds(lds0 + buf * (ROWS * 128) + r * 128, p ? offp : offq, base + j * 128);
+    load_to_lds(lds0 + buf * (ROWS * 128) + r * 128, p ? offp[i & 1] : offq[i & 1], base + j * 128);
   };
   floatx16 acc[WM][WN] = {};
 #pragma unroll
-  for (int j = 0; j < NS - 1; ++j) {
-    const int js = min(j, steps - 1);   // always NS - 1 steps' loads, so that the counts below hold
+  for (int j = 0; j < NS; ++j) {
+    const int js = min(j, steps - 1);   // always NS steps' loads, so that the counts below hold
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) load(j, js, i);
   }
@@ -340,50 +346,68 @@ __global__ __launch_bounds__(64 * NWM * NWN, 2) void product_kernel(Sched S, Mat
   const char* const fb = &lds[0][0] + (BM + wn * WN * 32 + li) * 128;
   int fo[4];
 #pragma unroll
-  for (int q = 0; q < 4; ++q) fo[q] = ((2 * q + lh) ^ (li & 7)) * 16;
-  int buf = 0, free = NS - 1;
-  for (int j = 0; j < steps; ++j) {
-    // step j has arrived when at most the loads of the NS - 2 steps after it are out
-    wait_loads<LOADS * (NS - 2)>();
-    lds_barrier();
-    {
-      const int js = min(j + NS - 1, steps - 1);   // past the end: the last step again, never read
-#pragma unroll
-      for (int i = 0; i < LOADS; ++i) load(free, js, i);
-    }
+  for (int q = 0; q < 4; ++q) fo[q] = ((2 * q + lh) ^ (li >> 1 & 7)) * 16;
+  half8 a[2][WM][NP], b[2][WN][NP];   // fragments of this depth and of the next
+  auto read = [&](int to, int buf, int q) {
     const int bo = buf * (ROWS * 128);
 #pragma unroll
+    for (int s = 0; s < NP; ++s) {
+#pragma unroll
+      for (int x = 0; x < WM; ++x)
+        a[to][x][s] = *reinterpret_cast<const half8*>(fa + bo + x * 4096 + fo[2 * s + q]);
+#pragma unroll
+      for (int x = 0; x < WN; ++x)
+        b[to][x][s] = *reinterpret_cast<const half8*>(fb + bo + x * 4096 + fo[2 * s + q]);
+    }
+  };
+  wait_loads<LOADS * (NS - 1)>();
+  lds_barrier();
+  read(0, 0, 0);
+  int buf = 0, next = 1 % NS;
+  for (int j = 0; j < steps; ++j) {
+#pragma unroll
     for (int q = 0; q < QN; ++q) {
-      half8 a[WM][NP], b[WN][NP];
+      const int f = q & 1;
+      if (q + 1 < QN) {
+        read(f ^ 1, buf, q + 1);
+      } else {
+        // The last depth of step j: its buffer has been read by this wave, and
+        // behind the barrier by all, so it takes step j + NS; step j + 1 has
+        // arrived when at most NS - 2 steps' loads are out.  Its first
+        // fragments are read while the matrix cores still work on step j.
+        wait_loads<LOADS * (NS - 2)>();
+        lds_barrier();
+        const int js = min(j + NS, steps - 1);   // past the end: the last step again, never used
 #pragma unroll
-      for (int s = 0; s < NP; ++s) {
-#pragma unroll
-        for (int x = 0; x < WM; ++x)
-          a[x][s] = *reinterpret_cast<const half8*>(fa + bo + x * 4096 + fo[2 * s + q]);
-#pragma unroll
-        for (int x = 0; x < WN; ++x)
-          b[x][s] = *reinterpret_cast<const half8*>(fb + bo + x * 4096 + fo[2 * s + q]);
+        for (int i = 0; i < LOADS; ++i) load(buf, js, i);
+        read(f ^ 1, next, 0);
       }
       if constexpr (NP == 2) {
 #pragma unroll
         for (int x = 0; x < WM; ++x)
 #pragma unroll
           for (int y = 0; y < WN; ++y)
-            acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[x][0], b[y][1], acc[x][y], 0, 0, 0);
+            acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[f][x][0], b[f][y][1], acc[x][y], 0, 0, 0);
 #pragma unroll
         for (int x = 0; x < WM; ++x)
 #pragma unroll
           for (int y = 0; y < WN; ++y)
-            acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[x][1], b[y][0], acc[x][y], 0, 0, 0);
+            acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[f][x][1], b[f][y][0], acc[x][y], 0, 0, 0);
       }
 #pragma unroll
       for (int x = 0; x < WM; ++x)
 #pragma unroll
         for (int y = 0; y < WN; ++y)
-          acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[x][0], b[y][0], acc[x][y], 0, 0, 0);
+          acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[f][x][0], b[f][y][0], acc[x][y], 0, 0, 0);
+#pragma unroll
+      for (int m = 0; m < WM * WN * (NP == 2 ? 3 : 1); ++m) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);   // an MFMA
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);   // an LDS read
+      }
+      __builtin_amdgcn_sched_barrier(0);
     }
-    buf = buf + 1 == NS ? 0 : buf + 1;
-    free = free + 1 == NS ? 0 : free + 1;
+    buf = next;
+    next = next + 1 == NS ? 0 : next + 1;
   }
   wait_loads<0>();   // nothing may still be on its way to LDS when the workgroup ends
   if (u >= 0) {   // a slice: its sums, 32 x 32 blocks in accumulator order
