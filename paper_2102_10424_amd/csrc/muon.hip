@@ -33,7 +33,7 @@ constexpr float kS = 4096.f, kInvS = 1.f / 4096.f;
 constexpr int kNormBlocks = 256;
 
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
-typedef _Float16 half4 __attribute__((ext_vector_type(4)));
+typedef float floatx2 __attribute__((ext_vector_type(2)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
@@ -165,37 +165,41 @@ struct Epi {
   int64_t si, sj, group;  // kLast: element (i, j) at i * si + j * sj
   float keep, eta;
   int o_half;
+  int vec;                // kLast: eight consecutive elements are 16-byte aligned
 };
 
-// Four values of consecutive rows i..i+3 of column j, and back as values i..i+3
-// of row j (i a multiple of 4).
+// Eight consecutive values j..j+7 of row i (j a multiple of 8).
 template <int NP>
-__device__ __forceinline__ void put4(const Mat& a, int64_t g, int64_t j, int64_t i, const float (&v)[4]) {
-  half4 h[NP];
+__device__ __forceinline__ void put8(const Mat& a, int64_t g, int64_t i, int64_t j, const float (&v)[8]) {
+  half8 h[NP];
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
+  for (int q = 0; q < 8; ++q) {
     _Float16 s[NP];
     parts_of<NP>(v[q], s);
 #pragma unroll
     for (int x = 0; x < NP; ++x) h[x][q] = s[x];
   }
 #pragma unroll
-  for (int x = 0; x < NP; ++x) *reinterpret_cast<half4*>(a.p + g * a.group + at<NP>(a, j, i, x)) = h[x];
+  for (int x = 0; x < NP; ++x) *reinterpret_cast<half8*>(a.p + g * a.group + at<NP>(a, i, j, x)) = h[x];
 }
 
 template <int NP>
-__device__ __forceinline__ void put1(const Mat& a, int64_t g, int64_t i, int64_t j, float v) {
-  _Float16 s[NP];
-  parts_of<NP>(v, s);
+__device__ __forceinline__ void get8(const Mat& a, int64_t g, int64_t i, int64_t j, float (&v)[8]) {
+  half8 h[NP];
 #pragma unroll
-  for (int x = 0; x < NP; ++x) a.p[g * a.group + at<NP>(a, i, j, x)] = s[x];
+  for (int x = 0; x < NP; ++x) h[x] = *reinterpret_cast<const half8*>(a.p + g * a.group + at<NP>(a, i, j, x));
+#pragma unroll
+  for (int q = 0; q < 8; ++q) {
+    v[q] = static_cast<float>(h[0][q]);
+    if constexpr (NP == 2) v[q] += static_cast<float>(h[1][q]);
+  }
 }
 
-template <int NP>
-__device__ __forceinline__ float get1(const Mat& a, int64_t g, int64_t i, int64_t j) {
-  float v = static_cast<float>(a.p[g * a.group + at<NP>(a, i, j, 0)]);
-  if constexpr (NP == 2) v += static_cast<float>(a.p[g * a.group + at<NP>(a, i, j, 1)]);
-  return v;
+// Orders a wave's LDS writes before its later reads.
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
 }
 
 // Workgroup barrier that orders LDS only.
@@ -249,37 +253,100 @@ __device__ __forceinline__ void tile_of(const Sched& S, int64_t id, int64_t& g, 
   }
 }
 
-// One 32 x 32 block at (row, col) of group g's result.  Accumulator register r
-// of lane l: row 8 (r / 4) + 4 (l / 32) + r mod 4, column l mod 32.
-template <int NP, int MODE>
-__device__ __forceinline__ void finish_block(const floatx16& acc, const Epi& E, int64_t g, int row, int col,
-                                             int lane, bool off_diagonal) {
-  const int64_t j = col + (lane & 31);
+// The weights' step, or the factor, for eight consecutive elements from e on,
+// the first `left` of them in the matrix.
+__device__ __forceinline__ void last8(const Epi& E, int64_t e, int left, const float (&v)[8]) {
+  if (left <= 0) return;
+  if (E.vec && left >= 8) {
+    if (!E.W && E.o_half) {
+      half8 h;
 #pragma unroll
-  for (int r4 = 0; r4 < 4; ++r4) {
-    const int64_t i0 = row + 8 * r4 + 4 * (lane >> 5);
-    float v[4];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      v[q] = acc[4 * r4 + q] * kInvS;   // the product times S
-      if constexpr (MODE != kGram) v[q] = fmaf(E.alpha, get1<NP>(E.add, g, i0 + q, j), E.beta * v[q]);
+      for (int q = 0; q < 8; ++q) h[q] = static_cast<_Float16>(v[q] * kInvS);
+      *reinterpret_cast<half8*>(static_cast<_Float16*>(E.O) + e) = h;
+      return;
     }
-    if constexpr (MODE == kLast) {
+#pragma unroll
+    for (int h = 0; h < 8; h += 4) {
+      floatx4* p = reinterpret_cast<floatx4*>((E.W ? E.W : static_cast<float*>(E.O)) + e + h);
+      floatx4 w;
+      if (E.W) w = *p;
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const int64_t i = i0 + q;
-        if (i >= E.m || j >= E.n) continue;
-        const int64_t e = g * E.group + i * E.si + j * E.sj;
-        const float o = v[q] * kInvS;
-        if (E.W) E.W[e] = fmaf(-E.eta, o, E.keep * E.W[e]);
-        else if (E.o_half) static_cast<_Float16*>(E.O)[e] = static_cast<_Float16>(o);
-        else static_cast<float*>(E.O)[e] = o;
+        const float o = v[h + q] * kInvS;
+        w[q] = E.W ? fmaf(-E.eta, o, E.keep * w[q]) : o;
       }
-    } else {
+      *p = w;
+    }
+    return;
+  }
 #pragma unroll
-      for (int q = 0; q < 4; ++q) put1<NP>(E.out, g, i0 + q, j, v[q]);
-      if constexpr (MODE == kStep) put4<NP>(E.outT, g, j, i0, v);
-      else if (off_diagonal) put4<NP>(E.out, g, j, i0, v);
+  for (int q = 0; q < 8; ++q) {
+    if (q >= left) break;
+    const float o = v[q] * kInvS;
+    if (E.W) E.W[e + q] = fmaf(-E.eta, o, E.keep * E.W[e + q]);
+    else if (E.o_half) static_cast<_Float16*>(E.O)[e + q] = static_cast<_Float16>(o);
+    else static_cast<float*>(E.O)[e + q] = o;
+  }
+}
+
+// One 32 x 32 block at (row, col) of group g's result.  Accumulator register r
+// of lane l: row 8 (r / 4) + 4 (l / 32) + r mod 4, column l mod 32.  The block
+// goes through the wave's own LDS (32 rows of 34 floats), so that memory sees
+// 16 bytes per lane both for the rows and for the columns of the result:
+// element by element, the loads and stores of a 256 x 256 tile kept the load
+// path busy for 40 us.
+constexpr int kScratch = 32 * 34;
+template <int NP, int MODE>
+__device__ __forceinline__ void finish_block(const floatx16& acc, const Epi& E, int64_t g, int row, int col,
+                                             int lane, bool off_diagonal, float* sc) {
+  wave_sync();   // the last block's values are read
+#pragma unroll
+  for (int r = 0; r < 16; ++r)   // the product times S
+    sc[(8 * (r >> 2) + 4 * (lane >> 5) + (r & 3)) * 34 + (lane & 31)] = acc[r] * kInvS;
+  wave_sync();
+  const bool rows = MODE != kLast || E.sj == 1;
+  const bool cols = MODE == kStep || (MODE == kLast ? E.sj != 1 : off_diagonal);
+  const int p = 8 * (lane & 3);
+#pragma unroll
+  for (int it = 0; it < 2; ++it) {
+    const int i = it * 16 + (lane >> 2);
+    float v[8];
+#pragma unroll
+    for (int q = 0; q < 8; q += 2) {
+      const floatx2 x = *reinterpret_cast<const floatx2*>(sc + i * 34 + p + q);
+      v[q] = x[0];
+      v[q + 1] = x[1];
+    }
+    if constexpr (MODE != kGram) {
+      float o[8];
+      get8<NP>(E.add, g, row + i, col + p, o);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) v[q] = fmaf(E.alpha, o[q], E.beta * v[q]);
+      if (cols) {
+#pragma unroll
+        for (int q = 0; q < 8; q += 2) *reinterpret_cast<floatx2*>(sc + i * 34 + p + q) = floatx2{v[q], v[q + 1]};
+      }
+    }
+    if constexpr (MODE == kLast) {
+      if (rows && row + i < E.m)
+        last8(E, g * E.group + (row + i) * E.si + col + p, static_cast<int>(E.n) - col - p, v);
+    } else {
+      put8<NP>(E.out, g, row + i, col + p, v);
+    }
+  }
+  if (!cols) return;
+  wave_sync();
+#pragma unroll
+  for (int it = 0; it < 2; ++it) {
+    const int j = it * 16 + (lane >> 2);
+    float v[8];
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[q] = sc[(p + q) * 34 + j];
+    if constexpr (MODE == kLast) {
+      if (col + j < E.n)
+        last8(E, g * E.group + (col + j) * E.sj + row + p, static_cast<int>(E.m) - row - p, v);
+    } else {
+      put8<NP>(MODE == kStep ? E.outT : E.out, g, col + j, row + p, v);
     }
   }
 }
@@ -424,17 +491,21 @@ __global__ __launch_bounds__(64 * NWM * NWN, 2) void product_kernel(Sched S, Mat
         }
     return;
   }
+  lds_barrier();   // every wave is done with its fragments: their LDS serves finish_block
+  float* const sc = reinterpret_cast<float*>(&lds[0][0]) + wave * kScratch;
+  static_assert(sizeof(lds) >= NWM * NWN * kScratch * 4, "scratch of all waves");
 #pragma unroll
   for (int x = 0; x < WM; ++x)
 #pragma unroll
     for (int y = 0; y < WN; ++y)
       finish_block<NP, MODE>(acc[x][y], E, g, ti * BM + (wm * WM + x) * 32, tj * BN + (wn * WN + y) * 32,
-                             lane, ti != tj);
+                             lane, ti != tj, sc);
 }
 
 // Tiles that were cut in K: a wave per 32 x 32 block adds the slices in order.
 template <int NP, int MODE>
 __global__ __launch_bounds__(kBlock) void join_kernel(Sched S, int tile, const float* __restrict__ part, Epi E) {
+  __shared__ __attribute__((aligned(16))) float scratch[kBlock / 64][kScratch];
   const int lane = threadIdx.x & 63, bt = tile / 32;
   const int64_t w = (static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x) >> 6;
   const int blk = static_cast<int>(w % (bt * bt));
@@ -453,7 +524,8 @@ __global__ __launch_bounds__(kBlock) void join_kernel(Sched S, int tile, const f
       for (int q = 0; q < 4; ++q) acc[4 * r4 + q] += v[q];
     }
   }
-  finish_block<NP, MODE>(acc, E, g, ti * tile + (blk / bt) * 32, tj * tile + (blk % bt) * 32, lane, ti != tj);
+  finish_block<NP, MODE>(acc, E, g, ti * tile + (blk / bt) * 32, tj * tile + (blk % bt) * 32, lane, ti != tj,
+                         scratch[threadIdx.x >> 6]);
 }
 
 size_t up256(size_t x) { return (x + 255) & ~size_t(255); }
@@ -616,6 +688,8 @@ gist_status run(hipStream_t st, const gist_muon_desc* D, const float* G, void* O
       e.keep = u.keep;
       e.eta = u.eta;
       e.o_half = NP == 1;
+      // every group and row begins at a multiple of eight elements
+      e.vec = D->cols % 8 == 0 && reinterpret_cast<uintptr_t>(W ? static_cast<void*>(W) : O) % 16 == 0;
       product<NP, kLast>(st, p, p.mp, p.np, p.mp, B, T[cur], e, parts);
     }
   }
