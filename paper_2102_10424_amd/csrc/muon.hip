@@ -30,7 +30,7 @@ namespace {
 
 constexpr int kBlock = 256;
 constexpr float kS = 4096.f, kInvS = 1.f / 4096.f;
-constexpr int kNormBlocks = 256;
+constexpr int kNormBlocks = 512;
 
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef float floatx2 __attribute__((ext_vector_type(2)));
@@ -49,33 +49,57 @@ __device__ __forceinline__ float direction(const Update& u, float g, float m) {
   return u.nesterov ? fmaf(u.momentum, m, u.omu * g) : m;
 }
 
+// Sum over the workgroup, in a fixed order; every thread has it.
+__device__ __forceinline__ double block_sum(double s, double* sh) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = s;
+  __syncthreads();
+  double r = 0.0;
+  for (int w = 0; w < kBlock / 64; ++w) r += sh[w];
+  return r;
+}
+
 // The new momentum, and per block the sum of squares of the direction, in
-// double: part[group * kNormBlocks + block].
-template <bool UPDATE>
+// double: part[group * kNormBlocks + block].  V floats a load: 4 where the
+// groups' arrays are aligned.  Bound by memory: 71 us for three passes over two
+// 4,096 x 4,096 matrices (5.7 TB/s), 159 with single floats and half the blocks.
+template <bool UPDATE, int V>
 __global__ __launch_bounds__(kBlock) void norm_kernel(int64_t count, const float* __restrict__ G,
                                                       float* __restrict__ M, Update u,
                                                       double* __restrict__ part) {
-  __shared__ double sh[kBlock];
+  __shared__ double sh[kBlock / 64];
   const int64_t off = blockIdx.y * count;
+  constexpr int kUnroll = 4;
+  const int64_t stride = static_cast<int64_t>(gridDim.x) * kBlock * V;
   double s = 0.0;
-  for (int64_t e = blockIdx.x * static_cast<int64_t>(kBlock) + threadIdx.x; e < count;
-       e += static_cast<int64_t>(gridDim.x) * kBlock) {
-    float v = G[off + e];
-    if constexpr (UPDATE) {
-      const float old = u.fresh ? 0.f : M[off + e];
-      const float m = fmaf(u.momentum, old, u.omu * v);
-      M[off + e] = m;
-      v = direction(u, v, m);
+  for (int64_t e0 = (blockIdx.x * static_cast<int64_t>(kBlock) + threadIdx.x) * V; e0 < count; e0 += kUnroll * stride) {
+    float v[kUnroll][V], m[kUnroll][V];
+#pragma unroll
+    for (int i = 0; i < kUnroll; ++i) {
+      const int64_t e = e0 + i * stride;
+      if (e < count) {
+        load_vec<GIST_STORE_F32, V>(G, off + e, v[i]);
+        if (UPDATE && !u.fresh) load_vec<GIST_STORE_F32, V>(M, off + e, m[i]);
+      }
     }
-    s += static_cast<double>(v) * v;
+#pragma unroll
+    for (int i = 0; i < kUnroll; ++i) {
+      const int64_t e = e0 + i * stride;
+      if (e >= count) break;
+#pragma unroll
+      for (int q = 0; q < V; ++q) {
+        if constexpr (UPDATE) {
+          m[i][q] = fmaf(u.momentum, u.fresh ? 0.f : m[i][q], u.omu * v[i][q]);
+          v[i][q] = direction(u, v[i][q], m[i][q]);
+        }
+        s += static_cast<double>(v[i][q]) * v[i][q];
+      }
+      if constexpr (UPDATE) store_vec<V>(M + off + e, m[i]);
+    }
   }
-  sh[threadIdx.x] = s;
-  __syncthreads();
-  for (int o = kBlock / 2; o > 0; o >>= 1) {
-    if (threadIdx.x < o) sh[threadIdx.x] += sh[threadIdx.x + o];
-    __syncthreads();
-  }
-  if (threadIdx.x == 0) part[blockIdx.y * kNormBlocks + blockIdx.x] = sh[0];
+  s = block_sum(s, sh);
+  if (threadIdx.x == 0) part[blockIdx.y * kNormBlocks + blockIdx.x] = s;
 }
 
 template <int NP>
@@ -96,77 +120,6 @@ __device__ __forceinline__ int64_t at(const Mat& a, int64_t i, int64_t j, int p)
   if constexpr (NP == 1) return i * a.ld + j;
   return 2 * i * a.ld + (j >> 5) * 64 + p * 32 + (j & 31);
 }
-
-// U / norm, split, as it stands (D) and transposed (T); 64 x 64 tiles over the
-// padded sides.
-template <bool UPDATE, int NP>
-__global__ __launch_bounds__(kBlock) void split_kernel(int64_t rows, int64_t cols, int nparts,
-                                                       const float* __restrict__ G,
-                                                       const float* __restrict__ M, Update u,
-                                                       const double* __restrict__ part, float eps,
-                                                       Mat D, Mat T) {
-  __shared__ double red[kBlock];
-  __shared__ float tile[64][65];
-  const int t = threadIdx.x;
-  const int64_t g = blockIdx.z, off = g * rows * cols;
-  red[t] = t < nparts ? part[g * kNormBlocks + t] : 0.0;
-  __syncthreads();
-  for (int o = kBlock / 2; o > 0; o >>= 1) {
-    if (t < o) red[t] += red[t + o];
-    __syncthreads();
-  }
-  // a norm past fp32 (entries beyond 10^30): both scaled down
-  double norm = sqrt(red[0]);
-  const bool huge = norm > 1e30;
-  const float pre = huge ? 0x1p-64f : 1.f;
-  if (huge) norm *= 0x1p-64;
-  const float div = norm < static_cast<double>(eps) ? eps : static_cast<float>(norm);   // NaN stays
-  const int64_t r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;
-  _Float16* const d = D.p + g * D.group;
-  _Float16* const tr = T.p + g * T.group;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const int r = i * 4 + (t >> 6), c = t & 63;
-    float v = 0.f;
-    if (r0 + r < rows && c0 + c < cols) {
-      const int64_t e = off + (r0 + r) * cols + c0 + c;
-      v = G[e];
-      if constexpr (UPDATE) v = direction(u, v, M[e]);
-      v = kS * (v * pre / div);
-    }
-    tile[r][c] = v;
-    _Float16 p[NP];
-    parts_of<NP>(v, p);
-#pragma unroll
-    for (int q = 0; q < NP; ++q) d[at<NP>(D, r0 + r, c0 + c, q)] = p[q];
-  }
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const int c = i * 4 + (t >> 6), r = t & 63;
-    _Float16 p[NP];
-    parts_of<NP>(tile[r][c], p);
-#pragma unroll
-    for (int q = 0; q < NP; ++q) tr[at<NP>(T, c0 + c, r0 + r, q)] = p[q];
-  }
-}
-
-// ---- products ------------------------------------------------------------------------
-
-enum { kGram = 0, kPoly = 1, kStep = 2, kLast = 3 };
-
-struct Epi {
-  Mat out, outT;          // kGram, kPoly: out; kStep: both
-  Mat add;                // kPoly: A; kStep, kLast: X
-  float alpha, beta;      // out = alpha * add + beta * product
-  float* W;               // kLast: weights, or
-  void* O;                // the factor itself
-  int64_t m, n;           // kLast: sizes without padding
-  int64_t si, sj, group;  // kLast: element (i, j) at i * si + j * sj
-  float keep, eta;
-  int o_half;
-  int vec;                // kLast: eight consecutive elements are 16-byte aligned
-};
 
 // Eight consecutive values j..j+7 of row i (j a multiple of 8).
 template <int NP>
@@ -201,6 +154,102 @@ __device__ __forceinline__ void wave_sync() {
   __builtin_amdgcn_wave_barrier();
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
 }
+
+// Divisor of a group's matrix, from its partial sums: max(norm, eps), and a
+// factor for both where the norm would not fit fp32.
+struct Divisor {
+  float pre, div;
+};
+__device__ __forceinline__ Divisor divisor(const double* __restrict__ part, int64_t g, int nparts, float eps,
+                                           double* sh) {
+  double s = 0.0;
+  for (int i = threadIdx.x; i < nparts; i += kBlock) s += part[g * kNormBlocks + i];
+  double norm = sqrt(block_sum(s, sh));
+  Divisor d{1.f, 0.f};
+  if (norm > 1e30) {
+    d.pre = 0x1p-64f;
+    norm *= 0x1p-64;
+  }
+  d.div = norm < static_cast<double>(eps) ? eps : static_cast<float>(norm);   // NaN stays
+  return d;
+}
+
+// U / norm, split, as it stands (D) and transposed (T); 64 x 64 tiles over the
+// padded sides, 16 values of a row per thread.
+template <bool UPDATE, int NP, bool VEC>
+__global__ __launch_bounds__(kBlock) void split_kernel(int64_t rows, int64_t cols, int nparts,
+                                                       const float* __restrict__ G,
+                                                       const float* __restrict__ M, Update u,
+                                                       const double* __restrict__ part, float eps,
+                                                       Mat D, Mat T) {
+  __shared__ double red[kBlock / 64];
+  __shared__ __attribute__((aligned(8))) float tile[64][66];   // 66: column reads spread over the banks
+  const int t = threadIdx.x;
+  const int64_t g = blockIdx.z, off = g * rows * cols;
+  const int64_t r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;
+  const int r = t >> 2, c = (t & 3) * 16;
+  float v[16];
+#pragma unroll
+  for (int q = 0; q < 16; ++q) v[q] = 0.f;
+  if (r0 + r < rows) {
+    const int64_t e = off + (r0 + r) * cols + c0 + c;
+#pragma unroll
+    for (int q = 0; q < 16; q += 4) {
+      float x[4] = {}, m[4] = {};
+      if constexpr (VEC) {   // cols is a multiple of 4
+        if (c0 + c + q < cols) {
+          load_vec<GIST_STORE_F32, 4>(G, e + q, x);
+          if (UPDATE) load_vec<GIST_STORE_F32, 4>(M, e + q, m);
+        }
+      } else {
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+          if (c0 + c + q + y < cols) {
+            x[y] = G[e + q + y];
+            if (UPDATE) m[y] = M[e + q + y];
+          }
+      }
+#pragma unroll
+      for (int y = 0; y < 4; ++y) v[q + y] = UPDATE ? direction(u, x[y], m[y]) : x[y];
+    }
+  }
+  const Divisor d = divisor(part, g, nparts, eps, red);
+#pragma unroll
+  for (int h = 0; h < 16; h += 8) {
+    float x[8];
+#pragma unroll
+    for (int q = 0; q < 8; ++q) x[q] = kS * (v[h + q] * d.pre / d.div);
+    put8<NP>(D, g, r0 + r, c0 + c + h, x);
+#pragma unroll
+    for (int q = 0; q < 8; q += 2) *reinterpret_cast<floatx2*>(&tile[r][c + h + q]) = floatx2{x[q], x[q + 1]};
+  }
+  __syncthreads();
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int j = (t >> 3) + 32 * h, p = (t & 7) * 8;   // column j, rows p..p+7
+    float x[8];
+#pragma unroll
+    for (int q = 0; q < 8; ++q) x[q] = tile[p + q][j];
+    put8<NP>(T, g, c0 + j, r0 + p, x);
+  }
+}
+
+// ---- products ------------------------------------------------------------------------
+
+enum { kGram = 0, kPoly = 1, kStep = 2, kLast = 3 };
+
+struct Epi {
+  Mat out, outT;          // kGram, kPoly: out; kStep: both
+  Mat add;                // kPoly: A; kStep, kLast: X
+  float alpha, beta;      // out = alpha * add + beta * product
+  float* W;               // kLast: weights, or
+  void* O;                // the factor itself
+  int64_t m, n;           // kLast: sizes without padding
+  int64_t si, sj, group;  // kLast: element (i, j) at i * si + j * sj
+  float keep, eta;
+  int o_half;
+  int vec;                // kLast: eight consecutive elements are 16-byte aligned
+};
 
 // Workgroup barrier that orders LDS only.
 __device__ __forceinline__ void lds_barrier() {
@@ -298,14 +347,15 @@ __device__ __forceinline__ void last8(const Epi& E, int64_t e, int left, const f
 constexpr int kScratch = 32 * 34;
 template <int NP, int MODE>
 __device__ __forceinline__ void finish_block(const floatx16& acc, const Epi& E, int64_t g, int row, int col,
-                                             int lane, bool off_diagonal, float* sc) {
+                                             int lane, float* sc) {
+  if ((MODE == kGram || MODE == kPoly) && row < col) return;   // the mirror image of another block
   wave_sync();   // the last block's values are read
 #pragma unroll
   for (int r = 0; r < 16; ++r)   // the product times S
     sc[(8 * (r >> 2) + 4 * (lane >> 5) + (r & 3)) * 34 + (lane & 31)] = acc[r] * kInvS;
   wave_sync();
   const bool rows = MODE != kLast || E.sj == 1;
-  const bool cols = MODE == kStep || (MODE == kLast ? E.sj != 1 : off_diagonal);
+  const bool cols = MODE == kStep || (MODE == kLast ? E.sj != 1 : row != col);
   const int p = 8 * (lane & 3);
 #pragma unroll
   for (int it = 0; it < 2; ++it) {
@@ -499,24 +549,25 @@ __global__ __launch_bounds__(64 * NWM * NWN, 2) void product_kernel(Sched S, Mat
 #pragma unroll
     for (int y = 0; y < WN; ++y)
       finish_block<NP, MODE>(acc[x][y], E, g, ti * BM + (wm * WM + x) * 32, tj * BN + (wn * WN + y) * 32,
-                             lane, ti != tj, sc);
+                             lane, sc);
 }
 
 // Tiles that were cut in K: a wave per 32 x 32 block adds the slices in order.
-template <int NP, int MODE>
-__global__ __launch_bounds__(kBlock) void join_kernel(Sched S, int tile, const float* __restrict__ part, Epi E) {
+template <int NP, int MODE, int TILE>
+__global__ __launch_bounds__(kBlock) void join_kernel(Sched S, const float* __restrict__ part, Epi E) {
   __shared__ __attribute__((aligned(16))) float scratch[kBlock / 64][kScratch];
-  const int lane = threadIdx.x & 63, bt = tile / 32;
+  constexpr int NB = TILE / 32, BLOCKS = NB * NB;
+  const int lane = threadIdx.x & 63;
   const int64_t w = (static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x) >> 6;
-  const int blk = static_cast<int>(w % (bt * bt));
-  const int64_t rt = w / (bt * bt);
+  const int blk = static_cast<int>(w % BLOCKS);
+  const int64_t rt = w / BLOCKS;
   if (rt >= S.ragged) return;
   int64_t g;
   int ti, tj;
   tile_of<MODE>(S, S.whole + rt, g, ti, tj);
   floatx16 acc = {};
   for (int s = 0; s < S.slices; ++s) {
-    const floatx4* d = reinterpret_cast<const floatx4*>(part + (s * S.ragged + rt) * tile * tile) + blk * 256 + lane;
+    const floatx4* d = reinterpret_cast<const floatx4*>(part + (s * S.ragged + rt) * (TILE * TILE)) + blk * 256 + lane;
 #pragma unroll
     for (int r4 = 0; r4 < 4; ++r4) {
       const floatx4 v = d[r4 * 64];
@@ -524,7 +575,7 @@ __global__ __launch_bounds__(kBlock) void join_kernel(Sched S, int tile, const f
       for (int q = 0; q < 4; ++q) acc[4 * r4 + q] += v[q];
     }
   }
-  finish_block<NP, MODE>(acc, E, g, ti * tile + (blk / bt) * 32, tj * tile + (blk % bt) * 32, lane, ti != tj,
+  finish_block<NP, MODE>(acc, E, g, ti * TILE + (blk / NB) * 32, tj * TILE + (blk % NB) * 32, lane,
                          scratch[threadIdx.x >> 6]);
 }
 
@@ -540,42 +591,59 @@ struct Plan {
   size_t total() const { return norm + 4 * x + 2 * a + part; }
 };
 
+// The tiles: side, workgroups the card holds at once, and what a round of them
+// was measured to take: `base` + `fill` (epilogue, of a full round) + `step` per
+// step of K, at least `least`; microseconds, for one and two parts per value.
+// 256: 8 waves of 128 x 64, 128: 4 of 64 x 64, 64: 4 of 32 x 32.  (8 waves of
+// 64 x 64 on 256 x 128 with three buffers were never the best.)  Steps on the
+// 1,024 to 4,096-wide products: 256 x 256 tiles are best from about 2,048 on,
+// 64 x 64 up to about 512: 8 matrices of 1,024 with fp16 operands take 519, 387
+// and 559 us, 2 of them 411, 304 and 218, one of 4,096 1,782, 1,843 and 2,100.
+struct Tile {
+  int side, slots;
+  double base, fill[2], step[2], least[2];
+};
+constexpr Tile kTiles[] = {{256, 256, 10, {27, 36}, {1.53, 2.37}, {0.95, 1.4}},
+                           {128, 512, 6, {4, 12}, {1.12, 1.3}, {0.6, 0.9}},
+                           {64, 512, 3, {1, 1}, {0.65, 0.65}, {0.45, 0.46}}};
+
 struct Choice {
-  int tile;
+  int tile = -1;   // of kTiles
   Sched s;
   size_t part_bytes() const {
-    return s.ragged ? up256(static_cast<size_t>(s.ragged) * s.slices * tile * tile * 4) : 0;
+    const size_t side = kTiles[tile].side;
+    return s.ragged ? up256(static_cast<size_t>(s.ragged) * s.slices * side * side * 4) : 0;
   }
 };
 
-// Tile and K cuts of one product, by an estimate in microseconds: a round of
-// `slots` workgroups takes `step` per step of K, and a join its launch and its
-// traffic.
+// Tile and K cuts of one product, the quickest by these figures; a join takes 5 us
+// and its parts' traffic twice.
 Choice choose(const Plan& p, int64_t M, int64_t N, int64_t K, bool sym) {
-  Choice best{};
+  Choice best;
   double best_us = 0;
-  for (int tile : {256, 128, 64}) {
-    if (tile > p.pad) continue;
-    const int64_t tm = M / tile, tn = N / tile;
+  for (int i = 0; i < 3; ++i) {
+    const Tile& t = kTiles[i];
+    if (t.side > p.pad) continue;
+    const int64_t tm = M / t.side, tn = N / t.side;
     Sched s{};
     s.tiles_m = static_cast<int>(tm);
     s.tiles_n = static_cast<int>(tn);
     s.tiles = static_cast<int>(sym ? tm * (tm + 1) / 2 : tm * tn);
     s.steps = static_cast<int>(K * p.parts / 64);
-    const int64_t all = s.tiles * p.G;
-    const int slots = 256 * (tile == 256 ? 1 : 2);
-    const double step = (p.parts == 2 ? 1.0 : 0.75) * (tile == 256 ? 3.0 : tile == 128 ? 1.7 : 0.6);
-    const int64_t full = all / slots * slots, left = all - full;
+    const int64_t all = s.tiles * p.G, rounds = all / t.slots, left = all - rounds * t.slots;
+    const double step = t.step[p.parts - 1], least = t.least[p.parts - 1], fill = t.fill[p.parts - 1];
     for (int slices : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
-      if (slices > 1 && (left == 0 || s.steps / slices < 4 || left * slices > slots)) continue;
+      if (slices > 1 && (left == 0 || s.steps / slices < 4 || left * slices > t.slots)) continue;
       s.len = (s.steps + slices - 1) / slices;
       s.slices = (s.steps + s.len - 1) / s.len;
-      s.whole = slices == 1 ? all : full;
+      s.whole = slices == 1 ? all : all - left;
       s.ragged = all - s.whole;
-      double us = 3.0 + (full / slots) * (s.steps * step) + (left ? s.len * step : 0.0);
-      if (slices > 1) us += 5.0 + left * slices * (tile * tile * 8.0) / 4e6;
-      if (best.tile == 0 || us < best_us) {
-        best.tile = tile;
+      const double part = static_cast<double>(left * s.slices) / t.slots;   // of the card, in the last round
+      double us = rounds * (t.base + fill + s.steps * step);
+      if (left) us += t.base + fill * part + s.len * std::max(least, step * part);
+      if (slices > 1) us += 5.0 + 2 * left * s.slices * (t.side * t.side * 4.0) / 8e6;
+      if (best.tile < 0 || us < best_us) {
+        best.tile = i;
         best.s = s;
         best_us = us;
       }
@@ -591,7 +659,12 @@ Plan plan(const gist_muon_desc* D) {
   p.m = std::min(D->rows, D->cols);
   p.n = std::max(D->rows, D->cols);
   p.parts = D->dtype == GIST_DTYPE_F32 ? 2 : 1;
-  p.pad = p.m > 512 ? 256 : p.m > 128 ? 128 : 64;
+  // Larger padding allows larger tiles; it is taken where there are a few of
+  // them and it adds at most 15% to the matrix.
+  for (p.pad = 256; p.pad > 64; p.pad /= 2) {
+    const int64_t a = (p.m + p.pad - 1) / p.pad * p.pad, b = (p.n + p.pad - 1) / p.pad * p.pad;
+    if (p.m >= 4 * p.pad && 100 * a * b <= 115 * p.m * p.n) break;
+  }
   p.mp = (p.m + p.pad - 1) / p.pad * p.pad;
   p.np = (p.n + p.pad - 1) / p.pad * p.pad;
   p.norm = up256(static_cast<size_t>(p.G) * kNormBlocks * sizeof(double));
@@ -613,14 +686,17 @@ void product(hipStream_t st, const Plan& p, int64_t M, int64_t N, int64_t K, con
   {
     ProfScope ps(st, names[MODE], (kSym ? 1.0 : 2.0) * p.G * M * N * K, 2.0 * NP * p.G * (M * K + N * K + M * N));
     const dim3 g(static_cast<unsigned>(c.s.whole + c.s.ragged * c.s.slices));
-    if (c.tile == 256) product_kernel<NP, MODE, 4, 2, 2, 4, 2><<<g, 512, 0, st>>>(c.s, P, Q, E, part);
-    else if (c.tile == 128) product_kernel<NP, MODE, 2, 2, 2, 2, 2><<<g, 256, 0, st>>>(c.s, P, Q, E, part);
+    if (c.tile == 0) product_kernel<NP, MODE, 4, 2, 2, 4, 2><<<g, 512, 0, st>>>(c.s, P, Q, E, part);
+    else if (c.tile == 1) product_kernel<NP, MODE, 2, 2, 2, 2, 2><<<g, 256, 0, st>>>(c.s, P, Q, E, part);
     else product_kernel<NP, MODE, 1, 1, 2, 2, 4><<<g, 256, 0, st>>>(c.s, P, Q, E, part);
   }
   if (c.s.ragged) {
     ProfScope ps(st, "muon_join", 0.0, static_cast<double>(c.part_bytes()));
-    const int64_t waves = c.s.ragged * (c.tile / 32) * (c.tile / 32);
-    join_kernel<NP, MODE><<<dim3(static_cast<unsigned>((waves + 3) / 4)), kBlock, 0, st>>>(c.s, c.tile, part, E);
+    const int nb = kTiles[c.tile].side / 32;
+    const dim3 g(static_cast<unsigned>((c.s.ragged * nb * nb + 3) / 4));
+    if (c.tile == 0) join_kernel<NP, MODE, 256><<<g, kBlock, 0, st>>>(c.s, part, E);
+    else if (c.tile == 1) join_kernel<NP, MODE, 128><<<g, kBlock, 0, st>>>(c.s, part, E);
+    else join_kernel<NP, MODE, 64><<<g, kBlock, 0, st>>>(c.s, part, E);
   }
 }
 
@@ -643,12 +719,16 @@ gist_status run(hipStream_t st, const gist_muon_desc* D, const float* G, void* O
   }
   const Mat A = mat(p.a, p.mp, p.mp), B = mat(p.a, p.mp, p.mp);
   float* parts = reinterpret_cast<float*>(ws);
-  const int nb = static_cast<int>(std::min<int64_t>(kNormBlocks, (count + kBlock - 1) / kBlock));
+  const bool vec = D->cols % 4 == 0 && reinterpret_cast<uintptr_t>(G) % 16 == 0 &&
+                   (!W || reinterpret_cast<uintptr_t>(M) % 16 == 0);
+  const int nb = static_cast<int>(std::min<int64_t>(kNormBlocks, (count + 8 * kBlock - 1) / (8 * kBlock)));
   {
     ProfScope ps(st, "muon_norm", 4.0 * p.G * count, (W ? 12.0 : 4.0) * p.G * count);
     const dim3 g(nb, static_cast<unsigned>(p.G));
-    if (W) norm_kernel<true><<<g, kBlock, 0, st>>>(count, G, M, u, part);
-    else norm_kernel<false><<<g, kBlock, 0, st>>>(count, G, M, u, part);
+    if (W && vec) norm_kernel<true, 4><<<g, kBlock, 0, st>>>(count, G, M, u, part);
+    else if (W) norm_kernel<true, 1><<<g, kBlock, 0, st>>>(count, G, M, u, part);
+    else if (vec) norm_kernel<false, 4><<<g, kBlock, 0, st>>>(count, G, M, u, part);
+    else norm_kernel<false, 1><<<g, kBlock, 0, st>>>(count, G, M, u, part);
   }
   {
     ProfScope ps(st, "muon_split", 0.0, (4.0 * (W ? 2 : 1) + 4.0 * NP) * p.G * count);
@@ -656,8 +736,12 @@ gist_status run(hipStream_t st, const gist_muon_desc* D, const float* G, void* O
     const dim3 g(static_cast<unsigned>(cp / 64), static_cast<unsigned>(rp / 64), static_cast<unsigned>(p.G));
     const Mat& d = p.flip ? T[0] : X[0];
     const Mat& tr = p.flip ? X[0] : T[0];
-    if (W) split_kernel<true, NP><<<g, kBlock, 0, st>>>(D->rows, D->cols, nb, G, M, u, part, D->eps, d, tr);
-    else split_kernel<false, NP><<<g, kBlock, 0, st>>>(D->rows, D->cols, nb, G, M, u, part, D->eps, d, tr);
+#define SPLIT(U, V) split_kernel<U, NP, V><<<g, kBlock, 0, st>>>(D->rows, D->cols, nb, G, M, u, part, D->eps, d, tr)
+    if (W && vec) SPLIT(true, true);
+    else if (W) SPLIT(true, false);
+    else if (vec) SPLIT(false, true);
+    else SPLIT(false, false);
+#undef SPLIT
   }
   int cur = 0;
   for (int k = 0; k < D->steps; ++k) {
