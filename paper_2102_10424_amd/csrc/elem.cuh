@@ -7,11 +7,14 @@
 
 namespace gist {
 
-typedef float fx4 __attribute__((ext_vector_type(4)));
-typedef float fx2 __attribute__((ext_vector_type(2)));
-typedef unsigned short us8 __attribute__((ext_vector_type(8)));
-typedef unsigned short us4 __attribute__((ext_vector_type(4)));
-typedef unsigned short us2 __attribute__((ext_vector_type(2)));
+// Aligned as their elements are: rows of any width and leading dimension are
+// moved 16 bytes at a time (the hardware takes any address for global accesses;
+// only a lane whose bytes cross a line costs more).
+typedef float fx4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef float fx2 __attribute__((ext_vector_type(2), aligned(4)));
+typedef unsigned short us8 __attribute__((ext_vector_type(8), aligned(2)));
+typedef unsigned short us4 __attribute__((ext_vector_type(4), aligned(2)));
+typedef unsigned short us2 __attribute__((ext_vector_type(2), aligned(2)));
 
 // ---- stored elements as floats ------------------------------------------------
 
@@ -109,20 +112,38 @@ __device__ __forceinline__ void store_as(void* base, int64_t e, const float (&x)
   }
 }
 
+// Elements e .. e + V - 1, of which the first `left` are there; the others are `fill`.
+template <int STORE, int V>
+__device__ __forceinline__ void load_some(const void* base, int64_t e, int64_t left, float fill, float (&x)[V]) {
+  if (left >= V) {
+    load_vec<STORE, V>(base, e, x);
+  } else {
+#pragma unroll
+    for (int q = 0; q < V; ++q) {
+      float y[1] = {fill};
+      if (q < left) load_vec<STORE, 1>(base, e + q, y);
+      x[q] = y[0];
+    }
+  }
+}
+
+template <int STORE, int V>
+__device__ __forceinline__ void store_some(void* base, int64_t e, int64_t left, const float (&x)[V]) {
+  if (left >= V) {
+    store_as<STORE, V>(base, e, x);
+  } else {
+#pragma unroll
+    for (int q = 0; q < V; ++q) {
+      const float y[1] = {x[q]};
+      if (q < left) store_as<STORE, 1>(base, e + q, y);
+    }
+  }
+}
+
 inline int ceil_log2(int64_t x) {
   int l = 0;
   while ((int64_t{1} << l) < x) ++l;
   return l;
-}
-
-// Elements per access: as many as divide the width and the leading dimension
-// and leave every row's address aligned to the access.
-inline int vec_of(int most, int64_t width, int64_t ld, const void* p, int elem_bytes) {
-  int v = most;
-  while (v > 1 && (width % v != 0 || ld % v != 0 ||
-                   reinterpret_cast<uintptr_t>(p) % static_cast<uintptr_t>(v * elem_bytes > 16 ? 16 : v * elem_bytes) != 0))
-    v /= 2;
-  return v;
 }
 
 }  // namespace gist

@@ -38,10 +38,10 @@ __global__ __launch_bounds__(kBlock) void lookup_kernel(int n, int64_t V_rows, i
     const int64_t base = id * ldt;
     for (int j = V * lane; j < d; j += step) {
       float x[V] = {};
-      if (in) load_vec<STORE, V>(table, base + j, x);
+      if (in) load_some<STORE, V>(table, base + j, d - j, 0.f, x);
 #pragma unroll
       for (int q = 0; q < V; ++q) x[q] *= scale;
-      store_vec<V>(o + j, x);
+      store_some<GIST_STORE_F32, V>(o, j, d - j, x);
     }
   }
 }
@@ -168,28 +168,135 @@ __global__ __launch_bounds__(kBlock) void scatter_digit_kernel(
   }
 }
 
-// ---- sums over equal ids -----------------------------------------------------------
-
-// A row's finished sum: the dense gradient, or the SGD step on the table.
-template <bool SGD, int V>
-__device__ __forceinline__ void finish(float* p, const float (&acc)[V], float scale, float lr) {
-  float x[V];
-  if constexpr (SGD) {
-    load_vec<GIST_STORE_F32, V>(p, 0, x);
+// Up to kSmall ids: the whole sort in one workgroup, keys and positions in
+// registers and, between two digits, in LDS.  Ids that ascend already (the node
+// map of a cluster mini-batch) are only copied.
+constexpr int kSmallThreads = 1024, kSmallItems = 8, kSmall = kSmallThreads * kSmallItems;
+__global__ __launch_bounds__(kSmallThreads) void small_sort_kernel(int n, int V, const int* __restrict__ ids,
+                                                                   int passes, int* __restrict__ keys,
+                                                                   int* __restrict__ pos) {
+  constexpr int kWaves = kSmallThreads / 64;
+  __shared__ int cnt[kWaves][kBins];
+  __shared__ int lk[kSmall], lp[kSmall];
+  __shared__ int wsum[kBins / 64];
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  const int items = (n + kSmallThreads - 1) / kSmallThreads;   // of 64 keys per wave
+  const int base = wave * items * 64;
+  int key[kSmallItems], ps[kSmallItems];
+  int down = 0;
 #pragma unroll
-    for (int q = 0; q < V; ++q) x[q] = fmaf(-lr, scale * acc[q], x[q]);
-  } else {
-#pragma unroll
-    for (int q = 0; q < V; ++q) x[q] = scale * acc[q];
+  for (int i = 0; i < kSmallItems; ++i) {
+    const int e = base + i * 64 + lane;
+    key[i] = V;
+    ps[i] = e;
+    if (i < items && e < n) {
+      key[i] = key_of(ids[e], V);
+      if (e > 0) down |= key_of(ids[e - 1], V) > key[i];
+    }
   }
-  store_vec<V>(p, x);
+  if (!__syncthreads_or(down)) passes = 0;
+  for (int p = 0; p < passes; ++p) {
+    const int shift = p * kDigit;
+    for (int x = t; x < kWaves * kBins; x += kSmallThreads) (&cnt[0][0])[x] = 0;
+    __syncthreads();
+    int rank[kSmallItems];
+#pragma unroll
+    for (int i = 0; i < kSmallItems; ++i) {
+      if (i >= items) break;
+      const bool in = base + i * 64 + lane < n;
+      const int dg = (key[i] >> shift) & (kBins - 1);
+      unsigned long long m = __ballot(in);
+#pragma unroll
+      for (int b = 0; b < kDigit; ++b) {
+        const unsigned long long s = __ballot((dg >> b) & 1);
+        m &= (dg >> b) & 1 ? s : ~s;
+      }
+      const int before = __popcll(m & ((1ull << lane) - 1));
+      const int had = cnt[wave][dg];
+      rank[i] = had + before;
+      __builtin_amdgcn_wave_barrier();
+      if (in && before == 0) cnt[wave][dg] = had + __popcll(m);
+      __builtin_amdgcn_wave_barrier();
+    }
+    __syncthreads();
+    int total = 0, inc = 0;
+    if (t < kBins) {   // digit t: keys of all waves, then of the digits before it
+      for (int w = 0; w < kWaves; ++w) {
+        const int c = cnt[w][t];
+        cnt[w][t] = total;
+        total += c;
+      }
+      inc = total;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int u = __shfl_up(inc, o, 64);
+        if (lane >= o) inc += u;
+      }
+      if (lane == 63) wsum[wave] = inc;
+    }
+    __syncthreads();
+    if (t < kBins) {
+      int start = inc - total;
+      for (int w = 0; w < wave; ++w) start += wsum[w];
+      for (int w = 0; w < kWaves; ++w) cnt[w][t] += start;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kSmallItems; ++i) {
+      if (i >= items) break;
+      if (base + i * 64 + lane < n) {
+        const int to = cnt[wave][(key[i] >> shift) & (kBins - 1)] + rank[i];
+        lk[to] = key[i];
+        lp[to] = ps[i];
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kSmallItems; ++i) {
+      if (i >= items) break;
+      const int e = base + i * 64 + lane;
+      if (e < n) {
+        key[i] = lk[e];
+        ps[i] = lp[e];
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kSmallItems; ++i) {
+    const int e = base + i * 64 + lane;
+    if (i < items && e < n) {
+      keys[e] = key[i];
+      pos[e] = ps[i];
+    }
+  }
 }
 
-// Chunks of `len` sorted positions, one group of threads each; blockIdx.y:
-// slab of columns.  part[2 c] is the sum of chunk c's first id where that id
-// began in an earlier chunk, part[2 c + 1] that of its last id where it
-// began in this chunk and goes on in the next.
-template <bool SGD, int V>
+// ---- sums over equal ids -----------------------------------------------------------
+
+constexpr int kV = 4;   // columns per thread
+
+// A row's finished sum: the dense gradient, or the SGD step on the table.
+template <bool SGD>
+__device__ __forceinline__ void finish(float* p, int left, const float (&acc)[kV], float scale, float lr) {
+  float x[kV];
+  if constexpr (SGD) {
+    load_some<GIST_STORE_F32, kV>(p, 0, left, 0.f, x);
+#pragma unroll
+    for (int q = 0; q < kV; ++q) x[q] = fmaf(-lr, scale * acc[q], x[q]);
+  } else {
+#pragma unroll
+    for (int q = 0; q < kV; ++q) x[q] = scale * acc[q];
+  }
+  store_some<GIST_STORE_F32, kV>(p, 0, left, x);
+}
+
+// Chunks of `len` sorted positions (a multiple of kBatch), one group of threads
+// each; blockIdx.y: slab of columns.  part[2 c] is the sum of chunk c's first id
+// where that id began in an earlier chunk, part[2 c + 1] that of its last id where
+// it began in this chunk and goes on in the next.  Rows are loaded kBatch at a
+// time and added in order.
+constexpr int kBatch = 8;
+template <bool SGD>
 __global__ __launch_bounds__(kBlock) void sum_kernel(int n, int Vn, int d, int tpr_log2, int len,
                                                      const int* __restrict__ keys,
                                                      const int* __restrict__ pos, float scale,
@@ -202,63 +309,90 @@ __global__ __launch_bounds__(kBlock) void sum_kernel(int n, int Vn, int d, int t
   const int64_t b64 = c * len;
   if (b64 >= n) return;
   const int b = static_cast<int>(b64), e = static_cast<int>(min<int64_t>(n, b64 + len));
-  const int j = V * (lane + (static_cast<int>(blockIdx.y) << tpr_log2));
+  const int j = kV * (lane + (static_cast<int>(blockIdx.y) << tpr_log2));
   if (j >= d) return;
   int cur = keys[b];
   if (cur == Vn) return;   // padding only
   bool head = b > 0 && keys[b - 1] == cur;
-  float acc[V] = {};
-  for (int i = b; i < e; ++i) {
-    const int k = keys[i];
-    if (k != cur) {
-      if (head) store_vec<V>(part + 2 * c * ldp + j, acc);
-      else finish<SGD, V>(out + cur * ldo + j, acc, scale, lr);
-      head = false;
-      cur = k;
+  float acc[kV] = {};
+  for (int i = b; i < e; i += kBatch) {
+    int k[kBatch], p[kBatch];
+    float x[kBatch][kV];
+    // the arrays are padded to whole batches
 #pragma unroll
-      for (int q = 0; q < V; ++q) acc[q] = 0.f;
-      if (k == Vn) return;
+    for (int u = 0; u < kBatch; u += 4) {
+      const int4 kk = *reinterpret_cast<const int4*>(keys + i + u), pp = *reinterpret_cast<const int4*>(pos + i + u);
+      k[u] = kk.x; k[u + 1] = kk.y; k[u + 2] = kk.z; k[u + 3] = kk.w;
+      p[u] = pp.x; p[u + 1] = pp.y; p[u + 2] = pp.z; p[u + 3] = pp.w;
     }
-    float x[V];
-    load_vec<GIST_STORE_F32, V>(dY, pos[i] * ldy + j, x);
 #pragma unroll
-    for (int q = 0; q < V; ++q) acc[q] += x[q];
+    for (int u = 0; u < kBatch; ++u)
+      if (i + u < e && k[u] != Vn) load_some<GIST_STORE_F32, kV>(dY, p[u] * ldy + j, d - j, 0.f, x[u]);
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      if (i + u >= e) break;
+      if (k[u] != cur) {
+        if (head) store_vec<kV>(part + 2 * c * ldp + j, acc);
+        else finish<SGD>(out + cur * ldo + j, d - j, acc, scale, lr);
+        head = false;
+        cur = k[u];
+#pragma unroll
+        for (int q = 0; q < kV; ++q) acc[q] = 0.f;
+        if (cur == Vn) return;
+      }
+#pragma unroll
+      for (int q = 0; q < kV; ++q) acc[q] += x[u][q];
+    }
   }
-  if (head) store_vec<V>(part + 2 * c * ldp + j, acc);
-  else if (e < n && keys[e] == cur) store_vec<V>(part + (2 * c + 1) * ldp + j, acc);
-  else finish<SGD, V>(out + cur * ldo + j, acc, scale, lr);
+  if (head) store_vec<kV>(part + 2 * c * ldp + j, acc);
+  else if (e < n && keys[e] == cur) store_vec<kV>(part + (2 * c + 1) * ldp + j, acc);
+  else finish<SGD>(out + cur * ldo + j, d - j, acc, scale, lr);
 }
 
 // Ids that cross chunk borders: the group of the chunk where such an id begins
 // adds its parts in chunk order.
-template <bool SGD, int V>
+template <bool SGD>
 __global__ __launch_bounds__(kBlock) void join_kernel(int n, int Vn, int d, int tpr_log2, int len,
                                                       const int* __restrict__ keys, float scale,
                                                       float lr, float* __restrict__ out,
                                                       int64_t ldo, const float* __restrict__ part,
                                                       int64_t ldp) {
   const int lane = threadIdx.x & ((1 << tpr_log2) - 1);
-  int64_t c = (static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x) >> tpr_log2;
-  int64_t b = c * len, e = b + len;
+  const int64_t c = (static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x) >> tpr_log2;
+  const int64_t b = c * len, e = b + len;
   if (e >= n) return;   // the last chunk: nothing goes on
-  const int j = V * (lane + (static_cast<int>(blockIdx.y) << tpr_log2));
+  const int j = kV * (lane + (static_cast<int>(blockIdx.y) << tpr_log2));
   if (j >= d) return;
   const int cur = keys[e - 1];
   if (cur == Vn || keys[e] != cur) return;
   if (keys[b] == cur && b > 0 && keys[b - 1] == cur) return;   // began earlier
-  float acc[V];
-  load_vec<GIST_STORE_F32, V>(part, (2 * c + 1) * ldp + j, acc);
-  for (;;) {
-    ++c;
-    b = e;
-    e = min<int64_t>(n, e + len);
-    float x[V];
-    load_vec<GIST_STORE_F32, V>(part, 2 * c * ldp + j, x);
-#pragma unroll
-    for (int q = 0; q < V; ++q) acc[q] += x[q];
-    if (e >= n || keys[e - 1] != cur || keys[e] != cur) break;
+  // the id's last position, by bisection: its parts are those of chunks c + 1 .. last
+  int lo = static_cast<int>(e), hi = n;   // keys[lo] == cur, keys[hi] != cur or hi == n
+  while (hi - lo > 1) {
+    const int mid = lo + ((hi - lo) >> 1);
+    if (keys[mid] == cur) lo = mid;
+    else hi = mid;
   }
-  finish<SGD, V>(out + cur * ldo + j, acc, scale, lr);
+  const int64_t last = lo / len;
+  float acc[kV];
+  load_vec<GIST_STORE_F32, kV>(part, (2 * c + 1) * ldp + j, acc);
+  int64_t x = c + 1;
+  for (; x + kBatch <= last + 1; x += kBatch) {
+    float y[kBatch][kV];
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) load_vec<GIST_STORE_F32, kV>(part, 2 * (x + u) * ldp + j, y[u]);
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u)
+#pragma unroll
+      for (int q = 0; q < kV; ++q) acc[q] += y[u][q];
+  }
+  for (; x <= last; ++x) {
+    float y[kV];
+    load_vec<GIST_STORE_F32, kV>(part, 2 * x * ldp + j, y);
+#pragma unroll
+    for (int q = 0; q < kV; ++q) acc[q] += y[q];
+  }
+  finish<SGD>(out + cur * ldo + j, d - j, acc, scale, lr);
 }
 
 // Zero rows that no id names (dense gradient): a wave per 64 rows, each lane
@@ -282,7 +416,8 @@ __global__ __launch_bounds__(kBlock) void zero_rows_kernel(int n, int Vn, int d,
     const int q = __ffsll(m) - 1;
     m &= m - 1;
     float* p = out + (r0 + q) * ldo;
-    for (int j = lane; j < d; j += 64) p[j] = 0.f;
+    const float z[4] = {};
+    for (int j = 4 * lane; j < d; j += 256) store_some<GIST_STORE_F32, 4>(p, j, d - j, z);
   }
 }
 
@@ -299,7 +434,9 @@ GradPlan plan(int64_t n, int64_t V, int d) {
   GradPlan p;
   p.tiles = (n + kTile - 1) / kTile;
   p.passes = (ceil_log2(V + 1) + kDigit - 1) / kDigit;
-  p.len = 32;
+  // short chunks where there are few rows, so that there are enough groups; parts
+  // cost two rows a chunk
+  p.len = n <= 32768 ? kBatch : n <= (1 << 20) ? 32 : 128;
   p.chunks = (n + p.len - 1) / p.len;
   p.ldp = (d + 3) / 4 * 4;
   p.keys = up256(static_cast<size_t>(n) * 4);
@@ -313,11 +450,7 @@ GradPlan plan(int64_t n, int64_t V, int d) {
 gist_status embed_lookup(hipStream_t st, int64_t n, int64_t V, int d, const void* table,
                          int64_t ldt, int store, const int32_t* ids, float scale, float* out,
                          int64_t ldo) {
-  const int eb = store == GIST_STORE_F32 ? 4 : 2;
-  const int most = store == GIST_STORE_F32 ? 4 : 8;
-  // eight values go out as two 16-byte stores, so the rows of out need no more
-  const int vt = vec_of(most, d, ldt, table, eb), vo = vec_of(4, d, ldo, out, 4);
-  const int v = vo == 4 ? vt : std::min(vt, vo);
+  const int eb = store == GIST_STORE_F32 ? 4 : 2, v = store == GIST_STORE_F32 ? 4 : 8;
   const int tl = std::min(8, ceil_log2((d + v - 1) / v));
   const int64_t blocks = std::min<int64_t>(((n << tl) + kBlock - 1) / kBlock, 1 << 22);
   ProfScope ps(st, "embed_lookup", static_cast<double>(n) * d,
@@ -325,21 +458,9 @@ gist_status embed_lookup(hipStream_t st, int64_t n, int64_t V, int d, const void
 #define LOOKUP(S, W)                                                                         \
   lookup_kernel<S, W><<<dim3(static_cast<unsigned>(blocks)), kBlock, 0, st>>>(               \
       static_cast<int>(n), V, d, tl, table, ldt, ids, scale, out, ldo)
-  if (store == GIST_STORE_F32) {
-    if (v == 4) LOOKUP(GIST_STORE_F32, 4);
-    else if (v == 2) LOOKUP(GIST_STORE_F32, 2);
-    else LOOKUP(GIST_STORE_F32, 1);
-  } else if (store == GIST_STORE_BF16) {
-    if (v == 8) LOOKUP(GIST_STORE_BF16, 8);
-    else if (v == 4) LOOKUP(GIST_STORE_BF16, 4);
-    else if (v == 2) LOOKUP(GIST_STORE_BF16, 2);
-    else LOOKUP(GIST_STORE_BF16, 1);
-  } else {
-    if (v == 8) LOOKUP(GIST_STORE_F16, 8);
-    else if (v == 4) LOOKUP(GIST_STORE_F16, 4);
-    else if (v == 2) LOOKUP(GIST_STORE_F16, 2);
-    else LOOKUP(GIST_STORE_F16, 1);
-  }
+  if (store == GIST_STORE_F32) LOOKUP(GIST_STORE_F32, 4);
+  else if (store == GIST_STORE_BF16) LOOKUP(GIST_STORE_BF16, 8);
+  else LOOKUP(GIST_STORE_F16, 8);
 #undef LOOKUP
   return check_launch("embed_lookup");
 }
@@ -357,7 +478,10 @@ gist_status embed_grad(hipStream_t st, int64_t n, int64_t V, int d, const int32_
   float* part = reinterpret_cast<float*>(c + 4 * p.keys + p.hist);
   const int ni = static_cast<int>(n), vi = static_cast<int>(V), tiles = static_cast<int>(p.tiles);
   int cur = 0;
-  if (n > 0) {
+  if (n > 0 && n <= kSmall) {
+    ProfScope ps(st, "embed_sort_small", 0.0, 12.0 * n);
+    small_sort_kernel<<<1, kSmallThreads, 0, st>>>(ni, vi, ids, p.passes, k[0], q[0]);
+  } else if (n > 0) {
     ProfScope ps(st, "embed_sort", 0.0, 8.0 * n * p.passes);
     for (int i = 0; i < p.passes; ++i) {
       const int* kin = i == 0 ? ids : k[cur ^ 1];
@@ -383,30 +507,27 @@ gist_status embed_grad(hipStream_t st, int64_t n, int64_t V, int d, const int32_
                                                                             out, ldo);
   }
   if (n > 0) {
-    const int v = std::min(vec_of(4, d, ldy, dY, 4), vec_of(4, d, ldo, out, 4));
-    const int tl = std::min(8, ceil_log2((d + v - 1) / v));
+    const int tl = std::min(8, ceil_log2((d + kV - 1) / kV));
     if ((p.chunks << tl) >= (int64_t{1} << 32) - kBlock)
       return set_error(GIST_E_UNSUPPORTED, "embed_grad: n * d exceeds the grid");
     const dim3 g(static_cast<unsigned>(((p.chunks << tl) + kBlock - 1) / kBlock),
-                 static_cast<unsigned>((d + (v << tl) - 1) / (v << tl)));
-    ProfScope ps(st, "embed_sum", static_cast<double>(n) * d, 8.0 * n * d);
-#define SUMS(S, W)                                                                             \
-  do {                                                                                         \
-    sum_kernel<S, W><<<g, kBlock, 0, st>>>(ni, vi, d, tl, p.len, k[cur], q[cur], scale, dY, ldy, \
-                                           lr, out, ldo, part, p.ldp);                         \
-    join_kernel<S, W><<<g, kBlock, 0, st>>>(ni, vi, d, tl, p.len, k[cur], scale, lr, out, ldo, \
-                                            part, p.ldp);                                      \
-  } while (0)
-    if (sgd) {
-      if (v == 4) SUMS(true, 4);
-      else if (v == 2) SUMS(true, 2);
-      else SUMS(true, 1);
-    } else {
-      if (v == 4) SUMS(false, 4);
-      else if (v == 2) SUMS(false, 2);
-      else SUMS(false, 1);
+                 static_cast<unsigned>((d + (kV << tl) - 1) / (kV << tl)));
+    {
+      ProfScope ps(st, "embed_sum", static_cast<double>(n) * d, 8.0 * n * d);
+      if (sgd)
+        sum_kernel<true><<<g, kBlock, 0, st>>>(ni, vi, d, tl, p.len, k[cur], q[cur], scale, dY, ldy, lr, out, ldo,
+                                               part, p.ldp);
+      else
+        sum_kernel<false><<<g, kBlock, 0, st>>>(ni, vi, d, tl, p.len, k[cur], q[cur], scale, dY, ldy, lr, out, ldo,
+                                                part, p.ldp);
     }
-#undef SUMS
+    if (p.chunks > 1) {
+      ProfScope ps(st, "embed_join", 0.0, 0.0);
+      if (sgd)
+        join_kernel<true><<<g, kBlock, 0, st>>>(ni, vi, d, tl, p.len, k[cur], scale, lr, out, ldo, part, p.ldp);
+      else
+        join_kernel<false><<<g, kBlock, 0, st>>>(ni, vi, d, tl, p.len, k[cur], scale, lr, out, ldo, part, p.ldp);
+    }
   }
   return check_launch("embed_grad");
 }

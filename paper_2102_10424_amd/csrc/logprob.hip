@@ -75,22 +75,53 @@ __device__ __forceinline__ u64 pack(float z, unsigned cls) {
   return (static_cast<u64>(order_bits(z)) << 32) | (0xffffffffu - cls);
 }
 
+__device__ __forceinline__ u64 lane_of(u64 x, int l) {   // l uniform
+  const unsigned lo = __builtin_amdgcn_readlane(static_cast<unsigned>(x), l);
+  const unsigned hi = __builtin_amdgcn_readlane(static_cast<unsigned>(x >> 32), l);
+  return (static_cast<u64>(hi) << 32) | lo;
+}
+__device__ __forceinline__ u64 from_left(u64 x) {   // lane l - 1's
+  const unsigned lo = __builtin_amdgcn_update_dpp(0, static_cast<int>(x), 0x138, 0xf, 0xf, false);
+  const unsigned hi = __builtin_amdgcn_update_dpp(0, static_cast<int>(x >> 32), 0x138, 0xf, 0xf, false);
+  return (static_cast<u64>(hi) << 32) | lo;
+}
+
 // A wave's sorted list, lane l holding the l-th best; thr is the K-th.
 struct Top {
   u64 mine = 0, thr = 0;
   int K;
-  // Candidates of all lanes (0: none).
+  __device__ __forceinline__ void exchange(int o, bool larger) {
+    const u64 other = __shfl_xor(mine, o, 64);
+    mine = (mine > other) == larger ? mine : other;
+  }
+  // Sorts any 64 integers, the greatest to lane 0.
+  __device__ __forceinline__ void sort(u64 x, int lane) {
+    mine = x;
+#pragma unroll
+    for (int size = 2; size <= 64; size <<= 1)
+#pragma unroll
+      for (int o = size >> 1; o > 0; o >>= 1) exchange(o, ((lane & o) == 0) == ((lane & size) == 0 || size == 64));
+    thr = lane_of(mine, K - 1);
+  }
+  // Joins another sorted list, given in reverse (lane l holding its 63 - l-th).
+  __device__ __forceinline__ void join(u64 reversed, int lane) {
+    if (mine < reversed) mine = reversed;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) exchange(o, (lane & o) == 0);
+    thr = lane_of(mine, K - 1);
+  }
+  // Candidates of all lanes (0: none), one insertion each.
   __device__ __forceinline__ void offer(u64 x, int lane) {
     u64 want = __ballot(x > thr);
     while (want) {
       const int src = __ffsll(want) - 1;
       want &= want - 1;
-      const u64 c = __shfl(x, src, 64);
+      const u64 c = lane_of(x, src);
       if (c <= thr) continue;
       const int at = __popcll(__ballot(mine > c));
-      const u64 up = __shfl_up(mine, 1, 64);
+      const u64 up = from_left(mine);
       mine = lane < at ? mine : lane == at ? c : up;
-      thr = __shfl(mine, K - 1, 64);
+      thr = lane_of(mine, K - 1);
     }
   }
 };
@@ -101,16 +132,16 @@ struct Out {
   int* idx;
 };
 
-// A row's outputs from its statistics; called by one wave.
+// A row's outputs from its statistics, by one lane; returns the log-sum-exp.
 template <int STORE>
-__device__ __forceinline__ void write_row(const Out& o, int64_t row, int C, const void* Z,
-                                          int64_t ldz, Stat a, const Top& top, int K, int lane) {
+__device__ __forceinline__ float write_stats(const Out& o, int64_t row, int C, const void* Z, int64_t ldz,
+                                             const Stat& a, bool write) {
   const float nan = __uint_as_float(0x7fc00000u);
   const bool ok = a.m < INFINITY;            // no NaN, no +Inf in the row
   const bool some = ok && a.m > -INFINITY;   // not masked throughout
   const float l2 = lg2(a.s);
   const float lse = some ? fmaf(kLn2, l2, a.m) : ok ? -INFINITY : nan;
-  if (lane == 0) {
+  if (write) {
     if (o.lse) o.lse[row] = lse;
     if (o.entropy) o.entropy[row] = some ? kLn2 * (l2 - a.t / a.s) : ok ? 0.f : nan;
     if (o.logp) {
@@ -126,20 +157,133 @@ __device__ __forceinline__ void write_row(const Out& o, int64_t row, int C, cons
       o.logp[row] = ok ? v : nan;
     }
   }
-  if (lane < K) {
-    const float z = from_order(static_cast<unsigned>(top.mine >> 32));
-    o.top[row * K + lane] = !ok ? nan : z == -INFINITY ? z : z - lse;
-    o.idx[row * K + lane] = ok ? static_cast<int>(0xffffffffu - static_cast<unsigned>(top.mine)) : -1;
+  return lse;
+}
+
+// The k-th best class (its order bits and itself) of a row.
+__device__ __forceinline__ void write_top(const Out& o, int64_t row, int K, int k, unsigned bits, unsigned cls,
+                                          float m, float lse) {
+  const bool ok = m < INFINITY;
+  const float z = from_order(bits);
+  o.top[row * K + k] = !ok ? __uint_as_float(0x7fc00000u) : z == -INFINITY ? z : z - lse;
+  o.idx[row * K + k] = ok ? static_cast<int>(cls) : -1;
+}
+
+// All of a row's outputs, by one wave.
+template <int STORE>
+__device__ __forceinline__ void write_row(const Out& o, int64_t row, int C, const void* Z, int64_t ldz,
+                                          const Stat& a, const Top& top, int K, int lane) {
+  const float lse = write_stats<STORE>(o, row, C, Z, ldz, a, lane == 0);
+  if (lane < K)
+    write_top(o, row, K, lane, static_cast<unsigned>(top.mine >> 32), 0xffffffffu - static_cast<unsigned>(top.mine),
+              a.m, lse);
+}
+
+// ---- rows of up to 1,024 classes: LPR lanes a row, E classes a lane ----------------
+
+template <int CTRL>
+__device__ __forceinline__ float dpp_f(float x) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(x), __float_as_int(x), CTRL, 0xf, 0xf, false));
+}
+template <int CTRL>
+__device__ __forceinline__ unsigned dpp_u(unsigned x) {
+  return static_cast<unsigned>(__builtin_amdgcn_update_dpp(static_cast<int>(x), static_cast<int>(x), CTRL, 0xf, 0xf, false));
+}
+// f over the LPR lanes of a row, every lane with the result (f commutative).
+// Within 16 lanes by lane permutations (swaps in a quad, then mirrors of 8 and
+// 16), which cost an instruction each.
+template <int LPR, class F>
+__device__ __forceinline__ float reduce_f(float x, F f) {
+  x = f(x, dpp_f<0xB1>(x));
+  x = f(x, dpp_f<0x4E>(x));
+  x = f(x, dpp_f<0x141>(x));
+  if constexpr (LPR > 8) x = f(x, dpp_f<0x140>(x));
+  if constexpr (LPR > 16) x = f(x, __shfl_xor(x, 16, 64));
+  if constexpr (LPR > 32) x = f(x, __shfl_xor(x, 32, 64));
+  return x;
+}
+template <int LPR, class F>
+__device__ __forceinline__ unsigned reduce_u(unsigned x, F f) {
+  x = f(x, dpp_u<0xB1>(x));
+  x = f(x, dpp_u<0x4E>(x));
+  x = f(x, dpp_u<0x141>(x));
+  if constexpr (LPR > 8) x = f(x, dpp_u<0x140>(x));
+  if constexpr (LPR > 16) x = f(x, static_cast<unsigned>(__shfl_xor(static_cast<int>(x), 16, 64)));
+  if constexpr (LPR > 32) x = f(x, static_cast<unsigned>(__shfl_xor(static_cast<int>(x), 32, 64)));
+  return x;
+}
+
+// A row is in registers, so its maximum comes first and nothing is rescaled; the
+// K best are taken out one by one.  What bounds it: issue (a round of the K best
+// is about 5 E + 10 instructions for 64 / LPR rows).
+template <int STORE, int LPR, int E, bool TOP>
+__global__ __launch_bounds__(kBlock) void short_rows_kernel(int64_t n, int C, const void* __restrict__ Z,
+                                                            int64_t ldz, Out o, int K) {
+  constexpr int RPB = kBlock / LPR;
+  const int l = threadIdx.x & (LPR - 1);
+  // rows of a wave in step: all its lanes reach the permutations below
+  for (int64_t r0 = static_cast<int64_t>(blockIdx.x) * RPB; r0 < n; r0 += static_cast<int64_t>(gridDim.x) * RPB) {
+    const int64_t row = r0 + threadIdx.x / LPR;
+    const bool live = row < n;
+    float z[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      float x[1] = {-INFINITY};
+      if (live && l + LPR * e < C) load_vec<STORE, 1>(Z, row * ldz + l + LPR * e, x);
+      z[e] = x[0];
+    }
+    Stat a{z[0], 0.f, 0.f};
+#pragma unroll
+    for (int e = 1; e < E; ++e) a.m = max_nan(a.m, z[e]);
+    a.m = reduce_f<LPR>(a.m, [](float x, float y) { return max_nan(x, y); });
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const float y = fmaxf((z[e] - a.m) * kL, kFloor), p = ex2(y);
+      a.s += p;
+      a.t = fmaf(p, y, a.t);
+    }
+    a.s = reduce_f<LPR>(a.s, [](float x, float y) { return x + y; });
+    a.t = reduce_f<LPR>(a.t, [](float x, float y) { return x + y; });
+    const float lse = write_stats<STORE>(o, row, C, Z, ldz, a, live && l == 0);
+    if constexpr (TOP) {
+      unsigned key[E];
+#pragma unroll
+      for (int e = 0; e < E; ++e) key[e] = l + LPR * e < C ? order_bits(z[e]) : 0u;
+      unsigned kb = 0, kc = 0;   // this lane's share of the last LPR results
+      for (int k = 0; k < K; ++k) {
+        unsigned best = key[0];
+#pragma unroll
+        for (int e = 1; e < E; ++e) best = max(best, key[e]);
+        best = reduce_u<LPR>(best, [](unsigned x, unsigned y) { return max(x, y); });
+        unsigned c = 0xffffffffu;
+#pragma unroll
+        for (int e = E - 1; e >= 0; --e) c = key[e] == best ? static_cast<unsigned>(l + LPR * e) : c;
+        c = reduce_u<LPR>(c, [](unsigned x, unsigned y) { return min(x, y); });
+#pragma unroll
+        for (int e = 0; e < E; ++e) key[e] = static_cast<unsigned>(l + LPR * e) == c ? 0u : key[e];
+        if ((k & (LPR - 1)) == l) {
+          kb = best;
+          kc = c;
+        }
+        if ((k & (LPR - 1)) == LPR - 1 || k == K - 1) {
+          const int at = (k & ~(LPR - 1)) + l;
+          if (live && at <= k) write_top(o, row, K, at, kb, kc, a.m, lse);
+        }
+      }
+    }
   }
 }
 
+// ---- longer rows ---------------------------------------------------------------------
+
 // One workgroup per (row, part of the row).  parts == 1 writes the outputs,
 // else the part's statistics (4 floats) and list (K integers) go to `part`.
-template <int STORE, int V, bool TOP>
+template <int STORE, bool TOP>
 __global__ __launch_bounds__(kBlock) void rows_kernel(int64_t items, int parts, int64_t len, int C,
                                                       const void* __restrict__ Z, int64_t ldz,
                                                       Out o, int K, float* __restrict__ pstat,
                                                       u64* __restrict__ ptop) {
+  constexpr int V = STORE == GIST_STORE_F32 ? 4 : 8;
   __shared__ Stat wst[kWaves];
   __shared__ u64 wtop[kWaves][64];
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
@@ -153,18 +297,31 @@ __global__ __launch_bounds__(kBlock) void rows_kernel(int64_t items, int parts, 
     for (int64_t j0 = c0; j0 < c1; j0 += V * kBlock) {   // block-uniform: ballots inside
       const int64_t j = j0 + V * t;
       float z[V];
-#pragma unroll
-      for (int q = 0; q < V; ++q) z[q] = -INFINITY;
-      const bool in = j < c1;   // widths are multiples of V
-      if (in) load_vec<STORE, V>(Z, row * ldz + j, z);
+      load_some<STORE, V>(Z, row * ldz + j, c1 - j, -INFINITY, z);
       float m = z[0];
 #pragma unroll
       for (int q = 1; q < V; ++q) m = max_nan(m, z[q]);
       if constexpr (TOP) {
-        if (__any(in && pack(m, 0u) > top.thr)) {
+        if (j0 == c0) {
+          // The list begins with the lanes' best: most others then fail its K-th.
+          u64 best = 0;
+          int at = 0;
+#pragma unroll
+          for (int q = 0; q < V; ++q) {
+            const u64 x = j + q < c1 ? pack(z[q], static_cast<unsigned>(j + q)) : 0;
+            if (x > best) {
+              best = x;
+              at = q;
+            }
+          }
+          top.sort(best, lane);
 #pragma unroll
           for (int q = 0; q < V; ++q)
-            top.offer(in ? pack(z[q], static_cast<unsigned>(j + q)) : 0, lane);
+            top.offer(j + q < c1 && q != at ? pack(z[q], static_cast<unsigned>(j + q)) : 0, lane);
+        } else if (__any(j < c1 && pack(m, 0u) > top.thr)) {
+#pragma unroll
+          for (int q = 0; q < V; ++q)
+            top.offer(j + q < c1 ? pack(z[q], static_cast<unsigned>(j + q)) : 0, lane);
         }
       }
       rescale(a, max_nan(a.m, m));
@@ -179,13 +336,13 @@ __global__ __launch_bounds__(kBlock) void rows_kernel(int64_t items, int parts, 
     a = wave_merge(a);
     __syncthreads();   // the previous item's LDS is read
     if (lane == 0) wst[wave] = a;
-    if (TOP) wtop[wave][lane] = top.mine;
+    if (TOP) wtop[wave][63 - lane] = lane < K ? top.mine : 0;
     __syncthreads();
     if (wave == 0) {
 #pragma unroll
       for (int w = 1; w < kWaves; ++w) {
         merge(a, wst[w]);
-        if (TOP) top.offer(lane < K ? wtop[w][lane] : 0, lane);
+        if (TOP) top.join(wtop[w][lane], lane);
       }
       if (parts == 1) {
         write_row<STORE>(o, row, C, Z, ldz, a, top, TOP ? K : 0, lane);
@@ -202,14 +359,15 @@ __global__ __launch_bounds__(kBlock) void rows_kernel(int64_t items, int parts, 
   }
 }
 
-// Joins the parts of a row: one wave per row.
+// Joins the parts of a row: each wave a share of them, then the first wave.
 template <int STORE>
-__global__ __launch_bounds__(64) void join_rows_kernel(int64_t n, int parts, int C,
-                                                       const void* __restrict__ Z, int64_t ldz,
-                                                       Out o, int K,
-                                                       const float* __restrict__ pstat,
-                                                       const u64* __restrict__ ptop) {
-  const int lane = threadIdx.x;
+__global__ __launch_bounds__(kBlock) void join_rows_kernel(int64_t n, int parts, int C,
+                                                           const void* __restrict__ Z, int64_t ldz,
+                                                           Out o, int K,
+                                                           const float* __restrict__ pstat,
+                                                           const u64* __restrict__ ptop) {
+  __shared__ u64 wtop[kWaves][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   for (int64_t row = blockIdx.x; row < n; row += gridDim.x) {
     Stat a{-INFINITY, 0.f, 0.f};
     for (int p = lane; p < parts; p += 64) {
@@ -219,9 +377,16 @@ __global__ __launch_bounds__(64) void join_rows_kernel(int64_t n, int parts, int
     a = wave_merge(a);
     Top top;
     top.K = K > 0 ? K : 1;
-    for (int i = 0; i < parts * K; i += 64)
-      top.offer(i + lane < parts * K ? ptop[row * parts * K + i + lane] : 0, lane);
-    write_row<STORE>(o, row, C, Z, ldz, a, top, K, lane);
+    if (K > 0) {
+      for (int p = wave; p < parts; p += kWaves)
+        top.join(63 - lane < K ? ptop[(row * parts + p) * K + 63 - lane] : 0, lane);
+      __syncthreads();   // the previous row's lists are read
+      wtop[wave][63 - lane] = top.mine;
+      __syncthreads();
+      if (wave == 0)
+        for (int w = 1; w < kWaves; ++w) top.join(wtop[w][lane], lane);
+    }
+    if (wave == 0) write_row<STORE>(o, row, C, Z, ldz, a, top, K, lane);
   }
 }
 
@@ -254,7 +419,7 @@ __global__ __launch_bounds__(kBlock) void bwd_kernel(int64_t items, int slabs, i
     if (none) gy = 0.f;
     for (int64_t j = c0 + V * lane; j < c1; j += V << tl) {
       float z[V], d[V];
-      load_vec<STORE, V>(Z, row * ldz + j, z);
+      load_some<STORE, V>(Z, row * ldz + j, c1 - j, 0.f, z);
 #pragma unroll
       for (int q = 0; q < V; ++q) {
         const float x = fmaxf(z[q] - l, -200.f);
@@ -264,20 +429,23 @@ __global__ __launch_bounds__(kBlock) void bwd_kernel(int64_t items, int slabs, i
         if (j + q == y) d[q] += gy;
         if (bad) d[q] = __uint_as_float(0x7fc00000u);
       }
-      store_as<STORE, V>(dZ, row * ldd + j, d);
+      store_some<STORE, V>(dZ, row * ldd + j, c1 - j, d);
     }
   }
 }
 
 struct Plan {
-  int v, parts;
+  int parts;
   int64_t len;
 };
+
+constexpr int64_t kShort = 1024;   // classes that short_rows_kernel takes
 
 // Parts of a row: as many as fill the card, of at least 4,096 elements each
 // (16 per thread).
 Plan plan_rows(int64_t n, int64_t C) {
-  Plan p{1, 1, C};
+  Plan p{1, C};
+  if (C <= kShort) return p;
   const int64_t want = n >= 1024 ? 1 : (1024 + n - 1) / std::max<int64_t>(n, 1);
   const int64_t most = C / 4096;
   p.parts = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({want, most, 256})));
@@ -300,52 +468,63 @@ gist_status log_probs(hipStream_t st, int64_t n, int64_t C, const void* Z, int64
                       const int32_t* tokens, float* logp, float* entropy, float* lse, int K,
                       float* top_logp, int32_t* top_idx, void* ws) {
   const Plan p = plan_rows(n, C);
-  const int eb = store == GIST_STORE_F32 ? 4 : 2;
-  const int v = vec_of(store == GIST_STORE_F32 ? 4 : 8, C, ldz, Z, eb);
+  const int eb = store == GIST_STORE_F32 ? 4 : 2, c = static_cast<int>(C);
   const Out o{tokens, logp, entropy, lse, top_logp, top_idx};
   float* pstat = static_cast<float*>(ws);
   u64* ptop = p.parts == 1 ? nullptr
                            : reinterpret_cast<u64*>(static_cast<char*>(ws) +
                                                     up256(static_cast<size_t>(n) * p.parts * 16));
   const int64_t items = n * p.parts;
-  const dim3 g(static_cast<unsigned>(std::min<int64_t>(items, 1 << 22)));
-  {
-    ProfScope ps(st, "log_probs", 6.0 * n * C, static_cast<double>(n) * C * eb);
-#define ROWS1(S, W, T)                                                                         \
-  rows_kernel<S, W, T><<<g, kBlock, 0, st>>>(items, p.parts, p.len, static_cast<int>(C), Z, ldz, o, \
-                                             K, pstat, ptop)
-#define ROWS(S, W)                     \
-  do {                                 \
-    if (K > 0) ROWS1(S, W, true);      \
-    else ROWS1(S, W, false);           \
+  ProfScope ps(st, "log_probs", 6.0 * n * C, static_cast<double>(n) * C * eb);
+#define BY_STORE(CALL)                                      \
+  do {                                                      \
+    if (store == GIST_STORE_F32) CALL(GIST_STORE_F32);      \
+    else if (store == GIST_STORE_BF16) CALL(GIST_STORE_BF16); \
+    else CALL(GIST_STORE_F16);                              \
   } while (0)
-    if (store == GIST_STORE_F32) {
-      if (v == 4) ROWS(GIST_STORE_F32, 4);
-      else if (v == 2) ROWS(GIST_STORE_F32, 2);
-      else ROWS(GIST_STORE_F32, 1);
-    } else if (store == GIST_STORE_BF16) {
-      if (v == 8) ROWS(GIST_STORE_BF16, 8);
-      else if (v == 4) ROWS(GIST_STORE_BF16, 4);
-      else if (v == 2) ROWS(GIST_STORE_BF16, 2);
-      else ROWS(GIST_STORE_BF16, 1);
-    } else {
-      if (v == 8) ROWS(GIST_STORE_F16, 8);
-      else if (v == 4) ROWS(GIST_STORE_F16, 4);
-      else if (v == 2) ROWS(GIST_STORE_F16, 2);
-      else ROWS(GIST_STORE_F16, 1);
-    }
+  if (C <= kShort) {
+#define SHORT2(S, L, E, T)                                                                         \
+  short_rows_kernel<S, L, E, T>                                                                    \
+      <<<dim3(static_cast<unsigned>(std::min<int64_t>((n + kBlock / L - 1) / (kBlock / L), 1 << 20))), \
+         kBlock, 0, st>>>(n, c, Z, ldz, o, K)
+#define SHORT1(S, L, E)                 \
+  do {                                  \
+    if (K > 0) SHORT2(S, L, E, true);   \
+    else SHORT2(S, L, E, false);        \
+  } while (0)
+#define SHORT(S)                        \
+  do {                                  \
+    if (C <= 8) SHORT1(S, 8, 1);        \
+    else if (C <= 16) SHORT1(S, 8, 2);  \
+    else if (C <= 32) SHORT1(S, 8, 4);  \
+    else if (C <= 48) SHORT1(S, 8, 6);  \
+    else if (C <= 64) SHORT1(S, 8, 8);  \
+    else if (C <= 128) SHORT1(S, 16, 8); \
+    else if (C <= 256) SHORT1(S, 32, 8); \
+    else if (C <= 512) SHORT1(S, 64, 8); \
+    else SHORT1(S, 64, 16);             \
+  } while (0)
+    BY_STORE(SHORT);
+#undef SHORT
+#undef SHORT1
+#undef SHORT2
+    return check_launch("log_probs");
+  }
+  {
+    const dim3 g(static_cast<unsigned>(std::min<int64_t>(items, 1 << 22)));
+#define ROWS(S)                                                                                             \
+  do {                                                                                                      \
+    if (K > 0) rows_kernel<S, true><<<g, kBlock, 0, st>>>(items, p.parts, p.len, c, Z, ldz, o, K, pstat, ptop); \
+    else rows_kernel<S, false><<<g, kBlock, 0, st>>>(items, p.parts, p.len, c, Z, ldz, o, K, pstat, ptop);      \
+  } while (0)
+    BY_STORE(ROWS);
 #undef ROWS
-#undef ROWS1
   }
   if (p.parts > 1) {
-    ProfScope ps(st, "log_probs_join", 0.0, static_cast<double>(items) * (16 + 8 * K));
     const dim3 gj(static_cast<unsigned>(std::min<int64_t>(n, 1 << 22)));
-    if (store == GIST_STORE_F32)
-      join_rows_kernel<GIST_STORE_F32><<<gj, 64, 0, st>>>(n, p.parts, static_cast<int>(C), Z, ldz, o, K, pstat, ptop);
-    else if (store == GIST_STORE_BF16)
-      join_rows_kernel<GIST_STORE_BF16><<<gj, 64, 0, st>>>(n, p.parts, static_cast<int>(C), Z, ldz, o, K, pstat, ptop);
-    else
-      join_rows_kernel<GIST_STORE_F16><<<gj, 64, 0, st>>>(n, p.parts, static_cast<int>(C), Z, ldz, o, K, pstat, ptop);
+#define JOIN(S) join_rows_kernel<S><<<gj, kBlock, 0, st>>>(n, p.parts, c, Z, ldz, o, K, pstat, ptop)
+    BY_STORE(JOIN);
+#undef JOIN
   }
   return check_launch("log_probs");
 }
@@ -355,7 +534,8 @@ gist_status log_probs_bwd(hipStream_t st, int64_t n, int64_t C, const void* Z, i
                           const float* entropy, const float* g_logp, const float* g_entropy,
                           void* dZ, int64_t ldd) {
   const int eb = store == GIST_STORE_F32 ? 4 : 2, most = store == GIST_STORE_F32 ? 4 : 8;
-  const int v = std::min(vec_of(most, C, ldz, Z, eb), vec_of(most, C, ldd, dZ, eb));
+  // short rows: a class per lane, so that a wave's accesses are one run of bytes
+  const int v = C <= 64 ? 1 : most;
   const int tl = std::min(8, ceil_log2((C + v - 1) / v));
   // slabs of eight steps where a row takes more than one
   const int64_t step = static_cast<int64_t>(v) << tl;
@@ -369,20 +549,16 @@ gist_status log_probs_bwd(hipStream_t st, int64_t n, int64_t C, const void* Z, i
                                          g_entropy, dZ, ldd)
   if (store == GIST_STORE_F32) {
     if (v == 4) BWD(GIST_STORE_F32, 4);
-    else if (v == 2) BWD(GIST_STORE_F32, 2);
     else BWD(GIST_STORE_F32, 1);
   } else if (store == GIST_STORE_BF16) {
     if (v == 8) BWD(GIST_STORE_BF16, 8);
-    else if (v == 4) BWD(GIST_STORE_BF16, 4);
-    else if (v == 2) BWD(GIST_STORE_BF16, 2);
     else BWD(GIST_STORE_BF16, 1);
   } else {
     if (v == 8) BWD(GIST_STORE_F16, 8);
-    else if (v == 4) BWD(GIST_STORE_F16, 4);
-    else if (v == 2) BWD(GIST_STORE_F16, 2);
     else BWD(GIST_STORE_F16, 1);
   }
 #undef BWD
+#undef BY_STORE
   return check_launch("log_probs_bwd");
 }
 
