@@ -49,8 +49,8 @@ __global__ __launch_bounds__(kBlock) void lookup_kernel(int n, int64_t V_rows, i
 // ---- sort -----------------------------------------------------------------------
 
 constexpr int kDigit = 8, kBins = 1 << kDigit;
-constexpr int kItems = 16;                  // keys per thread and tile
-constexpr int kTile = kBlock * kItems;      // 4,096
+constexpr int kItems = 8;                   // keys per thread and tile
+constexpr int kTile = kBlock * kItems;      // 2,048
 
 __device__ __forceinline__ int key_of(int id, int V) {   // padding sorts last
   return id >= 0 && id < V ? id : V;
@@ -60,8 +60,9 @@ __device__ __forceinline__ int key_of(int id, int V) {   // padding sorts last
 template <bool FIRST>
 __global__ __launch_bounds__(kBlock) void hist_kernel(int n, int V, const int* __restrict__ keys,
                                                       int shift, int tiles,
-                                                      int* __restrict__ hist) {
+                                                      int* __restrict__ hist, int* __restrict__ crossing) {
   __shared__ int cnt[kBins];
+  if (FIRST && blockIdx.x == 0 && threadIdx.x < 2) crossing[threadIdx.x] = 0;
   cnt[threadIdx.x] = 0;
   __syncthreads();
   const int64_t base = static_cast<int64_t>(blockIdx.x) * kTile;
@@ -77,19 +78,21 @@ __global__ __launch_bounds__(kBlock) void hist_kernel(int n, int V, const int* _
   hist[static_cast<int64_t>(threadIdx.x) * tiles + blockIdx.x] = cnt[threadIdx.x];
 }
 
-// In-place exclusive scan of `count` ints by one workgroup.
+// In-place exclusive scan of `count` ints (a multiple of 256) by one workgroup,
+// 16 a thread and round.
 __global__ __launch_bounds__(1024) void scan_kernel(int64_t count, int* __restrict__ v) {
   __shared__ int wsum[16];
-  __shared__ int carry_s;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-  if (t == 0) carry_s = 0;
-  __syncthreads();
-  for (int64_t base = 0; base < count; base += 4096) {
-    const int64_t e = base + 4 * t;
-    int x[4];
+  int carry = 0;
+  for (int64_t base = 0; base < count; base += 16384) {
+    const int64_t e = base + 16 * t;
+    int4 x[4];
+    int mine = 0;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) x[q] = e + q < count ? v[e + q] : 0;
-    const int mine = x[0] + x[1] + x[2] + x[3];
+    for (int q = 0; q < 4; ++q) {
+      x[q] = e < count ? reinterpret_cast<const int4*>(v + e)[q] : int4{0, 0, 0, 0};
+      mine += x[q].x + x[q].y + x[q].z + x[q].w;
+    }
     int inc = mine;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -98,17 +101,25 @@ __global__ __launch_bounds__(1024) void scan_kernel(int64_t count, int* __restri
     }
     if (lane == 63) wsum[wave] = inc;
     __syncthreads();
-    int before = carry_s;
-    for (int w = 0; w < wave; ++w) before += wsum[w];
-    int run = before + inc - mine;
+    int run = carry + inc - mine;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      if (e + q < count) v[e + q] = run;
-      run += x[q];
+    for (int w = 0; w < 16; ++w) {
+      if (w < wave) run += wsum[w];
+      carry += wsum[w];
     }
-    __syncthreads();   // everyone has read carry_s and wsum
-    if (t == 1023) carry_s = before + inc;
-    __syncthreads();
+    if (e < count) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        int4 y;
+        y.x = run;
+        y.y = y.x + x[q].x;
+        y.z = y.y + x[q].y;
+        y.w = y.z + x[q].z;
+        run = y.w + x[q].w;
+        reinterpret_cast<int4*>(v + e)[q] = y;
+      }
+    }
+    __syncthreads();   // wsum is read
   }
 }
 
@@ -174,7 +185,8 @@ __global__ __launch_bounds__(kBlock) void scatter_digit_kernel(
 constexpr int kSmallThreads = 1024, kSmallItems = 8, kSmall = kSmallThreads * kSmallItems;
 __global__ __launch_bounds__(kSmallThreads) void small_sort_kernel(int n, int V, const int* __restrict__ ids,
                                                                    int passes, int* __restrict__ keys,
-                                                                   int* __restrict__ pos) {
+                                                                   int* __restrict__ pos,
+                                                                   int* __restrict__ crossing) {
   constexpr int kWaves = kSmallThreads / 64;
   __shared__ int cnt[kWaves][kBins];
   __shared__ int lk[kSmall], lp[kSmall];
@@ -184,6 +196,7 @@ __global__ __launch_bounds__(kSmallThreads) void small_sort_kernel(int n, int V,
   const int base = wave * items * 64;
   int key[kSmallItems], ps[kSmallItems];
   int down = 0;
+  if (t < 2) crossing[t] = 0;
 #pragma unroll
   for (int i = 0; i < kSmallItems; ++i) {
     const int e = base + i * 64 + lane;
@@ -293,8 +306,11 @@ __device__ __forceinline__ void finish(float* p, int left, const float (&acc)[kV
 // Chunks of `len` sorted positions (a multiple of kBatch), one group of threads
 // each; blockIdx.y: slab of columns.  part[2 c] is the sum of chunk c's first id
 // where that id began in an earlier chunk, part[2 c + 1] that of its last id where
-// it began in this chunk and goes on in the next.  Rows are loaded kBatch at a
-// time and added in order.
+// it began in this chunk and goes on in the next.  The chunks with such an id are
+// listed, in no order: crossing[0] of them, from crossing[2] on, and crossing[1] with
+// an id of more than kFew parts, from crossing[1 + chunks] down.  Rows are loaded kBatch
+// at a time and added in order.
+constexpr int kFew = 16;
 constexpr int kBatch = 8;
 template <bool SGD>
 __global__ __launch_bounds__(kBlock) void sum_kernel(int n, int Vn, int d, int tpr_log2, int len,
@@ -303,7 +319,7 @@ __global__ __launch_bounds__(kBlock) void sum_kernel(int n, int Vn, int d, int t
                                                      const float* __restrict__ dY, int64_t ldy,
                                                      float lr, float* __restrict__ out,
                                                      int64_t ldo, float* __restrict__ part,
-                                                     int64_t ldp) {
+                                                     int64_t ldp, int* __restrict__ crossing) {
   const int lane = threadIdx.x & ((1 << tpr_log2) - 1);
   const int64_t c = (static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x) >> tpr_log2;
   const int64_t b64 = c * len;
@@ -345,54 +361,98 @@ __global__ __launch_bounds__(kBlock) void sum_kernel(int n, int Vn, int d, int t
     }
   }
   if (head) store_vec<kV>(part + 2 * c * ldp + j, acc);
-  else if (e < n && keys[e] == cur) store_vec<kV>(part + (2 * c + 1) * ldp + j, acc);
-  else finish<SGD>(out + cur * ldo + j, d - j, acc, scale, lr);
+  else if (e < n && keys[e] == cur) {
+    store_vec<kV>(part + (2 * c + 1) * ldp + j, acc);
+    if (j == 0) {
+      const int64_t far = b64 + static_cast<int64_t>(kFew) * len;   // the id's part kFew begins here
+      if (far < n && keys[far] == cur) crossing[1 + (n + len - 1) / len - atomicAdd(crossing + 1, 1)] = static_cast<int>(c);
+      else crossing[2 + atomicAdd(crossing, 1)] = static_cast<int>(c);
+    }
+  } else finish<SGD>(out + cur * ldo + j, d - j, acc, scale, lr);
 }
 
-// Ids that cross chunk borders: the group of the chunk where such an id begins
-// adds its parts in chunk order.
-template <bool SGD>
-__global__ __launch_bounds__(kBlock) void join_kernel(int n, int Vn, int d, int tpr_log2, int len,
-                                                      const int* __restrict__ keys, float scale,
-                                                      float lr, float* __restrict__ out,
-                                                      int64_t ldo, const float* __restrict__ part,
-                                                      int64_t ldp) {
-  const int lane = threadIdx.x & ((1 << tpr_log2) - 1);
-  const int64_t c = (static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x) >> tpr_log2;
-  const int64_t b = c * len, e = b + len;
-  if (e >= n) return;   // the last chunk: nothing goes on
-  const int j = kV * (lane + (static_cast<int>(blockIdx.y) << tpr_log2));
-  if (j >= d) return;
-  const int cur = keys[e - 1];
-  if (cur == Vn || keys[e] != cur) return;
-  if (keys[b] == cur && b > 0 && keys[b - 1] == cur) return;   // began earlier
-  // the id's last position, by bisection: its parts are those of chunks c + 1 .. last
-  int lo = static_cast<int>(e), hi = n;   // keys[lo] == cur, keys[hi] != cur or hi == n
-  while (hi - lo > 1) {
-    const int mid = lo + ((hi - lo) >> 1);
-    if (keys[mid] == cur) lo = mid;
-    else hi = mid;
-  }
-  const int64_t last = lo / len;
-  float acc[kV];
-  load_vec<GIST_STORE_F32, kV>(part, (2 * c + 1) * ldp + j, acc);
-  int64_t x = c + 1;
-  for (; x + kBatch <= last + 1; x += kBatch) {
+// Ids that cross chunk borders: the parts of a listed chunk's id are added in chunk
+// order.  Most have two or three parts and take a group of threads each.  A
+// frequent id takes a workgroup per 128 columns, 32 groups of 32 threads, each
+// adding a run of the parts, and then the runs' sums in order.  (131,072 ids of
+// 50,000 by a power law, 1,024 columns: 25 us with a group per id, whose longest, 262
+// parts, took that long; 16 so.)
+constexpr int kJoinThreads = 1024, kJoinBlocks = 256, kSlabLog2 = 5;
+
+// Sum of parts x0 .. x1 - 1 of the id that begins in chunk c (part 0 is that
+// chunk's second), column j.
+__device__ __forceinline__ void add_parts(const float* part, int64_t ldp, int64_t c, int64_t x0, int64_t x1, int j,
+                                          float (&acc)[kV]) {
+  for (int64_t x = x0; x < x1; x += kBatch) {
     float y[kBatch][kV];
 #pragma unroll
-    for (int u = 0; u < kBatch; ++u) load_vec<GIST_STORE_F32, kV>(part, 2 * (x + u) * ldp + j, y[u]);
+    for (int u = 0; u < kBatch; ++u) {
+      const int64_t i = min(x + u, x1 - 1);
+      load_vec<GIST_STORE_F32, kV>(part, (2 * (c + i) + (i == 0)) * ldp + j, y[u]);
+    }
 #pragma unroll
     for (int u = 0; u < kBatch; ++u)
+      if (x + u < x1) {
 #pragma unroll
-      for (int q = 0; q < kV; ++q) acc[q] += y[u][q];
+        for (int q = 0; q < kV; ++q) acc[q] += y[u][q];
+      }
   }
-  for (; x <= last; ++x) {
-    float y[kV];
-    load_vec<GIST_STORE_F32, kV>(part, 2 * x * ldp + j, y);
+}
+
+template <bool SGD>
+__global__ __launch_bounds__(kJoinThreads) void join_kernel(int n, int d, int tpr_log2, int len,
+                                                            const int* __restrict__ keys, float scale,
+                                                            float lr, float* __restrict__ out,
+                                                            int64_t ldo, const float* __restrict__ part,
+                                                            int64_t ldp, const int* __restrict__ crossing) {
+  __shared__ float sh[kJoinThreads][kV];
+  const int t = threadIdx.x, chunks = (n + len - 1) / len;
+  // chunk x begins with the id (then all of the chunk before it, from c + 1 on, is the id's)
+  auto begins = [&](int64_t x, int cur) { return x * len < n && keys[x * len] == cur; };
+  if (blockIdx.x >= kJoinBlocks) {   // ids of few parts
+    const int lane = t & ((1 << tpr_log2) - 1), groups = kJoinThreads >> tpr_log2, listed = crossing[0];
+    for (int it = (blockIdx.x - kJoinBlocks) * groups + (t >> tpr_log2); it < listed; it += (gridDim.x - kJoinBlocks) * groups) {
+      const int64_t c = crossing[2 + it];
+      const int cur = keys[(c + 1) * len];
+      int count = 2;
 #pragma unroll
-    for (int q = 0; q < kV; ++q) acc[q] += y[q];
+      for (int x = 2; x < kFew; ++x) count += begins(c + x, cur);
+      for (int j = kV * lane; j < d; j += kV << tpr_log2) {
+        float acc[kV] = {};
+        add_parts(part, ldp, c, 0, count, j, acc);
+        finish<SGD>(out + cur * ldo + j, d - j, acc, scale, lr);
+      }
+    }
+    return;
   }
-  finish<SGD>(out + cur * ldo + j, d - j, acc, scale, lr);
+  constexpr int kGroups = kJoinThreads >> kSlabLog2, kSlab = kV << kSlabLog2;
+  const int lane = t & ((1 << kSlabLog2) - 1), grp = t >> kSlabLog2;
+  const int slabs = (d + kSlab - 1) / kSlab;
+  const int64_t units = static_cast<int64_t>(crossing[1]) * slabs;
+  for (int64_t it = blockIdx.x; it < units; it += kJoinBlocks) {
+    const int64_t c = crossing[1 + chunks - it / slabs];
+    const int j = static_cast<int>(it % slabs) * kSlab + kV * lane;
+    const int cur = keys[(c + 1) * len];
+    int64_t count = 1;
+    for (int64_t x = c + 1;; x += kJoinThreads) {
+      const int more = __syncthreads_count(begins(x + t, cur));   // and sh is read
+      count += more;
+      if (more < kJoinThreads) break;
+    }
+    const int64_t run = (count + kGroups - 1) / kGroups;
+    const int64_t x0 = min<int64_t>(count, grp * run), x1 = min<int64_t>(count, x0 + run);
+    float acc[kV] = {};
+    if (j < d) add_parts(part, ldp, c, x0, x1, j, acc);
+#pragma unroll
+    for (int q = 0; q < kV; ++q) sh[t][q] = acc[q];
+    __syncthreads();
+    if (grp == 0 && j < d) {
+      for (int g = 1; g < kGroups && g * run < count; ++g)
+#pragma unroll
+        for (int q = 0; q < kV; ++q) acc[q] += sh[(g << kSlabLog2) + lane][q];
+      finish<SGD>(out + cur * ldo + j, d - j, acc, scale, lr);
+    }
+  }
 }
 
 // Zero rows that no id names (dense gradient): a wave per 64 rows, each lane
@@ -426,8 +486,8 @@ size_t up256(size_t x) { return (x + 255) & ~size_t(255); }
 struct GradPlan {
   int64_t tiles, chunks, ldp;
   int len, passes;
-  size_t keys, hist, part;
-  size_t total() const { return 4 * keys + hist + part; }
+  size_t keys, hist, part, cross;
+  size_t total() const { return 4 * keys + hist + part + cross; }
 };
 
 GradPlan plan(int64_t n, int64_t V, int d) {
@@ -442,6 +502,7 @@ GradPlan plan(int64_t n, int64_t V, int d) {
   p.keys = up256(static_cast<size_t>(n) * 4);
   p.hist = up256(static_cast<size_t>(p.tiles) * kBins * 4);
   p.part = up256(static_cast<size_t>(p.chunks) * 2 * p.ldp * 4);
+  p.cross = up256(static_cast<size_t>(p.chunks + 2) * 4);
   return p;
 }
 
@@ -476,19 +537,20 @@ gist_status embed_grad(hipStream_t st, int64_t n, int64_t V, int d, const int32_
   int* q[2] = {reinterpret_cast<int*>(c + 2 * p.keys), reinterpret_cast<int*>(c + 3 * p.keys)};
   int* hist = reinterpret_cast<int*>(c + 4 * p.keys);
   float* part = reinterpret_cast<float*>(c + 4 * p.keys + p.hist);
+  int* cross = reinterpret_cast<int*>(c + 4 * p.keys + p.hist + p.part);
   const int ni = static_cast<int>(n), vi = static_cast<int>(V), tiles = static_cast<int>(p.tiles);
   int cur = 0;
   if (n > 0 && n <= kSmall) {
     ProfScope ps(st, "embed_sort_small", 0.0, 12.0 * n);
-    small_sort_kernel<<<1, kSmallThreads, 0, st>>>(ni, vi, ids, p.passes, k[0], q[0]);
+    small_sort_kernel<<<1, kSmallThreads, 0, st>>>(ni, vi, ids, p.passes, k[0], q[0], cross);
   } else if (n > 0) {
     ProfScope ps(st, "embed_sort", 0.0, 8.0 * n * p.passes);
     for (int i = 0; i < p.passes; ++i) {
       const int* kin = i == 0 ? ids : k[cur ^ 1];
       const int shift = i * kDigit;
       const dim3 g(static_cast<unsigned>(tiles));
-      if (i == 0) hist_kernel<true><<<g, kBlock, 0, st>>>(ni, vi, kin, shift, tiles, hist);
-      else hist_kernel<false><<<g, kBlock, 0, st>>>(ni, vi, kin, shift, tiles, hist);
+      if (i == 0) hist_kernel<true><<<g, kBlock, 0, st>>>(ni, vi, kin, shift, tiles, hist, cross);
+      else hist_kernel<false><<<g, kBlock, 0, st>>>(ni, vi, kin, shift, tiles, hist, cross);
       scan_kernel<<<1, 1024, 0, st>>>(p.tiles * kBins, hist);
       if (i == 0)
         scatter_digit_kernel<true><<<g, kBlock, 0, st>>>(ni, vi, kin, nullptr, shift, tiles, hist,
@@ -516,17 +578,16 @@ gist_status embed_grad(hipStream_t st, int64_t n, int64_t V, int d, const int32_
       ProfScope ps(st, "embed_sum", static_cast<double>(n) * d, 8.0 * n * d);
       if (sgd)
         sum_kernel<true><<<g, kBlock, 0, st>>>(ni, vi, d, tl, p.len, k[cur], q[cur], scale, dY, ldy, lr, out, ldo,
-                                               part, p.ldp);
+                                               part, p.ldp, cross);
       else
         sum_kernel<false><<<g, kBlock, 0, st>>>(ni, vi, d, tl, p.len, k[cur], q[cur], scale, dY, ldy, lr, out, ldo,
-                                                part, p.ldp);
+                                                part, p.ldp, cross);
     }
     if (p.chunks > 1) {
       ProfScope ps(st, "embed_join", 0.0, 0.0);
-      if (sgd)
-        join_kernel<true><<<g, kBlock, 0, st>>>(ni, vi, d, tl, p.len, k[cur], scale, lr, out, ldo, part, p.ldp);
-      else
-        join_kernel<false><<<g, kBlock, 0, st>>>(ni, vi, d, tl, p.len, k[cur], scale, lr, out, ldo, part, p.ldp);
+      const dim3 gj(2 * kJoinBlocks);   // 1,024 threads each: two a CU
+      if (sgd) join_kernel<true><<<gj, kJoinThreads, 0, st>>>(ni, d, tl, p.len, k[cur], scale, lr, out, ldo, part, p.ldp, cross);
+      else join_kernel<false><<<gj, kJoinThreads, 0, st>>>(ni, d, tl, p.len, k[cur], scale, lr, out, ldo, part, p.ldp, cross);
     }
   }
   return check_launch("embed_grad");

@@ -283,7 +283,7 @@ __global__ __launch_bounds__(kBlock) void rows_kernel(int64_t items, int parts, 
                                                       const void* __restrict__ Z, int64_t ldz,
                                                       Out o, int K, float* __restrict__ pstat,
                                                       u64* __restrict__ ptop) {
-  constexpr int V = STORE == GIST_STORE_F32 ? 4 : 8;
+  constexpr int V = STORE == GIST_STORE_F32 ? 4 : 8, kU = 2;
   __shared__ Stat wst[kWaves];
   __shared__ u64 wtop[kWaves][64];
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
@@ -294,44 +294,58 @@ __global__ __launch_bounds__(kBlock) void rows_kernel(int64_t items, int parts, 
     Stat a{-INFINITY, 0.f, 0.f};
     Top top;
     top.K = K;
-    for (int64_t j0 = c0; j0 < c1; j0 += V * kBlock) {   // block-uniform: ballots inside
-      const int64_t j = j0 + V * t;
-      float z[V];
-      load_some<STORE, V>(Z, row * ldz + j, c1 - j, -INFINITY, z);
-      float m = z[0];
+    // kU vectors a step: both loads are out before either is used, and the sums
+    // are rescaled once for both
+    for (int64_t j0 = c0; j0 < c1; j0 += kU * V * kBlock) {   // block-uniform: ballots inside
+      float z[kU][V], m = -INFINITY;
 #pragma unroll
-      for (int q = 1; q < V; ++q) m = max_nan(m, z[q]);
+      for (int u = 0; u < kU; ++u) {
+        const int64_t j = j0 + (u * kBlock + t) * V;
+        load_some<STORE, V>(Z, row * ldz + j, c1 - j, -INFINITY, z[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < kU; ++u)
+#pragma unroll
+        for (int q = 0; q < V; ++q) m = max_nan(m, z[u][q]);
       if constexpr (TOP) {
-        if (j0 == c0) {
+        const bool first = j0 == c0;
+        int at = -1;
+        if (first) {
           // The list begins with the lanes' best: most others then fail its K-th.
           u64 best = 0;
-          int at = 0;
 #pragma unroll
-          for (int q = 0; q < V; ++q) {
-            const u64 x = j + q < c1 ? pack(z[q], static_cast<unsigned>(j + q)) : 0;
-            if (x > best) {
-              best = x;
-              at = q;
+          for (int u = 0; u < kU; ++u)
+#pragma unroll
+            for (int q = 0; q < V; ++q) {
+              const int64_t j = j0 + (u * kBlock + t) * V + q;
+              const u64 x = j < c1 ? pack(z[u][q], static_cast<unsigned>(j)) : 0;
+              if (x > best) {
+                best = x;
+                at = u * V + q;
+              }
             }
-          }
           top.sort(best, lane);
+        }
+        if (__any(pack(m, 0u) > top.thr)) {
 #pragma unroll
-          for (int q = 0; q < V; ++q)
-            top.offer(j + q < c1 && q != at ? pack(z[q], static_cast<unsigned>(j + q)) : 0, lane);
-        } else if (__any(j < c1 && pack(m, 0u) > top.thr)) {
+          for (int u = 0; u < kU; ++u)
 #pragma unroll
-          for (int q = 0; q < V; ++q)
-            top.offer(j + q < c1 ? pack(z[q], static_cast<unsigned>(j + q)) : 0, lane);
+            for (int q = 0; q < V; ++q) {
+              const int64_t j = j0 + (u * kBlock + t) * V + q;
+              top.offer(j < c1 && u * V + q != at ? pack(z[u][q], static_cast<unsigned>(j)) : 0, lane);
+            }
         }
       }
       rescale(a, max_nan(a.m, m));
 #pragma unroll
-      for (int q = 0; q < V; ++q) {
-        const float y = fmaxf((z[q] - a.m) * kL, kFloor);
-        const float e = ex2(y);
-        a.s += e;
-        a.t = fmaf(e, y, a.t);
-      }
+      for (int u = 0; u < kU; ++u)
+#pragma unroll
+        for (int q = 0; q < V; ++q) {
+          const float y = fmaxf((z[u][q] - a.m) * kL, kFloor);
+          const float e = ex2(y);
+          a.s += e;
+          a.t = fmaf(e, y, a.t);
+        }
     }
     a = wave_merge(a);
     __syncthreads();   // the previous item's LDS is read
