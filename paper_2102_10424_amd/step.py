@@ -11,6 +11,8 @@ context's stream (torch only provides the device buffers).
   ``subAgg`` (slice scatter), optionally with Adam moments.
 * :func:`gist_train` -- Algorithm 1: T rounds of zeta local steps per
   sub-GCN, with SGD or Adam (the optimizer of the paper's experiments).
+* :class:`LearnedRows` -- a trained table in place of given features: the
+  lookup of a mini-batch's rows and the SGD step on them.
 """
 
 import numpy as np
@@ -821,16 +823,21 @@ class SubGCN:
     GAT: (s_l + 2, s_{l+1}), Theta followed by the rows a_src and a_dst), and
     the gradients ``dW[l]`` have the same layout, so one optimizer call
     updates a layer.  A GAT batch's CSR is the pattern of A + I (the GCN
-    matrix; its values are not read).
+    matrix; its values are not read).  With ``input_grad`` the backward pass
+    also leaves the gradient of the batch's input rows in ``dH[0]`` (for
+    :class:`LearnedRows`).
     """
 
     def __init__(self, ctx, kind, widths, n_cap, dtype=G.GIST_DTYPE_F32, device="cuda",
-                 order=G.GIST_ORDER_AUTO):
+                 order=G.GIST_ORDER_AUTO, input_grad=False):
         if kind not in ("gcn", "sage", "gat"):
             raise ValueError("kind is 'gcn', 'sage' or 'gat'")
         self.ctx = ctx
         self.kind = kind
         self.gat = kind == "gat"
+        self.input_grad = input_grad
+        self.muon_ws = None
+        self.lp = None
         self.nnz_cap = 0
         self.alpha = None
         self.widths = list(widths)
@@ -963,7 +970,7 @@ class SubGCN:
             n, n_in = batch.rows(l + 1), batch.rows(l)
             A, A_T = batch.adj(l)
             Hin = batch.X if l == 0 else self.H[l][:n_in]
-            dH = self.dH[l][:n_in] if l > 0 else None
+            dH = self.dH[l][:n_in] if l > 0 or self.input_grad else None
             if self.gat:
                 W, a1, a2 = self._gat_parts(params[l], l)
                 gW, g1, g2 = self._gat_parts(self.dW[l], l)
@@ -1009,17 +1016,106 @@ class SubGCN:
             G.gist_adam_update_dev(self.ctx, params[l], self.dW[l], M[l], V[l], params[l].numel(),
                                    coef_dev, betas[0], betas[1], eps)
 
-    def step(self, batch, params, lr, adam=None, loss_out=None):
+    def muon_desc(self, l, fresh=False, dtype=None):
+        """Layer l's weights as the matrices Muon steps: GCN one, SAGE [W_self;
+        W_neigh] two, GAT Theta."""
+        return G.muon_desc(self.widths[l], self.widths[l + 1],
+                           groups=2 if self.kind == "sage" else 1,
+                           dtype=G.GIST_DTYPE_F32 if dtype is None else dtype,
+                           flags=G.GIST_MUON_NESTEROV | (G.GIST_MUON_FRESH if fresh else 0))
+
+    def prepare_muon(self, dtype=None):
+        """Allocate the workspace :meth:`muon` needs (before a capture)."""
+        need = max(G.gist_muon_workspace_size(self.muon_desc(l, dtype=dtype))
+                   for l in range(self.L))
+        if self.muon_ws is None or self.muon_ws.numel() < need:
+            self.muon_ws = torch.empty(need, dtype=torch.uint8, device=self.device)
+
+    def muon(self, params, M, lr, fresh=False, momentum=0.95, weight_decay=0.0, dtype=None):
+        """Muon on every layer's weight matrices with their momenta M[l] (shaped
+        as ``params[l]``), steps of about Adam's size; ``fresh`` restarts the
+        momenta from zero.  A GAT layer's attention vectors take an SGD step."""
+        self.prepare_muon(dtype)
+        for l in range(self.L):
+            r, c = self.widths[l], self.widths[l + 1]
+            G.gist_muon_update(self.ctx, self.muon_desc(l, fresh, dtype), params[l], self.dW[l],
+                               M[l], lr, momentum, weight_decay, 0.2 * max(r, c) ** 0.5,
+                               self.muon_ws)
+            if self.gat:
+                G.gist_sgd_update(self.ctx, params[l][r:], self.dW[l][r:], 2 * c, lr)
+
+    def log_probs(self, batch, K=0):
+        """Of the last forward pass's logits: the labels' log probabilities, every
+        row's entropy and log-sum-exp, and its K best classes (``top_logp``,
+        ``top_idx``), as a dict of device tensors that the next call reuses."""
+        n, C = batch.rows(self.L), self.widths[-1]
+        ws = G.gist_log_probs_workspace(n, C, K)
+        if self.lp is None or self.lp["n"] < n or self.lp["K"] != K or self.lp["ws"].numel() < ws:
+            f = lambda *s: torch.empty(*s, device=self.device)
+            self.lp = dict(n=n, K=K, logp=f(n), entropy=f(n), lse=f(n), top_logp=f(n, K),
+                           top_idx=torch.empty(n, K, dtype=torch.int32, device=self.device),
+                           ws=torch.empty(max(ws, 16), dtype=torch.uint8, device=self.device))
+        p = self.lp
+        G.gist_log_probs(self.ctx, n, C, self.H[self.L], C, G.GIST_STORE_F32, batch.labels,
+                         p["logp"], p["entropy"], p["lse"], K, p["top_logp"] if K else None,
+                         p["top_idx"] if K else None, p["ws"])
+        return {k: p[k][:n] for k in ("logp", "entropy", "lse", "top_logp", "top_idx")}
+
+    def log_probs_grad(self, batch, g_logp, g_entropy=None):
+        """In place of :meth:`loss_and_grad`, after :meth:`log_probs`: ``dlogits`` of
+        sum(g_logp * logp + g_entropy * entropy)."""
+        n, C = batch.rows(self.L), self.widths[-1]
+        G.gist_log_probs_bwd(self.ctx, n, C, self.H[self.L], C, G.GIST_STORE_F32, batch.labels,
+                             self.lp["lse"], self.lp["entropy"], g_logp, g_entropy, self.dlogits, C)
+
+    def step(self, batch, params, lr, adam=None, loss_out=None, muon=None):
         """``subTrain``: forward, loss, backward, update (all enqueued, nothing
-        synced).  ``adam`` = (M, V, step, fresh) selects Adam, else SGD."""
+        synced).  ``adam`` = (M, V, step, fresh) selects Adam, ``muon`` = (M,
+        fresh) Muon, else SGD."""
         self.forward(batch, params)
         self.loss_and_grad(batch, loss_out)
-        if adam is None:
+        if muon is not None:
+            self.backward(batch, params)
+            self.muon(params, muon[0], lr, muon[1])
+        elif adam is None:
             self.backward(batch, params, sgd_lr=lr)
         else:
             self.backward(batch, params)
             M, V, k, fresh = adam
             self.adam(params, M, V, lr, k, fresh)
+
+
+class LearnedRows:
+    """A learned table (``table``: N x d fp32 on the device) whose scaled rows
+    are a graph's features: ``lookup`` fills a mini-batch's input rows in place
+    of the gather of given ones, ``sgd`` steps the rows that were looked up by
+    the input gradient of a ``SubGCN(input_grad=True)``.  ``ids`` are device
+    int32 node ids (a batch's node map); ids outside the table are padding."""
+
+    def __init__(self, ctx, table, scale=1.0, n_cap=0, device="cuda"):
+        self.ctx, self.table, self.scale, self.device = ctx, table, float(scale), device
+        self.N, self.d = table.shape
+        self.n_cap = 0
+        self.ws = None
+        if n_cap:
+            self._reserve(n_cap)
+
+    def _reserve(self, n):
+        if n > self.n_cap:
+            need = G.gist_embed_grad_workspace(n, self.N, self.d)
+            self.ws = torch.empty(need, dtype=torch.uint8, device=self.device)
+            self.n_cap = n
+
+    def lookup(self, ids, n, X):
+        """X[:n] = scale * table[ids[:n]]."""
+        G.gist_embed_lookup(self.ctx, n, self.N, self.d, self.table, self.d, G.GIST_STORE_F32, ids,
+                            self.scale, X, self.d)
+
+    def sgd(self, ids, n, dX, lr):
+        """The SGD step of the looked-up rows, from the gradient dX of X."""
+        self._reserve(n)
+        G.gist_embed_grad_sgd(self.ctx, n, self.N, self.d, ids, self.scale, dX, self.d, lr,
+                              self.table, self.d, self.ws)
 
 
 class SubGCNBatch:
