@@ -33,6 +33,9 @@ constexpr float kS = 4096.f, kInvS = 1.f / 4096.f;
 constexpr int kNormBlocks = 512;
 
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef _Float16 half4 __attribute__((ext_vector_type(4)));
+typedef unsigned uintx2 __attribute__((ext_vector_type(2)));
+typedef unsigned uintx4 __attribute__((ext_vector_type(4)));
 typedef float floatx2 __attribute__((ext_vector_type(2)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
@@ -160,11 +163,8 @@ __device__ __forceinline__ void wave_sync() {
 struct Divisor {
   float pre, div;
 };
-__device__ __forceinline__ Divisor divisor(const double* __restrict__ part, int64_t g, int nparts, float eps,
-                                           double* sh) {
-  double s = 0.0;
-  for (int i = threadIdx.x; i < nparts; i += kBlock) s += part[g * kNormBlocks + i];
-  double norm = sqrt(block_sum(s, sh));
+__device__ __forceinline__ Divisor divisor_of(double squares, float eps) {
+  double norm = sqrt(squares);
   Divisor d{1.f, 0.f};
   if (norm > 1e30) {
     d.pre = 0x1p-64f;
@@ -172,6 +172,12 @@ __device__ __forceinline__ Divisor divisor(const double* __restrict__ part, int6
   }
   d.div = norm < static_cast<double>(eps) ? eps : static_cast<float>(norm);   // NaN stays
   return d;
+}
+__device__ __forceinline__ Divisor divisor(const double* __restrict__ part, int64_t g, int nparts, float eps,
+                                           double* sh) {
+  double s = 0.0;
+  for (int i = threadIdx.x; i < nparts; i += kBlock) s += part[g * kNormBlocks + i];
+  return divisor_of(block_sum(s, sh), eps);
 }
 
 // U / norm, split, as it stands (D) and transposed (T); 64 x 64 tiles over the
@@ -579,6 +585,397 @@ __global__ __launch_bounds__(kBlock) void join_kernel(Sched S, const float* __re
                          scratch[threadIdx.x >> 6]);
 }
 
+// ---- matrices with a side of up to 128 -------------------------------------------------
+//
+// A workgroup keeps a slab of 128 columns of X (both ways round) in LDS, computes
+// A and B itself and steps its slab; slabs meet only in A, whose parts (one per
+// slab) go through memory from one launch to the next.  So a step is one launch
+// instead of three, and one slab (n <= 128) takes all steps in one.
+// B = b A + c A A is symmetric: a block B[k][r] as an MFMA result, lane = column r,
+// four k in a lane's registers, is B[r][k] in the layout of an MFMA operand but for
+// which half of the wave holds which four of eight k.
+
+constexpr int kSlab = 128, kSmallThreads = 512, kSmallWaves = 8;
+
+struct SmallArgs {
+  int64_t rows, cols;
+  int m, n, slabs, flip;
+  const float* G;
+  float *M, *W;
+  void* O;
+  Update u;
+  const double* norm;      // sums of squares (slabs > 1)
+  int nparts;
+  float eps, ca, cb, cc;
+  int first, k0, k1, steps;
+  const float* pin;        // A's parts of the last launch
+  float* pout;
+  char* T;                 // the slabs between launches, as they lie in LDS
+};
+
+// Byte of value k, part p in a row, and its place: pieces of 16 bytes in an order
+// that spreads a column of rows over the banks.
+template <int NP, int RB>
+__device__ __forceinline__ int small_at(int row, int k, int p) {
+  const int byte = NP == 1 ? 2 * k : (k >> 5) * 128 + p * 64 + (k & 31) * 2;
+  const int swz = RB >= 256 ? row & 15 : row >> 1 & 7;
+  return row * RB + (((byte >> 4) ^ swz) << 4) + (byte & 15);
+}
+// The same for an MFMA fragment (row li of a block of 32, k = 16 d + 8 lh): a lane's
+// base, into which depth and part go by exclusive or; blocks are 32 RB apart.
+template <int RB>
+__device__ __forceinline__ int small_base(int li, int lh) {
+  return li * RB + (((RB >= 256 ? li & 15 : li >> 1 & 7) ^ lh) << 4);
+}
+// A copy the compiler cannot see through: addresses are then formed where they are
+// used, rather than kept, by the dozen, in registers across the loop.
+__device__ __forceinline__ int fresh(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+template <int NP>
+__device__ __forceinline__ void small_frag(const char* r, int base, int d, half8 (&f)[NP]) {
+#pragma unroll
+  for (int p = 0; p < NP; ++p)
+    f[p] = *reinterpret_cast<const half8*>(r + (base ^ (NP == 1 ? 32 * d : (d >> 1) * 128 + p * 64 + (d & 1) * 32)));
+}
+// Four consecutive values k .. k + 3 of row li, k = K0 + 8 r4 + 4 lh with K0 a multiple
+// of 32: a lane's base and, by exclusive or, K0, r4 and the part.
+template <int RB>
+__device__ __forceinline__ int quad_base(int li, int lh) {
+  return li * RB + ((RB >= 256 ? li & 15 : li >> 1 & 7) << 4) + 8 * lh;
+}
+template <int NP>
+__device__ __forceinline__ int quad_at(int k0, int r4, int p) {
+  return (NP == 1 ? 2 * k0 : 4 * k0 + 64 * p) + 16 * r4;
+}
+// One value of row R0 + 8 r4 + 4 lh + q (R0 a multiple of 32) at k = K0 + li.
+template <int RB>
+__device__ __forceinline__ int cross_base(int li, int lh) {
+  return 4 * lh * RB + (((li >> 3) ^ (RB >= 256 ? 4 * lh : 2 * lh)) << 4) + (li & 7) * 2;
+}
+template <int NP, int RB>
+__device__ __forceinline__ int cross_at(int k0, int r4, int q, int p) {
+  return (NP == 1 ? 2 * k0 : 4 * k0 + 64 * p) ^ ((RB >= 256 ? 8 * (r4 & 1) + q : 4 * (r4 & 1) + (q >> 1)) << 4);
+}
+template <int NP>
+__device__ __forceinline__ floatx4 get_quad(const char* r, int base, int k0, int r4) {
+  floatx4 v = __builtin_convertvector(*reinterpret_cast<const half4*>(r + (base ^ quad_at<NP>(k0, r4, 0))), floatx4);
+  if constexpr (NP == 2)
+    v += __builtin_convertvector(*reinterpret_cast<const half4*>(r + (base ^ quad_at<NP>(k0, r4, 1))), floatx4);
+  return v;
+}
+template <int NP>
+__device__ __forceinline__ void split4(floatx4 v, half4 (&h)[NP]) {
+  h[0] = __builtin_convertvector(v, half4);
+  if constexpr (NP == 2) h[1] = __builtin_convertvector(v - __builtin_convertvector(h[0], floatx4), half4);
+}
+template <int NP>
+__device__ __forceinline__ void put_quad(char* r, int base, int k0, int r4, const half4 (&h)[NP]) {
+#pragma unroll
+  for (int p = 0; p < NP; ++p) *reinterpret_cast<half4*>(r + (base ^ quad_at<NP>(k0, r4, p))) = h[p];
+}
+// The four as values of four rows (r: the first row's block).
+template <int NP, int RB>
+__device__ __forceinline__ void put_cross(char* r, int base, int k0, int r4, const half4 (&h)[NP]) {
+#pragma unroll
+  for (int p = 0; p < NP; ++p)
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      *reinterpret_cast<_Float16*>(r + (8 * r4 + q) * RB + (base ^ cross_at<NP, RB>(k0, r4, q, p))) = h[p][q];
+}
+template <int NP, int RB>
+__device__ __forceinline__ void small_put1(char* r, int row, int k, float v) {
+  _Float16 s[NP];
+  parts_of<NP>(v, s);
+#pragma unroll
+  for (int p = 0; p < NP; ++p) *reinterpret_cast<_Float16*>(r + small_at<NP, RB>(row, k, p)) = s[p];
+}
+template <int NP>
+__device__ __forceinline__ void mma(floatx16& acc, const half8 (&a)[NP], const half8 (&b)[NP]) {
+  if constexpr (NP == 2) {
+    acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[0], b[1], acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[1], b[0], acc, 0, 0, 0);
+  }
+  acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[0], b[0], acc, 0, 0, 0);
+}
+// Block b of the lower triangle of blocks, row by row.
+__device__ __forceinline__ void lower_block(int b, int& rb, int& cb) {
+  rb = b < 1 ? 0 : b < 3 ? 1 : b < 6 ? 2 : 3;
+  cb = b - rb * (rb + 1) / 2;
+}
+
+template <int NP, int MP, bool UPDATE>
+__global__ __launch_bounds__(kSmallThreads, 2) void small_kernel(SmallArgs a) {
+  constexpr int RT = MP * NP * 2, RX = kSlab * NP * 2;      // bytes of a row of A and X^T, of X
+  constexpr int NRB = MP / 32, LOW = NRB * (NRB + 1) / 2;   // 32-row blocks, blocks of the lower triangle
+  constexpr int KD = MP / 16, NB = NRB / 2;                 // depths of K = MP, column blocks per wave
+  constexpr int OWN = (LOW + kSmallWaves - 1) / kSmallWaves;
+  constexpr int KPG = NRB * NRB > kSmallWaves ? NRB * NRB / kSmallWaves : 1;   // blocks of B per wave
+  __shared__ __attribute__((aligned(16))) char ra[MP * RX];   // A (RT <= RX), then the new X
+  __shared__ __attribute__((aligned(16))) char rt[kSlab * RT];
+  __shared__ double red[kSmallWaves];
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, li = lane & 31, lh = lane >> 5;
+  const int slab = blockIdx.x;
+  const int64_t g = blockIdx.y, off = g * a.rows * a.cols;
+  const int rb = wave % NRB, cg = wave / NRB;
+  auto elem = [&](int i, int j) { return off + (a.flip ? (slab * kSlab + j) * a.cols + i : i * a.cols + slab * kSlab + j); };
+  char* const tg = a.T + (g * a.slabs + slab) * (kSlab * RT);
+  float* const pout = a.pout + (g * a.slabs + slab) * (LOW * 1024);
+  floatx16 low[OWN];   // this wave's blocks of A
+
+  // A's blocks, to LDS: both triangles.
+  auto put_a = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int x = 0; x < OWN; ++x) {
+      const int b = wave + x * kSmallWaves;
+      if (b >= LOW) continue;
+      int br, bc;
+      lower_block(b, br, bc);
+      const int qb = fresh(quad_base<RT>(li, lh)), xb = fresh(cross_base<RT>(li, lh));
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) {
+        half4 h[NP];
+        split4<NP>(floatx4{low[x][4 * r4], low[x][4 * r4 + 1], low[x][4 * r4 + 2], low[x][4 * r4 + 3]} * kInvS, h);
+        put_quad<NP>(ra + bc * 32 * RT, qb, br * 32, r4, h);
+        if (br != bc) put_cross<NP, RT>(ra + br * 32 * RT, xb, bc * 32, r4, h);
+      }
+    }
+  };
+  // A's blocks from X, to the last part of K this slab has.
+  auto gram = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int x = 0; x < OWN; ++x) {
+      const int b = wave + x * kSmallWaves;
+      low[x] = floatx16{};
+      if (b >= LOW) continue;
+      int br, bc;
+      lower_block(b, br, bc);
+      const int fb = fresh(small_base<RX>(li, lh));
+#pragma unroll
+      for (int d = 0; d < kSlab / 16; ++d) {
+        half8 p[NP], q[NP];
+        small_frag<NP>(ra + br * 32 * RX, fb, d, p);
+        small_frag<NP>(ra + bc * 32 * RX, fb, d, q);
+        mma<NP>(low[x], p, q);
+        if (d & 1) __builtin_amdgcn_sched_barrier(0);   // else all reads come first, into too many registers
+      }
+    }
+    if (a.slabs == 1) {
+      __syncthreads();   // X is read: A takes its place
+      put_a();
+    } else {
+#pragma unroll
+      for (int x = 0; x < OWN; ++x) {
+        const int b = wave + x * kSmallWaves;
+        if (b >= LOW) continue;
+        floatx4* d = reinterpret_cast<floatx4*>(pout + b * 1024) + lane;
+#pragma unroll
+        for (int r4 = 0; r4 < 4; ++r4)
+          d[r4 * 64] = floatx4{low[x][4 * r4], low[x][4 * r4 + 1], low[x][4 * r4 + 2], low[x][4 * r4 + 3]};
+      }
+    }
+  };
+  auto save_slab = [&]() __attribute__((always_inline)) {
+    for (int x = t * 16; x < kSlab * RT; x += kSmallThreads * 16)
+      *reinterpret_cast<uint4*>(tg + x) = *reinterpret_cast<const uint4*>(rt + x);
+  };
+
+  if (a.first) {
+    constexpr int PER = MP * kSlab / kSmallThreads;
+    float v[PER], mo[UPDATE ? PER : 1];
+    auto place = [&](int x, int& i, int& j) __attribute__((always_inline)) {   // in the matrix?
+      const int e = x * kSmallThreads + t;
+      i = a.flip ? e & (MP - 1) : e / kSlab;
+      j = a.flip ? e / MP : e & (kSlab - 1);
+      return i < a.m && slab * kSlab + j < a.n;
+    };
+    // every load is made, at the group's first element outside the matrix: none waits for
+    // another behind a branch
+#pragma unroll
+    for (int x = 0; x < PER; ++x) {
+      int i, j;
+      const int64_t at = place(x, i, j) ? elem(i, j) : off;
+      v[x] = a.G[at];
+      if constexpr (UPDATE) mo[x] = a.u.fresh && a.slabs == 1 ? 0.f : a.M[at];
+    }
+    double s = 0.0;
+#pragma unroll
+    for (int x = 0; x < PER; ++x) {
+      int i, j;
+      const bool in = place(x, i, j);
+      if constexpr (UPDATE) {
+        if (a.slabs == 1) {   // else norm_kernel has stepped it
+          mo[x] = fmaf(a.u.momentum, mo[x], a.u.omu * v[x]);
+          if (in) a.M[elem(i, j)] = mo[x];
+        }
+        v[x] = direction(a.u, v[x], mo[x]);
+      }
+      if (!in) v[x] = 0.f;
+      s += static_cast<double>(v[x]) * v[x];
+    }
+    if (a.slabs > 1) {
+      s = 0.0;
+      for (int x = t; x < a.nparts; x += kSmallThreads) s += a.norm[g * kNormBlocks + x];
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+    if (lane == 0) red[wave] = s;
+    __syncthreads();
+    s = 0.0;
+    for (int w = 0; w < kSmallWaves; ++w) s += red[w];
+    const Divisor dv = divisor_of(s, a.eps);
+#pragma unroll
+    for (int x = 0; x < PER; ++x) {
+      int i, j;
+      place(x, i, j);
+      const float y = kS * (v[x] * dv.pre / dv.div);
+      small_put1<NP, RT>(rt, j, i, y);
+      small_put1<NP, RX>(ra, i, j, y);
+    }
+    __syncthreads();
+    gram();
+    if (a.slabs > 1) save_slab();
+  } else {
+    for (int x = t * 16; x < kSlab * RT; x += kSmallThreads * 16)
+      *reinterpret_cast<uint4*>(rt + x) = *reinterpret_cast<const uint4*>(tg + x);
+    // A: the slabs' parts, in order
+#pragma unroll
+    for (int x = 0; x < OWN; ++x) {
+      const int b = wave + x * kSmallWaves;
+      low[x] = floatx16{};
+      if (b >= LOW) continue;
+      const floatx4* d = reinterpret_cast<const floatx4*>(a.pin + g * a.slabs * (LOW * 1024) + b * 1024) + lane;
+#pragma unroll 4
+      for (int y = 0; y < a.slabs; ++y) {
+#pragma unroll
+        for (int r4 = 0; r4 < 4; ++r4) {
+          const floatx4 w = d[y * (LOW * 256) + r4 * 64];
+#pragma unroll
+          for (int q = 0; q < 4; ++q) low[x][4 * r4 + q] += w[q];
+        }
+      }
+    }
+    put_a();
+  }
+  for (int k = a.k0; k < a.k1; ++k) {
+    __syncthreads();
+    // B: a wave computes KPG of its rows' blocks and the waves of the same rows trade
+    // them through LDS, in A's place
+    half4 mine[KPG][4][NP];
+    if (cg < NRB / KPG) {
+#pragma unroll
+      for (int x = 0; x < KPG; ++x) {
+        const int kb = cg * KPG + x;
+        floatx16 acc = {};
+        const int fb = fresh(small_base<RT>(li, lh));
+#pragma unroll
+        for (int d = 0; d < KD; ++d) {
+          half8 p[NP], q[NP];
+          small_frag<NP>(ra + kb * 32 * RT, fb, d, p);
+          small_frag<NP>(ra + rb * 32 * RT, fb, d, q);
+          mma<NP>(acc, p, q);
+          if (d & 1) __builtin_amdgcn_sched_barrier(0);
+        }
+        const int qb = fresh(quad_base<RT>(li, lh));
+#pragma unroll
+        for (int r4 = 0; r4 < 4; ++r4) {
+          const floatx4 v = get_quad<NP>(ra + rb * 32 * RT, qb, kb * 32, r4);
+          const floatx4 c = floatx4{acc[4 * r4], acc[4 * r4 + 1], acc[4 * r4 + 2], acc[4 * r4 + 3]} * (a.cc * kInvS);
+          split4<NP>(a.cb * v + c, mine[x][r4]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    __syncthreads();   // A is read
+    // depth d, part p of rows rb: 1 KB at ((rb KD + d) NP + p), a lane's 16 bytes (eight k) in
+    // two halves: k 0..3 from the lower half of the wave, 4..7 from the upper
+    if (cg < NRB / KPG) {
+#pragma unroll
+      for (int x = 0; x < KPG; ++x)
+#pragma unroll
+        for (int r4 = 0; r4 < 4; ++r4)
+#pragma unroll
+          for (int p = 0; p < NP; ++p) {
+            const int d = 2 * (cg * KPG + x) + (r4 >> 1);
+            *reinterpret_cast<half4*>(ra + (((rb * KD + d) * NP + p) * 64 + (r4 & 1) * 32 + li) * 16 + lh * 8) = mine[x][r4][p];
+          }
+    }
+    __syncthreads();
+    half8 B[KD][NP];   // rows rb of B
+#pragma unroll
+    for (int d = 0; d < KD; ++d)
+#pragma unroll
+      for (int p = 0; p < NP; ++p)
+        B[d][p] = *reinterpret_cast<const half8*>(ra + (((rb * KD + d) * NP + p) * 64 + lane) * 16);
+    floatx4 v[NB][4];
+#pragma unroll
+    for (int y = 0; y < NB; ++y) {
+      const char* const tr = rt + (cg * NB + y) * 32 * RT;
+      const int fb = fresh(small_base<RT>(li, lh)), qb = fresh(quad_base<RT>(li, lh));
+      floatx16 acc = {};
+#pragma unroll
+      for (int d = 0; d < KD; ++d) {
+        half8 q[NP];
+        small_frag<NP>(tr, fb, d, q);
+        mma<NP>(acc, B[d], q);
+        if (d & 1) __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4)
+        v[y][r4] = a.ca * get_quad<NP>(tr, qb, rb * 32, r4) +
+                   floatx4{acc[4 * r4], acc[4 * r4 + 1], acc[4 * r4 + 2], acc[4 * r4 + 3]} * kInvS;
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if (k + 1 == a.steps) {
+#pragma unroll
+      for (int y = 0; y < NB; ++y) {
+        const int j = (cg * NB + y) * 32 + li;
+        const bool jn = slab * kSlab + j < a.n;
+        float w[4][4];
+        if constexpr (UPDATE) {
+#pragma unroll
+          for (int r4 = 0; r4 < 4; ++r4)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              const int i = rb * 32 + 8 * r4 + 4 * lh + q;
+              w[r4][q] = a.W[jn && i < a.m ? elem(i, j) : off];
+            }
+        }
+#pragma unroll
+        for (int r4 = 0; r4 < 4; ++r4)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const int i = rb * 32 + 8 * r4 + 4 * lh + q;
+            const float o = v[y][r4][q] * kInvS;
+            if (jn && i < a.m) {
+              const int64_t e = elem(i, j);
+              if constexpr (UPDATE) a.W[e] = fmaf(-a.u.eta, o, a.u.keep * w[r4][q]);
+              else if constexpr (NP == 1) static_cast<_Float16*>(a.O)[e] = static_cast<_Float16>(o);
+              else static_cast<float*>(a.O)[e] = o;
+            }
+          }
+      }
+      return;
+    }
+    __syncthreads();   // A and X^T are read
+#pragma unroll
+    for (int y = 0; y < NB; ++y) {
+      const int qb = fresh(quad_base<RT>(li, lh)), xb = fresh(cross_base<RX>(li, lh));
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) {
+        half4 h[NP];
+        split4<NP>(v[y][r4], h);
+        put_quad<NP>(rt + (cg * NB + y) * 32 * RT, qb, rb * 32, r4, h);
+        put_cross<NP, RX>(ra + rb * 32 * RX, xb, (cg * NB + y) * 32, r4, h);
+      }
+    }
+    __syncthreads();
+    gram();
+    if (a.slabs > 1) save_slab();
+  }
+}
+
 size_t up256(size_t x) { return (x + 255) & ~size_t(255); }
 
 struct Plan {
@@ -588,7 +985,8 @@ struct Plan {
   bool flip;                  // rows > cols
   size_t norm, x, a;          // bytes: norm partials, one X (or X^T), one A (or B)
   size_t part;                // partial tiles
-  size_t total() const { return norm + 4 * x + 2 * a + part; }
+  int slabs;                  // small_kernel's, 0: products of tiles
+  size_t total() const { return slabs ? norm + x + 2 * a : norm + 4 * x + 2 * a + part; }
 };
 
 // The tiles: side, workgroups the card holds at once, and what a round of them
@@ -652,13 +1050,29 @@ Choice choose(const Plan& p, int64_t M, int64_t N, int64_t K, bool sym) {
   return best;
 }
 
+// Columns up to which slabs are used (each launch reads every slab's part of A).
+// Measured against products of tiles, us: 64 x 64 25 and 69, 64 x 602 52 and 94,
+// 64 x 8,192 89 and 147, 128 x 128 58 and 83 with fp32 products; 15 and 58, 40 and 79,
+// 77 and 132, 31 and 69 with fp16 operands.  Of more than 64 rows and 128 columns: with fp32
+// products 93 and 91 (128 x 256), 202 and 165 (128 x 8,192), an update of 128 x 1,433 134
+// and 115; with fp16 operands 62 and 74, 170 and 144, 82 and 96 (128 x 1,433).
+int64_t small_most(int64_t m, int parts) { return m <= 64 ? 8192 : m > 128 ? 0 : parts == 1 ? 2048 : kSlab; }
+
 Plan plan(const gist_muon_desc* D) {
-  Plan p;
+  Plan p{};
   p.G = D->groups > 1 ? D->groups : 1;
   p.flip = D->rows > D->cols;
   p.m = std::min(D->rows, D->cols);
   p.n = std::max(D->rows, D->cols);
   p.parts = D->dtype == GIST_DTYPE_F32 ? 2 : 1;
+  p.norm = up256(static_cast<size_t>(p.G) * kNormBlocks * sizeof(double));
+  p.slabs = p.n <= small_most(p.m, p.parts) ? static_cast<int>((p.n + kSlab - 1) / kSlab) : 0;
+  if (p.slabs) {   // the slabs, and A's parts of two launches
+    const size_t mp = p.m <= 64 ? 64 : 128, low = p.m <= 64 ? 3 : 10;
+    p.x = up256(static_cast<size_t>(p.G) * p.slabs * kSlab * mp * p.parts * 2);
+    p.a = up256(static_cast<size_t>(p.G) * p.slabs * low * 4096);
+    return p;
+  }
   // Larger padding allows larger tiles; it is taken where there are a few of
   // them and it adds at most 15% to the matrix.
   for (p.pad = 256; p.pad > 64; p.pad /= 2) {
@@ -667,7 +1081,6 @@ Plan plan(const gist_muon_desc* D) {
   }
   p.mp = (p.m + p.pad - 1) / p.pad * p.pad;
   p.np = (p.n + p.pad - 1) / p.pad * p.pad;
-  p.norm = up256(static_cast<size_t>(p.G) * kNormBlocks * sizeof(double));
   p.x = up256(static_cast<size_t>(p.G) * p.parts * p.mp * p.np * 2);
   p.a = up256(static_cast<size_t>(p.G) * p.parts * p.mp * p.mp * 2);
   p.part = 0;
@@ -700,11 +1113,80 @@ void product(hipStream_t st, const Plan& p, int64_t M, int64_t N, int64_t K, con
   }
 }
 
+dim3 norm_grid(int64_t count, int64_t G) {
+  return dim3(static_cast<unsigned>(std::min<int64_t>(kNormBlocks, (count + 8 * kBlock - 1) / (8 * kBlock))),
+              static_cast<unsigned>(G));
+}
+
+void launch_norm(hipStream_t st, const Plan& p, int64_t count, const float* G, float* M, bool update, bool vec,
+                 const Update& u, double* part) {
+  ProfScope ps(st, "muon_norm", 4.0 * p.G * count, (update ? 12.0 : 4.0) * p.G * count);
+  const dim3 g = norm_grid(count, p.G);
+  if (update && vec) norm_kernel<true, 4><<<g, kBlock, 0, st>>>(count, G, M, u, part);
+  else if (update) norm_kernel<true, 1><<<g, kBlock, 0, st>>>(count, G, M, u, part);
+  else if (vec) norm_kernel<false, 4><<<g, kBlock, 0, st>>>(count, G, M, u, part);
+  else norm_kernel<false, 1><<<g, kBlock, 0, st>>>(count, G, M, u, part);
+}
+
+template <int NP>
+gist_status run_small(hipStream_t st, const gist_muon_desc* D, const Plan& p, const float* G, void* O, float* W,
+                      float* M, const Update& u, bool vec, char* ws) {
+  const int64_t count = D->rows * D->cols;
+  SmallArgs a{};
+  a.rows = D->rows;
+  a.cols = D->cols;
+  a.m = static_cast<int>(p.m);
+  a.n = static_cast<int>(p.n);
+  a.slabs = p.slabs;
+  a.flip = p.flip;
+  a.G = G;
+  a.M = M;
+  a.W = W;
+  a.O = O;
+  a.u = u;
+  a.norm = reinterpret_cast<const double*>(ws);
+  a.eps = D->eps;
+  a.ca = D->coef[0];
+  a.cb = D->coef[1];
+  a.cc = D->coef[2];
+  a.steps = D->steps;
+  a.T = ws + p.norm;
+  float* const parts[2] = {reinterpret_cast<float*>(ws + p.norm + p.x),
+                           reinterpret_cast<float*>(ws + p.norm + p.x + p.a)};
+  if (p.slabs > 1) {
+    launch_norm(st, p, count, G, M, W != nullptr, vec, u, reinterpret_cast<double*>(ws));
+    a.nparts = static_cast<int>(norm_grid(count, p.G).x);
+  }
+  // one slab takes every step in one launch; several a launch for A's first parts and
+  // one for each step
+  for (int k = p.slabs > 1 ? -1 : 0; k < (p.slabs > 1 ? D->steps : 1); ++k) {
+    a.first = p.slabs == 1 || k < 0;
+    a.k0 = std::max(k, 0);
+    a.k1 = p.slabs == 1 ? D->steps : k + 1;
+    a.pin = parts[k & 1];
+    a.pout = parts[(k & 1) ^ 1];
+    ProfScope ps(st, "muon_small", 0.0, 0.0);
+    const dim3 g(static_cast<unsigned>(p.slabs), static_cast<unsigned>(p.G));
+#define SMALL(MP)                                                                      \
+  do {                                                                                 \
+    if (W) small_kernel<NP, MP, true><<<g, kSmallThreads, 0, st>>>(a);                 \
+    else small_kernel<NP, MP, false><<<g, kSmallThreads, 0, st>>>(a);                  \
+  } while (0)
+    if (p.m <= 64) SMALL(64);
+    else SMALL(128);
+#undef SMALL
+  }
+  return check_launch("muon");
+}
+
 template <int NP>
 gist_status run(hipStream_t st, const gist_muon_desc* D, const float* G, void* O, float* W,
                 float* M, Update u, char* ws) {
   const Plan p = plan(D);
   const int64_t count = D->rows * D->cols;
+  const bool vec = D->cols % 4 == 0 && reinterpret_cast<uintptr_t>(G) % 16 == 0 &&
+                   (!W || reinterpret_cast<uintptr_t>(M) % 16 == 0);
+  if (p.slabs) return run_small<NP>(st, D, p, G, O, W, M, u, vec, ws);
   double* part = reinterpret_cast<double*>(ws);
   ws += p.norm;
   auto mat = [&](size_t bytes, int64_t r, int64_t c) {
@@ -719,17 +1201,8 @@ gist_status run(hipStream_t st, const gist_muon_desc* D, const float* G, void* O
   }
   const Mat A = mat(p.a, p.mp, p.mp), B = mat(p.a, p.mp, p.mp);
   float* parts = reinterpret_cast<float*>(ws);
-  const bool vec = D->cols % 4 == 0 && reinterpret_cast<uintptr_t>(G) % 16 == 0 &&
-                   (!W || reinterpret_cast<uintptr_t>(M) % 16 == 0);
-  const int nb = static_cast<int>(std::min<int64_t>(kNormBlocks, (count + 8 * kBlock - 1) / (8 * kBlock)));
-  {
-    ProfScope ps(st, "muon_norm", 4.0 * p.G * count, (W ? 12.0 : 4.0) * p.G * count);
-    const dim3 g(nb, static_cast<unsigned>(p.G));
-    if (W && vec) norm_kernel<true, 4><<<g, kBlock, 0, st>>>(count, G, M, u, part);
-    else if (W) norm_kernel<true, 1><<<g, kBlock, 0, st>>>(count, G, M, u, part);
-    else if (vec) norm_kernel<false, 4><<<g, kBlock, 0, st>>>(count, G, M, u, part);
-    else norm_kernel<false, 1><<<g, kBlock, 0, st>>>(count, G, M, u, part);
-  }
+  const int nb = static_cast<int>(norm_grid(count, p.G).x);
+  launch_norm(st, p, count, G, M, W != nullptr, vec, u, part);
   {
     ProfScope ps(st, "muon_split", 0.0, (4.0 * (W ? 2 : 1) + 4.0 * NP) * p.G * count);
     const int64_t rp = p.flip ? p.np : p.mp, cp = p.flip ? p.mp : p.np;

@@ -60,7 +60,9 @@ def store_slack(want, dtype):
 
 SHAPES = [(1, 1, 1), (1, 1, 9), (1, 9, 1), (1, 2, 3), (2, 16, 16), (1, 31, 33), (1, 64, 64), (3, 41, 64),
           (1, 65, 63), (1, 100, 700), (2, 700, 100), (1, 128, 128), (1, 129, 257), (4, 257, 130),
-          (1, 512, 512), (1, 1433, 128), (2, 300, 1024), (1, 1000, 640)]
+          (1, 512, 512), (1, 1433, 128), (2, 300, 1024), (1, 1000, 640), (1, 64, 128), (1, 129, 128),
+          (2, 65, 128), (2, 128, 66), (1, 3, 1000), (3, 127, 127), (1, 33, 8300), (1, 2047, 100), (1, 100, 2050),
+          (70, 40, 300), (1, 640, 64)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "f16"])
@@ -69,7 +71,7 @@ def test_orthogonalize(G, ctx, dtype, g, r, c):
     rng = np.random.default_rng(g * 1000 + r * 7 + c)
     U = matrices(g, r, c, rng)
     got = orthogonalize(G, ctx, U, dtype)
-    for i in range(g):
+    for i in range(0, g, max(1, g // 4)):
         want = R.orthogonal(U[i])
         tol = R.muon_tolerance(U[i], dtype) + store_slack(want, dtype)
         err = np.linalg.norm(got[i] - want)
@@ -159,7 +161,7 @@ def test_eps_zero_and_nonfinite(G, ctx, dtype):
 
 @pytest.mark.parametrize("dtype", ["f32", "f16"])
 @pytest.mark.parametrize("nesterov", [False, True])
-@pytest.mark.parametrize("g,r,c", [(1, 1, 1), (2, 48, 100), (1, 130, 70), (1, 333, 333)])
+@pytest.mark.parametrize("g,r,c", [(1, 1, 1), (2, 48, 100), (1, 130, 70), (1, 333, 333), (2, 602, 64), (3, 128, 100)])
 def test_update(G, ctx, dtype, nesterov, g, r, c):
     """Three steps, the first with fresh momentum over garbage.  M: two products and a sum,
     three roundings of its terms a step.  W: the factor's bound times lr scale, and three
@@ -203,7 +205,7 @@ def test_workspace_contents_do_not_matter(G, ctx):
     """Workspace and outputs full of NaN before the call; the same bits again."""
     import torch
     rng = np.random.default_rng(12)
-    for r, c in ((100, 200), (65, 64), (300, 30)):
+    for r, c in ((100, 200), (65, 64), (300, 30), (100, 100), (500, 200)):
         U = to_dev(matrices(1, r, c, rng))
         d = G.muon_desc(r, c)
         ws = workspace(G, d)
@@ -223,7 +225,7 @@ def test_empty(G, ctx):
         G.gist_muon_update(ctx, d, None, None, None, 0.1, 0.9, 0.0, 1.0, None)
 
 
-@pytest.mark.parametrize("r,c", [(96, 200), (1500, 40)])
+@pytest.mark.parametrize("r,c", [(96, 200), (1500, 40), (64, 64), (200, 180)])
 def test_replays(G, r, c):
     """An update recorded once and replayed with new gradients equals the eager updates."""
     import torch
