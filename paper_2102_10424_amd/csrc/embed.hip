@@ -502,7 +502,7 @@ GradPlan plan(int64_t n, int64_t V, int d) {
   p.keys = up256(static_cast<size_t>(n) * 4);
   p.hist = up256(static_cast<size_t>(p.tiles) * kBins * 4);
   p.part = up256(static_cast<size_t>(p.chunks) * 2 * p.ldp * 4);
-  p.cross = up256(static_cast<size_t>(p.chunks + 2) * 4);
+  p.cross = n > 0 ? up256(static_cast<size_t>(p.chunks + 2) * 4) : 0;
   return p;
 }
 

@@ -276,7 +276,8 @@ __device__ __forceinline__ void wait_loads() {
 __device__ __forceinline__ void load_to_lds(unsigned dst, unsigned off, const char* base) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
                :
-               : "s"(dst), "v"(off), "s"(base));
+               : "s"(dst), "v"(off), "s"(base)
+               : "memory");
 }
 
 // Work of one product: tiles of all groups.  The first `whole` are one
@@ -978,17 +979,6 @@ __global__ __launch_bounds__(kSmallThreads, 2) void small_kernel(SmallArgs a) {
 
 size_t up256(size_t x) { return (x + 255) & ~size_t(255); }
 
-struct Plan {
-  int64_t G, m, n, mp, np;    // smaller and larger side, padded
-  int parts;                  // per value
-  int pad;                    // 256, 128 or 64: both sides are padded to it, tiles are at most it
-  bool flip;                  // rows > cols
-  size_t norm, x, a;          // bytes: norm partials, one X (or X^T), one A (or B)
-  size_t part;                // partial tiles
-  int slabs;                  // small_kernel's, 0: products of tiles
-  size_t total() const { return slabs ? norm + x + 2 * a : norm + 4 * x + 2 * a + part; }
-};
-
 // The tiles: side, workgroups the card holds at once, and what a round of them
 // was measured to take: `base` + `fill` (epilogue, of a full round) + `step` per
 // step of K, at least `least`; microseconds, for one and two parts per value.
@@ -1012,6 +1002,18 @@ struct Choice {
     const size_t side = kTiles[tile].side;
     return s.ragged ? up256(static_cast<size_t>(s.ragged) * s.slices * side * side * 4) : 0;
   }
+};
+
+struct Plan {
+  int64_t G, m, n, mp, np;    // smaller and larger side, padded
+  int parts;                  // per value
+  int pad;                    // 256, 128 or 64: both sides are padded to it, tiles are at most it
+  bool flip;                  // rows > cols
+  size_t norm, x, a;          // bytes: norm partials, one X (or X^T), one A (or B)
+  size_t part;                // partial tiles
+  int slabs;                  // small_kernel's, 0: products of tiles
+  Choice gram, poly, step;
+  size_t total() const { return slabs ? norm + x + 2 * a : norm + 4 * x + 2 * a + part; }
 };
 
 // Tile and K cuts of one product, the quickest by these figures; a join takes 5 us
@@ -1084,9 +1086,10 @@ Plan plan(const gist_muon_desc* D) {
   p.x = up256(static_cast<size_t>(p.G) * p.parts * p.mp * p.np * 2);
   p.a = up256(static_cast<size_t>(p.G) * p.parts * p.mp * p.mp * 2);
   p.part = 0;
-  for (const Choice& c : {choose(p, p.mp, p.mp, p.np, true), choose(p, p.mp, p.mp, p.mp, true),
-                          choose(p, p.mp, p.np, p.mp, false)})
-    p.part = std::max(p.part, c.part_bytes());
+  p.gram = choose(p, p.mp, p.mp, p.np, true);
+  p.poly = choose(p, p.mp, p.mp, p.mp, true);
+  p.step = choose(p, p.mp, p.np, p.mp, false);
+  for (const Choice* c : {&p.gram, &p.poly, &p.step}) p.part = std::max(p.part, c->part_bytes());
   return p;
 }
 
@@ -1095,7 +1098,7 @@ void product(hipStream_t st, const Plan& p, int64_t M, int64_t N, int64_t K, con
              const Epi& E, float* part) {
   static const char* const names[4] = {"muon_gram", "muon_poly", "muon_step", "muon_last"};
   constexpr bool kSym = MODE == kGram || MODE == kPoly;
-  const Choice c = choose(p, M, N, K, kSym);
+  const Choice& c = MODE == kGram ? p.gram : MODE == kPoly ? p.poly : p.step;
   {
     ProfScope ps(st, names[MODE], (kSym ? 1.0 : 2.0) * p.G * M * N * K, 2.0 * NP * p.G * (M * K + N * K + M * N));
     const dim3 g(static_cast<unsigned>(c.s.whole + c.s.ragged * c.s.slices));
