@@ -315,7 +315,7 @@ __device__ __forceinline__ void finish(float* p, int left, const float (&acc)[kV
 // listed, in no order: crossing[0] of them, from crossing[2] on, and crossing[1] with
 // an id of more than kFew parts, from crossing[1 + chunks] down.  Rows are loaded kBatch
 // at a time and added in order.  Bound by memory: 131,072 rows of 1,024 columns in
-// 150 us (537 MB of rows, 4.5 TB/s with results and parts); 190 one row at a time.
+// 150 us (537 MB of rows, 4.5 TB/s with results and parts).
 constexpr int kFew = 16;
 constexpr int kBatch = 8;
 template <bool SGD>

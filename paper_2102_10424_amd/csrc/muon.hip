@@ -566,7 +566,7 @@ __global__ __launch_bounds__(64 * NWM * NWN, 2) void product_kernel(Sched S, Mat
 }
 
 // Tiles that were cut in K: a wave per 32 x 32 block adds the slices in order
-// (16 tiles of 256 x 256 in four slices 9 us; uncut, they were a round of 290).
+// (16 tiles of 256 x 256 in eight slices 9 us; uncut, they were a round of 290).
 template <int NP, int MODE, int TILE>
 __global__ __launch_bounds__(kBlock) void join_kernel(Sched S, const float* __restrict__ part, Epi E) {
   __shared__ __attribute__((aligned(16))) float scratch[kBlock / 64][kScratch];
