@@ -554,11 +554,12 @@ gist_status gist_log_probs(gist_ctx* ctx, int64_t n, int64_t C, const void* logi
  * respect to the logits:
  *   dz_j = g_logp (1[j = y] - p_j) - g_entropy p_j (log p_j + entropy),
  * formed in fp32 from the logits, the lse and entropy of the forward call,
- * and rounded once to `store`.  dlogits is n x C (leading dimension ldd,
- * stored as the logits) and may be the logits themselves.  g_logp (then
- * tokens) or g_entropy (then entropy) may be NULL, meaning zero.  A row that
- * is -Inf throughout has gradient 0; a row with a NaN lse, a NaN gradient.
- * Errors as gist_log_probs. */
+ * and rounded once to `store`.  (Where |lse| > 64 a row's probabilities are
+ * summed again, so that bits its lse has lost to a large offset do not show.)
+ * dlogits is n x C (leading dimension ldd, stored as the logits) and may be the
+ * logits themselves.  g_logp (then tokens) or g_entropy (then entropy) may be
+ * NULL, meaning zero.  A row that is -Inf throughout has gradient 0; a row with
+ * a NaN lse, a NaN gradient.  Errors as gist_log_probs. */
 gist_status gist_log_probs_bwd(gist_ctx* ctx, int64_t n, int64_t C, const void* logits,
                                int64_t ldz, int32_t store, const int32_t* tokens,
                                const float* lse, const float* entropy, const float* g_logp,

@@ -132,7 +132,9 @@ struct Out {
   int* idx;
 };
 
-// A row's outputs from its statistics, by one lane; returns the log-sum-exp.
+// A row's outputs from its statistics, by one lane; returns log s = lse - m.  Log
+// probabilities are (z - m) - log s, not z - lse: that keeps the bits of log s that lse
+// loses to a large m (all of them in a row of the type's lowest value).
 template <int STORE>
 __device__ __forceinline__ float write_stats(const Out& o, int64_t row, int C, const void* Z, int64_t ldz,
                                              const Stat& a, bool write) {
@@ -140,9 +142,8 @@ __device__ __forceinline__ float write_stats(const Out& o, int64_t row, int C, c
   const bool ok = a.m < INFINITY;            // no NaN, no +Inf in the row
   const bool some = ok && a.m > -INFINITY;   // not masked throughout
   const float l2 = lg2(a.s);
-  const float lse = some ? fmaf(kLn2, l2, a.m) : ok ? -INFINITY : nan;
   if (write) {
-    if (o.lse) o.lse[row] = lse;
+    if (o.lse) o.lse[row] = some ? fmaf(kLn2, l2, a.m) : ok ? -INFINITY : nan;
     if (o.entropy) o.entropy[row] = some ? kLn2 * (l2 - a.t / a.s) : ok ? 0.f : nan;
     if (o.logp) {
       const int y = o.tokens[row];
@@ -152,20 +153,20 @@ __device__ __forceinline__ float write_stats(const Out& o, int64_t row, int C, c
       } else if (y >= 0) {
         float z[1];
         load_vec<STORE, 1>(Z, row * ldz + y, z);
-        v = z[0] == -INFINITY && ok ? -INFINITY : z[0] - lse;
+        v = z[0] == -INFINITY && ok ? -INFINITY : (z[0] - a.m) - kLn2 * l2;
       }
       o.logp[row] = ok ? v : nan;
     }
   }
-  return lse;
+  return kLn2 * l2;
 }
 
 // The k-th best class (its order bits and itself) of a row.
 __device__ __forceinline__ void write_top(const Out& o, int64_t row, int K, int k, unsigned bits, unsigned cls,
-                                          float m, float lse) {
+                                          float m, float ls) {
   const bool ok = m < INFINITY;
   const float z = from_order(bits);
-  o.top[row * K + k] = !ok ? __uint_as_float(0x7fc00000u) : z == -INFINITY ? z : z - lse;
+  o.top[row * K + k] = !ok ? __uint_as_float(0x7fc00000u) : z == -INFINITY ? z : (z - m) - ls;
   o.idx[row * K + k] = ok ? static_cast<int>(cls) : -1;
 }
 
@@ -173,10 +174,10 @@ __device__ __forceinline__ void write_top(const Out& o, int64_t row, int K, int 
 template <int STORE>
 __device__ __forceinline__ void write_row(const Out& o, int64_t row, int C, const void* Z, int64_t ldz,
                                           const Stat& a, const Top& top, int K, int lane) {
-  const float lse = write_stats<STORE>(o, row, C, Z, ldz, a, lane == 0);
+  const float ls = write_stats<STORE>(o, row, C, Z, ldz, a, lane == 0);
   if (lane < K)
     write_top(o, row, K, lane, static_cast<unsigned>(top.mine >> 32), 0xffffffffu - static_cast<unsigned>(top.mine),
-              a.m, lse);
+              a.m, ls);
 }
 
 // ---- rows of up to 1,024 classes: LPR lanes a row, E classes a lane ----------------
@@ -245,7 +246,7 @@ __global__ __launch_bounds__(kBlock) void short_rows_kernel(int64_t n, int C, co
     }
     a.s = reduce_f<LPR>(a.s, [](float x, float y) { return x + y; });
     a.t = reduce_f<LPR>(a.t, [](float x, float y) { return x + y; });
-    const float lse = write_stats<STORE>(o, row, C, Z, ldz, a, live && l == 0);
+    const float ls = write_stats<STORE>(o, row, C, Z, ldz, a, live && l == 0);
     if constexpr (TOP) {
       unsigned key[E];
 #pragma unroll
@@ -268,7 +269,7 @@ __global__ __launch_bounds__(kBlock) void short_rows_kernel(int64_t n, int C, co
         }
         if ((k & (LPR - 1)) == LPR - 1 || k == K - 1) {
           const int at = (k & ~(LPR - 1)) + l;
-          if (live && at <= k) write_top(o, row, K, at, kb, kc, a.m, lse);
+          if (live && at <= k) write_top(o, row, K, at, kb, kc, a.m, ls);
         }
       }
     }
@@ -411,8 +412,11 @@ __global__ __launch_bounds__(kBlock) void join_rows_kernel(int64_t n, int parts,
 }
 
 // dz = g_l (1[j = y] - p) - g_H p (log p + H), p = exp(z - lse).  A group of
-// 1 << tl threads per (row, slab of columns); with slabs the group is the block.
+// 1 << tl threads per (row, slab of columns): 64 lanes of a wave or fewer, or the block.
+// An lse beyond kFar has lost bits of log s (2^-19 and more), so the group sums the row's
+// exp(z - lse) first, 1 but for that, and takes its logarithm off.
 // Bound by memory: 8,192 x 32,000 bf16 in 183 us (5.7 TB/s).
+constexpr float kFar = 64.f;
 template <int STORE, int V>
 __global__ __launch_bounds__(kBlock) void bwd_kernel(int64_t items, int slabs, int slab, int tl, int C,
                                                      const void* Z, int64_t ldz,
@@ -422,6 +426,7 @@ __global__ __launch_bounds__(kBlock) void bwd_kernel(int64_t items, int slabs, i
                                                      const float* __restrict__ gl,
                                                      const float* __restrict__ gh, void* dZ,
                                                      int64_t ldd) {
+  __shared__ float sums[kWaves];
   const int lane = threadIdx.x & ((1 << tl) - 1);
   for (int64_t item = (static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x) >> tl; item < items;
        item += (static_cast<int64_t>(gridDim.x) * kBlock) >> tl) {
@@ -438,12 +443,30 @@ __global__ __launch_bounds__(kBlock) void bwd_kernel(int64_t items, int slabs, i
     const bool none = l == -INFINITY;
     const bool bad = l != l || l == INFINITY || y >= C;
     if (none) gy = 0.f;
+    float ls = 0.f;
+    if (!none && !bad && fabsf(l) > kFar) {
+      float s = 0.f;
+      for (int64_t j = V * lane; j < C; j += V << tl) {
+        float z[V];
+        load_some<STORE, V>(Z, row * ldz + j, C - j, -INFINITY, z);
+#pragma unroll
+        for (int q = 0; q < V; ++q) s += ex2(fmaxf(z[q] - l, -200.f) * kL);
+      }
+      for (int o = min(32, (1 << tl) >> 1); o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+      if (tl == 8) {   // the block's threads have one item
+        __syncthreads();   // the last item's sums are read
+        if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = s;
+        __syncthreads();   // and in place, the row is read
+        s = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+      }
+      ls = kLn2 * lg2(s);
+    }
     for (int64_t j = c0 + V * lane; j < c1; j += V << tl) {
       float z[V], d[V];
       load_some<STORE, V>(Z, row * ldz + j, c1 - j, 0.f, z);
 #pragma unroll
       for (int q = 0; q < V; ++q) {
-        const float x = fmaxf(z[q] - l, -200.f);
+        const float x = fmaxf((z[q] - l) - ls, -200.f);
         const float p = ex2(x * kL);
         d[q] = -p * fmaf(w1, x, w0);
         if (none) d[q] = 0.f;
@@ -557,10 +580,12 @@ gist_status log_probs_bwd(hipStream_t st, int64_t n, int64_t C, const void* Z, i
   const int eb = store == GIST_STORE_F32 ? 4 : 2, most = store == GIST_STORE_F32 ? 4 : 8;
   // short rows: a class per lane, so that a wave's accesses are one run of bytes
   const int v = C <= 64 ? 1 : most;
-  const int tl = std::min(8, ceil_log2((C + v - 1) / v));
-  // slabs of eight steps where a row takes more than one
+  int tl = std::min(8, ceil_log2((C + v - 1) / v));
+  if (tl == 7) tl = 6;   // a wave or a block
+  // slabs of eight steps where a row takes more than one; in place, where a group may
+  // read its whole row before it writes, one
   const int64_t step = static_cast<int64_t>(v) << tl;
-  const int64_t slab = C <= 8 * step ? C : 8 * step;
+  const int64_t slab = C <= 8 * step || dZ == Z ? C : 8 * step;
   const int64_t slabs = (C + slab - 1) / slab, items = n * slabs;
   const dim3 g(static_cast<unsigned>(std::min<int64_t>(((items << tl) + kBlock - 1) / kBlock, 1 << 22)));
   ProfScope ps(st, "log_probs_bwd", 8.0 * n * C, 2.0 * n * C * eb);

@@ -204,6 +204,56 @@ def test_backward_special_rows(G, ctx, C):
           np.nan_to_num(R.grad_bound(z, y, gl, gh, "f32")) + 1e-45)
 
 
+FAR = dict(f32=[1e5, -3e7, 2e30], bf16=[1e4, -3e7, 2e30], f16=[3e4, -6e4])
+
+
+@pytest.mark.parametrize("store", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("n,C,K", [(3, 1, 1), (40, 47, 5), (9, 130, 3), (5, 400, 2), (6, 1000, 8), (3, 20011, 4),
+                                   (1100, 1100, 2), (1, 100003, 20)])
+def test_far_rows(G, ctx, store, n, C, K):
+    """Rows whose offset swallows log s in an fp32 lse: whole rows of the type's lowest value,
+    and offsets of up to 2e30.  Log probabilities and gradients are those of the row without
+    its offset (an exact subtraction in 64 bits), in place too.  Bounds: (z - m) is rounded
+    once (u of |logp| + log C), log s errs as an lse without maximum.  The gradient's exponents
+    (z - l) - log s' take two roundings more, and s' as many errors as s: twice grad_bound."""
+    import torch
+    rng = np.random.default_rng(n + C)
+    low = dict(f32=float(np.finfo(np.float32).min), bf16=-3.3895e38, f16=-65504.0)[store]
+    for far in FAR[store] + ["lowest"]:
+        z = (rng.standard_normal((n, C)) * 3).astype(np.float32)
+        if far == "lowest":
+            z[:] = low
+            if n > 2:
+                z[2, ::2] = np.float32(low / 2)
+        else:
+            z = np.float32(far) + z
+            z[rng.random((n, C)) < 0.2] = -np.inf
+            z[:, C // 2] = np.float32(far)
+        t = torch.from_numpy(z).to(R.torch_type(store))
+        z = t.double().numpy()
+        z = z - z.max(1, keepdims=True)
+        y = rng.integers(0, C, n).astype(np.int32)
+        dev, lp, H, l, top, idx = forward(G, ctx, t, store, y, K)
+        _, wlp, wH = R.log_probs(z, y)
+        near = R.lse_bound(z) + 4 * R.U32 * np.log(C + 1)
+        close(to_host(lp), wlp, near + 4 * R.U32 * np.abs(np.where(np.isfinite(wlp), wlp, 0)))
+        close(to_host(H), wH, R.entropy_bound(z))
+        wi = R.top_classes(z, K)
+        assert np.array_equal(to_host(idx), wi)
+        wt = np.stack([R.log_probs(z, wi[:, k])[1] for k in range(K)], 1)
+        close(to_host(top), wt, near[:, None] + 4 * R.U32 * np.abs(np.where(np.isfinite(wt), wt, 0)))
+        gl, gh = (rng.standard_normal(n).astype(np.float32) for _ in range(2))
+        want = R.log_probs_grad(z, y, gl, gh)
+        bound = 2 * R.grad_bound(z, y, gl, gh, store) + 1e-45
+        dz = torch.full_like(dev, 5.0)
+        G.gist_log_probs_bwd(ctx, n, C, dev, C, R.store_of(G, store), to_dev(y), l, H, to_dev(gl), to_dev(gh), dz, C)
+        w = close(to_host(dz.float()), want, bound)
+        G.gist_log_probs_bwd(ctx, n, C, dev, C, R.store_of(G, store), to_dev(y), l, H, to_dev(gl), to_dev(gh), dev, C)
+        assert torch.equal(dev.float().isnan(), dz.float().isnan())
+        close(to_host(dev.float()), want, bound)
+        log(f"far rows {store} n={n} C={C} {far}: error / bound {w:.2f}")
+
+
 def test_gradient_against_differences(G, ctx):
     """The gradient against differences of the library's own values: a change h of one logit
     changes logp and entropy by h g + O(h^2); with h = 2^-6 the second-order term is below
