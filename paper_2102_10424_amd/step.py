@@ -837,7 +837,9 @@ class SubGCN:
         self.gat = kind == "gat"
         self.input_grad = input_grad
         self.muon_ws = None
-        self.lp = None
+        self.lp = None         # the last log_probs call's buffers
+        self._lp = {}          # by K
+        self._kept = []        # outgrown buffers that a recorded step may still use
         self.nnz_cap = 0
         self.alpha = None
         self.widths = list(widths)
@@ -1029,6 +1031,7 @@ class SubGCN:
         need = max(G.gist_muon_workspace_size(self.muon_desc(l, dtype=dtype))
                    for l in range(self.L))
         if self.muon_ws is None or self.muon_ws.numel() < need:
+            self._kept.append(self.muon_ws)
             self.muon_ws = torch.empty(need, dtype=torch.uint8, device=self.device)
 
     def muon(self, params, M, lr, fresh=False, momentum=0.95, weight_decay=0.0, dtype=None):
@@ -1044,18 +1047,29 @@ class SubGCN:
             if self.gat:
                 G.gist_sgd_update(self.ctx, params[l][r:], self.dW[l][r:], 2 * c, lr)
 
+    def _log_probs_buffers(self, n, K):
+        """Buffers of :meth:`log_probs`, one set for each K."""
+        ws = G.gist_log_probs_workspace(n, self.widths[-1], K)
+        p = self._lp.get(K)
+        if p is None or p["n"] < n or p["ws"].numel() < ws:
+            self._kept.append(p)
+            n = max(n, self.n_cap)
+            f = lambda *s: torch.empty(*s, device=self.device)
+            p = dict(n=n, logp=f(n), entropy=f(n), lse=f(n), top_logp=f(n, K),
+                     top_idx=torch.empty(n, K, dtype=torch.int32, device=self.device),
+                     ws=torch.empty(max(ws, 16), dtype=torch.uint8, device=self.device))
+            self._lp[K] = p
+        self.lp = p
+        return p
+
     def log_probs(self, batch, K=0):
         """Of the last forward pass's logits: the labels' log probabilities, every
         row's entropy and log-sum-exp, and its K best classes (``top_logp``,
-        ``top_idx``), as a dict of device tensors that the next call reuses."""
+        ``top_idx``), as a dict of device tensors that the next call with this K
+        reuses.  The rows that pad a batch of fixed layout are rows like any
+        other here: give them weight 0 in :meth:`log_probs_grad`, or label -1."""
         n, C = batch.rows(self.L), self.widths[-1]
-        ws = G.gist_log_probs_workspace(n, C, K)
-        if self.lp is None or self.lp["n"] < n or self.lp["K"] != K or self.lp["ws"].numel() < ws:
-            f = lambda *s: torch.empty(*s, device=self.device)
-            self.lp = dict(n=n, K=K, logp=f(n), entropy=f(n), lse=f(n), top_logp=f(n, K),
-                           top_idx=torch.empty(n, K, dtype=torch.int32, device=self.device),
-                           ws=torch.empty(max(ws, 16), dtype=torch.uint8, device=self.device))
-        p = self.lp
+        p = self._log_probs_buffers(n, K)
         G.gist_log_probs(self.ctx, n, C, self.H[self.L], C, G.GIST_STORE_F32, batch.labels,
                          p["logp"], p["entropy"], p["lse"], K, p["top_logp"] if K else None,
                          p["top_idx"] if K else None, p["ws"])
@@ -1097,14 +1111,16 @@ class LearnedRows:
         self.N, self.d = table.shape
         self.n_cap = 0
         self.ws = None
+        self._kept = []        # outgrown workspaces that a recorded step may still use
         if n_cap:
             self._reserve(n_cap)
 
     def _reserve(self, n):
         if n > self.n_cap:
+            self._kept.append(self.ws)
+            self.n_cap = n = max(n, 2 * self.n_cap)     # what is kept adds up to less than ws
             need = G.gist_embed_grad_workspace(n, self.N, self.d)
             self.ws = torch.empty(need, dtype=torch.uint8, device=self.device)
-            self.n_cap = n
 
     def lookup(self, ids, n, X):
         """X[:n] = scale * table[ids[:n]]."""
