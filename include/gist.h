@@ -650,10 +650,11 @@ enum {
 /* Device bytes both calls need. */
 gist_status gist_muon_workspace_size(const gist_muon_desc* D, size_t* bytes);
 /* O = the orthogonalised G (groups x rows x cols): fp32, or fp16 with
- * GIST_DTYPE_F16_IN.  The update's flags are ignored.  Errors: GIST_E_INVAL
- * (NULL pointers, rows, cols or groups out of range, unknown dtype or flags,
- * steps, eps or coefficients out of range), GIST_E_UNSUPPORTED (rows or cols
- * above 65,536), GIST_E_NOMEM.  rows == 0 or cols == 0 is a no-op. */
+ * GIST_DTYPE_F16_IN.  O may be G itself where it is fp32.  The update's flags
+ * are ignored.  Errors: GIST_E_INVAL (NULL pointers, negative sizes, fp16 output
+ * in place, unknown dtype or flags, steps, eps or coefficients out of range),
+ * GIST_E_UNSUPPORTED (rows or cols above 65,536, more than 65,535 groups),
+ * GIST_E_NOMEM.  rows == 0 or cols == 0 is a no-op. */
 gist_status gist_orthogonalize(gist_ctx* ctx, const gist_muon_desc* D, const float* G, void* O,
                                void* ws, size_t ws_bytes);
 /* One step of momentum with an orthogonalised direction (Muon), for the
@@ -664,7 +665,8 @@ gist_status gist_orthogonalize(gist_ctx* ctx, const gist_muon_desc* D, const flo
  * W and M (groups x rows x cols fp32) are updated in place, dW is read.  `scale`
  * sizes the update: sqrt(max(1, cols / rows)), or 0.2 sqrt(max(rows, cols))
  * for steps the size of Adam's.  Errors as gist_orthogonalize, and GIST_E_INVAL
- * for momentum outside [0, 1) or a non-finite lr, weight_decay or scale. */
+ * for momentum outside [0, 1), a non-finite lr, weight_decay or scale, or two
+ * equal pointers among W, dW and M. */
 gist_status gist_muon_update(gist_ctx* ctx, const gist_muon_desc* D, float* W, const float* dW,
                              float* M, float lr, float momentum, float weight_decay, float scale,
                              void* ws, size_t ws_bytes);

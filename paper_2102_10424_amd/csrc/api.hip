@@ -1189,6 +1189,8 @@ extern "C" gist_status gist_orthogonalize(gist_ctx* ctx, const gist_muon_desc* D
   GIST_TRY(check_muon("orthogonalize", D));
   if (D->rows == 0 || D->cols == 0) return GIST_OK;
   if (!G || !O) return set_error(GIST_E_INVAL, "orthogonalize: NULL pointer");
+  if (G == O && D->dtype != GIST_DTYPE_F32)
+    return set_error(GIST_E_INVAL, "orthogonalize: in place needs fp32 output");
   GIST_TRY(muon_ws("orthogonalize", D, ws, ws_bytes));
   gist::DeviceGuard dg(ctx->device);
   return gist::muon(ctx->stream, D, G, O, nullptr, nullptr, 0.f, 0.f, 0.f, 0.f, ws);
@@ -1209,6 +1211,8 @@ extern "C" gist_status gist_muon_update(gist_ctx* ctx, const gist_muon_desc* D, 
   if (D->rows == 0 || D->cols == 0) return GIST_OK;
   if (!W || !dW || !M) return set_error(GIST_E_INVAL, "muon_update: NULL pointer");
   GIST_TRY(muon_ws("muon_update", D, ws, ws_bytes));
+  if (W == dW || W == M || M == dW)
+    return set_error(GIST_E_INVAL, "muon_update: W, dW and M must be three arrays");
   gist::DeviceGuard dg(ctx->device);
   return gist::muon(ctx->stream, D, dW, nullptr, W, M, lr, momentum, weight_decay, scale, ws);
 }

@@ -217,6 +217,20 @@ def test_workspace_contents_do_not_matter(G, ctx):
         assert torch.equal(a, b) and bool(torch.isfinite(a).all())
 
 
+@pytest.mark.parametrize("g,r,c", [(2, 20, 30), (2, 40, 300), (1, 130, 200), (2, 300, 140)])
+def test_in_place(G, ctx, g, r, c):
+    """The fp32 factor in its gradient's place: the bits of one written elsewhere."""
+    import torch
+    U = to_dev(matrices(g, r, c, np.random.default_rng(r)))
+    d = G.muon_desc(r, c, groups=g)
+    ws = torch.empty(G.gist_muon_workspace_size(d), dtype=torch.uint8, device="cuda")
+    O = torch.empty_like(U)
+    G.gist_orthogonalize(ctx, d, U, O, ws)
+    G.gist_orthogonalize(ctx, d, U, U, ws)
+    torch.cuda.synchronize()
+    assert torch.equal(U, O)
+
+
 def test_empty(G, ctx):
     for r, c in ((0, 5), (5, 0)):
         d = G.muon_desc(r, c)

@@ -173,6 +173,45 @@ def test_muon_calls():
     refused(NOMEM, G.gist_muon_update, ctx, d, **{**ok, "ws": Ws(need - 1)})
 
 
+def test_muon_arrays_that_overlap():
+    """An update reads dW again after M is written and W is the last to be: three arrays.  The
+    factor may take its gradient's place where both are fp32."""
+    B, D = np.zeros(64, dtype=np.float32), np.zeros(64, dtype=np.float32)
+    d = G.muon_desc(8, 6)
+    w = Ws(G.gist_muon_workspace_size(d))
+    for W, dW, M in ((A, A, B), (A, B, A), (B, A, A)):
+        refused(INVAL, G.gist_muon_update, ctx, d, W, dW, M, 0.1, 0.9, 0.0, 1.0, w)
+    h = G.muon_desc(8, 6, dtype=G.GIST_DTYPE_F16_IN)
+    refused(INVAL, G.gist_orthogonalize, ctx, h, D, D, Ws(G.gist_muon_workspace_size(h)))
+
+
+def test_outgrown_buffers_live_on():
+    """A recorded step keeps the addresses of the buffers it was recorded with, so none of them
+    is freed when a later call needs a larger one, or one for another K."""
+    import weakref
+    import torch
+    from paper_2102_10424_amd import step as S
+    rows = S.LearnedRows(None, torch.zeros(50, 4), n_cap=10, device="cpu")
+    first = weakref.ref(rows.ws)
+    for n in (11, 40, 300, 5000):
+        rows._reserve(n)
+        assert rows.ws.numel() >= G.gist_embed_grad_workspace(n, 50, 4)
+    assert first() is not None and first() is not rows.ws
+    run = S.SubGCN(None, "gcn", [8, 300, 5000], 16, device="cpu")
+    run.prepare_muon(G.GIST_DTYPE_F16_IN)
+    ws = weakref.ref(run.muon_ws)
+    run.prepare_muon(G.GIST_DTYPE_F32)
+    assert ws() is not None and ws() is not run.muon_ws
+    three = run._log_probs_buffers(16, 3)
+    refs = [weakref.ref(t) for k, t in three.items() if k != "n"]
+    run._log_probs_buffers(16, 0)
+    assert run.lp is not three
+    assert run._log_probs_buffers(12, 3) is three and run.lp is three
+    assert run._log_probs_buffers(40, 3)["n"] >= 40     # a larger batch
+    del three
+    assert all(r() is not None for r in refs)
+
+
 def test_layers_refuse_fp16_operands():
     refused(INVAL, G.gist_layer_workspace_size,
             G.layer_desc(G.GIST_LAYER_GCN, G.GIST_ACT_NONE, 8, 4, 4, G.GIST_DTYPE_F16_IN))
