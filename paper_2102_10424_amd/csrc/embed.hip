@@ -540,6 +540,9 @@ gist_status embed_grad(hipStream_t st, int64_t n, int64_t V, int d, const int32_
                        float scale, const float* dY, int64_t ldy, bool sgd, float lr, float* out,
                        int64_t ldo, void* ws) {
   const GradPlan p = plan(n, V, d);
+  const int tl = std::min(8, ceil_log2((d + kV - 1) / kV));
+  if ((p.chunks << tl) >= (int64_t{1} << 32) - kBlock)
+    return set_error(GIST_E_UNSUPPORTED, "embed_grad: n * d exceeds the grid");
   char* c = static_cast<char*>(ws);
   int* k[2] = {reinterpret_cast<int*>(c), reinterpret_cast<int*>(c + p.keys)};
   int* q[2] = {reinterpret_cast<int*>(c + 2 * p.keys), reinterpret_cast<int*>(c + 3 * p.keys)};
@@ -577,9 +580,6 @@ gist_status embed_grad(hipStream_t st, int64_t n, int64_t V, int d, const int32_
                                                                             out, ldo);
   }
   if (n > 0) {
-    const int tl = std::min(8, ceil_log2((d + kV - 1) / kV));
-    if ((p.chunks << tl) >= (int64_t{1} << 32) - kBlock)
-      return set_error(GIST_E_UNSUPPORTED, "embed_grad: n * d exceeds the grid");
     const dim3 g(static_cast<unsigned>(((p.chunks << tl) + kBlock - 1) / kBlock),
                  static_cast<unsigned>((d + (kV << tl) - 1) / (kV << tl)));
     {
