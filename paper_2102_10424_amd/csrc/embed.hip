@@ -509,8 +509,10 @@ GradPlan plan(int64_t n, int64_t V, int d) {
   p.ldp = (d + 3) / 4 * 4;
   p.keys = up256(static_cast<size_t>(n) * 4);
   p.hist = up256(static_cast<size_t>(p.tiles) * kBins * 4);
-  p.part = up256(static_cast<size_t>(p.chunks) * 2 * p.ldp * 4);
-  p.cross = n > 0 ? up256(static_cast<size_t>(p.chunks + 2) * 4) : 0;
+  // room for the chunks of any smaller n too: a workspace for n ids serves fewer
+  const int64_t room = std::max<int64_t>(p.chunks, n > (1 << 20) ? (1 << 20) / 32 : n > 32768 ? 32768 / kBatch : 0);
+  p.part = up256(static_cast<size_t>(room) * 2 * p.ldp * 4);
+  p.cross = n > 0 ? up256(static_cast<size_t>(room + 2) * 4) : 0;
   return p;
 }
 

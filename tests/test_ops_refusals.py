@@ -173,6 +173,14 @@ def test_muon_calls():
     refused(NOMEM, G.gist_muon_update, ctx, d, **{**ok, "ws": Ws(need - 1)})
 
 
+def test_embed_workspace_serves_fewer_ids():
+    """A runner allocates for its largest batch and passes the same workspace for every other."""
+    sizes = sorted({n + k for n in (1, 8, 32, 64, 2048, 8192, 32768, 1 << 17, 1 << 20, 1 << 22) for k in (-1, 0, 1, 7)})
+    for d in (1, 30, 1024):
+        need = [G.gist_embed_grad_workspace(n, 1000, d) for n in sizes]
+        assert need == sorted(need)
+
+
 def test_muon_arrays_that_overlap():
     """An update reads dW again after M is written and W is the last to be: three arrays.  The
     factor may take its gradient's place where both are fp32."""
