@@ -308,6 +308,37 @@ __device__ __forceinline__ void finish(float* p, int left, const float (&acc)[kV
   store_some<GIST_STORE_F32, kV>(p, 0, left, x);
 }
 
+// Lanes (their logarithm) that zero a row's `width` columns together.
+__host__ __device__ __forceinline__ int zero_lanes_log2(int width) {
+  int l = 0;
+  while (l < 6 && (kV << l) < width) ++l;
+  return l;
+}
+
+// Zero rows that no id names (dense gradient), columns j0 .. j1 - 1: a wave per
+// 1 << rows_log2 rows, each lane looking its row up in the sorted ids.  Writing them
+// here, and not all rows before the sums, leaves each row one write.
+__device__ __forceinline__ void zero_rows(int n, int Vn, int j0, int j1, int rows_log2, int64_t wave,
+                                          const int* __restrict__ keys, float* __restrict__ out,
+                                          int64_t ldo) {
+  const int lane = threadIdx.x & 63, R = 1 << rows_log2;
+  const int64_t r0 = wave << rows_log2;
+  if (r0 >= Vn) return;
+  const int64_t r = r0 + (lane & (R - 1));
+  int lo = 0, hi = n;
+  while (lo < hi) {
+    const int mid = lo + ((hi - lo) >> 1);
+    if (keys[mid] < r) lo = mid + 1;
+    else hi = mid;
+  }
+  const unsigned long long m = __ballot(r < Vn && (lo >= n || keys[lo] != r));
+  const int tl = zero_lanes_log2(j1 - j0), l = lane & ((1 << tl) - 1);
+  const float z[kV] = {};
+  for (int q = lane >> tl; q < R; q += 64 >> tl)
+    if (m >> q & 1)
+      for (int j = j0 + kV * l; j < j1; j += kV << tl) store_some<GIST_STORE_F32, kV>(out + (r0 + q) * ldo, j, j1 - j, z);
+}
+
 // Chunks of `len` sorted positions (a multiple of kBatch), one group of threads
 // each; blockIdx.y: slab of columns.  part[2 c] is the sum of chunk c's first id
 // where that id began in an earlier chunk, part[2 c + 1] that of its last id where
@@ -318,14 +349,24 @@ __device__ __forceinline__ void finish(float* p, int left, const float (&acc)[kV
 // 150 us (537 MB of rows, 4.5 TB/s with results and parts).
 constexpr int kFew = 16;
 constexpr int kBatch = 8;
+// Dense: the blocks behind the chunks' (from blockIdx.x == sums on) zero the other rows,
+// 164 us together for a table of 50,000 rows, where a launch of their own took 24 beside
+// 152; and 8 ids of a table of 1,063 x 563 take 10.5 us, 31 with that launch, in which 17
+// waves zeroed 64 rows each.
 template <bool SGD>
-__global__ __launch_bounds__(kBlock) void sum_kernel(int n, int Vn, int d, int tpr_log2, int len,
+__global__ __launch_bounds__(kBlock) void sum_kernel(int sums, int rows_log2, int n, int Vn, int d, int tpr_log2, int len,
                                                      const int* __restrict__ keys,
                                                      const int* __restrict__ pos, float scale,
                                                      const float* __restrict__ dY, int64_t ldy,
                                                      float lr, float* __restrict__ out,
                                                      int64_t ldo, float* __restrict__ part,
                                                      int64_t ldp, int* __restrict__ crossing) {
+  if (!SGD && blockIdx.x >= sums) {
+    const int j0 = (kV * static_cast<int>(blockIdx.y)) << tpr_log2;
+    zero_rows(n, Vn, j0, min(d, j0 + (kV << tpr_log2)), rows_log2,
+              (static_cast<int64_t>(blockIdx.x - sums) * kBlock + threadIdx.x) >> 6, keys, out, ldo);
+    return;
+  }
   const int lane = threadIdx.x & ((1 << tpr_log2) - 1);
   const int64_t c = (static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x) >> tpr_log2;
   const int64_t b64 = c * len;
@@ -461,34 +502,6 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(int n, int d, int tp
   }
 }
 
-// Zero rows that no id names (dense gradient): a wave per 64 rows, each lane
-// looking its row up in the sorted ids.  Writing them here, and not all rows
-// before the sums, leaves each row one write; 21 us for 50,000 rows of 1,024, about
-// half of them missing.
-__global__ __launch_bounds__(kBlock) void zero_rows_kernel(int n, int Vn, int d,
-                                                           const int* __restrict__ keys,
-                                                           float* __restrict__ out, int64_t ldo) {
-  const int lane = threadIdx.x & 63;
-  const int64_t r0 = ((static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x) >> 6) * 64;
-  if (r0 >= Vn) return;
-  const int64_t r = r0 + lane;
-  int lo = 0, hi = n;
-  while (lo < hi) {
-    const int mid = lo + ((hi - lo) >> 1);
-    if (keys[mid] < r) lo = mid + 1;
-    else hi = mid;
-  }
-  const bool missing = r < Vn && (lo >= n || keys[lo] != r);
-  unsigned long long m = __ballot(missing);
-  while (m) {
-    const int q = __ffsll(m) - 1;
-    m &= m - 1;
-    float* p = out + (r0 + q) * ldo;
-    const float z[4] = {};
-    for (int j = 4 * lane; j < d; j += 256) store_some<GIST_STORE_F32, 4>(p, j, d - j, z);
-  }
-}
-
 size_t up256(size_t x) { return (x + 255) & ~size_t(255); }
 
 struct GradPlan {
@@ -503,8 +516,9 @@ GradPlan plan(int64_t n, int64_t V, int d) {
   p.tiles = (n + kTile - 1) / kTile;
   p.passes = (ceil_log2(V + 1) + kDigit - 1) / kDigit;
   // short chunks where there are few rows, so that there are enough groups; parts
-  // cost two rows a chunk
-  p.len = n <= 32768 ? kBatch : n <= (1 << 20) ? 32 : 128;
+  // cost two rows a chunk.  One chunk, which needs no join, for up to 32 ids: 19.5 us for
+  // 30 ids of a table of 23,673 x 107, 27 with four chunks.
+  p.len = n <= 32 ? 32 : n <= 32768 ? kBatch : n <= (1 << 20) ? 32 : 128;
   p.chunks = (n + p.len - 1) / p.len;
   p.ldp = (d + 3) / 4 * 4;
   p.keys = up256(static_cast<size_t>(n) * 4);
@@ -543,8 +557,16 @@ gist_status embed_grad(hipStream_t st, int64_t n, int64_t V, int d, const int32_
                        int64_t ldo, void* ws) {
   const GradPlan p = plan(n, V, d);
   const int tl = std::min(8, ceil_log2((d + kV - 1) / kV));
-  if ((p.chunks << tl) >= (int64_t{1} << 32) - kBlock)
-    return set_error(GIST_E_UNSUPPORTED, "embed_grad: n * d exceeds the grid");
+  const int slabs = (d + (kV << tl) - 1) / (kV << tl);
+  const int64_t sums = ((p.chunks << tl) + kBlock - 1) / kBlock;
+  // rows to be zeroed per wave: 64, fewer where that leaves the card short of waves, and not
+  // fewer than a wave's lanes reach at once
+  int rl = 6;
+  while (rl > 0 && (V >> rl) * slabs < 4096) --rl;
+  rl = std::max(rl, 6 - zero_lanes_log2(std::min(d, kV << tl)));
+  const int64_t zeros = sgd ? 0 : (((V + (1 << rl) - 1) >> rl) * 64 + kBlock - 1) / kBlock;
+  if ((sums + zeros) * kBlock >= int64_t{1} << 32)
+    return set_error(GIST_E_UNSUPPORTED, "embed_grad: n * d or V exceeds the grid");
   char* c = static_cast<char*>(ws);
   int* k[2] = {reinterpret_cast<int*>(c), reinterpret_cast<int*>(c + p.keys)};
   int* q[2] = {reinterpret_cast<int*>(c + 2 * p.keys), reinterpret_cast<int*>(c + 3 * p.keys)};
@@ -575,30 +597,22 @@ gist_status embed_grad(hipStream_t st, int64_t n, int64_t V, int d, const int32_
     }
     cur ^= 1;
   }
-  if (!sgd) {
-    ProfScope ps(st, "embed_zero_rows", 0.0, 4.0 * V * d);
-    const int64_t blocks = (V + kBlock - 1) / kBlock;
-    zero_rows_kernel<<<dim3(static_cast<unsigned>(blocks)), kBlock, 0, st>>>(ni, vi, d, k[cur],
-                                                                            out, ldo);
+  if (sums + zeros > 0) {
+    ProfScope ps(st, "embed_sum", static_cast<double>(n) * d, 4.0 * d * (2.0 * n + (sgd ? n : V)));
+    const dim3 g(static_cast<unsigned>(sums + zeros), static_cast<unsigned>(slabs));
+    const int first = static_cast<int>(sums);
+    if (sgd)
+      sum_kernel<true><<<g, kBlock, 0, st>>>(first, rl, ni, vi, d, tl, p.len, k[cur], q[cur], scale, dY, ldy, lr, out,
+                                             ldo, part, p.ldp, cross);
+    else
+      sum_kernel<false><<<g, kBlock, 0, st>>>(first, rl, ni, vi, d, tl, p.len, k[cur], q[cur], scale, dY, ldy, lr, out,
+                                              ldo, part, p.ldp, cross);
   }
-  if (n > 0) {
-    const dim3 g(static_cast<unsigned>(((p.chunks << tl) + kBlock - 1) / kBlock),
-                 static_cast<unsigned>((d + (kV << tl) - 1) / (kV << tl)));
-    {
-      ProfScope ps(st, "embed_sum", static_cast<double>(n) * d, 8.0 * n * d);
-      if (sgd)
-        sum_kernel<true><<<g, kBlock, 0, st>>>(ni, vi, d, tl, p.len, k[cur], q[cur], scale, dY, ldy, lr, out, ldo,
-                                               part, p.ldp, cross);
-      else
-        sum_kernel<false><<<g, kBlock, 0, st>>>(ni, vi, d, tl, p.len, k[cur], q[cur], scale, dY, ldy, lr, out, ldo,
-                                                part, p.ldp, cross);
-    }
-    if (p.chunks > 1) {
-      ProfScope ps(st, "embed_join", 0.0, 0.0);
-      const dim3 gj(2 * kJoinBlocks);   // 1,024 threads each: two a CU
-      if (sgd) join_kernel<true><<<gj, kJoinThreads, 0, st>>>(ni, d, tl, p.len, k[cur], scale, lr, out, ldo, part, p.ldp, cross);
-      else join_kernel<false><<<gj, kJoinThreads, 0, st>>>(ni, d, tl, p.len, k[cur], scale, lr, out, ldo, part, p.ldp, cross);
-    }
+  if (p.chunks > 1) {
+    ProfScope ps(st, "embed_join", 0.0, 0.0);
+    const dim3 gj(2 * kJoinBlocks);   // 1,024 threads each: two a CU
+    if (sgd) join_kernel<true><<<gj, kJoinThreads, 0, st>>>(ni, d, tl, p.len, k[cur], scale, lr, out, ldo, part, p.ldp, cross);
+    else join_kernel<false><<<gj, kJoinThreads, 0, st>>>(ni, d, tl, p.len, k[cur], scale, lr, out, ldo, part, p.ldp, cross);
   }
   return check_launch("embed_grad");
 }
