@@ -51,33 +51,40 @@ __global__ __launch_bounds__(kBlock) void lookup_kernel(int n, int64_t V_rows, i
 // ---- sort -----------------------------------------------------------------------
 
 constexpr int kDigit = 8, kBins = 1 << kDigit;
-constexpr int kItems = 8;                   // keys per thread and tile
-constexpr int kTile = kBlock * kItems;      // 2,048
+constexpr int kSortBlock = 1024, kItems = 2;   // threads, keys per thread and tile
+constexpr int kTile = kSortBlock * kItems;     // 2,048
 
 __device__ __forceinline__ int key_of(int id, int V) {   // padding sorts last
   return id >= 0 && id < V ? id : V;
 }
 
-// Digit counts of every tile, digit-major: hist[digit * tiles + tile].
+// Where a tile's count of a digit lies: tile-major where the scatters add them up
+// themselves, digit-major for the scan.
+struct HistAt {
+  int tiles;
+  bool direct;
+  __device__ __forceinline__ int64_t operator()(int64_t tile, int digit) const {
+    return direct ? tile * kBins + digit : static_cast<int64_t>(digit) * tiles + tile;
+  }
+};
+
+// Counts of every tile's digits.
 template <bool FIRST>
-__global__ __launch_bounds__(kBlock) void hist_kernel(int n, int V, const int* __restrict__ keys,
-                                                      int shift, int tiles,
-                                                      int* __restrict__ hist, int* __restrict__ crossing) {
+__global__ __launch_bounds__(kSortBlock) void hist_kernel(int n, int V, const int* __restrict__ keys, int shift,
+                                                          HistAt at, int* __restrict__ hist,
+                                                          int* __restrict__ crossing) {
   __shared__ int cnt[kBins];
   if (FIRST && blockIdx.x == 0 && threadIdx.x < 2) crossing[threadIdx.x] = 0;
-  cnt[threadIdx.x] = 0;
+  if (threadIdx.x < kBins) cnt[threadIdx.x] = 0;
   __syncthreads();
   const int64_t base = static_cast<int64_t>(blockIdx.x) * kTile;
 #pragma unroll
   for (int i = 0; i < kItems; ++i) {
-    const int64_t e = base + i * kBlock + threadIdx.x;
-    if (e < n) {
-      const int k = FIRST ? key_of(keys[e], V) : keys[e];
-      atomicAdd(&cnt[(k >> shift) & (kBins - 1)], 1);
-    }
+    const int64_t e = base + i * kSortBlock + threadIdx.x;
+    if (e < n) atomicAdd(&cnt[((FIRST ? key_of(keys[e], V) : keys[e]) >> shift) & (kBins - 1)], 1);
   }
   __syncthreads();
-  hist[static_cast<int64_t>(threadIdx.x) * tiles + blockIdx.x] = cnt[threadIdx.x];
+  if (threadIdx.x < kBins) hist[at(blockIdx.x, threadIdx.x)] = cnt[threadIdx.x];
 }
 
 // In-place exclusive scan of `count` ints (a multiple of 256) by one workgroup,
@@ -127,26 +134,45 @@ __global__ __launch_bounds__(1024) void scan_kernel(int64_t count, int* __restri
 
 // Stable scatter of every tile's (key, position) pairs by one digit.  A wave
 // holds kItems * 64 consecutive keys, 64 at a time; equal digits among a
-// wave's 64 keys are found by matching the digit's bits with ballots.  Bound by
-// launches and latency: 131,072 ids below 50,000 (two passes of three kernels)
-// 38 us; 54 with tiles of 4,096 keys and a scan of four a thread.
+// wave's 64 keys are found by matching the digit's bits with ballots.  Up to kDirect
+// tiles each workgroup adds up the tiles' counts itself: one launch less than with the
+// scan (two passes over 400,000 ids 31 us and 53, over 2,000,000 154 and 179).  Bound by
+// launches and latency: 131,072 ids below 50,000 in 23 us.  (Adding the next digit's counts up on the way, with an atomic per
+// wave and digit, made a pass one launch, of 18 us in place of 7.)
+constexpr int kDirect = 1024;
 template <bool FIRST>
-__global__ __launch_bounds__(kBlock) void scatter_digit_kernel(
-    int n, int V, const int* __restrict__ kin, const int* __restrict__ pin, int shift, int tiles,
+__global__ __launch_bounds__(kSortBlock) void scatter_digit_kernel(
+    int n, int V, const int* __restrict__ kin, const int* __restrict__ pin, int shift, HistAt at,
     const int* __restrict__ offs, int* __restrict__ kout, int* __restrict__ pout) {
-  constexpr int kWaves = kBlock / 64;
+  constexpr int kWaves = kSortBlock / 64, kQ = kSortBlock / kBins;
   __shared__ int cnt[kWaves][kBins];
+  __shared__ int sums[kQ][2][kBins];
+  __shared__ int wsum[kBins / 64];
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) cnt[w][t] = 0;
-  __syncthreads();
+  for (int x = t; x < kWaves * kBins; x += kSortBlock) (&cnt[0][0])[x] = 0;
+  if (at.direct) {   // thread t: digit t mod kBins, every kQ-th tile
+    const int dg = t & (kBins - 1), part = t / kBins;
+    int total = 0, before = 0;
+#pragma unroll 16
+    for (int x = part; x < at.tiles; x += kQ) {
+      const int c = offs[x * kBins + dg];
+      total += c;
+      before += x < static_cast<int>(blockIdx.x) ? c : 0;
+    }
+    sums[part][0][dg] = total;
+    sums[part][1][dg] = before;
+  }
   const int64_t base = static_cast<int64_t>(blockIdx.x) * kTile + wave * (kItems * 64);
   int key[kItems], rank[kItems];
 #pragma unroll
   for (int i = 0; i < kItems; ++i) {
     const int64_t e = base + i * 64 + lane;
-    const bool in = e < n;
-    key[i] = in ? (FIRST ? key_of(kin[e], V) : kin[e]) : 0;
+    key[i] = e < n ? (FIRST ? key_of(kin[e], V) : kin[e]) : 0;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kItems; ++i) {
+    const bool in = base + i * 64 + lane < n;
     const int dg = (key[i] >> shift) & (kBins - 1);
     unsigned long long m = __ballot(in);
 #pragma unroll
@@ -161,14 +187,36 @@ __global__ __launch_bounds__(kBlock) void scatter_digit_kernel(
     if (in && before == 0) cnt[wave][dg] = had + __popcll(m);
     __builtin_amdgcn_wave_barrier();
   }
-  __syncthreads();
-  {   // thread t turns digit t's counts into the waves' first places
-    int run = offs[static_cast<int64_t>(t) * tiles + blockIdx.x];
+  int first = 0, total = 0, inc = 0;   // digit t: its keys' first place in the tile
+  if (t < kBins) {
+    if (at.direct) {
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
+      for (int x = 0; x < kQ; ++x) {
+        total += sums[x][0][t];
+        first += sums[x][1][t];
+      }
+      inc = total;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int u = __shfl_up(inc, o, 64);
+        if (lane >= o) inc += u;
+      }
+      if (lane == 63) wsum[wave] = inc;
+    } else {
+      first = offs[at(blockIdx.x, t)];
+    }
+  }
+  __syncthreads();
+  if (t < kBins) {
+    if (at.direct) {
+      first += inc - total;
+      for (int w = 0; w < wave; ++w) first += wsum[w];
+    }
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {   // the waves' first places
       const int c = cnt[w][t];
-      cnt[w][t] = run;
-      run += c;
+      cnt[w][t] = first;
+      first += c;
     }
   }
   __syncthreads();
@@ -458,7 +506,9 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(int n, int d, int tp
   auto begins = [&](int64_t x, int cur) { return x * len < n && keys[x * len] == cur; };
   if (blockIdx.x >= kJoinBlocks) {   // ids of few parts
     const int lane = t & ((1 << tpr_log2) - 1), groups = kJoinThreads >> tpr_log2, listed = crossing[0];
-    for (int it = (blockIdx.x - kJoinBlocks) * groups + (t >> tpr_log2); it < listed; it += (gridDim.x - kJoinBlocks) * groups) {
+    const int blocks = gridDim.x - kJoinBlocks;
+    // neighbouring items to different workgroups: with narrow rows a few could take them all
+    for (int it = (t >> tpr_log2) * blocks + (blockIdx.x - kJoinBlocks); it < listed; it += blocks * groups) {
       const int64_t c = crossing[2 + it];
       const int cur = keys[(c + 1) * len];
       int count = 2;
@@ -504,6 +554,9 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(int n, int d, int tp
 
 size_t up256(size_t x) { return (x + 255) & ~size_t(255); }
 
+// Threads (their logarithm) that a row's sum takes.
+int group_log2(int d) { return std::min(8, ceil_log2((d + kV - 1) / kV)); }
+
 struct GradPlan {
   int64_t tiles, chunks, ldp;
   int len, passes;
@@ -515,16 +568,21 @@ GradPlan plan(int64_t n, int64_t V, int d) {
   GradPlan p;
   p.tiles = (n + kTile - 1) / kTile;
   p.passes = (ceil_log2(V + 1) + kDigit - 1) / kDigit;
-  // short chunks where there are few rows, so that there are enough groups; parts
-  // cost two rows a chunk.  One chunk, which needs no join, for up to 32 ids: 19.5 us for
-  // 30 ids of a table of 23,673 x 107, 27 with four chunks.
-  p.len = n <= 32 ? 32 : n <= 32768 ? kBatch : n <= (1 << 20) ? 32 : 128;
+  // short chunks where there are few rows, or narrow ones (a group of few threads each), so
+  // that there are enough groups; parts cost two rows a chunk.  (131,072 ids: one column 12 us
+  // with chunks of 8, 23 of 32; 32 columns 35 and 34, 64 columns 60 and 40; 2,000,000 ids of one
+  // column 66 with chunks of 32, 100 of 128.)  One chunk, which needs no
+  // join, for up to 32 ids.
+  const int tl = group_log2(d);
+  const int64_t most8 = std::max<int64_t>(32768, (int64_t{1} << 20) >> tl);
+  const int64_t most32 = std::max<int64_t>(1 << 20, (int64_t{1} << 23) >> tl);
+  p.len = n <= 32 ? 32 : n <= most8 ? kBatch : n <= most32 ? 32 : 128;
   p.chunks = (n + p.len - 1) / p.len;
   p.ldp = (d + 3) / 4 * 4;
   p.keys = up256(static_cast<size_t>(n) * 4);
   p.hist = up256(static_cast<size_t>(p.tiles) * kBins * 4);
   // room for the chunks of any smaller n too: a workspace for n ids serves fewer
-  const int64_t room = std::max<int64_t>(p.chunks, n > (1 << 20) ? (1 << 20) / 32 : n > 32768 ? 32768 / kBatch : 0);
+  const int64_t room = std::max<int64_t>(p.chunks, n > most32 ? most32 / 32 : n > most8 ? most8 / kBatch : 0);
   p.part = up256(static_cast<size_t>(room) * 2 * p.ldp * 4);
   p.cross = n > 0 ? up256(static_cast<size_t>(room + 2) * 4) : 0;
   return p;
@@ -556,7 +614,7 @@ gist_status embed_grad(hipStream_t st, int64_t n, int64_t V, int d, const int32_
                        float scale, const float* dY, int64_t ldy, bool sgd, float lr, float* out,
                        int64_t ldo, void* ws) {
   const GradPlan p = plan(n, V, d);
-  const int tl = std::min(8, ceil_log2((d + kV - 1) / kV));
+  const int tl = group_log2(d);
   const int slabs = (d + (kV << tl) - 1) / (kV << tl);
   const int64_t sums = ((p.chunks << tl) + kBlock - 1) / kBlock;
   // rows to be zeroed per wave: 64, fewer where that leaves the card short of waves, and not
@@ -580,19 +638,16 @@ gist_status embed_grad(hipStream_t st, int64_t n, int64_t V, int d, const int32_
     small_sort_kernel<<<1, kSmallThreads, 0, st>>>(ni, vi, ids, p.passes, k[0], q[0], cross);
   } else if (n > 0) {
     ProfScope ps(st, "embed_sort", 0.0, 8.0 * n * p.passes);
+    const HistAt at{tiles, tiles <= kDirect};
+    const dim3 g(static_cast<unsigned>(tiles));
     for (int i = 0; i < p.passes; ++i) {
-      const int* kin = i == 0 ? ids : k[cur ^ 1];
+      const int *const kin = i == 0 ? ids : k[cur ^ 1], *const pin = i == 0 ? nullptr : q[cur ^ 1];
       const int shift = i * kDigit;
-      const dim3 g(static_cast<unsigned>(tiles));
-      if (i == 0) hist_kernel<true><<<g, kBlock, 0, st>>>(ni, vi, kin, shift, tiles, hist, cross);
-      else hist_kernel<false><<<g, kBlock, 0, st>>>(ni, vi, kin, shift, tiles, hist, cross);
-      scan_kernel<<<1, 1024, 0, st>>>(p.tiles * kBins, hist);
-      if (i == 0)
-        scatter_digit_kernel<true><<<g, kBlock, 0, st>>>(ni, vi, kin, nullptr, shift, tiles, hist,
-                                                         k[cur], q[cur]);
-      else
-        scatter_digit_kernel<false><<<g, kBlock, 0, st>>>(ni, vi, kin, q[cur ^ 1], shift, tiles,
-                                                          hist, k[cur], q[cur]);
+      if (i == 0) hist_kernel<true><<<g, kSortBlock, 0, st>>>(ni, vi, kin, shift, at, hist, cross);
+      else hist_kernel<false><<<g, kSortBlock, 0, st>>>(ni, vi, kin, shift, at, hist, cross);
+      if (!at.direct) scan_kernel<<<1, 1024, 0, st>>>(p.tiles * kBins, hist);
+      if (i == 0) scatter_digit_kernel<true><<<g, kSortBlock, 0, st>>>(ni, vi, kin, pin, shift, at, hist, k[cur], q[cur]);
+      else scatter_digit_kernel<false><<<g, kSortBlock, 0, st>>>(ni, vi, kin, pin, shift, at, hist, k[cur], q[cur]);
       cur ^= 1;
     }
     cur ^= 1;

@@ -135,6 +135,16 @@ def test_grad(G, ctx, n, V, d, kind):
     assert np.array_equal(Th[:, d:], T0[:, d:])
 
 
+@pytest.mark.parametrize("n,V,d,kind", [(262144, 300, 2, "mixed"), (262145, 70000, 3, "zipf"),
+                                        (300000, 20000000, 1, "distinct"), (1050001, 65537, 1, "zipf"),
+                                        (270000, 1, 5, "same"), (2200000, 100000, 1, "zipf"),
+                                        (8400000, 3000, 1, "mixed"), (140000, 9000, 60, "zipf"), (30, 23673, 107, "zipf"), (9, 1063, 563, "mixed"),
+                                        (40, 4464, 16, "padding"), (3, 500000, 9, "distinct")])
+def test_grad_many_and_few(G, ctx, n, V, d, kind):
+    """Ids of more tiles than a workgroup adds up itself; few ids of a long table."""
+    test_grad(G, ctx, n, V, d, kind)
+
+
 def test_grad_of_nothing(G, ctx):
     """No rows: the dense gradient is zero and the fused step leaves the table alone."""
     import torch
