@@ -180,6 +180,118 @@ __device__ __forceinline__ void write_row(const Out& o, int64_t row, int C, cons
               a.m, ls);
 }
 
+// ---- many short rows, one after another in memory: a lane a row ---------------
+
+// 64 rows through LDS (an odd number of floats apart: lanes fall on different banks).  A
+// lane walks its row twice, for the maximum and the K best, then for the sums.  The K best
+// are a sorted list in registers: where v[k - 1] >= v[k], a logit's insertion leaves
+// v[k] = the median of (z, v[k - 1], v[k]), one instruction; strictly greater logits alone
+// move classes, so equal ones stay in order.  What bounds it: issue, 4 K + 12 instructions
+// for 64 logits, and memory before it: 232,965 rows of 41 classes with the five best
+// take 18 us; with lanes sharing a row (below), 21.
+// When it is taken, us, here and there: 232,965 rows of 16 classes with the eight best 15.5
+// and 18.4, of 24 with five 10.6 and 16.8, of 43 without any 11 and 10, of 47 13 and 11;
+// 100,000 of 40 with five 9.3 and 10.2, 60,000 of them 7.6 and 7.2, 1,536 6.3 and 4.8.
+constexpr int kLaneClasses = 42, kLaneTop = 8;
+constexpr int64_t kLaneRows = 98304;   // six waves a CU
+template <int STORE, int K>
+__global__ __launch_bounds__(64) void lane_rows_kernel(int64_t n, int C, unsigned inv, const void* __restrict__ Z,
+                                                       Out o) {
+  constexpr int V = STORE == GIST_STORE_F32 ? 4 : 8, kU = 4;
+  extern __shared__ __attribute__((aligned(16))) float lds[];   // 64 rows of C | 1, and a vector
+  const int lane = threadIdx.x, ld = C | 1;
+  const int64_t r0 = static_cast<int64_t>(blockIdx.x) * 64;
+  const int rows = static_cast<int>(min<int64_t>(64, n - r0)), count = rows * C;
+  for (int e0 = V * lane; e0 < count; e0 += kU * 64 * V) {
+    float x[kU][V];
+#pragma unroll
+    for (int u = 0; u < kU; ++u) load_some<STORE, V>(Z, r0 * C + e0 + u * 64 * V, count - e0 - u * 64 * V, 0.f, x[u]);
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+      const int e = e0 + u * 64 * V;
+      if (e >= count) break;
+      if (C & 1) {
+#pragma unroll
+        for (int q = 0; q < V; q += 4)
+          *reinterpret_cast<float4*>(lds + e + q) = float4{x[u][q], x[u][q + 1], x[u][q + 2], x[u][q + 3]};
+      } else {
+#pragma unroll
+        for (int q = 0; q < V; q += 2) {   // a pair lies in one row; e / C by inv = 2^20 / C, rounded up
+          const int at = e + q + static_cast<int>((static_cast<unsigned>(e + q) * inv) >> 20);
+          lds[at] = x[u][q];
+          lds[at + 1] = x[u][q + 1];
+        }
+      }
+    }
+  }
+  __syncthreads();
+  if (lane >= rows) return;
+  const float* const z = lds + lane * ld;
+  float m = -INFINITY, v[K > 0 ? K : 1];
+  int cls[K > 0 ? K : 1];
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    v[k] = -INFINITY;
+    cls[k] = -1;
+  }
+#pragma unroll 8
+  for (int j = 0; j < C; ++j) {
+    const float x = z[j];
+    m = max_nan(m, x);
+    if constexpr (K > 0) {
+      bool up[K];
+#pragma unroll
+      for (int k = 0; k < K; ++k) up[k] = x > v[k];
+#pragma unroll
+      for (int k = K - 1; k > 0; --k) {
+        cls[k] = up[k - 1] ? cls[k - 1] : up[k] ? j : cls[k];
+        v[k] = __builtin_amdgcn_fmed3f(x, v[k - 1], v[k]);
+      }
+      cls[0] = up[0] ? j : cls[0];
+      v[0] = fmaxf(x, v[0]);
+    }
+  }
+  Stat a{m, 0.f, 0.f};
+#pragma unroll 8
+  for (int j = 0; j < C; ++j) {
+    const float y = fmaxf((z[j] - m) * kL, kFloor), p = ex2(y);
+    a.s += p;
+    a.t = fmaf(p, y, a.t);
+  }
+  const int64_t row = r0 + lane;
+  const float ls = write_stats<STORE>(o, row, C, Z, C, a, true);
+  if constexpr (K > 0) {
+    if (cls[K - 1] < 0) {   // fewer than K classes above -Inf: then those at -Inf, ascending
+      int f = 0;
+#pragma unroll
+      for (int k = 0; k < K; ++k) f += cls[k] >= 0;
+      for (int j = 0; j < C && f < K; ++j)
+        if (z[j] == -INFINITY) {
+#pragma unroll
+          for (int k = 0; k < K; ++k) cls[k] = k == f ? j : cls[k];
+          ++f;
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < K; ++k) write_top(o, row, K, k, order_bits(v[k]), static_cast<unsigned>(cls[k]), m, ls);
+  }
+}
+
+template <int STORE>
+void lane_rows(hipStream_t st, int64_t n, int C, const void* Z, const Out& o, int K) {
+  const dim3 g(static_cast<unsigned>((n + 63) / 64));
+  const unsigned inv = ((1u << 20) + C - 1) / C;
+  const unsigned lds = (64 * (C | 1) + 8) * 4;
+  switch (K) {
+#define LANE(K)                                                  \
+  case K:                                                        \
+    lane_rows_kernel<STORE, K><<<g, 64, lds, st>>>(n, C, inv, Z, o); \
+    break
+    LANE(0); LANE(1); LANE(2); LANE(3); LANE(4); LANE(5); LANE(6); LANE(7); LANE(8);
+#undef LANE
+  }
+}
+
 // ---- rows of up to 1,024 classes: LPR lanes a row, E classes a lane ----------------
 
 template <int CTRL>
@@ -216,8 +328,8 @@ __device__ __forceinline__ unsigned reduce_u(unsigned x, F f) {
 
 // A row is in registers, so its maximum comes first and nothing is rescaled; the
 // K best are taken out one by one.  What bounds it: issue (a round of the K best
-// is about 5 E + 10 instructions for 64 / LPR rows).  232,965 rows of 41 classes with the
-// five best take 19 us; with a workgroup per row, 735.
+// is about 5 E + 10 instructions for 64 / LPR rows).  232,965 rows of 47 classes with the
+// five best take 21 us.
 template <int STORE, int LPR, int E, bool TOP>
 __global__ __launch_bounds__(kBlock) void short_rows_kernel(int64_t n, int C, const void* __restrict__ Z,
                                                             int64_t ldz, Out o, int K) {
@@ -526,6 +638,12 @@ gist_status log_probs(hipStream_t st, int64_t n, int64_t C, const void* Z, int64
     else if (store == GIST_STORE_BF16) CALL(GIST_STORE_BF16); \
     else CALL(GIST_STORE_F16);                              \
   } while (0)
+  if (n >= kLaneRows && C <= kLaneClasses && K <= kLaneTop && ldz == C) {
+#define LANES(S) lane_rows<S>(st, n, c, Z, o, K)
+    BY_STORE(LANES);
+#undef LANES
+    return check_launch("log_probs");
+  }
   if (C <= kShort) {
 #define SHORT2(S, L, E, T)                                                                         \
   short_rows_kernel<S, L, E, T>                                                                    \

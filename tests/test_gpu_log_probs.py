@@ -204,6 +204,42 @@ def test_backward_special_rows(G, ctx, C):
           np.nan_to_num(R.grad_bound(z, y, gl, gh, "f32")) + 1e-45)
 
 
+@pytest.mark.parametrize("store", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("C,K", [(1, 1), (2, 2), (3, 0), (5, 3), (16, 8), (24, 6), (33, 4), (41, 5), (42, 7)])
+def test_many_short_rows(G, ctx, store, C, K):
+    """Many rows one after another take a lane each; the same rows a column further apart take
+    several.  The same classes and, where both are within the bound of the 64-bit values, at
+    most two bounds between them; some rows against those values."""
+    import torch
+    n = 98304 + 37
+    rng = np.random.default_rng(C * 10 + K)
+    for kind in ("plain", "masked", "ties", "lowest", "offset"):
+        t = logits(n, C, store, rng, kind)
+        y = rng.integers(-1, C + 1, n).astype(np.int32)
+        t[n // 2, C // 2], t[n - 1, 0], t[7] = float("nan"), float("inf"), -float("inf")
+        a = [to_host(x) for x in forward(G, ctx, t, store, y, K, C)[1:]]
+        b = [to_host(x) for x in forward(G, ctx, t, store, y, K, C + 1)[1:]]
+        z = t.float().numpy()
+        lb = R.lse_bound(z) * 2
+        assert np.array_equal(a[4], b[4])
+        with np.errstate(invalid="ignore"):
+            close(a[2], b[2], lb)
+            close(a[1], b[1], 2 * R.entropy_bound(z))
+            for i in (0, 3):
+                bound = lb if i == 0 else lb[:, None]
+                close(a[i], b[i], bound + 2 * R.U32 * np.abs(np.where(np.isfinite(b[i]), b[i], 0)))
+        some = np.unique(np.concatenate([np.arange(0, n, 991), [7, n // 2, n - 1]]))
+        z = z[some]
+        wl, wlp, wH = R.log_probs(z, y[some])
+        lb = R.lse_bound(z)
+        close(a[2][some], wl, lb)
+        close(a[0][some], wlp, lb + R.U32 * np.abs(np.where(np.isfinite(wlp), wlp, 0)))
+        close(a[1][some], wH, R.entropy_bound(z))
+        if K:
+            wi = np.where(np.isnan(wl)[:, None], -1, R.top_classes(z, K))
+            assert np.array_equal(a[4][some], wi)
+
+
 FAR = dict(f32=[1e5, -3e7, 2e30], bf16=[1e4, -3e7, 2e30], f16=[3e4, -6e4])
 
 
