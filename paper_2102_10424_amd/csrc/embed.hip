@@ -341,18 +341,13 @@ __global__ __launch_bounds__(kSmallThreads) void small_sort_kernel(int n, int V,
 
 constexpr int kV = 4;   // columns per thread
 
-// A row's finished sum: the dense gradient, or the SGD step on the table.
+// A row's finished sum: the dense gradient, or the SGD step on the table's row `t`.
 template <bool SGD>
-__device__ __forceinline__ void finish(float* p, int left, const float (&acc)[kV], float scale, float lr) {
+__device__ __forceinline__ void finish(float* p, int left, const float (&acc)[kV], const float (&t)[kV], float scale,
+                                       float lr) {
   float x[kV];
-  if constexpr (SGD) {
-    load_some<GIST_STORE_F32, kV>(p, 0, left, 0.f, x);
 #pragma unroll
-    for (int q = 0; q < kV; ++q) x[q] = fmaf(-lr, scale * acc[q], x[q]);
-  } else {
-#pragma unroll
-    for (int q = 0; q < kV; ++q) x[q] = scale * acc[q];
-  }
+  for (int q = 0; q < kV; ++q) x[q] = SGD ? fmaf(-lr, scale * acc[q], t[q]) : scale * acc[q];
   store_some<GIST_STORE_F32, kV>(p, 0, left, x);
 }
 
@@ -425,10 +420,11 @@ __global__ __launch_bounds__(kBlock) void sum_kernel(int sums, int rows_log2, in
   int cur = keys[b];
   if (cur == Vn) return;   // padding only
   bool head = b > 0 && keys[b - 1] == cur;
-  float acc[kV] = {};
+  float acc[kV] = {}, old[kV];   // the sum of cur's rows, and its row of the table
+  if (SGD) load_some<GIST_STORE_F32, kV>(out + cur * ldo + j, 0, d - j, 0.f, old);
   for (int i = b; i < e; i += kBatch) {
     int k[kBatch], p[kBatch];
-    float x[kBatch][kV];
+    float x[kBatch][kV], o[kBatch][kV];
     // the arrays are padded to whole batches
 #pragma unroll
     for (int u = 0; u < kBatch; u += 4) {
@@ -438,15 +434,24 @@ __global__ __launch_bounds__(kBlock) void sum_kernel(int sums, int rows_log2, in
     }
 #pragma unroll
     for (int u = 0; u < kBatch; ++u)
-      if (i + u < e && k[u] != Vn) load_some<GIST_STORE_F32, kV>(dY, p[u] * ldy + j, d - j, 0.f, x[u]);
+      if (i + u < e && k[u] != Vn) {
+        load_some<GIST_STORE_F32, kV>(dY, p[u] * ldy + j, d - j, 0.f, x[u]);
+        // The table rows of ids that begin here, all on their way before the first is needed:
+        // 131,072 ids of 64 columns 32 us, 40 with each loaded when its sum was done.
+        if (SGD && k[u] != (u ? k[u - 1] : cur)) load_some<GIST_STORE_F32, kV>(out + k[u] * ldo + j, 0, d - j, 0.f, o[u]);
+      }
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
       if (i + u >= e) break;
       if (k[u] != cur) {
         if (head) store_vec<kV>(part + 2 * c * ldp + j, acc);
-        else finish<SGD>(out + cur * ldo + j, d - j, acc, scale, lr);
+        else finish<SGD>(out + cur * ldo + j, d - j, acc, old, scale, lr);
         head = false;
         cur = k[u];
+        if (SGD) {
+#pragma unroll
+          for (int q = 0; q < kV; ++q) old[q] = o[u][q];
+        }
 #pragma unroll
         for (int q = 0; q < kV; ++q) acc[q] = 0.f;
         if (cur == Vn) return;
@@ -463,7 +468,7 @@ __global__ __launch_bounds__(kBlock) void sum_kernel(int sums, int rows_log2, in
       if (far < n && keys[far] == cur) crossing[1 + (n + len - 1) / len - atomicAdd(crossing + 1, 1)] = static_cast<int>(c);
       else crossing[2 + atomicAdd(crossing, 1)] = static_cast<int>(c);
     }
-  } else finish<SGD>(out + cur * ldo + j, d - j, acc, scale, lr);
+  } else finish<SGD>(out + cur * ldo + j, d - j, acc, old, scale, lr);
 }
 
 // Ids that cross chunk borders: the parts of a listed chunk's id are added in chunk
@@ -515,9 +520,10 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(int n, int d, int tp
 #pragma unroll
       for (int x = 2; x < kFew; ++x) count += begins(c + x, cur);
       for (int j = kV * lane; j < d; j += kV << tpr_log2) {
-        float acc[kV] = {};
+        float acc[kV] = {}, old[kV];
+        if (SGD) load_some<GIST_STORE_F32, kV>(out + cur * ldo + j, 0, d - j, 0.f, old);
         add_parts(part, ldp, c, 0, count, j, acc);
-        finish<SGD>(out + cur * ldo + j, d - j, acc, scale, lr);
+        finish<SGD>(out + cur * ldo + j, d - j, acc, old, scale, lr);
       }
     }
     return;
@@ -547,7 +553,9 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(int n, int d, int tp
       for (int g = 1; g < kGroups && g * run < count; ++g)
 #pragma unroll
         for (int q = 0; q < kV; ++q) acc[q] += sh[(g << kSlabLog2) + lane][q];
-      finish<SGD>(out + cur * ldo + j, d - j, acc, scale, lr);
+      float old[kV];
+      if (SGD) load_some<GIST_STORE_F32, kV>(out + cur * ldo + j, 0, d - j, 0.f, old);
+      finish<SGD>(out + cur * ldo + j, d - j, acc, old, scale, lr);
     }
   }
 }
