@@ -395,7 +395,7 @@ __global__ __launch_bounds__(kBlock) void short_rows_kernel(int64_t n, int C, co
 // Bound by memory, and for 16-bit logits by issue beside it: 4,093 rows of 50,001
 // floats with the eight best 164 us (5.0 TB/s; 316 with 4-byte loads, which an odd
 // width took), 8,192 of 32,000 bf16 without any 131 us (4.0 TB/s).  One row of
-// 131,072 bf16 with the 20 best, in 32 parts and a join, 15.7 us; 44.6 with lists begun
+// 131,072 bf16 with the 20 best, in 32 parts and a join, 14.7 us; 44.6 with lists begun
 // by insertions and moved by LDS shuffles.
 template <int STORE, bool TOP>
 __global__ __launch_bounds__(kBlock) void rows_kernel(int64_t items, int parts, int64_t len, int C,
@@ -492,13 +492,16 @@ __global__ __launch_bounds__(kBlock) void rows_kernel(int64_t items, int parts, 
   }
 }
 
-// Joins the parts of a row: each wave a share of them, then the first wave.
+// Joins the parts of a row: each wave a share of them, then the first wave.  32 parts of the
+// 20 best: 6.8 us, 7.8 with one list on its way at a time (lists joined in pairs, fewer one
+// after another, made no difference).
 template <int STORE>
 __global__ __launch_bounds__(kBlock) void join_rows_kernel(int64_t n, int parts, int C,
                                                            const void* __restrict__ Z, int64_t ldz,
                                                            Out o, int K,
                                                            const float* __restrict__ pstat,
                                                            const u64* __restrict__ ptop) {
+  constexpr int kU = 8;
   __shared__ u64 wtop[kWaves][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   for (int64_t row = blockIdx.x; row < n; row += gridDim.x) {
@@ -511,8 +514,17 @@ __global__ __launch_bounds__(kBlock) void join_rows_kernel(int64_t n, int parts,
     Top top;
     top.K = K > 0 ? K : 1;
     if (K > 0) {
-      for (int p = wave; p < parts; p += kWaves)
-        top.join(63 - lane < K ? ptop[(row * parts + p) * K + 63 - lane] : 0, lane);
+      for (int p = wave; p < parts; p += kU * kWaves) {   // kU lists on their way at once
+        u64 x[kU];
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+          const int q = p + u * kWaves;
+          x[u] = q < parts && 63 - lane < K ? ptop[(row * parts + q) * K + 63 - lane] : 0;
+        }
+#pragma unroll
+        for (int u = 0; u < kU; ++u)
+          if (p + u * kWaves < parts) top.join(x[u], lane);
+      }
       __syncthreads();   // the previous row's lists are read
       wtop[wave][63 - lane] = top.mine;
       __syncthreads();
