@@ -557,7 +557,7 @@ gist_status gist_log_probs(gist_ctx* ctx, int64_t n, int64_t C, const void* logi
  * and rounded once to `store`.  (Where |lse| > 64 a row's probabilities are
  * summed again, so that bits its lse has lost to a large offset do not show.)
  * dlogits is n x C (leading dimension ldd, stored as the logits) and may be the
- * logits themselves.  g_logp (then tokens) or g_entropy (then entropy) may be
+ * logits themselves (each row is then one workgroup's: slower for few long ones).  g_logp (then tokens) or g_entropy (then entropy) may be
  * NULL, meaning zero.  A row that is -Inf throughout has gradient 0; a row with
  * a NaN lse, a NaN gradient.  Errors as gist_log_probs. */
 gist_status gist_log_probs_bwd(gist_ctx* ctx, int64_t n, int64_t C, const void* logits,
