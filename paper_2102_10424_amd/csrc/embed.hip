@@ -137,8 +137,9 @@ __global__ __launch_bounds__(1024) void scan_kernel(int64_t count, int* __restri
 // wave's 64 keys are found by matching the digit's bits with ballots.  Up to kDirect
 // tiles each workgroup adds up the tiles' counts itself: one launch less than with the
 // scan (two passes over 400,000 ids 31 us and 53, over 2,000,000 154 and 179).  Bound by
-// launches and latency: 131,072 ids below 50,000 in 23 us.  (Adding the next digit's counts up on the way, with an atomic per
-// wave and digit, made a pass one launch, of 18 us in place of 7.)
+// launches and latency: 131,072 ids below 50,000 in 23 us.  (Adding the next digit's counts
+// up on the way, with an atomic per wave and digit, made a pass one launch, of 18 us in
+// place of 7.)
 constexpr int kDirect = 1024;
 template <bool FIRST>
 __global__ __launch_bounds__(kSortBlock) void scatter_digit_kernel(
