@@ -258,6 +258,7 @@ class Context:
         _check(_lib.gist_create(int(device), _P(stream), C.byref(h)))
         self.handle = h
         self.device = device
+        self.captures = 0      # recordings begun on this context
 
     def set_stream(self, stream):
         _check(_lib.gist_set_stream(self.handle, _P(stream)))
@@ -691,6 +692,7 @@ class Event:
 
 def gist_capture_begin(ctx):
     _check(_lib.gist_capture_begin(ctx.handle))
+    ctx.captures += 1
 
 
 def gist_capture_end(ctx):

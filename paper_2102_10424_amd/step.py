@@ -805,6 +805,18 @@ class LadiesView:
         return self._A[l], self._AT[l]
 
 
+def _recorded(ctx):
+    """Whether a step recorded on ``ctx`` may hold the addresses of a runner's buffers
+    (without a context: assumed)."""
+    return getattr(ctx, "captures", 1) > 0
+
+
+def _grown(need, cap, ctx):
+    """Capacity of a buffer that outgrows ``cap``: what is needed, or, where outgrown
+    buffers are kept, at least twice as much, so that they add up to less than the new one."""
+    return max(need, 2 * cap) if _recorded(ctx) else need
+
+
 def relu_chain_flags(l, L):
     """Backward flags of layer l of L that fuse every hidden layer's ReLU
     derivative into the kernel writing the gradient it multiplies: a hidden
@@ -898,8 +910,27 @@ class SubGCN:
                 f, b = G.gist_layer_workspace_size(self._ldesc(batch, l))
             need = max(need, f, b)
         if self.ws.numel() < need:
+            self._outgrown(self.ws)
+            need = _grown(need, self.ws.numel(), self.ctx)
             self.ws = torch.empty(need, dtype=torch.uint8, device=self.device)
         return self.ws
+
+    def _outgrown(self, *buffers):
+        """Buffers about to be replaced by larger ones live on where a recorded step may
+        use them."""
+        if _recorded(self.ctx):
+            self._kept.append(buffers)
+
+    def _reserve(self, batch):
+        """Activations, gradients and attention coefficients for ``batch``."""
+        n_max = max(batch.rows(l) for l in range(self.L + 1))
+        if n_max > self.n_cap:
+            self._outgrown(self.H, self.agg, self.dH, self.dlogits, self.loss_ws)
+            self._alloc(_grown(n_max, self.n_cap, self.ctx))
+        if self.gat and (self.alpha is None or batch.nnz > self.nnz_cap):
+            self._outgrown(self.alpha)
+            self.nnz_cap = _grown(max(batch.nnz, 1), self.nnz_cap, self.ctx)
+            self.alpha = [torch.empty(self.nnz_cap, device=self.device) for _ in range(self.L)]
 
     def _gat_parts(self, t, l):
         """(Theta, a_src, a_dst) views of a GAT layer's stacked parameters."""
@@ -911,12 +942,7 @@ class SubGCN:
         (``rows(l)``) and each layer's matrix (``adj(l)``): the same for every
         layer for a cluster mini-batch, per layer for a LADIES one."""
         nnz = batch.nnz
-        n_max = max(batch.rows(l) for l in range(self.L + 1))
-        if n_max > self.n_cap:
-            self._alloc(n_max)
-        if self.gat and (self.alpha is None or nnz > self.nnz_cap):
-            self.nnz_cap = max(nnz, 1)
-            self.alpha = [torch.empty(self.nnz_cap, device=self.device) for _ in range(self.L)]
+        self._reserve(batch)
         ws = self._workspace(batch)
         H = batch.X
         for l in range(self.L):
@@ -948,13 +974,10 @@ class SubGCN:
                                 out, self.dlogits[:n], self.loss_ws)
 
     def prepare(self, batch):
-        """Allocate every buffer a step on ``batch`` needs (before a capture)."""
-        n_max = max(batch.rows(l) for l in range(self.L + 1))
-        if n_max > self.n_cap:
-            self._alloc(n_max)
-        if self.gat and (self.alpha is None or batch.nnz > self.nnz_cap):
-            self.nnz_cap = max(batch.nnz, 1)
-            self.alpha = [torch.empty(self.nnz_cap, device=self.device) for _ in range(self.L)]
+        """Allocate every buffer a step on ``batch`` needs (before a capture).  A step
+        recorded on this runner's context (``gist_capture_begin``) keeps working after
+        larger batches: the buffers it was recorded with live as long as the runner."""
+        self._reserve(batch)
         self._workspace(batch)
 
     def backward(self, batch, params, sgd_lr=None):
@@ -1160,6 +1183,7 @@ class SubGCNBatch:
         self.parts = 2 if kind == "sage" else 1
         self.n_cap = 0
         self.clustered = False   # the current batch is a cluster mini-batch
+        self._kept = []          # outgrown workspaces that a recorded step may still use
         self.ws = torch.empty(0, dtype=torch.uint8, device=device)
         self._alloc(n_cap)
         w = self.widths
@@ -1201,6 +1225,9 @@ class SubGCNBatch:
             f, b = G.gist_layer_workspace_size(self.desc(l, n))
             need = max(need, f, b)
         if self.ws.numel() < need:
+            if _recorded(self.ctx):
+                self._kept.append(self.ws)
+            need = _grown(need, self.ws.numel(), self.ctx)
             self.ws = torch.empty(need, dtype=torch.uint8, device=self.device)
         return self.ws
 

@@ -193,3 +193,42 @@ def test_muon_step_trains(G):
     torch.cuda.synchronize()
     for x, y in zip(a[4] + a[5], b[4] + b[5]):
         assert torch.equal(x, y) and bool(torch.isfinite(x).all())
+
+
+@pytest.mark.parametrize("kind", ["gcn", "sage", "gat"])
+def test_replay_after_a_larger_batch(G, kind):
+    """A recorded step works on the buffers it was recorded with after its runner has seen a
+    larger batch, whatever is allocated since: the bits of a runner that saw none."""
+    import torch
+    from paper_2102_10424_amd import step as S
+    inp = setup(kind, 34)
+    st = torch.cuda.Stream()
+    cctx, ectx = G.Context(0, stream=st.cuda_stream), G.Context(0)
+    a, b = device_state(S, cctx, kind, *inp), device_state(S, ectx, kind, *inp)
+    a[0].log_probs(a[2], 3)        # allocates
+    torch.cuda.synchronize()
+    G.gist_capture_begin(cctx)
+    run_step(G, S, cctx, *a)
+    r = G.gist_capture_end(cctx)
+    g = erdos_renyi(900, 6000, seed=35, clusters=3)
+    csr = OM.build(g, [0, 1, 2], "sage" if kind == "sage" else "gcn")
+    csr = {k: np.asarray(v, dtype=np.float32 if k.endswith("val") else np.int32) if np.ndim(v) else v
+           for k, v in csr.items()}
+    n, w = int(csr["n"]), inp[2]
+    big = S.DeviceBatch(csr, torch.ones(n, w[0], device="cuda"), to_dev(np.zeros(n, np.int32)), "cuda")
+    params, ones = [p.clone() for p in a[4]], torch.ones(n, device="cuda")
+    torch.cuda.synchronize()
+    a[0].forward(big, params)
+    lp = a[0].log_probs(big, 3)
+    a[0].log_probs_grad(big, ones)
+    a[0].backward(big, params)
+    torch.cuda.synchronize()
+    assert n > inp[1] and bool(torch.isfinite(lp["logp"]).all())
+    junk = [torch.full((k, inp[1]), float("nan"), device="cuda") for k in (w + [1]) * 4]
+    for k in range(3):
+        run_step(G, S, ectx, *b)
+        G.gist_replay_launch(ectx, r)
+        torch.cuda.synchronize()
+        for x, y in zip(a[4] + a[5] + [a[1].table], b[4] + b[5] + [b[1].table]):
+            assert torch.equal(x, y), k
+    assert all(bool(torch.isnan(j).all()) for j in junk)
