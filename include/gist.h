@@ -468,8 +468,9 @@ gist_status gist_embed_lookup(gist_ctx* ctx, int64_t n, int64_t V, int32_t d, co
  * a fixed order, so results are deterministic: no floating-point atomics.
  * Ids outside [0, V) contribute nothing.  Columns past d are left as they
  * were.  `ws` needs gist_embed_grad_workspace(n, V, d) bytes (0 for
- * arguments the calls reject); what serves n ids serves fewer.  Errors as gist_embed_lookup, and
- * GIST_E_NOMEM for a small workspace. */
+ * arguments the calls reject); what serves n ids serves fewer.  Errors as
+ * gist_embed_lookup, GIST_E_UNSUPPORTED for n above 2^31 - 128, and GIST_E_NOMEM for a small
+ * workspace. */
 size_t gist_embed_grad_workspace(int64_t n, int64_t V, int32_t d);
 gist_status gist_embed_grad(gist_ctx* ctx, int64_t n, int64_t V, int32_t d, const int32_t* ids,
                             float scale, const float* dY, int64_t ldy, float* dTable, int64_t ldg,

@@ -1006,8 +1006,13 @@ extern "C" gist_status gist_embed_lookup(gist_ctx* ctx, int64_t n, int64_t V, in
   return gist::embed_lookup(ctx->stream, n, V, d, table, ldt, store, ids, scale, out, ldo);
 }
 
+namespace {
+// Ids of a table's gradient: its kernels round n up to whole chunks, of at most 128, in int32.
+constexpr int64_t kMostGradIds = (int64_t{1} << 31) - 128;
+}  // namespace
+
 extern "C" size_t gist_embed_grad_workspace(int64_t n, int64_t V, int32_t d) {
-  if (n < 0 || V < 0 || d < 1 || d > (1 << 22) || n >= INT32_MAX || V >= INT32_MAX) return 0;
+  if (n < 0 || V < 0 || d < 1 || d > (1 << 22) || n > kMostGradIds || V >= INT32_MAX) return 0;
   return gist::embed_grad_workspace(n, V, d);
 }
 
@@ -1019,6 +1024,7 @@ gist_status embed_grad_call(const char* what, gist_ctx* ctx, int64_t n, int64_t 
   if (!ctx) return bad(what, GIST_E_INVAL, ": NULL ctx");
   gist::ProfBind pb(ctx);
   GIST_TRY(check_embed(what, n, V, d, ids, scale, ldy, ldo));
+  if (n > kMostGradIds) return bad(what, GIST_E_UNSUPPORTED, ": n above 2^31 - 128");
   if (sgd && !std::isfinite(lr)) return bad(what, GIST_E_INVAL, ": non-finite lr");
   if (V == 0 || (sgd && n == 0)) return GIST_OK;
   if (!out || (n > 0 && !dY)) return bad(what, GIST_E_INVAL, ": NULL pointer");

@@ -384,7 +384,7 @@ __device__ __forceinline__ void zero_rows(int n, int Vn, int j0, int j1, int row
 }
 
 // Chunks of `len` sorted positions (a multiple of kBatch), one group of threads
-// each; blockIdx.y: slab of columns.  part[2 c] is the sum of chunk c's first id
+// each (n + len - 1 fits int32: the caller refuses more than 2^31 - 128 ids); blockIdx.y: slab of columns.  part[2 c] is the sum of chunk c's first id
 // where that id began in an earlier chunk, part[2 c + 1] that of its last id where
 // it began in this chunk and goes on in the next.  The chunks with such an id are
 // listed, in no order: crossing[0] of them, from crossing[2] on, and crossing[1] with

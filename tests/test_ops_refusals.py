@@ -181,6 +181,19 @@ def test_embed_workspace_serves_fewer_ids():
         assert need == sorted(need)
 
 
+def test_embed_grad_ids_that_chunks_would_carry_past_int32():
+    """The gradient's kernels round n up to whole chunks (of 128 for this many ids) in int32:
+    an n that this carries past 2^31 - 1 is refused, and has no workspace."""
+    w = Ws(1 << 62)
+    for n in (2**31 - 127, 2**31 - 8, 2**31 - 2):
+        refused(UNSUP, G.gist_embed_grad, ctx, n, 5, 1, I, 1.0, A, 1, A, 1, w)
+        refused(UNSUP, G.gist_embed_grad_sgd, ctx, n, 5, 1, I, 1.0, A, 1, 0.1, A, 1, w)
+        assert G.gist_embed_grad_workspace(n, 5, 1) == 0
+    need = G.gist_embed_grad_workspace(2**31 - 128, 5, 1)     # the largest accepted: on to the next check
+    assert need > 4 * 4 * (2**31 - 128)
+    refused(NOMEM, G.gist_embed_grad, ctx, 2**31 - 128, 5, 1, I, 1.0, A, 1, A, 1, Ws(need - 1))
+
+
 def test_muon_arrays_that_overlap():
     """An update reads dW again after M is written and W is the last to be: three arrays.  The
     factor may take its gradient's place where both are fp32."""
