@@ -817,6 +817,17 @@ def _grown(need, cap, ctx):
     return max(need, 2 * cap) if _recorded(ctx) else need
 
 
+def _check_array(name, t, dtype, n, d=None):
+    """The kernels take addresses: a tensor of another type, with gaps or too short would be
+    read as something else, or past its end."""
+    if t.dtype != dtype or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor")
+    if d is not None and (t.dim() != 2 or t.shape[1] != d):
+        raise ValueError(f"{name} must have rows of {d}")
+    if n < 0 or t.shape[0] < n:
+        raise ValueError(f"{name} has fewer than {n} rows")
+
+
 def relu_chain_flags(l, L):
     """Backward flags of layer l of L that fuse every hidden layer's ReLU
     derivative into the kernel writing the gradient it multiplies: a hidden
@@ -1127,9 +1138,13 @@ class LearnedRows:
     are a graph's features: ``lookup`` fills a mini-batch's input rows in place
     of the gather of given ones, ``sgd`` steps the rows that were looked up by
     the input gradient of a ``SubGCN(input_grad=True)``.  ``ids`` are device
-    int32 node ids (a batch's node map); ids outside the table are padding."""
+    int32 node ids (a batch's node map); ids outside the table are padding.
+    Arrays of another type, with gaps or too few rows are refused (ValueError)."""
 
     def __init__(self, ctx, table, scale=1.0, n_cap=0, device="cuda"):
+        if table.dim() != 2:
+            raise ValueError("the table is a matrix")
+        _check_array("the table", table, torch.float32, 0)
         self.ctx, self.table, self.scale, self.device = ctx, table, float(scale), device
         self.N, self.d = table.shape
         self.n_cap = 0
@@ -1147,11 +1162,15 @@ class LearnedRows:
 
     def lookup(self, ids, n, X):
         """X[:n] = scale * table[ids[:n]]."""
+        _check_array("ids", ids, torch.int32, n)
+        _check_array("X", X, torch.float32, n, self.d)
         G.gist_embed_lookup(self.ctx, n, self.N, self.d, self.table, self.d, G.GIST_STORE_F32, ids,
                             self.scale, X, self.d)
 
     def sgd(self, ids, n, dX, lr):
         """The SGD step of the looked-up rows, from the gradient dX of X."""
+        _check_array("ids", ids, torch.int32, n)
+        _check_array("dX", dX, torch.float32, n, self.d)
         self._reserve(n)
         G.gist_embed_grad_sgd(self.ctx, n, self.N, self.d, ids, self.scale, dX, self.d, lr,
                               self.table, self.d, self.ws)

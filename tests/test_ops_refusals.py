@@ -277,3 +277,41 @@ def test_orthogonal_reference_forms_agree():
         x = R.orthogonal_noisy(a, 0.0, 0.0, rng)
         # coefficients differ by their rounding to fp32 in the first
         assert np.linalg.norm(w - x) < 1e-5 * np.linalg.norm(w)
+
+
+# ---- the runners' own checks ---------------------------------------------------------
+def no_library(monkeypatch, *names):
+    """Library calls replaced by a count: a refused call makes none."""
+    from paper_2102_10424_amd import step as S
+    calls = []
+    for name in names:
+        monkeypatch.setattr(S.G, name, lambda *a, name=name: calls.append(name))
+    return S, calls
+
+
+def test_learned_rows_check_their_arrays(monkeypatch):
+    """Types, gaps and lengths that the kernels, which see addresses, cannot check."""
+    import torch
+    S, calls = no_library(monkeypatch, "gist_embed_lookup", "gist_embed_grad_sgd")
+    T = torch.zeros(50, 4)
+    for bad in (T.double(), T.half(), T[:, :3], T.t(), torch.zeros(50), torch.zeros(2, 25, 4)):
+        with pytest.raises(ValueError):
+            S.LearnedRows(None, bad, device="cpu")
+    rows = S.LearnedRows(None, T, n_cap=10, device="cpu")
+    ids, X = torch.zeros(10, dtype=torch.int32), torch.zeros(10, 4)
+    bad_ids = (ids.long(), ids.short(), torch.zeros(20, dtype=torch.int32)[::2], ids[:9], ids[:1].expand(10))
+    bad_X = (X.double(), X[:9], torch.zeros(10, 5), torch.zeros(10, 5)[:, :4], torch.zeros(40), X[:1].expand(10, 4))
+    for call in (lambda i, x: rows.lookup(i, 10, x), lambda i, x: rows.sgd(i, 10, x, 0.1)):
+        for i in bad_ids:
+            with pytest.raises(ValueError):
+                call(i, X)
+        for x in bad_X:
+            with pytest.raises(ValueError):
+                call(ids, x)
+    with pytest.raises(ValueError):
+        rows.lookup(ids, -1, X)
+    assert not calls
+    rows.lookup(ids, 10, X)
+    rows.sgd(torch.zeros(64, dtype=torch.int32), 10, torch.zeros(16, 4), 0.1)   # longer ones serve
+    rows.lookup(ids[:0], 0, X[:0])
+    assert calls == ["gist_embed_lookup", "gist_embed_grad_sgd", "gist_embed_lookup"]
