@@ -860,7 +860,8 @@ class SubGCN:
         self.gat = kind == "gat"
         self.input_grad = input_grad
         self.muon_ws = None
-        self.lp = None         # the last log_probs call's buffers
+        self.lp = None         # the last log_probs call's buffers, of the last forward pass
+        self._lp_of = None     # and its rows and labels
         self._lp = {}          # by K
         self._kept = []        # outgrown buffers that a recorded step may still use
         self.nnz_cap = 0
@@ -954,6 +955,7 @@ class SubGCN:
         layer for a cluster mini-batch, per layer for a LADIES one."""
         nnz = batch.nnz
         self._reserve(batch)
+        self.lp = None         # other logits from here on
         ws = self._workspace(batch)
         H = batch.X
         for l in range(self.L):
@@ -1104,6 +1106,7 @@ class SubGCN:
         other here: give them weight 0 in :meth:`log_probs_grad`, or label -1."""
         n, C = batch.rows(self.L), self.widths[-1]
         p = self._log_probs_buffers(n, K)
+        self._lp_of = n, batch.labels.data_ptr()
         G.gist_log_probs(self.ctx, n, C, self.H[self.L], C, G.GIST_STORE_F32, batch.labels,
                          p["logp"], p["entropy"], p["lse"], K, p["top_logp"] if K else None,
                          p["top_idx"] if K else None, p["ws"])
@@ -1111,8 +1114,12 @@ class SubGCN:
 
     def log_probs_grad(self, batch, g_logp, g_entropy=None):
         """In place of :meth:`loss_and_grad`, after :meth:`log_probs`: ``dlogits`` of
-        sum(g_logp * logp + g_entropy * entropy)."""
+        sum(g_logp * logp + g_entropy * entropy), one fp32 weight a row (either may be
+        None).  Refused (ValueError) unless the last forward pass was followed by
+        :meth:`log_probs` of this batch, whose log-sum-exp and entropy it takes."""
         n, C = batch.rows(self.L), self.widths[-1]
+        if self.lp is None or self._lp_of != (n, batch.labels.data_ptr()):
+            raise ValueError("log_probs of this batch's logits comes first")
         G.gist_log_probs_bwd(self.ctx, n, C, self.H[self.L], C, G.GIST_STORE_F32, batch.labels,
                              self.lp["lse"], self.lp["entropy"], g_logp, g_entropy, self.dlogits, C)
 

@@ -315,3 +315,52 @@ def test_learned_rows_check_their_arrays(monkeypatch):
     rows.sgd(torch.zeros(64, dtype=torch.int32), 10, torch.zeros(16, 4), 0.1)   # longer ones serve
     rows.lookup(ids[:0], 0, X[:0])
     assert calls == ["gist_embed_lookup", "gist_embed_grad_sgd", "gist_embed_lookup"]
+
+
+class CpuBatch:
+    """Sizes and labels of a mini-batch without matrices: no library call is made on it."""
+
+    def __init__(self, n):
+        import torch
+        self.n, self.nnz, self.X = n, n, torch.zeros(n, 8)
+        self.labels = torch.zeros(n, dtype=torch.int32)
+
+    def rows(self, l):
+        return self.n
+
+    def adj(self, l):
+        return None, None
+
+
+def test_log_probs_grad_takes_the_last_forward_pass(monkeypatch):
+    """The gradient needs the log-sum-exp of the logits as they are: after another forward
+    pass, of another batch, or without log_probs, it is refused."""
+    import torch
+    S, calls = no_library(monkeypatch, "gist_gcn_layer_fwd", "gist_log_probs", "gist_log_probs_bwd")
+    run = S.SubGCN(None, "gcn", [8, 24, 5], 16, device="cpu")
+    a, b = CpuBatch(16), CpuBatch(16)
+    g = torch.zeros(16)
+    params = [torch.zeros(8, 24), torch.zeros(24, 5)]
+
+    def refuse(batch, *grads):
+        n = len(calls)
+        with pytest.raises(ValueError):
+            run.log_probs_grad(batch, *grads)
+        assert len(calls) == n
+
+    refuse(a, g)                       # no log_probs yet
+    run.forward(a, params)
+    refuse(a, g)
+    run.log_probs(a)
+    run.log_probs_grad(a, g)
+    run.log_probs_grad(a, g, torch.zeros(20))
+    run.log_probs_grad(a, None, g)
+    refuse(b, g)                       # another batch's labels
+    refuse(CpuBatch(9), g)
+    run.log_probs(a, K=3)              # another K, the same logits
+    run.log_probs_grad(a, g)
+    run.forward(b, params)
+    refuse(a, g)
+    refuse(b, g)
+    run.log_probs(b)
+    run.log_probs_grad(b, g)
