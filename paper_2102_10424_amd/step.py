@@ -1077,6 +1077,7 @@ class SubGCN:
         self.prepare_muon(dtype)
         for l in range(self.L):
             r, c = self.widths[l], self.widths[l + 1]
+            _check_array(f"M[{l}]", M[l], torch.float32, r * (2 if self.kind == "sage" else 1), c)
             G.gist_muon_update(self.ctx, self.muon_desc(l, fresh, dtype), params[l], self.dW[l],
                                M[l], lr, momentum, weight_decay, 0.2 * max(r, c) ** 0.5,
                                self.muon_ws)
@@ -1105,6 +1106,8 @@ class SubGCN:
         reuses.  The rows that pad a batch of fixed layout are rows like any
         other here: give them weight 0 in :meth:`log_probs_grad`, or label -1."""
         n, C = batch.rows(self.L), self.widths[-1]
+        if n > self.n_cap:
+            raise ValueError("more rows than any forward pass has had")
         p = self._log_probs_buffers(n, K)
         self._lp_of = n, batch.labels.data_ptr()
         G.gist_log_probs(self.ctx, n, C, self.H[self.L], C, G.GIST_STORE_F32, batch.labels,
@@ -1120,6 +1123,9 @@ class SubGCN:
         n, C = batch.rows(self.L), self.widths[-1]
         if self.lp is None or self._lp_of != (n, batch.labels.data_ptr()):
             raise ValueError("log_probs of this batch's logits comes first")
+        for name, g in (("g_logp", g_logp), ("g_entropy", g_entropy)):
+            if g is not None:
+                _check_array(name, g, torch.float32, n)
         G.gist_log_probs_bwd(self.ctx, n, C, self.H[self.L], C, G.GIST_STORE_F32, batch.labels,
                              self.lp["lse"], self.lp["entropy"], g_logp, g_entropy, self.dlogits, C)
 

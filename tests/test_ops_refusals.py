@@ -357,6 +357,9 @@ def test_log_probs_grad_takes_the_last_forward_pass(monkeypatch):
     run.log_probs_grad(a, None, g)
     refuse(b, g)                       # another batch's labels
     refuse(CpuBatch(9), g)
+    for bad in (g.double(), g[:15], g[:1].expand(16), torch.zeros(32)[::2]):
+        refuse(a, bad)
+        refuse(a, g, bad)
     run.log_probs(a, K=3)              # another K, the same logits
     run.log_probs_grad(a, g)
     run.forward(b, params)
@@ -364,3 +367,21 @@ def test_log_probs_grad_takes_the_last_forward_pass(monkeypatch):
     refuse(b, g)
     run.log_probs(b)
     run.log_probs_grad(b, g)
+    n = len(calls)
+    with pytest.raises(ValueError):
+        run.log_probs(CpuBatch(17))    # more rows than the logits have
+    assert len(calls) == n
+
+
+def test_muon_checks_its_momenta(monkeypatch):
+    import torch
+    S, calls = no_library(monkeypatch, "gist_muon_update")
+    run = S.SubGCN(None, "sage", [8, 24, 5], 16, device="cpu")
+    params = [torch.zeros(16, 24), torch.zeros(48, 5)]
+    ok = [torch.zeros(16, 24), torch.zeros(48, 5)]
+    run.muon(params, ok, 0.1)
+    assert len(calls) == 2
+    for bad in (ok[0].double(), torch.zeros(8, 24), torch.zeros(16, 25)[:, :24], torch.zeros(16 * 24)):
+        with pytest.raises(ValueError):
+            run.muon(params, [bad, ok[1]], 0.1)
+    assert len(calls) == 2
