@@ -1132,7 +1132,9 @@ class SubGCN:
     def step(self, batch, params, lr, adam=None, loss_out=None, muon=None):
         """``subTrain``: forward, loss, backward, update (all enqueued, nothing
         synced).  ``adam`` = (M, V, step, fresh) selects Adam, ``muon`` = (M,
-        fresh) Muon, else SGD."""
+        fresh) Muon, else SGD; both are refused (ValueError)."""
+        if adam is not None and muon is not None:
+            raise ValueError("one optimizer a step: adam or muon")
         self.forward(batch, params)
         self.loss_and_grad(batch, loss_out)
         if muon is not None:

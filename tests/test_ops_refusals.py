@@ -385,3 +385,13 @@ def test_muon_checks_its_momenta(monkeypatch):
         with pytest.raises(ValueError):
             run.muon(params, [bad, ok[1]], 0.1)
     assert len(calls) == 2
+
+
+def test_one_optimizer_a_step(monkeypatch):
+    import torch
+    S, calls = no_library(monkeypatch, "gist_gcn_layer_fwd")
+    run = S.SubGCN(None, "gcn", [8, 24, 5], 16, device="cpu")
+    params = [torch.zeros(8, 24), torch.zeros(24, 5)]
+    with pytest.raises(ValueError):
+        run.step(CpuBatch(16), params, 0.1, adam=(params, params, 1, True), muon=(params, True))
+    assert not calls
