@@ -1090,7 +1090,8 @@ class SubGCN:
         p = self._lp.get(K)
         if p is None or p["n"] < n or p["ws"].numel() < ws:
             self._kept.append(p)
-            n = max(n, self.n_cap)
+            # at least twice as many rows: what is kept adds up to less than what is in use
+            n = max(n, self.n_cap if p is None else 2 * p["n"])
             f = lambda *s: torch.empty(*s, device=self.device)
             p = dict(n=n, logp=f(n), entropy=f(n), lse=f(n), top_logp=f(n, K),
                      top_idx=torch.empty(n, K, dtype=torch.int32, device=self.device),

@@ -70,3 +70,15 @@ def test_workspace_of_a_recorded_batched_step_lives_on():
         sizes.append(run._workspace(n).numel())
     gc.collect()
     assert sizes == sorted(sizes) and ws() is not None
+
+
+def test_log_probs_buffers_double():
+    """Batches that grow one row at a time: few sets of buffers are kept, of fewer rows
+    together than the one in use."""
+    from paper_2102_10424_amd import step as S
+    run = S.SubGCN(Ctx(1), "gcn", [8, 24, 5], 16, device="cpu")
+    for n in range(1, 600):
+        p = run._log_probs_buffers(n, 3)
+        assert p["n"] >= n and p["logp"].shape[0] == p["n"] and p["top_idx"].shape == (p["n"], 3)
+    kept = [k["n"] for k in run._kept if k is not None]
+    assert sum(kept) < p["n"] and len(kept) <= 6
