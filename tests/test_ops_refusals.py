@@ -395,3 +395,18 @@ def test_one_optimizer_a_step(monkeypatch):
     with pytest.raises(ValueError):
         run.step(CpuBatch(16), params, 0.1, adam=(params, params, 1, True), muon=(params, True))
     assert not calls
+
+
+@pytest.mark.parametrize("change,message", [
+    (dict(K=0, top_logp=A), "K == 0 takes no"), (dict(K=0, top_idx=I), "K == 0 takes no"),
+    (dict(K=0, top_logp=A, top_idx=I), "K == 0 takes no"),
+    (dict(K=2), "K > 0 needs"), (dict(K=2, top_logp=A), "K > 0 needs"), (dict(K=2, top_idx=I), "K > 0 needs"),
+    (dict(K=8, top_logp=A, top_idx=I), "K outside"), (dict(K=-1), "K outside"), (dict(tokens=None), "logp needs tokens"),
+    (dict(logits=None), "NULL logits"), (dict(store=3), "unknown store"), (dict(ldz=6), "bad sizes")])
+def test_log_probs_top_outputs_match_K(change, message):
+    """From a call that is right but for the change, each refusal by its own message."""
+    a = dict(n=2, C_=7, logits=A, ldz=7, store=0, tokens=I, logp=A, entropy=A, lse=A, K=0,
+             top_logp=None, top_idx=None, ws=None)
+    with pytest.raises(G.GistError) as e:
+        G.gist_log_probs(ctx, **{**a, **change})
+    assert e.value.status == INVAL and message in str(e.value)
