@@ -541,7 +541,8 @@ gist_status gist_softmax_xent_noalloc(gist_ctx* ctx, int64_t n, int32_t C,
  * Tokens: a negative one means no given class (logp 0; its gradient has no
  * log-probability term); one >= C is the caller's error, reported as a NaN
  * logp (and gradient row).  logp != NULL requires tokens.
- * `ws` needs gist_log_probs_workspace(n, C, K) bytes, which may be 0.
+ * `ws` needs gist_log_probs_workspace(n, C, K) bytes, which may be 0; what
+ * serves n rows serves fewer.
  * Errors: GIST_E_INVAL (n < 0, C < 1, ldz < C, unknown store, K out of
  * range, top outputs not matching K, NULL logits with n > 0, logp without
  * tokens), GIST_E_UNSUPPORTED (n or C >= 2^31 - 1), GIST_E_NOMEM. */

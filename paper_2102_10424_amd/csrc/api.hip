@@ -1092,7 +1092,7 @@ extern "C" gist_status gist_log_probs(gist_ctx* ctx, int64_t n, int64_t C, const
   if (logp && !tokens) return set_error(GIST_E_INVAL, "log_probs: logp needs tokens");
   if (K == 0 && (top_logp || top_idx))
     return set_error(GIST_E_INVAL, "log_probs: K == 0 takes no top_logp or top_idx");
-  const size_t need = gist::log_probs_workspace(n, C, K);
+  const size_t need = gist::log_probs_need(n, C, K);
   if (ws_bytes < need || (need > 0 && !ws))
     return set_error(GIST_E_NOMEM, "log_probs: workspace too small");
   if (need > 0 && (reinterpret_cast<uintptr_t>(ws) & 15u))

@@ -220,7 +220,8 @@ gist_status embed_grad(hipStream_t st, int64_t n, int64_t V, int d, const int32_
                        int64_t ldo, void* ws);
 
 // ---- log probabilities (logprob.hip) ----
-size_t log_probs_workspace(int64_t n, int64_t C, int K);
+size_t log_probs_workspace(int64_t n, int64_t C, int K);   // of up to n rows
+size_t log_probs_need(int64_t n, int64_t C, int K);        // of n rows
 gist_status log_probs(hipStream_t st, int64_t n, int64_t C, const void* Z, int64_t ldz, int store,
                       const int32_t* tokens, float* logp, float* entropy, float* lse, int K,
                       float* top_logp, int32_t* top_idx, void* ws);

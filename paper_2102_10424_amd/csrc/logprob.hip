@@ -609,14 +609,17 @@ struct Plan {
 
 constexpr int64_t kShort = 1024;   // classes that short_rows_kernel takes
 
+constexpr int64_t kManyRows = 1024;   // rows from which each is one part
+
+int64_t most_parts(int64_t C) { return std::max<int64_t>(1, std::min<int64_t>(C / 4096, 256)); }
+
 // Parts of a row: as many as fill the card, of at least 4,096 elements each
 // (16 per thread).
 Plan plan_rows(int64_t n, int64_t C) {
   Plan p{1, C};
   if (C <= kShort) return p;
-  const int64_t want = n >= 1024 ? 1 : (1024 + n - 1) / std::max<int64_t>(n, 1);
-  const int64_t most = C / 4096;
-  p.parts = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({want, most, 256})));
+  const int64_t want = n >= kManyRows ? 1 : (kManyRows + n - 1) / std::max<int64_t>(n, 1);
+  p.parts = static_cast<int>(std::min(want, most_parts(C)));
   p.len = ((C + p.parts - 1) / p.parts + 7) / 8 * 8;
   p.parts = static_cast<int>((C + p.len - 1) / p.len);
   return p;
@@ -624,12 +627,26 @@ Plan plan_rows(int64_t n, int64_t C) {
 
 size_t up256(size_t x) { return (x + 255) & ~size_t(255); }
 
+// Statistics and lists of so many parts.
+size_t part_bytes(int64_t parts, int K) {
+  return up256(static_cast<size_t>(parts) * 16) + static_cast<size_t>(parts) * K * 8;
+}
+
 }  // namespace
 
-size_t log_probs_workspace(int64_t n, int64_t C, int K) {
+size_t log_probs_need(int64_t n, int64_t C, int K) {
   const Plan p = plan_rows(n, C);
   if (p.parts == 1) return 0;
-  return up256(static_cast<size_t>(n) * p.parts * 16) + static_cast<size_t>(n) * p.parts * K * 8;
+  return part_bytes(n * p.parts, K);
+}
+
+// Room for any number of rows up to n: the fewer they are, the more parts a row has.  n rows
+// of ceil(1024 / n) parts are fewer than n + 1024.
+size_t log_probs_workspace(int64_t n, int64_t C, int K) {
+  const int64_t most = most_parts(C);
+  if (most == 1) return 0;
+  n = std::min(n, kManyRows - 1);
+  return part_bytes(std::min(n * most, n + kManyRows - 1), K);
 }
 
 gist_status log_probs(hipStream_t st, int64_t n, int64_t C, const void* Z, int64_t ldz, int store,

@@ -1086,12 +1086,12 @@ class SubGCN:
 
     def _log_probs_buffers(self, n, K):
         """Buffers of :meth:`log_probs`, one set for each K."""
-        ws = G.gist_log_probs_workspace(n, self.widths[-1], K)
         p = self._lp.get(K)
-        if p is None or p["n"] < n or p["ws"].numel() < ws:
+        if p is None or p["n"] < n:
             self._kept.append(p)
             # at least twice as many rows: what is kept adds up to less than what is in use
             n = max(n, self.n_cap if p is None else 2 * p["n"])
+            ws = G.gist_log_probs_workspace(n, self.widths[-1], K)     # of any batch up to n
             f = lambda *s: torch.empty(*s, device=self.device)
             p = dict(n=n, logp=f(n), entropy=f(n), lse=f(n), top_logp=f(n, K),
                      top_idx=torch.empty(n, K, dtype=torch.int32, device=self.device),

@@ -410,3 +410,21 @@ def test_log_probs_top_outputs_match_K(change, message):
     with pytest.raises(G.GistError) as e:
         G.gist_log_probs(ctx, **{**a, **change})
     assert e.value.status == INVAL and message in str(e.value)
+
+
+@pytest.mark.parametrize("C", [5, 1025, 4096, 8191, 8192, 20011, 131072, 1 << 20, 1 << 22])
+def test_log_probs_workspace_serves_fewer_rows(C):
+    """Fewer rows are cut into more parts each: a workspace sized for the largest batch serves
+    every other.  A call's own need is no more than what is reported for it."""
+    sizes = sorted({max(0, n + k) for n in (0, 1, 2, 3, 7, 32, 63, 128, 341, 512, 1000, 1024, 5000, 1 << 20) for k in (-1, 0, 1)})
+    for K in (0, 5):
+        need = [G.gist_log_probs_workspace(n, C, K) for n in sizes]
+        assert need == sorted(need)
+        assert need[-1] < (1 << 17)     # 2,047 parts at most
+        a = dict(C_=C, logits=A, ldz=C, store=0, tokens=I, logp=A, entropy=A, lse=A, K=K,
+                 top_logp=A if K else None, top_idx=I if K else None)
+        for n, w in zip(sizes, need):      # past the size check, on to that of the address
+            if 0 < n < 1024 and w:         # (more rows need no workspace: nothing would be refused)
+                with pytest.raises(G.GistError) as e:
+                    G.gist_log_probs(ctx, n=n, **a, ws=Ws(w, 4104))
+                assert "aligned" in str(e.value), (n, str(e.value))
