@@ -538,11 +538,14 @@ __global__ __launch_bounds__(kBlock) void join_rows_kernel(int64_t n, int parts,
 // dz = g_l (1[j = y] - p) - g_H p (log p + H), p = exp(z - lse).  A group of
 // 1 << tl threads per (row, slab of columns): 64 lanes of a wave or fewer, or the block.
 // An lse beyond kFar has lost bits of log s (2^-19 and more), so the group sums the row's
-// exp(z - lse) first, 1 but for that, and takes its logarithm off.
+// exp(z - lse) first, 1 but for that, and takes its logarithm off.  Each group that does so
+// reads the whole row, so such a row goes to at most `far` groups, of `far_len` columns
+// each, and its other groups have nothing to do: two reads and a write per element.
 // Bound by memory: 8,192 x 32,000 bf16 in 183 us (5.7 TB/s).
 constexpr float kFar = 64.f;
 template <int STORE, int V>
-__global__ __launch_bounds__(kBlock) void bwd_kernel(int64_t items, int slabs, int slab, int tl, int C,
+__global__ __launch_bounds__(kBlock) void bwd_kernel(int64_t items, int slabs, int slab, int far, int far_len,
+                                                     int turn, int tl, int C,
                                                      const void* Z, int64_t ldz,
                                                      const int* __restrict__ tokens,
                                                      const float* __restrict__ lse,
@@ -555,8 +558,8 @@ __global__ __launch_bounds__(kBlock) void bwd_kernel(int64_t items, int slabs, i
   for (int64_t item = (static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x) >> tl; item < items;
        item += (static_cast<int64_t>(gridDim.x) * kBlock) >> tl) {
     const int64_t row = slabs == 1 ? item : item / slabs;
-    const int64_t c0 = slabs == 1 ? 0 : (item - row * slabs) * slab;
-    const int64_t c1 = min<int64_t>(C, c0 + slab);
+    int part = slabs == 1 ? 0 : static_cast<int>(item - row * slabs);
+    int64_t c0 = static_cast<int64_t>(part) * slab, c1 = min<int64_t>(C, c0 + slab);
     const float l = lse[row];
     const float a = gl ? gl[row] : 0.f, b = gh ? gh[row] : 0.f;
     const float h = gh ? ent[row] : 0.f;
@@ -569,6 +572,14 @@ __global__ __launch_bounds__(kBlock) void bwd_kernel(int64_t items, int slabs, i
     if (none) gy = 0.f;
     float ls = 0.f;
     if (!none && !bad && fabsf(l) > kFar) {
+      // Workgroups go to the 8 XCDs in turn, and to the 4 shader engines of each: the first
+      // parts of all rows, 1 << turn of whose multiples meet mod 32, would leave some idle,
+      // so they begin one further after each round of them.
+      part -= static_cast<int>(row >> (5 - turn)) & ((1 << turn) - 1);
+      part += part < 0 ? slabs : 0;
+      if (part >= far) continue;   // more than one part: all of the block's threads
+      c0 = static_cast<int64_t>(part) * far_len;
+      c1 = min<int64_t>(C, c0 + far_len);
       float s = 0.f;
       for (int64_t j = V * lane; j < C; j += V << tl) {
         float z[V];
@@ -601,6 +612,13 @@ __global__ __launch_bounds__(kBlock) void bwd_kernel(int64_t items, int slabs, i
     }
   }
 }
+
+// Groups that far rows go to together: each reads its whole row, so more of them cost more
+// where there are many rows, and fewer leave compute units idle where there are few.  us with
+// 256, 512, 1,024 and with every group of every row, fp32: 64 rows of 131,072 classes 70, 65, 67
+// and 66, 256 of them 135, 109, 118 and 185, 1,100 of them 400, 405, 404 and 868, 40 of 1,000,003
+// 550, 538, 545 and 1,239 (not far: 12, 42, 206 and 55).
+constexpr int64_t kFarGroups = 512;
 
 struct Plan {
   int parts;
@@ -734,10 +752,16 @@ gist_status log_probs_bwd(hipStream_t st, int64_t n, int64_t C, const void* Z, i
   const int64_t step = static_cast<int64_t>(v) << tl;
   const int64_t slab = C <= 8 * step || dZ == Z ? C : 8 * step;
   const int64_t slabs = (C + slab - 1) / slab, items = n * slabs;
+  int64_t far = std::min(slabs, std::max<int64_t>(1, kFarGroups / n));
+  const int64_t far_len = ((C + far - 1) / far + step - 1) / step * step;
+  far = (C + far_len - 1) / far_len;
+  int turn = 0;   // 1 << turn: the largest power of two, up to 32, that divides slabs
+  while (turn < 5 && slabs % (int64_t{2} << turn) == 0) ++turn;
   const dim3 g(static_cast<unsigned>(std::min<int64_t>(((items << tl) + kBlock - 1) / kBlock, 1 << 22)));
   ProfScope ps(st, "log_probs_bwd", 8.0 * n * C, 2.0 * n * C * eb);
 #define BWD(S, W)                                                                                 \
-  bwd_kernel<S, W><<<g, kBlock, 0, st>>>(items, static_cast<int>(slabs), static_cast<int>(slab), tl, \
+  bwd_kernel<S, W><<<g, kBlock, 0, st>>>(items, static_cast<int>(slabs), static_cast<int>(slab),      \
+                                         static_cast<int>(far), static_cast<int>(far_len), turn, tl,  \
                                          static_cast<int>(C), Z, ldz, tokens, lse, entropy, g_logp,  \
                                          g_entropy, dZ, ldd)
   if (store == GIST_STORE_F32) {

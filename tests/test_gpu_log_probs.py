@@ -290,6 +290,76 @@ def test_far_rows(G, ctx, store, n, C, K):
         log(f"far rows {store} n={n} C={C} {far}: error / bound {w:.2f}")
 
 
+@pytest.mark.parametrize("store,n,C", [("f32", 600, 16400), ("f32", 200, 70000), ("f32", 70, 65536), ("f32", 520, 32768),
+                                       ("bf16", 1100, 32000), ("f16", 530, 65537), ("bf16", 90, 131072), ("f32", 3, 300000),
+                                       ("f32", 513, 16384 + 8192)])
+def test_far_rows_among_near_ones(G, ctx, store, n, C):
+    """Rows of several column slabs, every third far: those go to fewer groups than the others.
+    Rows at every place of a round of workgroups against 64 bits, within the bounds of
+    test_far_rows; all rows within two of them of the gradient in place, which has one group a row
+    (its sum of exp(z - lse) and its rounding differ)."""
+    import torch
+    rng = np.random.default_rng(n + C)
+    g = torch.Generator(device="cuda").manual_seed(n + C)
+    dev = torch.randn(n, C, generator=g, device="cuda") * 3
+    dev[::3] += 1000.0
+    dev[1::5, : C // 3] = -float("inf")
+    dev = dev.to(R.torch_type(store))
+    y = rng.integers(0, C, n).astype(np.int32)
+    o = lambda: torch.empty(n, device="cuda")
+    lp, H, l, ws = o(), o(), o(), torch.empty(max(16, G.gist_log_probs_workspace(n, C, 0)), dtype=torch.uint8, device="cuda")
+    s = R.store_of(G, store)
+    G.gist_log_probs(ctx, n, C, dev, C, s, to_dev(y), lp, H, l, 0, None, None, ws)
+    glh, ghh = (rng.standard_normal(n).astype(np.float32) for _ in range(2))
+    gl, gh = to_dev(glh), to_dev(ghh)
+    dz = torch.full((n + 1, C), 5.0, dtype=dev.dtype, device="cuda")
+    G.gist_log_probs_bwd(ctx, n, C, dev, C, s, to_dev(y), l, H, gl, gh, dz, C)
+    assert bool((dz[n].float() == 5).all())
+    some = np.unique(np.concatenate([np.arange(0, min(n, 66), 3), [1, 2, n // 2, n - 1], np.arange(n % 3, n, 96)]))
+    some = some[some < n][:40]
+    bound = np.empty((len(some), C))
+    for i, v in enumerate(some):
+        z = dev[v:v + 1].double().cpu().numpy()
+        z = z - z.max()
+        w = slice(v, v + 1)
+        bound[i] = 2 * R.grad_bound(z, y[w], glh[w], ghh[w], store) + 1e-45
+        close(to_host(dz[w].float()), R.log_probs_grad(z, y[w], glh[w], ghh[w]), bound[i])
+    G.gist_log_probs_bwd(ctx, n, C, dev, C, s, to_dev(y), l, H, gl, gh, dev, C)
+    assert not bool((dz[:n].float() - dev.float()).isnan().any())
+    got, inp = to_host(dz[torch.from_numpy(some).cuda()].float()), to_host(dev[torch.from_numpy(some).cuda()].float())
+    assert (np.abs(got.astype(np.float64) - inp) <= 2 * bound).all()
+    # an element left unwritten or written by the wrong row would be off by whole probabilities
+    assert float((dz[:n].float() - dev.float()).abs().max()) <= float(2 * bound.max())
+
+
+def test_far_rows_cost_no_more_with_more_columns(G, ctx):
+    """An offset of the logits makes a row's gradient read it twice, not once per slab: 300
+    rows of 123 slabs take about twice the time of rows without one, not tens of times."""
+    import torch
+    n, C = 300, 1000003
+    z = torch.randn(n, C, device="cuda")
+    y = torch.zeros(n, dtype=torch.int32, device="cuda")
+    gl = torch.ones(n, device="cuda")
+    lp, H, l = (torch.empty(n, device="cuda") for _ in range(3))
+    ws = torch.empty(G.gist_log_probs_workspace(n, C, 0), dtype=torch.uint8, device="cuda")
+    dz = torch.empty_like(z)
+    us = []
+    for offset in (0.0, 1000.0):
+        z += offset
+        G.gist_log_probs(ctx, n, C, z, C, 0, y, lp, H, l, 0, None, None, ws)
+        times = []
+        for _ in range(5):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            G.gist_log_probs_bwd(ctx, n, C, z, C, 0, y, l, H, gl, gl, dz, C)
+            b.record()
+            torch.cuda.synchronize()
+            times.append(a.elapsed_time(b) * 1e3)
+        us.append(sorted(times)[2])
+    log(f"far rows: {us[0]:.0f} us without an offset, {us[1]:.0f} with one")
+    assert us[1] < 8 * us[0]
+
+
 def test_gradient_against_differences(G, ctx):
     """The gradient against differences of the library's own values: a change h of one logit
     changes logp and entropy by h g + O(h^2); with h = 2^-6 the second-order term is below
