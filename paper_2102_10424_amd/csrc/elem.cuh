@@ -140,6 +140,13 @@ __device__ __forceinline__ void store_some(void* base, int64_t e, int64_t left, 
   }
 }
 
+// Orders a wave's LDS reads and writes before it and after it, whichever lanes make them.
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
 inline int ceil_log2(int64_t x) {
   int l = 0;
   while ((int64_t{1} << l) < x) ++l;

@@ -184,9 +184,9 @@ __global__ __launch_bounds__(kSortBlock) void scatter_digit_kernel(
     const int before = __popcll(m & ((1ull << lane) - 1));
     const int had = cnt[wave][dg];   // the wave's keys of this digit so far
     rank[i] = had + before;
-    __builtin_amdgcn_wave_barrier();
+    wave_sync();
     if (in && before == 0) cnt[wave][dg] = had + __popcll(m);
-    __builtin_amdgcn_wave_barrier();
+    wave_sync();
   }
   int first = 0, total = 0, inc = 0;   // digit t: its keys' first place in the tile
   if (t < kBins) {
@@ -281,9 +281,9 @@ __global__ __launch_bounds__(kSmallThreads) void small_sort_kernel(int n, int V,
       const int before = __popcll(m & ((1ull << lane) - 1));
       const int had = cnt[wave][dg];
       rank[i] = had + before;
-      __builtin_amdgcn_wave_barrier();
+      wave_sync();
       if (in && before == 0) cnt[wave][dg] = had + __popcll(m);
-      __builtin_amdgcn_wave_barrier();
+      wave_sync();
     }
     __syncthreads();
     int total = 0, inc = 0;

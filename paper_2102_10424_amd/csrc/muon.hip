@@ -151,13 +151,6 @@ __device__ __forceinline__ void get8(const Mat& a, int64_t g, int64_t i, int64_t
   }
 }
 
-// Orders a wave's LDS writes before its later reads.
-__device__ __forceinline__ void wave_sync() {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
-}
-
 // Divisor of a group's matrix, from its partial sums: max(norm, eps), and a
 // factor for both where the norm would not fit fp32.
 struct Divisor {
