@@ -266,13 +266,17 @@ __device__ __forceinline__ void wait_loads() {
 }
 
 // 16 bytes per lane from memory straight to LDS: base + off (per lane) to
-// dst + 16 lane.  No register is written; the caller waits for vmcnt.
+// dst + 16 lane.  No vector register is written; the caller waits for vmcnt.
+// (m0, which holds dst, is a register the compiler reserves, of which it warns.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void load_to_lds(unsigned dst, unsigned off, const char* base) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
                :
                : "s"(dst), "v"(off), "s"(base)
-               : "memory");
+               : "memory", "m0");
 }
+#pragma clang diagnostic pop
 
 // Work of one product: tiles of all groups.  The first `whole` are one
 // workgroup's each; the others (`ragged` of them) are cut in K into `slices`
