@@ -11,10 +11,7 @@ namespace gist {
 // moved 16 bytes at a time (the hardware takes any address for global accesses;
 // only a lane whose bytes cross a line costs more).
 typedef float fx4 __attribute__((ext_vector_type(4), aligned(4)));
-typedef float fx2 __attribute__((ext_vector_type(2), aligned(4)));
 typedef unsigned short us8 __attribute__((ext_vector_type(8), aligned(2)));
-typedef unsigned short us4 __attribute__((ext_vector_type(4), aligned(2)));
-typedef unsigned short us2 __attribute__((ext_vector_type(2), aligned(2)));
 
 // ---- stored elements as floats ------------------------------------------------
 
@@ -32,11 +29,8 @@ __device__ __forceinline__ void load_vec(const void* base, int64_t e, float (&x)
       const fx4 t = *reinterpret_cast<const fx4*>(p);
 #pragma unroll
       for (int q = 0; q < 4; ++q) x[q] = t[q];
-    } else if constexpr (V == 2) {
-      const fx2 t = *reinterpret_cast<const fx2*>(p);
-      x[0] = t[0];
-      x[1] = t[1];
     } else {
+      static_assert(V == 1, "one float or four");
       x[0] = *p;
     }
   } else {
@@ -45,15 +39,8 @@ __device__ __forceinline__ void load_vec(const void* base, int64_t e, float (&x)
       const us8 t = *reinterpret_cast<const us8*>(p);
 #pragma unroll
       for (int q = 0; q < 8; ++q) x[q] = widen<STORE>(t[q]);
-    } else if constexpr (V == 4) {
-      const us4 t = *reinterpret_cast<const us4*>(p);
-#pragma unroll
-      for (int q = 0; q < 4; ++q) x[q] = widen<STORE>(t[q]);
-    } else if constexpr (V == 2) {
-      const us2 t = *reinterpret_cast<const us2*>(p);
-      x[0] = widen<STORE>(t[0]);
-      x[1] = widen<STORE>(t[1]);
     } else {
+      static_assert(V == 1, "one 16-bit element or eight");
       x[0] = widen<STORE>(*p);
     }
   }
@@ -61,7 +48,7 @@ __device__ __forceinline__ void load_vec(const void* base, int64_t e, float (&x)
 
 template <int V>
 __device__ __forceinline__ void store_vec(float* p, const float (&x)[V]) {
-  if constexpr (V >= 4) {
+  if constexpr (V == 4 || V == 8) {
 #pragma unroll
     for (int h = 0; h < V; h += 4) {
       fx4 t;
@@ -69,12 +56,8 @@ __device__ __forceinline__ void store_vec(float* p, const float (&x)[V]) {
       for (int q = 0; q < 4; ++q) t[q] = x[h + q];
       *reinterpret_cast<fx4*>(p + h) = t;
     }
-  } else if constexpr (V == 2) {
-    fx2 t;
-    t[0] = x[0];
-    t[1] = x[1];
-    *reinterpret_cast<fx2*>(p) = t;
   } else {
+    static_assert(V == 1, "one float, four or eight");
     *p = x[0];
   }
 }
@@ -96,17 +79,8 @@ __device__ __forceinline__ void store_as(void* base, int64_t e, const float (&x)
 #pragma unroll
       for (int q = 0; q < 8; ++q) t[q] = narrow<STORE>(x[q]);
       *reinterpret_cast<us8*>(p) = t;
-    } else if constexpr (V == 4) {
-      us4 t;
-#pragma unroll
-      for (int q = 0; q < 4; ++q) t[q] = narrow<STORE>(x[q]);
-      *reinterpret_cast<us4*>(p) = t;
-    } else if constexpr (V == 2) {
-      us2 t;
-      t[0] = narrow<STORE>(x[0]);
-      t[1] = narrow<STORE>(x[1]);
-      *reinterpret_cast<us2*>(p) = t;
     } else {
+      static_assert(V == 1, "one 16-bit element or eight");
       *p = narrow<STORE>(x[0]);
     }
   }
