@@ -190,8 +190,12 @@ __device__ __forceinline__ void write_row(const Out& o, int64_t row, int C, cons
 // for 64 logits, and memory before it: 232,965 rows of 41 classes with the five best
 // take 18 us; with lanes sharing a row (below), 21.
 // When it is taken, us, here and there: 232,965 rows of 16 classes with the eight best 15.5
-// and 18.4, of 24 with five 10.6 and 16.8, of 43 without any 11 and 10, of 47 13 and 11;
-// 100,000 of 40 with five 9.3 and 10.2, 60,000 of them 7.6 and 7.2, 1,536 6.3 and 4.8.
+// and 18.4, of 24 with five 10.6 and 16.8; 100,000 of 40 with five 9.3 and 10.2, 60,000 of them
+// 7.6 and 7.2, 1,536 6.3 and 4.8.  The most classes: 232,965 fp32 rows without any best take
+// (43, 47, 56, 64 classes) 11.6, 12.6, 14.4, 16.2 and 9.7, 10.3, 11.4, 12.4, with five 18.3, 20.2,
+// 24.9, 29.0 and 18.8, 19.0, 21.5, 21.5, with eight 24.9, 27.6, 32.8, 36.7 and 24.1, 24.1, 27.9,
+// 27.9: the two meet at 42 or 43.  (A million rows with five: 56, 60, 76, 89 and 67, 67, 82, 86;
+// the limit does not follow them up to where those meet, near 60.)
 constexpr int kLaneClasses = 42, kLaneTop = 8;
 constexpr int64_t kLaneRows = 98304;   // six waves a CU
 template <int STORE, int K>
