@@ -556,12 +556,14 @@ gist_status gist_log_probs(gist_ctx* ctx, int64_t n, int64_t C, const void* logi
  * respect to the logits:
  *   dz_j = g_logp (1[j = y] - p_j) - g_entropy p_j (log p_j + entropy),
  * formed in fp32 from the logits, the lse and entropy of the forward call,
- * and rounded once to `store`.  (Where |lse| > 64 a row's probabilities are
- * summed again, so that bits its lse has lost to a large offset do not show.)
- * dlogits is n x C (leading dimension ldd, stored as the logits) and may be the
- * logits themselves (each row is then one workgroup's: slower for few long ones).  g_logp (then tokens) or g_entropy (then entropy) may be
- * NULL, meaning zero.  A row that is -Inf throughout has gradient 0; a row with
- * a NaN lse, a NaN gradient.  Errors as gist_log_probs. */
+ * and rounded once to `store`.  Up to |lse| = 64 the lse's rounding leaves a
+ * probability off by up to 2^-19 of its value; where |lse| > 64 a row is read twice, its
+ * probabilities summed again, so that bits its lse has lost to a large offset do not show.
+ * dlogits is n x C (leading dimension ldd, stored as the logits) and may be the logits
+ * themselves (each row is then one workgroup's: slower for few long ones).  g_logp (then
+ * tokens) or g_entropy (then entropy) may be NULL, meaning zero.  A row that is -Inf
+ * throughout has gradient 0; a row with a NaN lse, a NaN gradient.  Errors as
+ * gist_log_probs. */
 gist_status gist_log_probs_bwd(gist_ctx* ctx, int64_t n, int64_t C, const void* logits,
                                int64_t ldz, int32_t store, const int32_t* tokens,
                                const float* lse, const float* entropy, const float* g_logp,
@@ -627,11 +629,13 @@ gist_status gist_adam_update_dev(gist_ctx* ctx, float* W, const float* dW, float
  * With the usual coefficients (3.4445, -4.7750, 2.0315) and five steps the
  * singular values end between about 0.7 and 1.2 (Jordan et al., the Muon
  * optimiser); singular vectors are kept.  The norm is summed in double.
- *   dtype GIST_DTYPE_F32      every operand of a product is held in two fp16
- *         parts (22 to 23 significant bits), sums in fp32; output fp32;
- *   dtype GIST_DTYPE_F16_IN   operands are rounded once to fp16 (scaled by
- *         2^12, so that entries down to 2^-26 keep all 11 bits), sums in fp32:
- *         a third of the matrix work.  gist_orthogonalize then writes fp16.
+ *   dtype GIST_DTYPE_F32      every operand of a product (X, A and B) is held in
+ *         two fp16 parts, off by at most 2^-22 of its value and 2^-37 (entries of 2^-15
+ *         and more: 22 bits; of 2^-26: about 11), sums in fp32; output fp32;
+ *   dtype GIST_DTYPE_F16_IN   X, A and B are rounded to fp16 in every step (scaled
+ *         by 2^12, so that entries down to 2^-26 keep all 11 bits), sums in fp32:
+ *         a third of the matrix work, and a factor within about 1.2e-3 of its norm.
+ *         gist_orthogonalize then writes fp16, whose own rounding is 2e-4 of that.
  * Entries are held up to 15 in magnitude, so the coefficients must not let a
  * singular value of [0, 1] (or its square, or |b s^2 + c s^4|) grow past 8 in
  * any step (checked; GIST_E_INVAL).  A zero matrix gives zero; a matrix holding NaN or
@@ -643,7 +647,7 @@ typedef struct gist_muon_desc {
   int32_t steps;   /* Newton-Schulz steps, 1 .. 32                        */
   uint32_t flags;  /* GIST_MUON_NESTEROV | GIST_MUON_FRESH (update only)  */
   float coef[3];   /* a, b, c                                             */
-  float eps;       /* > 0: smallest divisor                               */
+  float eps;       /* smallest divisor, a normal number (>= FLT_MIN)      */
 } gist_muon_desc;
 enum {
   GIST_MUON_NESTEROV = 1,

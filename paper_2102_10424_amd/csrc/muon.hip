@@ -5,9 +5,10 @@
 // Operands.  |entries| <= singular values <= 8 (checked by the caller), so
 // matrices are held times S = 2^12: fp16 then keeps 11 significant bits of
 // entries from 2^-26 up, and all that is below 2^-37 is lost.  fp32 products hold
-// every value in two parts, hi = fp16(v), lo = fp16(v - hi) (22 to 23 bits, a
-// float has 24) and take three products, hi hi' + hi lo' + lo hi'; lo lo' is
-// below 2^-24 of the product.  With fp16 operands there is the one part.
+// every value in two parts, hi = fp16(v), lo = fp16(v - hi) (off by 2^-22 of the value
+// and 2^-37) and take three products, hi hi' + hi lo' + lo hi'; lo lo' is at most
+// 2^-22 of the product of the values.  With fp16 operands there is the one part, of 11 bits:
+// X, A and B are rounded so in every step, which leaves the factor within 1.2e-3 of its norm.
 // The parts are written by the kernel that produces a matrix, so the products
 // load them as they are.  Matrices are padded with zeros to whole tiles, so
 // that no product has edges: zero rows and columns stay zero.
