@@ -757,7 +757,7 @@ gist_status log_probs_bwd(hipStream_t st, int64_t n, int64_t C, const void* Z, i
   const int64_t slab = C <= 8 * step || dZ == Z ? C : 8 * step;
   const int64_t slabs = (C + slab - 1) / slab, items = n * slabs;
   int64_t far = std::min(slabs, std::max<int64_t>(1, kFarGroups / n));
-  const int64_t far_len = ((C + far - 1) / far + step - 1) / step * step;
+  const int64_t far_len = std::min(C, ((C + far - 1) / far + step - 1) / step * step);
   far = (C + far_len - 1) / far_len;
   int turn = 0;   // 1 << turn: the largest power of two, up to 32, that divides slabs
   while (turn < 5 && slabs % (int64_t{2} << turn) == 0) ++turn;
