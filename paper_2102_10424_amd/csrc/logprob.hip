@@ -621,7 +621,8 @@ __global__ __launch_bounds__(kBlock) void bwd_kernel(int64_t items, int slabs, i
 // where there are many rows, and fewer leave compute units idle where there are few.  us with
 // 256, 512, 1,024 and with every group of every row, fp32: 64 rows of 131,072 classes 70, 65, 67
 // and 66, 256 of them 135, 109, 118 and 185, 1,100 of them 400, 405, 404 and 868, 40 of 1,000,003
-// 550, 538, 545 and 1,239 (not far: 12, 42, 206 and 55).
+// 550, 538, 545 and 1,239 (not far: 12, 42, 206 and 55).  Rounded up: 300 rows of 1,000,003 take
+// 1,363, 1,577 with one group each.
 constexpr int64_t kFarGroups = 512;
 
 struct Plan {
@@ -756,7 +757,7 @@ gist_status log_probs_bwd(hipStream_t st, int64_t n, int64_t C, const void* Z, i
   const int64_t step = static_cast<int64_t>(v) << tl;
   const int64_t slab = C <= 8 * step || dZ == Z ? C : 8 * step;
   const int64_t slabs = (C + slab - 1) / slab, items = n * slabs;
-  int64_t far = std::min(slabs, std::max<int64_t>(1, kFarGroups / n));
+  int64_t far = std::min(slabs, (kFarGroups + n - 1) / n);
   const int64_t far_len = std::min(C, ((C + far - 1) / far + step - 1) / step * step);
   far = (C + far_len - 1) / far_len;
   int turn = 0;   // 1 << turn: the largest power of two, up to 32, that divides slabs
