@@ -824,8 +824,8 @@ def _check_array(name, t, dtype, n, d=None):
         raise ValueError(f"{name} must be a contiguous {dtype} tensor")
     if d is not None and (t.dim() != 2 or t.shape[1] != d):
         raise ValueError(f"{name} must have rows of {d}")
-    if n < 0 or t.shape[0] < n:
-        raise ValueError(f"{name} has fewer than {n} rows")
+    if n < 0 or (t.numel() if d is None else t.shape[0]) < n:
+        raise ValueError(f"{name} has fewer than {n} entries")
 
 
 def relu_chain_flags(l, L):

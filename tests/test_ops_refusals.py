@@ -355,6 +355,8 @@ def test_log_probs_grad_takes_the_last_forward_pass(monkeypatch):
     run.log_probs_grad(a, g)
     run.log_probs_grad(a, g, torch.zeros(20))
     run.log_probs_grad(a, None, g)
+    run.log_probs_grad(a, g[:, None], g[None])   # any shape of so many in a row
+    refuse(a, torch.tensor(1.0))
     refuse(b, g)                       # another batch's labels
     refuse(CpuBatch(9), g)
     for bad in (g.double(), g[:15], g[:1].expand(16), torch.zeros(32)[::2]):
