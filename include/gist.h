@@ -17,10 +17,14 @@
  *   gist_gat_layer_fwd/_bwd    the graph attention layer GIST also trains (device)
  *   gist_softmax_xent          loss and its gradient                    (device)
  *   gist_log_probs/_bwd        log probabilities, entropy, best classes (device)
+ *   gist_rms_norm/_bwd         residual's addition and RMS norm         (device)
+ *   gist_quantize_rows         rows in 8 bits with a scale each         (device)
+ *   gist_table_xent            loss against a class table, no logits    (device)
  *   gist_embed_*               learned input rows and their gradient    (device)
  *   gist_sgd_update            one SGD step                             (device)
  *   gist_adam_update           one Adam step (the experiments' optimizer) (device)
  *   gist_adam_update_dev       the same, coefficients read from the device (device)
+ *   gist_adamw_update/_dev     one AdamW step over many tensors         (device)
  *   gist_muon_update           momentum step along an orthogonal factor (device)
  *   gist_subagg                subAgg: Theta[D_in, D_out] <- Theta^(i)  (device)
  *   gist_subagg_gather         subAgg of one round + gather of the next (device)
@@ -237,7 +241,11 @@ typedef enum gist_dtype {
 typedef enum gist_store {
   GIST_STORE_F32 = 0,
   GIST_STORE_BF16 = 1,
-  GIST_STORE_F16 = 2
+  GIST_STORE_F16 = 2,
+  GIST_STORE_E4M3 = 3   /* 8-bit floats (4 exponent, 3 mantissa bits, largest 448) */
+                        /* with an fp32 scale per row: value = code * scale.  Only */
+                        /* gist_rms_norm's and gist_quantize_rows' results and     */
+                        /* gist_table_xent's operands                              */
 } gist_store;
 typedef enum gist_order {
   GIST_ORDER_AUTO = 0,        /* GCN: aggregate at min(s_in, s_out)        */
@@ -569,6 +577,102 @@ gist_status gist_log_probs_bwd(gist_ctx* ctx, int64_t n, int64_t C, const void* 
                                const float* lse, const float* entropy, const float* g_logp,
                                const float* g_entropy, void* dlogits, int64_t ldd);
 
+/* ---- root-mean-square norm, rows in 8 bits ------------------------------ */
+
+/* Per row v < n of width d:
+ *   h = x + residual, rounded to `store` (x and residual are stored so; a
+ *       NULL residual means h = x);
+ *   rstd[v] = 1 / sqrt(mean_j h_j^2 + eps);
+ *   y = h rstd gain, rounded to `out_store`.
+ * gain is fp32 (d entries); h (stored as x) and rstd (fp32) are what the
+ * backward pass takes, either may be NULL.  With out_store GIST_STORE_E4M3 a
+ * row's largest |y| becomes 448 (nearest even), y_scale[v] = largest / 448;
+ * a row of zeros (below 2^-100) has scale 0, one that holds a NaN or an Inf
+ * is NaN throughout.  y_scale must be NULL for the other stores.
+ * Sums are fp32: the norm of a row with |h| above 1e18 overflows (y = 0).
+ * h may be x or residual where the leading dimensions agree, and so may y where
+ * the stores agree too; y may not be h.
+ * Errors: GIST_E_INVAL (n < 0, d < 1, a leading dimension below d, unknown
+ * store, E4M3 as `store`, eps negative or not finite, NULL x, gain or y with
+ * n > 0, y_scale not matching out_store, arrays shared as above does not
+ * allow), GIST_E_UNSUPPORTED (n >= 2^31 - 1, d above 2^22). */
+gist_status gist_rms_norm(gist_ctx* ctx, int64_t n, int32_t d, const void* x, int64_t ldx,
+                          const void* residual, int64_t ldr, int32_t store, const float* gain,
+                          float eps, void* h, int64_t ldh, void* y, int64_t ldy,
+                          int32_t out_store, float* y_scale, float* rstd);
+/* Gradients: with u = dy gain and m = h rstd,
+ *   dx = rstd (u - m mean_j(u_j m_j)) + dsum,   dgain_j = sum_v dy_vj m_vj.
+ * dx is the gradient of x and of the residual alike; dsum (NULL: zero) is
+ * what reaches h itself, the residual stream of the layers above.  dy is
+ * stored as dy_store; h, dsum and dx as `store`; rstd is the forward call's.
+ * dx or dgain (fp32, overwritten) may be NULL.  dgain is summed in a fixed
+ * order: no floating-point atomics.  dx may be dsum or h, or dy where the
+ * stores agree, with one leading dimension.  `ws` needs
+ * gist_rms_norm_bwd_workspace(n, d) bytes (of up to n rows; not needed
+ * without dgain).  Errors as gist_rms_norm, and GIST_E_NOMEM. */
+size_t gist_rms_norm_bwd_workspace(int64_t n, int32_t d);
+gist_status gist_rms_norm_bwd(gist_ctx* ctx, int64_t n, int32_t d, const void* dy, int64_t lddy,
+                              int32_t dy_store, const void* h, int64_t ldh, int32_t store,
+                              const float* gain, const float* rstd, const void* dsum, int64_t ldds,
+                              void* dx, int64_t lddx, float* dgain, void* ws, size_t ws_bytes);
+/* y = the rows of x (n x d, stored as `store`) as e4m3 codes with a scale per
+ * row, by the rule above: a table or rows for gist_table_xent.  Columns past d
+ * are left as they were.  Errors as gist_rms_norm; y may not be x. */
+gist_status gist_quantize_rows(gist_ctx* ctx, int64_t n, int32_t d, const void* x, int64_t ldx,
+                               int32_t store, void* y, int64_t ldy, float* scale);
+
+/* ---- loss against a class table ----------------------------------------- */
+
+/* Softmax cross-entropy of n rows H (n x d) against a table T of class
+ * vectors (C x d: the layout of gist_embed_lookup's table, so the two may be
+ * one), in pieces that never hold all n x C logits:
+ *   z_vj = scale <h_v, t_j>,  lse[v] = log sum_j exp z_vj,
+ *   logp[v] = z_vy - lse[v],  *loss_dev = - mean logp over the labelled rows.
+ * Rows and classes: row v is labelled if v < *n_valid_dev (one device int32,
+ * clamped to [0, n]; NULL: n) and its label is not negative.  A row that is
+ * not labelled adds nothing, has logp 0 and gradient 0, whatever it holds;
+ * with no labelled row the loss is 0.  A label >= C is the caller's error,
+ * reported as a NaN loss and logp.  A NaN in a row makes that row's results and the
+ * loss NaN, a NaN in the table those of every row.
+ * Gradients, where dH and dT are not NULL (both or neither), times grad_scale
+ * (a loss scale for 16-bit gradients; 1 otherwise):
+ *   G_vj = grad_scale scale / count (exp(z_vj - lse[v]) - [j = y_v]),
+ *   dH = G T (n x d),  dT = G^T H (C x d), overwritten.
+ * Operands and products:
+ *   GIST_STORE_F32 with GIST_DTYPE_F32       fp32 products; gradients fp32
+ *   GIST_STORE_F32 with GIST_DTYPE_BF16_IN   operands (H, T and the exponentials)
+ *         rounded to bf16, fp32 sums; gradients fp32
+ *   GIST_STORE_BF16 / F16 (dtype ignored)    operands as stored, exponentials
+ *         rounded to bf16 / fp16, fp32 sums; gradients rounded once to `store`
+ *   GIST_STORE_E4M3   h_v = code h_scale[v], t_j = code t_scale[j] (fp32 scales,
+ *         NULL for the other stores); no gradients.  Sums of 8-bit products lose
+ *         bits below 2^-13 of their largest term.
+ * logp and lse (n fp32 each) may be NULL.  Sums and statistics are fp32.
+ * `ws` needs gist_table_xent_workspace() bytes for this descriptor (gradients:
+ * whether the call has any).  Results are deterministic.  Errors: GIST_E_INVAL (negative n, C < 1,
+ * d < 1, a leading dimension below d, unknown store or dtype, non-finite scale
+ * or grad_scale, NULL H, T or labels with n > 0, NULL loss_dev, one gradient without
+ * the other, gradients of E4M3 operands, scales not matching the store,
+ * gradients that share an array with another operand), GIST_E_UNSUPPORTED (n or C
+ * above 2^30, d above 65,536), GIST_E_NOMEM.
+ * With n == 0 the loss is 0 and dT is zeroed. */
+typedef struct gist_table_xent_desc {
+  int64_t n, C;
+  int32_t d;
+  int32_t store;                  /* gist_store of H, T, dH and dT */
+  int32_t dtype;                  /* gist_dtype: GIST_STORE_F32 only */
+  float scale;                    /* of the logits */
+  float grad_scale;               /* of the gradients */
+  int64_t ldh, ldt, lddh, lddt;   /* 0 means d */
+} gist_table_xent_desc;
+gist_status gist_table_xent_workspace(const gist_table_xent_desc* D, int32_t gradients,
+                                      size_t* bytes);
+gist_status gist_table_xent(gist_ctx* ctx, const gist_table_xent_desc* D, const void* H,
+                            const float* h_scale, const void* T, const float* t_scale,
+                            const int32_t* labels, const int32_t* n_valid_dev, float* loss_dev,
+                            float* logp, float* lse, void* dH, void* dT, void* ws,
+                            size_t ws_bytes);
+
 /* ---- subGCNs slice gather (Section 2.1) ----------------------------- */
 
 /* Ws[i][j] = Wg[rows[i]][cols[j]], i < nr, j < nc: the sub-GCN weight
@@ -618,6 +722,53 @@ gist_status gist_adam_coefficients(float lr, float beta1, float beta2, float eps
 gist_status gist_adam_update_dev(gist_ctx* ctx, float* W, const float* dW, float* m, float* v,
                                  int64_t n, float beta1, float beta2, float eps,
                                  const float* coef_dev);
+
+/* One AdamW step (Loshchilov & Hutter, ICLR 2019: Adam with the weight decay
+ * beside the gradient) over `count` tensors, in one launch for up to 40:
+ *   g = grad_scale dW,  m <- beta1 m + (1 - beta1) g,  v <- beta2 v + (1 - beta2) g^2,
+ *   W <- (1 - lr weight_decay) W
+ *        - lr (m / (1 - beta1^k)) / (sqrt(v / (1 - beta2^k)) + eps).
+ * With weight_decay 0 and grad_scale 1 bitwise gist_adam_update.
+ * 8-bit moments (m_scale and v_scale not NULL): m and sqrt(v) are held as
+ * e4m3 codes, GIST_ADAMW_BLOCK consecutive elements sharing an fp32 scale
+ * (largest magnitude / 448; a block below 2^-100 is zero).  Codes are rounded
+ * stochastically, up with the probability of what is cut off, from 16 bits
+ * each of a mixture of the element's index, the tensor's place in the list and
+ * `seed` (give each step its own): the same call gives the same bits.  A sqrt(v) above
+ * zero is not rounded to zero.  A value that is not finite takes the code of
+ * NaN and leaves the rest of its block alone.  Zero codes and scales are zero
+ * moments.  W, dW, m, v and the copy may be of any alignment their elements have. */
+#define GIST_ADAMW_BLOCK 256
+typedef struct gist_adamw_tensor {
+  float* W;             /* n weights, updated in place                     */
+  const void* dW;       /* n gradients, stored as grad_store               */
+  void* m;              /* n moments: fp32, or codes of one byte           */
+  void* v;
+  float* m_scale;       /* NULL, or ceil(n / GIST_ADAMW_BLOCK) scales each */
+  float* v_scale;
+  void* copy;           /* NULL, or the new W rounded to copy_store        */
+  int64_t n;
+  float weight_decay;
+  int32_t grad_store;   /* GIST_STORE_F32, BF16 or F16                     */
+  int32_t copy_store;   /* GIST_STORE_BF16 or F16                          */
+} gist_adamw_tensor;
+/* `tensors` is host memory, read during the call only.  flags: GIST_ADAM_FRESH.
+ * Errors: GIST_E_INVAL (as gist_adam_update; count or an n negative, unknown
+ * stores, one scale array without the other, a non-finite weight_decay or
+ * grad_scale, NULL or equal pointers among a tensor's W, dW, m, v and copy),
+ * GIST_E_UNSUPPORTED (an n of 2^34 or more).  All tensors are checked before
+ * anything is launched.  Arrays of different tensors must not overlap. */
+gist_status gist_adamw_update(gist_ctx* ctx, const gist_adamw_tensor* tensors, int64_t count,
+                              float lr, float beta1, float beta2, float eps, int64_t step,
+                              uint32_t flags, float grad_scale, uint32_t seed);
+/* The same with what changes from step to step read from device memory, for
+ * recorded steps: coef6 = {lr / (1 - beta1^k), 1 / sqrt(1 - beta2^k), 1 if
+ * GIST_ADAM_FRESH else 0, lr, grad_scale, the bits of seed}.  The tensors' addresses
+ * and sizes are recorded with the launch. */
+gist_status gist_adamw_coefficients(float lr, float beta1, float beta2, float eps, int64_t step,
+                                    uint32_t flags, float grad_scale, uint32_t seed, float* coef6);
+gist_status gist_adamw_update_dev(gist_ctx* ctx, const gist_adamw_tensor* tensors, int64_t count,
+                                  float beta1, float beta2, float eps, const float* coef_dev);
 
 /* ---- orthogonalised updates ------------------------------------------- */
 

@@ -1226,6 +1226,246 @@ extern "C" gist_status gist_muon_update(gist_ctx* ctx, const gist_muon_desc* D, 
 }
 
 // ---------------------------------------------------------------------------
+// Root-mean-square norm, rows in 8 bits, loss against a class table, AdamW
+// ---------------------------------------------------------------------------
+
+namespace {
+bool any_store(int32_t s) { return known_store(s) || s == GIST_STORE_E4M3; }
+
+gist_status check_rows(const char* what, int64_t n, int32_t d) {
+  if (n < 0 || d < 1) return bad(what, GIST_E_INVAL, ": bad sizes");
+  if (n >= INT32_MAX) return bad(what, GIST_E_UNSUPPORTED, ": n exceeds int32");
+  if (d > (1 << 22)) return bad(what, GIST_E_UNSUPPORTED, ": d above 4194304");
+  return GIST_OK;
+}
+
+// Two arrays of one call at one address: only where every element lies at its own place in both.
+bool shared_badly(const void* a, int64_t lda, int32_t sa, const void* b, int64_t ldb, int32_t sb) {
+  return a && a == b && (lda != ldb || sa != sb);
+}
+}  // namespace
+
+extern "C" gist_status gist_rms_norm(gist_ctx* ctx, int64_t n, int32_t d, const void* x, int64_t ldx,
+                                     const void* residual, int64_t ldr, int32_t store,
+                                     const float* gain, float eps, void* h, int64_t ldh, void* y,
+                                     int64_t ldy, int32_t out_store, float* y_scale, float* rstd) {
+  gist::clear_error();
+  if (!ctx) return set_error(GIST_E_INVAL, "rms_norm: NULL ctx");
+  gist::ProfBind pb(ctx);
+  GIST_TRY(check_rows("rms_norm", n, d));
+  if (ldx < d || ldy < d || (residual && ldr < d) || (h && ldh < d))
+    return set_error(GIST_E_INVAL, "rms_norm: leading dimension below d");
+  if (!known_store(store) || !any_store(out_store))
+    return set_error(GIST_E_INVAL, "rms_norm: unknown store");
+  if (!(eps >= 0.f) || !std::isfinite(eps)) return set_error(GIST_E_INVAL, "rms_norm: bad eps");
+  if (n == 0) return GIST_OK;
+  if (!x || !gain || !y) return set_error(GIST_E_INVAL, "rms_norm: NULL pointer");
+  if ((y_scale != nullptr) != (out_store == GIST_STORE_E4M3))
+    return set_error(GIST_E_INVAL, "rms_norm: y_scale goes with an 8-bit result");
+  if (shared_badly(x, ldx, 0, h, ldh, 0) || shared_badly(residual, ldr, 0, h, ldh, 0) ||
+      shared_badly(x, ldx, store, y, ldy, out_store) ||
+      shared_badly(residual, ldr, store, y, ldy, out_store) || (h && h == y))
+    return set_error(GIST_E_INVAL, "rms_norm: arrays share memory otherwise than element by element");
+  gist::DeviceGuard dg(ctx->device);
+  return gist::rms_norm(ctx->stream, n, d, x, ldx, residual, ldr, store, gain, eps, h, ldh, y, ldy,
+                        out_store, y_scale, rstd);
+}
+
+extern "C" size_t gist_rms_norm_bwd_workspace(int64_t n, int32_t d) {
+  if (n < 0 || d < 1 || n >= INT32_MAX || d > (1 << 22)) return 0;
+  return gist::rms_norm_bwd_workspace(n, d);
+}
+
+extern "C" gist_status gist_rms_norm_bwd(gist_ctx* ctx, int64_t n, int32_t d, const void* dy,
+                                         int64_t lddy, int32_t dy_store, const void* h, int64_t ldh,
+                                         int32_t store, const float* gain, const float* rstd,
+                                         const void* dsum, int64_t ldds, void* dx, int64_t lddx,
+                                         float* dgain, void* ws, size_t ws_bytes) {
+  gist::clear_error();
+  if (!ctx) return set_error(GIST_E_INVAL, "rms_norm_bwd: NULL ctx");
+  gist::ProfBind pb(ctx);
+  GIST_TRY(check_rows("rms_norm_bwd", n, d));
+  if (lddy < d || ldh < d || (dsum && ldds < d) || (dx && lddx < d))
+    return set_error(GIST_E_INVAL, "rms_norm_bwd: leading dimension below d");
+  if (!known_store(store) || !known_store(dy_store))
+    return set_error(GIST_E_INVAL, "rms_norm_bwd: unknown store");
+  if (n > 0 && (!dy || !h || !gain || !rstd))
+    return set_error(GIST_E_INVAL, "rms_norm_bwd: NULL pointer");
+  if (shared_badly(dy, lddy, dy_store, dx, lddx, store) || shared_badly(h, ldh, 0, dx, lddx, 0) ||
+      shared_badly(dsum, ldds, 0, dx, lddx, 0))
+    return set_error(GIST_E_INVAL, "rms_norm_bwd: arrays share memory otherwise than element by element");
+  if (!dx && !dgain) return GIST_OK;
+  if (dgain && n > 0) {
+    if (ws_bytes < gist::rms_norm_bwd_workspace(n, d) || !ws)
+      return set_error(GIST_E_NOMEM, "rms_norm_bwd: workspace too small");
+    if (reinterpret_cast<uintptr_t>(ws) & 15u)
+      return set_error(GIST_E_INVAL, "rms_norm_bwd: workspace not aligned to 16 bytes");
+  }
+  gist::DeviceGuard dg(ctx->device);
+  return gist::rms_norm_bwd(ctx->stream, n, d, dy, lddy, dy_store, h, ldh, store, gain, rstd, dsum,
+                            ldds, dx, lddx, dgain, ws);
+}
+
+extern "C" gist_status gist_quantize_rows(gist_ctx* ctx, int64_t n, int32_t d, const void* x,
+                                          int64_t ldx, int32_t store, void* y, int64_t ldy,
+                                          float* scale) {
+  gist::clear_error();
+  if (!ctx) return set_error(GIST_E_INVAL, "quantize_rows: NULL ctx");
+  gist::ProfBind pb(ctx);
+  GIST_TRY(check_rows("quantize_rows", n, d));
+  if (ldx < d || ldy < d) return set_error(GIST_E_INVAL, "quantize_rows: leading dimension below d");
+  if (!known_store(store)) return set_error(GIST_E_INVAL, "quantize_rows: unknown store");
+  if (n == 0) return GIST_OK;
+  if (!x || !y || !scale) return set_error(GIST_E_INVAL, "quantize_rows: NULL pointer");
+  if (x == y) return set_error(GIST_E_INVAL, "quantize_rows: not in place");
+  gist::DeviceGuard dg(ctx->device);
+  return gist::quantize_rows(ctx->stream, n, d, x, ldx, store, y, ldy, scale);
+}
+
+namespace {
+// The descriptor with its leading dimensions filled in.
+gist_status check_table_xent(const char* what, const gist_table_xent_desc* in,
+                             gist_table_xent_desc* D) {
+  if (!in) return bad(what, GIST_E_INVAL, ": NULL descriptor");
+  *D = *in;
+  if (D->n < 0 || D->C < 1 || D->d < 1) return bad(what, GIST_E_INVAL, ": bad sizes");
+  for (int64_t* ld : {&D->ldh, &D->ldt, &D->lddh, &D->lddt}) {
+    if (*ld == 0) *ld = D->d;
+    if (*ld < D->d) return bad(what, GIST_E_INVAL, ": leading dimension below d");
+  }
+  if (!any_store(D->store)) return bad(what, GIST_E_INVAL, ": unknown store");
+  if (D->store == GIST_STORE_F32 && D->dtype != GIST_DTYPE_F32 && D->dtype != GIST_DTYPE_BF16_IN)
+    return bad(what, GIST_E_INVAL, ": dtype is F32 or BF16_IN");
+  if (!std::isfinite(D->scale) || !std::isfinite(D->grad_scale))
+    return bad(what, GIST_E_INVAL, ": non-finite scale");
+  if (D->n > (1 << 30) || D->C > (1 << 30))
+    return bad(what, GIST_E_UNSUPPORTED, ": n or C above 2^30");
+  if (D->d > 65536) return bad(what, GIST_E_UNSUPPORTED, ": d above 65536");
+  return GIST_OK;
+}
+}  // namespace
+
+extern "C" gist_status gist_table_xent_workspace(const gist_table_xent_desc* D, int32_t gradients,
+                                                 size_t* bytes) {
+  gist::clear_error();
+  if (!bytes) return set_error(GIST_E_INVAL, "table_xent_workspace: NULL out");
+  gist_table_xent_desc E;
+  GIST_TRY(check_table_xent("table_xent_workspace", D, &E));
+  if (gradients && E.store == GIST_STORE_E4M3)
+    return set_error(GIST_E_INVAL, "table_xent_workspace: 8-bit operands have no gradients");
+  *bytes = gist::table_xent_workspace(&E, gradients != 0);
+  return GIST_OK;
+}
+
+extern "C" gist_status gist_table_xent(gist_ctx* ctx, const gist_table_xent_desc* D, const void* H,
+                                       const float* h_scale, const void* T, const float* t_scale,
+                                       const int32_t* labels, const int32_t* n_valid_dev,
+                                       float* loss_dev, float* logp, float* lse, void* dH, void* dT,
+                                       void* ws, size_t ws_bytes) {
+  gist::clear_error();
+  if (!ctx) return set_error(GIST_E_INVAL, "table_xent: NULL ctx");
+  gist::ProfBind pb(ctx);
+  gist_table_xent_desc E;
+  GIST_TRY(check_table_xent("table_xent", D, &E));
+  if (!loss_dev) return set_error(GIST_E_INVAL, "table_xent: NULL loss");
+  const bool eight = E.store == GIST_STORE_E4M3;
+  // rows without entries have no gradient to point to
+  if (E.n > 0 && (dH != nullptr) != (dT != nullptr))
+    return set_error(GIST_E_INVAL, "table_xent: one gradient without the other");
+  if (eight && (dH || dT))
+    return set_error(GIST_E_INVAL, "table_xent: 8-bit operands have no gradients");
+  if (E.n > 0 && (!H || !T || !labels)) return set_error(GIST_E_INVAL, "table_xent: NULL pointer");
+  if (E.n > 0 && ((h_scale != nullptr) != eight || (t_scale != nullptr) != eight))
+    return set_error(GIST_E_INVAL, "table_xent: scales go with 8-bit operands, both of them");
+  if (dH && (dH == H || dH == T || dT == H || dT == T || dH == dT))
+    return set_error(GIST_E_INVAL, "table_xent: gradients need arrays of their own");
+  const size_t need = gist::table_xent_need(&E, H, T, dH != nullptr);
+  if (ws_bytes < need || (need > 0 && !ws))
+    return set_error(GIST_E_NOMEM, "table_xent: workspace too small");
+  if (need > 0 && (reinterpret_cast<uintptr_t>(ws) & 15u))
+    return set_error(GIST_E_INVAL, "table_xent: workspace not aligned to 16 bytes");
+  gist::DeviceGuard dg(ctx->device);
+  return gist::table_xent(ctx->stream, &E, H, h_scale, T, t_scale, labels, n_valid_dev, loss_dev, logp,
+                          lse, dH, dT, ws);
+}
+
+namespace {
+gist_status adamw_coef(const char* what, float lr, float beta1, float beta2, float eps, int64_t step,
+                       uint32_t flags, float grad_scale, uint32_t seed, float* out) {
+  GIST_TRY(adam_coef(what, lr, beta1, beta2, eps, step, flags, out));
+  if (!std::isfinite(grad_scale)) return bad(what, GIST_E_INVAL, ": non-finite grad_scale");
+  out[3] = lr;
+  out[4] = grad_scale;
+  std::memcpy(&out[5], &seed, sizeof(seed));
+  return GIST_OK;
+}
+
+gist_status check_adamw(const char* what, const gist_adamw_tensor* T, int64_t count) {
+  if (count < 0 || (count > 0 && !T)) return bad(what, GIST_E_INVAL, ": bad list of tensors");
+  if (count >= INT32_MAX) return bad(what, GIST_E_UNSUPPORTED, ": too many tensors");
+  for (int64_t i = 0; i < count; ++i) {
+    const gist_adamw_tensor& t = T[i];
+    if (t.n < 0) return bad(what, GIST_E_INVAL, ": negative n");
+    if (t.n >= (int64_t{1} << 34)) return bad(what, GIST_E_UNSUPPORTED, ": n of 2^34 or more");
+    if (!known_store(t.grad_store)) return bad(what, GIST_E_INVAL, ": unknown store of a gradient");
+    if (t.copy && t.copy_store != GIST_STORE_BF16 && t.copy_store != GIST_STORE_F16)
+      return bad(what, GIST_E_INVAL, ": a copy is bf16 or fp16");
+    if (!std::isfinite(t.weight_decay)) return bad(what, GIST_E_INVAL, ": non-finite weight_decay");
+    if ((t.m_scale != nullptr) != (t.v_scale != nullptr))
+      return bad(what, GIST_E_INVAL, ": scales of one moment only");
+    if (t.n == 0) continue;
+    if (!t.W || !t.dW || !t.m || !t.v) return bad(what, GIST_E_INVAL, ": NULL pointer");
+    const void* p[] = {t.W, t.dW, t.m, t.v, t.copy, t.m_scale, t.v_scale};
+    for (int a = 0; a < 7; ++a)
+      for (int b = 0; b < a; ++b)
+        if (p[a] && p[a] == p[b]) return bad(what, GIST_E_INVAL, ": a tensor's arrays must differ");
+  }
+  return GIST_OK;
+}
+}  // namespace
+
+extern "C" gist_status gist_adamw_coefficients(float lr, float beta1, float beta2, float eps,
+                                               int64_t step, uint32_t flags, float grad_scale,
+                                               uint32_t seed, float* coef6) {
+  gist::clear_error();
+  if (!coef6) return set_error(GIST_E_INVAL, "adamw_coefficients: NULL out");
+  float c[6];
+  GIST_TRY(adamw_coef("adamw_coefficients", lr, beta1, beta2, eps, step, flags, grad_scale, seed, c));
+  std::memcpy(coef6, c, sizeof(c));
+  return GIST_OK;
+}
+
+extern "C" gist_status gist_adamw_update(gist_ctx* ctx, const gist_adamw_tensor* tensors,
+                                         int64_t count, float lr, float beta1, float beta2, float eps,
+                                         int64_t step, uint32_t flags, float grad_scale,
+                                         uint32_t seed) {
+  gist::clear_error();
+  if (!ctx) return set_error(GIST_E_INVAL, "adamw_update: NULL ctx");
+  gist::ProfBind pb(ctx);
+  float c[6];
+  GIST_TRY(adamw_coef("adamw_update", lr, beta1, beta2, eps, step, flags, grad_scale, seed, c));
+  GIST_TRY(check_adamw("adamw_update", tensors, count));
+  gist::DeviceGuard dg(ctx->device);
+  return gist::adamw(ctx->stream, tensors, count, c, beta1, beta2, eps, nullptr);
+}
+
+extern "C" gist_status gist_adamw_update_dev(gist_ctx* ctx, const gist_adamw_tensor* tensors,
+                                             int64_t count, float beta1, float beta2, float eps,
+                                             const float* coef_dev) {
+  gist::clear_error();
+  if (!ctx) return set_error(GIST_E_INVAL, "adamw_update_dev: NULL ctx");
+  gist::ProfBind pb(ctx);
+  if (!(beta1 >= 0.f && beta1 < 1.f) || !(beta2 >= 0.f && beta2 < 1.f))
+    return set_error(GIST_E_INVAL, "adamw_update_dev: beta outside [0, 1)");
+  if (!(eps >= 0.f) || !std::isfinite(eps))
+    return set_error(GIST_E_INVAL, "adamw_update_dev: bad eps");
+  if (!coef_dev) return set_error(GIST_E_INVAL, "adamw_update_dev: NULL coefficients");
+  GIST_TRY(check_adamw("adamw_update_dev", tensors, count));
+  gist::DeviceGuard dg(ctx->device);
+  return gist::adamw(ctx->stream, tensors, count, nullptr, beta1, beta2, eps, coef_dev);
+}
+
+// ---------------------------------------------------------------------------
 // Instrumentation
 // ---------------------------------------------------------------------------
 

@@ -236,4 +236,31 @@ size_t muon_workspace(const gist_muon_desc* D);
 gist_status muon(hipStream_t st, const gist_muon_desc* D, const float* G, void* O, float* W,
                  float* M, float lr, float momentum, float decay, float scale, void* ws);
 
+// ---- root-mean-square norm (norm.hip) ----
+gist_status rms_norm(hipStream_t st, int64_t n, int d, const void* x, int64_t ldx, const void* r,
+                     int64_t ldr, int store, const float* gain, float eps, void* h, int64_t ldh,
+                     void* y, int64_t ldy, int out_store, float* y_scale, float* rstd);
+size_t rms_norm_bwd_workspace(int64_t n, int d);
+gist_status rms_norm_bwd(hipStream_t st, int64_t n, int d, const void* dy, int64_t lddy,
+                         int dy_store, const void* h, int64_t ldh, int store, const float* gain,
+                         const float* rstd, const void* dsum, int64_t ldds, void* dx, int64_t lddx,
+                         float* dgain, void* ws);
+gist_status quantize_rows(hipStream_t st, int64_t n, int d, const void* x, int64_t ldx, int store,
+                          void* y, int64_t ldy, float* scale);
+
+// ---- loss against a class table (table_xent.hip) ----
+// D: leading dimensions filled in.  The workspace serves operands at any address; `need` is
+// what these take.
+size_t table_xent_workspace(const gist_table_xent_desc* D, bool gradients);
+size_t table_xent_need(const gist_table_xent_desc* D, const void* H, const void* T, bool gradients);
+gist_status table_xent(hipStream_t st, const gist_table_xent_desc* D, const void* H,
+                       const float* h_scale, const void* T, const float* t_scale,
+                       const int32_t* labels, const int32_t* n_dev, float* loss, float* logp,
+                       float* lse, void* dH, void* dT, void* ws);
+
+// ---- AdamW over many tensors (adamw.hip) ----
+// coef (host, six floats) or coef_dev.
+gist_status adamw(hipStream_t st, const gist_adamw_tensor* T, int64_t count, const float* coef,
+                  float beta1, float beta2, float eps, const float* coef_dev);
+
 }  // namespace gist

@@ -1,0 +1,569 @@
+// Root-mean-square norm with the residual's addition, its gradients, and rows
+// in 8 bits.
+//
+//   h = x + r (rounded to its store),  s = (mean_j h_j^2 + eps)^-1/2,  y = h s g;
+//   with u = dy g and n = h s:  dx = s (u - n mean_j(u_j n_j)) + dsum,  dg = sum_v dy n.
+//
+// All of it is bound by memory: every array is read or written once.  A row is
+// held in the registers of a wave, or of a workgroup of 256 where rows are long
+// or few; longer rows than a workgroup holds are read twice.  Sums are fp32.
+//
+// 8-bit rows: e4m3, the row's largest magnitude at 448, nearest even.
+//
+// The gain's gradient: a workgroup keeps its rows' sum of dy n in registers (every
+// thread has the same columns in each of its rows), writes it once, and a second
+// launch adds the workgroups' sums in order: the same bits every time.
+
+#include <algorithm>
+
+#include "elem.cuh"
+
+namespace gist {
+
+namespace {
+
+constexpr int kBlock = 256;
+constexpr float kTop = 448.f;             // largest e4m3 value
+constexpr int64_t kMostBlocks = 1 << 16;  // rows go around them
+
+typedef unsigned u32u __attribute__((aligned(1)));
+
+template <int STORE>
+constexpr int vec_of() { return STORE == GIST_STORE_F32 ? 4 : 8; }
+
+// Sums over the THREADS threads of a row, in a fixed order.  `sh`: two floats a wave, used in
+// turn (`turn` flips), so that one barrier a sum is enough.
+template <int THREADS>
+__device__ __forceinline__ float row_sum(float v, float* sh, int& turn) {
+  v = wave_sum(v);
+  if constexpr (THREADS == 64) return v;
+  float* s = sh + turn * (THREADS / 64);
+  turn ^= 1;
+  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = 0.f;
+#pragma unroll
+  for (int w = 0; w < THREADS / 64; ++w) v += s[w];
+  return v;
+}
+// The largest of magnitudes; as integers their bits are in the same order, and a NaN's are
+// above all others'.
+template <int THREADS>
+__device__ __forceinline__ float row_max(float m, float* sh, int& turn) {
+  int v = __float_as_int(m);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v = max(v, __shfl_xor(v, o, 64));
+  if constexpr (THREADS == 64) return __int_as_float(v);
+  float* s = sh + turn * (THREADS / 64);
+  turn ^= 1;
+  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = __int_as_float(v);
+  __syncthreads();
+  v = __float_as_int(s[0]);
+#pragma unroll
+  for (int w = 1; w < THREADS / 64; ++w) v = max(v, __float_as_int(s[w]));
+  return __int_as_float(v);
+}
+__device__ __forceinline__ float larger(float big, float y) {
+  return __int_as_float(max(__float_as_int(big), __float_as_int(fabsf(y))));
+}
+
+// V values times inv as e4m3 codes, the first `left` of them stored.
+template <int V>
+__device__ __forceinline__ void store_e4m3(void* base, int64_t e, int64_t left, const float (&y)[V], float inv) {
+  unsigned char* p = static_cast<unsigned char*>(base) + e;
+#pragma unroll
+  for (int h = 0; h < V; h += 4) {
+    float c[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const float a = y[h + q] * inv;
+      c[q] = a > kTop ? kTop : a < -kTop ? -kTop : a;   // the product's rounding; NaN stays
+    }
+    int u = __builtin_amdgcn_cvt_pk_fp8_f32(c[0], c[1], 0, false);
+    u = __builtin_amdgcn_cvt_pk_fp8_f32(c[2], c[3], u, true);
+    if (left >= h + 4) {
+      *reinterpret_cast<u32u*>(p + h) = static_cast<unsigned>(u);
+    } else {
+#pragma unroll
+      for (int q = 0; q < 3; ++q)
+        if (h + q < left) p[h + q] = static_cast<unsigned char>(u >> (8 * q));
+    }
+  }
+}
+
+struct Fwd {
+  int64_t n, ldx, ldr, ldh, ldy;
+  int d;
+  const void* x;
+  const void* r;
+  const float* gain;
+  void* h;
+  void* y;
+  float* y_scale;
+  float* rstd;
+  float eps;
+};
+
+template <int STORE, int V>
+__device__ __forceinline__ void load_h(const Fwd& a, int64_t row, int c, int left, float (&h)[V]) {
+  load_some<STORE, V>(a.x, row * a.ldx + c, left, 0.f, h);
+  if (a.r) {
+    float r[V];
+    load_some<STORE, V>(a.r, row * a.ldr + c, left, 0.f, r);
+#pragma unroll
+    for (int q = 0; q < V; ++q) {
+      h[q] += r[q];
+      if constexpr (STORE != GIST_STORE_F32) h[q] = widen<STORE>(narrow<STORE>(h[q]));
+    }
+  }
+}
+
+template <int OUT, int V>
+__device__ __forceinline__ void store_y(void* base, int64_t e, int left, const float (&y)[V], float inv) {
+  if constexpr (OUT == GIST_STORE_E4M3) {
+    store_e4m3<V>(base, e, left, y, inv);
+  } else if constexpr (OUT != GIST_STORE_F32 && V == 4) {
+    typedef unsigned short us4 __attribute__((ext_vector_type(4), aligned(2)));
+    unsigned short* p = static_cast<unsigned short*>(base) + e;
+    us4 t;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) t[q] = narrow<OUT>(y[q]);
+    if (left >= 4) {
+      *reinterpret_cast<us4*>(p) = t;
+    } else {
+#pragma unroll
+      for (int q = 0; q < 3; ++q)
+        if (q < left) p[q] = t[q];
+    }
+  } else {
+    store_some<OUT, V>(base, e, left, y);
+  }
+}
+
+// A row's scale from its largest magnitude, and what takes its values to codes.  A row that
+// holds a NaN or an Inf is NaN throughout; one below kLeast is zero.
+constexpr float kLeast = 0x1p-100f;
+__device__ __forceinline__ float scale_of(float big, float& inv) {
+  if (!(big < __builtin_inff())) big = __builtin_nanf("");
+  const bool zero = big < kLeast;
+  inv = zero ? 0.f : kTop / big;
+  return zero ? 0.f : big / kTop;
+}
+
+// A row in the registers of THREADS threads: CH loads of V elements each.  NORM false: no
+// norm, the row's codes alone.
+template <int STORE, int OUT, int THREADS, int CH, bool NORM>
+__global__ __launch_bounds__(kBlock) void rows_kernel(Fwd a) {
+  constexpr int V = vec_of<STORE>();
+  __shared__ float sh[2 * kBlock / 64];
+  int turn = 0;
+  const int lane = threadIdx.x % THREADS;
+  const float inv_d = 1.f / static_cast<float>(a.d);
+  constexpr int RB = kBlock / THREADS;
+  for (int64_t row = blockIdx.x * RB + threadIdx.x / THREADS; row < a.n; row += static_cast<int64_t>(gridDim.x) * RB) {
+    float h[CH][V];
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+      const int c = (i * THREADS + lane) * V;
+#pragma unroll
+      for (int q = 0; q < V; ++q) h[i][q] = 0.f;
+      if (c < a.d) load_h<STORE, V>(a, row, c, a.d - c, h[i]);
+    }
+    float big = 0.f;
+    if constexpr (NORM) {
+      float s = 0.f;
+#pragma unroll
+      for (int i = 0; i < CH; ++i) {
+        float p = 0.f;
+#pragma unroll
+        for (int q = 0; q < V; ++q) p = fmaf(h[i][q], h[i][q], p);
+        s += p;
+      }
+      const float rstd = 1.f / sqrtf(row_sum<THREADS>(s, sh, turn) * inv_d + a.eps);
+      if (a.rstd && lane == 0) a.rstd[row] = rstd;
+#pragma unroll
+      for (int i = 0; i < CH; ++i) {
+        const int c = (i * THREADS + lane) * V;
+        if (c >= a.d) continue;
+        if (a.h) store_some<STORE, V>(a.h, row * a.ldh + c, a.d - c, h[i]);
+        float g[V];
+#pragma unroll
+        for (int q = 0; q < V; q += 4) {
+          float t[4];
+          load_some<GIST_STORE_F32, 4>(a.gain, c + q, a.d - c - q, 0.f, t);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) g[q + k] = t[k];
+        }
+#pragma unroll
+        for (int q = 0; q < V; ++q) h[i][q] = h[i][q] * rstd * g[q];
+        if constexpr (OUT != GIST_STORE_E4M3) store_y<OUT, V>(a.y, row * a.ldy + c, a.d - c, h[i], 0.f);
+      }
+    }
+    if constexpr (OUT == GIST_STORE_E4M3) {
+#pragma unroll
+      for (int i = 0; i < CH; ++i)
+#pragma unroll
+        for (int q = 0; q < V; ++q) big = larger(big, h[i][q]);
+      float inv;
+      const float scale = scale_of(row_max<THREADS>(big, sh, turn), inv);
+      if (lane == 0) a.y_scale[row] = scale;
+#pragma unroll
+      for (int i = 0; i < CH; ++i) {
+        const int c = (i * THREADS + lane) * V;
+        if (c < a.d) store_y<OUT, V>(a.y, row * a.ldy + c, a.d - c, h[i], inv);
+      }
+    }
+  }
+}
+
+// Rows longer than a workgroup's registers: read again from x and r for each pass.
+template <int STORE, int OUT, bool NORM>
+__global__ __launch_bounds__(kBlock) void long_rows_kernel(Fwd a) {
+  constexpr int V = vec_of<STORE>();
+  __shared__ float sh[2 * kBlock / 64];
+  int turn = 0;
+  const float inv_d = 1.f / static_cast<float>(a.d);
+  for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
+    float rstd = 1.f;
+    if constexpr (NORM) {
+      float s = 0.f;
+      for (int64_t c = threadIdx.x * V; c < a.d; c += kBlock * V) {
+        float h[V], p = 0.f;
+        load_h<STORE, V>(a, row, c, a.d - c, h);
+#pragma unroll
+        for (int q = 0; q < V; ++q) p = fmaf(h[q], h[q], p);
+        s += p;
+      }
+      rstd = 1.f / sqrtf(row_sum<kBlock>(s, sh, turn) * inv_d + a.eps);
+      if (a.rstd && threadIdx.x == 0) a.rstd[row] = rstd;
+    }
+    float big = 0.f, inv = 0.f;
+    // for codes: first the largest magnitude, then the codes
+    for (int pass = OUT == GIST_STORE_E4M3 ? 0 : 1; pass < 2; ++pass) {
+      for (int64_t c = threadIdx.x * V; c < a.d; c += kBlock * V) {
+        float h[V];
+        const int left = static_cast<int>(min(static_cast<int64_t>(V), a.d - c));
+        load_h<STORE, V>(a, row, c, left, h);
+        float y[V];
+#pragma unroll
+        for (int q = 0; q < V; ++q) y[q] = NORM ? h[q] * rstd * (q < left ? a.gain[c + q] : 0.f) : h[q];
+        if (pass == 0) {
+#pragma unroll
+          for (int q = 0; q < V; ++q) big = larger(big, y[q]);
+        } else {
+          store_y<OUT, V>(a.y, row * a.ldy + c, left, y, inv);
+          if (NORM && a.h) store_some<STORE, V>(a.h, row * a.ldh + c, left, h);
+        }
+      }
+      if (pass == 0) {
+        const float scale = scale_of(row_max<kBlock>(big, sh, turn), inv);
+        if (threadIdx.x == 0) a.y_scale[row] = scale;
+      }
+    }
+  }
+}
+
+struct Bwd {
+  int64_t n, lddy, ldh, ldds, lddx;
+  int d;
+  const void* dy;
+  const void* h;
+  const float* gain;
+  const float* rstd;
+  const void* dsum;
+  void* dx;
+  float* part;      // [grid][d]
+};
+
+// V elements of any store (V as the rows' own loads have it).
+template <int STORE, int V>
+__device__ __forceinline__ void load_any(const void* base, int64_t e, int left, float (&x)[V]) {
+  if constexpr (STORE == GIST_STORE_F32 && V == 8) {
+#pragma unroll
+    for (int h = 0; h < 8; h += 4) {
+      float t[4];
+      load_some<STORE, 4>(base, e + h, left - h, 0.f, t);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) x[h + q] = t[q];
+    }
+  } else if constexpr (STORE != GIST_STORE_F32 && V == 4) {
+    typedef unsigned short us4 __attribute__((ext_vector_type(4), aligned(2)));
+    const unsigned short* p = static_cast<const unsigned short*>(base) + e;
+    if (left >= 4) {
+      const us4 t = *reinterpret_cast<const us4*>(p);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) x[q] = widen<STORE>(t[q]);
+    } else {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) x[q] = q < left ? widen<STORE>(p[q]) : 0.f;
+    }
+  } else {
+    load_some<STORE, V>(base, e, left, 0.f, x);
+  }
+}
+
+template <int STORE, int DY, int THREADS, int CH>
+__global__ __launch_bounds__(kBlock) void bwd_kernel(Bwd a) {
+  constexpr int V = vec_of<STORE>();
+  __shared__ float sh[2 * kBlock / 64];
+  __shared__ __attribute__((aligned(16))) float join[THREADS == 64 ? 64 * CH * V : 4];
+  int turn = 0;
+  const int lane = threadIdx.x % THREADS, sub = threadIdx.x / THREADS;
+  const float inv_d = 1.f / static_cast<float>(a.d);
+  constexpr int RB = kBlock / THREADS;
+  float acc[CH][V] = {}, g[CH][V];
+#pragma unroll
+  for (int i = 0; i < CH; ++i) {
+    const int c = (i * THREADS + lane) * V;
+#pragma unroll
+    for (int q = 0; q < V; ++q) g[i][q] = 0.f;
+    if (c < a.d) load_any<GIST_STORE_F32, V>(a.gain, c, a.d - c, g[i]);
+  }
+  for (int64_t row = blockIdx.x * RB + sub; row < a.n; row += static_cast<int64_t>(gridDim.x) * RB) {
+    const float s = a.rstd[row];
+    float h[CH][V], y[CH][V], dot = 0.f;
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+      const int c = (i * THREADS + lane) * V;
+#pragma unroll
+      for (int q = 0; q < V; ++q) h[i][q] = y[i][q] = 0.f;
+      if (c < a.d) {
+        load_some<STORE, V>(a.h, row * a.ldh + c, a.d - c, 0.f, h[i]);
+        load_any<DY, V>(a.dy, row * a.lddy + c, a.d - c, y[i]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < CH; ++i)
+#pragma unroll
+      for (int q = 0; q < V; ++q) {
+        h[i][q] *= s;
+        acc[i][q] = fmaf(y[i][q], h[i][q], acc[i][q]);
+        y[i][q] *= g[i][q];
+        dot = fmaf(y[i][q], h[i][q], dot);
+      }
+    dot = row_sum<THREADS>(dot, sh, turn) * inv_d;
+    if (a.dx) {
+#pragma unroll
+      for (int i = 0; i < CH; ++i) {
+        const int c = (i * THREADS + lane) * V;
+        if (c >= a.d) continue;
+        float z[V];
+#pragma unroll
+        for (int q = 0; q < V; ++q) z[q] = 0.f;
+        if (a.dsum) load_some<STORE, V>(a.dsum, row * a.ldds + c, a.d - c, 0.f, z);
+#pragma unroll
+        for (int q = 0; q < V; ++q) z[q] = fmaf(s, y[i][q] - h[i][q] * dot, z[q]);
+        store_some<STORE, V>(a.dx, row * a.lddx + c, a.d - c, z);
+      }
+    }
+  }
+  if (!a.part) return;
+  if constexpr (THREADS == 64) {     // the workgroup's waves, in order
+    for (int w = 0; w < RB; ++w) {
+      if (sub == w) {
+#pragma unroll
+        for (int i = 0; i < CH; ++i)
+#pragma unroll
+          for (int q = 0; q < V; ++q) {
+            float* p = join + (i * 64 + lane) * V + q;
+            acc[i][q] += w == 0 ? 0.f : *p;
+            if (w + 1 < RB) *p = acc[i][q];
+          }
+      }
+      if (w + 1 < RB) __syncthreads();
+    }
+    if (sub != RB - 1) return;
+  }
+  float* const out = a.part + static_cast<int64_t>(blockIdx.x) * a.d;
+#pragma unroll
+  for (int i = 0; i < CH; ++i) {
+    const int c = (i * THREADS + lane) * V;
+    if (c >= a.d) continue;
+#pragma unroll
+    for (int q = 0; q < V; ++q)
+      if (c + q < a.d) out[c + q] = acc[i][q];
+  }
+}
+
+// Rows longer than a workgroup's registers: two passes a row; the gain's sums lie in `part`,
+// where the same thread adds to the same columns.
+template <int STORE, int DY>
+__global__ __launch_bounds__(kBlock) void long_bwd_kernel(Bwd a) {
+  constexpr int V = vec_of<STORE>();
+  __shared__ float sh[2 * kBlock / 64];
+  int turn = 0;
+  const float inv_d = 1.f / static_cast<float>(a.d);
+  float* const out = a.part ? a.part + static_cast<int64_t>(blockIdx.x) * a.d : nullptr;
+  bool first = true;
+  for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
+    const float s = a.rstd[row];
+    float dot = 0.f;
+    for (int64_t c = threadIdx.x * V; c < a.d; c += kBlock * V) {
+      const int left = static_cast<int>(min(static_cast<int64_t>(V), a.d - c));
+      float h[V], y[V];
+      load_some<STORE, V>(a.h, row * a.ldh + c, left, 0.f, h);
+      load_any<DY, V>(a.dy, row * a.lddy + c, left, y);
+#pragma unroll
+      for (int q = 0; q < V; ++q) {
+        if (q >= left) break;
+        h[q] *= s;
+        const float p = y[q] * h[q];
+        if (out) out[c + q] = first ? p : out[c + q] + p;
+        dot = fmaf(y[q] * a.gain[c + q], h[q], dot);
+      }
+    }
+    dot = row_sum<kBlock>(dot, sh, turn) * inv_d;
+    first = false;
+    if (!a.dx) continue;
+    for (int64_t c = threadIdx.x * V; c < a.d; c += kBlock * V) {
+      const int left = static_cast<int>(min(static_cast<int64_t>(V), a.d - c));
+      float h[V], y[V], z[V];
+#pragma unroll
+      for (int q = 0; q < V; ++q) z[q] = 0.f;
+      load_some<STORE, V>(a.h, row * a.ldh + c, left, 0.f, h);
+      load_any<DY, V>(a.dy, row * a.lddy + c, left, y);
+      if (a.dsum) load_some<STORE, V>(a.dsum, row * a.ldds + c, left, 0.f, z);
+#pragma unroll
+      for (int q = 0; q < V; ++q) {
+        const float g = q < left ? a.gain[c + q] : 0.f;
+        z[q] = fmaf(s, y[q] * g - h[q] * s * dot, z[q]);
+      }
+      store_some<STORE, V>(a.dx, row * a.lddx + c, left, z);
+    }
+  }
+}
+
+// dgain[c] = sum of `parts` rows of part: 64 columns a workgroup, its 16 groups of 64 threads
+// each every 16th row, joined in order.
+constexpr int kJoinWaves = 16;
+__global__ __launch_bounds__(64 * kJoinWaves) void gain_kernel(int parts, int d, const float* __restrict__ part,
+                                                               float* __restrict__ dgain) {
+  __shared__ float sh[kJoinWaves][64];
+  const int c = blockIdx.x * 64 + (threadIdx.x & 63), w = threadIdx.x >> 6;
+  float s = 0.f;
+  if (c < d) {
+    int p = w;
+    for (; p + 3 * kJoinWaves < parts; p += 4 * kJoinWaves) {
+      float v[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = part[static_cast<int64_t>(p + i * kJoinWaves) * d + c];
+      s += (v[0] + v[1]) + (v[2] + v[3]);
+    }
+    for (; p < parts; p += kJoinWaves) s += part[static_cast<int64_t>(p) * d + c];
+  }
+  sh[w][threadIdx.x & 63] = s;
+  __syncthreads();
+  if (w == 0 && c < d) {
+    s = 0.f;
+#pragma unroll
+    for (int i = 0; i < kJoinWaves; ++i) s += sh[i][threadIdx.x];
+    dgain[c] = s;
+  }
+}
+
+constexpr int kFwdCh(int v) { return 32 / v; }   // 32 elements a thread, 16 in the backward pass
+constexpr int kBwdCh(int v) { return 16 / v; }
+
+template <int STORE, int OUT, bool NORM>
+void launch_rows(hipStream_t st, const Fwd& a) {
+  constexpr int CH = kFwdCh(vec_of<STORE>());
+  // A wave a row leaves more rows in flight; 256 threads a row end a few long rows sooner.
+  if (a.d <= 512 || (a.d <= 64 * 32 && a.n >= 1024)) {
+    const int64_t g = std::min<int64_t>((a.n + 3) / 4, kMostBlocks);
+    hipLaunchKernelGGL((rows_kernel<STORE, OUT, 64, CH, NORM>), dim3(static_cast<unsigned>(g)), dim3(kBlock), 0, st, a);
+  } else if (a.d <= kBlock * 32) {
+    const int64_t g = std::min<int64_t>(a.n, kMostBlocks);
+    hipLaunchKernelGGL((rows_kernel<STORE, OUT, kBlock, CH, NORM>), dim3(static_cast<unsigned>(g)), dim3(kBlock), 0, st, a);
+  } else {
+    const int64_t g = std::min<int64_t>(a.n, kMostBlocks);
+    hipLaunchKernelGGL((long_rows_kernel<STORE, OUT, NORM>), dim3(static_cast<unsigned>(g)), dim3(kBlock), 0, st, a);
+  }
+}
+
+template <int STORE>
+void launch_norm(hipStream_t st, const Fwd& a, int out) {
+  if (out == GIST_STORE_F32) launch_rows<STORE, GIST_STORE_F32, true>(st, a);
+  else if (out == GIST_STORE_BF16) launch_rows<STORE, GIST_STORE_BF16, true>(st, a);
+  else if (out == GIST_STORE_F16) launch_rows<STORE, GIST_STORE_F16, true>(st, a);
+  else launch_rows<STORE, GIST_STORE_E4M3, true>(st, a);
+}
+
+// Rows a workgroup of the backward pass takes at a time, and workgroups: enough to fill the
+// card twice over, no more than rows (their sums are added by a second launch).
+int rows_a_block(int d) { return d <= 64 * 16 ? kBlock / 64 : 1; }
+int64_t bwd_blocks(int64_t n, int d) {
+  const int64_t rb = rows_a_block(d);
+  return std::min<int64_t>((n + rb - 1) / rb, 1024);
+}
+
+template <int STORE, int DY>
+void launch_bwd(hipStream_t st, const Bwd& a) {
+  constexpr int CH = kBwdCh(vec_of<STORE>());
+  const dim3 grid(static_cast<unsigned>(bwd_blocks(a.n, a.d))), block(kBlock);
+  if (rows_a_block(a.d) > 1) hipLaunchKernelGGL((bwd_kernel<STORE, DY, 64, CH>), grid, block, 0, st, a);
+  else if (a.d <= kBlock * 16) hipLaunchKernelGGL((bwd_kernel<STORE, DY, kBlock, CH>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((long_bwd_kernel<STORE, DY>), grid, block, 0, st, a);
+}
+
+template <int STORE>
+void launch_bwd_of(hipStream_t st, const Bwd& a, int dy_store) {
+  if (dy_store == GIST_STORE_F32) launch_bwd<STORE, GIST_STORE_F32>(st, a);
+  else if (dy_store == GIST_STORE_BF16) launch_bwd<STORE, GIST_STORE_BF16>(st, a);
+  else launch_bwd<STORE, GIST_STORE_F16>(st, a);
+}
+
+double width_of(int store) { return store == GIST_STORE_F32 ? 4.0 : store == GIST_STORE_E4M3 ? 1.0 : 2.0; }
+
+}  // namespace
+
+gist_status rms_norm(hipStream_t st, int64_t n, int d, const void* x, int64_t ldx, const void* r, int64_t ldr,
+                     int store, const float* gain, float eps, void* h, int64_t ldh, void* y, int64_t ldy,
+                     int out_store, float* y_scale, float* rstd) {
+  const Fwd a{n, ldx, ldr, ldh, ldy, d, x, r, gain, h, y, y_scale, rstd, eps};
+  ProfScope ps(st, "rms_norm", 0.0,
+               static_cast<double>(n) * d * (width_of(store) * (1.0 + (r ? 1 : 0) + (h ? 1 : 0)) + width_of(out_store)));
+  if (store == GIST_STORE_F32) launch_norm<GIST_STORE_F32>(st, a, out_store);
+  else if (store == GIST_STORE_BF16) launch_norm<GIST_STORE_BF16>(st, a, out_store);
+  else launch_norm<GIST_STORE_F16>(st, a, out_store);
+  return check_launch("rms_norm");
+}
+
+gist_status quantize_rows(hipStream_t st, int64_t n, int d, const void* x, int64_t ldx, int store, void* y,
+                          int64_t ldy, float* scale) {
+  const Fwd a{n, ldx, 0, 0, ldy, d, x, nullptr, nullptr, nullptr, y, scale, nullptr, 0.f};
+  ProfScope ps(st, "quantize_rows", 0.0, static_cast<double>(n) * d * (width_of(store) + 1.0));
+  if (store == GIST_STORE_F32) launch_rows<GIST_STORE_F32, GIST_STORE_E4M3, false>(st, a);
+  else if (store == GIST_STORE_BF16) launch_rows<GIST_STORE_BF16, GIST_STORE_E4M3, false>(st, a);
+  else launch_rows<GIST_STORE_F16, GIST_STORE_E4M3, false>(st, a);
+  return check_launch("quantize_rows");
+}
+
+size_t rms_norm_bwd_workspace(int64_t n, int d) {
+  return static_cast<size_t>(bwd_blocks(n, d)) * static_cast<size_t>(d) * 4;
+}
+
+gist_status rms_norm_bwd(hipStream_t st, int64_t n, int d, const void* dy, int64_t lddy, int dy_store,
+                         const void* h, int64_t ldh, int store, const float* gain, const float* rstd,
+                         const void* dsum, int64_t ldds, void* dx, int64_t lddx, float* dgain, void* ws) {
+  if (n > 0) {
+    const Bwd a{n, lddy, ldh, ldds, lddx, d, dy, h, gain, rstd, dsum, dx, dgain ? static_cast<float*>(ws) : nullptr};
+    ProfScope ps(st, "rms_norm_bwd", 0.0,
+                 static_cast<double>(n) * d *
+                     (width_of(store) * (1.0 + (dsum && dx ? 1 : 0) + (dx ? 1 : 0)) + width_of(dy_store)));
+    if (store == GIST_STORE_F32) launch_bwd_of<GIST_STORE_F32>(st, a, dy_store);
+    else if (store == GIST_STORE_BF16) launch_bwd_of<GIST_STORE_BF16>(st, a, dy_store);
+    else launch_bwd_of<GIST_STORE_F16>(st, a, dy_store);
+    const gist_status s = check_launch("rms_norm_bwd");
+    if (s != GIST_OK) return s;
+  }
+  if (dgain) {
+    const int parts = n > 0 ? static_cast<int>(bwd_blocks(n, d)) : 0;
+    ProfScope ps(st, "rms_norm_gain", 0.0, 4.0 * static_cast<double>(parts) * d);
+    hipLaunchKernelGGL(gain_kernel, dim3(static_cast<unsigned>((d + 63) / 64)), dim3(64 * kJoinWaves), 0, st, parts, d,
+                       static_cast<const float*>(ws), dgain);
+    return check_launch("rms_norm_gain");
+  }
+  return GIST_OK;
+}
+
+}  // namespace gist

@@ -1,0 +1,1230 @@
+// Softmax cross-entropy of rows against a table of class vectors, without the
+// logits, and its gradients.
+//
+//   z_vj = scale <h_v, t_j>,  lse_v = log sum_j e^z_vj,  G_vj = e^(z_vj - lse_v) - [j = y_v],
+//   dH = f G T,  dT = f G^T H,  f = grad_scale scale / count.
+//
+// 16-bit operands: three tiled products on the matrix cores.
+//   forward   a tile's logits stay in its accumulators; every wave leaves the
+//             maximum and the sum of exponentials over its classes for each of
+//             its rows, and a second kernel joins them.
+//   gradient  piece by piece of the table: the piece's logits again, as G in 16
+//             bits in the workspace; then its share of dH and its rows of dT.
+// G is rounded to the operands' type (relative 2^-9 in bf16, 2^-11 in fp16, where it is
+// held times 2^15 so that probabilities down to 2^-29 keep all bits), as matrix
+// instructions want it; everything else is fp32.
+//
+// All products have the result's rows in the lanes and its columns in the
+// accumulator's registers: a row's maximum and sum over the classes are then
+// sums over registers, and results leave as 16 bytes a lane.  dH and dT
+// contract over the slow index of T and H: those operands lie in LDS as they
+// do in memory and are transposed by the LDS reads.
+//
+// fp32 operands (GIST_DTYPE_F32): rows piece by piece through the library's fp32
+// products, with one kernel between them that turns a piece's logits into G.
+//
+// 8-bit operands: forward only, twice the products per step.
+
+#include <algorithm>
+
+#include "elem.cuh"
+
+#define GIST_LAUNCHED(what)                        \
+  do {                                             \
+    const gist_status s_ = check_launch(what);     \
+    if (s_ != GIST_OK) return s_;                  \
+  } while (0)
+
+namespace gist {
+
+namespace {
+
+constexpr int kBlock = 256;
+constexpr float kL = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr size_t kPieceBytes = size_t{256} << 20;   // G of one piece, or an fp32 piece's logits
+constexpr size_t kPartBytes = size_t{64} << 20;     // fp32 partial results beyond one
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef short short4v __attribute__((ext_vector_type(4)));
+typedef short short8v __attribute__((ext_vector_type(8)));
+typedef int intx4 __attribute__((ext_vector_type(4)));
+typedef int intx8 __attribute__((ext_vector_type(8)));
+typedef float floatx2 __attribute__((ext_vector_type(2)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef int intx4u __attribute__((ext_vector_type(4), aligned(2)));
+typedef float floatx4u __attribute__((ext_vector_type(4), aligned(4)));
+
+__device__ __forceinline__ float ex2(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float lg2(float x) { return __builtin_amdgcn_logf(x); }
+
+// ---- products -------------------------------------------------------------------------
+
+enum { kStats = 0, kGrad = 1, kPart = 2, kOut = 3 };
+
+// out[n][m] over m < M, n < N: sum over K of P[m][k] Q[n][k].  An operand is
+// either rows with K contiguous (ld: bytes from row to row) or, "transposed", K
+// rows with its own index contiguous (ld: bytes from one k to the next).
+// RP, RQ: rows of the operand that can be read (transposed: values of its own
+// index, a multiple of 8); KP, KQ: values of K that can be, of a transposed one.
+// What lies behind them is read as the last again: a step's values of K that only
+// one operand has must be zero there.
+struct Prod {
+  const char* P;
+  const char* Q;
+  int64_t ldp, ldq;
+  int64_t M, N, RP, RQ, KP, KQ;
+  int tiles_m, tiles_n, steps, slices, len;   // steps: of 128 bytes of K; len: of one slice
+  // kStats, kGrad: classes are m (class0 the first), rows are n
+  float scale;
+  const float* ps;            // 8-bit scales of P's and Q's rows
+  const float* qs;
+  const int32_t* labels;
+  const int32_t* n_dev;
+  int64_t class0;
+  floatx2* stats;             // [tiles_m NWM][ldstat]: maximum and sum
+  int64_t ldstat;
+  float* zy;                  // the given class's logit
+  const float* lse;
+  void* out;                  // kGrad: G (16 bits); kPart: fp32 [slice][N][ldo]; kOut: the gradient
+  int64_t ldo;
+  int add;                    // kPart: add to what is there
+  const float* factor;        // kOut
+  int out_store;
+};
+
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  static_assert(N >= 0 && N < 64, "vmcnt");
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
+// 16 bytes per lane from memory straight to LDS: base + off (per lane) to dst + 16 lane.
+// No vector register is written; the caller waits for vmcnt.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void load_to_lds(unsigned dst, unsigned off, const char* base) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+               :
+               : "s"(dst), "v"(off), "s"(base)
+               : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
+template <int STORE>
+struct Frag {          // 16-bit operands: 8 values of K a lane
+  intx4 v;
+};
+template <>
+struct Frag<GIST_STORE_E4M3> {   // 32 values of K a lane
+  intx8 v;
+};
+
+template <int STORE>
+__device__ __forceinline__ floatx16 mma(const Frag<STORE>& a, const Frag<STORE>& b, floatx16 c) {
+  if constexpr (STORE == GIST_STORE_BF16)
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a.v), __builtin_bit_cast(bf16x8, b.v), c, 0, 0, 0);
+  else if constexpr (STORE == GIST_STORE_F16)
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, a.v), __builtin_bit_cast(half8, b.v), c, 0, 0, 0);
+  else   // block scales of 1 (exponent 127)
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a.v, b.v, c, 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);
+}
+
+// One operand's share of a step in LDS, ROWS of its own index by 128 bytes of K.
+//  As rows: 128 bytes a row, its 16-byte piece p at p ^ (row / 2 mod 8), which spreads a
+//   fragment read (one piece of 32 rows) over the banks.
+//  Transposed: 64 k, 2 ROWS bytes each; 32-byte chunk c (16 of its own index) at c ^ f(k),
+//   f(k) = k mod 4 + 4 (k / 8 mod 2): a transposing read takes four k of two
+//   chunks for each half of a fragment, which f sends to different banks.
+template <int ROWS, bool TR>
+struct Tile {
+  static constexpr int kPieces = TR ? ROWS / 8 : 8;   // 16-byte pieces of a line's row
+  // Where lane's 16 bytes of line L (1 KB of the tile, in LDS order) come from; `left`: rows (or,
+  // transposed, values of its own index) that are there; klim: values of K.
+  __device__ __forceinline__ static unsigned offset(int L, int lane, int64_t ld, int64_t left, int klim) {
+    if constexpr (!TR) {
+      const int row = 8 * L + (lane >> 3);
+      const int piece = (lane & 7) ^ (row >> 1 & 7);
+      return static_cast<unsigned>(min(static_cast<int64_t>(row), left - 1)) * static_cast<unsigned>(ld) + piece * 16;
+    } else {
+      const int k = L * (64 / kPieces) + lane / kPieces, s = lane % kPieces;
+      const int f = (k & 3) | ((k >> 3 & 1) << 2);
+      const int piece = ((s >> 1 ^ f) << 1) | (s & 1);
+      const int last = static_cast<int>(min(static_cast<int64_t>(kPieces), left / 8)) - 1;
+      return static_cast<unsigned>(min(k, klim - 1)) * static_cast<unsigned>(ld) + min(piece, last) * 16;
+    }
+  }
+  // A lane's part of a fragment's address: block of 32 rows.
+  __device__ __forceinline__ static int base(int lane, int blk) {
+    const int li = lane & 31, lh = lane >> 5;
+    if constexpr (!TR) {
+      return (blk * 32 + li) * 128;
+    } else {
+      const int i = lane & 15, k = 8 * lh + (i >> 2), f = (i >> 2) | (lh << 2);
+      return k * (2 * ROWS) + (((2 * blk + (lane >> 4 & 1)) ^ f) << 5) + (i & 3) * 8;
+    }
+  }
+  // Fragment of depth q (16 values of K; 64 of 8 bits); sw: (row / 2 mod 8) of the lane's row.
+  template <int STORE>
+  __device__ __forceinline__ static void read(const char* tile, int base, int q, int lane, Frag<STORE>& f) {
+    const int lh = lane >> 5, sw = lane >> 1 & 7;
+    if constexpr (TR) {
+      typedef __attribute__((address_space(3))) short4v* Ptr;
+      const char* p = tile + base + q * (16 * 2 * ROWS);
+      const short4v a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Ptr)(const __attribute__((address_space(3))) char*)p);
+      const short4v b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (Ptr)(const __attribute__((address_space(3))) char*)(p + 4 * 2 * ROWS));
+      f.v = __builtin_bit_cast(intx4, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+    } else if constexpr (STORE == GIST_STORE_E4M3) {
+      // the 64 values of a depth lie in pieces 4 q .. 4 q + 3: any two of them a lane, in both operands
+      const intx4 a = *reinterpret_cast<const intx4*>(tile + base + (((4 * q + 2 * lh) ^ sw) << 4));
+      const intx4 b = *reinterpret_cast<const intx4*>(tile + base + (((4 * q + 2 * lh + 1) ^ sw) << 4));
+      f.v = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    } else {
+      f.v = *reinterpret_cast<const intx4*>(tile + base + (((2 * q + lh) ^ sw) << 4));
+    }
+  }
+};
+
+// Four fp32 values to 16 bits, two to a word.
+template <int STORE>
+__device__ __forceinline__ void pack4(const float (&v)[4], int (&u)[2]) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+    u[h] = static_cast<int>(static_cast<unsigned>(narrow<STORE>(v[2 * h])) |
+                            static_cast<unsigned>(narrow<STORE>(v[2 * h + 1])) << 16);
+}
+
+// Registers 4 r4 .. 4 r4 + 3 of a 32 x 32 block hold, in lane l, columns 8 r4 + 4 (l / 32) + 0..3
+// of row l mod 32.  Two such groups (a: r4 even, b: r4 + 1), packed, become eight
+// consecutive columns: 8 r4 + 8 (l / 32) + 0..7.
+__device__ __forceinline__ intx4 join8(const int (&a)[2], const int (&b)[2]) {
+  intx4 r;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const auto s = __builtin_amdgcn_permlane32_swap(a[h], b[h], false, false);
+    r[h] = s[0];
+    r[2 + h] = s[1];
+  }
+  return r;
+}
+
+__device__ __forceinline__ int rows_real(const Prod& a) {
+  const int64_t n = a.N;
+  if (!a.n_dev) return static_cast<int>(n);
+  const int64_t k = *a.n_dev;
+  return static_cast<int>(k < 0 ? 0 : k < n ? k : n);
+}
+
+// Tiles of 32 WM NWM columns (M) by 32 WN NWN rows (N); NS buffers in LDS, one barrier a step.
+template <int STORE, int WM, int WN, int NWM, int NWN, int NS, bool PT, bool QT, int EPI>
+__global__ __launch_bounds__(64 * NWM * NWN, NS == 2 ? 2 : 1) void product_kernel(Prod a) {
+  constexpr int BM = 32 * WM * NWM, BN = 32 * WN * NWN;
+  constexpr int LINES = (BM + BN) / 8, WAVES = NWM * NWN, LOADS = LINES / WAVES;
+  static_assert(LINES % WAVES == 0, "a wave's loads");
+  constexpr bool E8 = STORE == GIST_STORE_E4M3;
+  constexpr int QN = E8 ? 2 : 4;      // depths of a step
+  constexpr int KSTEP = E8 ? 128 : 64;
+  using TP = Tile<BM, PT>;
+  using TQ = Tile<BN, QT>;
+  __shared__ __attribute__((aligned(1024))) char lds[NS][(BM + BN) * 128];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave / NWN, wn = wave % NWN;
+  const unsigned tiles = static_cast<unsigned>(a.tiles_m) * static_cast<unsigned>(a.tiles_n);   // < 2^31
+  const unsigned id = static_cast<unsigned>(xcd_remap(blockIdx.x, gridDim.x));
+  const int slice = __builtin_amdgcn_readfirstlane(id / tiles);
+  const unsigned t = id - slice * tiles;
+  // bands of 8 tile columns: what an XCD works on together shares operands
+  const unsigned in_bands = 8u * static_cast<unsigned>(a.tiles_n);
+  const int band = static_cast<int>(t / in_bands);
+  const int in_band = static_cast<int>(t - band * in_bands);
+  const int wide = min(8, a.tiles_m - band * 8);
+  const int tm = __builtin_amdgcn_readfirstlane(band * 8 + in_band % wide);
+  const int tn = __builtin_amdgcn_readfirstlane(in_band / wide);
+  const int64_t m0 = static_cast<int64_t>(tm) * BM, n0 = static_cast<int64_t>(tn) * BN;
+  const int k0 = slice * a.len;
+  const int steps = min(a.len, a.steps - k0);
+  const char* const pb = a.P + (PT ? m0 * 2 : m0 * a.ldp);
+  const char* const qb = a.Q + (QT ? n0 * 2 : n0 * a.ldq);
+  const unsigned lds0 = static_cast<unsigned>(reinterpret_cast<uintptr_t>(
+      (__attribute__((address_space(3))) char*)&lds[0][0]));
+  unsigned off[LOADS];
+  auto offset_of = [&](int i, int kp, int kq) {
+    const int L = wave * LOADS + i;
+    return L < BM / 8 ? TP::offset(L, lane, a.ldp, a.RP - m0, kp)
+                      : TQ::offset(L - BM / 8, lane, a.ldq, a.RQ - n0, kq);
+  };
+#pragma unroll
+  for (int i = 0; i < LOADS; ++i) off[i] = offset_of(i, KSTEP, KSTEP);
+  auto load = [&](int buf, int j) {
+    const int64_t k = k0 + j;
+    const char* const p = pb + (PT ? k * KSTEP * a.ldp : k * 128);
+    const char* const q = qb + (QT ? k * KSTEP * a.ldq : k * 128);
+    const int kp = PT ? static_cast<int>(min(static_cast<int64_t>(KSTEP), a.KP - k * KSTEP)) : KSTEP;
+    const int kq = QT ? static_cast<int>(min(static_cast<int64_t>(KSTEP), a.KQ - k * KSTEP)) : KSTEP;
+    const bool tail = kp < KSTEP || kq < KSTEP;
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int L = wave * LOADS + i;
+      const unsigned o = tail ? offset_of(i, kp, kq) : off[i];
+      load_to_lds(lds0 + buf * ((BM + BN) * 128) + L * 1024, o, L < BM / 8 ? p : q);
+    }
+  };
+  floatx16 acc[WM][WN] = {};
+#pragma unroll
+  for (int j = 0; j < NS; ++j) load(j, min(j, steps - 1));   // always NS: the counts below hold
+  int fa[WM], fb[WN];
+#pragma unroll
+  for (int x = 0; x < WM; ++x) fa[x] = TP::base(lane, wm * WM + x);
+#pragma unroll
+  for (int y = 0; y < WN; ++y) fb[y] = BM * 128 + TQ::base(lane, wn * WN + y);
+  constexpr int FB = E8 ? 1 : 2;      // fragments are read a depth ahead; 8-bit ones are too large
+  Frag<STORE> A[FB][WM], B[FB][WN];
+  auto read = [&](int to, int buf, int q) {
+    const char* tile = &lds[0][0] + buf * ((BM + BN) * 128);
+#pragma unroll
+    for (int x = 0; x < WM; ++x) TP::template read<STORE>(tile, fa[x], q, lane, A[to][x]);
+#pragma unroll
+    for (int y = 0; y < WN; ++y) TQ::template read<STORE>(tile, fb[y], q, lane, B[to][y]);
+  };
+  wait_loads<LOADS * (NS - 1)>();
+  lds_barrier();
+  if constexpr (!E8) read(0, 0, 0);
+  int buf = 0, next = 1 % NS;
+  for (int j = 0; j < steps; ++j) {
+#pragma unroll
+    for (int q = 0; q < QN; ++q) {
+      const int f = E8 ? 0 : q & 1;
+      if constexpr (E8) read(0, buf, q);
+      if (q + 1 < QN) {
+        if constexpr (!E8) read(f ^ 1, buf, q + 1);
+      } else {
+        // the last depth of step j: its fragments are read by this wave and, behind the
+        // barrier, by all, so its buffer takes step j + NS; step j + 1 has arrived
+        wait_loads<LOADS * (NS - 2)>();
+        lds_barrier();
+        load(buf, min(j + NS, steps - 1));   // past the end: the last step again, never used
+        if constexpr (!E8) read(f ^ 1, next, 0);
+      }
+#pragma unroll
+      for (int x = 0; x < WM; ++x)
+#pragma unroll
+        for (int y = 0; y < WN; ++y) acc[x][y] = mma<STORE>(A[f][x], B[f][y], acc[x][y]);
+      if constexpr (!E8) {
+        constexpr int READS = (PT ? 2 : 1) * WM + (QT ? 2 : 1) * WN;
+#pragma unroll
+        for (int m = 0; m < WM * WN; ++m) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                                    // an MFMA
+          __builtin_amdgcn_sched_group_barrier(0x100, (READS + WM * WN - 1) / (WM * WN), 0);    // LDS reads
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    buf = next;
+    next = next + 1 == NS ? 0 : next + 1;
+  }
+  wait_loads<0>();   // nothing may still be on its way to LDS when the workgroup ends
+
+  const int li = lane & 31, lh = lane >> 5;
+  const int64_t mw = m0 + wm * (WM * 32);   // the wave's first column
+  if constexpr (EPI == kStats || EPI == kGrad) {
+    const int real = rows_real(a);
+    const bool edge = mw + WM * 32 > a.M;
+    if constexpr (E8) {      // the classes' scales
+#pragma unroll
+      for (int x = 0; x < WM; ++x)
+#pragma unroll
+        for (int r4 = 0; r4 < 4; ++r4) {
+          const int64_t c = mw + x * 32 + 8 * r4 + 4 * lh;
+          float t[4];
+          load_some<GIST_STORE_F32, 4>(a.ps, c, a.M - c, 0.f, t);
+#pragma unroll
+          for (int y = 0; y < WN; ++y)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) acc[x][y][4 * r4 + q] *= t[q];
+        }
+    }
+#pragma unroll
+    for (int y = 0; y < WN; ++y) {
+      const int64_t row = n0 + (wn * WN + y) * 32 + li;
+      const bool there = row < a.N;
+      float zs = a.scale;
+      if (E8 && there) zs *= a.qs[row];
+      const int label = there ? a.labels[row] : -1;
+      // the label's place among the wave's classes
+      const int64_t mine = label >= 0 ? label - (a.class0 + mw) : -1;
+      const bool any_label = __any(mine >= 0 && mine < WM * 32);
+      float z[WM][16];
+#pragma unroll
+      for (int x = 0; x < WM; ++x)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) z[x][r] = acc[x][y][r] * zs;
+      if constexpr (EPI == kStats) {
+        if (edge) {
+#pragma unroll
+          for (int x = 0; x < WM; ++x)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+              if (mw + x * 32 + 8 * (r >> 2) + 4 * lh + (r & 3) >= a.M) z[x][r] = -__builtin_inff();
+        }
+        float m = z[0][0];
+#pragma unroll
+        for (int x = 0; x < WM; ++x)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) m = fmaxf(m, z[x][r]);
+        m = fmaxf(m, __shfl_xor(m, 32, 64));
+        const float ref = m == -__builtin_inff() ? 0.f : m;
+        float s = 0.f;
+#pragma unroll
+        for (int x = 0; x < WM; ++x) {
+          float p[4] = {};
+#pragma unroll
+          for (int r = 0; r < 16; ++r) p[r & 3] += ex2((z[x][r] - ref) * kL);
+          s += (p[0] + p[1]) + (p[2] + p[3]);
+        }
+        s += __shfl_xor(s, 32, 64);
+        if (there && lh == 0) a.stats[(static_cast<int64_t>(tm) * NWM + wm) * a.ldstat + row] = floatx2{m, s};
+        if (any_label) {
+#pragma unroll
+          for (int x = 0; x < WM; ++x)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+              if (mine == x * 32 + 8 * (r >> 2) + 4 * lh + (r & 3)) a.zy[row] = z[x][r];
+        }
+      } else {
+        // G, also of rows and classes that only fill up tiles: zeros
+        constexpr float kHold = STORE == GIST_STORE_F16 ? 32768.f : 1.f;
+        const bool used = there && row < real && label >= 0;
+        const float lse = used ? a.lse[row] : 0.f;
+        unsigned short* const g = static_cast<unsigned short*>(a.out) + row * a.ldo + mw + 8 * lh;
+#pragma unroll
+        for (int x = 0; x < WM; ++x) {
+          int u[4][2];
+#pragma unroll
+          for (int r4 = 0; r4 < 4; ++r4) {
+            float v[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              const int c = x * 32 + 8 * r4 + 4 * lh + q;
+              v[q] = ex2((z[x][4 * r4 + q] - lse) * kL);
+              if (any_label && mine == c) v[q] -= 1.f;
+              v[q] *= kHold;
+              if (!used || (edge && mw + c >= a.M)) v[q] = 0.f;
+            }
+            pack4<E8 ? static_cast<int>(GIST_STORE_BF16) : STORE>(v, u[r4]);
+          }
+          *reinterpret_cast<intx4*>(g + x * 32) = join8(u[0], u[1]);
+          *reinterpret_cast<intx4*>(g + x * 32 + 16) = join8(u[2], u[3]);
+        }
+      }
+    }
+  } else if constexpr (EPI == kPart) {
+#pragma unroll
+    for (int y = 0; y < WN; ++y) {
+      const int64_t row = n0 + (wn * WN + y) * 32 + li;
+      if (row >= a.N) continue;
+      float* const o = static_cast<float*>(a.out) + (slice * a.N + row) * a.ldo + mw + 4 * lh;
+#pragma unroll
+      for (int x = 0; x < WM; ++x)
+#pragma unroll
+        for (int r4 = 0; r4 < 4; ++r4) {
+          const int c = x * 32 + 8 * r4;
+          if (mw + c + 4 * lh >= a.ldo) continue;    // ldo: a multiple of 4
+          floatx4 v{acc[x][y][4 * r4], acc[x][y][4 * r4 + 1], acc[x][y][4 * r4 + 2], acc[x][y][4 * r4 + 3]};
+          floatx4* const p = reinterpret_cast<floatx4*>(o + c);
+          if (a.add) v += *p;
+          *p = v;
+        }
+    }
+  } else {
+    const float f = *a.factor;
+#pragma unroll
+    for (int y = 0; y < WN; ++y) {
+      const int64_t row = n0 + (wn * WN + y) * 32 + li;
+      const bool there = row < a.N;
+#pragma unroll
+      for (int x = 0; x < WM; ++x) {
+        if (a.out_store == GIST_STORE_F32) {
+#pragma unroll
+          for (int r4 = 0; r4 < 4; ++r4) {
+            const int64_t c = mw + x * 32 + 8 * r4 + 4 * lh;
+            float v[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[q] = acc[x][y][4 * r4 + q] * f;
+            if (there && c < a.M) store_some<GIST_STORE_F32, 4>(a.out, row * a.ldo + c, a.M - c, v);
+          }
+        } else {
+          int u[4][2];
+#pragma unroll
+          for (int r4 = 0; r4 < 4; ++r4) {
+            float v[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[q] = acc[x][y][4 * r4 + q] * f;
+            pack4<E8 ? static_cast<int>(GIST_STORE_BF16) : STORE>(v, u[r4]);
+          }
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const intx4 w = join8(u[2 * h], u[2 * h + 1]);
+            const int64_t c = mw + x * 32 + 16 * h + 8 * lh;
+            if (!there || c >= a.M) continue;
+            unsigned short* const o = static_cast<unsigned short*>(a.out) + row * a.ldo + c;
+            if (c + 8 <= a.M) {
+              *reinterpret_cast<intx4u*>(o) = w;
+            } else {
+#pragma unroll
+              for (int q = 0; q < 8; ++q)
+                if (c + q < a.M) o[q] = static_cast<unsigned short>(static_cast<unsigned>(w[q >> 1]) >> (16 * (q & 1)));
+            }
+          }
+        }
+      }
+    }
+  }
+}
+
+// ---- around the products ------------------------------------------------------------------
+
+// Rows of any store as 16-bit rows (or bytes as bytes) of `wide` elements, zeros behind d and behind
+// n; with labels, rows that are not labelled are zero.  Eight elements a thread.
+template <int SRC, int DST>
+__global__ __launch_bounds__(kBlock) void copy_rows_kernel(int64_t n, int64_t n_pad, int d, int wide, const void* __restrict__ x,
+                                                           int64_t ldx, void* __restrict__ y,
+                                                           const int32_t* __restrict__ labels,
+                                                           const int32_t* __restrict__ n_dev) {
+  const int per = wide / 8;
+  const int64_t count = n_pad * per;
+  const int64_t real = n_dev ? max(0, *n_dev) : n;
+  for (int64_t e = blockIdx.x * static_cast<int64_t>(kBlock) + threadIdx.x; e < count;
+       e += static_cast<int64_t>(gridDim.x) * kBlock) {
+    const int64_t row = e / per;
+    const int c = static_cast<int>(e - row * per) * 8;
+    const bool live = row < n && (!labels || (row < real && labels[row] >= 0));
+    if constexpr (DST == GIST_STORE_E4M3) {
+      const unsigned char* p = static_cast<const unsigned char*>(x) + row * ldx + c;
+      unsigned u[2] = {};
+      if (live) {
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+          if (c + q < d) u[q >> 2] |= static_cast<unsigned>(p[q]) << (8 * (q & 3));
+      }
+      unsigned* const o = reinterpret_cast<unsigned*>(static_cast<unsigned char*>(y) + row * wide + c);
+      o[0] = u[0];
+      o[1] = u[1];
+    } else {
+      float v[8];
+#pragma unroll
+      for (int q = 0; q < 8; ++q) v[q] = 0.f;
+      if (live) {
+        if constexpr (SRC == GIST_STORE_F32) {
+#pragma unroll
+          for (int h = 0; h < 8; h += 4) {
+            float t[4];
+            load_some<SRC, 4>(x, row * ldx + c + h, d - c - h, 0.f, t);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[h + q] = t[q];
+          }
+        } else {
+          load_some<SRC, 8>(x, row * ldx + c, d - c, 0.f, v);
+        }
+      }
+      store_as<DST, 8>(y, row * wide + c, v);
+    }
+  }
+}
+
+// Joins the maxima and sums of rows row0 ..  (all arrays begin there): ROWS rows a workgroup,
+// the others of its threads over the parts.  lse, and the given class's log probability (0
+// without one).
+template <int ROWS>
+__global__ __launch_bounds__(1024) void join_stats_kernel(int64_t row0, int64_t n, int64_t C, int parts, const floatx2* __restrict__ stats,
+                                                          int64_t ldstat, const float* __restrict__ zy,
+                                                          const int32_t* __restrict__ labels,
+                                                          const int32_t* __restrict__ n_dev, float* __restrict__ lse,
+                                                          float* __restrict__ lse_out, float* __restrict__ logp,
+                                                          float* __restrict__ logp_out) {
+  constexpr int G = 1024 / ROWS;
+  __shared__ float sm[G][ROWS], ss[G][ROWS];
+  const int r = threadIdx.x % ROWS, g = threadIdx.x / ROWS;
+  const int64_t row = blockIdx.x * static_cast<int64_t>(ROWS) + r;
+  float m = -__builtin_inff(), s = 0.f;
+  auto take = [&](float pm, float ps) {
+    const float w = fmaxf(m, pm), ref = w == -__builtin_inff() ? 0.f : w;
+    s = s * ex2((m - ref) * kL) + ps * ex2((pm - ref) * kL);
+    m = w;
+  };
+  if (row < n) {
+    int p = g;
+    for (; p + 3 * G < parts; p += 4 * G) {
+      floatx2 v[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = stats[static_cast<int64_t>(p + i * G) * ldstat + row];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) take(v[i][0], v[i][1]);
+    }
+    for (; p < parts; p += G) {
+      const floatx2 v = stats[static_cast<int64_t>(p) * ldstat + row];
+      take(v[0], v[1]);
+    }
+  }
+  sm[g][r] = m;
+  ss[g][r] = s;
+  __syncthreads();
+  for (int h = G / 2; h > 0; h >>= 1) {
+    if (g < h) {
+      take(sm[g + h][r], ss[g + h][r]);
+      sm[g][r] = m;
+      ss[g][r] = s;
+    }
+    __syncthreads();
+  }
+  if (g != 0 || row >= n) return;
+  const float ls = lg2(s) * kLn2, l = m + ls;
+  lse[row] = l;
+  if (lse_out) lse_out[row] = l;
+  const int y = !n_dev || row0 + row < *n_dev ? labels[row] : -1;
+  const float lp = y < 0 ? 0.f : y >= C ? __builtin_nanf("") : zy[row] - m - ls;
+  logp[row] = lp;
+  if (logp_out) logp_out[row] = lp;
+}
+
+// Loss and the gradients' factor; one workgroup, every thread a stride of rows, in a fixed order.
+__global__ __launch_bounds__(1024) void loss_kernel(int64_t n, const float* __restrict__ logp,
+                                                    const int32_t* __restrict__ labels, const int32_t* __restrict__ n_dev,
+                                                    float gscale, float* __restrict__ loss, float* __restrict__ factor) {
+  __shared__ double sh[16];
+  __shared__ int sc[16];
+  int64_t real = n_dev ? max(0, *n_dev) : n;
+  real = real < n ? real : n;
+  double s = 0.0;
+  int c = 0;
+  for (int64_t i = threadIdx.x; i < real; i += 1024) {
+    s += logp[i];
+    c += labels[i] >= 0;
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    s += __shfl_xor(s, o, 64);
+    c += __shfl_xor(c, o, 64);
+  }
+  if ((threadIdx.x & 63) == 0) {
+    sh[threadIdx.x >> 6] = s;
+    sc[threadIdx.x >> 6] = c;
+  }
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  s = 0.0;
+  c = 0;
+  for (int w = 0; w < 16; ++w) {
+    s += sh[w];
+    c += sc[w];
+  }
+  *loss = c > 0 ? static_cast<float>(-s / c) : 0.f;
+  if (factor) *factor = c > 0 ? gscale / static_cast<float>(c) : 0.f;
+}
+
+// out = f sum of the slices' partial results, in order; four elements a thread.
+template <int STORE>
+__global__ __launch_bounds__(kBlock) void join_out_kernel(int64_t rows, int d, int64_t ldp, int slices, int64_t slice,
+                                                          const float* __restrict__ part, const float* __restrict__ factor,
+                                                          void* __restrict__ out, int64_t ldo) {
+  const int per = static_cast<int>(ldp / 4);
+  const float f = *factor;
+  for (int64_t e = blockIdx.x * static_cast<int64_t>(kBlock) + threadIdx.x; e < rows * per;
+       e += static_cast<int64_t>(gridDim.x) * kBlock) {
+    const int64_t row = e / per;
+    const int c = static_cast<int>(e - row * per) * 4;
+    floatx4 v = *reinterpret_cast<const floatx4*>(part + row * ldp + c);
+    for (int s = 1; s < slices; ++s) v += *reinterpret_cast<const floatx4*>(part + s * slice + row * ldp + c);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const float x[1] = {v[q] * f};
+      if (c + q < d) store_as<STORE, 1>(out, row * ldo + c + q, x);
+    }
+  }
+}
+
+// fp32 pieces: a row's logits (a product's, not yet scaled) become its G, times the factor.  A
+// workgroup a row; three passes over it, the last two out of the cache.
+__global__ __launch_bounds__(kBlock) void piece_kernel(int64_t row0, int64_t rows, int64_t n, int64_t C, float scale,
+                                                       float* __restrict__ Z, int64_t ldz, const int32_t* __restrict__ labels,
+                                                       const int32_t* __restrict__ n_dev, const float* __restrict__ factor,
+                                                       int grad, float* __restrict__ lse_out, float* __restrict__ logp,
+                                                       float* __restrict__ logp_out) {
+  __shared__ float sm[kBlock / 64], ss[kBlock / 64];
+  const int64_t real = n_dev ? max(0, *n_dev) : n;
+  const float f = grad ? *factor : 0.f;
+  for (int64_t i = blockIdx.x; i < rows; i += gridDim.x) {
+    float* const z = Z + i * ldz;
+    const int64_t row = row0 + i;
+    const int y = row < real ? labels[row] : -1;
+    float m = -__builtin_inff(), s = 0.f;
+    // ldz is a multiple of 4
+    for (int64_t c = threadIdx.x * 4; c < C; c += kBlock * 4) {
+      const floatx4 v = *reinterpret_cast<const floatx4*>(z + c);
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (c + q < C) m = fmaxf(m, v[q] * scale);
+    }
+    m = wave_max(m);
+    if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
+    const float ref = m == -__builtin_inff() ? 0.f : m;
+    for (int64_t c = threadIdx.x * 4; c < C; c += kBlock * 4) {
+      const floatx4 v = *reinterpret_cast<const floatx4*>(z + c);
+      float p = 0.f;
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (c + q < C) p += ex2((v[q] * scale - ref) * kL);
+      s += p;
+    }
+    s = wave_sum(s);
+    if ((threadIdx.x & 63) == 0) ss[threadIdx.x >> 6] = s;
+    __syncthreads();
+    s = (ss[0] + ss[1]) + (ss[2] + ss[3]);
+    const float ls = lg2(s) * kLn2;
+    if (threadIdx.x == 0) {
+      const float lp = y < 0 ? 0.f : y >= C ? __builtin_nanf("") : z[y] * scale - m - ls;
+      logp[row] = lp;
+      if (logp_out) logp_out[row] = lp;
+      if (lse_out) lse_out[row] = m + ls;
+    }
+    __syncthreads();   // z[y] is read
+    if (!grad) continue;
+    const float fs = y < 0 ? 0.f : f;
+    for (int64_t c = threadIdx.x * 4; c < ldz; c += kBlock * 4) {
+      floatx4 v = *reinterpret_cast<const floatx4*>(z + c);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        float p = ex2((v[q] * scale - m - ls) * kL);
+        if (c + q == y) p -= 1.f;
+        v[q] = y < 0 || c + q >= C ? 0.f : p * fs;
+      }
+      *reinterpret_cast<floatx4*>(z + c) = v;
+    }
+  }
+}
+
+// The gradients' factor alone (fp32 pieces need it before their loss is known).
+__global__ __launch_bounds__(1024) void count_kernel(int64_t n, const int32_t* __restrict__ labels,
+                                                     const int32_t* __restrict__ n_dev, float gscale, float* __restrict__ factor) {
+  __shared__ int sc[16];
+  int64_t real = n_dev ? max(0, *n_dev) : n;
+  real = real < n ? real : n;
+  int c = 0;
+  for (int64_t i = threadIdx.x; i < real; i += 1024) c += labels[i] >= 0;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) c += __shfl_xor(c, o, 64);
+  if ((threadIdx.x & 63) == 0) sc[threadIdx.x >> 6] = c;
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  c = 0;
+  for (int w = 0; w < 16; ++w) c += sc[w];
+  *factor = c > 0 ? gscale / static_cast<float>(c) : 0.f;
+}
+
+// Rows of fp32 with those that are not labelled zeroed.
+__global__ __launch_bounds__(kBlock) void mask_rows_kernel(int64_t row0, int64_t rows, int64_t n, int d, const float* __restrict__ x,
+                                                           int64_t ldx, float* __restrict__ y, const int32_t* __restrict__ labels,
+                                                           const int32_t* __restrict__ n_dev) {
+  const int64_t real = n_dev ? max(0, *n_dev) : n;
+  for (int64_t e = blockIdx.x * static_cast<int64_t>(kBlock) + threadIdx.x; e < rows * d;
+       e += static_cast<int64_t>(gridDim.x) * kBlock) {
+    const int64_t i = e / d, c = e - i * d;
+    const bool live = row0 + i < real && labels[row0 + i] >= 0;
+    y[e] = live ? x[(row0 + i) * ldx + c] : 0.f;
+  }
+}
+
+// ---- plans -----------------------------------------------------------------------------------
+
+size_t up256(size_t x) { return (x + 255) & ~size_t{255}; }
+int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
+unsigned grid_of(int64_t count) { return static_cast<unsigned>(std::max<int64_t>(1, std::min<int64_t>((count + kBlock - 1) / kBlock, 16384))); }
+
+int size_of(int store) { return store == GIST_STORE_F32 ? 4 : store == GIST_STORE_E4M3 ? 1 : 2; }
+
+// How a product is cut: tiles of 256 (one workgroup a CU) or 128 (two).
+struct Cut {
+  int tile;        // 256, 128, or 32 rows (a forward product of few rows)
+  int tiles_m, tiles_n, slices, len;
+};
+
+// A gradient's product (M x N, `steps` of K).  A round of workgroups takes as long for one
+// tile as for one on every CU, so K is cut where the tiles do not fill rounds: the
+// number of slices with the least time in units of a whole product's tile, a
+// fortieth of it added for every slice (its partial result is written and read).
+Cut cut_of(int64_t M, int64_t N, int steps) {
+  Cut c{};
+  const int64_t t256 = ((M + 255) / 256) * ((N + 255) / 256);
+  c.tile = t256 * 4 >= 256 && M >= 256 && N >= 256 ? 256 : 128;
+  c.tiles_m = static_cast<int>((M + c.tile - 1) / c.tile);
+  c.tiles_n = static_cast<int>((N + c.tile - 1) / c.tile);
+  const int64_t tiles = static_cast<int64_t>(c.tiles_m) * c.tiles_n;
+  const int64_t at_once = c.tile == 256 ? 256 : 512;
+  const int64_t most_by_room = std::max<int64_t>(1, static_cast<int64_t>(kPartBytes / 4) / std::max<int64_t>(1, M * N));
+  double best = 1e30;
+  c.slices = 1;
+  for (int s = 1; s <= 64 && s <= most_by_room && s * 4 <= std::max(4, steps); ++s) {
+    const double t = static_cast<double>((tiles * s + at_once - 1) / at_once) / s * (1.0 + 0.0) + (s > 1 ? 0.025 * s : 0.0) *
+                     static_cast<double>(tiles) / at_once;
+    if (t < best * 0.999) {
+      best = t;
+      c.slices = s;
+    }
+  }
+  c.len = (steps + c.slices - 1) / c.slices;
+  c.slices = (steps + c.len - 1) / c.len;
+  return c;
+}
+
+// The logits' product: rows of a tile by how many there are.  (8-bit fragments are twice as
+// large: a tile of 256 would not fit the registers.)
+Cut cut_logits(int64_t C, int64_t n, int steps, bool eight) {
+  Cut c{};
+  if (n <= 32) c.tile = 32;
+  else if (!eight && ((C + 255) / 256) * ((n + 255) / 256) >= 192) c.tile = 256;
+  else c.tile = 128;
+  const int bm = c.tile == 128 ? 128 : 256, bn = c.tile;
+  c.tiles_m = static_cast<int>((C + bm - 1) / bm);
+  c.tiles_n = static_cast<int>((n + bn - 1) / bn);
+  c.slices = 1;
+  c.len = steps;
+  return c;
+}
+
+// Where everything lies in the workspace (offsets).
+struct Plan {
+  bool f32;                 // fp32 products
+  int op;                   // store of the products' operands
+  bool copy_h, copy_t;      // operands that the products cannot read where they are
+  int64_t wide;             // elements of a row of both operands; fp32: of a piece's logits
+  int64_t rows;             // forward, and fp32: rows of a piece
+  int64_t n_pad, Cp;        // rows of G; classes of a piece (a multiple of 256)
+  Cut dh, dt;               // the gradients' products, of the first piece
+  bool parts_h;             // dH is summed in fp32 parts
+  size_t h, hm, t, stats, zy, lse, logp, factor, g, part, z, gemm, total;
+  size_t gemm_bytes;
+};
+
+// Rows that the products load as they are: whole 128-byte steps, 16-byte pieces, offsets within a
+// tile of 32 bits.
+bool direct(const void* p, int64_t ld, int d, int store) {
+  const int e = size_of(store);
+  return (static_cast<int64_t>(d) * e) % 128 == 0 && (ld * e) % 16 == 0 && aligned16(p) && ld <= (1 << 22);
+}
+
+constexpr int waves_m(int tile) { return tile == 32 ? 4 : 2; }
+
+// `any`: room for operands at any address.
+Plan plan_of(const gist_table_xent_desc* D, const void* H, const void* T, bool grad, bool any) {
+  Plan p{};
+  const int64_t n = D->n, C = D->C;
+  const int d = D->d;
+  p.f32 = D->store == GIST_STORE_F32 && D->dtype == GIST_DTYPE_F32;
+  size_t o = 0;
+  auto take = [&](size_t bytes) {
+    const size_t at = o;
+    o += up256(bytes);
+    return at;
+  };
+  p.logp = take(static_cast<size_t>(n) * 4);
+  p.factor = take(16);
+  if (p.f32) {
+    p.wide = up(C, 4);
+    int64_t rows = static_cast<int64_t>(kPieceBytes / 4) / p.wide;
+    rows = rows >= 256 ? rows / 256 * 256 : std::max<int64_t>(1, rows);
+    p.rows = std::min(n, rows);
+    p.z = take(static_cast<size_t>(p.rows) * p.wide * 4);
+    if (grad) p.hm = take(static_cast<size_t>(p.rows) * d * 4);
+    for (const int64_t r : {p.rows, n % p.rows}) {
+      if (r == 0) continue;
+      p.gemm_bytes = std::max(p.gemm_bytes, gemm_workspace(r, C, d, D->ldh, D->ldt, GIST_DTYPE_F32));
+      if (!grad) continue;
+      p.gemm_bytes = std::max(p.gemm_bytes, gemm_workspace(r, d, C, p.wide, D->ldt, GIST_DTYPE_F32));
+      p.gemm_bytes = std::max(p.gemm_bytes, gemm_workspace(C, d, r, p.wide, d, GIST_DTYPE_F32));
+    }
+    p.gemm = take(p.gemm_bytes);
+    p.total = o;
+    return p;
+  }
+  p.op = D->store == GIST_STORE_F32 ? static_cast<int>(GIST_STORE_BF16) : D->store;
+  const int e = size_of(p.op);
+  p.wide = up(d, 128 / e);
+  p.copy_h = D->store == GIST_STORE_F32 || !direct(H, D->ldh, d, D->store);
+  p.copy_t = D->store == GIST_STORE_F32 || !direct(T, D->ldt, d, D->store);
+  // at most so many rows at a time that their maxima and sums take a piece's room; every cut has
+  // at most a part for 64 classes and one more tile
+  const int64_t parts = C / 64 + 4;
+  p.rows = std::min(n, std::max<int64_t>(256, static_cast<int64_t>(kPieceBytes / 8) / parts / 256 * 256));
+  p.stats = take(static_cast<size_t>(parts) * p.rows * 8);
+  p.zy = take(static_cast<size_t>(n) * 4);
+  p.lse = take(static_cast<size_t>(n) * 4);
+  if (p.copy_h || any) p.h = take(static_cast<size_t>(n) * p.wide * e);
+  if (p.copy_t || any) p.t = take(static_cast<size_t>(C) * p.wide * e);
+  if (grad) {
+    p.n_pad = up(n, 256);
+    const int64_t fit = static_cast<int64_t>(kPieceBytes / 2) / p.n_pad / 256 * 256;
+    p.Cp = std::min(up(C, 256), std::max<int64_t>(256, fit));
+    const int64_t cn = std::min(C, p.Cp), ldp = up(d, 4);
+    p.hm = take(static_cast<size_t>(up(n, 64)) * p.wide * 2);
+    p.g = take(static_cast<size_t>(p.n_pad) * p.Cp * 2);
+    p.dh = cut_of(d, n, static_cast<int>(up(cn, 64) / 64));
+    p.dt = cut_of(d, cn, static_cast<int>(up(n, 64) / 64));
+    p.parts_h = p.dh.slices > 1 || p.Cp < C;
+    size_t part = p.parts_h ? static_cast<size_t>(p.dh.slices) * n * ldp * 4 : 0;
+    if (p.dt.slices > 1) part += static_cast<size_t>(p.dt.slices) * cn * ldp * 4;
+    p.part = take(part);
+  }
+  p.total = o;
+  return p;
+}
+
+template <int STORE, int EPI, bool PT, bool QT>
+void launch_product(hipStream_t st, int tile, const Prod& a) {
+  const dim3 grid(static_cast<unsigned>(static_cast<int64_t>(a.tiles_m) * a.tiles_n * a.slices));
+  if constexpr (EPI == kStats || EPI == kGrad) {
+    if (tile == 32) {
+      hipLaunchKernelGGL((product_kernel<STORE, 2, 1, 4, 1, 4, PT, QT, EPI>), grid, dim3(256), 0, st, a);
+      return;
+    }
+  }
+  if constexpr (STORE != GIST_STORE_E4M3) {
+    if (tile == 256) {
+      hipLaunchKernelGGL((product_kernel<STORE, 4, 2, 2, 4, 2, PT, QT, EPI>), grid, dim3(512), 0, st, a);
+      return;
+    }
+  }
+  hipLaunchKernelGGL((product_kernel<STORE, 2, 2, 2, 2, 2, PT, QT, EPI>), grid, dim3(256), 0, st, a);
+}
+
+void set_cut(Prod& a, const Cut& c) {
+  a.tiles_m = c.tiles_m;
+  a.tiles_n = c.tiles_n;
+  a.slices = c.slices;
+  a.len = c.len;
+}
+
+template <int STORE>
+void join_out(hipStream_t st, const gist_table_xent_desc* D, int64_t rows, int slices, int64_t slice, const float* part,
+              const float* factor, void* out, int64_t ldo) {
+  const int64_t ldp = up(D->d, 4);
+  const dim3 grid(grid_of(rows * ldp / 4));
+  if (D->store == GIST_STORE_F32)
+    hipLaunchKernelGGL(join_out_kernel<GIST_STORE_F32>, grid, dim3(kBlock), 0, st, rows, D->d, ldp, slices, slice, part, factor, out, ldo);
+  else
+    hipLaunchKernelGGL(join_out_kernel<STORE>, grid, dim3(kBlock), 0, st, rows, D->d, ldp, slices, slice, part, factor, out, ldo);
+}
+
+// Operands of 16 or 8 bits, ready to be loaded: H and T with ldh and ldt bytes from row to row.
+template <int STORE>
+gist_status run16(hipStream_t st, const gist_table_xent_desc* D, const Plan& p, const char* H, int64_t ldh, const char* T,
+                  int64_t ldt, const float* h_scale, const float* t_scale, const int32_t* labels, const int32_t* n_dev,
+                  float* loss, float* logp, float* lse, void* dH, void* dT, char* w) {
+  const int64_t n = D->n, C = D->C;
+  const int d = D->d, e = size_of(STORE);
+  const bool grad = dH != nullptr;
+  auto f32 = [&](size_t at) { return reinterpret_cast<float*>(w + at); };
+  Prod a{};
+  a.P = T;
+  a.ldp = ldt;
+  a.ldq = ldh;
+  a.M = a.RP = C;
+  a.steps = static_cast<int>(p.wide * e / 128);
+  a.scale = D->scale;
+  a.ps = t_scale;
+  a.stats = reinterpret_cast<floatx2*>(w + p.stats);
+  for (int64_t r0 = 0; r0 < n; r0 += p.rows) {
+    const int64_t rn = std::min(p.rows, n - r0);
+    const Cut c = cut_logits(C, rn, a.steps, STORE == GIST_STORE_E4M3);
+    set_cut(a, c);
+    a.Q = H + r0 * ldh;
+    a.N = a.RQ = a.ldstat = rn;
+    a.qs = h_scale ? h_scale + r0 : nullptr;
+    a.labels = labels + r0;
+    a.zy = f32(p.zy) + r0;
+    {
+      ProfScope ps(st, "table_xent_logits", 2.0 * rn * C * d, static_cast<double>(rn + C) * d * e);
+      launch_product<STORE, kStats, false, false>(st, c.tile, a);
+      GIST_LAUNCHED("table_xent_logits");
+    }
+    const int parts = c.tiles_m * waves_m(c.tile);
+    ProfScope ps(st, "table_xent_join", 0.0, 8.0 * parts * rn);
+    const int per = rn <= 256 ? 4 : 32;
+    const dim3 grid(static_cast<unsigned>((rn + per - 1) / per));
+    float* const lse_out = lse ? lse + r0 : nullptr;
+    float* const logp_out = logp ? logp + r0 : nullptr;
+    if (per == 4)
+      hipLaunchKernelGGL(join_stats_kernel<4>, grid, dim3(1024), 0, st, r0, rn, C, parts, a.stats, rn, a.zy, a.labels, n_dev,
+                         f32(p.lse) + r0, lse_out, f32(p.logp) + r0, logp_out);
+    else
+      hipLaunchKernelGGL(join_stats_kernel<32>, grid, dim3(1024), 0, st, r0, rn, C, parts, a.stats, rn, a.zy, a.labels, n_dev,
+                         f32(p.lse) + r0, lse_out, f32(p.logp) + r0, logp_out);
+    GIST_LAUNCHED("table_xent_join");
+  }
+  {
+    constexpr float kUnhold = STORE == GIST_STORE_F16 ? 1.f / 32768.f : 1.f;
+    ProfScope ps(st, "table_xent_loss", 0.0, 8.0 * n);
+    hipLaunchKernelGGL(loss_kernel, dim3(1), dim3(1024), 0, st, n, f32(p.logp), labels, n_dev,
+                       D->grad_scale * D->scale * kUnhold, loss, grad ? f32(p.factor) : nullptr);
+    GIST_LAUNCHED("table_xent_loss");
+  }
+  if (!grad) return GIST_OK;
+  if constexpr (STORE != GIST_STORE_E4M3) {
+    const int64_t ldp = up(d, 4);
+    char* const hm = w + p.hm;
+    char* const g = w + p.g;
+    float* const factor = f32(p.factor);
+    float* const part_h = f32(p.part);
+    float* const part_t = part_h + (p.parts_h ? p.dh.slices * n * ldp : 0);
+    a.Q = H;
+    a.N = a.RQ = n;
+    a.labels = labels;
+    a.n_dev = n_dev;
+    a.lse = f32(p.lse);
+    for (int64_t c0 = 0; c0 < C; c0 += p.Cp) {
+      const int64_t cn = std::min(p.Cp, C - c0);
+      const int64_t moved = 2 * n * cn;
+      const char* const Tp = T + c0 * ldt;
+      const Cut cg = cut_logits(cn, n, a.steps, false);
+      {   // G [n_pad][Cp]: all rows and classes of the tiles
+        Prod b = a;
+        set_cut(b, cg);
+        b.P = Tp;
+        b.M = b.RP = cn;
+        b.class0 = c0;
+        b.out = g;
+        b.ldo = p.Cp;
+        ProfScope ps(st, "table_xent_grad", 2.0 * n * cn * d, static_cast<double>(n + cn) * d * e + moved);
+        launch_product<STORE, kGrad, false, false>(st, cg.tile, b);
+        GIST_LAUNCHED("table_xent_grad");
+      }
+      {   // dH [n][d]: G T over the piece's classes.  G is zero behind the last class.
+        Prod b{};
+        b.P = Tp;
+        b.ldp = ldt;
+        b.Q = g;
+        b.ldq = p.Cp * 2;
+        b.M = d;
+        b.N = b.RQ = n;
+        b.RP = p.wide;
+        b.KP = cn;
+        b.steps = static_cast<int>(up(cn, 64) / 64);
+        set_cut(b, p.dh);
+        b.len = (b.steps + b.slices - 1) / b.slices;
+        b.slices = (b.steps + b.len - 1) / b.len;   // no more than the first piece's
+        ProfScope ps(st, "table_xent_dh", 2.0 * n * cn * d, moved + static_cast<double>(n + cn) * d * e);
+        if (p.parts_h) {
+          b.out = part_h;
+          b.ldo = ldp;
+          b.add = c0 > 0;
+          launch_product<STORE, kPart, true, false>(st, p.dh.tile, b);
+        } else {
+          b.out = dH;
+          b.ldo = D->lddh;
+          b.factor = factor;
+          b.out_store = D->store;
+          launch_product<STORE, kOut, true, false>(st, p.dh.tile, b);
+        }
+        GIST_LAUNCHED("table_xent_dh");
+      }
+      {   // dT [cn][d]: G^T H over the rows.  The copy of H is zero behind the last row.
+        Prod b{};
+        b.P = hm;
+        b.ldp = p.wide * 2;
+        b.Q = g;
+        b.ldq = p.Cp * 2;
+        b.M = d;
+        b.N = cn;
+        b.RP = p.wide;
+        b.RQ = up(cn, cg.tile == 128 ? 128 : 256);   // columns of G that have been written
+        b.KP = up(n, 64);
+        b.KQ = std::min(b.KP, up(n, cg.tile));       // and rows
+        b.steps = static_cast<int>(b.KP / 64);
+        set_cut(b, p.dt);
+        b.tiles_n = static_cast<int>((cn + p.dt.tile - 1) / p.dt.tile);
+        char* const out = static_cast<char*>(dT) + c0 * D->lddt * size_of(D->store);
+        ProfScope ps(st, "table_xent_dt", 2.0 * n * cn * d, moved + static_cast<double>(n + cn) * d * e);
+        if (p.dt.slices > 1) {
+          b.out = part_t;
+          b.ldo = ldp;
+          launch_product<STORE, kPart, true, true>(st, p.dt.tile, b);
+          GIST_LAUNCHED("table_xent_dt");
+          join_out<STORE>(st, D, cn, b.slices, cn * ldp, part_t, factor, out, D->lddt);
+        } else {
+          b.out = out;
+          b.ldo = D->lddt;
+          b.factor = factor;
+          b.out_store = D->store;
+          launch_product<STORE, kOut, true, true>(st, p.dt.tile, b);
+        }
+        GIST_LAUNCHED("table_xent_dt");
+      }
+    }
+    if (p.parts_h) {
+      ProfScope ps(st, "table_xent_dh_join", 0.0, 4.0 * p.dh.slices * n * ldp);
+      join_out<STORE>(st, D, n, p.dh.slices, n * ldp, part_h, factor, dH, D->lddh);
+      GIST_LAUNCHED("table_xent_dh_join");
+    }
+  }
+  return GIST_OK;
+}
+
+template <int SRC, int DST>
+void copy_rows(hipStream_t st, int64_t n, int64_t n_pad, int d, int64_t wide, const void* x, int64_t ldx, void* y,
+               const int32_t* labels, const int32_t* n_dev) {
+  ProfScope ps(st, "table_xent_copy", 0.0, static_cast<double>(n_pad) * wide * (size_of(SRC) + size_of(DST)));
+  hipLaunchKernelGGL((copy_rows_kernel<SRC, DST>), dim3(grid_of(n_pad * wide / 8)), dim3(kBlock), 0, st, n, n_pad, d,
+                     static_cast<int>(wide), x, ldx, y, labels, n_dev);
+}
+
+template <int SRC, int STORE>
+gist_status run_copied(hipStream_t st, const gist_table_xent_desc* D, const Plan& p, const void* H, const float* h_scale,
+                       const void* T, const float* t_scale, const int32_t* labels, const int32_t* n_dev, float* loss,
+                       float* logp, float* lse, void* dH, void* dT, char* w) {
+  const int e = size_of(STORE);
+  const char* h = static_cast<const char*>(H);
+  const char* t = static_cast<const char*>(T);
+  int64_t ldh = D->ldh * e, ldt = D->ldt * e;
+  if (p.copy_h) {
+    copy_rows<SRC, STORE>(st, D->n, D->n, D->d, p.wide, H, D->ldh, w + p.h, nullptr, nullptr);
+    h = w + p.h;
+    ldh = p.wide * e;
+  }
+  if (p.copy_t) {
+    copy_rows<SRC, STORE>(st, D->C, D->C, D->d, p.wide, T, D->ldt, w + p.t, nullptr, nullptr);
+    t = w + p.t;
+    ldt = p.wide * e;
+  }
+  if constexpr (STORE != GIST_STORE_E4M3)
+    if (dH) copy_rows<SRC, STORE>(st, D->n, up(D->n, 64), D->d, p.wide, H, D->ldh, w + p.hm, labels, n_dev);
+  GIST_LAUNCHED("table_xent_copy");
+  return run16<STORE>(st, D, p, h, ldh, t, ldt, h_scale, t_scale, labels, n_dev, loss, logp, lse, dH, dT, w);
+}
+
+gist_status run32(hipStream_t st, const gist_table_xent_desc* D, const Plan& p, const float* H, const float* T,
+                  const int32_t* labels, const int32_t* n_dev, float* loss, float* logp, float* lse, float* dH, float* dT,
+                  char* w) {
+  const int64_t n = D->n, C = D->C;
+  const int d = D->d;
+  const bool grad = dH != nullptr;
+  float* const z = reinterpret_cast<float*>(w + p.z);
+  float* const hm = reinterpret_cast<float*>(w + p.hm);
+  float* const logp_ws = reinterpret_cast<float*>(w + p.logp);
+  float* const factor = reinterpret_cast<float*>(w + p.factor);
+  void* const gws = w + p.gemm;
+  if (grad) {
+    ProfScope ps(st, "table_xent_count", 0.0, 4.0 * n);
+    hipLaunchKernelGGL(count_kernel, dim3(1), dim3(1024), 0, st, n, labels, n_dev, D->grad_scale * D->scale, factor);
+    GIST_LAUNCHED("table_xent_count");
+  }
+  for (int64_t r0 = 0; r0 < n; r0 += p.rows) {
+    const int64_t rn = std::min(p.rows, n - r0);
+    Operand A, B;
+    GemmOut O;
+    A.p0 = H + r0 * D->ldh;
+    A.ld0 = D->ldh;
+    B.p0 = T;
+    B.ld0 = D->ldt;
+    O.c0 = z;
+    O.ldc0 = p.wide;
+    gist_status s = gemm(st, rn, C, d, A, B, O, GIST_DTYPE_F32, gws, p.gemm_bytes);
+    if (s != GIST_OK) return s;
+    {
+      ProfScope ps(st, "table_xent_piece", 0.0, (grad ? 8.0 : 4.0) * rn * C);
+      hipLaunchKernelGGL(piece_kernel, dim3(static_cast<unsigned>(std::min<int64_t>(rn, 1 << 20))), dim3(kBlock), 0, st, r0, rn,
+                         n, C, D->scale, z, p.wide, labels, n_dev, factor, grad ? 1 : 0, lse, logp_ws, logp);
+      GIST_LAUNCHED("table_xent_piece");
+    }
+    if (!grad) continue;
+    {
+      ProfScope ps(st, "table_xent_mask", 0.0, 8.0 * rn * d);
+      hipLaunchKernelGGL(mask_rows_kernel, dim3(grid_of(rn * d)), dim3(kBlock), 0, st, r0, rn, n, d, H, D->ldh, hm, labels, n_dev);
+      GIST_LAUNCHED("table_xent_mask");
+    }
+    // dH = G T: T's rows are values of K
+    Operand G1, T1;
+    GemmOut O1;
+    G1.p0 = z;
+    G1.ld0 = p.wide;
+    T1.p0 = T;
+    T1.ld0 = D->ldt;
+    T1.k_major = false;
+    O1.c0 = dH + r0 * D->lddh;
+    O1.ldc0 = D->lddh;
+    s = gemm(st, rn, d, C, G1, T1, O1, GIST_DTYPE_F32, gws, p.gemm_bytes);
+    if (s != GIST_OK) return s;
+    // dT += G^T H: both operands' rows are values of K
+    Operand G2, H2;
+    GemmOut O2;
+    G2.p0 = z;
+    G2.ld0 = p.wide;
+    G2.k_major = false;
+    H2.p0 = hm;
+    H2.ld0 = d;
+    H2.k_major = false;
+    O2.c0 = dT;
+    O2.ldc0 = D->lddt;
+    O2.sgd = r0 > 0;     // pieces after the first add to it: C <- C - (-1) product
+    O2.lr = -1.f;
+    s = gemm(st, C, d, rn, G2, H2, O2, GIST_DTYPE_F32, gws, p.gemm_bytes);
+    if (s != GIST_OK) return s;
+  }
+  ProfScope ps(st, "table_xent_loss", 0.0, 8.0 * n);
+  hipLaunchKernelGGL(loss_kernel, dim3(1), dim3(1024), 0, st, n, logp_ws, labels, n_dev, 0.f, loss, nullptr);
+  return check_launch("table_xent_loss");
+}
+
+__global__ __launch_bounds__(kBlock) void zero_rows_kernel(int64_t rows, int64_t bytes, char* __restrict__ x, int64_t ld) {
+  for (int64_t e = blockIdx.x * static_cast<int64_t>(kBlock) + threadIdx.x; e < rows * bytes;
+       e += static_cast<int64_t>(gridDim.x) * kBlock)
+    x[e / bytes * ld + e % bytes] = 0;
+}
+
+}  // namespace
+
+size_t table_xent_workspace(const gist_table_xent_desc* D, bool grad) {
+  return D->n == 0 ? 0 : plan_of(D, nullptr, nullptr, grad, true).total;
+}
+
+size_t table_xent_need(const gist_table_xent_desc* D, const void* H, const void* T, bool grad) {
+  return D->n == 0 ? 0 : plan_of(D, H, T, grad, false).total;
+}
+
+gist_status table_xent(hipStream_t st, const gist_table_xent_desc* D, const void* H, const float* h_scale, const void* T,
+                       const float* t_scale, const int32_t* labels, const int32_t* n_dev, float* loss, float* logp,
+                       float* lse, void* dH, void* dT, void* ws) {
+  char* const w = static_cast<char*>(ws);
+  if (D->n == 0) {
+    if (dT) {
+      const int64_t bytes = static_cast<int64_t>(D->d) * size_of(D->store);
+      hipLaunchKernelGGL(zero_rows_kernel, dim3(grid_of(D->C * bytes)), dim3(kBlock), 0, st, D->C, bytes,
+                         static_cast<char*>(dT), D->lddt * size_of(D->store));
+    }
+    return fill_zero(st, loss, 1);
+  }
+  const Plan p = plan_of(D, H, T, dH != nullptr, false);
+  if (p.f32)
+    return run32(st, D, p, static_cast<const float*>(H), static_cast<const float*>(T), labels, n_dev, loss, logp, lse,
+                 static_cast<float*>(dH), static_cast<float*>(dT), w);
+  switch (D->store) {
+    case GIST_STORE_F32:
+      return run_copied<GIST_STORE_F32, GIST_STORE_BF16>(st, D, p, H, nullptr, T, nullptr, labels, n_dev, loss, logp, lse, dH, dT, w);
+    case GIST_STORE_BF16:
+      return run_copied<GIST_STORE_BF16, GIST_STORE_BF16>(st, D, p, H, nullptr, T, nullptr, labels, n_dev, loss, logp, lse, dH, dT, w);
+    case GIST_STORE_F16:
+      return run_copied<GIST_STORE_F16, GIST_STORE_F16>(st, D, p, H, nullptr, T, nullptr, labels, n_dev, loss, logp, lse, dH, dT, w);
+    default:
+      return run_copied<GIST_STORE_E4M3, GIST_STORE_E4M3>(st, D, p, H, h_scale, T, t_scale, labels, n_dev, loss, logp, lse, nullptr, nullptr, w);
+  }
+}
+
+}  // namespace gist

@@ -44,12 +44,13 @@ GIST_NORM_GCN_SYM, GIST_NORM_SAGE_MEAN, GIST_NORM_THEORY = 0, 1, 2
 GIST_LAYER_GCN, GIST_LAYER_SAGE_MEAN = 0, 1
 GIST_ACT_NONE, GIST_ACT_RELU = 0, 1
 GIST_DTYPE_F32, GIST_DTYPE_BF16_IN, GIST_DTYPE_F16_IN = 0, 1, 2
-GIST_STORE_F32, GIST_STORE_BF16, GIST_STORE_F16 = 0, 1, 2
+GIST_STORE_F32, GIST_STORE_BF16, GIST_STORE_F16, GIST_STORE_E4M3 = 0, 1, 2, 3
 GIST_LOG_PROBS_MAX_TOP = 64
 GIST_MUON_NESTEROV, GIST_MUON_FRESH = 1, 2
 GIST_ORDER_AUTO, GIST_ORDER_AGG_FIRST, GIST_ORDER_XFORM_FIRST = 0, 1, 2
 GIST_SUBAGG_CHECK_FINITE = 1
 GIST_ADAM_FRESH = 1
+GIST_ADAMW_BLOCK = 256
 GIST_NOALLOC_LOSS_MAX_ROWS = 4194304
 GIST_LAYER_SHARED_INPUT, GIST_LAYER_GROUP_MAJOR_OUT, GIST_LAYER_CLUSTERED = 1, 2, 4
 GIST_LAYER_DZ_IN, GIST_LAYER_MASK_DH = 8, 16
@@ -68,6 +69,9 @@ EXPORTED = (
     "gist_softmax_xent_noalloc",
     "gist_embed_lookup", "gist_embed_grad_workspace", "gist_embed_grad", "gist_embed_grad_sgd",
     "gist_log_probs_workspace", "gist_log_probs", "gist_log_probs_bwd",
+    "gist_rms_norm", "gist_rms_norm_bwd_workspace", "gist_rms_norm_bwd", "gist_quantize_rows",
+    "gist_table_xent_workspace", "gist_table_xent",
+    "gist_adamw_update", "gist_adamw_coefficients", "gist_adamw_update_dev",
     "gist_muon_workspace_size", "gist_orthogonalize", "gist_muon_update",
     "gist_gather_slice",
     "gist_sgd_update", "gist_adam_update", "gist_adam_coefficients", "gist_adam_update_dev",
@@ -129,6 +133,19 @@ class gist_muon_desc(C.Structure):
     _fields_ = [("rows", C.c_int64), ("cols", C.c_int64), ("groups", C.c_int32),
                 ("dtype", C.c_int32), ("steps", C.c_int32), ("flags", C.c_uint32),
                 ("coef", C.c_float * 3), ("eps", C.c_float)]
+
+
+class gist_table_xent_desc(C.Structure):
+    _fields_ = [("n", C.c_int64), ("C", C.c_int64), ("d", C.c_int32), ("store", C.c_int32),
+                ("dtype", C.c_int32), ("scale", C.c_float), ("grad_scale", C.c_float),
+                ("ldh", C.c_int64), ("ldt", C.c_int64), ("lddh", C.c_int64), ("lddt", C.c_int64)]
+
+
+class gist_adamw_tensor(C.Structure):
+    _fields_ = [("W", C.c_void_p), ("dW", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p),
+                ("m_scale", C.c_void_p), ("v_scale", C.c_void_p), ("copy", C.c_void_p),
+                ("n", C.c_int64), ("weight_decay", C.c_float), ("grad_store", C.c_int32),
+                ("copy_store", C.c_int32)]
 
 
 class gist_slice_set(C.Structure):
@@ -202,6 +219,25 @@ _sigs = {
                                  _P, C.c_int32, _P, _P, _P, C.c_size_t]),
     "gist_log_probs_bwd": (C.c_int, [_P, C.c_int64, C.c_int64, _P, C.c_int64, C.c_int32, _P, _P,
                                      _P, _P, _P, _P, C.c_int64]),
+    "gist_rms_norm": (C.c_int, [_P, C.c_int64, C.c_int32, _P, C.c_int64, _P, C.c_int64, C.c_int32,
+                                _P, C.c_float, _P, C.c_int64, _P, C.c_int64, C.c_int32, _P, _P]),
+    "gist_rms_norm_bwd_workspace": (C.c_size_t, [C.c_int64, C.c_int32]),
+    "gist_rms_norm_bwd": (C.c_int, [_P, C.c_int64, C.c_int32, _P, C.c_int64, C.c_int32, _P,
+                                    C.c_int64, C.c_int32, _P, _P, _P, C.c_int64, _P, C.c_int64, _P,
+                                    _P, C.c_size_t]),
+    "gist_quantize_rows": (C.c_int, [_P, C.c_int64, C.c_int32, _P, C.c_int64, C.c_int32, _P,
+                                     C.c_int64, _P]),
+    "gist_table_xent_workspace": (C.c_int, [C.POINTER(gist_table_xent_desc), C.c_int32,
+                                            C.POINTER(C.c_size_t)]),
+    "gist_table_xent": (C.c_int, [_P, C.POINTER(gist_table_xent_desc)] + [_P] * 12 +
+                        [C.c_size_t]),
+    "gist_adamw_update": (C.c_int, [_P, C.POINTER(gist_adamw_tensor), C.c_int64, C.c_float,
+                                    C.c_float, C.c_float, C.c_float, C.c_int64, C.c_uint32,
+                                    C.c_float, C.c_uint32]),
+    "gist_adamw_coefficients": (C.c_int, [C.c_float, C.c_float, C.c_float, C.c_float, C.c_int64,
+                                          C.c_uint32, C.c_float, C.c_uint32, _P]),
+    "gist_adamw_update_dev": (C.c_int, [_P, C.POINTER(gist_adamw_tensor), C.c_int64, C.c_float,
+                                        C.c_float, C.c_float, _P]),
     "gist_muon_workspace_size": (C.c_int, [C.POINTER(gist_muon_desc), C.POINTER(C.c_size_t)]),
     "gist_orthogonalize": (C.c_int, [_P, C.POINTER(gist_muon_desc), _P, _P, _P, C.c_size_t]),
     "gist_muon_update": (C.c_int, [_P, C.POINTER(gist_muon_desc), _P, _P, _P, C.c_float,
@@ -536,6 +572,92 @@ def gist_log_probs_bwd(ctx, n, C_, logits, ldz, store, tokens, lse, entropy, g_l
     _check(_lib.gist_log_probs_bwd(ctx.handle, int(n), int(C_), _ptr(logits), int(ldz),
                                    int(store), _ptr(tokens), _ptr(lse), _ptr(entropy),
                                    _ptr(g_logp), _ptr(g_entropy), _ptr(dlogits), int(ldd)))
+
+
+def gist_rms_norm(ctx, n, d, x, ldx, residual, ldr, store, gain, eps, h, ldh, y, ldy, out_store,
+                  y_scale, rstd):
+    """h = x + residual, y = h * rstd * gain (e4m3 codes with GIST_STORE_E4M3); residual, h and
+    rstd may be None."""
+    _check(_lib.gist_rms_norm(ctx.handle, int(n), int(d), _ptr(x), int(ldx), _ptr(residual),
+                              int(ldr), int(store), _ptr(gain), float(eps), _ptr(h), int(ldh),
+                              _ptr(y), int(ldy), int(out_store), _ptr(y_scale), _ptr(rstd)))
+
+
+def gist_rms_norm_bwd_workspace(n, d):
+    return int(_lib.gist_rms_norm_bwd_workspace(int(n), int(d)))
+
+
+def gist_rms_norm_bwd(ctx, n, d, dy, lddy, dy_store, h, ldh, store, gain, rstd, dsum, ldds, dx, lddx,
+                      dgain, ws):
+    """Gradients of ``gist_rms_norm``: dx (of x and of the residual, with dsum added) and dgain."""
+    _check(_lib.gist_rms_norm_bwd(ctx.handle, int(n), int(d), _ptr(dy), int(lddy), int(dy_store),
+                                  _ptr(h), int(ldh), int(store), _ptr(gain), _ptr(rstd),
+                                  _ptr(dsum), int(ldds), _ptr(dx), int(lddx), _ptr(dgain), _ptr(ws),
+                                  _nbytes(ws)))
+
+
+def gist_quantize_rows(ctx, n, d, x, ldx, store, y, ldy, scale):
+    """Rows as e4m3 codes with a scale each."""
+    _check(_lib.gist_quantize_rows(ctx.handle, int(n), int(d), _ptr(x), int(ldx), int(store),
+                                   _ptr(y), int(ldy), _ptr(scale)))
+
+
+def table_xent_desc(n, C_, d, store, dtype=GIST_DTYPE_F32, scale=1.0, grad_scale=1.0, ldh=0, ldt=0,
+                    lddh=0, lddt=0):
+    """``dtype``: of the products of fp32 arrays; leading dimensions of 0 mean d."""
+    return gist_table_xent_desc(int(n), int(C_), int(d), int(store), int(dtype), float(scale),
+                                float(grad_scale), int(ldh), int(ldt), int(lddh), int(lddt))
+
+
+def gist_table_xent_workspace(desc, gradients):
+    b = C.c_size_t()
+    _check(_lib.gist_table_xent_workspace(C.byref(desc), int(bool(gradients)), C.byref(b)))
+    return int(b.value)
+
+
+def gist_table_xent(ctx, desc, H, h_scale, T, t_scale, labels, n_valid_dev, loss_dev, logp, lse, dH,
+                    dT, ws):
+    """Loss of rows H against a class table T, log probabilities and log-sum-exp (may be None), and
+    the gradients dH and dT (None, None: the loss alone)."""
+    _check(_lib.gist_table_xent(ctx.handle, C.byref(desc), _ptr(H), _ptr(h_scale), _ptr(T),
+                                _ptr(t_scale), _ptr(labels), _ptr(n_valid_dev), _ptr(loss_dev),
+                                _ptr(logp), _ptr(lse), _ptr(dH), _ptr(dT), _ptr(ws), _nbytes(ws)))
+
+
+def adamw_tensor(W, dW, m, v, n, weight_decay=0.0, grad_store=GIST_STORE_F32, m_scale=None,
+                 v_scale=None, copy=None, copy_store=GIST_STORE_BF16):
+    """One tensor of an AdamW step (the arrays must outlive it)."""
+    return gist_adamw_tensor(_ptr(W), _ptr(dW), _ptr(m), _ptr(v), _ptr(m_scale), _ptr(v_scale),
+                             _ptr(copy), int(n), float(weight_decay), int(grad_store),
+                             int(copy_store))
+
+
+def adamw_tensors(tensors):
+    """The list ``gist_adamw_update`` takes."""
+    return (gist_adamw_tensor * len(tensors))(*tensors)
+
+
+def gist_adamw_update(ctx, tensors, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, flags=0,
+                      grad_scale=1.0, seed=0):
+    """One AdamW step on every tensor of ``tensors`` (:func:`adamw_tensors`)."""
+    _check(_lib.gist_adamw_update(ctx.handle, tensors, len(tensors), float(lr), float(beta1),
+                                  float(beta2), float(eps), int(step), int(flags),
+                                  float(grad_scale), int(seed) & 0xffffffff))
+
+
+def gist_adamw_coefficients(lr, step, beta1=0.9, beta2=0.999, eps=1e-8, flags=0, grad_scale=1.0,
+                            seed=0):
+    """float32[6] for gist_adamw_update_dev; the last one holds the seed's bits."""
+    out = np.empty(6, dtype=np.float32)
+    _check(_lib.gist_adamw_coefficients(float(lr), float(beta1), float(beta2), float(eps),
+                                        int(step), int(flags), float(grad_scale),
+                                        int(seed) & 0xffffffff, _ptr(out)))
+    return out
+
+
+def gist_adamw_update_dev(ctx, tensors, coef_dev, beta1=0.9, beta2=0.999, eps=1e-8):
+    _check(_lib.gist_adamw_update_dev(ctx.handle, tensors, len(tensors), float(beta1), float(beta2),
+                                      float(eps), _ptr(coef_dev)))
 
 
 def muon_desc(rows, cols, groups=1, dtype=GIST_DTYPE_F32, steps=5, flags=0,

@@ -1,0 +1,284 @@
+"""GPU parity of the loss against a class table and its gradients with 64 bits: every store,
+sizes around tiles and steps, one row and many, odd widths and strides, rows without labels that
+hold anything, padded batches, tables in several pieces, non-finite values, replays."""
+
+import numpy as np
+import pytest
+
+import more_ref as R
+from gpu_util import log, to_dev, to_host
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def G():
+    from paper_2102_10424_amd import gist
+    return gist
+
+
+@pytest.fixture(scope="module")
+def ctx(G):
+    return G.Context(0)
+
+
+def inputs(n, C, d, rng, skip=0.1):
+    T = (rng.standard_normal((C, d)) * 3 / np.sqrt(d)).astype(np.float32)
+    y = rng.integers(0, C, n).astype(np.int32)
+    H = (rng.standard_normal((n, d)) + T[y] * rng.random((n, 1))).astype(np.float32)
+    y[rng.random(n) < skip] = -1
+    return H, T, y
+
+
+def run(G, ctx, H, T, y, store, dtype=None, scale=0.7, gscale=3.0, grad=True, pad=0, n_valid=None, shift=0):
+    """H, T: fp32 arrays, rounded to the store here (e4m3: quantised by the library).  Arrays lie in
+    rows of d + pad, `shift` elements into their memory.  Returns results on the host and the
+    values as stored."""
+    import torch
+    n, d = H.shape
+    C = T.shape[0]
+    ld = d + pad
+    t = R.torch_type(store)
+    hs = ts = None
+
+    def place(a):
+        big = torch.full((shift + a.shape[0] * ld + 64,), float("nan")).to(a.dtype)
+        big[shift:shift + a.shape[0] * ld].view(a.shape[0], ld)[:, :d] = a
+        return big.cuda()[shift:]
+
+    if store == "e4m3":
+        hs, ts = torch.empty(n, device="cuda"), torch.empty(C, device="cuda")
+        h8 = torch.zeros(n * ld + 64, dtype=torch.uint8, device="cuda")
+        t8 = torch.zeros(C * ld + 64, dtype=torch.uint8, device="cuda")
+        G.gist_quantize_rows(ctx, n, d, to_dev(H), d, 0, h8, ld, hs)
+        G.gist_quantize_rows(ctx, C, d, to_dev(T), d, 0, t8, ld, ts)
+        val = lambda q, s, k: to_host(q[:k * ld].view(torch.float8_e4m3fn).float().view(k, ld)[:, :d].double() * s.double()[:, None])
+        Hv, Tv, Hd, Td = val(h8, hs, n), val(t8, ts, C), h8, t8
+    else:
+        Hs, Ts = torch.from_numpy(H).to(t), torch.from_numpy(T).to(t)
+        if store == "f32" and dtype == "bf16":
+            Hv, Tv = Hs.bfloat16().double().numpy(), Ts.bfloat16().double().numpy()
+        else:
+            Hv, Tv = Hs.double().numpy(), Ts.double().numpy()
+        Hd, Td = place(Hs), place(Ts)
+    D = G.table_xent_desc(n, C, d, R.store_of(G, store),
+                          G.GIST_DTYPE_BF16_IN if dtype == "bf16" else G.GIST_DTYPE_F32, scale, gscale,
+                          ld, ld, ld, ld)
+    ws = torch.empty(max(16, G.gist_table_xent_workspace(D, grad)), dtype=torch.uint8, device="cuda")
+    ws.fill_(0xff)                                   # NaN wherever it is read unwritten
+    loss = torch.full((2,), 9.0, device="cuda")
+    logp, lse = torch.full((n + 1,), 9.0, device="cuda"), torch.full((n + 1,), 9.0, device="cuda")
+    dH = dT = None
+    if grad:
+        dH = torch.full((n + 1, ld), 9.0, device="cuda").to(t)
+        dT = torch.full((C + 1, ld), 9.0, device="cuda").to(t)
+    nv = None if n_valid is None else torch.tensor([n_valid], dtype=torch.int32, device="cuda")
+    args = (ctx, D, Hd, hs, Td, ts, to_dev(y), nv, loss, logp, lse, dH, dT, ws)
+    G.gist_table_xent(*args)
+    out = dict(loss=float(loss[0]), logp=to_host(logp)[:n], lse=to_host(lse)[:n])
+    assert float(loss[1]) == 9 and float(logp[n]) == 9 and float(lse[n]) == 9
+    if grad:
+        for name, a, k in (("dH", dH, n), ("dT", dT, C)):
+            h = to_host(a.float()).astype(np.float64)
+            assert (h[k:] == 9).all() and (h[:, d:] == 9).all(), name
+            out[name] = h[:k, :d]
+    return out, Hv, Tv, args
+
+
+def check(out, Hv, Tv, y, store, dtype=None, scale=0.7, gscale=3.0, n_valid=None, grad=True):
+    scale, gscale = float(np.float32(scale)), float(np.float32(gscale))
+    r = R.table_xent(Hv, Tv, y, scale, gscale, n_valid)
+    op = "bf16" if store == "f32" and dtype == "bf16" else store
+    b = R.table_xent_bounds(Hv, Tv, y, scale, r, op, store)
+    worst = {}
+    for k in ("lse", "logp", "loss") + (("dH", "dT") if grad else ()):
+        e = np.abs(out[k] - r[k])
+        worst[k] = float(np.max(e / np.maximum(b[k], 1e-300)))
+    log(f"worst of the bounds: {worst}")
+    assert max(worst.values()) <= 1, worst
+
+
+SHAPES = [(1, 1, 1), (1, 2, 8), (3, 5, 7), (2, 300, 64), (31, 257, 64), (32, 256, 128), (33, 255, 63),
+          (64, 64, 64), (65, 129, 200), (100, 1000, 130), (127, 700, 256), (257, 513, 320),
+          (300, 47, 512), (700, 2000, 96), (40, 9000, 72)]
+
+
+@pytest.mark.parametrize("n,C,d", SHAPES)
+@pytest.mark.parametrize("store,dtype", [("f32", "f32"), ("f32", "bf16"), ("bf16", None), ("f16", None)])
+def test_loss_and_gradients(G, ctx, n, C, d, store, dtype):
+    rng = np.random.default_rng(n * 31 + C * 7 + d)
+    H, T, y = inputs(n, C, d, rng)
+    y[0] = C - 1
+    out, Hv, Tv, _ = run(G, ctx, H, T, y, store, dtype)
+    check(out, Hv, Tv, y, store, dtype)
+
+
+@pytest.mark.parametrize("n,C,d", SHAPES + [(5, 40000, 256), (600, 5000, 200)])
+@pytest.mark.parametrize("store", ["bf16", "e4m3"])
+def test_loss_alone(G, ctx, n, C, d, store):
+    rng = np.random.default_rng(n * 31 + C * 7 + d + 1)
+    H, T, y = inputs(n, C, d, rng)
+    out, Hv, Tv, _ = run(G, ctx, H, T, y, store, grad=False)
+    check(out, Hv, Tv, y, store, grad=False)
+
+
+@pytest.mark.parametrize("store,dtype", [("f32", "f32"), ("f32", "bf16"), ("bf16", None), ("f16", None)])
+@pytest.mark.parametrize("pad,shift", [(8, 0), (3, 0), (0, 1), (5, 3), (64, 8)])
+def test_strides_and_alignment(G, ctx, store, dtype, pad, shift):
+    rng = np.random.default_rng(pad * 10 + shift)
+    H, T, y = inputs(70, 300, 128, rng)
+    out, Hv, Tv, _ = run(G, ctx, H, T, y, store, dtype, pad=pad, shift=shift)
+    check(out, Hv, Tv, y, store, dtype)
+
+
+@pytest.mark.parametrize("pad", [0, 1, 16])
+def test_strides_of_8_bit_rows(G, ctx, pad):
+    rng = np.random.default_rng(pad)
+    H, T, y = inputs(70, 300, 256, rng)
+    out, Hv, Tv, _ = run(G, ctx, H, T, y, "e4m3", pad=pad, grad=False)
+    check(out, Hv, Tv, y, "e4m3", grad=False)
+
+
+@pytest.mark.parametrize("store", ["f32", "bf16", "f16"])
+def test_rows_without_labels_hold_anything(G, ctx, store):
+    """NaN and Inf in rows that have no label, or lie behind the valid ones, reach nothing."""
+    rng = np.random.default_rng(5)
+    n, C, d = 150, 400, 128
+    H, T, y = inputs(n, C, d, rng, 0.3)
+    H[y < 0] = np.where(rng.random((n, d)) < 0.5, np.nan, np.inf)[y < 0]
+    H[130:] = np.nan
+    out, Hv, Tv, _ = run(G, ctx, H, T, y, store, n_valid=130)
+    real = (y >= 0) & (np.arange(n) < 130)
+    clean = np.where(real[:, None], Hv, 0.0)
+    r = R.table_xent(clean, Tv, np.where(real, y, -1), float(np.float32(0.7)), 3.0)
+    b = R.table_xent_bounds(clean, Tv, np.where(real, y, -1), float(np.float32(0.7)), r, store, store)
+    assert (out["logp"][~real] == 0).all() and (out["dH"][~real] == 0).all()
+    for k in ("loss", "logp", "dH", "dT"):
+        assert (np.abs(out[k] - r[k]) <= b[k]).all(), k
+    assert (np.abs(out["lse"] - r["lse"]) <= b["lse"])[real].all()
+
+
+@pytest.mark.parametrize("store", ["f32", "bf16"])
+@pytest.mark.parametrize("n_valid", [-3, 0, 1, 64, 99, 100, 1000])
+def test_padded_batch(G, ctx, store, n_valid):
+    rng = np.random.default_rng(n_valid + 10)
+    H, T, y = inputs(100, 300, 64, rng)
+    out, Hv, Tv, _ = run(G, ctx, H, T, y, store, n_valid=n_valid)
+    check(out, Hv, Tv, y, store, n_valid=n_valid)
+
+
+@pytest.mark.parametrize("store", ["f32", "bf16"])
+def test_no_labels_and_no_rows(G, ctx, store):
+    import torch
+    rng = np.random.default_rng(3)
+    H, T, y = inputs(50, 70, 64, rng)
+    y[:] = -1
+    out, Hv, Tv, args = run(G, ctx, H, T, y, store)
+    assert out["loss"] == 0 and (out["logp"] == 0).all() and (out["dH"] == 0).all() and (out["dT"] == 0).all()
+    D = G.table_xent_desc(0, 70, 64, R.store_of(G, store))
+    loss, dT = torch.full((1,), 5.0, device="cuda"), torch.full((70, 64), 5.0, device="cuda").to(R.torch_type(store))
+    G.gist_table_xent(ctx, D, None, None, None, None, None, None, loss, None, None, None, dT, None)
+    assert float(loss[0]) == 0 and (to_host(dT.float()) == 0).all()
+
+
+@pytest.mark.parametrize("store", ["f32", "bf16", "f16"])
+def test_wrong_labels_and_non_finite_values(G, ctx, store):
+    """A label of C or more is reported; a NaN row is NaN alone in logp and dH."""
+    rng = np.random.default_rng(9)
+    n, C, d = 90, 200, 64
+    H, T, y = inputs(n, C, d, rng, 0.0)
+    y[7] = C
+    out, _, _, _ = run(G, ctx, H, T, y, store)
+    assert np.isnan(out["loss"]) and np.isnan(out["logp"][7]) and np.isfinite(np.delete(out["logp"], 7)).all()
+    y[7] = 3
+    H[11, 5] = np.nan
+    out, _, _, _ = run(G, ctx, H, T, y, store)
+    assert np.isnan(out["loss"]) and np.isnan(out["lse"][11]) and np.isnan(out["dH"][11]).all()
+    assert np.isfinite(np.delete(out["logp"], 11)).all() and np.isfinite(np.delete(out["dH"], 11, 0)).all()
+    assert np.isnan(out["dT"]).all()
+
+
+@pytest.mark.parametrize("store", ["f32", "bf16", "f16"])
+def test_large_logits(G, ctx, store):
+    """Logits of several hundred: the largest class takes everything."""
+    rng = np.random.default_rng(2)
+    H, T, y = inputs(80, 500, 64, rng)
+    out, Hv, Tv, _ = run(G, ctx, H * 30, T * 10, y, store)
+    check(out, Hv, Tv, y, store)
+
+
+@pytest.mark.parametrize("store", ["f32", "bf16"])
+def test_several_pieces(G, ctx, store):
+    """More rows and classes than one piece of the workspace holds (n C above 2^27 16-bit or 2^26 fp32
+    values): the gradients against pieces computed with 64-bit sums on a sample of rows and classes."""
+    import torch
+    n, C, d = (3000, 50000, 64) if store == "bf16" else (2000, 40001, 32)
+    rng = np.random.default_rng(1)
+    H, T, y = inputs(n, C, d, rng)
+    out, Hv, Tv, _ = run(G, ctx, H, T, y, store)
+    scale = float(np.float32(0.7))
+    z = scale * (torch.from_numpy(Hv) @ torch.from_numpy(Tv).t())
+    lse = torch.logsumexp(z, 1)
+    real = torch.from_numpy(y >= 0)
+    g = torch.exp(z - lse[:, None]) * real[:, None]
+    g[torch.arange(n)[real], torch.from_numpy(y).long()[real]] -= 1
+    f = 3.0 * scale / int(real.sum())
+    dH, dT = f * (g @ torch.from_numpy(Tv)).numpy(), f * (g.t() @ torch.from_numpy(Hv)).numpy()
+    # a logit's error (as in more_ref) times p, G's rounding and the sums': relative to the magnitudes
+    mag = f * (g.abs() @ torch.from_numpy(np.abs(Tv))).numpy(), f * (g.abs().t() @ torch.from_numpy(np.abs(Hv))).numpy()
+    ez = 4 * R.U32 * (d + 16) * float(scale * (np.abs(Hv) @ np.abs(Tv[:200]).T).max()) + 2e-5
+    for k, want, m, terms in (("dH", dH, mag[0], C), ("dT", dT, mag[1], n)):
+        b = m * (ez + R.HALF[store] + 2 * R.U32 * (terms + 24)) + R.HALF[store] * np.abs(want)
+        assert (np.abs(out[k] - want) <= b).all(), k
+    assert (np.abs(out["lse"] - lse.numpy()) <= ez + R.lse_bound(z.numpy())).all()
+
+
+def test_gradient_against_differences(G, ctx):
+    """Central differences of the fp32 loss: step 2^-4 loses 2^-8 / 6 of third derivatives below
+    one; the loss's own error (2^-22 of about 3, with d = 8) over 2^-3 adds 6e-6."""
+    rng = np.random.default_rng(8)
+    n, C, d = 6, 9, 8
+    H, T, y = inputs(n, C, d, rng, 0.0)
+    out, _, _, _ = run(G, ctx, H, T, y, "f32", gscale=1.0)
+    s = 2.0 ** -4
+    f = lambda a, b: run(G, ctx, a, b, y, "f32", grad=False)[0]["loss"]
+    for name, x in (("dH", H), ("dT", T)):
+        for _ in range(12):
+            i, j = rng.integers(x.shape[0]), rng.integers(d)
+            p, q = x.copy(), x.copy()
+            p[i, j] += s
+            q[i, j] -= s
+            diff = (f(p, T) - f(q, T)) if name == "dH" else (f(H, p) - f(H, q))
+            assert abs(diff / (2 * s) - out[name][i, j]) < 1e-3
+
+
+@pytest.mark.parametrize("store", ["f32", "bf16"])
+def test_same_bits_again_and_replayed(G, ctx, store):
+    """Twice eagerly, and three replays with the program's own work between: the same bits."""
+    import torch
+    rng = np.random.default_rng(12)
+    H, T, y = inputs(200, 700, 128, rng)
+    _, _, _, args = run(G, ctx, H, T, y, store)
+    outs = lambda: [x.clone() for x in (args[8], args[9], args[10], args[11], args[12])]
+    first = outs()
+    side = torch.cuda.Stream()
+    cap = G.Context(0, stream=side.cuda_stream)
+    torch.cuda.synchronize()
+    G.gist_capture_begin(cap)
+    try:
+        G.gist_table_xent(cap, *args[1:])
+    finally:
+        rep = G.gist_capture_end(cap)
+    for k in range(3):
+        for x in (args[8], args[9], args[10], args[11], args[12]):
+            x[..., :1].zero_()
+        args[13].fill_(0xff)
+        if k == 0:
+            G.gist_table_xent(*args)
+        else:
+            G.gist_replay_launch(ctx, rep)
+        torch.cuda.synchronize()
+        got = outs()
+        assert torch.equal(got[0][:1], first[0][:1])
+        for a, b, m in zip(got[1:], first[1:], (200, 200, 200, 700)):
+            assert torch.equal(a[:m], b[:m]), k

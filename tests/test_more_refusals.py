@@ -1,0 +1,245 @@
+"""Arguments that the norm, 8-bit rows, class-table loss and AdamW calls refuse, and their workspace
+sizes.  No GPU needed: every check runs on the host before anything touches the device."""
+
+import ctypes
+
+import numpy as np
+import pytest
+
+import more_ref as R
+
+G = pytest.importorskip("paper_2102_10424_amd.gist",
+                        reason="libgist.so not built (python -m paper_2102_10424_amd.build)")
+
+
+class NoDevice:
+    """A context handle over zeroed memory: device 0, the default stream.  A refused call
+    reads no more of it."""
+
+    def __init__(self):
+        self.mem = ctypes.create_string_buffer(256)
+        self.handle = ctypes.cast(self.mem, ctypes.c_void_p)
+
+
+class Null:
+    handle = None
+
+
+class Ws:
+    def __init__(self, nbytes, addr=4096):
+        self.n, self.a = nbytes, addr
+
+    def numel(self):
+        return self.n
+
+    def element_size(self):
+        return 1
+
+    def data_ptr(self):
+        return self.a
+
+
+ctx = NoDevice()
+arr = lambda: np.zeros(64, dtype=np.float32)     # stand for device memory; never read
+A, B, D, E, F, H = (arr() for _ in range(6))
+I = np.zeros(64, dtype=np.int32)
+INVAL, NOMEM, UNSUP = G.GIST_E_INVAL, G.GIST_E_NOMEM, G.GIST_E_UNSUPPORTED
+NAN, INF = float("nan"), float("inf")
+
+
+def refused(status, fn, *args, **kw):
+    with pytest.raises(G.GistError) as e:
+        fn(*args, **kw)
+    assert e.value.status == status, e.value
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(n=-1), INVAL), (dict(d=0), INVAL), (dict(n=2**31 - 1), UNSUP),
+    (dict(d=(1 << 22) + 1, ldx=1 << 23, ldr=1 << 23, ldh=1 << 23, ldy=1 << 23), UNSUP),
+    (dict(ldx=3), INVAL), (dict(ldr=3), INVAL), (dict(ldh=3), INVAL), (dict(ldy=3), INVAL),
+    (dict(store=3), INVAL), (dict(store=-1), INVAL), (dict(out_store=4), INVAL),
+    (dict(eps=-1.0), INVAL), (dict(eps=NAN), INVAL), (dict(eps=INF), INVAL),
+    (dict(x=None), INVAL), (dict(gain=None), INVAL), (dict(y=None), INVAL),
+    (dict(out_store=3), INVAL), (dict(y_scale=F), INVAL), (dict(h=A, ldh=5), INVAL),
+    (dict(h=B, ldh=5), INVAL), (dict(y=A, out_store=1), INVAL), (dict(y=A, ldy=5), INVAL),
+    (dict(y=B, out_store=3, y_scale=F), INVAL), (dict(y=E), INVAL)])
+def test_rms_norm(change, status):
+    a = dict(n=2, d=4, x=A, ldx=4, residual=B, ldr=4, store=0, gain=D, eps=1e-6, h=E, ldh=4, y=F,
+             ldy=4, out_store=0, y_scale=None, rstd=None)
+    refused(status, G.gist_rms_norm, ctx, **{**a, **change})
+    refused(INVAL, G.gist_rms_norm, Null, **a)
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(n=-1), INVAL), (dict(d=0), INVAL), (dict(n=2**31 - 1), UNSUP), (dict(lddy=3), INVAL),
+    (dict(ldh=3), INVAL), (dict(ldds=3), INVAL), (dict(lddx=3), INVAL), (dict(store=3), INVAL),
+    (dict(dy_store=3), INVAL), (dict(dy=None), INVAL), (dict(h=None), INVAL),
+    (dict(gain=None), INVAL), (dict(rstd=None), INVAL), (dict(dx=A, lddx=5), INVAL),
+    (dict(dx=A, dy_store=1), INVAL), (dict(dx=B, lddx=6), INVAL), (dict(dx=E, lddx=6), INVAL),
+    (dict(ws=None), NOMEM), (dict(ws="small"), NOMEM), (dict(ws="odd"), INVAL)])
+def test_rms_norm_bwd(change, status):
+    need = G.gist_rms_norm_bwd_workspace(2, 4)
+    a = dict(n=2, d=4, dy=A, lddy=4, dy_store=0, h=B, ldh=4, store=0, gain=D, rstd=D, dsum=E, ldds=4,
+             dx=F, lddx=4, dgain=H, ws=Ws(need))
+    a.update(change)
+    if a["ws"] == "small":
+        a["ws"] = Ws(need - 1)
+    if a["ws"] == "odd":
+        a["ws"] = Ws(need, 4100)
+    refused(status, G.gist_rms_norm_bwd, ctx, **a)
+    refused(INVAL, G.gist_rms_norm_bwd, Null, **a)
+
+
+def test_rms_norm_bwd_workspace():
+    for bad in ((-1, 4), (2, 0), (2**31, 4), (2, (1 << 22) + 1)):
+        assert G.gist_rms_norm_bwd_workspace(*bad) == 0
+    for d in (1, 64, 1024, 1025, 5000):
+        need = [G.gist_rms_norm_bwd_workspace(n, d) for n in (1, 3, 4, 5, 1000, 4096, 10**6)]
+        assert need == sorted(need) and need[0] >= 4 * d
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(n=-1), INVAL), (dict(d=0), INVAL), (dict(n=2**31 - 1), UNSUP), (dict(ldx=3), INVAL),
+    (dict(ldy=3), INVAL), (dict(store=3), INVAL), (dict(x=None), INVAL), (dict(y=None), INVAL),
+    (dict(scale=None), INVAL), (dict(y=A), INVAL)])
+def test_quantize_rows(change, status):
+    a = dict(n=2, d=4, x=A, ldx=4, store=0, y=B, ldy=4, scale=D)
+    refused(status, G.gist_quantize_rows, ctx, **{**a, **change})
+    refused(INVAL, G.gist_quantize_rows, Null, **a)
+
+
+DESC = [(dict(n=-1), INVAL), (dict(C_=0), INVAL), (dict(d=0), INVAL), (dict(ldh=3), INVAL),
+        (dict(ldt=3), INVAL), (dict(lddh=3), INVAL), (dict(lddt=-1), INVAL), (dict(store=4), INVAL),
+        (dict(store=-1), INVAL), (dict(store=0, dtype=G.GIST_DTYPE_F16_IN), INVAL),
+        (dict(scale=NAN), INVAL), (dict(grad_scale=INF), INVAL), (dict(n=2**30 + 1), UNSUP),
+        (dict(C_=2**30 + 1), UNSUP), (dict(d=65537), UNSUP)]
+
+
+@pytest.mark.parametrize("change,status", DESC)
+def test_table_xent_desc(change, status):
+    d = G.table_xent_desc(**{**dict(n=2, C_=3, d=4, store=1), **change})
+    refused(status, G.gist_table_xent_workspace, d, False)
+    refused(status, G.gist_table_xent, ctx, d, A, None, B, None, I, None, D, None, None, None, None,
+            Ws(1 << 40))
+
+
+def test_table_xent_calls():
+    d = G.table_xent_desc(2, 3, 4, G.GIST_STORE_BF16)
+    need = G.gist_table_xent_workspace(d, True)
+    ok = dict(H=A, h_scale=None, T=B, t_scale=None, labels=I, n_valid_dev=None, loss_dev=D, logp=None,
+              lse=None, dH=E, dT=F, ws=Ws(need))
+    call = lambda desc=d, c=ctx, **ch: (c, desc) + tuple({**ok, **ch}.values())
+    for ch in (dict(H=None), dict(T=None), dict(labels=None), dict(loss_dev=None), dict(dH=None),
+               dict(dT=None), dict(h_scale=D), dict(t_scale=D), dict(dH=A), dict(dT=B), dict(dH=B),
+               dict(dT=A), dict(dT=E), dict(ws=Ws(need, 4104))):
+        refused(INVAL, G.gist_table_xent, *call(**ch))
+    refused(INVAL, G.gist_table_xent, *call(c=Null))
+    refused(NOMEM, G.gist_table_xent, *call(ws=Ws(64)))
+    refused(NOMEM, G.gist_table_xent, *call(ws=None))
+    e = G.table_xent_desc(2, 3, 4, G.GIST_STORE_E4M3)
+    refused(INVAL, G.gist_table_xent_workspace, e, True)
+    refused(INVAL, G.gist_table_xent, *call(e, h_scale=D, t_scale=D))
+    for ch in (dict(h_scale=D), dict(t_scale=D), dict()):
+        refused(INVAL, G.gist_table_xent, *call(e, dH=None, dT=None, **ch))
+
+
+@pytest.mark.parametrize("store,dtype", [(0, 0), (0, 1), (1, 0), (2, 0), (3, 0)])
+def test_table_xent_workspace_holds_no_logits(store, dtype):
+    """Far below n C values where these are many, whatever the shape."""
+    for n, C, d in ((1, 1, 1), (1, 1 << 20, 64), (8192, 131072, 1024), (1 << 20, 50000, 256), (33, 7, 5000)):
+        D = G.table_xent_desc(n, C, d, store, dtype)
+        for grad in (False, True) if store != 3 else (False,):
+            need = G.gist_table_xent_workspace(D, grad)
+            operands = 8 * (n + 64) * (d + 128) + 4 * (C + 64) * (d + 128)
+            parts = 4 * 4 * max(n, 1) * (d + 4) + 4 * 4 * (1 << 20) * 64
+            assert 0 < need < (2 << 30) + operands + parts
+    assert G.gist_table_xent_workspace(G.table_xent_desc(0, 5, 4, 1), True) == 0
+
+
+TENSOR = dict(W=A, dW=B, m=D, v=E, n=64)
+
+
+def tensors(**change):
+    return G.adamw_tensors([G.adamw_tensor(**TENSOR), G.adamw_tensor(**{**TENSOR, **change})])
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(n=-1), INVAL), (dict(n=2**34), UNSUP), (dict(W=None), INVAL), (dict(dW=None), INVAL),
+    (dict(m=None), INVAL), (dict(v=None), INVAL), (dict(grad_store=3), INVAL),
+    (dict(grad_store=-1), INVAL), (dict(copy=F, copy_store=0), INVAL), (dict(copy=F, copy_store=3), INVAL),
+    (dict(weight_decay=NAN), INVAL), (dict(m_scale=F), INVAL), (dict(v_scale=F), INVAL),
+    (dict(m_scale=F, v_scale=F), INVAL), (dict(dW=A), INVAL), (dict(m=A), INVAL), (dict(v=D), INVAL),
+    (dict(copy=A), INVAL), (dict(m_scale=D, v_scale=F), INVAL)])
+def test_adamw_tensors(change, status):
+    refused(status, G.gist_adamw_update, ctx, tensors(**change), 0.1, 1)
+    refused(status, G.gist_adamw_update_dev, ctx, tensors(**change), F)
+
+
+@pytest.mark.parametrize("change", [
+    dict(lr=NAN), dict(step=0), dict(beta1=1.0), dict(beta1=-0.1), dict(beta2=1.0), dict(eps=-1.0),
+    dict(eps=INF), dict(flags=2), dict(grad_scale=NAN)])
+def test_adamw_arguments(change):
+    a = dict(lr=0.1, step=1)
+    refused(INVAL, G.gist_adamw_update, ctx, tensors(), **{**a, **change})
+    refused(INVAL, G.gist_adamw_coefficients, **{**a, **change})
+    refused(INVAL, G.gist_adamw_update, Null, tensors(), **a)
+    refused(INVAL, G.gist_adamw_update_dev, Null, tensors(), F)
+    refused(INVAL, G.gist_adamw_update_dev, ctx, tensors(), None)
+    for k in ("beta1", "beta2", "eps"):
+        if k in change:
+            refused(INVAL, G.gist_adamw_update_dev, ctx, tensors(), F, **change)
+
+
+def test_adamw_coefficients():
+    c = G.gist_adamw_coefficients(1e-3, 7, 0.9, 0.99, flags=G.GIST_ADAM_FRESH, grad_scale=0.5, seed=0xfedcba98)
+    assert c[0] == np.float32(float(np.float32(1e-3)) / (1 - float(np.float32(0.9)) ** 7))
+    assert c[2] == 1 and c[3] == np.float32(1e-3) and c[4] == 0.5
+    assert c[5:].view(np.uint32)[0] == 0xfedcba98
+    assert np.array_equal(c[:3], G.gist_adam_coefficients(1e-3, 7, 0.9, 0.99, flags=G.GIST_ADAM_FRESH))
+
+
+# ---- the references ---------------------------------------------------------------
+def test_table_xent_reference_against_differences():
+    """The gradient formula against central differences in 64 bits: step 1e-4 loses 1e-8 of third
+    derivatives below 10 and 2^-52 / 1e-4 of the value."""
+    rng = np.random.default_rng(0)
+    H, T = rng.standard_normal((4, 5)), rng.standard_normal((6, 5))
+    y = np.array([2, -1, 0, 5])
+    r = R.table_xent(H, T, y, 0.8, 1.0)
+    f = lambda a, b: R.table_xent(a, b, y, 0.8, 1.0)["loss"]
+    for name, x in (("dH", H), ("dT", T)):
+        for i in range(x.shape[0]):
+            for j in range(5):
+                p, q = x.copy(), x.copy()
+                p[i, j] += 1e-4
+                q[i, j] -= 1e-4
+                d = (f(p, T) - f(q, T)) if name == "dH" else (f(H, p) - f(H, q))
+                assert abs(d / 2e-4 - r[name][i, j]) < 1e-7
+
+
+def test_rms_reference_against_differences():
+    rng = np.random.default_rng(1)
+    h, dy, ds = (rng.standard_normal((3, 6)) for _ in range(3))
+    g = rng.standard_normal(6)
+    dx, _, dg, _ = R.rms_grad(dy, h, g, 1e-3, ds)
+    f = lambda a, b: float((dy * R.rms(a, b, 1e-3)[1]).sum() + (ds * a).sum())
+    for j in range(6):
+        for i in range(3):
+            p, q = h.copy(), h.copy()
+            p[i, j] += 1e-5
+            q[i, j] -= 1e-5
+            assert abs((f(p, g) - f(q, g)) / 2e-5 - dx[i, j]) < 1e-7
+        p, q = g.copy(), g.copy()
+        p[j] += 1e-5
+        q[j] -= 1e-5
+        assert abs((f(h, p) - f(h, q)) / 2e-5 - dg[j]) < 1e-7
+
+
+def test_random_bits_are_uniform():
+    """Mean and deviation of 2^16 draws, within six standard errors, and no link between the two."""
+    a, b = R.random_bits(1 << 16, 3, 12345)
+    for x in (a, b):
+        assert 0 <= x.min() and x.max() < 65536
+        assert abs(x.mean() - 32767.5) < 6 * 65536 / np.sqrt(12 * 65536)
+    assert abs(np.corrcoef(a, b)[0, 1]) < 6 / 256
+    assert abs(np.corrcoef(a[1:], a[:-1])[0, 1]) < 6 / 256
