@@ -8,10 +8,20 @@
 //   forward   a tile's logits stay in its accumulators; every wave leaves the
 //             maximum and the sum of exponentials over its classes for each of
 //             its rows, and a second kernel joins them.
-//   gradient  piece by piece of the table: the piece's logits again, as G in 16
-//             bits in the workspace; then its share of dH and its rows of dT.
-// G is rounded to the operands' type (relative 2^-9 in bf16, 2^-11 in fp16, where it is
-// held times 2^15 so that probabilities down to 2^-29 keep all bits), as matrix
+//   gradient, bf16   rows piece by piece (all of them where a piece's room allows):
+//             the forward product also leaves E_vj = e^(z_vj - r_v) in bf16, r_v the
+//             given class's logit.  bf16 has fp32's range, so an r_v far from the
+//             row's largest logit will do, and G_v = e^(r_v - lse_v) E_v needs a factor
+//             for the row only: dH takes it with the sums, dT with the rows of H.
+//             The given class's entries are left out of E: they are most of a
+//             gradient, and p - 1 is small where p is known to bf16 only.  dH adds
+//             (p - 1) t_y in fp32 at its end, dT the rows (p - 1) h through the
+//             learned rows' sums (embed.hip).  Rows with a logit of more than r_v + 30 get
+//             their E again, from lse_v.  Three products of n C d, no more than there are.
+//   gradient, fp16   (whose range would not do) the table piece by piece: the
+//             piece's logits again, as G; then its share of dH and its rows of dT.
+// E and G are rounded to the operands' type (relative 2^-9 in bf16, 2^-11 in fp16, where
+// G is held times 2^15 so that probabilities down to 2^-29 keep all bits), as matrix
 // instructions want it; everything else is fp32.
 //
 // All products have the result's rows in the lanes and its columns in the
@@ -42,6 +52,8 @@ namespace {
 constexpr int kBlock = 256;
 constexpr float kL = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr size_t kPieceBytes = size_t{256} << 20;   // G of one piece, or an fp32 piece's logits
+constexpr size_t kExpBytes = size_t{1} << 30;       // E of one piece
+constexpr float kFar = 30.f;                        // a row's largest logit above its reference
 constexpr size_t kPartBytes = size_t{64} << 20;     // fp32 partial results beyond one
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -61,7 +73,7 @@ __device__ __forceinline__ float lg2(float x) { return __builtin_amdgcn_logf(x);
 
 // ---- products -------------------------------------------------------------------------
 
-enum { kStats = 0, kGrad = 1, kPart = 2, kOut = 3 };
+enum { kStats = 0, kGrad = 1, kPart = 2, kOut = 3, kExp = 4, kAgain = 5 };
 
 // out[n][m] over m < M, n < N: sum over K of P[m][k] Q[n][k].  An operand is
 // either rows with K contiguous (ld: bytes from row to row) or, "transposed", K
@@ -76,21 +88,27 @@ struct Prod {
   int64_t ldp, ldq;
   int64_t M, N, RP, RQ, KP, KQ;
   int tiles_m, tiles_n, steps, slices, len;   // steps: of 128 bytes of K; len: of one slice
-  // kStats, kGrad: classes are m (class0 the first), rows are n
+  // kStats, kGrad, kExp, kAgain: classes are m (class0 the first), rows are n
   float scale;
   const float* ps;            // 8-bit scales of P's and Q's rows
   const float* qs;
   const int32_t* labels;
   const int32_t* n_dev;
-  int64_t class0;
+  int64_t row0, class0;
   floatx2* stats;             // [tiles_m NWM][ldstat]: maximum and sum
   int64_t ldstat;
   float* zy;                  // the given class's logit
-  const float* lse;
-  void* out;                  // kGrad: G (16 bits); kPart: fp32 [slice][N][ldo]; kOut: the gradient
+  const float* lse;           // kGrad; kExp, kAgain: the rows' references r_v
+  const int* far;             // kAgain: by 256 rows, whether one of them is far from its first reference
+  void* out;                  // kGrad: G, kExp, kAgain: E (16 bits); kPart: fp32 [slice][N][ldo]; kOut: the gradient
   int64_t ldo;
   int add;                    // kPart: add to what is there
   const float* factor;        // kOut
+  const float* row_factor;    // kOut: or NULL; then also pm1 T[ids] is added before the factor
+  const float* pm1;
+  const int32_t* ids;
+  const char* T;
+  int64_t ldt;
   int out_store;
 };
 
@@ -193,6 +211,15 @@ struct Tile {
   }
 };
 
+// Four 16-bit values as fp32.
+template <int STORE>
+__device__ __forceinline__ void load4_16(const char* base, int64_t e, float (&x)[4]) {
+  typedef unsigned short us4 __attribute__((ext_vector_type(4), aligned(2)));
+  const us4 t = *reinterpret_cast<const us4*>(reinterpret_cast<const unsigned short*>(base) + e);
+#pragma unroll
+  for (int q = 0; q < 4; ++q) x[q] = widen<STORE>(t[q]);
+}
+
 // Four fp32 values to 16 bits, two to a word.
 template <int STORE>
 __device__ __forceinline__ void pack4(const float (&v)[4], int (&u)[2]) {
@@ -216,12 +243,8 @@ __device__ __forceinline__ intx4 join8(const int (&a)[2], const int (&b)[2]) {
   return r;
 }
 
-__device__ __forceinline__ int rows_real(const Prod& a) {
-  const int64_t n = a.N;
-  if (!a.n_dev) return static_cast<int>(n);
-  const int64_t k = *a.n_dev;
-  return static_cast<int>(k < 0 ? 0 : k < n ? k : n);
-}
+// Rows of these that a label counts for.
+__device__ __forceinline__ int64_t rows_real(const Prod& a) { return a.n_dev ? *a.n_dev - a.row0 : a.N; }
 
 // Tiles of 32 WM NWM columns (M) by 32 WN NWN rows (N); NS buffers in LDS, one barrier a step.
 template <int STORE, int WM, int WN, int NWM, int NWN, int NS, bool PT, bool QT, int EPI>
@@ -249,6 +272,9 @@ __global__ __launch_bounds__(64 * NWM * NWN, NS == 2 ? 2 : 1) void product_kerne
   const int wide = min(8, a.tiles_m - band * 8);
   const int tm = __builtin_amdgcn_readfirstlane(band * 8 + in_band % wide);
   const int tn = __builtin_amdgcn_readfirstlane(in_band / wide);
+  if constexpr (EPI == kAgain) {
+    if (a.far[static_cast<int64_t>(tn) * BN >> 8] == 0) return;   // the whole workgroup
+  }
   const int64_t m0 = static_cast<int64_t>(tm) * BM, n0 = static_cast<int64_t>(tn) * BN;
   const int k0 = slice * a.len;
   const int steps = min(a.len, a.steps - k0);
@@ -335,8 +361,8 @@ __global__ __launch_bounds__(64 * NWM * NWN, NS == 2 ? 2 : 1) void product_kerne
 
   const int li = lane & 31, lh = lane >> 5;
   const int64_t mw = m0 + wm * (WM * 32);   // the wave's first column
-  if constexpr (EPI == kStats || EPI == kGrad) {
-    const int real = rows_real(a);
+  if constexpr (EPI == kStats || EPI == kGrad || EPI == kExp || EPI == kAgain) {
+    const int64_t real = rows_real(a);
     const bool edge = mw + WM * 32 > a.M;
     if constexpr (E8) {      // the classes' scales
 #pragma unroll
@@ -367,7 +393,29 @@ __global__ __launch_bounds__(64 * NWM * NWN, NS == 2 ? 2 : 1) void product_kerne
       for (int x = 0; x < WM; ++x)
 #pragma unroll
         for (int r = 0; r < 16; ++r) z[x][r] = acc[x][y][r] * zs;
-      if constexpr (EPI == kStats) {
+      if constexpr (EPI == kExp || EPI == kAgain) {
+        // E, also of rows and classes that only fill up tiles, and of rows without a label: zeros
+        const bool used = there && row < real && label >= 0;
+        const float ref = used ? a.lse[row] : 0.f;
+        unsigned short* const g = static_cast<unsigned short*>(a.out) + row * a.ldo + mw + 8 * lh;
+#pragma unroll
+        for (int x = 0; x < WM; ++x) {
+          int u[4][2];
+#pragma unroll
+          for (int r4 = 0; r4 < 4; ++r4) {
+            float v[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              v[q] = ex2((z[x][4 * r4 + q] - ref) * kL);
+              if (!used || (edge && mw + x * 32 + 8 * r4 + 4 * lh + q >= a.M)) v[q] = 0.f;
+            }
+            pack4<GIST_STORE_BF16>(v, u[r4]);
+          }
+          *reinterpret_cast<intx4*>(g + x * 32) = join8(u[0], u[1]);
+          *reinterpret_cast<intx4*>(g + x * 32 + 16) = join8(u[2], u[3]);
+        }
+      }
+      if constexpr (EPI == kStats || EPI == kExp) {
         if (edge) {
 #pragma unroll
           for (int x = 0; x < WM; ++x)
@@ -399,7 +447,7 @@ __global__ __launch_bounds__(64 * NWM * NWN, NS == 2 ? 2 : 1) void product_kerne
             for (int r = 0; r < 16; ++r)
               if (mine == x * 32 + 8 * (r >> 2) + 4 * lh + (r & 3)) a.zy[row] = z[x][r];
         }
-      } else {
+      } else if constexpr (EPI == kGrad) {
         // G, also of rows and classes that only fill up tiles: zeros
         constexpr float kHold = STORE == GIST_STORE_F16 ? 32768.f : 1.f;
         const bool used = there && row < real && label >= 0;
@@ -445,11 +493,32 @@ __global__ __launch_bounds__(64 * NWM * NWN, NS == 2 ? 2 : 1) void product_kerne
         }
     }
   } else {
-    const float f = *a.factor;
+    const float f0 = *a.factor;
 #pragma unroll
     for (int y = 0; y < WN; ++y) {
       const int64_t row = n0 + (wn * WN + y) * 32 + li;
       const bool there = row < a.N;
+      const float rf = a.row_factor && there ? a.row_factor[row] : 1.f;
+      // a row that takes no part has factor 0, whatever its sums are; a row without a class in the
+      // table (a wrong label) has the other term alone
+      const int id = a.row_factor && there ? a.ids[row] : -1;
+      if (id >= 0 || rf == 0.f) {
+        const float g = id >= 0 ? a.pm1[row] : 0.f;
+#pragma unroll
+        for (int x = 0; x < WM; ++x)
+#pragma unroll
+          for (int r4 = 0; r4 < 4; ++r4) {
+            const int64_t c = mw + x * 32 + 8 * r4 + 4 * lh;
+            float t[4] = {};
+            if (id >= 0 && c < a.RP) load4_16<E8 ? static_cast<int>(GIST_STORE_BF16) : STORE>(a.T + id * a.ldt, c, t);   // RP: a multiple of 64
+#pragma unroll
+            for (int q = 0; q < 4; ++q) acc[x][y][4 * r4 + q] = rf == 0.f ? 0.f : fmaf(g, t[q], rf * acc[x][y][4 * r4 + q]);
+          }
+      } else if (a.row_factor) {
+#pragma unroll
+        for (int x = 0; x < WM; ++x) acc[x][y] *= rf;
+      }
+      const float f = f0;
 #pragma unroll
       for (int x = 0; x < WM; ++x) {
         if (a.out_store == GIST_STORE_F32) {
@@ -493,12 +562,14 @@ __global__ __launch_bounds__(64 * NWM * NWN, NS == 2 ? 2 : 1) void product_kerne
 // ---- around the products ------------------------------------------------------------------
 
 // Rows of any store as 16-bit rows (or bytes as bytes) of `wide` elements, zeros behind d and behind
-// n; with labels, rows that are not labelled are zero.  Eight elements a thread.
+// n; with labels, rows that are not labelled are zero; with factors, rows times theirs (0: zero,
+// whatever they hold).  Eight elements a thread.
 template <int SRC, int DST>
 __global__ __launch_bounds__(kBlock) void copy_rows_kernel(int64_t n, int64_t n_pad, int d, int wide, const void* __restrict__ x,
                                                            int64_t ldx, void* __restrict__ y,
                                                            const int32_t* __restrict__ labels,
-                                                           const int32_t* __restrict__ n_dev) {
+                                                           const int32_t* __restrict__ n_dev,
+                                                           const float* __restrict__ factor) {
   const int per = wide / 8;
   const int64_t count = n_pad * per;
   const int64_t real = n_dev ? max(0, *n_dev) : n;
@@ -506,7 +577,8 @@ __global__ __launch_bounds__(kBlock) void copy_rows_kernel(int64_t n, int64_t n_
        e += static_cast<int64_t>(gridDim.x) * kBlock) {
     const int64_t row = e / per;
     const int c = static_cast<int>(e - row * per) * 8;
-    const bool live = row < n && (!labels || (row < real && labels[row] >= 0));
+    const float f = factor && row < n ? factor[row] : 1.f;
+    const bool live = row < n && (!labels || (row < real && labels[row] >= 0)) && f != 0.f;
     if constexpr (DST == GIST_STORE_E4M3) {
       const unsigned char* p = static_cast<const unsigned char*>(x) + row * ldx + c;
       unsigned u[2] = {};
@@ -535,6 +607,10 @@ __global__ __launch_bounds__(kBlock) void copy_rows_kernel(int64_t n, int64_t n_
           load_some<SRC, 8>(x, row * ldx + c, d - c, 0.f, v);
         }
       }
+      if (factor) {
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v[q] *= f;
+      }
       store_as<DST, 8>(y, row * wide + c, v);
     }
   }
@@ -549,7 +625,8 @@ __global__ __launch_bounds__(1024) void join_stats_kernel(int64_t row0, int64_t 
                                                           const int32_t* __restrict__ labels,
                                                           const int32_t* __restrict__ n_dev, float* __restrict__ lse,
                                                           float* __restrict__ lse_out, float* __restrict__ logp,
-                                                          float* __restrict__ logp_out) {
+                                                          float* __restrict__ logp_out, float* __restrict__ ref,
+                                                          float* __restrict__ row_factor, int* __restrict__ far) {
   constexpr int G = 1024 / ROWS;
   __shared__ float sm[G][ROWS], ss[G][ROWS];
   const int r = threadIdx.x % ROWS, g = threadIdx.x / ROWS;
@@ -593,6 +670,75 @@ __global__ __launch_bounds__(1024) void join_stats_kernel(int64_t row0, int64_t 
   const float lp = y < 0 ? 0.f : y >= C ? __builtin_nanf("") : zy[row] - m - ls;
   logp[row] = lp;
   if (logp_out) logp_out[row] = lp;
+  if (!ref) return;
+  // What E needs: the row's factor e^(r - lse) (0: no part in the gradients), and whether its reference was too
+  // far off; then E comes again, from lse, and its given class after it.
+  float f = 0.f;
+  if (y >= 0) {
+    if (m - ref[row] > kFar) {
+      far[row >> 8] = 1;
+      ref[row] = l;
+    }
+    f = ex2((ref[row] - l) * kL);
+  }
+  row_factor[row] = f;
+}
+
+// The given classes: out of E; p - 1 and the class of every row that takes part (0 and -1 of others).
+__global__ __launch_bounds__(kBlock) void given_kernel(int64_t row0, int64_t n, int64_t C, const float* __restrict__ logp,
+                                                       const int32_t* __restrict__ labels, const int32_t* __restrict__ n_dev,
+                                                       unsigned short* __restrict__ E, int64_t ldE, float* __restrict__ pm1,
+                                                       int32_t* __restrict__ ids) {
+  const int64_t row = blockIdx.x * static_cast<int64_t>(kBlock) + threadIdx.x;
+  if (row >= n) return;
+  const int y = !n_dev || row0 + row < *n_dev ? labels[row] : -1;
+  const bool live = y >= 0 && y < C;
+  if (live) E[row * ldE + y] = 0;
+  pm1[row] = live ? expm1f(logp[row]) : 0.f;
+  ids[row] = live ? y : -1;
+}
+
+// Y = rows of H times p - 1, in fp32; eight elements a thread.
+__global__ __launch_bounds__(kBlock) void given_rows_kernel(int64_t n, int64_t wide, const char* __restrict__ H, int64_t ldh,
+                                                            const float* __restrict__ pm1, float* __restrict__ Y) {
+  const int64_t per = wide / 8;
+  for (int64_t e = blockIdx.x * static_cast<int64_t>(kBlock) + threadIdx.x; e < n * per;
+       e += static_cast<int64_t>(gridDim.x) * kBlock) {
+    const int64_t row = e / per, c = (e - row * per) * 8;
+    const float f = pm1[row];
+    float h[8];
+    load_vec<GIST_STORE_BF16, 8>(H + row * ldh, c, h);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) h[q] *= f;
+    store_vec<8>(Y + row * wide + c, h);
+  }
+}
+
+// The rows' first references: scale <h, t_y>; a wave a row, 16 bytes a lane.  Also clears the marks of far rows.
+__global__ __launch_bounds__(kBlock) void ref_kernel(int64_t row0, int64_t n, int64_t C, int wide, float scale,
+                                                     const char* __restrict__ H, int64_t ldh, const char* __restrict__ T,
+                                                     int64_t ldt, const int32_t* __restrict__ labels,
+                                                     const int32_t* __restrict__ n_dev, float* __restrict__ ref,
+                                                     int* __restrict__ far) {
+  const int64_t row = blockIdx.x * static_cast<int64_t>(kBlock / 64) + (threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
+  if (blockIdx.x * static_cast<int64_t>(kBlock / 64) % 256 == 0 && threadIdx.x == 0)
+    far[blockIdx.x * static_cast<int64_t>(kBlock / 64) / 256] = 0;
+  if (row >= n) return;
+  const int y = !n_dev || row0 + row < *n_dev ? labels[row] : -1;
+  float s = 0.f;
+  if (y >= 0 && y < C) {
+    for (int c = lane * 8; c < wide; c += 512) {
+      float h[8], t[8];
+      load_vec<GIST_STORE_BF16, 8>(H + row * ldh, c, h);
+      load_vec<GIST_STORE_BF16, 8>(T + y * ldt, c, t);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) s = fmaf(h[q], t[q], s);
+    }
+  }
+  s = wave_sum(s) * scale;
+  // a reference that is no number would spoil rows whose own logits are; their results are NaN by themselves
+  if (lane == 0) ref[row] = fabsf(s) < 1e30f ? s : 0.f;
 }
 
 // Loss and the gradients' factor; one workgroup, every thread a stride of rows, in a fixed order.
@@ -630,11 +776,19 @@ __global__ __launch_bounds__(1024) void loss_kernel(int64_t n, const float* __re
   if (factor) *factor = c > 0 ? gscale / static_cast<float>(c) : 0.f;
 }
 
-// out = f sum of the slices' partial results, in order; four elements a thread.
-template <int STORE>
+// out = f sum of the slices' partial results, in order; four elements a thread.  With factors of
+// the rows: f (factor sum + pm1 T[ids]), 0 where the factor is.
+struct Given {
+  const float* row_factor;
+  const float* pm1;
+  const int32_t* ids;
+  const char* T;
+  int64_t ldt;
+};
+template <int STORE, int OPS>
 __global__ __launch_bounds__(kBlock) void join_out_kernel(int64_t rows, int d, int64_t ldp, int slices, int64_t slice,
                                                           const float* __restrict__ part, const float* __restrict__ factor,
-                                                          void* __restrict__ out, int64_t ldo) {
+                                                          Given g, void* __restrict__ out, int64_t ldo) {
   const int per = static_cast<int>(ldp / 4);
   const float f = *factor;
   for (int64_t e = blockIdx.x * static_cast<int64_t>(kBlock) + threadIdx.x; e < rows * per;
@@ -643,10 +797,29 @@ __global__ __launch_bounds__(kBlock) void join_out_kernel(int64_t rows, int d, i
     const int c = static_cast<int>(e - row * per) * 4;
     floatx4 v = *reinterpret_cast<const floatx4*>(part + row * ldp + c);
     for (int s = 1; s < slices; ++s) v += *reinterpret_cast<const floatx4*>(part + s * slice + row * ldp + c);
+    if (g.row_factor) {
+      const float rf = g.row_factor[row];
+      const int id = g.ids[row];
+      float t[4] = {};
+      if (id >= 0) load4_16<OPS>(g.T + id * g.ldt, c, t);   // a row of T has a multiple of 64
+      const float p = id >= 0 ? g.pm1[row] : 0.f;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const float x[1] = {v[q] * f};
-      if (c + q < d) store_as<STORE, 1>(out, row * ldo + c + q, x);
+      for (int q = 0; q < 4; ++q) v[q] = rf == 0.f ? 0.f : fmaf(p, t[q], rf * v[q]);
+    }
+    if (c + 4 <= d && STORE != GIST_STORE_F32) {
+      float x[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) x[q] = v[q] * f;
+      int u[2];
+      pack4<STORE == GIST_STORE_F32 ? static_cast<int>(GIST_STORE_BF16) : STORE>(x, u);
+      typedef int intx2u __attribute__((ext_vector_type(2), aligned(2)));
+      *reinterpret_cast<intx2u*>(static_cast<unsigned short*>(out) + row * ldo + c) = intx2u{u[0], u[1]};
+    } else {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const float x[1] = {v[q] * f};
+        if (c + q < d) store_as<STORE, 1>(out, row * ldo + c + q, x);
+      }
     }
   }
 }
@@ -808,10 +981,12 @@ struct Plan {
   bool copy_h, copy_t;      // operands that the products cannot read where they are
   int64_t wide;             // elements of a row of both operands; fp32: of a piece's logits
   int64_t rows;             // forward, and fp32: rows of a piece
-  int64_t n_pad, Cp;        // rows of G; classes of a piece (a multiple of 256)
+  int64_t n_pad, Cp;        // rows of G or E; classes of a piece (a multiple of 256)
   Cut dh, dt;               // the gradients' products, of the first piece
+  bool exps;                // rows piece by piece, by their exponentials
   bool parts_h;             // dH is summed in fp32 parts
-  size_t h, hm, t, stats, zy, lse, logp, factor, g, part, z, gemm, total;
+  size_t h, hm, t, stats, zy, lse, logp, factor, g, ref, row_factor, far, pm1, ids, y, embed, part,
+      z, gemm, total;
   size_t gemm_bytes;
 };
 
@@ -865,12 +1040,32 @@ Plan plan_of(const gist_table_xent_desc* D, const void* H, const void* T, bool g
   // at most a part for 64 classes and one more tile
   const int64_t parts = C / 64 + 4;
   p.rows = std::min(n, std::max<int64_t>(256, static_cast<int64_t>(kPieceBytes / 8) / parts / 256 * 256));
+  p.exps = grad && p.op == GIST_STORE_BF16;
+  if (p.exps) p.rows = std::min(p.rows, std::max<int64_t>(256, static_cast<int64_t>(kExpBytes / 2) / up(C, 256) / 256 * 256));
   p.stats = take(static_cast<size_t>(parts) * p.rows * 8);
   p.zy = take(static_cast<size_t>(n) * 4);
   p.lse = take(static_cast<size_t>(n) * 4);
   if (p.copy_h || any) p.h = take(static_cast<size_t>(n) * p.wide * e);
   if (p.copy_t || any) p.t = take(static_cast<size_t>(C) * p.wide * e);
-  if (grad) {
+  if (p.exps) {
+    const int64_t ldp = up(d, 4), rn = p.rows;
+    p.n_pad = up(rn, 256);
+    p.Cp = up(C, 256);
+    p.hm = take(static_cast<size_t>(up(rn, 64)) * p.wide * 2);
+    p.g = take(static_cast<size_t>(p.n_pad) * p.Cp * 2);
+    p.ref = take(static_cast<size_t>(rn) * 4);
+    p.row_factor = take(static_cast<size_t>(rn) * 4);
+    p.far = take(static_cast<size_t>(p.n_pad / 256) * 4);
+    p.dh = cut_of(d, rn, static_cast<int>(up(C, 64) / 64));
+    p.dt = cut_of(d, C, static_cast<int>(up(rn, 64) / 64));
+    p.parts_h = p.dh.slices > 1;
+    p.part = take((p.parts_h ? static_cast<size_t>(p.dh.slices) * rn * ldp * 4 : 0) +
+                  static_cast<size_t>(p.dt.slices) * C * ldp * 4);
+    p.pm1 = take(static_cast<size_t>(rn) * 4);
+    p.ids = take(static_cast<size_t>(rn) * 4);
+    p.y = take(static_cast<size_t>(rn) * p.wide * 4);
+    p.embed = take(embed_grad_workspace(rn, C, d));
+  } else if (grad) {
     p.n_pad = up(n, 256);
     const int64_t fit = static_cast<int64_t>(kPieceBytes / 2) / p.n_pad / 256 * 256;
     p.Cp = std::min(up(C, 256), std::max<int64_t>(256, fit));
@@ -891,7 +1086,7 @@ Plan plan_of(const gist_table_xent_desc* D, const void* H, const void* T, bool g
 template <int STORE, int EPI, bool PT, bool QT>
 void launch_product(hipStream_t st, int tile, const Prod& a) {
   const dim3 grid(static_cast<unsigned>(static_cast<int64_t>(a.tiles_m) * a.tiles_n * a.slices));
-  if constexpr (EPI == kStats || EPI == kGrad) {
+  if constexpr (EPI != kPart && EPI != kOut) {
     if (tile == 32) {
       hipLaunchKernelGGL((product_kernel<STORE, 2, 1, 4, 1, 4, PT, QT, EPI>), grid, dim3(256), 0, st, a);
       return;
@@ -915,13 +1110,29 @@ void set_cut(Prod& a, const Cut& c) {
 
 template <int STORE>
 void join_out(hipStream_t st, const gist_table_xent_desc* D, int64_t rows, int slices, int64_t slice, const float* part,
-              const float* factor, void* out, int64_t ldo) {
+              const float* factor, const Given& g, void* out, int64_t ldo) {
   const int64_t ldp = up(D->d, 4);
   const dim3 grid(grid_of(rows * ldp / 4));
   if (D->store == GIST_STORE_F32)
-    hipLaunchKernelGGL(join_out_kernel<GIST_STORE_F32>, grid, dim3(kBlock), 0, st, rows, D->d, ldp, slices, slice, part, factor, out, ldo);
+    hipLaunchKernelGGL((join_out_kernel<GIST_STORE_F32, STORE>), grid, dim3(kBlock), 0, st, rows, D->d, ldp, slices, slice, part,
+                       factor, g, out, ldo);
   else
-    hipLaunchKernelGGL(join_out_kernel<STORE>, grid, dim3(kBlock), 0, st, rows, D->d, ldp, slices, slice, part, factor, out, ldo);
+    hipLaunchKernelGGL((join_out_kernel<STORE, STORE>), grid, dim3(kBlock), 0, st, rows, D->d, ldp, slices, slice, part, factor,
+                       g, out, ldo);
+}
+
+template <int SRC, int DST>
+void copy_rows(hipStream_t st, int64_t n, int64_t n_pad, int d, int64_t wide, const void* x, int64_t ldx, void* y,
+               const int32_t* labels, const int32_t* n_dev, const float* factor = nullptr) {
+  ProfScope ps(st, "table_xent_copy", 0.0, static_cast<double>(n_pad) * wide * (size_of(SRC) + size_of(DST)));
+  hipLaunchKernelGGL((copy_rows_kernel<SRC, DST>), dim3(grid_of(n_pad * wide / 8)), dim3(kBlock), 0, st, n, n_pad, d,
+                     static_cast<int>(wide), x, ldx, y, labels, n_dev, factor);
+}
+
+// The same cut for fewer rows (N).
+Cut cut_rows(Cut c, int64_t N) {
+  c.tiles_n = static_cast<int>((N + c.tile - 1) / c.tile);
+  return c;
 }
 
 // Operands of 16 or 8 bits, ready to be loaded: H and T with ldh and ldt bytes from row to row.
@@ -942,43 +1153,170 @@ gist_status run16(hipStream_t st, const gist_table_xent_desc* D, const Plan& p, 
   a.scale = D->scale;
   a.ps = t_scale;
   a.stats = reinterpret_cast<floatx2*>(w + p.stats);
+  float* const ref = p.exps ? f32(p.ref) : nullptr;
+  float* const row_factor = p.exps ? f32(p.row_factor) : nullptr;
+  int* const far = p.exps ? reinterpret_cast<int*>(w + p.far) : nullptr;
+  float* const pm1 = p.exps ? f32(p.pm1) : nullptr;
+  int32_t* const ids = p.exps ? reinterpret_cast<int32_t*>(w + p.ids) : nullptr;
+  a.lse = ref;
+  a.out = w + p.g;
+  a.ldo = p.Cp;
+  a.far = far;
+  if (p.exps) {
+    ProfScope ps(st, "table_xent_count", 0.0, 4.0 * n);
+    hipLaunchKernelGGL(count_kernel, dim3(1), dim3(1024), 0, st, n, labels, n_dev, D->grad_scale * D->scale, f32(p.factor));
+    GIST_LAUNCHED("table_xent_count");
+  }
   for (int64_t r0 = 0; r0 < n; r0 += p.rows) {
     const int64_t rn = std::min(p.rows, n - r0);
     const Cut c = cut_logits(C, rn, a.steps, STORE == GIST_STORE_E4M3);
     set_cut(a, c);
     a.Q = H + r0 * ldh;
     a.N = a.RQ = a.ldstat = rn;
+    a.row0 = r0;
+    a.n_dev = n_dev;
     a.qs = h_scale ? h_scale + r0 : nullptr;
     a.labels = labels + r0;
     a.zy = f32(p.zy) + r0;
+    if constexpr (STORE == GIST_STORE_BF16) {
+      if (p.exps) {
+        ProfScope ps(st, "table_xent_ref", 0.0, 4.0 * rn * d);
+        hipLaunchKernelGGL(ref_kernel, dim3(static_cast<unsigned>((rn + 3) / 4)), dim3(kBlock), 0, st, r0, rn, C,
+                           static_cast<int>(p.wide), D->scale, a.Q, ldh, T, ldt, a.labels, n_dev, ref, far);
+        GIST_LAUNCHED("table_xent_ref");
+      }
+    }
     {
-      ProfScope ps(st, "table_xent_logits", 2.0 * rn * C * d, static_cast<double>(rn + C) * d * e);
-      launch_product<STORE, kStats, false, false>(st, c.tile, a);
+      ProfScope ps(st, "table_xent_logits", 2.0 * rn * C * d,
+                   static_cast<double>(rn + C) * d * e + (p.exps ? 2.0 * rn * C : 0.0));
+      if constexpr (STORE == GIST_STORE_BF16) {
+        if (p.exps) launch_product<STORE, kExp, false, false>(st, c.tile, a);
+        else launch_product<STORE, kStats, false, false>(st, c.tile, a);
+      } else {
+        launch_product<STORE, kStats, false, false>(st, c.tile, a);
+      }
       GIST_LAUNCHED("table_xent_logits");
     }
-    const int parts = c.tiles_m * waves_m(c.tile);
-    ProfScope ps(st, "table_xent_join", 0.0, 8.0 * parts * rn);
-    const int per = rn <= 256 ? 4 : 32;
-    const dim3 grid(static_cast<unsigned>((rn + per - 1) / per));
-    float* const lse_out = lse ? lse + r0 : nullptr;
-    float* const logp_out = logp ? logp + r0 : nullptr;
-    if (per == 4)
-      hipLaunchKernelGGL(join_stats_kernel<4>, grid, dim3(1024), 0, st, r0, rn, C, parts, a.stats, rn, a.zy, a.labels, n_dev,
-                         f32(p.lse) + r0, lse_out, f32(p.logp) + r0, logp_out);
-    else
-      hipLaunchKernelGGL(join_stats_kernel<32>, grid, dim3(1024), 0, st, r0, rn, C, parts, a.stats, rn, a.zy, a.labels, n_dev,
-                         f32(p.lse) + r0, lse_out, f32(p.logp) + r0, logp_out);
-    GIST_LAUNCHED("table_xent_join");
+    {
+      const int parts = c.tiles_m * waves_m(c.tile);
+      ProfScope ps(st, "table_xent_join", 0.0, 8.0 * parts * rn);
+      const int per = rn <= 256 ? 4 : 32;
+      const dim3 grid(static_cast<unsigned>((rn + per - 1) / per));
+      float* const lse_out = lse ? lse + r0 : nullptr;
+      float* const logp_out = logp ? logp + r0 : nullptr;
+      if (per == 4)
+        hipLaunchKernelGGL(join_stats_kernel<4>, grid, dim3(1024), 0, st, r0, rn, C, parts, a.stats, rn, a.zy, a.labels, n_dev,
+                           f32(p.lse) + r0, lse_out, f32(p.logp) + r0, logp_out, ref, row_factor, far);
+      else
+        hipLaunchKernelGGL(join_stats_kernel<32>, grid, dim3(1024), 0, st, r0, rn, C, parts, a.stats, rn, a.zy, a.labels, n_dev,
+                           f32(p.lse) + r0, lse_out, f32(p.logp) + r0, logp_out, ref, row_factor, far);
+      GIST_LAUNCHED("table_xent_join");
+    }
+    if constexpr (STORE == GIST_STORE_BF16) {
+      if (!p.exps) continue;
+      {
+        ProfScope ps(st, "table_xent_again", 0.0, 0.0);   // does nothing but for far rows
+        launch_product<STORE, kAgain, false, false>(st, c.tile, a);
+        GIST_LAUNCHED("table_xent_again");
+      }
+      {
+        ProfScope ps(st, "table_xent_given", 0.0, 18.0 * rn);
+        hipLaunchKernelGGL(given_kernel, dim3(static_cast<unsigned>((rn + kBlock - 1) / kBlock)), dim3(kBlock), 0, st, r0, rn, C,
+                           f32(p.logp) + r0, a.labels, n_dev, reinterpret_cast<unsigned short*>(w + p.g), p.Cp, pm1, ids);
+        GIST_LAUNCHED("table_xent_given");
+      }
+      // the rows of H times their factors, zeros behind the last
+      copy_rows<GIST_STORE_BF16, GIST_STORE_BF16>(st, rn, up(rn, 64), static_cast<int>(p.wide), p.wide, a.Q, ldh / 2, w + p.hm,
+                                                  nullptr, nullptr, row_factor);
+      GIST_LAUNCHED("table_xent_copy");
+      const int64_t ldp = up(d, 4), moved = 2 * rn * C;
+      float* const part_h = f32(p.part);
+      float* const part_t = part_h + (p.parts_h ? p.dh.slices * p.rows * ldp : 0);
+      {   // dH [rn][d] = E T, a row times its factor.  E is zero behind the last class.
+        Prod b{};
+        b.P = T;
+        b.ldp = ldt;
+        b.Q = w + p.g;
+        b.ldq = p.Cp * 2;
+        b.M = d;
+        b.N = b.RQ = rn;
+        b.RP = p.wide;
+        b.KP = C;
+        b.steps = static_cast<int>(up(C, 64) / 64);
+        const Cut k = rn == p.rows ? p.dh : cut_rows(p.dh, rn);
+        set_cut(b, k);
+        char* const out = static_cast<char*>(dH) + r0 * D->lddh * size_of(D->store);
+        ProfScope ps(st, "table_xent_dh", 2.0 * rn * C * d, moved + static_cast<double>(rn + C) * d * e);
+        if (p.parts_h) {
+          b.out = part_h;
+          b.ldo = ldp;
+          launch_product<STORE, kPart, true, false>(st, k.tile, b);
+          GIST_LAUNCHED("table_xent_dh");
+          join_out<STORE>(st, D, rn, b.slices, rn * ldp, part_h, f32(p.factor), Given{row_factor, pm1, ids, T, ldt}, out,
+                          D->lddh);
+        } else {
+          b.out = out;
+          b.ldo = D->lddh;
+          b.factor = f32(p.factor);
+          b.row_factor = row_factor;
+          b.pm1 = pm1;
+          b.ids = ids;
+          b.T = T;
+          b.ldt = ldt;
+          b.out_store = D->store;
+          launch_product<STORE, kOut, true, false>(st, k.tile, b);
+        }
+        GIST_LAUNCHED("table_xent_dh");
+      }
+      {   // dT [C][d] (+)= E^T H, over the piece's rows
+        Prod b{};
+        b.P = w + p.hm;
+        b.ldp = p.wide * 2;
+        b.Q = w + p.g;
+        b.ldq = p.Cp * 2;
+        b.M = d;
+        b.N = C;
+        b.RP = p.wide;
+        b.RQ = up(C, c.tile == 128 ? 128 : 256);    // columns of E that have been written
+        b.KP = up(rn, 64);
+        b.KQ = std::min(b.KP, up(rn, c.tile));      // and rows
+        b.steps = static_cast<int>(b.KP / 64);
+        set_cut(b, p.dt);
+        b.len = (b.steps + b.slices - 1) / b.slices;
+        b.slices = (b.steps + b.len - 1) / b.len;   // no more than the first piece's
+        ProfScope ps(st, "table_xent_dt", 2.0 * rn * C * d, moved + static_cast<double>(rn + C) * d * e);
+        b.out = part_t;
+        b.ldo = ldp;
+        b.add = r0 > 0;
+        launch_product<STORE, kPart, true, true>(st, p.dt.tile, b);
+        GIST_LAUNCHED("table_xent_dt");
+      }
+      {   // and the given classes' rows of H, times p - 1
+        float* const Y = f32(p.y);
+        {
+          ProfScope ps(st, "table_xent_given_rows", 0.0, 6.0 * rn * d);
+          hipLaunchKernelGGL(given_rows_kernel, dim3(grid_of(rn * p.wide / 8)), dim3(kBlock), 0, st, rn, p.wide, a.Q, ldh, pm1, Y);
+          GIST_LAUNCHED("table_xent_given_rows");
+        }
+        const gist_status s = embed_grad(st, rn, C, d, ids, 1.f, Y, p.wide, true, -1.f, part_t, ldp, w + p.embed);
+        if (s != GIST_OK) return s;
+      }
+      if (r0 + rn == n) {
+        ProfScope ps(st, "table_xent_dt_join", 0.0, 4.0 * p.dt.slices * C * ldp);
+        join_out<STORE>(st, D, C, p.dt.slices, C * ldp, part_t, f32(p.factor), Given{}, dT, D->lddt);
+        GIST_LAUNCHED("table_xent_dt_join");
+      }
+    }
   }
   {
     constexpr float kUnhold = STORE == GIST_STORE_F16 ? 1.f / 32768.f : 1.f;
     ProfScope ps(st, "table_xent_loss", 0.0, 8.0 * n);
     hipLaunchKernelGGL(loss_kernel, dim3(1), dim3(1024), 0, st, n, f32(p.logp), labels, n_dev,
-                       D->grad_scale * D->scale * kUnhold, loss, grad ? f32(p.factor) : nullptr);
+                       D->grad_scale * D->scale * kUnhold, loss, grad && !p.exps ? f32(p.factor) : nullptr);
     GIST_LAUNCHED("table_xent_loss");
   }
-  if (!grad) return GIST_OK;
-  if constexpr (STORE != GIST_STORE_E4M3) {
+  if (!grad || p.exps) return GIST_OK;
+  if constexpr (STORE == GIST_STORE_F16) {
     const int64_t ldp = up(d, 4);
     char* const hm = w + p.hm;
     char* const g = w + p.g;
@@ -988,7 +1326,7 @@ gist_status run16(hipStream_t st, const gist_table_xent_desc* D, const Plan& p, 
     a.Q = H;
     a.N = a.RQ = n;
     a.labels = labels;
-    a.n_dev = n_dev;
+    a.row0 = 0;
     a.lse = f32(p.lse);
     for (int64_t c0 = 0; c0 < C; c0 += p.Cp) {
       const int64_t cn = std::min(p.Cp, C - c0);
@@ -1058,7 +1396,7 @@ gist_status run16(hipStream_t st, const gist_table_xent_desc* D, const Plan& p, 
           b.ldo = ldp;
           launch_product<STORE, kPart, true, true>(st, p.dt.tile, b);
           GIST_LAUNCHED("table_xent_dt");
-          join_out<STORE>(st, D, cn, b.slices, cn * ldp, part_t, factor, out, D->lddt);
+          join_out<STORE>(st, D, cn, b.slices, cn * ldp, part_t, factor, Given{}, out, D->lddt);
         } else {
           b.out = out;
           b.ldo = D->lddt;
@@ -1071,19 +1409,11 @@ gist_status run16(hipStream_t st, const gist_table_xent_desc* D, const Plan& p, 
     }
     if (p.parts_h) {
       ProfScope ps(st, "table_xent_dh_join", 0.0, 4.0 * p.dh.slices * n * ldp);
-      join_out<STORE>(st, D, n, p.dh.slices, n * ldp, part_h, factor, dH, D->lddh);
+      join_out<STORE>(st, D, n, p.dh.slices, n * ldp, part_h, factor, Given{}, dH, D->lddh);
       GIST_LAUNCHED("table_xent_dh_join");
     }
   }
   return GIST_OK;
-}
-
-template <int SRC, int DST>
-void copy_rows(hipStream_t st, int64_t n, int64_t n_pad, int d, int64_t wide, const void* x, int64_t ldx, void* y,
-               const int32_t* labels, const int32_t* n_dev) {
-  ProfScope ps(st, "table_xent_copy", 0.0, static_cast<double>(n_pad) * wide * (size_of(SRC) + size_of(DST)));
-  hipLaunchKernelGGL((copy_rows_kernel<SRC, DST>), dim3(grid_of(n_pad * wide / 8)), dim3(kBlock), 0, st, n, n_pad, d,
-                     static_cast<int>(wide), x, ldx, y, labels, n_dev);
 }
 
 template <int SRC, int STORE>
@@ -1104,7 +1434,7 @@ gist_status run_copied(hipStream_t st, const gist_table_xent_desc* D, const Plan
     t = w + p.t;
     ldt = p.wide * e;
   }
-  if constexpr (STORE != GIST_STORE_E4M3)
+  if constexpr (STORE == GIST_STORE_F16)
     if (dH) copy_rows<SRC, STORE>(st, D->n, up(D->n, 64), D->d, p.wide, H, D->ldh, w + p.hm, labels, n_dev);
   GIST_LAUNCHED("table_xent_copy");
   return run16<STORE>(st, D, p, h, ldh, t, ldt, h_scale, t_scale, labels, n_dev, loss, logp, lse, dH, dT, w);

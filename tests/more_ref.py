@@ -128,6 +128,8 @@ def table_xent_bounds(H, T, y, scale, r, op, store):
         return dict(lse=lse, logp=logp, loss=loss)
     p = np.where(r["real"][:, None], np.exp(np.minimum(r["z"] - r["lse"][:, None], 0.0)), 0.0)
     eg = p * (ez + lse[:, None] + U32 * (np.abs(r["z"] - r["lse"][:, None]) + 6)) + U32 * np.abs(r["G"])
+    # bf16: e^(z - r) e^(r - lse), r about the given class's logit
+    eg = eg + p * U32 * 2 * (np.abs(r["z"][at, yy] - r["lse"])[:, None] + 4)
     # G's rounding: fp16 holds it times 2^15
     eg = eg + HALF[op] * (np.abs(r["G"]) + eg) + (2.0 ** -25 / 32768 if op == "f16" else 0.0)
     f = abs(r["f"])
@@ -136,7 +138,9 @@ def table_xent_bounds(H, T, y, scale, r, op, store):
     aG = np.abs(r["G"]) + eg
     out = {}
     for name, a, b, k in (("dH", aG, np.abs(T), C), ("dT", aG.T, np.abs(r["Hz"]), n)):
-        e = f * ((eg if name == "dH" else eg.T) @ b + 2 * U32 * (k + 24) * (a @ b)) + 2.0 ** -126
+        # dT in bf16: the rows of H times their factors are rounded as well
+        more = HALF[op] * (a @ b) if name == "dT" and op == "bf16" else 0.0
+        e = f * (more + (eg if name == "dH" else eg.T) @ b + 2 * U32 * (k + 24) * (a @ b)) + 2.0 ** -126
         out[name] = e + HALF[store] * (np.abs(r[name]) + e) + (2.0 ** -25 if store == "f16" else 0.0)
     return dict(lse=lse, logp=logp, loss=loss, **out)
 

@@ -207,30 +207,80 @@ def test_large_logits(G, ctx, store):
     check(out, Hv, Tv, y, store)
 
 
-@pytest.mark.parametrize("store", ["f32", "bf16"])
-def test_several_pieces(G, ctx, store):
-    """More rows and classes than one piece of the workspace holds (n C above 2^27 16-bit or 2^26 fp32
-    values): the gradients against pieces computed with 64-bit sums on a sample of rows and classes."""
+@pytest.mark.parametrize("store", ["f32", "bf16", "f16"])
+def test_some_rows_far_from_their_class(G, ctx, store):
+    """Rows whose largest logit is hundreds above their label's, among others, in one of three
+    groups of 256."""
+    rng = np.random.default_rng(2)
+    H, T, y = inputs(700, 300, 64, rng)
+    H[300:311] *= 60
+    out, Hv, Tv, _ = run(G, ctx, H, T, y, store)
+    check(out, Hv, Tv, y, store)
+
+
+def on_the_gpu(Hv, Tv, y, scale, gscale, grad, rows=100):
+    """lse, and dH, dT with the sums of their terms' magnitudes, in 64 bits, some rows at a time."""
     import torch
-    n, C, d = (3000, 50000, 64) if store == "bf16" else (2000, 40001, 32)
+    H, T = torch.from_numpy(Hv).cuda(), torch.from_numpy(Tv).cuda()
+    n = len(y)
+    f = gscale * scale / max(1, int((y >= 0).sum()))
+    lse = torch.empty(n, dtype=torch.float64, device="cuda")
+    dH, mH = torch.zeros_like(H), torch.zeros_like(H)
+    dT, mT = torch.zeros_like(T), torch.zeros_like(T)
+    far, aH, aT = 0.0, H.abs(), T.abs()
+    for a in range(0, n, rows):
+        z = scale * (H[a:a + rows] @ T.t().contiguous())
+        lse[a:a + rows] = torch.logsumexp(z, 1)
+        far = max(far, float(scale * (aH[a:a + rows] @ aT.t().contiguous()).max()))
+        if not grad:
+            continue
+        g = torch.exp(z - lse[a:a + rows, None])
+        for i in range(len(g)):
+            if y[a + i] < 0:
+                g[i] = 0
+            else:
+                g[i, int(y[a + i])] -= 1
+        dH[a:a + rows] = f * (g @ T)
+        mH[a:a + rows] = f * (g.abs() @ aT)
+        dT += f * (g.t().contiguous() @ H[a:a + rows])
+        mT += f * (g.abs().t().contiguous() @ aH[a:a + rows])
+    return lse.cpu().numpy(), [(t.cpu().numpy()) for t in (dH, mH, dT, mT)], far
+
+
+@pytest.mark.parametrize("store,n,C,d", [("f32", 2000, 40001, 32), ("f16", 3000, 50000, 64),
+                                         ("bf16", 1000, 600001, 16)])
+def test_several_pieces(G, ctx, store, n, C, d):
+    """More rows or classes than one piece of the workspace holds (2^26 fp32 logits, 2^27 fp16
+    gradients, 2^29 bf16 exponentials)."""
     rng = np.random.default_rng(1)
     H, T, y = inputs(n, C, d, rng)
     out, Hv, Tv, _ = run(G, ctx, H, T, y, store)
     scale = float(np.float32(0.7))
-    z = scale * (torch.from_numpy(Hv) @ torch.from_numpy(Tv).t())
-    lse = torch.logsumexp(z, 1)
-    real = torch.from_numpy(y >= 0)
-    g = torch.exp(z - lse[:, None]) * real[:, None]
-    g[torch.arange(n)[real], torch.from_numpy(y).long()[real]] -= 1
-    f = 3.0 * scale / int(real.sum())
-    dH, dT = f * (g @ torch.from_numpy(Tv)).numpy(), f * (g.t() @ torch.from_numpy(Hv)).numpy()
-    # a logit's error (as in more_ref) times p, G's rounding and the sums': relative to the magnitudes
-    mag = f * (g.abs() @ torch.from_numpy(np.abs(Tv))).numpy(), f * (g.abs().t() @ torch.from_numpy(np.abs(Hv))).numpy()
-    ez = 4 * R.U32 * (d + 16) * float(scale * (np.abs(Hv) @ np.abs(Tv[:200]).T).max()) + 2e-5
-    for k, want, m, terms in (("dH", dH, mag[0], C), ("dT", dT, mag[1], n)):
-        b = m * (ez + R.HALF[store] + 2 * R.U32 * (terms + 24)) + R.HALF[store] * np.abs(want)
-        assert (np.abs(out[k] - want) <= b).all(), k
-    assert (np.abs(out["lse"] - lse.numpy()) <= ez + R.lse_bound(z.numpy())).all()
+    lse, (dH, mH, dT, mT), far = on_the_gpu(Hv, Tv, y, scale, 3.0, True)
+    # a logit's error (as in more_ref), that of lse and of the exponentials, times p; G's rounding,
+    # bf16's of the scaled rows, and the sums', relative to the magnitudes
+    ez = 4 * R.U32 * (d + 16) * far + R.U32 * (C / 64 + 28 + 4 * np.log2(C) + 200)
+    half = R.HALF[store]
+    for k, want, m, terms in (("dH", dH, mH, C), ("dT", dT, mT, n)):
+        b = m * (ez + (2.1 if store == "bf16" else 1.1) * half + 2 * R.U32 * (terms + 24)) + half * np.abs(want)
+        assert (np.abs(out[k] - want) <= b + (2.0 ** -25 if store == "f16" else 2.0 ** -120)).all(), k
+    assert (np.abs(out["lse"] - lse) <= ez).all()
+
+
+@pytest.mark.parametrize("store", ["bf16", "e4m3"])
+def test_more_rows_than_the_statistics_hold(G, ctx, store):
+    """Forward pass of 4,000 rows against 600,001 classes: the parts' maxima and sums of 3,328 rows
+    fill their room."""
+    rng = np.random.default_rng(6)
+    H, T, y = inputs(4000, 600001, 16, rng)
+    out, Hv, Tv, _ = run(G, ctx, H, T, y, store, grad=False)
+    scale = float(np.float32(0.7))
+    lse, _, far = on_the_gpu(Hv, Tv, y, scale, 3.0, False)
+    e = (2.0 ** -12 if store == "e4m3" else 4 * R.U32 * 32) * far + R.U32 * (600001 / 64 + 300)
+    assert (np.abs(out["lse"] - lse) <= e).all()
+    real = y >= 0
+    zy = scale * (Hv * Tv[np.maximum(y, 0)]).sum(1)
+    assert (np.abs(out["logp"] - (zy - lse)) <= 2 * e)[real].all() and (out["logp"][~real] == 0).all()
 
 
 def test_gradient_against_differences(G, ctx):
