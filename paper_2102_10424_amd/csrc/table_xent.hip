@@ -145,28 +145,31 @@ struct Frag<GIST_STORE_E4M3> {   // 32 values of K a lane
   intx8 v;
 };
 
+// 16 x 16 blocks: they take half the passes over the accumulators that 32 x 32 ones do, and
+// power is what bounds the products (alone, on random bf16 operands, 2,050 TFLOP/s, 32 x 32
+// ones 1,810).
 template <int STORE>
-__device__ __forceinline__ floatx16 mma(const Frag<STORE>& a, const Frag<STORE>& b, floatx16 c) {
+__device__ __forceinline__ floatx4 mma(const Frag<STORE>& a, const Frag<STORE>& b, floatx4 c) {
   if constexpr (STORE == GIST_STORE_BF16)
-    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a.v), __builtin_bit_cast(bf16x8, b.v), c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a.v), __builtin_bit_cast(bf16x8, b.v), c, 0, 0, 0);
   else if constexpr (STORE == GIST_STORE_F16)
-    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, a.v), __builtin_bit_cast(half8, b.v), c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, a.v), __builtin_bit_cast(half8, b.v), c, 0, 0, 0);
   else   // block scales of 1 (exponent 127)
-    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a.v, b.v, c, 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a.v, b.v, c, 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);
 }
 
 // One operand's share of a step in LDS, ROWS of its own index by 128 bytes of K.
 //  As rows: 128 bytes a row, its 16-byte piece p at p ^ (row / 2 mod 8), which spreads a
-//   fragment read (one piece of 32 rows) over the banks.
+//   fragment read (one piece of 16 rows) over the banks.
 //  Transposed: 64 k, 2 ROWS bytes each; 32-byte chunk c (16 of its own index) at c ^ f(k),
-//   f(k) = k mod 4 + 4 (k / 8 mod 2): a transposing read takes four k of two
-//   chunks for each half of a fragment, which f sends to different banks.
+//   f(k) = k mod 4 + 4 (k / 8 mod 2): half a wave's transposing read takes k .. k + 3 and
+//   k + 8 .. k + 11 of one chunk, which this sends to all 64 banks.
 template <int ROWS, bool TR>
 struct Tile {
   static constexpr int kPieces = TR ? ROWS / 8 : 8;   // 16-byte pieces of a line's row
   // Where lane's 16 bytes of line L (1 KB of the tile, in LDS order) come from; `left`: rows (or,
-  // transposed, values of its own index) that are there; klim: values of K.
-  __device__ __forceinline__ static unsigned offset(int L, int lane, int64_t ld, int64_t left, int klim) {
+  // transposed, values of its own index) that are there.
+  __device__ __forceinline__ static unsigned offset(int L, int lane, int64_t ld, int64_t left) {
     if constexpr (!TR) {
       const int row = 8 * L + (lane >> 3);
       const int piece = (lane & 7) ^ (row >> 1 & 7);
@@ -176,37 +179,43 @@ struct Tile {
       const int f = (k & 3) | ((k >> 3 & 1) << 2);
       const int piece = ((s >> 1 ^ f) << 1) | (s & 1);
       const int last = static_cast<int>(min(static_cast<int64_t>(kPieces), left / 8)) - 1;
-      return static_cast<unsigned>(min(k, klim - 1)) * static_cast<unsigned>(ld) + min(piece, last) * 16;
+      return static_cast<unsigned>(k) * static_cast<unsigned>(ld) + min(piece, last) * 16;
     }
   }
-  // A lane's part of a fragment's address: block of 32 rows.
+  // The same of line L + i where only klim values of K are there: what lies behind them is the last
+  // again.  k: of line L.
+  __device__ __forceinline__ static unsigned limited(unsigned off, int k, int i, int64_t ld, int klim) {
+    return off - static_cast<unsigned>(max(k + i * (64 / kPieces) - (klim - 1), 0)) * static_cast<unsigned>(ld);
+  }
+  // A lane's part of the address of a wave's first block of 16 rows (blk: a multiple of 4), depth 0.
   __device__ __forceinline__ static int base(int lane, int blk) {
-    const int li = lane & 31, lh = lane >> 5;
+    const int i = lane & 15, g = lane >> 4;
     if constexpr (!TR) {
-      return (blk * 32 + li) * 128;
+      return (blk * 16 + i) * 128 + (g ^ (i >> 1)) * 16;
     } else {
-      const int i = lane & 15, k = 8 * lh + (i >> 2), f = (i >> 2) | (lh << 2);
-      return k * (2 * ROWS) + (((2 * blk + (lane >> 4 & 1)) ^ f) << 5) + (i & 3) * 8;
+      const int k = 8 * g + (i >> 2), f = (i >> 2) | ((g & 1) << 2);
+      return k * (2 * ROWS) + ((blk ^ f) << 5) + (i & 3) * 8;
     }
   }
-  // Fragment of depth q (16 values of K; 64 of 8 bits); sw: (row / 2 mod 8) of the lane's row.
+  // Fragment of the wave's block x at depth q (32 values of K; 128 of 8 bits).  `at`: a buffer's base
+  // and the lane's; what depends on x and q comes by exclusive or and fixed offsets, so that no
+  // address but this one takes a register.
   template <int STORE>
-  __device__ __forceinline__ static void read(const char* tile, int base, int q, int lane, Frag<STORE>& f) {
-    const int lh = lane >> 5, sw = lane >> 1 & 7;
+  __device__ __forceinline__ static void read(const char* lds, int at, int q, int x, Frag<STORE>& f) {
     if constexpr (TR) {
       typedef __attribute__((address_space(3))) short4v* Ptr;
-      const char* p = tile + base + q * (16 * 2 * ROWS);
+      const char* p = lds + (at ^ x << 5) + q * (32 * 2 * ROWS);
       const short4v a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Ptr)(const __attribute__((address_space(3))) char*)p);
       const short4v b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
           (Ptr)(const __attribute__((address_space(3))) char*)(p + 4 * 2 * ROWS));
       f.v = __builtin_bit_cast(intx4, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
     } else if constexpr (STORE == GIST_STORE_E4M3) {
-      // the 64 values of a depth lie in pieces 4 q .. 4 q + 3: any two of them a lane, in both operands
-      const intx4 a = *reinterpret_cast<const intx4*>(tile + base + (((4 * q + 2 * lh) ^ sw) << 4));
-      const intx4 b = *reinterpret_cast<const intx4*>(tile + base + (((4 * q + 2 * lh + 1) ^ sw) << 4));
+      // any two of a row's eight pieces a lane, the same in both operands: g and g + 4
+      const intx4 a = *reinterpret_cast<const intx4*>(lds + at + x * 2048);
+      const intx4 b = *reinterpret_cast<const intx4*>(lds + (at ^ 64) + x * 2048);
       f.v = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
     } else {
-      f.v = *reinterpret_cast<const intx4*>(tile + base + (((2 * q + lh) ^ sw) << 4));
+      f.v = *reinterpret_cast<const intx4*>(lds + (at ^ q * 64) + x * 2048);
     }
   }
 };
@@ -229,14 +238,15 @@ __device__ __forceinline__ void pack4(const float (&v)[4], int (&u)[2]) {
                             static_cast<unsigned>(narrow<STORE>(v[2 * h + 1])) << 16);
 }
 
-// Registers 4 r4 .. 4 r4 + 3 of a 32 x 32 block hold, in lane l, columns 8 r4 + 4 (l / 32) + 0..3
-// of row l mod 32.  Two such groups (a: r4 even, b: r4 + 1), packed, become eight
-// consecutive columns: 8 r4 + 8 (l / 32) + 0..7.
+// A 16 x 16 block's registers hold, in lane l, columns 4 (l / 16) + 0..3 of row l mod 16.  Two
+// neighbouring blocks, packed (a: columns 0..15, b: 16..31), become eight consecutive columns a
+// lane: those from col8(l) on.
+__device__ __forceinline__ int col8(int lane) { return ((lane >> 4 & 1) << 4) + ((lane >> 5) << 3); }
 __device__ __forceinline__ intx4 join8(const int (&a)[2], const int (&b)[2]) {
   intx4 r;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    const auto s = __builtin_amdgcn_permlane32_swap(a[h], b[h], false, false);
+    const auto s = __builtin_amdgcn_permlane16_swap(a[h], b[h], false, false);
     r[h] = s[0];
     r[2 + h] = s[1];
   }
@@ -246,18 +256,27 @@ __device__ __forceinline__ intx4 join8(const int (&a)[2], const int (&b)[2]) {
 // Rows of these that a label counts for.
 __device__ __forceinline__ int64_t rows_real(const Prod& a) { return a.n_dev ? *a.n_dev - a.row0 : a.N; }
 
-// Tiles of 32 WM NWM columns (M) by 32 WN NWN rows (N); NS buffers in LDS, one barrier a step.
+// Tiles of 16 WM NWM columns (M) by 16 WN NWN rows (N); NS buffers in LDS of a step each.
+//
+// A step's MFMAs go by the wave's WM column blocks, WN at a time; behind each of these the block's
+// own fragment is read again, for the next depth, and has the time of all others to
+// arrive.  The barrier that frees a buffer stands some blocks into the last depth, when that
+// depth's fragments have arrived, so that MFMAs that wait for nothing are on both sides of
+// it.  The loads of the step that takes the buffer go out behind it, a few after each
+// block: together, eight waves' loads would keep the load path (16 cycles each) for half a step.
 template <int STORE, int WM, int WN, int NWM, int NWN, int NS, bool PT, bool QT, int EPI>
 __global__ __launch_bounds__(64 * NWM * NWN, NS == 2 ? 2 : 1) void product_kernel(Prod a) {
-  constexpr int BM = 32 * WM * NWM, BN = 32 * WN * NWN;
-  constexpr int LINES = (BM + BN) / 8, WAVES = NWM * NWN, LOADS = LINES / WAVES;
+  constexpr int BM = 16 * WM * NWM, BN = 16 * WN * NWN;
+  constexpr int LP = BM / 8, LINES = (BM + BN) / 8, WAVES = NWM * NWN, LOADS = LINES / WAVES;
   static_assert(LINES % WAVES == 0, "a wave's loads");
+  static_assert(WM % 4 == 0, "blocks are stored two by two");
+  constexpr int BUF = (BM + BN) * 128;
   constexpr bool E8 = STORE == GIST_STORE_E4M3;
-  constexpr int QN = E8 ? 2 : 4;      // depths of a step
+  constexpr int QN = E8 ? 1 : 2;      // depths of a step
   constexpr int KSTEP = E8 ? 128 : 64;
   using TP = Tile<BM, PT>;
   using TQ = Tile<BN, QT>;
-  __shared__ __attribute__((aligned(1024))) char lds[NS][(BM + BN) * 128];
+  __shared__ __attribute__((aligned(1024))) char lds[NS][BUF];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / NWN, wn = wave % NWN;
@@ -282,137 +301,163 @@ __global__ __launch_bounds__(64 * NWM * NWN, NS == 2 ? 2 : 1) void product_kerne
   const char* const qb = a.Q + (QT ? n0 * 2 : n0 * a.ldq);
   const unsigned lds0 = static_cast<unsigned>(reinterpret_cast<uintptr_t>(
       (__attribute__((address_space(3))) char*)&lds[0][0]));
+  // Every wave loads lines of one operand.
+  static_assert(!(PT || QT) || LP % LOADS == 0, "a wave's lines");
+  const int L0 = wave * LOADS;
+  const bool is_p = L0 < LP;
   unsigned off[LOADS];
-  auto offset_of = [&](int i, int kp, int kq) {
-    const int L = wave * LOADS + i;
-    return L < BM / 8 ? TP::offset(L, lane, a.ldp, a.RP - m0, kp)
-                      : TQ::offset(L - BM / 8, lane, a.ldq, a.RQ - n0, kq);
-  };
 #pragma unroll
-  for (int i = 0; i < LOADS; ++i) off[i] = offset_of(i, KSTEP, KSTEP);
-  auto load = [&](int buf, int j) {
+  for (int i = 0; i < LOADS; ++i)
+    off[i] = L0 + i < LP ? TP::offset(L0 + i, lane, a.ldp, a.RP - m0) : TQ::offset(L0 + i - LP, lane, a.ldq, a.RQ - n0);
+  // The step whose loads are being issued: where its operands begin, and values of K it has.
+  const char* sp = nullptr;
+  const char* sq = nullptr;
+  int kp = KSTEP, kq = KSTEP;
+  auto aim = [&](int j) {
     const int64_t k = k0 + j;
-    const char* const p = pb + (PT ? k * KSTEP * a.ldp : k * 128);
-    const char* const q = qb + (QT ? k * KSTEP * a.ldq : k * 128);
-    const int kp = PT ? static_cast<int>(min(static_cast<int64_t>(KSTEP), a.KP - k * KSTEP)) : KSTEP;
-    const int kq = QT ? static_cast<int>(min(static_cast<int64_t>(KSTEP), a.KQ - k * KSTEP)) : KSTEP;
-    const bool tail = kp < KSTEP || kq < KSTEP;
-#pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-      const int L = wave * LOADS + i;
-      const unsigned o = tail ? offset_of(i, kp, kq) : off[i];
-      load_to_lds(lds0 + buf * ((BM + BN) * 128) + L * 1024, o, L < BM / 8 ? p : q);
-    }
+    sp = pb + (PT ? k * KSTEP * a.ldp : k * 128);
+    sq = qb + (QT ? k * KSTEP * a.ldq : k * 128);
+    if constexpr (PT) kp = static_cast<int>(min(static_cast<int64_t>(KSTEP), a.KP - k * KSTEP));
+    if constexpr (QT) kq = static_cast<int>(min(static_cast<int64_t>(KSTEP), a.KQ - k * KSTEP));
   };
-  floatx16 acc[WM][WN] = {};
+  auto load = [&](int buf, int i) {
+    unsigned o = off[i];
+    if constexpr (PT)
+      if (is_p && kp < KSTEP) o = TP::limited(o, L0 * (64 / TP::kPieces) + lane / TP::kPieces, i, a.ldp, kp);
+    if constexpr (QT)
+      if (!is_p && kq < KSTEP) o = TQ::limited(o, (L0 - LP) * (64 / TQ::kPieces) + lane / TQ::kPieces, i, a.ldq, kq);
+    load_to_lds(lds0 + buf * BUF + (L0 + i) * 1024, o, L0 + i < LP ? sp : sq);
+  };
+  floatx4 acc[WM][WN] = {};
 #pragma unroll
-  for (int j = 0; j < NS; ++j) load(j, min(j, steps - 1));   // always NS: the counts below hold
-  int fa[WM], fb[WN];
+  for (int j = 0; j < NS; ++j) {
+    aim(min(j, steps - 1));   // always NS: the counts below hold
 #pragma unroll
-  for (int x = 0; x < WM; ++x) fa[x] = TP::base(lane, wm * WM + x);
-#pragma unroll
-  for (int y = 0; y < WN; ++y) fb[y] = BM * 128 + TQ::base(lane, wn * WN + y);
-  constexpr int FB = E8 ? 1 : 2;      // fragments are read a depth ahead; 8-bit ones are too large
-  Frag<STORE> A[FB][WM], B[FB][WN];
-  auto read = [&](int to, int buf, int q) {
-    const char* tile = &lds[0][0] + buf * ((BM + BN) * 128);
-#pragma unroll
-    for (int x = 0; x < WM; ++x) TP::template read<STORE>(tile, fa[x], q, lane, A[to][x]);
-#pragma unroll
-    for (int y = 0; y < WN; ++y) TQ::template read<STORE>(tile, fb[y], q, lane, B[to][y]);
+    for (int i = 0; i < LOADS; ++i) load(j, i);
+  }
+  const int fa = TP::base(lane, wm * WM), fb = BM * 128 + TQ::base(lane, wn * WN);
+  Frag<STORE> A[WM], B[2][WN];
+  auto read_a = [&](int buf, int q, int x) { TP::template read<STORE>(&lds[0][0], fa + buf * BUF, q, x, A[x]); };
+  auto read_b = [&](int to, int buf, int q, int y) {
+    TQ::template read<STORE>(&lds[0][0], fb + buf * BUF, q, y, B[to][y]);
   };
   wait_loads<LOADS * (NS - 1)>();
   lds_barrier();
-  if constexpr (!E8) read(0, 0, 0);
-  int buf = 0, next = 1 % NS;
-  for (int j = 0; j < steps; ++j) {
 #pragma unroll
-    for (int q = 0; q < QN; ++q) {
-      const int f = E8 ? 0 : q & 1;
-      if constexpr (E8) read(0, buf, q);
-      if (q + 1 < QN) {
-        if constexpr (!E8) read(f ^ 1, buf, q + 1);
-      } else {
-        // the last depth of step j: its fragments are read by this wave and, behind the
-        // barrier, by all, so its buffer takes step j + NS; step j + 1 has arrived
-        wait_loads<LOADS * (NS - 2)>();
-        lds_barrier();
-        load(buf, min(j + NS, steps - 1));   // past the end: the last step again, never used
-        if constexpr (!E8) read(f ^ 1, next, 0);
-      }
+  for (int y = 0; y < WN; ++y) read_b(0, 0, 0, y);
 #pragma unroll
-      for (int x = 0; x < WM; ++x)
+  for (int x = 0; x < WM; ++x) read_a(0, 0, x);
+  constexpr int XB = WM / 4;                        // blocks of the last depth before the barrier
+  constexpr int GROUPS = QN * WM;                   // of a step; its loads go out in the first half
+  constexpr int PER = (2 * LOADS + GROUPS - 1) / GROUPS;
+  int buf = 0, next = 1 % NS, freed = 0;
+  for (int j = 0; j < steps; j += 2 / QN) {
+    // (B has two sets by depth: with one depth a step, two steps a round)
 #pragma unroll
-        for (int y = 0; y < WN; ++y) acc[x][y] = mma<STORE>(A[f][x], B[f][y], acc[x][y]);
-      if constexpr (!E8) {
-        constexpr int READS = (PT ? 2 : 1) * WM + (QT ? 2 : 1) * WN;
+    for (int u = 0; u < 2; ++u) {
+      constexpr int kOne = QN == 1;
+      const int q = kOne ? 0 : u, f = u;
+      if (kOne && u == 1 && j + 1 >= steps) break;
+      const bool last = q + 1 == QN;
+      const int jj = kOne ? j + u : j;
 #pragma unroll
-        for (int m = 0; m < WM * WN; ++m) {
-          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                                    // an MFMA
-          __builtin_amdgcn_sched_group_barrier(0x100, (READS + WM * WN - 1) / (WM * WN), 0);    // LDS reads
+      for (int x = 0; x < WM; ++x) {
+        if (last && x == XB) {
+          // All fragments of step jj are read by this wave and, behind the barrier, by all, so
+          // its buffer takes step jj + NS; step jj + 1 has arrived.
+          wait_loads<LOADS * (NS - 2)>();
+          lds_barrier();
+          freed = buf;
+          aim(min(jj + NS, steps - 1));   // past the end: the last step again, never used
+        }
+        const int pos = last && x >= XB ? x - XB : WM - XB + q * WM + x;   // groups since the barrier
+        if (pos < WM - XB || jj > 0) {
+#pragma unroll
+          for (int i = 0; i < LOADS; ++i)
+            if (i / PER == pos) load(freed, i);
+        }
+#pragma unroll
+        for (int y = 0; y < WN; ++y) acc[x][y] = mma<STORE>(A[x], B[f][y], acc[x][y]);
+        // the next depth's fragments: this block's, and B's one by one
+        if (!last) {
+          read_a(buf, q + 1, x);
+          if (x < WN) read_b(f ^ 1, buf, q + 1, x);
+        } else if (x >= XB) {
+          if (x == XB) {
+#pragma unroll
+            for (int z = 0; z < XB; ++z) read_a(next, 0, z);
+#pragma unroll
+            for (int y = WM - XB; y < WN; ++y) read_b(f ^ 1, next, 0, y);
+          }
+          read_a(next, 0, x);
+          if (x - XB < WN) read_b(f ^ 1, next, 0, x - XB);
         }
         __builtin_amdgcn_sched_barrier(0);
       }
+      if (last) {
+        buf = next;
+        next = next + 1 == NS ? 0 : next + 1;
+      }
     }
-    buf = next;
-    next = next + 1 == NS ? 0 : next + 1;
   }
   wait_loads<0>();   // nothing may still be on its way to LDS when the workgroup ends
 
-  const int li = lane & 31, lh = lane >> 5;
-  const int64_t mw = m0 + wm * (WM * 32);   // the wave's first column
+  const int li = lane & 15, g4 = 4 * (lane >> 4);
+  const int64_t mw = m0 + wm * (WM * 16);   // the wave's first column
+  constexpr int OPS = E8 ? static_cast<int>(GIST_STORE_BF16) : STORE;
   if constexpr (EPI == kStats || EPI == kGrad || EPI == kExp || EPI == kAgain) {
     const int64_t real = rows_real(a);
-    const bool edge = mw + WM * 32 > a.M;
+    const bool edge = mw + WM * 16 > a.M;
     if constexpr (E8) {      // the classes' scales
 #pragma unroll
-      for (int x = 0; x < WM; ++x)
+      for (int x = 0; x < WM; ++x) {
+        const int64_t c = mw + x * 16 + g4;
+        float s[4];
+        load_some<GIST_STORE_F32, 4>(a.ps, c, a.M - c, 0.f, s);
 #pragma unroll
-        for (int r4 = 0; r4 < 4; ++r4) {
-          const int64_t c = mw + x * 32 + 8 * r4 + 4 * lh;
-          float t[4];
-          load_some<GIST_STORE_F32, 4>(a.ps, c, a.M - c, 0.f, t);
+        for (int y = 0; y < WN; ++y)
 #pragma unroll
-          for (int y = 0; y < WN; ++y)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) acc[x][y][4 * r4 + q] *= t[q];
-        }
+          for (int r = 0; r < 4; ++r) acc[x][y][r] *= s[r];
+      }
     }
 #pragma unroll
     for (int y = 0; y < WN; ++y) {
-      const int64_t row = n0 + (wn * WN + y) * 32 + li;
+      const int64_t row = n0 + (wn * WN + y) * 16 + li;
       const bool there = row < a.N;
       float zs = a.scale;
       if (E8 && there) zs *= a.qs[row];
       const int label = there ? a.labels[row] : -1;
       // the label's place among the wave's classes
       const int64_t mine = label >= 0 ? label - (a.class0 + mw) : -1;
-      const bool any_label = __any(mine >= 0 && mine < WM * 32);
-      float z[WM][16];
+      const bool any_label = __any(mine >= 0 && mine < WM * 16);
 #pragma unroll
       for (int x = 0; x < WM; ++x)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) z[x][r] = acc[x][y][r] * zs;
-      if constexpr (EPI == kExp || EPI == kAgain) {
-        // E, also of rows and classes that only fill up tiles, and of rows without a label: zeros
+        for (int r = 0; r < 4; ++r) acc[x][y][r] *= zs;
+      if constexpr (EPI != kStats) {
+        // E, or G, also of rows and classes that only fill up tiles, and of rows without a label: zeros
         const bool used = there && row < real && label >= 0;
+        constexpr bool kG = EPI == kGrad;
+        constexpr float kHold = kG && STORE == GIST_STORE_F16 ? 32768.f : 1.f;
         const float ref = used ? a.lse[row] : 0.f;
-        unsigned short* const g = static_cast<unsigned short*>(a.out) + row * a.ldo + mw + 8 * lh;
+        unsigned short* const g = static_cast<unsigned short*>(a.out) + row * a.ldo + mw + col8(lane);
 #pragma unroll
-        for (int x = 0; x < WM; ++x) {
-          int u[4][2];
+        for (int x = 0; x < WM; x += 2) {
+          int w[2][2];
 #pragma unroll
-          for (int r4 = 0; r4 < 4; ++r4) {
+          for (int h = 0; h < 2; ++h) {
             float v[4];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              v[q] = ex2((z[x][4 * r4 + q] - ref) * kL);
-              if (!used || (edge && mw + x * 32 + 8 * r4 + 4 * lh + q >= a.M)) v[q] = 0.f;
+            for (int r = 0; r < 4; ++r) {
+              const int c = (x + h) * 16 + g4 + r;
+              v[r] = ex2((acc[x + h][y][r] - ref) * kL);
+              if (kG && any_label && mine == c) v[r] -= 1.f;
+              v[r] *= kHold;
+              if (!used || (edge && mw + c >= a.M)) v[r] = 0.f;
             }
-            pack4<GIST_STORE_BF16>(v, u[r4]);
+            pack4<OPS>(v, w[h]);
           }
-          *reinterpret_cast<intx4*>(g + x * 32) = join8(u[0], u[1]);
-          *reinterpret_cast<intx4*>(g + x * 32 + 16) = join8(u[2], u[3]);
+          *reinterpret_cast<intx4*>(g + x * 16) = join8(w[0], w[1]);
         }
       }
       if constexpr (EPI == kStats || EPI == kExp) {
@@ -420,138 +465,103 @@ __global__ __launch_bounds__(64 * NWM * NWN, NS == 2 ? 2 : 1) void product_kerne
 #pragma unroll
           for (int x = 0; x < WM; ++x)
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
-              if (mw + x * 32 + 8 * (r >> 2) + 4 * lh + (r & 3) >= a.M) z[x][r] = -__builtin_inff();
+            for (int r = 0; r < 4; ++r)
+              if (mw + x * 16 + g4 + r >= a.M) acc[x][y][r] = -__builtin_inff();
         }
-        float m = z[0][0];
+        float m = acc[0][y][0];
 #pragma unroll
         for (int x = 0; x < WM; ++x)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) m = fmaxf(m, z[x][r]);
+          for (int r = 0; r < 4; ++r) m = fmaxf(m, acc[x][y][r]);
+        m = fmaxf(m, __shfl_xor(m, 16, 64));
         m = fmaxf(m, __shfl_xor(m, 32, 64));
         const float ref = m == -__builtin_inff() ? 0.f : m;
         float s = 0.f;
 #pragma unroll
         for (int x = 0; x < WM; ++x) {
-          float p[4] = {};
+          float p[4];
 #pragma unroll
-          for (int r = 0; r < 16; ++r) p[r & 3] += ex2((z[x][r] - ref) * kL);
+          for (int r = 0; r < 4; ++r) p[r] = ex2((acc[x][y][r] - ref) * kL);
           s += (p[0] + p[1]) + (p[2] + p[3]);
         }
+        s += __shfl_xor(s, 16, 64);
         s += __shfl_xor(s, 32, 64);
-        if (there && lh == 0) a.stats[(static_cast<int64_t>(tm) * NWM + wm) * a.ldstat + row] = floatx2{m, s};
+        if (there && lane < 16) a.stats[(static_cast<int64_t>(tm) * NWM + wm) * a.ldstat + row] = floatx2{m, s};
         if (any_label) {
 #pragma unroll
           for (int x = 0; x < WM; ++x)
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
-              if (mine == x * 32 + 8 * (r >> 2) + 4 * lh + (r & 3)) a.zy[row] = z[x][r];
-        }
-      } else if constexpr (EPI == kGrad) {
-        // G, also of rows and classes that only fill up tiles: zeros
-        constexpr float kHold = STORE == GIST_STORE_F16 ? 32768.f : 1.f;
-        const bool used = there && row < real && label >= 0;
-        const float lse = used ? a.lse[row] : 0.f;
-        unsigned short* const g = static_cast<unsigned short*>(a.out) + row * a.ldo + mw + 8 * lh;
-#pragma unroll
-        for (int x = 0; x < WM; ++x) {
-          int u[4][2];
-#pragma unroll
-          for (int r4 = 0; r4 < 4; ++r4) {
-            float v[4];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              const int c = x * 32 + 8 * r4 + 4 * lh + q;
-              v[q] = ex2((z[x][4 * r4 + q] - lse) * kL);
-              if (any_label && mine == c) v[q] -= 1.f;
-              v[q] *= kHold;
-              if (!used || (edge && mw + c >= a.M)) v[q] = 0.f;
-            }
-            pack4<E8 ? static_cast<int>(GIST_STORE_BF16) : STORE>(v, u[r4]);
-          }
-          *reinterpret_cast<intx4*>(g + x * 32) = join8(u[0], u[1]);
-          *reinterpret_cast<intx4*>(g + x * 32 + 16) = join8(u[2], u[3]);
+            for (int r = 0; r < 4; ++r)
+              if (mine == x * 16 + g4 + r) a.zy[row] = acc[x][y][r];
         }
       }
     }
   } else if constexpr (EPI == kPart) {
 #pragma unroll
     for (int y = 0; y < WN; ++y) {
-      const int64_t row = n0 + (wn * WN + y) * 32 + li;
+      const int64_t row = n0 + (wn * WN + y) * 16 + li;
       if (row >= a.N) continue;
-      float* const o = static_cast<float*>(a.out) + (slice * a.N + row) * a.ldo + mw + 4 * lh;
+      float* const o = static_cast<float*>(a.out) + (slice * a.N + row) * a.ldo + mw + g4;
+#pragma unroll
+      for (int x = 0; x < WM; ++x) {
+        if (mw + x * 16 + g4 >= a.ldo) continue;    // ldo: a multiple of 4
+        floatx4* const p = reinterpret_cast<floatx4*>(o + x * 16);
+        floatx4 v = acc[x][y];
+        if (a.add) v += *p;
+        *p = v;
+      }
+    }
+  } else {
+    const float f = *a.factor;
+#pragma unroll
+    for (int y = 0; y < WN; ++y) {
+      const int64_t row = n0 + (wn * WN + y) * 16 + li;
+      const bool there = row < a.N;
+      if (a.row_factor) {
+        // a row that takes no part has factor 0, whatever its sums are; a row without a class in the
+        // table (a wrong label) has the other term alone
+        const float rf = there ? a.row_factor[row] : 0.f;
+        const int id = there ? a.ids[row] : -1;
+        const float g = id >= 0 ? a.pm1[row] : 0.f;
+#pragma unroll
+        for (int x = 0; x < WM; ++x) {
+          const int64_t c = mw + x * 16 + g4;
+          float t4[4] = {};
+          if (id >= 0 && c < a.RP) load4_16<OPS>(a.T + id * a.ldt, c, t4);   // RP: a multiple of 64
+#pragma unroll
+          for (int r = 0; r < 4; ++r) acc[x][y][r] = rf == 0.f ? 0.f : fmaf(g, t4[r], rf * acc[x][y][r]);
+        }
+      }
 #pragma unroll
       for (int x = 0; x < WM; ++x)
 #pragma unroll
-        for (int r4 = 0; r4 < 4; ++r4) {
-          const int c = x * 32 + 8 * r4;
-          if (mw + c + 4 * lh >= a.ldo) continue;    // ldo: a multiple of 4
-          floatx4 v{acc[x][y][4 * r4], acc[x][y][4 * r4 + 1], acc[x][y][4 * r4 + 2], acc[x][y][4 * r4 + 3]};
-          floatx4* const p = reinterpret_cast<floatx4*>(o + c);
-          if (a.add) v += *p;
-          *p = v;
+        for (int r = 0; r < 4; ++r) acc[x][y][r] *= f;
+      if (a.out_store == GIST_STORE_F32) {
+#pragma unroll
+        for (int x = 0; x < WM; ++x) {
+          const int64_t c = mw + x * 16 + g4;
+          const float v[4] = {acc[x][y][0], acc[x][y][1], acc[x][y][2], acc[x][y][3]};
+          if (there && c < a.M) store_some<GIST_STORE_F32, 4>(a.out, row * a.ldo + c, a.M - c, v);
         }
-    }
-  } else {
-    const float f0 = *a.factor;
+      } else {
 #pragma unroll
-    for (int y = 0; y < WN; ++y) {
-      const int64_t row = n0 + (wn * WN + y) * 32 + li;
-      const bool there = row < a.N;
-      const float rf = a.row_factor && there ? a.row_factor[row] : 1.f;
-      // a row that takes no part has factor 0, whatever its sums are; a row without a class in the
-      // table (a wrong label) has the other term alone
-      const int id = a.row_factor && there ? a.ids[row] : -1;
-      if (id >= 0 || rf == 0.f) {
-        const float g = id >= 0 ? a.pm1[row] : 0.f;
-#pragma unroll
-        for (int x = 0; x < WM; ++x)
-#pragma unroll
-          for (int r4 = 0; r4 < 4; ++r4) {
-            const int64_t c = mw + x * 32 + 8 * r4 + 4 * lh;
-            float t[4] = {};
-            if (id >= 0 && c < a.RP) load4_16<E8 ? static_cast<int>(GIST_STORE_BF16) : STORE>(a.T + id * a.ldt, c, t);   // RP: a multiple of 64
-#pragma unroll
-            for (int q = 0; q < 4; ++q) acc[x][y][4 * r4 + q] = rf == 0.f ? 0.f : fmaf(g, t[q], rf * acc[x][y][4 * r4 + q]);
-          }
-      } else if (a.row_factor) {
-#pragma unroll
-        for (int x = 0; x < WM; ++x) acc[x][y] *= rf;
-      }
-      const float f = f0;
-#pragma unroll
-      for (int x = 0; x < WM; ++x) {
-        if (a.out_store == GIST_STORE_F32) {
-#pragma unroll
-          for (int r4 = 0; r4 < 4; ++r4) {
-            const int64_t c = mw + x * 32 + 8 * r4 + 4 * lh;
-            float v[4];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) v[q] = acc[x][y][4 * r4 + q] * f;
-            if (there && c < a.M) store_some<GIST_STORE_F32, 4>(a.out, row * a.ldo + c, a.M - c, v);
-          }
-        } else {
-          int u[4][2];
-#pragma unroll
-          for (int r4 = 0; r4 < 4; ++r4) {
-            float v[4];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) v[q] = acc[x][y][4 * r4 + q] * f;
-            pack4<E8 ? static_cast<int>(GIST_STORE_BF16) : STORE>(v, u[r4]);
-          }
+        for (int x = 0; x < WM; x += 2) {
+          int w[2][2];
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const intx4 w = join8(u[2 * h], u[2 * h + 1]);
-            const int64_t c = mw + x * 32 + 16 * h + 8 * lh;
-            if (!there || c >= a.M) continue;
-            unsigned short* const o = static_cast<unsigned short*>(a.out) + row * a.ldo + c;
-            if (c + 8 <= a.M) {
-              *reinterpret_cast<intx4u*>(o) = w;
-            } else {
+            const float v[4] = {acc[x + h][y][0], acc[x + h][y][1], acc[x + h][y][2], acc[x + h][y][3]};
+            pack4<OPS>(v, w[h]);
+          }
+          const intx4 v = join8(w[0], w[1]);
+          const int64_t c = mw + x * 16 + col8(lane);
+          if (!there || c >= a.M) continue;
+          unsigned short* const o = static_cast<unsigned short*>(a.out) + row * a.ldo + c;
+          if (c + 8 <= a.M) {
+            *reinterpret_cast<intx4u*>(o) = v;
+          } else {
 #pragma unroll
-              for (int q = 0; q < 8; ++q)
-                if (c + q < a.M) o[q] = static_cast<unsigned short>(static_cast<unsigned>(w[q >> 1]) >> (16 * (q & 1)));
-            }
+            for (int q = 0; q < 8; ++q)
+              if (c + q < a.M) o[q] = static_cast<unsigned short>(static_cast<unsigned>(v[q >> 1]) >> (16 * (q & 1)));
           }
         }
       }
@@ -1088,17 +1098,17 @@ void launch_product(hipStream_t st, int tile, const Prod& a) {
   const dim3 grid(static_cast<unsigned>(static_cast<int64_t>(a.tiles_m) * a.tiles_n * a.slices));
   if constexpr (EPI != kPart && EPI != kOut) {
     if (tile == 32) {
-      hipLaunchKernelGGL((product_kernel<STORE, 2, 1, 4, 1, 4, PT, QT, EPI>), grid, dim3(256), 0, st, a);
+      hipLaunchKernelGGL((product_kernel<STORE, 4, 2, 4, 1, 4, PT, QT, EPI>), grid, dim3(256), 0, st, a);
       return;
     }
   }
   if constexpr (STORE != GIST_STORE_E4M3) {
     if (tile == 256) {
-      hipLaunchKernelGGL((product_kernel<STORE, 4, 2, 2, 4, 2, PT, QT, EPI>), grid, dim3(512), 0, st, a);
+      hipLaunchKernelGGL((product_kernel<STORE, 8, 4, 2, 4, 2, PT, QT, EPI>), grid, dim3(512), 0, st, a);
       return;
     }
   }
-  hipLaunchKernelGGL((product_kernel<STORE, 2, 2, 2, 2, 2, PT, QT, EPI>), grid, dim3(256), 0, st, a);
+  hipLaunchKernelGGL((product_kernel<STORE, 4, 4, 2, 2, 2, PT, QT, EPI>), grid, dim3(256), 0, st, a);
 }
 
 void set_cut(Prod& a, const Cut& c) {
