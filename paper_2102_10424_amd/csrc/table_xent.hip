@@ -53,6 +53,7 @@ constexpr int kBlock = 256;
 constexpr float kL = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr size_t kPieceBytes = size_t{256} << 20;   // G of one piece, or an fp32 piece's logits
 constexpr size_t kExpBytes = size_t{1} << 30;       // E of one piece
+constexpr int kNoSlot = INT32_MAX;
 constexpr float kFar = 30.f;                        // a row's largest logit above its reference
 constexpr size_t kPartBytes = size_t{64} << 20;     // fp32 partial results beyond one
 
@@ -110,6 +111,10 @@ struct Prod {
   const char* T;
   int64_t ldt;
   int out_store;
+  const int32_t* slots;       // kOut: or NULL; rows that have one go to rows[slot] instead, in fp32
+  float* rows;
+  const float* part;          // kOut: or NULL; added (both: leading dimension ldr)
+  int64_t ldr;
 };
 
 __device__ __forceinline__ void lds_barrier() {
@@ -434,12 +439,22 @@ __global__ __launch_bounds__(64 * NWM * NWN, NS == 2 ? 2 : 1) void product_kerne
       for (int x = 0; x < WM; ++x)
 #pragma unroll
         for (int r = 0; r < 4; ++r) acc[x][y][r] *= zs;
+      if constexpr (EPI == kStats || EPI == kExp) {
+        if (edge) {
+#pragma unroll
+          for (int x = 0; x < WM; ++x)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (mw + x * 16 + g4 + r >= a.M) acc[x][y][r] = -__builtin_inff();
+        }
+      }
+      float sum = 0.f, ref = 0.f;
       if constexpr (EPI != kStats) {
         // E, or G, also of rows and classes that only fill up tiles, and of rows without a label: zeros
         const bool used = there && row < real && label >= 0;
         constexpr bool kG = EPI == kGrad;
         constexpr float kHold = kG && STORE == GIST_STORE_F16 ? 32768.f : 1.f;
-        const float ref = used ? a.lse[row] : 0.f;
+        if (used) ref = a.lse[row];
         unsigned short* const g = static_cast<unsigned short*>(a.out) + row * a.ldo + mw + col8(lane);
 #pragma unroll
         for (int x = 0; x < WM; x += 2) {
@@ -451,6 +466,7 @@ __global__ __launch_bounds__(64 * NWM * NWN, NS == 2 ? 2 : 1) void product_kerne
             for (int r = 0; r < 4; ++r) {
               const int c = (x + h) * 16 + g4 + r;
               v[r] = ex2((acc[x + h][y][r] - ref) * kL);
+              if (EPI == kExp) sum += v[r];
               if (kG && any_label && mine == c) v[r] -= 1.f;
               v[r] *= kHold;
               if (!used || (edge && mw + c >= a.M)) v[r] = 0.f;
@@ -461,13 +477,6 @@ __global__ __launch_bounds__(64 * NWM * NWN, NS == 2 ? 2 : 1) void product_kerne
         }
       }
       if constexpr (EPI == kStats || EPI == kExp) {
-        if (edge) {
-#pragma unroll
-          for (int x = 0; x < WM; ++x)
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-              if (mw + x * 16 + g4 + r >= a.M) acc[x][y][r] = -__builtin_inff();
-        }
         float m = acc[0][y][0];
 #pragma unroll
         for (int x = 0; x < WM; ++x)
@@ -475,17 +484,24 @@ __global__ __launch_bounds__(64 * NWM * NWN, NS == 2 ? 2 : 1) void product_kerne
           for (int r = 0; r < 4; ++r) m = fmaxf(m, acc[x][y][r]);
         m = fmaxf(m, __shfl_xor(m, 16, 64));
         m = fmaxf(m, __shfl_xor(m, 32, 64));
-        const float ref = m == -__builtin_inff() ? 0.f : m;
-        float s = 0.f;
+        // The sum by E's exponentials, where these are neither too large nor all too small to be told
+        // from zero; else by exponentials of their own.
+        if (EPI == kStats || __any(!(fabsf(m - ref) < kFar))) {
+          ref = m == -__builtin_inff() ? 0.f : m;
+          sum = 0.f;
 #pragma unroll
-        for (int x = 0; x < WM; ++x) {
-          float p[4];
+          for (int x = 0; x < WM; ++x) {
+            float p[4];
 #pragma unroll
-          for (int r = 0; r < 4; ++r) p[r] = ex2((acc[x][y][r] - ref) * kL);
-          s += (p[0] + p[1]) + (p[2] + p[3]);
+            for (int r = 0; r < 4; ++r) p[r] = ex2((acc[x][y][r] - ref) * kL);
+            sum += (p[0] + p[1]) + (p[2] + p[3]);
+          }
         }
-        s += __shfl_xor(s, 16, 64);
-        s += __shfl_xor(s, 32, 64);
+        sum += __shfl_xor(sum, 16, 64);
+        sum += __shfl_xor(sum, 32, 64);
+        // kept relative to the largest
+        if (EPI == kExp) sum *= ex2((ref - (m == -__builtin_inff() ? 0.f : m)) * kL);
+        const float s = sum;
         if (there && lane < 16) a.stats[(static_cast<int64_t>(tm) * NWM + wm) * a.ldstat + row] = floatx2{m, s};
         if (any_label) {
 #pragma unroll
@@ -532,6 +548,20 @@ __global__ __launch_bounds__(64 * NWM * NWN, NS == 2 ? 2 : 1) void product_kerne
           for (int r = 0; r < 4; ++r) acc[x][y][r] = rf == 0.f ? 0.f : fmaf(g, t4[r], rf * acc[x][y][r]);
         }
       }
+      bool there_out = there;
+      if constexpr (QT) {
+        const int slot = a.slots && there ? a.slots[row] : kNoSlot;
+        if (a.part || slot != kNoSlot) {
+          there_out = there && slot == kNoSlot;
+#pragma unroll
+          for (int x = 0; x < WM; ++x) {
+            const int64_t c = mw + x * 16 + g4;
+            if (!there || c >= a.ldr) continue;    // ldr: a multiple of 4
+            if (a.part) acc[x][y] += *reinterpret_cast<const floatx4*>(a.part + row * a.ldr + c);
+            if (slot != kNoSlot) *reinterpret_cast<floatx4*>(a.rows + slot * a.ldr + c) = acc[x][y];
+          }
+        }
+      }
 #pragma unroll
       for (int x = 0; x < WM; ++x)
 #pragma unroll
@@ -541,7 +571,7 @@ __global__ __launch_bounds__(64 * NWM * NWN, NS == 2 ? 2 : 1) void product_kerne
         for (int x = 0; x < WM; ++x) {
           const int64_t c = mw + x * 16 + g4;
           const float v[4] = {acc[x][y][0], acc[x][y][1], acc[x][y][2], acc[x][y][3]};
-          if (there && c < a.M) store_some<GIST_STORE_F32, 4>(a.out, row * a.ldo + c, a.M - c, v);
+          if (there_out && c < a.M) store_some<GIST_STORE_F32, 4>(a.out, row * a.ldo + c, a.M - c, v);
         }
       } else {
 #pragma unroll
@@ -554,7 +584,7 @@ __global__ __launch_bounds__(64 * NWM * NWN, NS == 2 ? 2 : 1) void product_kerne
           }
           const intx4 v = join8(w[0], w[1]);
           const int64_t c = mw + x * 16 + col8(lane);
-          if (!there || c >= a.M) continue;
+          if (!there_out || c >= a.M) continue;
           unsigned short* const o = static_cast<unsigned short*>(a.out) + row * a.ldo + c;
           if (c + 8 <= a.M) {
             *reinterpret_cast<intx4u*>(o) = v;
@@ -698,7 +728,7 @@ __global__ __launch_bounds__(1024) void join_stats_kernel(int64_t row0, int64_t 
 __global__ __launch_bounds__(kBlock) void given_kernel(int64_t row0, int64_t n, int64_t C, const float* __restrict__ logp,
                                                        const int32_t* __restrict__ labels, const int32_t* __restrict__ n_dev,
                                                        unsigned short* __restrict__ E, int64_t ldE, float* __restrict__ pm1,
-                                                       int32_t* __restrict__ ids) {
+                                                       int32_t* __restrict__ ids, int* __restrict__ slots) {
   const int64_t row = blockIdx.x * static_cast<int64_t>(kBlock) + threadIdx.x;
   if (row >= n) return;
   const int y = !n_dev || row0 + row < *n_dev ? labels[row] : -1;
@@ -706,16 +736,45 @@ __global__ __launch_bounds__(kBlock) void given_kernel(int64_t row0, int64_t n, 
   if (live) E[row * ldE + y] = 0;
   pm1[row] = live ? expm1f(logp[row]) : 0.f;
   ids[row] = live ? y : -1;
+  if (slots && live) atomicMin(slots + y, static_cast<int>(row));   // a class's slot: the first of its rows
 }
 
-// Y = rows of H times p - 1, in fp32; eight elements a thread.
+__global__ __launch_bounds__(kBlock) void no_slots_kernel(int64_t C, int* __restrict__ slots) {
+  const int64_t c = blockIdx.x * static_cast<int64_t>(kBlock) + threadIdx.x;
+  if (c < C) slots[c] = kNoSlot;
+}
+
+// The rows that have been kept in fp32, by the first of a class's rows: rounded to the gradient's store.
+template <int STORE>
+__global__ __launch_bounds__(kBlock) void given_out_kernel(int64_t n, int d, const int32_t* __restrict__ ids,
+                                                           const int32_t* __restrict__ slot_ids, const float* __restrict__ rows,
+                                                           int64_t ldr, const float* __restrict__ factor, void* __restrict__ out,
+                                                           int64_t ldo) {
+  const int64_t row = blockIdx.x;
+  if (slot_ids[row] != row) return;
+  const float f = *factor;
+  const int64_t o = static_cast<int64_t>(ids[row]) * ldo;
+  for (int c = threadIdx.x * 4; c < d; c += kBlock * 4) {
+    const floatx4 v = *reinterpret_cast<const floatx4*>(rows + row * ldr + c);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const float x[1] = {v[q] * f};
+      if (c + q < d) store_as<STORE, 1>(out, o + c + q, x);
+    }
+  }
+}
+
+// Y = rows of H times p - 1, in fp32; eight elements a thread.  With slots, also every row's.
 __global__ __launch_bounds__(kBlock) void given_rows_kernel(int64_t n, int64_t wide, const char* __restrict__ H, int64_t ldh,
-                                                            const float* __restrict__ pm1, float* __restrict__ Y) {
+                                                            const float* __restrict__ pm1, float* __restrict__ Y,
+                                                            const int32_t* __restrict__ ids, const int* __restrict__ slots,
+                                                            int32_t* __restrict__ slot_ids) {
   const int64_t per = wide / 8;
   for (int64_t e = blockIdx.x * static_cast<int64_t>(kBlock) + threadIdx.x; e < n * per;
        e += static_cast<int64_t>(gridDim.x) * kBlock) {
     const int64_t row = e / per, c = (e - row * per) * 8;
     const float f = pm1[row];
+    if (slots && c == 0) slot_ids[row] = ids[row] >= 0 ? slots[ids[row]] : -1;
     float h[8];
     load_vec<GIST_STORE_BF16, 8>(H + row * ldh, c, h);
 #pragma unroll
@@ -995,8 +1054,8 @@ struct Plan {
   Cut dh, dt;               // the gradients' products, of the first piece
   bool exps;                // rows piece by piece, by their exponentials
   bool parts_h;             // dH is summed in fp32 parts
-  size_t h, hm, t, stats, zy, lse, logp, factor, g, ref, row_factor, far, pm1, ids, y, embed, part,
-      z, gemm, total;
+  size_t h, hm, t, stats, zy, lse, logp, factor, g, ref, row_factor, far, pm1, ids, y, embed, slots,
+      slot_ids, kept, part, z, gemm, total;
   size_t gemm_bytes;
 };
 
@@ -1069,12 +1128,18 @@ Plan plan_of(const gist_table_xent_desc* D, const void* H, const void* T, bool g
     p.dh = cut_of(d, rn, static_cast<int>(up(C, 64) / 64));
     p.dt = cut_of(d, C, static_cast<int>(up(rn, 64) / 64));
     p.parts_h = p.dh.slices > 1;
+    const bool parts_t = p.dt.slices > 1 || rn < n;
     p.part = take((p.parts_h ? static_cast<size_t>(p.dh.slices) * rn * ldp * 4 : 0) +
-                  static_cast<size_t>(p.dt.slices) * C * ldp * 4);
+                  (parts_t ? static_cast<size_t>(p.dt.slices) * C * ldp * 4 : 0));
+    if (p.dt.slices == 1) {
+      p.slots = take(static_cast<size_t>(C) * 4);
+      p.slot_ids = take(static_cast<size_t>(rn) * 4);
+      p.kept = take(static_cast<size_t>(rn) * ldp * 4);
+    }
     p.pm1 = take(static_cast<size_t>(rn) * 4);
     p.ids = take(static_cast<size_t>(rn) * 4);
     p.y = take(static_cast<size_t>(rn) * p.wide * 4);
-    p.embed = take(embed_grad_workspace(rn, C, d));
+    p.embed = take(std::max(embed_grad_workspace(rn, C, d), embed_grad_workspace(rn, rn, d)));   // serves fewer ids
   } else if (grad) {
     p.n_pad = up(n, 256);
     const int64_t fit = static_cast<int64_t>(kPieceBytes / 2) / p.n_pad / 256 * 256;
@@ -1229,10 +1294,20 @@ gist_status run16(hipStream_t st, const gist_table_xent_desc* D, const Plan& p, 
         launch_product<STORE, kAgain, false, false>(st, c.tile, a);
         GIST_LAUNCHED("table_xent_again");
       }
+      // The last piece's product writes dT where it is not cut; before, and where it is, parts are kept.
+      const bool straight = p.dt.slices == 1 && r0 + rn == n;
+      int* const slots = straight ? reinterpret_cast<int*>(w + p.slots) : nullptr;
+      int32_t* const slot_ids = reinterpret_cast<int32_t*>(w + p.slot_ids);
+      if (straight) {
+        ProfScope ps(st, "table_xent_slots", 0.0, 4.0 * C);
+        hipLaunchKernelGGL(no_slots_kernel, dim3(static_cast<unsigned>((C + kBlock - 1) / kBlock)), dim3(kBlock), 0, st, C, slots);
+        GIST_LAUNCHED("table_xent_slots");
+      }
       {
         ProfScope ps(st, "table_xent_given", 0.0, 18.0 * rn);
         hipLaunchKernelGGL(given_kernel, dim3(static_cast<unsigned>((rn + kBlock - 1) / kBlock)), dim3(kBlock), 0, st, r0, rn, C,
-                           f32(p.logp) + r0, a.labels, n_dev, reinterpret_cast<unsigned short*>(w + p.g), p.Cp, pm1, ids);
+                           f32(p.logp) + r0, a.labels, n_dev, reinterpret_cast<unsigned short*>(w + p.g), p.Cp, pm1, ids,
+                           slots);
         GIST_LAUNCHED("table_xent_given");
       }
       // the rows of H times their factors, zeros behind the last
@@ -1295,23 +1370,48 @@ gist_status run16(hipStream_t st, const gist_table_xent_desc* D, const Plan& p, 
         b.len = (b.steps + b.slices - 1) / b.slices;
         b.slices = (b.steps + b.len - 1) / b.len;   // no more than the first piece's
         ProfScope ps(st, "table_xent_dt", 2.0 * rn * C * d, moved + static_cast<double>(rn + C) * d * e);
-        b.out = part_t;
-        b.ldo = ldp;
-        b.add = r0 > 0;
-        launch_product<STORE, kPart, true, true>(st, p.dt.tile, b);
+        if (straight) {
+          b.out = dT;
+          b.ldo = D->lddt;
+          b.factor = f32(p.factor);
+          b.out_store = D->store;
+          b.slots = slots;
+          b.rows = f32(p.kept);
+          b.part = r0 > 0 ? part_t : nullptr;
+          b.ldr = ldp;
+          launch_product<STORE, kOut, true, true>(st, p.dt.tile, b);
+        } else {
+          b.out = part_t;
+          b.ldo = ldp;
+          b.add = r0 > 0;
+          launch_product<STORE, kPart, true, true>(st, p.dt.tile, b);
+        }
         GIST_LAUNCHED("table_xent_dt");
       }
       {   // and the given classes' rows of H, times p - 1
         float* const Y = f32(p.y);
         {
           ProfScope ps(st, "table_xent_given_rows", 0.0, 6.0 * rn * d);
-          hipLaunchKernelGGL(given_rows_kernel, dim3(grid_of(rn * p.wide / 8)), dim3(kBlock), 0, st, rn, p.wide, a.Q, ldh, pm1, Y);
+          hipLaunchKernelGGL(given_rows_kernel, dim3(grid_of(rn * p.wide / 8)), dim3(kBlock), 0, st, rn, p.wide, a.Q, ldh, pm1, Y,
+                             ids, slots, slot_ids);
           GIST_LAUNCHED("table_xent_given_rows");
         }
-        const gist_status s = embed_grad(st, rn, C, d, ids, 1.f, Y, p.wide, true, -1.f, part_t, ldp, w + p.embed);
+        const gist_status s =
+            straight ? embed_grad(st, rn, p.rows, d, slot_ids, 1.f, Y, p.wide, true, -1.f, f32(p.kept), ldp, w + p.embed)
+                     : embed_grad(st, rn, C, d, ids, 1.f, Y, p.wide, true, -1.f, part_t, ldp, w + p.embed);
         if (s != GIST_OK) return s;
       }
-      if (r0 + rn == n) {
+      if (straight) {
+        ProfScope ps(st, "table_xent_given_out", 0.0, 6.0 * rn * d);
+        const dim3 grid(static_cast<unsigned>(rn));
+        if (D->store == GIST_STORE_F32)
+          hipLaunchKernelGGL(given_out_kernel<GIST_STORE_F32>, grid, dim3(kBlock), 0, st, rn, d, ids, slot_ids, f32(p.kept), ldp,
+                             f32(p.factor), dT, D->lddt);
+        else
+          hipLaunchKernelGGL(given_out_kernel<STORE>, grid, dim3(kBlock), 0, st, rn, d, ids, slot_ids, f32(p.kept), ldp,
+                             f32(p.factor), dT, D->lddt);
+        GIST_LAUNCHED("table_xent_given_out");
+      } else if (r0 + rn == n) {
         ProfScope ps(st, "table_xent_dt_join", 0.0, 4.0 * p.dt.slices * C * ldp);
         join_out<STORE>(st, D, C, p.dt.slices, C * ldp, part_t, f32(p.factor), Given{}, dT, D->lddt);
         GIST_LAUNCHED("table_xent_dt_join");
