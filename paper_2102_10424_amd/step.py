@@ -13,6 +13,10 @@ context's stream (torch only provides the device buffers).
   sub-GCN, with SGD or Adam (the optimizer of the paper's experiments).
 * :class:`LearnedRows` -- a trained table in place of given features: the
   lookup of a mini-batch's rows and the SGD step on them.
+* :class:`TableHead` -- a table of class vectors in place of the last layer's
+  logits: norm (with the residual's addition), loss and gradients.
+* :class:`AdamW` -- one AdamW step over a list of tensors, moments in fp32 or in
+  8 bits.
 """
 
 import numpy as np
@@ -1130,15 +1134,40 @@ class SubGCN:
         G.gist_log_probs_bwd(self.ctx, n, C, self.H[self.L], C, G.GIST_STORE_F32, batch.labels,
                              self.lp["lse"], self.lp["entropy"], g_logp, g_entropy, self.dlogits, C)
 
-    def step(self, batch, params, lr, adam=None, loss_out=None, muon=None):
+    def adamw(self, params, head=None, weight_decay=0.01, eight=False):
+        """An :class:`AdamW` over ``params`` (GAT: the attention vectors without decay) and, with
+        ``head``, its table and gain, which is not decayed."""
+        items = []
+        for l in range(self.L):
+            r = self.widths[l] if self.gat else params[l].shape[0]
+            items.append(dict(W=params[l][:r], dW=self.dW[l][:r], weight_decay=weight_decay))
+            if self.gat:
+                items.append(dict(W=params[l][r:], dW=self.dW[l][r:]))
+        if head is not None:
+            items += head.items(weight_decay)
+        return AdamW(self.ctx, items, eight=eight, device=self.device)
+
+    def step(self, batch, params, lr, adam=None, loss_out=None, muon=None, adamw=None, head=None,
+             residual=None):
         """``subTrain``: forward, loss, backward, update (all enqueued, nothing
         synced).  ``adam`` = (M, V, step, fresh) selects Adam, ``muon`` = (M,
-        fresh) Muon, else SGD; both are refused (ValueError)."""
-        if adam is not None and muon is not None:
-            raise ValueError("one optimizer a step: adam or muon")
+        fresh) Muon, ``adamw`` = (optimizer of :meth:`adamw`, step) AdamW, else SGD; more than
+        one is refused (ValueError).  With ``head`` the loss is that :class:`TableHead`'s
+        (``residual``: rows added to the last layer's output), whose table and gain AdamW
+        steps and the other optimizers leave as they are."""
+        if sum(o is not None for o in (adam, muon, adamw)) > 1:
+            raise ValueError("one optimizer a step: adam, muon or adamw")
         self.forward(batch, params)
-        self.loss_and_grad(batch, loss_out)
-        if muon is not None:
+        if head is None:
+            if residual is not None:
+                raise ValueError("a residual goes with a head")
+            self.loss_and_grad(batch, loss_out)
+        else:
+            head.loss_and_grad(self, batch, residual, loss_out)
+        if adamw is not None:
+            self.backward(batch, params)
+            adamw[0].step(lr, adamw[1])
+        elif muon is not None:
             self.backward(batch, params)
             self.muon(params, muon[0], lr, muon[1])
         elif adam is None:
@@ -1190,6 +1219,196 @@ class LearnedRows:
         self._reserve(n)
         G.gist_embed_grad_sgd(self.ctx, n, self.N, self.d, ids, self.scale, dX, self.d, lr,
                               self.table, self.d, self.ws)
+
+
+_STORE = {torch.float32: G.GIST_STORE_F32, torch.bfloat16: G.GIST_STORE_BF16,
+          torch.float16: G.GIST_STORE_F16}
+
+
+class AdamW:
+    """One AdamW step (``gist_adamw_update``) over a list of tensors.  ``items``: dicts of ``W``
+    (fp32), ``dW`` (fp32, bf16 or fp16), and optionally ``weight_decay`` and ``copy`` (bf16 or fp16:
+    the new weights, rounded).  Moments are fp32, or with ``eight`` in 8 bits (``state``: per
+    tensor (m, v) or (m, v, m_scale, v_scale), zero at first).  Arrays of another type, with
+    gaps or of another size are refused (ValueError)."""
+
+    def __init__(self, ctx, items, eight=False, device="cuda"):
+        self.ctx, self.eight = ctx, eight
+        self.state, self._keep, tensors = [], [], []
+        for i, it in enumerate(items):
+            W, dW, copy = it["W"], it["dW"], it.get("copy")
+            n = W.numel()
+            _check_array(f"W[{i}]", W, torch.float32, n)
+            if dW.dtype not in _STORE or dW.numel() != n or not dW.is_contiguous():
+                raise ValueError(f"dW[{i}] must be a contiguous fp32, bf16 or fp16 tensor of {n}")
+            if copy is not None and (copy.dtype not in _STORE or copy.dtype == torch.float32
+                                     or copy.numel() != n or not copy.is_contiguous()):
+                raise ValueError(f"copy[{i}] must be a contiguous bf16 or fp16 tensor of {n}")
+            if eight:
+                nb = -(-n // G.GIST_ADAMW_BLOCK)
+                st = tuple(torch.zeros(n, dtype=torch.uint8, device=device) for _ in range(2)) + \
+                    tuple(torch.zeros(nb, device=device) for _ in range(2))
+            else:
+                st = tuple(torch.zeros(n, device=device) for _ in range(2))
+            self.state.append(st)
+            self._keep.append((W, dW, copy))
+            tensors.append(G.adamw_tensor(
+                W, dW, st[0], st[1], n, it.get("weight_decay", 0.0), _STORE[dW.dtype],
+                st[2] if eight else None, st[3] if eight else None, copy,
+                G.GIST_STORE_BF16 if copy is None else _STORE[copy.dtype]))
+        self.tensors = G.adamw_tensors(tensors)
+
+    def step(self, lr, step, betas=(0.9, 0.999), eps=1e-8, fresh=False, grad_scale=1.0, seed=None):
+        """Step number ``step`` (from 1); ``fresh`` takes the moments as zero, ``seed`` (default: the
+        step) draws the 8-bit moments' rounding."""
+        G.gist_adamw_update(self.ctx, self.tensors, lr, step, betas[0], betas[1], eps,
+                            G.GIST_ADAM_FRESH if fresh else 0, grad_scale,
+                            step if seed is None else seed)
+
+    def step_dev(self, coef_dev, betas=(0.9, 0.999), eps=1e-8):
+        """The same with ``gist_adamw_coefficients`` read from device memory: what a recorded step
+        uses."""
+        G.gist_adamw_update_dev(self.ctx, self.tensors, coef_dev, betas[0], betas[1], eps)
+
+
+class TableHead:
+    """Class vectors (``table``: C x d fp32 on the device, as :class:`LearnedRows` has them, so the
+    two may be one) in place of the last layer's logits: the rows that leave a ``SubGCN`` of
+    output width d, plus a residual, are normed (gain: ``gain``, ones at first) and
+    scored against the table, ``loss_and_grad`` taking the place of the runner's own.
+
+    ``dtype``: torch.float32 (``product`` GIST_DTYPE_F32 or GIST_DTYPE_BF16_IN), or bfloat16 or
+    float16: the normed rows, the table's copy ``table16`` and the gradients ``dT`` are held
+    so, and the gradients times ``grad_scale``.  ``scale`` multiplies the logits.
+    After a call: ``loss``, ``logp``, ``lse``, and after :meth:`loss_and_grad` ``dT`` and
+    ``dgain`` (both times grad_scale) and the runner's ``dlogits`` (as they are).  Arrays of another
+    type, with gaps or too short are refused (ValueError)."""
+
+    def __init__(self, ctx, table, n_cap=0, dtype=torch.float32, product=G.GIST_DTYPE_F32, scale=1.0,
+                 grad_scale=1.0, eps=1e-6, device="cuda"):
+        if table.dim() != 2:
+            raise ValueError("the table is a matrix")
+        if dtype not in _STORE:
+            raise ValueError("dtype is float32, bfloat16 or float16")
+        if not grad_scale > 0:
+            raise ValueError("grad_scale is positive")
+        _check_array("the table", table, torch.float32, 0)
+        self.ctx, self.table, self.device = ctx, table, device
+        self.C, self.d = table.shape
+        self.dtype, self.store, self.product = dtype, _STORE[dtype], product
+        self.scale, self.grad_scale, self.eps = float(scale), float(grad_scale), float(eps)
+        self.gain = torch.ones(self.d, device=device)
+        self.dgain = torch.empty(self.d, device=device)
+        self.table16 = None if dtype == torch.float32 else table.to(dtype)
+        self.dT = torch.empty(self.C, self.d, dtype=dtype, device=device)
+        self.t8 = self.ts = None
+        self._gain = torch.empty(self.d, device=device)
+        self._zero = torch.zeros(1, dtype=torch.int32, device=device)
+        self.loss = torch.zeros(1, device=device)
+        self.n_cap, self.ws, self.b = 0, {}, None
+        self._kept = []        # outgrown buffers that a recorded step may still use
+        if n_cap:
+            self._reserve(n_cap)
+
+    def items(self, weight_decay=0.0):
+        """The table and the gain for :class:`AdamW`; a 16-bit table's copy is kept in step."""
+        return [dict(W=self.table, dW=self.dT, weight_decay=weight_decay, copy=self.table16),
+                dict(W=self.gain, dW=self.dgain)]
+
+    def _reserve(self, n):
+        if n > self.n_cap:
+            self._kept.append(self.b)
+            self.n_cap = n = max(n, 2 * self.n_cap)     # what is kept adds up to less than what is in use
+            f = lambda *s, t=torch.float32: torch.empty(*s, dtype=t, device=self.device)
+            self.b = dict(h=f(n, self.d), y=f(n, self.d, t=self.dtype), dy=f(n, self.d, t=self.dtype),
+                          rstd=f(n), logp=f(n), lse=f(n), y8=f(n, self.d, t=torch.uint8), ys=f(n),
+                          norm_ws=f(max(16, G.gist_rms_norm_bwd_workspace(n, self.d)), t=torch.uint8))
+        return self.b
+
+    def _desc(self, n, store):
+        return G.table_xent_desc(n, self.C, self.d, store, self.product, self.scale, self.grad_scale)
+
+    def _workspace(self, desc, gradients):
+        """One for calls with gradients and one for calls without; a larger one replaces it."""
+        need = max(16, G.gist_table_xent_workspace(desc, gradients))
+        ws = self.ws.get(gradients)
+        if ws is None or ws.numel() < need:
+            self._kept.append(ws)
+            ws = self.ws[gradients] = torch.empty(need, dtype=torch.uint8, device=self.device)
+        return ws
+
+    def prepare(self, n, gradients=True):
+        """Allocate every buffer a call on ``n`` rows needs (before a capture)."""
+        self._reserve(n)
+        if n:
+            self._workspace(self._desc(n, self.store), gradients)
+
+    def _rows(self, run, batch, residual):
+        n = batch.rows(run.L)
+        if run.widths[-1] != self.d:
+            raise ValueError(f"the runner's output width is not the table's {self.d}")
+        if residual is not None:
+            _check_array("residual", residual, torch.float32, n, self.d)
+        _check_array("labels", batch.labels, torch.int32, n)
+        return n, run.H[run.L]
+
+    def _norm(self, n, x, residual, y, store, scales):
+        b = self.b
+        G.gist_rms_norm(self.ctx, n, self.d, x, self.d, residual, self.d, G.GIST_STORE_F32, self.gain,
+                        self.eps, b["h"] if residual is not None else None, self.d, y, self.d, store,
+                        scales, b["rstd"])
+
+    def loss_and_grad(self, run, batch, residual=None, loss_out=None):
+        """In place of ``run.loss_and_grad`` after its forward pass: the loss (into ``loss_out``, a
+        one-element device tensor, or ``loss``), ``run.dlogits``, which is the residual's gradient
+        as well, ``dT`` and ``dgain``.  Rows behind a padded batch's real ones (``n_dev``) and rows
+        with a negative label take no part."""
+        n, x = self._rows(run, batch, residual)
+        b = self._reserve(n)
+        d, st = self.d, self.store
+        self._norm(n, x, residual, b["y"], st, None)
+        desc = self._desc(n, st)
+        G.gist_table_xent(self.ctx, desc, b["y"], None,
+                          self.table if self.table16 is None else self.table16, None, batch.labels,
+                          getattr(batch, "n_dev", None), self.loss if loss_out is None else loss_out,
+                          b["logp"], b["lse"], b["dy"], self.dT, self._workspace(desc, True))
+        gain = self.gain
+        if self.grad_scale != 1.0:
+            # the rows' gradient is linear in the gain, the gain's does not depend on it: with
+            # gain / grad_scale the first comes out as it is, the second times grad_scale
+            G.gist_embed_lookup(self.ctx, 1, 1, d, gain, d, G.GIST_STORE_F32, self._zero,
+                                1.0 / self.grad_scale, self._gain, d)
+            gain = self._gain
+        G.gist_rms_norm_bwd(self.ctx, n, d, b["dy"], d, st, x if residual is None else b["h"], d,
+                            G.GIST_STORE_F32, gain, b["rstd"], None, d, run.dlogits, d, self.dgain,
+                            b["norm_ws"])
+        self.logp, self.lse = b["logp"][:n], b["lse"][:n]
+
+    def quantise(self):
+        """The table in 8 bits for :meth:`score`; again after the table has changed."""
+        if self.t8 is None:
+            self.t8 = torch.empty(self.C, self.d, dtype=torch.uint8, device=self.device)
+            self.ts = torch.empty(self.C, device=self.device)
+        G.gist_quantize_rows(self.ctx, self.C, self.d, self.table, self.d, G.GIST_STORE_F32, self.t8,
+                             self.d, self.ts)
+
+    def score(self, run, batch, residual=None, eight=False):
+        """Without gradients: ``loss`` and, as device tensors that the next call reuses, the labels'
+        log probabilities and the rows' log-sum-exp.  ``eight``: rows and table (:meth:`quantise`)
+        in 8 bits."""
+        n, x = self._rows(run, batch, residual)
+        if eight and self.t8 is None:
+            raise ValueError("quantise the table first")
+        b = self._reserve(n)
+        st = G.GIST_STORE_E4M3 if eight else self.store
+        self._norm(n, x, residual, b["y8"] if eight else b["y"], st, b["ys"] if eight else None)
+        desc = self._desc(n, st)
+        T = self.t8 if eight else self.table if self.table16 is None else self.table16
+        G.gist_table_xent(self.ctx, desc, b["y8"] if eight else b["y"], b["ys"] if eight else None, T,
+                          self.ts if eight else None, batch.labels, getattr(batch, "n_dev", None),
+                          self.loss, b["logp"], b["lse"], None, None, self._workspace(desc, False))
+        self.logp, self.lse = b["logp"][:n], b["lse"][:n]
+        return dict(loss=self.loss, logp=self.logp, lse=self.lse)
 
 
 class SubGCNBatch:

@@ -243,3 +243,87 @@ def test_random_bits_are_uniform():
         assert abs(x.mean() - 32767.5) < 6 * 65536 / np.sqrt(12 * 65536)
     assert abs(np.corrcoef(a, b)[0, 1]) < 6 / 256
     assert abs(np.corrcoef(a[1:], a[:-1])[0, 1]) < 6 / 256
+
+
+# ---- the runners' own checks ---------------------------------------------------------
+class CpuBatch:
+    """Sizes and labels of a mini-batch without matrices: no library call is made on it."""
+
+    def __init__(self, n):
+        import torch
+        self.n, self.nnz, self.X = n, n, torch.zeros(n, 8)
+        self.labels = torch.zeros(n, dtype=torch.int32)
+
+    def rows(self, l):
+        return self.n
+
+    def adj(self, l):
+        return None, None
+
+
+def test_adamw_checks_its_arrays():
+    import torch
+    from paper_2102_10424_amd import step as S
+    W, g = torch.zeros(6, 4), torch.zeros(6, 4)
+    for bad in (dict(W=W.double()), dict(W=W[:, :3]), dict(W=W.t()), dict(dW=g.double()),
+                dict(dW=g[:5]), dict(dW=torch.zeros(6, 8)[:, :4]), dict(copy=torch.zeros(6, 4)),
+                dict(copy=torch.zeros(5, 4, dtype=torch.bfloat16))):
+        with pytest.raises(ValueError):
+            S.AdamW(None, [dict(dict(W=W, dW=g), **bad)], device="cpu")
+    o = S.AdamW(None, [dict(W=W, dW=g.half(), copy=torch.zeros(24, dtype=torch.float16))], eight=True, device="cpu")
+    assert [t.numel() for t in o.state[0]] == [24, 24, 1, 1]
+    assert S.AdamW(None, [], device="cpu").step is not None
+
+
+def test_table_head_checks_its_arrays(monkeypatch):
+    import torch
+    from paper_2102_10424_amd import step as S
+    calls = []
+    for name in ("gist_rms_norm", "gist_rms_norm_bwd", "gist_table_xent", "gist_quantize_rows", "gist_gcn_layer_fwd"):
+        monkeypatch.setattr(S.G, name, lambda *a, name=name: calls.append(name))
+    T = torch.zeros(50, 5)
+    for bad in (T.double(), T[:, :4], T.t(), torch.zeros(250)):
+        with pytest.raises(ValueError):
+            S.TableHead(None, bad, device="cpu")
+    for kw in (dict(dtype=torch.float64), dict(grad_scale=0.0), dict(grad_scale=float("nan"))):
+        with pytest.raises(ValueError):
+            S.TableHead(None, T, device="cpu", **kw)
+    head = S.TableHead(None, T, device="cpu")
+    run, other = S.SubGCN(None, "gcn", [8, 24, 5], 16, device="cpu"), S.SubGCN(None, "gcn", [8, 24, 6], 16, device="cpu")
+    b = CpuBatch(16)
+    run.forward(b, [torch.zeros(8, 24), torch.zeros(24, 5)])
+    calls.clear()
+    with pytest.raises(ValueError):
+        head.loss_and_grad(other, b)
+    for res in (torch.zeros(16, 4), torch.zeros(15, 5), torch.zeros(16, 5).double(), torch.zeros(16, 10)[:, :5]):
+        with pytest.raises(ValueError):
+            head.loss_and_grad(run, b, res)
+    with pytest.raises(ValueError):
+        head.score(run, b, eight=True)
+    b.labels = b.labels.long()
+    with pytest.raises(ValueError):
+        head.loss_and_grad(run, b)
+    assert not calls
+    b.labels = b.labels.int()
+    head.loss_and_grad(run, b, torch.zeros(16, 5))
+    head.quantise()
+    head.score(run, b, eight=True)
+    assert calls == ["gist_rms_norm", "gist_table_xent", "gist_rms_norm_bwd", "gist_quantize_rows", "gist_rms_norm", "gist_table_xent"]
+    with pytest.raises(ValueError):
+        run.step(b, [], 0.1, adam=(1, 2, 3, 4), adamw=(None, 1))
+    with pytest.raises(ValueError):
+        run.step(b, [torch.zeros(8, 24), torch.zeros(24, 5)], 0.1, residual=b.X)
+
+
+def test_table_head_keeps_outgrown_buffers():
+    """A recorded step keeps the addresses of the buffers it was recorded with."""
+    import weakref
+    import torch
+    from paper_2102_10424_amd import step as S
+    head = S.TableHead(None, torch.zeros(50, 5), n_cap=16, device="cpu")
+    head.prepare(16)
+    refs = [weakref.ref(t) for t in head.b.values()] + [weakref.ref(head.ws[True])]
+    head.prepare(17)
+    head.prepare(5000)
+    assert all(r() is not None for r in refs) and head.n_cap >= 5000
+    assert head.ws[True].numel() >= S.G.gist_table_xent_workspace(head._desc(5000, head.store), True)
