@@ -60,13 +60,13 @@ constexpr size_t kPartBytes = size_t{64} << 20;     // fp32 partial results beyo
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef short short4v __attribute__((ext_vector_type(4)));
-typedef short short8v __attribute__((ext_vector_type(8)));
 typedef int intx4 __attribute__((ext_vector_type(4)));
 typedef int intx8 __attribute__((ext_vector_type(8)));
 typedef float floatx2 __attribute__((ext_vector_type(2)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 typedef int intx4u __attribute__((ext_vector_type(4), aligned(2)));
+typedef int intx4w __attribute__((ext_vector_type(4), aligned(4)));
 typedef float floatx4u __attribute__((ext_vector_type(4), aligned(4)));
 
 __device__ __forceinline__ float ex2(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -602,14 +602,12 @@ __global__ __launch_bounds__(64 * NWM * NWN, NS == 2 ? 2 : 1) void product_kerne
 // ---- around the products ------------------------------------------------------------------
 
 // Rows of any store as 16-bit rows (or bytes as bytes) of `wide` elements, zeros behind d and behind
-// n; with labels, rows that are not labelled are zero; with factors, rows times theirs (0: zero,
-// whatever they hold).  Eight elements a thread.
+// n; with labels, rows that are not labelled are zero.  Eight elements a thread.
 template <int SRC, int DST>
 __global__ __launch_bounds__(kBlock) void copy_rows_kernel(int64_t n, int64_t n_pad, int d, int wide, const void* __restrict__ x,
                                                            int64_t ldx, void* __restrict__ y,
                                                            const int32_t* __restrict__ labels,
-                                                           const int32_t* __restrict__ n_dev,
-                                                           const float* __restrict__ factor) {
+                                                           const int32_t* __restrict__ n_dev) {
   const int per = wide / 8;
   const int64_t count = n_pad * per;
   const int64_t real = n_dev ? max(0, *n_dev) : n;
@@ -617,8 +615,7 @@ __global__ __launch_bounds__(kBlock) void copy_rows_kernel(int64_t n, int64_t n_
        e += static_cast<int64_t>(gridDim.x) * kBlock) {
     const int64_t row = e / per;
     const int c = static_cast<int>(e - row * per) * 8;
-    const float f = factor && row < n ? factor[row] : 1.f;
-    const bool live = row < n && (!labels || (row < real && labels[row] >= 0)) && f != 0.f;
+    const bool live = row < n && (!labels || (row < real && labels[row] >= 0));
     if constexpr (DST == GIST_STORE_E4M3) {
       const unsigned char* p = static_cast<const unsigned char*>(x) + row * ldx + c;
       unsigned u[2] = {};
@@ -646,10 +643,6 @@ __global__ __launch_bounds__(kBlock) void copy_rows_kernel(int64_t n, int64_t n_
         } else {
           load_some<SRC, 8>(x, row * ldx + c, d - c, 0.f, v);
         }
-      }
-      if (factor) {
-#pragma unroll
-        for (int q = 0; q < 8; ++q) v[q] *= f;
       }
       store_as<DST, 8>(y, row * wide + c, v);
     }
@@ -739,11 +732,6 @@ __global__ __launch_bounds__(kBlock) void given_kernel(int64_t row0, int64_t n, 
   if (slots && live) atomicMin(slots + y, static_cast<int>(row));   // a class's slot: the first of its rows
 }
 
-__global__ __launch_bounds__(kBlock) void no_slots_kernel(int64_t C, int* __restrict__ slots) {
-  const int64_t c = blockIdx.x * static_cast<int64_t>(kBlock) + threadIdx.x;
-  if (c < C) slots[c] = kNoSlot;
-}
-
 // The rows that have been kept in fp32, by the first of a class's rows: rounded to the gradient's store.
 template <int STORE>
 __global__ __launch_bounds__(kBlock) void given_out_kernel(int64_t n, int d, const int32_t* __restrict__ ids,
@@ -764,50 +752,113 @@ __global__ __launch_bounds__(kBlock) void given_out_kernel(int64_t n, int d, con
   }
 }
 
-// Y = rows of H times p - 1, in fp32; eight elements a thread.  With slots, also every row's.
-__global__ __launch_bounds__(kBlock) void given_rows_kernel(int64_t n, int64_t wide, const char* __restrict__ H, int64_t ldh,
-                                                            const float* __restrict__ pm1, float* __restrict__ Y,
-                                                            const int32_t* __restrict__ ids, const int* __restrict__ slots,
-                                                            int32_t* __restrict__ slot_ids) {
+// Rows of H (bf16, `wide` elements) times their factors, in bf16 with zeros behind the last (and where
+// the factor is 0, whatever the row holds): dT's operand.  And times p - 1, in fp32.  With
+// slots, also every row's.  Eight elements a thread.
+__global__ __launch_bounds__(kBlock) void factored_kernel(int64_t n, int64_t n_pad, int64_t wide, const char* __restrict__ H,
+                                                          int64_t ldh, const float* __restrict__ factor, char* __restrict__ F,
+                                                          const float* __restrict__ pm1, float* __restrict__ Y,
+                                                          const int32_t* __restrict__ ids, const int* __restrict__ slots,
+                                                          int32_t* __restrict__ slot_ids) {
   const int64_t per = wide / 8;
-  for (int64_t e = blockIdx.x * static_cast<int64_t>(kBlock) + threadIdx.x; e < n * per;
+  for (int64_t e = blockIdx.x * static_cast<int64_t>(kBlock) + threadIdx.x; e < n_pad * per;
        e += static_cast<int64_t>(gridDim.x) * kBlock) {
     const int64_t row = e / per, c = (e - row * per) * 8;
-    const float f = pm1[row];
-    if (slots && c == 0) slot_ids[row] = ids[row] >= 0 ? slots[ids[row]] : -1;
-    float h[8];
-    load_vec<GIST_STORE_BF16, 8>(H + row * ldh, c, h);
+    float x[8];
 #pragma unroll
-    for (int q = 0; q < 8; ++q) h[q] *= f;
-    store_vec<8>(Y + row * wide + c, h);
+    for (int q = 0; q < 8; ++q) x[q] = 0.f;
+    if (row < n) {
+      const float f = factor[row], g = pm1[row];
+      if (slots && c == 0) slot_ids[row] = ids[row] >= 0 ? slots[ids[row]] : -1;
+      float h[8], y[8];
+      load_vec<GIST_STORE_BF16, 8>(H + row * ldh, c, h);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        y[q] = h[q] * g;
+        x[q] = f != 0.f ? h[q] * f : 0.f;
+      }
+      store_vec<8>(Y + row * wide + c, y);
+    }
+    store_as<GIST_STORE_BF16, 8>(F, row * wide + c, x);
   }
 }
 
-// The rows' first references: scale <h, t_y>; a wave a row, 16 bytes a lane.  Also clears the marks of far rows.
-__global__ __launch_bounds__(kBlock) void ref_kernel(int64_t row0, int64_t n, int64_t C, int wide, float scale,
-                                                     const char* __restrict__ H, int64_t ldh, const char* __restrict__ T,
-                                                     int64_t ldt, const int32_t* __restrict__ labels,
-                                                     const int32_t* __restrict__ n_dev, float* __restrict__ ref,
-                                                     int* __restrict__ far) {
-  const int64_t row = blockIdx.x * static_cast<int64_t>(kBlock / 64) + (threadIdx.x >> 6);
+// Labelled rows, by a workgroup of 1,024; the result is thread 0's.  Four rows a load, four
+// loads at a time: one workgroup reads a million labels in some 30 us.
+__device__ __forceinline__ int count_labels(int64_t n, const int32_t* __restrict__ labels, const int32_t* __restrict__ n_dev,
+                                            int (&sh)[16]) {
+  int64_t real = n_dev ? max(0, *n_dev) : n;
+  real = real < n ? real : n;
+  int c = 0;
+  const int64_t whole = real / 4;
+#pragma unroll 4
+  for (int64_t i = threadIdx.x; i < whole; i += 1024) {
+    const intx4w v = *reinterpret_cast<const intx4w*>(labels + i * 4);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) c += v[q] >= 0;
+  }
+  for (int64_t i = whole * 4 + threadIdx.x; i < real; i += 1024) c += labels[i] >= 0;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) c += __shfl_xor(c, o, 64);
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = c;
+  __syncthreads();
+  c = 0;
+  for (int w = 0; w < 16; ++w) c += sh[w];
+  return c;
+}
+
+// What comes before a piece's products, each by workgroups of its own in one launch (a launch is
+// some 3 us, which small problems consist of): the rows' first references scale <h, t_y>, a wave a row, 16
+// bytes a lane, and cleared marks of far rows; no class has a slot yet; and the gradients'
+// factor.  `slots`, `factor`: or NULL.
+struct Begin {
+  int64_t row0, n, C, total;   // total: rows of all pieces
+  int wide;
+  float scale, gscale;
+  const char* H;
+  const char* T;
+  int64_t ldh, ldt;
+  const int32_t* labels;       // the piece's
+  const int32_t* all_labels;
+  const int32_t* n_dev;
+  float* ref;
+  int* far;
+  int* slots;
+  float* factor;
+  int64_t ref_blocks, slot_blocks;
+};
+constexpr int kBegin = 1024;
+__global__ __launch_bounds__(kBegin) void begin_kernel(Begin a) {
+  __shared__ int sh[16];
+  int64_t b = blockIdx.x;
+  if (b >= a.ref_blocks + a.slot_blocks) {
+    const int c = count_labels(a.total, a.all_labels, a.n_dev, sh);
+    if (threadIdx.x == 0) *a.factor = c > 0 ? a.gscale / static_cast<float>(c) : 0.f;
+    return;
+  }
+  if (b >= a.ref_blocks) {
+    const int64_t c = (b - a.ref_blocks) * kBegin + threadIdx.x;
+    if (c < a.C) a.slots[c] = kNoSlot;
+    return;
+  }
+  const int64_t row = b * (kBegin / 64) + (threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
-  if (blockIdx.x * static_cast<int64_t>(kBlock / 64) % 256 == 0 && threadIdx.x == 0)
-    far[blockIdx.x * static_cast<int64_t>(kBlock / 64) / 256] = 0;
-  if (row >= n) return;
-  const int y = !n_dev || row0 + row < *n_dev ? labels[row] : -1;
+  if (row >= a.n) return;
+  if (row % 256 == 0 && lane == 0) a.far[row / 256] = 0;
+  const int y = !a.n_dev || a.row0 + row < *a.n_dev ? a.labels[row] : -1;
   float s = 0.f;
-  if (y >= 0 && y < C) {
-    for (int c = lane * 8; c < wide; c += 512) {
+  if (y >= 0 && y < a.C) {
+    for (int c = lane * 8; c < a.wide; c += 512) {
       float h[8], t[8];
-      load_vec<GIST_STORE_BF16, 8>(H + row * ldh, c, h);
-      load_vec<GIST_STORE_BF16, 8>(T + y * ldt, c, t);
+      load_vec<GIST_STORE_BF16, 8>(a.H + row * a.ldh, c, h);
+      load_vec<GIST_STORE_BF16, 8>(a.T + y * a.ldt, c, t);
 #pragma unroll
       for (int q = 0; q < 8; ++q) s = fmaf(h[q], t[q], s);
     }
   }
-  s = wave_sum(s) * scale;
+  s = wave_sum(s) * a.scale;
   // a reference that is no number would spoil rows whose own logits are; their results are NaN by themselves
-  if (lane == 0) ref[row] = fabsf(s) < 1e30f ? s : 0.f;
+  if (lane == 0) a.ref[row] = fabsf(s) < 1e30f ? s : 0.f;
 }
 
 // Loss and the gradients' factor; one workgroup, every thread a stride of rows, in a fixed order.
@@ -820,7 +871,18 @@ __global__ __launch_bounds__(1024) void loss_kernel(int64_t n, const float* __re
   real = real < n ? real : n;
   double s = 0.0;
   int c = 0;
-  for (int64_t i = threadIdx.x; i < real; i += 1024) {
+  const int64_t whole = real / 4;
+#pragma unroll 4
+  for (int64_t i = threadIdx.x; i < whole; i += 1024) {   // as count_labels reads
+    const floatx4 p = *reinterpret_cast<const floatx4*>(logp + i * 4);
+    const intx4w v = *reinterpret_cast<const intx4w*>(labels + i * 4);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      s += p[q];
+      c += v[q] >= 0;
+    }
+  }
+  for (int64_t i = whole * 4 + threadIdx.x; i < real; i += 1024) {
     s += logp[i];
     c += labels[i] >= 0;
   }
@@ -955,22 +1017,82 @@ __global__ __launch_bounds__(kBlock) void piece_kernel(int64_t row0, int64_t row
   }
 }
 
+// The same for more than 2 kChunk classes: kChunk of them a workgroup, held in its registers, which leaves
+// their maximum and sum for join_stats_kernel and the given class's logit; then G.  Whole
+// calls with d = 64, loss alone, by piece_kernel and so: 1 row of 131,072 classes 82 and 28 us, 1,024
+// rows 505 and 310 us; 1,024 rows of 9,000 classes 35 and 35 us; fewer classes are
+// one or two chunks, and the joining launch is for nothing.
+constexpr int kChunk = 4096;
+__global__ __launch_bounds__(kBlock) void chunk_stats_kernel(int64_t row0, int64_t rows, int64_t n, int64_t C, float scale,
+                                                             const float* __restrict__ Z, int64_t ldz,
+                                                             const int32_t* __restrict__ labels, const int32_t* __restrict__ n_dev,
+                                                             floatx2* __restrict__ stats, float* __restrict__ zy) {
+  __shared__ float sm[kBlock / 64], ss[kBlock / 64];
+  const int64_t i = blockIdx.y, c0 = static_cast<int64_t>(blockIdx.x) * kChunk, row = row0 + i;
+  const float* const z = Z + i * ldz;
+  constexpr int L = kChunk / (kBlock * 4);
+  floatx4 v[L];
+  float m = -__builtin_inff();
+#pragma unroll
+  for (int l = 0; l < L; ++l) {
+    const int64_t c = c0 + (l * kBlock + threadIdx.x) * 4;
+    v[l] = floatx4{} - __builtin_inff();
+    if (c < C) {     // ldz is a multiple of 4
+      const floatx4 t = *reinterpret_cast<const floatx4*>(z + c);
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (c + q < C) v[l][q] = t[q] * scale;
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) m = fmaxf(m, v[l][q]);
+  }
+  m = wave_max(m);
+  if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = m;
+  __syncthreads();
+  m = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
+  const float ref = m == -__builtin_inff() ? 0.f : m;
+  float s = 0.f;
+#pragma unroll
+  for (int l = 0; l < L; ++l)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) s += ex2((v[l][q] - ref) * kL);
+  s = wave_sum(s);
+  if ((threadIdx.x & 63) == 0) ss[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  stats[blockIdx.x * rows + i] = floatx2{m, (ss[0] + ss[1]) + (ss[2] + ss[3])};
+  const int64_t y = row < (n_dev ? static_cast<int64_t>(*n_dev) : n) ? labels[row] : -1;
+  if (y >= c0 && y < min(C, c0 + kChunk)) zy[i] = z[y] * scale;
+}
+__global__ __launch_bounds__(kBlock) void chunk_grad_kernel(int64_t row0, int64_t n, int64_t C, float scale, float* __restrict__ Z,
+                                                            int64_t ldz, const int32_t* __restrict__ labels,
+                                                            const int32_t* __restrict__ n_dev, const float* __restrict__ factor,
+                                                            const float* __restrict__ lse) {
+  const int64_t i = blockIdx.y, c0 = static_cast<int64_t>(blockIdx.x) * kChunk, row = row0 + i;
+  float* const z = Z + i * ldz;
+  const int64_t y = row < (n_dev ? static_cast<int64_t>(*n_dev) : n) ? labels[row] : -1;
+  const float f = *factor, l = lse[i];
+#pragma unroll
+  for (int h = 0; h < kChunk / (kBlock * 4); ++h) {
+    const int64_t c = c0 + (h * kBlock + threadIdx.x) * 4;
+    if (c >= ldz) break;
+    floatx4 v = *reinterpret_cast<const floatx4*>(z + c);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      float p = ex2((v[q] * scale - l) * kL);
+      if (c + q == y) p -= 1.f;
+      v[q] = y < 0 || c + q >= C ? 0.f : p * f;
+    }
+    *reinterpret_cast<floatx4*>(z + c) = v;
+  }
+}
+
 // The gradients' factor alone (fp32 pieces need it before their loss is known).
 __global__ __launch_bounds__(1024) void count_kernel(int64_t n, const int32_t* __restrict__ labels,
                                                      const int32_t* __restrict__ n_dev, float gscale, float* __restrict__ factor) {
   __shared__ int sc[16];
-  int64_t real = n_dev ? max(0, *n_dev) : n;
-  real = real < n ? real : n;
-  int c = 0;
-  for (int64_t i = threadIdx.x; i < real; i += 1024) c += labels[i] >= 0;
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) c += __shfl_xor(c, o, 64);
-  if ((threadIdx.x & 63) == 0) sc[threadIdx.x >> 6] = c;
-  __syncthreads();
-  if (threadIdx.x != 0) return;
-  c = 0;
-  for (int w = 0; w < 16; ++w) c += sc[w];
-  *factor = c > 0 ? gscale / static_cast<float>(c) : 0.f;
+  const int c = count_labels(n, labels, n_dev, sc);
+  if (threadIdx.x == 0) *factor = c > 0 ? gscale / static_cast<float>(c) : 0.f;
 }
 
 // Rows of fp32 with those that are not labelled zeroed.
@@ -1016,7 +1138,7 @@ Cut cut_of(int64_t M, int64_t N, int steps) {
   double best = 1e30;
   c.slices = 1;
   for (int s = 1; s <= 64 && s <= most_by_room && s * 4 <= std::max(4, steps); ++s) {
-    const double t = static_cast<double>((tiles * s + at_once - 1) / at_once) / s * (1.0 + 0.0) + (s > 1 ? 0.025 * s : 0.0) *
+    const double t = static_cast<double>((tiles * s + at_once - 1) / at_once) / s + (s > 1 ? 0.025 * s : 0.0) *
                      static_cast<double>(tiles) / at_once;
     if (t < best * 0.999) {
       best = t;
@@ -1050,6 +1172,7 @@ struct Plan {
   bool copy_h, copy_t;      // operands that the products cannot read where they are
   int64_t wide;             // elements of a row of both operands; fp32: of a piece's logits
   int64_t rows;             // forward, and fp32: rows of a piece
+  int chunks;               // fp32 rows cut into so many parts (0: a workgroup a row)
   int64_t n_pad, Cp;        // rows of G or E; classes of a piece (a multiple of 256)
   Cut dh, dt;               // the gradients' products, of the first piece
   bool exps;                // rows piece by piece, by their exponentials
@@ -1088,6 +1211,12 @@ Plan plan_of(const gist_table_xent_desc* D, const void* H, const void* T, bool g
     rows = rows >= 256 ? rows / 256 * 256 : std::max<int64_t>(1, rows);
     p.rows = std::min(n, rows);
     p.z = take(static_cast<size_t>(p.rows) * p.wide * 4);
+    p.chunks = C > 2 * kChunk ? static_cast<int>((C + kChunk - 1) / kChunk) : 0;
+    if (p.chunks) {
+      p.stats = take(static_cast<size_t>(p.rows) * p.chunks * 8);
+      p.zy = take(static_cast<size_t>(p.rows) * 4);
+      p.lse = take(static_cast<size_t>(p.rows) * 4);
+    }
     if (grad) p.hm = take(static_cast<size_t>(p.rows) * d * 4);
     for (const int64_t r : {p.rows, n % p.rows}) {
       if (r == 0) continue;
@@ -1198,10 +1327,10 @@ void join_out(hipStream_t st, const gist_table_xent_desc* D, int64_t rows, int s
 
 template <int SRC, int DST>
 void copy_rows(hipStream_t st, int64_t n, int64_t n_pad, int d, int64_t wide, const void* x, int64_t ldx, void* y,
-               const int32_t* labels, const int32_t* n_dev, const float* factor = nullptr) {
+               const int32_t* labels, const int32_t* n_dev) {
   ProfScope ps(st, "table_xent_copy", 0.0, static_cast<double>(n_pad) * wide * (size_of(SRC) + size_of(DST)));
   hipLaunchKernelGGL((copy_rows_kernel<SRC, DST>), dim3(grid_of(n_pad * wide / 8)), dim3(kBlock), 0, st, n, n_pad, d,
-                     static_cast<int>(wide), x, ldx, y, labels, n_dev, factor);
+                     static_cast<int>(wide), x, ldx, y, labels, n_dev);
 }
 
 // The same cut for fewer rows (N).
@@ -1237,11 +1366,6 @@ gist_status run16(hipStream_t st, const gist_table_xent_desc* D, const Plan& p, 
   a.out = w + p.g;
   a.ldo = p.Cp;
   a.far = far;
-  if (p.exps) {
-    ProfScope ps(st, "table_xent_count", 0.0, 4.0 * n);
-    hipLaunchKernelGGL(count_kernel, dim3(1), dim3(1024), 0, st, n, labels, n_dev, D->grad_scale * D->scale, f32(p.factor));
-    GIST_LAUNCHED("table_xent_count");
-  }
   for (int64_t r0 = 0; r0 < n; r0 += p.rows) {
     const int64_t rn = std::min(p.rows, n - r0);
     const Cut c = cut_logits(C, rn, a.steps, STORE == GIST_STORE_E4M3);
@@ -1253,12 +1377,37 @@ gist_status run16(hipStream_t st, const gist_table_xent_desc* D, const Plan& p, 
     a.qs = h_scale ? h_scale + r0 : nullptr;
     a.labels = labels + r0;
     a.zy = f32(p.zy) + r0;
+    // The last piece's product writes dT where it is not cut; before, and where it is, parts are kept.
+    const bool straight = p.exps && p.dt.slices == 1 && r0 + rn == n;
+    int* const slots = straight ? reinterpret_cast<int*>(w + p.slots) : nullptr;
+    int32_t* const slot_ids = straight ? reinterpret_cast<int32_t*>(w + p.slot_ids) : nullptr;
     if constexpr (STORE == GIST_STORE_BF16) {
       if (p.exps) {
-        ProfScope ps(st, "table_xent_ref", 0.0, 4.0 * rn * d);
-        hipLaunchKernelGGL(ref_kernel, dim3(static_cast<unsigned>((rn + 3) / 4)), dim3(kBlock), 0, st, r0, rn, C,
-                           static_cast<int>(p.wide), D->scale, a.Q, ldh, T, ldt, a.labels, n_dev, ref, far);
-        GIST_LAUNCHED("table_xent_ref");
+        Begin b{};
+        b.row0 = r0;
+        b.n = rn;
+        b.C = C;
+        b.total = n;
+        b.wide = static_cast<int>(p.wide);
+        b.scale = D->scale;
+        b.gscale = D->grad_scale * D->scale;
+        b.H = a.Q;
+        b.T = T;
+        b.ldh = ldh;
+        b.ldt = ldt;
+        b.labels = a.labels;
+        b.all_labels = labels;
+        b.n_dev = n_dev;
+        b.ref = ref;
+        b.far = far;
+        b.slots = slots;
+        b.factor = f32(p.factor);
+        b.ref_blocks = (rn + kBegin / 64 - 1) / (kBegin / 64);
+        b.slot_blocks = straight ? (C + kBegin - 1) / kBegin : 0;
+        ProfScope ps(st, "table_xent_begin", 0.0, 4.0 * rn * d);
+        hipLaunchKernelGGL(begin_kernel, dim3(static_cast<unsigned>(b.ref_blocks + b.slot_blocks + (r0 == 0))), dim3(kBegin), 0,
+                           st, b);
+        GIST_LAUNCHED("table_xent_begin");
       }
     }
     {
@@ -1294,15 +1443,6 @@ gist_status run16(hipStream_t st, const gist_table_xent_desc* D, const Plan& p, 
         launch_product<STORE, kAgain, false, false>(st, c.tile, a);
         GIST_LAUNCHED("table_xent_again");
       }
-      // The last piece's product writes dT where it is not cut; before, and where it is, parts are kept.
-      const bool straight = p.dt.slices == 1 && r0 + rn == n;
-      int* const slots = straight ? reinterpret_cast<int*>(w + p.slots) : nullptr;
-      int32_t* const slot_ids = reinterpret_cast<int32_t*>(w + p.slot_ids);
-      if (straight) {
-        ProfScope ps(st, "table_xent_slots", 0.0, 4.0 * C);
-        hipLaunchKernelGGL(no_slots_kernel, dim3(static_cast<unsigned>((C + kBlock - 1) / kBlock)), dim3(kBlock), 0, st, C, slots);
-        GIST_LAUNCHED("table_xent_slots");
-      }
       {
         ProfScope ps(st, "table_xent_given", 0.0, 18.0 * rn);
         hipLaunchKernelGGL(given_kernel, dim3(static_cast<unsigned>((rn + kBlock - 1) / kBlock)), dim3(kBlock), 0, st, r0, rn, C,
@@ -1310,10 +1450,13 @@ gist_status run16(hipStream_t st, const gist_table_xent_desc* D, const Plan& p, 
                            slots);
         GIST_LAUNCHED("table_xent_given");
       }
-      // the rows of H times their factors, zeros behind the last
-      copy_rows<GIST_STORE_BF16, GIST_STORE_BF16>(st, rn, up(rn, 64), static_cast<int>(p.wide), p.wide, a.Q, ldh / 2, w + p.hm,
-                                                  nullptr, nullptr, row_factor);
-      GIST_LAUNCHED("table_xent_copy");
+      float* const Y = f32(p.y);
+      {
+        ProfScope ps(st, "table_xent_factored", 0.0, 8.0 * rn * d);
+        hipLaunchKernelGGL(factored_kernel, dim3(grid_of(up(rn, 64) * p.wide / 8)), dim3(kBlock), 0, st, rn, up(rn, 64), p.wide,
+                           a.Q, ldh, row_factor, w + p.hm, pm1, Y, ids, slots, slot_ids);
+        GIST_LAUNCHED("table_xent_factored");
+      }
       const int64_t ldp = up(d, 4), moved = 2 * rn * C;
       float* const part_h = f32(p.part);
       float* const part_t = part_h + (p.parts_h ? p.dh.slices * p.rows * ldp : 0);
@@ -1388,14 +1531,7 @@ gist_status run16(hipStream_t st, const gist_table_xent_desc* D, const Plan& p, 
         }
         GIST_LAUNCHED("table_xent_dt");
       }
-      {   // and the given classes' rows of H, times p - 1
-        float* const Y = f32(p.y);
-        {
-          ProfScope ps(st, "table_xent_given_rows", 0.0, 6.0 * rn * d);
-          hipLaunchKernelGGL(given_rows_kernel, dim3(grid_of(rn * p.wide / 8)), dim3(kBlock), 0, st, rn, p.wide, a.Q, ldh, pm1, Y,
-                             ids, slots, slot_ids);
-          GIST_LAUNCHED("table_xent_given_rows");
-        }
+      {   // and the given classes' rows
         const gist_status s =
             straight ? embed_grad(st, rn, p.rows, d, slot_ids, 1.f, Y, p.wide, true, -1.f, f32(p.kept), ldp, w + p.embed)
                      : embed_grad(st, rn, C, d, ids, 1.f, Y, p.wide, true, -1.f, part_t, ldp, w + p.embed);
@@ -1578,7 +1714,24 @@ gist_status run32(hipStream_t st, const gist_table_xent_desc* D, const Plan& p, 
     O.ldc0 = p.wide;
     gist_status s = gemm(st, rn, C, d, A, B, O, GIST_DTYPE_F32, gws, p.gemm_bytes);
     if (s != GIST_OK) return s;
-    {
+    if (p.chunks) {
+      float* const zy = reinterpret_cast<float*>(w + p.zy);
+      float* const l = reinterpret_cast<float*>(w + p.lse);
+      floatx2* const stats = reinterpret_cast<floatx2*>(w + p.stats);
+      const dim3 grid(static_cast<unsigned>(p.chunks), static_cast<unsigned>(rn));
+      ProfScope ps(st, "table_xent_chunks", 0.0, (grad ? 12.0 : 4.0) * rn * C);
+      hipLaunchKernelGGL(chunk_stats_kernel, grid, dim3(kBlock), 0, st, r0, rn, n, C, D->scale, z, p.wide, labels, n_dev, stats,
+                         zy);
+      GIST_LAUNCHED("table_xent_chunks");
+      hipLaunchKernelGGL(join_stats_kernel<4>, dim3(static_cast<unsigned>((rn + 3) / 4)), dim3(1024), 0, st, r0, rn, C, p.chunks,
+                         stats, rn, zy, labels + r0, n_dev, l, lse ? lse + r0 : nullptr, logp_ws + r0, logp ? logp + r0 : nullptr,
+                         nullptr, nullptr, nullptr);
+      GIST_LAUNCHED("table_xent_chunks");
+      if (grad) {
+        hipLaunchKernelGGL(chunk_grad_kernel, grid, dim3(kBlock), 0, st, r0, n, C, D->scale, z, p.wide, labels, n_dev, factor, l);
+        GIST_LAUNCHED("table_xent_chunks");
+      }
+    } else {
       ProfScope ps(st, "table_xent_piece", 0.0, (grad ? 8.0 : 4.0) * rn * C);
       hipLaunchKernelGGL(piece_kernel, dim3(static_cast<unsigned>(std::min<int64_t>(rn, 1 << 20))), dim3(kBlock), 0, st, r0, rn,
                          n, C, D->scale, z, p.wide, labels, n_dev, factor, grad ? 1 : 0, lse, logp_ws, logp);
