@@ -5,8 +5,12 @@
 //   with u = dy g and n = h s:  dx = s (u - n mean_j(u_j n_j)) + dsum,  dg = sum_v dy n.
 //
 // All of it is bound by memory: every array is read or written once.  A row is
-// held in the registers of a wave, or of a workgroup of 256 where rows are long
-// or few; longer rows than a workgroup holds are read twice.  Sums are fp32.
+// held in the registers of 16 lanes, a wave, or a workgroup of 256 or 1,024; longer
+// rows are read twice (three times for codes).  Sums are fp32.  Both directions move 4.5 to 5 TB/s where
+// rows are whole 16-byte loads: 65,537 rows of 2,048 from fp32 to codes 134 us, 16,384 of 4,096 in bf16 with
+// residual and gradients 209 us.  A forward pass of 256 threads a row alone, long rows read again, took
+// 183 and 220 us there, 49 us for 100,000 rows of 64 in fp32 (now 11), and 180 us for 4,000 of
+// 16,384 in bf16 (now 111).
 //
 // 8-bit rows: e4m3, the row's largest magnitude at 448, nearest even.
 //
@@ -23,10 +27,13 @@ namespace gist {
 namespace {
 
 constexpr int kBlock = 256;
+constexpr int kWide = 1024;               // threads of a workgroup whose rows 256 do not hold
 constexpr float kTop = 448.f;             // largest e4m3 value
 constexpr int64_t kMostBlocks = 1 << 16;  // rows go around them
 
 typedef unsigned u32u __attribute__((aligned(1)));
+
+constexpr int block_of(int threads) { return threads < kBlock ? kBlock : threads; }
 
 template <int STORE>
 constexpr int vec_of() { return STORE == GIST_STORE_F32 ? 4 : 8; }
@@ -35,6 +42,11 @@ constexpr int vec_of() { return STORE == GIST_STORE_F32 ? 4 : 8; }
 // turn (`turn` flips), so that one barrier a sum is enough.
 template <int THREADS>
 __device__ __forceinline__ float row_sum(float v, float* sh, int& turn) {
+  if constexpr (THREADS < 64) {
+#pragma unroll
+    for (int o = THREADS / 2; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+    return v;
+  }
   v = wave_sum(v);
   if constexpr (THREADS == 64) return v;
   float* s = sh + turn * (THREADS / 64);
@@ -52,8 +64,8 @@ template <int THREADS>
 __device__ __forceinline__ float row_max(float m, float* sh, int& turn) {
   int v = __float_as_int(m);
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = max(v, __shfl_xor(v, o, 64));
-  if constexpr (THREADS == 64) return __int_as_float(v);
+  for (int o = (THREADS < 64 ? THREADS : 64) / 2; o > 0; o >>= 1) v = max(v, __shfl_xor(v, o, 64));
+  if constexpr (THREADS <= 64) return __int_as_float(v);
   float* s = sh + turn * (THREADS / 64);
   turn ^= 1;
   if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = __int_as_float(v);
@@ -73,14 +85,9 @@ __device__ __forceinline__ void store_e4m3(void* base, int64_t e, int64_t left, 
   unsigned char* p = static_cast<unsigned char*>(base) + e;
 #pragma unroll
   for (int h = 0; h < V; h += 4) {
-    float c[4];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const float a = y[h + q] * inv;
-      c[q] = a > kTop ? kTop : a < -kTop ? -kTop : a;   // the product's rounding; NaN stays
-    }
-    int u = __builtin_amdgcn_cvt_pk_fp8_f32(c[0], c[1], 0, false);
-    u = __builtin_amdgcn_cvt_pk_fp8_f32(c[2], c[3], u, true);
+    // |y inv| <= 448 (1 + 2^-23), which rounds to 448 (as all up to 464 do); NaN stays
+    int u = __builtin_amdgcn_cvt_pk_fp8_f32(y[h] * inv, y[h + 1] * inv, 0, false);
+    u = __builtin_amdgcn_cvt_pk_fp8_f32(y[h + 2] * inv, y[h + 3] * inv, u, true);
     if (left >= h + 4) {
       *reinterpret_cast<u32u*>(p + h) = static_cast<unsigned>(u);
     } else {
@@ -150,28 +157,31 @@ __device__ __forceinline__ float scale_of(float big, float& inv) {
   return zero ? 0.f : big / kTop;
 }
 
-// A row in the registers of THREADS threads: CH loads of V elements each.  NORM false: no
-// norm, the row's codes alone.
-template <int STORE, int OUT, int THREADS, int CH, bool NORM>
-__global__ __launch_bounds__(kBlock) void rows_kernel(Fwd a) {
+// A row in the registers of THREADS threads: CH loads of V elements each and, with TAIL, one element each
+// of what those leave (a load that may end inside a row takes a branch a load: 183 us for
+// 65,537 rows of 2,048 from fp32 to codes, 134 without; of 602, with a residual, 147 and 116).  NORM false: no norm, the row's codes alone.
+template <int STORE, int OUT, int THREADS, int CH, bool NORM, bool TAIL>
+__global__ __launch_bounds__(block_of(THREADS)) void rows_kernel(Fwd a) {
   constexpr int V = vec_of<STORE>();
-  __shared__ float sh[2 * kBlock / 64];
+  __shared__ float sh[2 * block_of(THREADS) / 64];
   int turn = 0;
   const int lane = threadIdx.x % THREADS;
+  const int whole = TAIL ? a.d - a.d % V : a.d, tail = whole + lane;
   const float inv_d = 1.f / static_cast<float>(a.d);
-  constexpr int RB = kBlock / THREADS;
+  constexpr int RB = block_of(THREADS) / THREADS;
   for (int64_t row = blockIdx.x * RB + threadIdx.x / THREADS; row < a.n; row += static_cast<int64_t>(gridDim.x) * RB) {
-    float h[CH][V];
+    float h[CH][V], t[1] = {0.f};
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
       const int c = (i * THREADS + lane) * V;
 #pragma unroll
       for (int q = 0; q < V; ++q) h[i][q] = 0.f;
-      if (c < a.d) load_h<STORE, V>(a, row, c, a.d - c, h[i]);
+      if (c < whole) load_h<STORE, V>(a, row, c, V, h[i]);
     }
+    if (TAIL && tail < a.d) load_h<STORE, 1>(a, row, tail, 1, t);
     float big = 0.f;
     if constexpr (NORM) {
-      float s = 0.f;
+      float s = TAIL ? t[0] * t[0] : 0.f;
 #pragma unroll
       for (int i = 0; i < CH; ++i) {
         float p = 0.f;
@@ -184,22 +194,28 @@ __global__ __launch_bounds__(kBlock) void rows_kernel(Fwd a) {
 #pragma unroll
       for (int i = 0; i < CH; ++i) {
         const int c = (i * THREADS + lane) * V;
-        if (c >= a.d) continue;
-        if (a.h) store_some<STORE, V>(a.h, row * a.ldh + c, a.d - c, h[i]);
+        if (c >= whole) continue;
+        if (a.h) store_as<STORE, V>(a.h, row * a.ldh + c, h[i]);
         float g[V];
 #pragma unroll
         for (int q = 0; q < V; q += 4) {
-          float t[4];
-          load_some<GIST_STORE_F32, 4>(a.gain, c + q, a.d - c - q, 0.f, t);
+          float u[4];
+          load_vec<GIST_STORE_F32, 4>(a.gain, c + q, u);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) g[q + k] = t[k];
+          for (int k = 0; k < 4; ++k) g[q + k] = u[k];
         }
 #pragma unroll
         for (int q = 0; q < V; ++q) h[i][q] = h[i][q] * rstd * g[q];
-        if constexpr (OUT != GIST_STORE_E4M3) store_y<OUT, V>(a.y, row * a.ldy + c, a.d - c, h[i], 0.f);
+        if constexpr (OUT != GIST_STORE_E4M3) store_y<OUT, V>(a.y, row * a.ldy + c, V, h[i], 0.f);
+      }
+      if (TAIL && tail < a.d) {
+        if (a.h) store_as<STORE, 1>(a.h, row * a.ldh + tail, t);
+        t[0] = t[0] * rstd * a.gain[tail];
+        if constexpr (OUT != GIST_STORE_E4M3) store_as<OUT, 1>(a.y, row * a.ldy + tail, t);
       }
     }
     if constexpr (OUT == GIST_STORE_E4M3) {
+      if (TAIL) big = larger(big, t[0]);
 #pragma unroll
       for (int i = 0; i < CH; ++i)
 #pragma unroll
@@ -210,8 +226,11 @@ __global__ __launch_bounds__(kBlock) void rows_kernel(Fwd a) {
 #pragma unroll
       for (int i = 0; i < CH; ++i) {
         const int c = (i * THREADS + lane) * V;
-        if (c < a.d) store_y<OUT, V>(a.y, row * a.ldy + c, a.d - c, h[i], inv);
+        if (c < whole) store_y<OUT, V>(a.y, row * a.ldy + c, V, h[i], inv);
       }
+      if (TAIL && tail < a.d)
+        static_cast<unsigned char*>(a.y)[row * a.ldy + tail] =
+            static_cast<unsigned char>(__builtin_amdgcn_cvt_pk_fp8_f32(t[0] * inv, 0.f, 0, false));
     }
   }
 }
@@ -302,35 +321,48 @@ __device__ __forceinline__ void load_any(const void* base, int64_t e, int left, 
   }
 }
 
-template <int STORE, int DY, int THREADS, int CH>
-__global__ __launch_bounds__(kBlock) void bwd_kernel(Bwd a) {
+template <int STORE, int DY, int THREADS, int CH, bool TAIL>
+__global__ __launch_bounds__(block_of(THREADS)) void bwd_kernel(Bwd a) {
   constexpr int V = vec_of<STORE>();
-  __shared__ float sh[2 * kBlock / 64];
-  __shared__ __attribute__((aligned(16))) float join[THREADS == 64 ? 64 * CH * V : 4];
+  __shared__ float sh[2 * block_of(THREADS) / 64];
+  __shared__ __attribute__((aligned(16))) float join[THREADS <= 64 ? THREADS * (CH * V + 1) : 4];
   int turn = 0;
   const int lane = threadIdx.x % THREADS, sub = threadIdx.x / THREADS;
+  const int whole = TAIL ? a.d - a.d % V : a.d, tail = whole + lane;   // as in rows_kernel
   const float inv_d = 1.f / static_cast<float>(a.d);
-  constexpr int RB = kBlock / THREADS;
-  float acc[CH][V] = {}, g[CH][V];
+  constexpr int RB = block_of(THREADS) / THREADS;
+  float acc[CH][V] = {}, g[CH][V], acct = 0.f;
+  const float gt = TAIL && tail < a.d ? a.gain[tail] : 0.f;
 #pragma unroll
   for (int i = 0; i < CH; ++i) {
     const int c = (i * THREADS + lane) * V;
 #pragma unroll
     for (int q = 0; q < V; ++q) g[i][q] = 0.f;
-    if (c < a.d) load_any<GIST_STORE_F32, V>(a.gain, c, a.d - c, g[i]);
+    if (c < whole) load_any<GIST_STORE_F32, V>(a.gain, c, V, g[i]);
   }
   for (int64_t row = blockIdx.x * RB + sub; row < a.n; row += static_cast<int64_t>(gridDim.x) * RB) {
     const float s = a.rstd[row];
-    float h[CH][V], y[CH][V], dot = 0.f;
+    float h[CH][V], y[CH][V], ht[1] = {0.f}, yt[1] = {0.f};
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
       const int c = (i * THREADS + lane) * V;
 #pragma unroll
       for (int q = 0; q < V; ++q) h[i][q] = y[i][q] = 0.f;
-      if (c < a.d) {
-        load_some<STORE, V>(a.h, row * a.ldh + c, a.d - c, 0.f, h[i]);
-        load_any<DY, V>(a.dy, row * a.lddy + c, a.d - c, y[i]);
+      if (c < whole) {
+        load_vec<STORE, V>(a.h, row * a.ldh + c, h[i]);
+        load_any<DY, V>(a.dy, row * a.lddy + c, V, y[i]);
       }
+    }
+    if (TAIL && tail < a.d) {
+      load_vec<STORE, 1>(a.h, row * a.ldh + tail, ht);
+      load_vec<DY, 1>(a.dy, row * a.lddy + tail, yt);
+    }
+    float dot = 0.f;
+    if constexpr (TAIL) {
+      ht[0] *= s;
+      acct = fmaf(yt[0], ht[0], acct);
+      yt[0] *= gt;
+      dot = yt[0] * ht[0];
     }
 #pragma unroll
     for (int i = 0; i < CH; ++i)
@@ -346,29 +378,36 @@ __global__ __launch_bounds__(kBlock) void bwd_kernel(Bwd a) {
 #pragma unroll
       for (int i = 0; i < CH; ++i) {
         const int c = (i * THREADS + lane) * V;
-        if (c >= a.d) continue;
+        if (c >= whole) continue;
         float z[V];
 #pragma unroll
         for (int q = 0; q < V; ++q) z[q] = 0.f;
-        if (a.dsum) load_some<STORE, V>(a.dsum, row * a.ldds + c, a.d - c, 0.f, z);
+        if (a.dsum) load_vec<STORE, V>(a.dsum, row * a.ldds + c, z);
 #pragma unroll
         for (int q = 0; q < V; ++q) z[q] = fmaf(s, y[i][q] - h[i][q] * dot, z[q]);
-        store_some<STORE, V>(a.dx, row * a.lddx + c, a.d - c, z);
+        store_as<STORE, V>(a.dx, row * a.lddx + c, z);
+      }
+      if (TAIL && tail < a.d) {
+        float z[1] = {0.f};
+        if (a.dsum) load_vec<STORE, 1>(a.dsum, row * a.ldds + tail, z);
+        z[0] = fmaf(s, yt[0] - ht[0] * dot, z[0]);
+        store_as<STORE, 1>(a.dx, row * a.lddx + tail, z);
       }
     }
   }
   if (!a.part) return;
-  if constexpr (THREADS == 64) {     // the workgroup's waves, in order
+  if constexpr (THREADS <= 64) {     // the workgroup's rows, in order
     for (int w = 0; w < RB; ++w) {
       if (sub == w) {
+        auto add = [&](float& x, float* p) {
+          x += w == 0 ? 0.f : *p;
+          if (w + 1 < RB) *p = x;
+        };
 #pragma unroll
         for (int i = 0; i < CH; ++i)
 #pragma unroll
-          for (int q = 0; q < V; ++q) {
-            float* p = join + (i * 64 + lane) * V + q;
-            acc[i][q] += w == 0 ? 0.f : *p;
-            if (w + 1 < RB) *p = acc[i][q];
-          }
+          for (int q = 0; q < V; ++q) add(acc[i][q], join + (i * THREADS + lane) * V + q);
+        if (TAIL) add(acct, join + THREADS * CH * V + lane);
       }
       if (w + 1 < RB) __syncthreads();
     }
@@ -378,11 +417,11 @@ __global__ __launch_bounds__(kBlock) void bwd_kernel(Bwd a) {
 #pragma unroll
   for (int i = 0; i < CH; ++i) {
     const int c = (i * THREADS + lane) * V;
-    if (c >= a.d) continue;
+    if (c >= whole) continue;
 #pragma unroll
-    for (int q = 0; q < V; ++q)
-      if (c + q < a.d) out[c + q] = acc[i][q];
+    for (int q = 0; q < V; ++q) out[c + q] = acc[i][q];
   }
+  if (TAIL && tail < a.d) out[tail] = acct;
 }
 
 // Rows longer than a workgroup's registers: two passes a row; the gain's sums lie in `part`,
@@ -464,20 +503,38 @@ __global__ __launch_bounds__(64 * kJoinWaves) void gain_kernel(int parts, int d,
 constexpr int kFwdCh(int v) { return 32 / v; }   // 32 elements a thread, 16 in the backward pass
 constexpr int kBwdCh(int v) { return 16 / v; }
 
-template <int STORE, int OUT, bool NORM>
-void launch_rows(hipStream_t st, const Fwd& a) {
-  constexpr int CH = kFwdCh(vec_of<STORE>());
-  // A wave a row leaves more rows in flight; 256 threads a row end a few long rows sooner.
-  if (a.d <= 512 || (a.d <= 64 * 32 && a.n >= 1024)) {
+template <int STORE, int OUT, bool NORM, bool TAIL>
+void launch_rows_of(hipStream_t st, const Fwd& a) {
+  constexpr int CH = kFwdCh(vec_of<STORE>()), few = 8 / vec_of<STORE>();
+  // A wave a row leaves more rows in flight (65,537 rows of 2,048 in fp32, to codes: 181 us, 254 by 256
+  // threads); 256 threads a row end a few long rows sooner.  Rows of a few hundred elements take eight a
+  // thread, not 32 (200,000 rows of 256 in bf16: 63 and 76 us), and 16 lanes where those hold them
+  // (300,000 of 41: 26 and 143 us).
+  if (a.d <= 16 * 8) {
+    const int64_t g = std::min<int64_t>((a.n + 15) / 16, kMostBlocks);
+    hipLaunchKernelGGL((rows_kernel<STORE, OUT, 16, few, NORM, TAIL>), dim3(static_cast<unsigned>(g)), dim3(kBlock), 0, st, a);
+  } else if (a.d <= 64 * 8) {
     const int64_t g = std::min<int64_t>((a.n + 3) / 4, kMostBlocks);
-    hipLaunchKernelGGL((rows_kernel<STORE, OUT, 64, CH, NORM>), dim3(static_cast<unsigned>(g)), dim3(kBlock), 0, st, a);
+    hipLaunchKernelGGL((rows_kernel<STORE, OUT, 64, few, NORM, TAIL>), dim3(static_cast<unsigned>(g)), dim3(kBlock), 0, st, a);
+  } else if (a.d <= 64 * 32 && a.n >= 1024) {
+    const int64_t g = std::min<int64_t>((a.n + 3) / 4, kMostBlocks);
+    hipLaunchKernelGGL((rows_kernel<STORE, OUT, 64, CH, NORM, TAIL>), dim3(static_cast<unsigned>(g)), dim3(kBlock), 0, st, a);
   } else if (a.d <= kBlock * 32) {
     const int64_t g = std::min<int64_t>(a.n, kMostBlocks);
-    hipLaunchKernelGGL((rows_kernel<STORE, OUT, kBlock, CH, NORM>), dim3(static_cast<unsigned>(g)), dim3(kBlock), 0, st, a);
+    hipLaunchKernelGGL((rows_kernel<STORE, OUT, kBlock, CH, NORM, TAIL>), dim3(static_cast<unsigned>(g)), dim3(kBlock), 0, st, a);
+  } else if (a.d <= kWide * 32) {
+    const int64_t g = std::min<int64_t>(a.n, kMostBlocks);
+    hipLaunchKernelGGL((rows_kernel<STORE, OUT, kWide, CH, NORM, TAIL>), dim3(static_cast<unsigned>(g)), dim3(kWide), 0, st, a);
   } else {
     const int64_t g = std::min<int64_t>(a.n, kMostBlocks);
     hipLaunchKernelGGL((long_rows_kernel<STORE, OUT, NORM>), dim3(static_cast<unsigned>(g)), dim3(kBlock), 0, st, a);
   }
+}
+
+template <int STORE, int OUT, bool NORM>
+void launch_rows(hipStream_t st, const Fwd& a) {
+  if (a.d % vec_of<STORE>() == 0) launch_rows_of<STORE, OUT, NORM, false>(st, a);
+  else launch_rows_of<STORE, OUT, NORM, true>(st, a);
 }
 
 template <int STORE>
@@ -490,19 +547,29 @@ void launch_norm(hipStream_t st, const Fwd& a, int out) {
 
 // Rows a workgroup of the backward pass takes at a time, and workgroups: enough to fill the
 // card twice over, no more than rows (their sums are added by a second launch).
-int rows_a_block(int d) { return d <= 64 * 16 ? kBlock / 64 : 1; }
+int rows_a_block(int d) { return d <= 16 * 8 ? kBlock / 16 : d <= 64 * 16 ? kBlock / 64 : 1; }
 int64_t bwd_blocks(int64_t n, int d) {
   const int64_t rb = rows_a_block(d);
   return std::min<int64_t>((n + rb - 1) / rb, 1024);
 }
 
+template <int STORE, int DY, bool TAIL>
+void launch_bwd_rows(hipStream_t st, const Bwd& a) {
+  constexpr int V = vec_of<STORE>(), CH = kBwdCh(V), few = 8 / V;
+  const dim3 grid(static_cast<unsigned>(bwd_blocks(a.n, a.d))), block(kBlock);
+  // threads and elements a row as in the forward pass, half as many elements
+  if (a.d <= 16 * 8) hipLaunchKernelGGL((bwd_kernel<STORE, DY, 16, few, TAIL>), grid, block, 0, st, a);
+  else if (a.d <= 64 * 8) hipLaunchKernelGGL((bwd_kernel<STORE, DY, 64, few, TAIL>), grid, block, 0, st, a);
+  else if (a.d <= 64 * 16) hipLaunchKernelGGL((bwd_kernel<STORE, DY, 64, CH, TAIL>), grid, block, 0, st, a);
+  else if (a.d <= kBlock * 16) hipLaunchKernelGGL((bwd_kernel<STORE, DY, kBlock, CH, TAIL>), grid, block, 0, st, a);
+  else if (a.d <= kWide * 16) hipLaunchKernelGGL((bwd_kernel<STORE, DY, kWide, CH, TAIL>), grid, dim3(kWide), 0, st, a);
+  else hipLaunchKernelGGL((long_bwd_kernel<STORE, DY>), grid, block, 0, st, a);
+}
+
 template <int STORE, int DY>
 void launch_bwd(hipStream_t st, const Bwd& a) {
-  constexpr int CH = kBwdCh(vec_of<STORE>());
-  const dim3 grid(static_cast<unsigned>(bwd_blocks(a.n, a.d))), block(kBlock);
-  if (rows_a_block(a.d) > 1) hipLaunchKernelGGL((bwd_kernel<STORE, DY, 64, CH>), grid, block, 0, st, a);
-  else if (a.d <= kBlock * 16) hipLaunchKernelGGL((bwd_kernel<STORE, DY, kBlock, CH>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((long_bwd_kernel<STORE, DY>), grid, block, 0, st, a);
+  if (a.d % vec_of<STORE>() == 0) launch_bwd_rows<STORE, DY, false>(st, a);
+  else launch_bwd_rows<STORE, DY, true>(st, a);
 }
 
 template <int STORE>

@@ -236,3 +236,38 @@ def test_no_rows(G, ctx):
     G.gist_rms_norm(ctx, 0, 5, e, 5, None, 5, 0, dg, EPS, None, 5, e, 5, 0, None, None)
     G.gist_rms_norm_bwd(ctx, 0, 5, e, 5, 0, e, 5, 0, dg.clone(), None, None, 5, e, 5, dg, None)
     assert (to_host(dg) == 0).all()       # the sum over no rows
+
+
+# Where the number of threads and of elements a row changes, and rows that no workgroup holds.
+EDGES = [(50, 16), (4097, 41), (33, 128), (17, 129), (1000, 130), (600, 512), (70, 516), (5, 520),
+         (40, 1025), (3, 4104), (2, 16384), (2, 16385), (3, 32768), (2, 32769), (2, 40003)]
+
+
+@pytest.mark.parametrize("n,d", EDGES)
+@pytest.mark.parametrize("store,out", [("f32", "f32"), ("bf16", "bf16"), ("f16", "e4m3"),
+                                       ("f32", "e4m3")])
+def test_forward_at_edges(G, ctx, n, d, store, out):
+    test_forward(G, ctx, n, d, store, out)
+
+
+@pytest.mark.parametrize("n,d", EDGES)
+@pytest.mark.parametrize("store,dys", [("f32", "f32"), ("bf16", "bf16"), ("f16", "f32"),
+                                       ("f32", "bf16")])
+def test_backward_at_edges(G, ctx, n, d, store, dys):
+    test_backward(G, ctx, n, d, store, dys)
+
+
+@pytest.mark.parametrize("d", [16, 130, 17000, 40000])
+def test_shared_arrays_at_edges(G, ctx, d):
+    test_shared_arrays(G, ctx, d)
+
+
+@pytest.mark.parametrize("d", [16, 100, 130, 17000, 40001])
+def test_non_finite_rows_at_edges(G, ctx, d):
+    test_non_finite_rows(G, ctx, d)
+
+
+@pytest.mark.parametrize("n,d", [(40, 16), (300, 128), (9, 512), (2, 40003)])
+@pytest.mark.parametrize("store", ["f32", "bf16", "f16"])
+def test_quantize_rows_at_edges(G, ctx, n, d, store):
+    test_quantize_rows(G, ctx, n, d, store)
