@@ -653,8 +653,9 @@ gist_status gist_quantize_rows(gist_ctx* ctx, int64_t n, int32_t d, const void* 
  * d < 1, a leading dimension below d, unknown store or dtype, non-finite scale
  * or grad_scale, NULL H, T or labels with n > 0, NULL loss_dev, one gradient without
  * the other, gradients of E4M3 operands, scales not matching the store,
- * gradients that share an array with another operand), GIST_E_UNSUPPORTED (n or C
- * above 2^30, d above 65,536), GIST_E_NOMEM.
+ * gradients that share an array with another operand), GIST_E_UNSUPPORTED (n
+ * above 2^30, C above 2^29, with gradients by bf16 products above 2^23, d above
+ * 65,536), GIST_E_NOMEM.
  * With n == 0 the loss is 0 and dT is zeroed. */
 typedef struct gist_table_xent_desc {
   int64_t n, C;

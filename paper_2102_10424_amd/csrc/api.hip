@@ -1324,7 +1324,7 @@ extern "C" gist_status gist_quantize_rows(gist_ctx* ctx, int64_t n, int32_t d, c
 
 namespace {
 // The descriptor with its leading dimensions filled in.
-gist_status check_table_xent(const char* what, const gist_table_xent_desc* in,
+gist_status check_table_xent(const char* what, const gist_table_xent_desc* in, bool gradients,
                              gist_table_xent_desc* D) {
   if (!in) return bad(what, GIST_E_INVAL, ": NULL descriptor");
   *D = *in;
@@ -1338,9 +1338,13 @@ gist_status check_table_xent(const char* what, const gist_table_xent_desc* in,
     return bad(what, GIST_E_INVAL, ": dtype is F32 or BF16_IN");
   if (!std::isfinite(D->scale) || !std::isfinite(D->grad_scale))
     return bad(what, GIST_E_INVAL, ": non-finite scale");
-  if (D->n > (1 << 30) || D->C > (1 << 30))
-    return bad(what, GIST_E_UNSUPPORTED, ": n or C above 2^30");
+  if (D->n > (1 << 30) || D->C > (1 << 29))
+    return bad(what, GIST_E_UNSUPPORTED, ": n above 2^30 or C above 2^29");
   if (D->d > 65536) return bad(what, GIST_E_UNSUPPORTED, ": d above 65536");
+  // a tile of 256 rows of the exponentials is addressed in 32 bits
+  const bool bf16 = D->store == GIST_STORE_BF16 || (D->store == GIST_STORE_F32 && D->dtype == GIST_DTYPE_BF16_IN);
+  if (gradients && bf16 && D->C > (1 << 23))
+    return bad(what, GIST_E_UNSUPPORTED, ": bf16 products' gradients of more than 2^23 classes");
   return GIST_OK;
 }
 }  // namespace
@@ -1350,7 +1354,7 @@ extern "C" gist_status gist_table_xent_workspace(const gist_table_xent_desc* D, 
   gist::clear_error();
   if (!bytes) return set_error(GIST_E_INVAL, "table_xent_workspace: NULL out");
   gist_table_xent_desc E;
-  GIST_TRY(check_table_xent("table_xent_workspace", D, &E));
+  GIST_TRY(check_table_xent("table_xent_workspace", D, gradients != 0, &E));
   if (gradients && E.store == GIST_STORE_E4M3)
     return set_error(GIST_E_INVAL, "table_xent_workspace: 8-bit operands have no gradients");
   *bytes = gist::table_xent_workspace(&E, gradients != 0);
@@ -1366,7 +1370,7 @@ extern "C" gist_status gist_table_xent(gist_ctx* ctx, const gist_table_xent_desc
   if (!ctx) return set_error(GIST_E_INVAL, "table_xent: NULL ctx");
   gist::ProfBind pb(ctx);
   gist_table_xent_desc E;
-  GIST_TRY(check_table_xent("table_xent", D, &E));
+  GIST_TRY(check_table_xent("table_xent", D, dH || dT, &E));
   if (!loss_dev) return set_error(GIST_E_INVAL, "table_xent: NULL loss");
   const bool eight = E.store == GIST_STORE_E4M3;
   // rows without entries have no gradient to point to

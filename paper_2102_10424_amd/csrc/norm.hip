@@ -8,9 +8,9 @@
 // held in the registers of 16 lanes, a wave, or a workgroup of 256 or 1,024; longer
 // rows are read twice (three times for codes).  Sums are fp32.  Both directions move 4.5 to 5 TB/s where
 // rows are whole 16-byte loads: 65,537 rows of 2,048 from fp32 to codes 134 us, 16,384 of 4,096 in bf16 with
-// residual and gradients 209 us.  A forward pass of 256 threads a row alone, long rows read again, took
-// 183 and 220 us there, 49 us for 100,000 rows of 64 in fp32 (now 11), and 180 us for 4,000 of
-// 16,384 in bf16 (now 111).
+// residual and gradients 209 us.  Held by a wave or 256 threads only, 32 elements a thread and a
+// branch a load, with long rows read again, these took 183 and 220 us, 100,000 rows of 64 in fp32
+// 49 us (now 11), and 4,000 of 16,384 in bf16 180 us (now 111).
 //
 // 8-bit rows: e4m3, the row's largest magnitude at 448, nearest even.
 //

@@ -1136,7 +1136,11 @@ class SubGCN:
 
     def adamw(self, params, head=None, weight_decay=0.01, eight=False):
         """An :class:`AdamW` over ``params`` (GAT: the attention vectors without decay) and, with
-        ``head``, its table and gain, which is not decayed."""
+        ``head``, its table and gain, which is not decayed.  A head with a loss scale is refused
+        (ValueError): its gradients are times that and the layers' are not, so its ``items`` take an
+        :class:`AdamW` of their own and ``grad_scale`` there."""
+        if head is not None and head.grad_scale != 1.0:
+            raise ValueError("a head with a loss scale needs an AdamW of its own")
         items = []
         for l in range(self.L):
             r = self.widths[l] if self.gat else params[l].shape[0]
@@ -1145,7 +1149,9 @@ class SubGCN:
                 items.append(dict(W=params[l][r:], dW=self.dW[l][r:]))
         if head is not None:
             items += head.items(weight_decay)
-        return AdamW(self.ctx, items, eight=eight, device=self.device)
+        opt = AdamW(self.ctx, items, eight=eight, device=self.device)
+        opt.of = (self, [p.data_ptr() for p in params])
+        return opt
 
     def step(self, batch, params, lr, adam=None, loss_out=None, muon=None, adamw=None, head=None,
              residual=None):
@@ -1157,6 +1163,9 @@ class SubGCN:
         steps and the other optimizers leave as they are."""
         if sum(o is not None for o in (adam, muon, adamw)) > 1:
             raise ValueError("one optimizer a step: adam, muon or adamw")
+        if adamw is not None and (adamw[0].of is None or adamw[0].of[0] is not self
+                                  or adamw[0].of[1] != [p.data_ptr() for p in params]):
+            raise ValueError("the AdamW is not this runner's adamw() of these weights")
         self.forward(batch, params)
         if head is None:
             if residual is not None:
@@ -1234,6 +1243,7 @@ class AdamW:
 
     def __init__(self, ctx, items, eight=False, device="cuda"):
         self.ctx, self.eight = ctx, eight
+        self.of = None         # the runner and the addresses of the weights that SubGCN.adamw made it for
         self.state, self._keep, tensors = [], [], []
         for i, it in enumerate(items):
             W, dW, copy = it["W"], it["dW"], it.get("copy")
@@ -1316,9 +1326,9 @@ class TableHead:
                 dict(W=self.gain, dW=self.dgain)]
 
     def _reserve(self, n):
-        if n > self.n_cap:
-            self._kept.append(self.b)
-            self.n_cap = n = max(n, 2 * self.n_cap)     # what is kept adds up to less than what is in use
+        if n > self.n_cap or self.b is None:
+            self._outgrown(self.b)
+            self.n_cap = n = max(1, _grown(n, self.n_cap, self.ctx))
             f = lambda *s, t=torch.float32: torch.empty(*s, dtype=t, device=self.device)
             self.b = dict(h=f(n, self.d), y=f(n, self.d, t=self.dtype), dy=f(n, self.d, t=self.dtype),
                           rstd=f(n), logp=f(n), lse=f(n), y8=f(n, self.d, t=torch.uint8), ys=f(n),
@@ -1333,9 +1343,14 @@ class TableHead:
         need = max(16, G.gist_table_xent_workspace(desc, gradients))
         ws = self.ws.get(gradients)
         if ws is None or ws.numel() < need:
-            self._kept.append(ws)
+            self._outgrown(ws)
+            need = _grown(need, 0 if ws is None else ws.numel(), self.ctx)
             ws = self.ws[gradients] = torch.empty(need, dtype=torch.uint8, device=self.device)
         return ws
+
+    def _outgrown(self, buffers):
+        if buffers is not None and _recorded(self.ctx):
+            self._kept.append(buffers)
 
     def prepare(self, n, gradients=True):
         """Allocate every buffer a call on ``n`` rows needs (before a capture)."""

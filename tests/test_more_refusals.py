@@ -327,3 +327,65 @@ def test_table_head_keeps_outgrown_buffers():
     head.prepare(5000)
     assert all(r() is not None for r in refs) and head.n_cap >= 5000
     assert head.ws[True].numel() >= S.G.gist_table_xent_workspace(head._desc(5000, head.store), True)
+
+
+def test_table_xent_most_classes():
+    """bf16 products' gradients address 256 rows of exponentials in 32 bits."""
+    for store, dtype, limit in ((1, 0, 23), (0, G.GIST_DTYPE_BF16_IN, 23), (2, 0, 29), (0, 0, 29)):
+        d = lambda C: G.table_xent_desc(1, C, 4, store, dtype)
+        assert G.gist_table_xent_workspace(d(1 << limit), True) > 0
+        refused(UNSUP, G.gist_table_xent_workspace, d((1 << limit) + 1), True)
+        refused(UNSUP, G.gist_table_xent, ctx, d((1 << limit) + 1), A, None, B, None, I, None, D, None, None,
+                E, F, Ws(1 << 50))
+        assert G.gist_table_xent_workspace(d(1 << 29), False) > 0
+        refused(UNSUP, G.gist_table_xent_workspace, d((1 << 29) + 1), False)
+
+
+def test_table_head_replaces_outgrown_buffers_without_a_recording():
+    import types
+    import weakref
+    import torch
+    from paper_2102_10424_amd import step as S
+    head = S.TableHead(types.SimpleNamespace(captures=0), torch.zeros(50, 5), n_cap=16, device="cpu")
+    head.prepare(16)
+    refs = [weakref.ref(t) for t in head.b.values()] + [weakref.ref(head.ws[True])]
+    head.prepare(5000)
+    assert all(r() is None for r in refs) and head.n_cap == 5000 and not head._kept
+
+
+def test_table_head_of_an_empty_batch(monkeypatch):
+    import torch
+    from paper_2102_10424_amd import step as S
+    calls = []
+    for name in ("gist_rms_norm", "gist_rms_norm_bwd", "gist_table_xent", "gist_gcn_layer_fwd"):
+        monkeypatch.setattr(S.G, name, lambda *a, name=name: calls.append(name))
+    head = S.TableHead(None, torch.zeros(50, 5), device="cpu")
+    run, b = S.SubGCN(None, "gcn", [8, 24, 5], 16, device="cpu"), CpuBatch(0)
+    head.loss_and_grad(run, b)
+    head.score(run, b)
+    assert calls == ["gist_rms_norm", "gist_table_xent", "gist_rms_norm_bwd", "gist_rms_norm", "gist_table_xent"]
+
+
+def test_adamw_belongs_to_its_runner_and_weights(monkeypatch):
+    import torch
+    from paper_2102_10424_amd import step as S
+    calls = []
+    for name in ("gist_gcn_layer_fwd", "gist_gcn_layer_bwd", "gist_rms_norm", "gist_rms_norm_bwd",
+                 "gist_table_xent", "gist_softmax_xent", "gist_adamw_update"):
+        monkeypatch.setattr(S.G, name, lambda *a, name=name: calls.append(name))
+    run, b = S.SubGCN(None, "gcn", [8, 24, 5], 16, device="cpu"), CpuBatch(16)
+    weights = lambda: [torch.zeros(8, 24), torch.zeros(24, 5)]
+    params = weights()
+    for gs in (2.0, 0.5):
+        with pytest.raises(ValueError):
+            run.adamw(params, S.TableHead(None, torch.zeros(50, 5), grad_scale=gs, device="cpu"))
+    head = S.TableHead(None, torch.zeros(50, 5), device="cpu")
+    opt = run.adamw(params, head)
+    twin = S.SubGCN(None, "gcn", [8, 24, 5], 16, device="cpu")
+    for r, p, o in ((run, weights(), opt), (twin, params, opt), (run, params[::-1], opt),
+                    (run, params, S.AdamW(None, head.items(), device="cpu"))):
+        with pytest.raises(ValueError):
+            r.step(b, p, 0.1, adamw=(o, 1), head=head)
+    assert not calls
+    run.step(b, params, 0.1, adamw=(opt, 1), head=head)
+    assert calls[-1] == "gist_adamw_update"
