@@ -645,8 +645,7 @@ gist_status gist_quantize_rows(gist_ctx* ctx, int64_t n, int32_t d, const void* 
  *   GIST_STORE_BF16 / F16 (dtype ignored)    operands as stored, exponentials
  *         rounded to bf16 / fp16, fp32 sums; gradients rounded once to `store`
  *   GIST_STORE_E4M3   h_v = code h_scale[v], t_j = code t_scale[j] (fp32 scales,
- *         NULL for the other stores); no gradients.  Sums of 8-bit products lose
- *         bits below 2^-13 of their largest term.
+ *         NULL for the other stores); no gradients.  fp32 sums of exact products.
  * logp and lse (n fp32 each) may be NULL.  Sums and statistics are fp32.
  * `ws` needs gist_table_xent_workspace() bytes for this descriptor (gradients:
  * whether the call has any).  Results are deterministic.  Errors: GIST_E_INVAL (negative n, C < 1,

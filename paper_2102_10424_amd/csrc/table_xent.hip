@@ -33,7 +33,8 @@
 // fp32 operands (GIST_DTYPE_F32): rows piece by piece through the library's fp32
 // products, with one kernel between them that turns a piece's logits into G.
 //
-// 8-bit operands: forward only, twice the products per step.
+// 8-bit operands: forward only.  They travel as bytes and are widened to bf16, which holds every e4m3
+// value, in front of the matrix instruction.
 
 #include <algorithm>
 
@@ -150,6 +151,21 @@ struct Frag<GIST_STORE_E4M3> {   // 32 values of K a lane
   intx8 v;
 };
 
+// Eight of a lane's 8-bit values in bf16, which holds all of them.  8-bit matrix instructions lose what
+// lies below some 2^-13 of the largest of a few products, 1.6e-5 of the sums' rms whatever
+// their depth, and with it log probabilities of short rows their fifth digit; sums of bf16 products are
+// fp32's (4e-8).  The price: 4,093 rows of 1,024 against 50,001 classes 385 us, 8-bit
+// instructions 280; one row of 2,048 against 131,072 classes 63 and 62.
+__device__ __forceinline__ bf16x8 bf16_of(const Frag<GIST_STORE_E4M3>& f, int s) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  union { bf16x8 v; bf16x2 p[4]; } u;
+  u.p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(f.v[2 * s], 1.f, false);
+  u.p[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(f.v[2 * s], 1.f, true);
+  u.p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(f.v[2 * s + 1], 1.f, false);
+  u.p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(f.v[2 * s + 1], 1.f, true);
+  return u.v;
+}
+
 // 16 x 16 blocks: they take half the passes over the accumulators that 32 x 32 ones do, and
 // power is what bounds the products (alone, on random bf16 operands, 2,050 TFLOP/s, 32 x 32
 // ones 1,810).
@@ -159,8 +175,11 @@ __device__ __forceinline__ floatx4 mma(const Frag<STORE>& a, const Frag<STORE>& 
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a.v), __builtin_bit_cast(bf16x8, b.v), c, 0, 0, 0);
   else if constexpr (STORE == GIST_STORE_F16)
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, a.v), __builtin_bit_cast(half8, b.v), c, 0, 0, 0);
-  else   // block scales of 1 (exponent 127)
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a.v, b.v, c, 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);
+  else {
+#pragma unroll
+    for (int s = 0; s < 4; ++s) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf16_of(a, s), bf16_of(b, s), c, 0, 0, 0);
+    return c;
+  }
 }
 
 // One operand's share of a step in LDS, ROWS of its own index by 128 bytes of K.

@@ -114,11 +114,12 @@ def table_xent_bounds(H, T, y, scale, r, op, store):
 
     A logit: products of two 16-bit values are exact in fp32 (those of fp32 values carry 2^-22
     each), every one of d additions loses at most 2 u (a matrix instruction may cut instead of
-    rounding) of the terms' magnitudes; 8-bit products keep 13 bits below their largest."""
+    rounding) of the terms' magnitudes.  8-bit values are widened exactly; their scales are
+    fp32 factors (2 u more)."""
     H, T = np.asarray(H, np.float64), np.asarray(T, np.float64)
     n, C, d = H.shape[0], T.shape[0], H.shape[1]
     mag = abs(scale) * (np.abs(H) @ np.abs(T).T)
-    ez = mag * (2.0 ** -12 if op == "e4m3" else 2 * U32 * (d + 16))
+    ez = mag * 2 * U32 * (d + 16)
     lse = ez.max(1) + lse_bound(r["z"]) + 4 * U32 * np.abs(r["lse"])
     yy = np.clip(y, 0, C - 1)
     at = np.arange(n)

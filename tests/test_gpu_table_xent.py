@@ -332,3 +332,55 @@ def test_same_bits_again_and_replayed(G, ctx, store):
         assert torch.equal(got[0][:1], first[0][:1])
         for a, b, m in zip(got[1:], first[1:], (200, 200, 200, 700)):
             assert torch.equal(a[:m], b[:m]), k
+
+
+def test_rows_cut_over_many_classes(G, ctx):
+    """fp32 rows whose classes several workgroups share: a row that holds a NaN, labels of C or more
+    and none, rows behind the batch's last, and again the same bits."""
+    rng = np.random.default_rng(21)
+    n, C, d = 40, 13000, 20
+    H, T, y = inputs(n, C, d, rng, 0.2)
+    y[:3] = 0, 4095, C - 1
+    out, Hv, Tv, args = run(G, ctx, H, T, y, "f32", n_valid=35)
+    check(out, Hv, Tv, y, "f32", n_valid=35)
+    assert (out["logp"][35:] == 0).all() and (out["dH"][35:] == 0).all()
+    before = [a.clone() for a in (args[8], args[9], args[10])]
+    G.gist_table_xent(*args)
+    assert all(bool((a == b).all()) for a, b in zip(before, (args[8], args[9], args[10])))
+    y[7] = C
+    H[11, 5], y[11] = np.nan, 6
+    out, _, _, _ = run(G, ctx, H, T, y, "f32")
+    assert np.isnan(out["loss"]) and np.isnan(out["logp"][[7, 11]]).all() and np.isnan(out["lse"][11])
+    rest = np.delete(np.arange(n), [7, 11])
+    assert np.isfinite(out["logp"][rest]).all() and np.isfinite(out["dH"][rest]).all()
+    assert np.isnan(out["dH"][11]).all() and np.isnan(out["dT"]).all()
+
+
+@pytest.mark.parametrize("n,C", [(3, 300), (70, 200), (200, 1000)])
+def test_nan_codes(G, ctx, n, C):
+    """An 8-bit row that holds NaN's code makes its own results NaN, a class's code all rows'."""
+    import torch
+    rng = np.random.default_rng(n)
+    H, T, y = inputs(n, C, 72, rng, 0.0)
+    for of in (2, 4):
+        _, _, _, args = run(G, ctx, H, T, y, "e4m3", grad=False)
+        args[of][72 + 5] = 0x7f                # row 1
+        G.gist_table_xent(*args)
+        lse, logp = to_host(args[10])[:n], to_host(args[9])[:n]
+        assert np.isnan(float(args[8][0]))
+        if of == 2:
+            assert np.isnan(lse[1]) and np.isnan(logp[1])
+            assert np.isfinite(np.delete(lse, 1)).all() and np.isfinite(np.delete(logp, 1)).all()
+        else:
+            assert np.isnan(lse).all() and np.isnan(logp).all()
+
+
+@pytest.mark.parametrize("n,C,d", [(1, 3, 128), (5, 70, 16), (33, 130, 64), (300, 2000, 128)])
+def test_8_bit_rows_of_unequal_terms(G, ctx, n, C, d):
+    """Terms from 2^-18 to 2^17 in one sum, as 8-bit values allow: all of them count."""
+    rng = np.random.default_rng(d)
+    H, T, y = inputs(n, C, d, rng)
+    H *= np.exp2(rng.integers(-9, 1, (1, d))).astype(np.float32)
+    T *= np.exp2(rng.integers(-9, 1, (1, d))).astype(np.float32)
+    out, Hv, Tv, _ = run(G, ctx, H, T, y, "e4m3", grad=False)
+    check(out, Hv, Tv, y, "e4m3", grad=False)
