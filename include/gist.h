@@ -756,7 +756,7 @@ typedef struct gist_adamw_tensor {
  * Errors: GIST_E_INVAL (as gist_adam_update; count or an n negative, unknown
  * stores, one scale array without the other, a non-finite weight_decay or
  * grad_scale, NULL or equal pointers among a tensor's W, dW, m, v and copy),
- * GIST_E_UNSUPPORTED (an n of 2^34 or more).  All tensors are checked before
+ * GIST_E_UNSUPPORTED (an n above 2^33).  All tensors are checked before
  * anything is launched.  Arrays of different tensors must not overlap. */
 gist_status gist_adamw_update(gist_ctx* ctx, const gist_adamw_tensor* tensors, int64_t count,
                               float lr, float beta1, float beta2, float eps, int64_t step,

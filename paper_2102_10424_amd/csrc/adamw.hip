@@ -14,7 +14,10 @@
 // step can be repeated bit for bit.  A sqrt(v) above zero is not rounded to zero: m over
 // eps alone would be a step of any size.
 //
-// Bound by memory: 28 bytes an element in fp32, 16 with 8-bit moments.
+// Bound by memory: 28 bytes an element in fp32, 16 with 8-bit moments, bf16 gradients and a bf16 copy.  A
+// table of 131,072 x 1,024 and five more tensors in 8 bits: 731 us (3.25 GB, 4.45 TB/s).  A workgroup
+// takes 1,024 elements; four times as many take 5 us longer of 95 (4,096 x 4,096, fp32 moments, bf16
+// gradients) and are no better in the others.
 
 #include "elem.cuh"
 
@@ -23,7 +26,7 @@ namespace gist {
 namespace {
 
 constexpr int kBlock = 256;
-constexpr int kPiece = 4 * kBlock;      // elements a workgroup takes at a time
+constexpr int kPiece = 4 * kBlock;      // elements of a workgroup
 constexpr int kMostTensors = 40;        // of one launch: their addresses are kernel arguments (4 KB)
 constexpr int64_t kMostGroups = int64_t{1} << 23;
 constexpr float kTop = 448.f;           // largest e4m3 value
@@ -49,7 +52,7 @@ struct Args {
   const float* coef_dev;
   float step_size, inv_sqrt_bc2, lr, gscale, beta1, beta2, eps;
   unsigned seed;
-  int fresh, count, pieces;    // pieces: of one workgroup
+  int fresh, count;
 };
 static_assert(sizeof(Args) <= 4096, "kernel arguments");
 
@@ -256,18 +259,15 @@ __global__ __launch_bounds__(kBlock) void adamw_kernel(Args a) {
   }
   c.keep = 1.f - lr * t.decay;
   const unsigned key = mix(seed ^ (t.place * 0x9e3779b9u));
-  const int64_t e0 = static_cast<int64_t>(b - t.first) * a.pieces * kPiece;
-  for (int i = 0; i < a.pieces; ++i) {
-    const int64_t e = e0 + static_cast<int64_t>(i) * kPiece;
-    if (t.eight) {
-      if (t.grad == GIST_STORE_F32) piece<GIST_STORE_F32, true>(t, c, fresh, key, e);
-      else if (t.grad == GIST_STORE_BF16) piece<GIST_STORE_BF16, true>(t, c, fresh, key, e);
-      else piece<GIST_STORE_F16, true>(t, c, fresh, key, e);
-    } else {
-      if (t.grad == GIST_STORE_F32) piece<GIST_STORE_F32, false>(t, c, fresh, key, e);
-      else if (t.grad == GIST_STORE_BF16) piece<GIST_STORE_BF16, false>(t, c, fresh, key, e);
-      else piece<GIST_STORE_F16, false>(t, c, fresh, key, e);
-    }
+  const int64_t e = static_cast<int64_t>(b - t.first) * kPiece;
+  if (t.eight) {
+    if (t.grad == GIST_STORE_F32) piece<GIST_STORE_F32, true>(t, c, fresh, key, e);
+    else if (t.grad == GIST_STORE_BF16) piece<GIST_STORE_BF16, true>(t, c, fresh, key, e);
+    else piece<GIST_STORE_F16, true>(t, c, fresh, key, e);
+  } else {
+    if (t.grad == GIST_STORE_F32) piece<GIST_STORE_F32, false>(t, c, fresh, key, e);
+    else if (t.grad == GIST_STORE_BF16) piece<GIST_STORE_BF16, false>(t, c, fresh, key, e);
+    else piece<GIST_STORE_F16, false>(t, c, fresh, key, e);
   }
 }
 
@@ -275,8 +275,6 @@ __global__ __launch_bounds__(kBlock) void adamw_kernel(Args a) {
 
 gist_status adamw(hipStream_t st, const gist_adamw_tensor* T, int64_t count, const float* coef, float beta1,
                   float beta2, float eps, const float* coef_dev) {
-  int64_t total = 0;
-  for (int64_t i = 0; i < count; ++i) total += (T[i].n + kPiece - 1) / kPiece;
   Args a{};
   a.coef_dev = coef_dev;
   if (coef) {
@@ -290,14 +288,13 @@ gist_status adamw(hipStream_t st, const gist_adamw_tensor* T, int64_t count, con
   a.beta1 = beta1;
   a.beta2 = beta2;
   a.eps = eps;
-  a.pieces = total > 8192 ? 4 : 1;
   for (int64_t i = 0; i < count;) {
     a.count = 0;
     int64_t groups = 0;
     double bytes = 0.0;
     while (i < count && a.count < kMostTensors) {
       const gist_adamw_tensor& s = T[i];
-      const int64_t g = (s.n + static_cast<int64_t>(kPiece) * a.pieces - 1) / (static_cast<int64_t>(kPiece) * a.pieces);
+      const int64_t g = (s.n + kPiece - 1) / kPiece;
       if (g > 0) {
         if (groups + g > kMostGroups && a.count > 0) break;
         Tensor& t = a.t[a.count++];

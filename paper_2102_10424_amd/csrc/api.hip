@@ -1410,7 +1410,7 @@ gist_status check_adamw(const char* what, const gist_adamw_tensor* T, int64_t co
   for (int64_t i = 0; i < count; ++i) {
     const gist_adamw_tensor& t = T[i];
     if (t.n < 0) return bad(what, GIST_E_INVAL, ": negative n");
-    if (t.n >= (int64_t{1} << 34)) return bad(what, GIST_E_UNSUPPORTED, ": n of 2^34 or more");
+    if (t.n > (int64_t{1} << 33)) return bad(what, GIST_E_UNSUPPORTED, ": n above 2^33");
     if (!known_store(t.grad_store)) return bad(what, GIST_E_INVAL, ": unknown store of a gradient");
     if (t.copy && t.copy_store != GIST_STORE_BF16 && t.copy_store != GIST_STORE_F16)
       return bad(what, GIST_E_INVAL, ": a copy is bf16 or fp16");
