@@ -830,12 +830,12 @@ __device__ __forceinline__ int count_labels(int64_t n, const int32_t* __restrict
 }
 
 // What comes before a piece's products, each by workgroups of its own in one launch (a launch is
-// some 3 us, which small problems consist of): the rows' first references scale <h, t_y>, a wave a row, 16
-// bytes a lane, and cleared marks of far rows; no class has a slot yet; and the gradients'
+// some 3 us, which small problems consist of): the rows' first references scale <h, t_y>, 16 bytes a
+// lane of as many lanes as a row has of them (8 to 64), and cleared marks of far rows; no class has a slot yet; and the gradients'
 // factor.  `slots`, `factor`: or NULL.
 struct Begin {
   int64_t row0, n, C, total;   // total: rows of all pieces
-  int wide;
+  int wide, lanes;
   float scale, gscale;
   const char* H;
   const char* T;
@@ -863,14 +863,14 @@ __global__ __launch_bounds__(kBegin) void begin_kernel(Begin a) {
     if (c < a.C) a.slots[c] = kNoSlot;
     return;
   }
-  const int64_t row = b * (kBegin / 64) + (threadIdx.x >> 6);
-  const int lane = threadIdx.x & 63;
-  if (row >= a.n) return;
+  const int lane = threadIdx.x & (a.lanes - 1);
+  const int64_t row = (b * kBegin + threadIdx.x) / a.lanes;
+  if (row >= a.n) return;                          // all of a row's lanes
   if (row % 256 == 0 && lane == 0) a.far[row / 256] = 0;
   const int y = !a.n_dev || a.row0 + row < *a.n_dev ? a.labels[row] : -1;
   float s = 0.f;
   if (y >= 0 && y < a.C) {
-    for (int c = lane * 8; c < a.wide; c += 512) {
+    for (int c = lane * 8; c < a.wide; c += a.lanes * 8) {
       float h[8], t[8];
       load_vec<GIST_STORE_BF16, 8>(a.H + row * a.ldh, c, h);
       load_vec<GIST_STORE_BF16, 8>(a.T + y * a.ldt, c, t);
@@ -878,35 +878,53 @@ __global__ __launch_bounds__(kBegin) void begin_kernel(Begin a) {
       for (int q = 0; q < 8; ++q) s = fmaf(h[q], t[q], s);
     }
   }
-  s = wave_sum(s) * a.scale;
+  for (int o = a.lanes >> 1; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+  s *= a.scale;
   // a reference that is no number would spoil rows whose own logits are; their results are NaN by themselves
   if (lane == 0) a.ref[row] = fabsf(s) < 1e30f ? s : 0.f;
 }
 
-// Loss and the gradients' factor; one workgroup, every thread a stride of rows, in a fixed order.
+// Loss and the gradients' factor, in a fixed order: every workgroup a share of the rows, every
+// thread a stride of it.  One workgroup gives the results; several leave theirs in `parts`, and a
+// second launch of one joins them (200,000 rows by one workgroup: 30 us).
+constexpr int64_t kLossRows = 16384;   // of a workgroup
+constexpr int kLossParts = 256;        // at most
+struct LossPart {
+  double sum;
+  int64_t count;
+};
 __global__ __launch_bounds__(1024) void loss_kernel(int64_t n, const float* __restrict__ logp,
                                                     const int32_t* __restrict__ labels, const int32_t* __restrict__ n_dev,
-                                                    float gscale, float* __restrict__ loss, float* __restrict__ factor) {
+                                                    float gscale, int64_t share, LossPart* __restrict__ parts, int joined,
+                                                    float* __restrict__ loss, float* __restrict__ factor) {
   __shared__ double sh[16];
-  __shared__ int sc[16];
-  int64_t real = n_dev ? max(0, *n_dev) : n;
-  real = real < n ? real : n;
+  __shared__ int64_t sc[16];
   double s = 0.0;
-  int c = 0;
-  const int64_t whole = real / 4;
-#pragma unroll 4
-  for (int64_t i = threadIdx.x; i < whole; i += 1024) {   // as count_labels reads
-    const floatx4 p = *reinterpret_cast<const floatx4*>(logp + i * 4);
-    const intx4w v = *reinterpret_cast<const intx4w*>(labels + i * 4);
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      s += p[q];
-      c += v[q] >= 0;
+  int64_t c = 0;
+  if (joined > 0) {      // parts of the launch before
+    if (threadIdx.x < joined) {
+      s = parts[threadIdx.x].sum;
+      c = parts[threadIdx.x].count;
     }
-  }
-  for (int64_t i = whole * 4 + threadIdx.x; i < real; i += 1024) {
-    s += logp[i];
-    c += labels[i] >= 0;
+  } else {
+    int64_t real = n_dev ? max(0, *n_dev) : n;
+    real = real < n ? real : n;
+    const int64_t first = blockIdx.x * share, last = min(real, first + share);   // share: a multiple of 4
+    const int64_t whole = first + max(int64_t{0}, last - first) / 4 * 4;
+#pragma unroll 4
+    for (int64_t i = first + threadIdx.x * 4; i < whole; i += 4096) {   // as count_labels reads
+      const floatx4 p = *reinterpret_cast<const floatx4*>(logp + i);
+      const intx4w v = *reinterpret_cast<const intx4w*>(labels + i);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        s += p[q];
+        c += v[q] >= 0;
+      }
+    }
+    for (int64_t i = whole + threadIdx.x; i < last; i += 1024) {
+      s += logp[i];
+      c += labels[i] >= 0;
+    }
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) {
@@ -924,6 +942,10 @@ __global__ __launch_bounds__(1024) void loss_kernel(int64_t n, const float* __re
   for (int w = 0; w < 16; ++w) {
     s += sh[w];
     c += sc[w];
+  }
+  if (gridDim.x > 1) {
+    parts[blockIdx.x] = LossPart{s, c};
+    return;
   }
   *loss = c > 0 ? static_cast<float>(-s / c) : 0.f;
   if (factor) *factor = c > 0 ? gscale / static_cast<float>(c) : 0.f;
@@ -977,64 +999,89 @@ __global__ __launch_bounds__(kBlock) void join_out_kernel(int64_t rows, int d, i
   }
 }
 
-// fp32 pieces: a row's logits (a product's, not yet scaled) become its G, times the factor.  A
-// workgroup a row; three passes over it, the last two out of the cache.
+// fp32 pieces: a row's logits (a product's, not yet scaled) become its G, times the factor.  A row in the
+// registers of THREADS threads, CH loads of four each: read once, written once.  200,000 rows of
+// 41 classes, d 256, with gradients: 664 us by 256 threads a row and three reads (and one workgroup's loss), 370 so.
+template <int THREADS, int CH>
 __global__ __launch_bounds__(kBlock) void piece_kernel(int64_t row0, int64_t rows, int64_t n, int64_t C, float scale,
                                                        float* __restrict__ Z, int64_t ldz, const int32_t* __restrict__ labels,
                                                        const int32_t* __restrict__ n_dev, const float* __restrict__ factor,
                                                        int grad, float* __restrict__ lse_out, float* __restrict__ logp,
                                                        float* __restrict__ logp_out) {
   __shared__ float sm[kBlock / 64], ss[kBlock / 64];
+  constexpr int RB = kBlock / THREADS;
+  const int lane = threadIdx.x % THREADS;
   const int64_t real = n_dev ? max(0, *n_dev) : n;
   const float f = grad ? *factor : 0.f;
-  for (int64_t i = blockIdx.x; i < rows; i += gridDim.x) {
+  for (int64_t i = blockIdx.x * static_cast<int64_t>(RB) + threadIdx.x / THREADS; i < rows;
+       i += static_cast<int64_t>(gridDim.x) * RB) {
     float* const z = Z + i * ldz;
     const int64_t row = row0 + i;
     const int y = row < real ? labels[row] : -1;
-    float m = -__builtin_inff(), s = 0.f;
-    // ldz is a multiple of 4
-    for (int64_t c = threadIdx.x * 4; c < C; c += kBlock * 4) {
-      const floatx4 v = *reinterpret_cast<const floatx4*>(z + c);
+    floatx4 v[CH];
+    float m = -__builtin_inff();
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
-        if (c + q < C) m = fmaxf(m, v[q] * scale);
+    for (int h = 0; h < CH; ++h) {
+      const int64_t c = (h * THREADS + lane) * 4;
+      v[h] = floatx4{} - __builtin_inff();
+      if (c < C) {     // ldz is a multiple of 4
+        const floatx4 t = *reinterpret_cast<const floatx4*>(z + c);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          if (c + q < C) v[h][q] = t[q] * scale;
+      }
+#pragma unroll
+      for (int q = 0; q < 4; ++q) m = fmaxf(m, v[h][q]);
     }
-    m = wave_max(m);
-    if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = m;
-    __syncthreads();
-    m = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
+#pragma unroll
+    for (int o = (THREADS < 64 ? THREADS : 64) / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+    if constexpr (THREADS > 64) {
+      if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = m;
+      __syncthreads();
+      m = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
+    }
     const float ref = m == -__builtin_inff() ? 0.f : m;
-    for (int64_t c = threadIdx.x * 4; c < C; c += kBlock * 4) {
-      const floatx4 v = *reinterpret_cast<const floatx4*>(z + c);
-      float p = 0.f;
+    float s = 0.f;
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
-        if (c + q < C) p += ex2((v[q] * scale - ref) * kL);
-      s += p;
+    for (int h = 0; h < CH; ++h) {
+      float p[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) p[q] = ex2((v[h][q] - ref) * kL);
+      s += (p[0] + p[1]) + (p[2] + p[3]);
     }
-    s = wave_sum(s);
-    if ((threadIdx.x & 63) == 0) ss[threadIdx.x >> 6] = s;
-    __syncthreads();
-    s = (ss[0] + ss[1]) + (ss[2] + ss[3]);
+#pragma unroll
+    for (int o = (THREADS < 64 ? THREADS : 64) / 2; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+    if constexpr (THREADS > 64) {
+      if ((threadIdx.x & 63) == 0) ss[threadIdx.x >> 6] = s;
+      __syncthreads();
+      s = (ss[0] + ss[1]) + (ss[2] + ss[3]);
+    }
     const float ls = lg2(s) * kLn2;
-    if (threadIdx.x == 0) {
-      const float lp = y < 0 ? 0.f : y >= C ? __builtin_nanf("") : z[y] * scale - m - ls;
-      logp[row] = lp;
-      if (logp_out) logp_out[row] = lp;
+    if (lane == 0) {
       if (lse_out) lse_out[row] = m + ls;
+      if (y < 0 || y >= C) {
+        const float lp = y < 0 ? 0.f : __builtin_nanf("");
+        logp[row] = lp;
+        if (logp_out) logp_out[row] = lp;
+      }
     }
-    __syncthreads();   // z[y] is read
-    if (!grad) continue;
     const float fs = y < 0 ? 0.f : f;
-    for (int64_t c = threadIdx.x * 4; c < ldz; c += kBlock * 4) {
-      floatx4 v = *reinterpret_cast<const floatx4*>(z + c);
+#pragma unroll
+    for (int h = 0; h < CH; ++h) {
+      const int64_t c = (h * THREADS + lane) * 4;
+      floatx4 g;
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        float p = ex2((v[q] * scale - m - ls) * kL);
-        if (c + q == y) p -= 1.f;
-        v[q] = y < 0 || c + q >= C ? 0.f : p * fs;
+        float p = ex2((v[h][q] - m - ls) * kL);
+        if (c + q == y && y < C) {
+          const float lp = v[h][q] - m - ls;
+          logp[row] = lp;
+          if (logp_out) logp_out[row] = lp;
+          p -= 1.f;
+        }
+        g[q] = y < 0 || c + q >= C ? 0.f : p * fs;
       }
-      *reinterpret_cast<floatx4*>(z + c) = v;
+      if (grad && c < ldz) *reinterpret_cast<floatx4*>(z + c) = g;
     }
   }
 }
@@ -1117,16 +1164,19 @@ __global__ __launch_bounds__(1024) void count_kernel(int64_t n, const int32_t* _
   if (threadIdx.x == 0) *factor = c > 0 ? gscale / static_cast<float>(c) : 0.f;
 }
 
-// Rows of fp32 with those that are not labelled zeroed.
+// Rows of fp32 with those that are not labelled zeroed; four elements a thread.
 __global__ __launch_bounds__(kBlock) void mask_rows_kernel(int64_t row0, int64_t rows, int64_t n, int d, const float* __restrict__ x,
                                                            int64_t ldx, float* __restrict__ y, const int32_t* __restrict__ labels,
                                                            const int32_t* __restrict__ n_dev) {
   const int64_t real = n_dev ? max(0, *n_dev) : n;
-  for (int64_t e = blockIdx.x * static_cast<int64_t>(kBlock) + threadIdx.x; e < rows * d;
+  const int per = (d + 3) / 4;
+  for (int64_t e = blockIdx.x * static_cast<int64_t>(kBlock) + threadIdx.x; e < rows * per;
        e += static_cast<int64_t>(gridDim.x) * kBlock) {
-    const int64_t i = e / d, c = e - i * d;
-    const bool live = row0 + i < real && labels[row0 + i] >= 0;
-    y[e] = live ? x[(row0 + i) * ldx + c] : 0.f;
+    const int64_t i = e / per;
+    const int c = static_cast<int>(e - i * per) * 4;
+    float v[4] = {};
+    if (row0 + i < real && labels[row0 + i] >= 0) load_some<GIST_STORE_F32, 4>(x, (row0 + i) * ldx + c, d - c, 0.f, v);
+    store_some<GIST_STORE_F32, 4>(y, i * d + c, d - c, v);
   }
 }
 
@@ -1183,7 +1233,7 @@ Cut cut_of(int64_t M, int64_t N, int steps) {
 Cut cut_logits(int64_t C, int64_t n, int steps, bool eight) {
   Cut c{};
   if (n <= 32) c.tile = 32;
-  else if (!eight && ((C + 255) / 256) * ((n + 255) / 256) >= 128) c.tile = 256;
+  else if (!eight && C > 128 && ((C + 255) / 256) * ((n + 255) / 256) >= 128) c.tile = 256;
   else c.tile = 128;
   const int bm = c.tile == 128 ? 128 : 256, bn = c.tile;
   c.tiles_m = static_cast<int>((C + bm - 1) / bm);
@@ -1205,7 +1255,7 @@ struct Plan {
   Cut dh, dt;               // the gradients' products, of the first piece
   bool exps;                // rows piece by piece, by their exponentials
   bool parts_h;             // dH is summed in fp32 parts
-  size_t h, hm, t, stats, zy, lse, logp, factor, g, ref, row_factor, far, pm1, ids, y, embed, slots,
+  size_t h, hm, t, stats, zy, lse, logp, factor, loss_parts, g, ref, row_factor, far, pm1, ids, y, embed, slots,
       slot_ids, kept, part, z, gemm, total;
   size_t gemm_bytes;
 };
@@ -1233,6 +1283,7 @@ Plan plan_of(const gist_table_xent_desc* D, const void* H, const void* T, bool g
   };
   p.logp = take(static_cast<size_t>(n) * 4);
   p.factor = take(16);
+  p.loss_parts = take(kLossParts * sizeof(LossPart));
   if (p.f32) {
     p.wide = up(C, 4);
     int64_t rows = static_cast<int64_t>(kPieceBytes / 4) / p.wide;
@@ -1361,6 +1412,19 @@ void copy_rows(hipStream_t st, int64_t n, int64_t n_pad, int d, int64_t wide, co
                      static_cast<int>(wide), x, ldx, y, labels, n_dev);
 }
 
+gist_status run_loss(hipStream_t st, int64_t n, const float* logp, const int32_t* labels, const int32_t* n_dev, float gscale,
+                     LossPart* parts, float* loss, float* factor) {
+  ProfScope ps(st, "table_xent_loss", 0.0, 8.0 * n);
+  const int64_t share = std::max(kLossRows, up((n + kLossParts - 1) / kLossParts, 4));
+  const int blocks = static_cast<int>((n + share - 1) / share);
+  hipLaunchKernelGGL(loss_kernel, dim3(static_cast<unsigned>(blocks)), dim3(1024), 0, st, n, logp, labels, n_dev, gscale, share,
+                     parts, 0, loss, factor);
+  if (blocks > 1)
+    hipLaunchKernelGGL(loss_kernel, dim3(1), dim3(1024), 0, st, n, logp, labels, n_dev, gscale, share, parts, blocks, loss,
+                       factor);
+  return check_launch("table_xent_loss");
+}
+
 // The same cut for fewer rows (N).
 Cut cut_rows(Cut c, int64_t N) {
   c.tiles_n = static_cast<int>((N + c.tile - 1) / c.tile);
@@ -1430,7 +1494,9 @@ gist_status run16(hipStream_t st, const gist_table_xent_desc* D, const Plan& p, 
         b.far = far;
         b.slots = slots;
         b.factor = f32(p.factor);
-        b.ref_blocks = (rn + kBegin / 64 - 1) / (kBegin / 64);
+        b.lanes = 8;
+        while (b.lanes < 64 && b.lanes * 8 < b.wide) b.lanes *= 2;
+        b.ref_blocks = (rn * b.lanes + kBegin - 1) / kBegin;
         b.slot_blocks = straight ? (C + kBegin - 1) / kBegin : 0;
         ProfScope ps(st, "table_xent_begin", 0.0, 4.0 * rn * d);
         hipLaunchKernelGGL(begin_kernel, dim3(static_cast<unsigned>(b.ref_blocks + b.slot_blocks + (r0 == 0))), dim3(kBegin), 0,
@@ -1452,16 +1518,16 @@ gist_status run16(hipStream_t st, const gist_table_xent_desc* D, const Plan& p, 
     {
       const int parts = c.tiles_m * waves_m(c.tile);
       ProfScope ps(st, "table_xent_join", 0.0, 8.0 * parts * rn);
-      const int per = rn <= 256 ? 4 : 32;
-      const dim3 grid(static_cast<unsigned>((rn + per - 1) / per));
-      float* const lse_out = lse ? lse + r0 : nullptr;
-      float* const logp_out = logp ? logp + r0 : nullptr;
-      if (per == 4)
-        hipLaunchKernelGGL(join_stats_kernel<4>, grid, dim3(1024), 0, st, r0, rn, C, parts, a.stats, rn, a.zy, a.labels, n_dev,
-                           f32(p.lse) + r0, lse_out, f32(p.logp) + r0, logp_out, ref, row_factor, far);
-      else
-        hipLaunchKernelGGL(join_stats_kernel<32>, grid, dim3(1024), 0, st, r0, rn, C, parts, a.stats, rn, a.zy, a.labels, n_dev,
-                           f32(p.lse) + r0, lse_out, f32(p.logp) + r0, logp_out, ref, row_factor, far);
+      // few parts leave most threads of a workgroup of few rows without one (200,000 rows of 2 parts
+      // by 32 rows a workgroup: 29 us)
+      auto launch = [&](auto kernel, int64_t per) {
+        hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>((rn + per - 1) / per)), dim3(1024), 0, st, r0, rn, C, parts, a.stats,
+                           rn, a.zy, a.labels, n_dev, f32(p.lse) + r0, lse ? lse + r0 : nullptr, f32(p.logp) + r0,
+                           logp ? logp + r0 : nullptr, ref, row_factor, far);
+      };
+      if (rn <= 256) launch(join_stats_kernel<4>, 4);
+      else if (parts <= 8) launch(join_stats_kernel<256>, 256);
+      else launch(join_stats_kernel<32>, 32);
       GIST_LAUNCHED("table_xent_join");
     }
     if constexpr (STORE == GIST_STORE_BF16) {
@@ -1582,13 +1648,10 @@ gist_status run16(hipStream_t st, const gist_table_xent_desc* D, const Plan& p, 
       }
     }
   }
-  {
-    constexpr float kUnhold = STORE == GIST_STORE_F16 ? 1.f / 32768.f : 1.f;
-    ProfScope ps(st, "table_xent_loss", 0.0, 8.0 * n);
-    hipLaunchKernelGGL(loss_kernel, dim3(1), dim3(1024), 0, st, n, f32(p.logp), labels, n_dev,
-                       D->grad_scale * D->scale * kUnhold, loss, grad && !p.exps ? f32(p.factor) : nullptr);
-    GIST_LAUNCHED("table_xent_loss");
-  }
+  constexpr float kUnhold = STORE == GIST_STORE_F16 ? 1.f / 32768.f : 1.f;
+  const gist_status sl = run_loss(st, n, f32(p.logp), labels, n_dev, D->grad_scale * D->scale * kUnhold,
+                                  reinterpret_cast<LossPart*>(w + p.loss_parts), loss, grad && !p.exps ? f32(p.factor) : nullptr);
+  if (sl != GIST_OK) return sl;
   if (!grad || p.exps) return GIST_OK;
   if constexpr (STORE == GIST_STORE_F16) {
     const int64_t ldp = up(d, 4);
@@ -1761,14 +1824,21 @@ gist_status run32(hipStream_t st, const gist_table_xent_desc* D, const Plan& p, 
       }
     } else {
       ProfScope ps(st, "table_xent_piece", 0.0, (grad ? 8.0 : 4.0) * rn * C);
-      hipLaunchKernelGGL(piece_kernel, dim3(static_cast<unsigned>(std::min<int64_t>(rn, 1 << 20))), dim3(kBlock), 0, st, r0, rn,
-                         n, C, D->scale, z, p.wide, labels, n_dev, factor, grad ? 1 : 0, lse, logp_ws, logp);
+      auto launch = [&](auto kernel, int threads) {
+        const int64_t g = std::min<int64_t>((rn * threads + kBlock - 1) / kBlock, 1 << 20);
+        hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(g)), dim3(kBlock), 0, st, r0, rn, n, C, D->scale, z, p.wide, labels,
+                           n_dev, factor, grad ? 1 : 0, lse, logp_ws, logp);
+      };
+      if (C <= 64) launch(piece_kernel<16, 1>, 16);
+      else if (C <= 256) launch(piece_kernel<64, 1>, 64);
+      else if (C <= 1024) launch(piece_kernel<64, 4>, 64);
+      else launch(piece_kernel<kBlock, 2 * kChunk / (4 * kBlock)>, kBlock);
       GIST_LAUNCHED("table_xent_piece");
     }
     if (!grad) continue;
     {
       ProfScope ps(st, "table_xent_mask", 0.0, 8.0 * rn * d);
-      hipLaunchKernelGGL(mask_rows_kernel, dim3(grid_of(rn * d)), dim3(kBlock), 0, st, r0, rn, n, d, H, D->ldh, hm, labels, n_dev);
+      hipLaunchKernelGGL(mask_rows_kernel, dim3(grid_of(rn * ((d + 3) / 4))), dim3(kBlock), 0, st, r0, rn, n, d, H, D->ldh, hm, labels, n_dev);
       GIST_LAUNCHED("table_xent_mask");
     }
     // dH = G T: T's rows are values of K
@@ -1799,9 +1869,7 @@ gist_status run32(hipStream_t st, const gist_table_xent_desc* D, const Plan& p, 
     s = gemm(st, C, d, rn, G2, H2, O2, GIST_DTYPE_F32, gws, p.gemm_bytes);
     if (s != GIST_OK) return s;
   }
-  ProfScope ps(st, "table_xent_loss", 0.0, 8.0 * n);
-  hipLaunchKernelGGL(loss_kernel, dim3(1), dim3(1024), 0, st, n, logp_ws, labels, n_dev, 0.f, loss, nullptr);
-  return check_launch("table_xent_loss");
+  return run_loss(st, n, logp_ws, labels, n_dev, 0.f, reinterpret_cast<LossPart*>(w + p.loss_parts), loss, nullptr);
 }
 
 __global__ __launch_bounds__(kBlock) void zero_rows_kernel(int64_t rows, int64_t bytes, char* __restrict__ x, int64_t ld) {

@@ -384,3 +384,30 @@ def test_8_bit_rows_of_unequal_terms(G, ctx, n, C, d):
     T *= np.exp2(rng.integers(-9, 1, (1, d))).astype(np.float32)
     out, Hv, Tv, _ = run(G, ctx, H, T, y, "e4m3", grad=False)
     check(out, Hv, Tv, y, "e4m3", grad=False)
+
+
+@pytest.mark.parametrize("store,dtype", [("f32", "f32"), ("f32", "bf16"), ("bf16", None), ("f16", None)])
+@pytest.mark.parametrize("n,C,d", [(16385, 3, 8), (20001, 41, 24), (70, 64, 16), (70, 65, 16), (40, 256, 8),
+                                   (40, 257, 8), (33, 1024, 8), (33, 1025, 16), (5, 8192, 8), (5, 8193, 8)])
+def test_where_a_rows_threads_change(G, ctx, store, dtype, n, C, d):
+    """Classes of a row in 16, 64 and 256 threads and in chunks; rows of several workgroups' losses."""
+    rng = np.random.default_rng(n + C)
+    H, T, y = inputs(n, C, d, rng)
+    y[:2] = 0, C - 1
+    out, Hv, Tv, _ = run(G, ctx, H, T, y, store, dtype, n_valid=n - 1, pad=1)
+    check(out, Hv, Tv, y, store, dtype, n_valid=n - 1)
+
+
+@pytest.mark.parametrize("C", [47, 200, 700, 3000])
+def test_wrong_labels_and_non_finite_rows_by_classes(G, ctx, C):
+    rng = np.random.default_rng(C)
+    n, d = 60, 24
+    H, T, y = inputs(n, C, d, rng, 0.0)
+    y[7], y[9] = C, C + 3
+    H[11, 5], y[11] = np.inf, C - 1
+    H[12], y[12] = np.nan, -1
+    out, _, _, _ = run(G, ctx, H, T, y, "f32")
+    assert np.isnan(out["loss"]) and np.isnan(out["logp"][[7, 9, 11]]).all() and out["logp"][12] == 0
+    rest = np.delete(np.arange(n), [7, 9, 11, 12])
+    assert np.isfinite(out["logp"][rest]).all() and np.isfinite(out["dH"][rest]).all()
+    assert (out["dH"][12] == 0).all()
