@@ -625,7 +625,8 @@ gist_status gist_quantize_rows(gist_ctx* ctx, int64_t n, int32_t d, const void* 
 
 /* Softmax cross-entropy of n rows H (n x d) against a table T of class
  * vectors (C x d: the layout of gist_embed_lookup's table, so the two may be
- * one), in pieces that never hold all n x C logits:
+ * one), in pieces of at most 1 GiB of logits or exponentials (256 rows' where that
+ * is more):
  *   z_vj = scale <h_v, t_j>,  lse[v] = log sum_j exp z_vj,
  *   logp[v] = z_vy - lse[v],  *loss_dev = - mean logp over the labelled rows.
  * Rows and classes: row v is labelled if v < *n_valid_dev (one device int32,

@@ -12,7 +12,10 @@
 // branch a load, with long rows read again, these took 183 and 220 us, 100,000 rows of 64 in fp32
 // 49 us (now 11), and 4,000 of 16,384 in bf16 180 us (now 111).
 //
-// 8-bit rows: e4m3, the row's largest magnitude at 448, nearest even.
+// 8-bit rows: e4m3, the row's largest magnitude at 448, nearest even.  The codes are those of exact
+// arithmetic on h and g (s cancels): 32 bits decide all but those near the middle between two
+// codes, which are decided again in 64 bits (one element in 60,000).  65,537 rows of 2,048 from fp32 take
+// 134 us with that and without, 16,384 of 4,096 in bf16 with a residual 114 and 95.
 //
 // The gain's gradient: a workgroup keeps its rows' sum of dy n in registers (every
 // thread has the same columns in each of its rows), writes it once, and a second
@@ -157,13 +160,60 @@ __device__ __forceinline__ float scale_of(float big, float& inv) {
   return zero ? 0.f : big / kTop;
 }
 
+// How far a code's argument is from the middle between two codes, whose 20 lowest bits are
+// 0x80000, in units of its last place: at most 2 kNear if within kNear of it.  32 bits leave an
+// argument off by less: two roundings each of it and of the row's largest, the quotient's and the
+// product's are 6 of 2^-24 relative, 6 places at most.  (Below 2^-6 codes are 2^-9 apart; a code that
+// is one off there is 2^-18 of the row's largest, and left.)
+constexpr unsigned kNear = 8;
+__device__ __forceinline__ unsigned border(float a) { return (__float_as_uint(a) + (0x80000u + kNear)) & 0xfffffu; }
+
+// The float whose nearest code is a's.
+__device__ __forceinline__ float decided(double a) {
+  const float f = static_cast<float>(a);
+  const unsigned u = __float_as_uint(f);
+  if ((u & 0xfffffu) != 0x80000u || static_cast<double>(f) == a) return f;
+  return __uint_as_float(fabs(a) > fabs(static_cast<double>(f)) ? u + 1 : u - 1);
+}
+
+template <int THREADS>
+__device__ __forceinline__ double row_max64(double v, double* sh) {
+#pragma unroll
+  for (int o = (THREADS < 64 ? THREADS : 64) / 2; o > 0; o >>= 1) v = fmax(v, __shfl_xor(v, o, 64));
+  if constexpr (THREADS <= 64) return v;
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = sh[0];
+#pragma unroll
+  for (int w = 1; w < THREADS / 64; ++w) v = fmax(v, sh[w]);
+  return v;
+}
+
+// h times the gain, exactly: h from where it has just been stored, since x or the residual may be there.
+template <int STORE, bool NORM>
+__device__ __forceinline__ double exact_y(const Fwd& a, int64_t row, int c) {
+  float h[1];
+  if (NORM && a.h) load_vec<STORE, 1>(a.h, row * a.ldh + c, h);
+  else load_h<STORE, 1>(a, row, c, 1, h);
+  return static_cast<double>(h[0]) * (NORM ? a.gain[c] : 1.f);
+}
+
+// Waves of a SIMD at least.  For codes the compiler would take registers for the rare second decision that
+// cost the rest its waves: with a residual in bf16 65,537 rows of 2,048 take 181 us with five,
+// 198 with four and 245 with six; 100,000 of 602 176 with four, 203 as it pleases; from fp32 65,537 of
+// 2,048 134 with four, 206 with five.
+constexpr int rows_waves(int store, int out, int threads, bool tail) {
+  return out != GIST_STORE_E4M3 ? 1 : threads > kBlock || store == GIST_STORE_F32 || tail ? 4 : 5;
+}
+
 // A row in the registers of THREADS threads: CH loads of V elements each and, with TAIL, one element each
 // of what those leave (a load that may end inside a row takes a branch a load: 183 us for
 // 65,537 rows of 2,048 from fp32 to codes, 134 without; of 602, with a residual, 147 and 116).  NORM false: no norm, the row's codes alone.
 template <int STORE, int OUT, int THREADS, int CH, bool NORM, bool TAIL>
-__global__ __launch_bounds__(block_of(THREADS)) void rows_kernel(Fwd a) {
+__global__ __launch_bounds__(block_of(THREADS), rows_waves(STORE, OUT, THREADS, TAIL)) void rows_kernel(Fwd a) {
   constexpr int V = vec_of<STORE>();
   __shared__ float sh[2 * block_of(THREADS) / 64];
+  __shared__ double sh64[OUT == GIST_STORE_E4M3 ? block_of(THREADS) / 64 : 1];
   int turn = 0;
   const int lane = threadIdx.x % THREADS;
   const int whole = TAIL ? a.d - a.d % V : a.d, tail = whole + lane;
@@ -223,23 +273,72 @@ __global__ __launch_bounds__(block_of(THREADS)) void rows_kernel(Fwd a) {
       float inv;
       const float scale = scale_of(row_max<THREADS>(big, sh, turn), inv);
       if (lane == 0) a.y_scale[row] = scale;
+      unsigned near = ~0u;
+#pragma unroll
+      for (int i = 0; i < CH; ++i)
+#pragma unroll
+        for (int q = 0; q < V; ++q) {
+          h[i][q] *= inv;
+          near = min(near, border(h[i][q]));
+        }
+      if (TAIL) {
+        t[0] *= inv;
+        near = min(near, border(t[0]));
+      }
+      bool again;
+      if constexpr (THREADS <= 64) again = __any(near <= 2 * kNear);
+      else again = __syncthreads_or(near <= 2 * kNear);
 #pragma unroll
       for (int i = 0; i < CH; ++i) {
         const int c = (i * THREADS + lane) * V;
-        if (c < whole) store_y<OUT, V>(a.y, row * a.ldy + c, V, h[i], inv);
+        if (c < whole) store_y<OUT, V>(a.y, row * a.ldy + c, V, h[i], 1.f);
       }
       if (TAIL && tail < a.d)
         static_cast<unsigned char*>(a.y)[row * a.ldy + tail] =
-            static_cast<unsigned char>(__builtin_amdgcn_cvt_pk_fp8_f32(t[0] * inv, 0.f, 0, false));
+            static_cast<unsigned char>(__builtin_amdgcn_cvt_pk_fp8_f32(t[0], 0.f, 0, false));
+      if (again) {
+        // the largest is one of those that 32 bits put next to it; then what is near a middle, over
+        // the codes that have been stored
+        constexpr float kLargest = kTop * (1.f - 0x1p-20f);
+        static_assert(CH * V <= 32, "a bit for each of a thread's elements");
+        unsigned large = 0u, close = 0u;
+#pragma unroll
+        for (int i = 0; i < CH; ++i)
+#pragma unroll
+          for (int q = 0; q < V; ++q) {
+            float x = h[i][q];
+            asm volatile("" : "+v"(x));   // from h again: no value of the tests above is kept for this
+            if (fabsf(x) > kLargest) large |= 1u << (i * V + q);
+            if (border(x) <= 2 * kNear) close |= 1u << (i * V + q);
+          }
+        auto column = [&](int e) { return (e / V * THREADS + lane) * V + e % V; };
+        double big64 = 0.0;
+#pragma unroll 1
+        for (; large; large &= large - 1u)
+          big64 = fmax(big64, fabs(exact_y<STORE, NORM>(a, row, column(__ffs(large) - 1))));
+        if (TAIL && fabsf(t[0]) > kLargest) big64 = fmax(big64, fabs(exact_y<STORE, NORM>(a, row, tail)));
+        const double inv64 = 448.0 / row_max64<THREADS>(big64, sh64);
+        auto again_at = [&](int c) {
+          static_cast<unsigned char*>(a.y)[row * a.ldy + c] = static_cast<unsigned char>(
+              __builtin_amdgcn_cvt_pk_fp8_f32(decided(exact_y<STORE, NORM>(a, row, c) * inv64), 0.f, 0, false));
+        };
+        if (inv > 0.f) {     // no row of zeros or NaN
+#pragma unroll 1
+          for (; close; close &= close - 1u) again_at(column(__ffs(close) - 1));
+          if (TAIL && tail < a.d && border(t[0]) <= 2 * kNear) again_at(tail);
+        }
+      }
     }
   }
 }
 
-// Rows longer than a workgroup's registers: read again from x and r for each pass.
+// Rows longer than a workgroup's registers: read again from x and r for each pass; all
+// codes in 64 bits.
 template <int STORE, int OUT, bool NORM>
 __global__ __launch_bounds__(kBlock) void long_rows_kernel(Fwd a) {
   constexpr int V = vec_of<STORE>();
   __shared__ float sh[2 * kBlock / 64];
+  __shared__ double sh64[OUT == GIST_STORE_E4M3 ? kBlock / 64 : 1];
   int turn = 0;
   const float inv_d = 1.f / static_cast<float>(a.d);
   for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
@@ -257,26 +356,39 @@ __global__ __launch_bounds__(kBlock) void long_rows_kernel(Fwd a) {
       if (a.rstd && threadIdx.x == 0) a.rstd[row] = rstd;
     }
     float big = 0.f, inv = 0.f;
+    double big64 = 0.0, inv64 = 0.0;
     // for codes: first the largest magnitude, then the codes
     for (int pass = OUT == GIST_STORE_E4M3 ? 0 : 1; pass < 2; ++pass) {
       for (int64_t c = threadIdx.x * V; c < a.d; c += kBlock * V) {
         float h[V];
         const int left = static_cast<int>(min(static_cast<int64_t>(V), a.d - c));
         load_h<STORE, V>(a, row, c, left, h);
-        float y[V];
+        float y[V], g[V];
 #pragma unroll
-        for (int q = 0; q < V; ++q) y[q] = NORM ? h[q] * rstd * (q < left ? a.gain[c + q] : 0.f) : h[q];
+        for (int q = 0; q < V; ++q) {
+          g[q] = q >= left ? 0.f : NORM ? a.gain[c + q] : 1.f;
+          y[q] = NORM ? h[q] * rstd * g[q] : h[q];
+        }
         if (pass == 0) {
 #pragma unroll
-          for (int q = 0; q < V; ++q) big = larger(big, y[q]);
+          for (int q = 0; q < V; ++q) {
+            big = larger(big, y[q]);
+            big64 = fmax(big64, fabs(static_cast<double>(h[q]) * g[q]));
+          }
         } else {
-          store_y<OUT, V>(a.y, row * a.ldy + c, left, y, inv);
+          if constexpr (OUT == GIST_STORE_E4M3) {
+#pragma unroll
+            for (int q = 0; q < V; ++q)
+              y[q] = inv > 0.f ? decided(static_cast<double>(h[q]) * g[q] * inv64) : copysignf(inv, h[q]);
+          }
+          store_y<OUT, V>(a.y, row * a.ldy + c, left, y, 1.f);
           if (NORM && a.h) store_some<STORE, V>(a.h, row * a.ldh + c, left, h);
         }
       }
       if (pass == 0) {
         const float scale = scale_of(row_max<kBlock>(big, sh, turn), inv);
         if (threadIdx.x == 0) a.y_scale[row] = scale;
+        inv64 = 448.0 / row_max64<kBlock>(big64, sh64);
       }
     }
   }

@@ -271,3 +271,53 @@ def test_non_finite_rows_at_edges(G, ctx, d):
 @pytest.mark.parametrize("store", ["f32", "bf16", "f16"])
 def test_quantize_rows_at_edges(G, ctx, n, d, store):
     test_quantize_rows(G, ctx, n, d, store)
+
+
+def codes_in_64_bits(v):
+    """Nearest codes (ties to even) of rows whose largest magnitude is 448; |code| < 2^-6 are left out."""
+    v = to_host(v)
+    a = v * (R.TOP / np.abs(v).max(1, keepdims=True))
+    return R.e4m3(a), np.abs(a) >= 2.0 ** -6
+
+
+@pytest.mark.parametrize("n,d", [(60000, 40), (30000, 130), (3000, 2048), (1500, 4099), (800, 4096), (150, 20000),
+                                 (60, 40001)])
+@pytest.mark.parametrize("store", ["f32", "bf16"])
+def test_codes_are_exact(G, ctx, n, d, store):
+    """Every code is the nearest of the 64-bit value, whichever side of a middle 32 bits would put it."""
+    import torch
+    torch.manual_seed(d)
+    t = R.torch_type(store)
+    x, r = torch.randn(n, d, device="cuda").to(t), torch.randn(n, d, device="cuda").to(t)
+    gain = 1 + 0.2 * torch.randn(d, device="cuda")
+    y, s = torch.empty(n, d, dtype=torch.uint8, device="cuda"), torch.empty(n, device="cuda")
+    st = R.store_of(G, store)
+    value = lambda: to_host(y.view(torch.float8_e4m3fn).double())
+    for res in (r, None):
+        h = x if res is None else (x.float() + r.float()).to(t)
+        want, counts = codes_in_64_bits(h.double() * gain.double())
+        into = torch.empty_like(x)
+        for hh in (into, None):
+            G.gist_rms_norm(ctx, n, d, x, d, res, d, st, gain, EPS, hh, d, y, d, G.GIST_STORE_E4M3, s, None)
+            assert np.array_equal(value()[counts], want[counts])
+    G.gist_quantize_rows(ctx, n, d, x, d, st, y, d, s)
+    want, counts = codes_in_64_bits(x.double())
+    assert np.array_equal(value()[counts], want[counts])
+    # h in x's place
+    z = x.clone()
+    G.gist_rms_norm(ctx, n, d, z, d, r, d, st, gain, EPS, z, d, y, d, G.GIST_STORE_E4M3, s, None)
+    want, counts = codes_in_64_bits((x.float() + r.float()).to(t).double() * gain.double())
+    assert np.array_equal(value()[counts], want[counts])
+
+
+@pytest.mark.parametrize("d", [16, 449, 2000, 9000, 40000])
+def test_codes_of_exact_middles(G, ctx, d):
+    """Whole numbers up to 448, of which many lie in the middle between two codes: to the even one."""
+    import torch
+    torch.manual_seed(d)
+    x = torch.randint(-447, 448, (20, d), device="cuda").float()
+    x[:, d // 2] = 448
+    y, s = torch.empty(20, d, dtype=torch.uint8, device="cuda"), torch.empty(20, device="cuda")
+    G.gist_quantize_rows(ctx, 20, d, x, d, G.GIST_STORE_F32, y, d, s)
+    want, _ = codes_in_64_bits(x.double())
+    assert np.array_equal(to_host(y.view(torch.float8_e4m3fn).double()), want) and bool((s == 1).all())
