@@ -615,6 +615,14 @@ gist_status gist_rms_norm_bwd(gist_ctx* ctx, int64_t n, int32_t d, const void* d
                               int32_t dy_store, const void* h, int64_t ldh, int32_t store,
                               const float* gain, const float* rstd, const void* dsum, int64_t ldds,
                               void* dx, int64_t lddx, float* dgain, void* ws, size_t ws_bytes);
+/* The same for the rows of gist_table_xent's labels: a row without a label (negative), or from
+ * *n_valid_dev on (one device int32; NULL: n), takes no part, whatever dy, h and rstd hold there.  It
+ * adds nothing to dgain, and its dx is dsum (zero without).  NULL labels: every row has one. */
+gist_status gist_rms_norm_bwd_padded(gist_ctx* ctx, int64_t n, int32_t d, const void* dy, int64_t lddy,
+                                     int32_t dy_store, const void* h, int64_t ldh, int32_t store,
+                                     const float* gain, const float* rstd, const void* dsum,
+                                     int64_t ldds, const int32_t* labels, const int32_t* n_valid_dev,
+                                     void* dx, int64_t lddx, float* dgain, void* ws, size_t ws_bytes);
 /* y = the rows of x (n x d, stored as `store`) as e4m3 codes with a scale per
  * row, by the rule above: a table or rows for gist_table_xent.  Columns past d
  * are left as they were.  Errors as gist_rms_norm; y may not be x. */

@@ -1276,11 +1276,12 @@ extern "C" size_t gist_rms_norm_bwd_workspace(int64_t n, int32_t d) {
   return gist::rms_norm_bwd_workspace(n, d);
 }
 
-extern "C" gist_status gist_rms_norm_bwd(gist_ctx* ctx, int64_t n, int32_t d, const void* dy,
-                                         int64_t lddy, int32_t dy_store, const void* h, int64_t ldh,
-                                         int32_t store, const float* gain, const float* rstd,
-                                         const void* dsum, int64_t ldds, void* dx, int64_t lddx,
-                                         float* dgain, void* ws, size_t ws_bytes) {
+extern "C" gist_status gist_rms_norm_bwd_padded(gist_ctx* ctx, int64_t n, int32_t d, const void* dy,
+                                                int64_t lddy, int32_t dy_store, const void* h, int64_t ldh,
+                                                int32_t store, const float* gain, const float* rstd,
+                                                const void* dsum, int64_t ldds, const int32_t* labels,
+                                                const int32_t* n_valid_dev, void* dx, int64_t lddx,
+                                                float* dgain, void* ws, size_t ws_bytes) {
   gist::clear_error();
   if (!ctx) return set_error(GIST_E_INVAL, "rms_norm_bwd: NULL ctx");
   gist::ProfBind pb(ctx);
@@ -1303,7 +1304,16 @@ extern "C" gist_status gist_rms_norm_bwd(gist_ctx* ctx, int64_t n, int32_t d, co
   }
   gist::DeviceGuard dg(ctx->device);
   return gist::rms_norm_bwd(ctx->stream, n, d, dy, lddy, dy_store, h, ldh, store, gain, rstd, dsum,
-                            ldds, dx, lddx, dgain, ws);
+                            ldds, labels, n_valid_dev, dx, lddx, dgain, ws);
+}
+
+extern "C" gist_status gist_rms_norm_bwd(gist_ctx* ctx, int64_t n, int32_t d, const void* dy,
+                                         int64_t lddy, int32_t dy_store, const void* h, int64_t ldh,
+                                         int32_t store, const float* gain, const float* rstd,
+                                         const void* dsum, int64_t ldds, void* dx, int64_t lddx,
+                                         float* dgain, void* ws, size_t ws_bytes) {
+  return gist_rms_norm_bwd_padded(ctx, n, d, dy, lddy, dy_store, h, ldh, store, gain, rstd, dsum, ldds,
+                                  nullptr, nullptr, dx, lddx, dgain, ws, ws_bytes);
 }
 
 extern "C" gist_status gist_quantize_rows(gist_ctx* ctx, int64_t n, int32_t d, const void* x,

@@ -243,8 +243,8 @@ gist_status rms_norm(hipStream_t st, int64_t n, int d, const void* x, int64_t ld
 size_t rms_norm_bwd_workspace(int64_t n, int d);
 gist_status rms_norm_bwd(hipStream_t st, int64_t n, int d, const void* dy, int64_t lddy,
                          int dy_store, const void* h, int64_t ldh, int store, const float* gain,
-                         const float* rstd, const void* dsum, int64_t ldds, void* dx, int64_t lddx,
-                         float* dgain, void* ws);
+                         const float* rstd, const void* dsum, int64_t ldds, const int32_t* labels,
+                         const int32_t* n_dev, void* dx, int64_t lddx, float* dgain, void* ws);
 gist_status quantize_rows(hipStream_t st, int64_t n, int d, const void* x, int64_t ldx, int store,
                           void* y, int64_t ldy, float* scale);
 

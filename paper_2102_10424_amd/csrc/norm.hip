@@ -404,7 +404,16 @@ struct Bwd {
   const void* dsum;
   void* dx;
   float* part;      // [grid][d]
+  const int32_t* labels;   // or NULL
+  const int32_t* n_dev;    // or NULL
 };
+
+// Whether a row takes part.  Where it does not, h, dy and rstd become zeros by selection before anything
+// is computed with them: 0 times a NaN would be a NaN in every row's gain.
+__device__ __forceinline__ int64_t rows_real(const Bwd& a) { return a.n_dev ? *a.n_dev : a.n; }
+__device__ __forceinline__ bool takes_part(const Bwd& a, int64_t row, int64_t real) {
+  return row < real && (!a.labels || a.labels[row] >= 0);
+}
 
 // V elements of any store (V as the rows' own loads have it).
 template <int STORE, int V>
@@ -452,8 +461,10 @@ __global__ __launch_bounds__(block_of(THREADS)) void bwd_kernel(Bwd a) {
     for (int q = 0; q < V; ++q) g[i][q] = 0.f;
     if (c < whole) load_any<GIST_STORE_F32, V>(a.gain, c, V, g[i]);
   }
+  const int64_t real = rows_real(a);
   for (int64_t row = blockIdx.x * RB + sub; row < a.n; row += static_cast<int64_t>(gridDim.x) * RB) {
-    const float s = a.rstd[row];
+    const bool part = takes_part(a, row, real);
+    const float s = part ? a.rstd[row] : 0.f;
     float h[CH][V], y[CH][V], ht[1] = {0.f}, yt[1] = {0.f};
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
@@ -468,6 +479,13 @@ __global__ __launch_bounds__(block_of(THREADS)) void bwd_kernel(Bwd a) {
     if (TAIL && tail < a.d) {
       load_vec<STORE, 1>(a.h, row * a.ldh + tail, ht);
       load_vec<DY, 1>(a.dy, row * a.lddy + tail, yt);
+    }
+    if (!part) {
+      ht[0] = yt[0] = 0.f;
+#pragma unroll
+      for (int i = 0; i < CH; ++i)
+#pragma unroll
+        for (int q = 0; q < V; ++q) h[i][q] = y[i][q] = 0.f;
     }
     float dot = 0.f;
     if constexpr (TAIL) {
@@ -546,8 +564,10 @@ __global__ __launch_bounds__(kBlock) void long_bwd_kernel(Bwd a) {
   const float inv_d = 1.f / static_cast<float>(a.d);
   float* const out = a.part ? a.part + static_cast<int64_t>(blockIdx.x) * a.d : nullptr;
   bool first = true;
+  const int64_t real = rows_real(a);
   for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
-    const float s = a.rstd[row];
+    const bool part = takes_part(a, row, real);
+    const float s = part ? a.rstd[row] : 0.f;
     float dot = 0.f;
     for (int64_t c = threadIdx.x * V; c < a.d; c += kBlock * V) {
       const int left = static_cast<int>(min(static_cast<int64_t>(V), a.d - c));
@@ -557,7 +577,8 @@ __global__ __launch_bounds__(kBlock) void long_bwd_kernel(Bwd a) {
 #pragma unroll
       for (int q = 0; q < V; ++q) {
         if (q >= left) break;
-        h[q] *= s;
+        h[q] = part ? h[q] * s : 0.f;
+        if (!part) y[q] = 0.f;
         const float p = y[q] * h[q];
         if (out) out[c + q] = first ? p : out[c + q] + p;
         dot = fmaf(y[q] * a.gain[c + q], h[q], dot);
@@ -577,7 +598,7 @@ __global__ __launch_bounds__(kBlock) void long_bwd_kernel(Bwd a) {
 #pragma unroll
       for (int q = 0; q < V; ++q) {
         const float g = q < left ? a.gain[c + q] : 0.f;
-        z[q] = fmaf(s, y[q] * g - h[q] * s * dot, z[q]);
+        if (part) z[q] = fmaf(s, y[q] * g - h[q] * s * dot, z[q]);
       }
       store_some<STORE, V>(a.dx, row * a.lddx + c, left, z);
     }
@@ -724,9 +745,11 @@ size_t rms_norm_bwd_workspace(int64_t n, int d) {
 
 gist_status rms_norm_bwd(hipStream_t st, int64_t n, int d, const void* dy, int64_t lddy, int dy_store,
                          const void* h, int64_t ldh, int store, const float* gain, const float* rstd,
-                         const void* dsum, int64_t ldds, void* dx, int64_t lddx, float* dgain, void* ws) {
+                         const void* dsum, int64_t ldds, const int32_t* labels, const int32_t* n_dev, void* dx, int64_t lddx,
+                         float* dgain, void* ws) {
   if (n > 0) {
-    const Bwd a{n, lddy, ldh, ldds, lddx, d, dy, h, gain, rstd, dsum, dx, dgain ? static_cast<float*>(ws) : nullptr};
+    const Bwd a{n, lddy, ldh, ldds, lddx, d, dy, h, gain, rstd, dsum, dx, dgain ? static_cast<float*>(ws) : nullptr,
+                labels, n_dev};
     ProfScope ps(st, "rms_norm_bwd", 0.0,
                  static_cast<double>(n) * d *
                      (width_of(store) * (1.0 + (dsum && dx ? 1 : 0) + (dx ? 1 : 0)) + width_of(dy_store)));

@@ -69,7 +69,8 @@ EXPORTED = (
     "gist_softmax_xent_noalloc",
     "gist_embed_lookup", "gist_embed_grad_workspace", "gist_embed_grad", "gist_embed_grad_sgd",
     "gist_log_probs_workspace", "gist_log_probs", "gist_log_probs_bwd",
-    "gist_rms_norm", "gist_rms_norm_bwd_workspace", "gist_rms_norm_bwd", "gist_quantize_rows",
+    "gist_rms_norm", "gist_rms_norm_bwd_workspace", "gist_rms_norm_bwd", "gist_rms_norm_bwd_padded",
+    "gist_quantize_rows",
     "gist_table_xent_workspace", "gist_table_xent",
     "gist_adamw_update", "gist_adamw_coefficients", "gist_adamw_update_dev",
     "gist_muon_workspace_size", "gist_orthogonalize", "gist_muon_update",
@@ -225,6 +226,9 @@ _sigs = {
     "gist_rms_norm_bwd": (C.c_int, [_P, C.c_int64, C.c_int32, _P, C.c_int64, C.c_int32, _P,
                                     C.c_int64, C.c_int32, _P, _P, _P, C.c_int64, _P, C.c_int64, _P,
                                     _P, C.c_size_t]),
+    "gist_rms_norm_bwd_padded": (C.c_int, [_P, C.c_int64, C.c_int32, _P, C.c_int64, C.c_int32, _P,
+                                           C.c_int64, C.c_int32, _P, _P, _P, C.c_int64, _P, _P, _P,
+                                           C.c_int64, _P, _P, C.c_size_t]),
     "gist_quantize_rows": (C.c_int, [_P, C.c_int64, C.c_int32, _P, C.c_int64, C.c_int32, _P,
                                      C.c_int64, _P]),
     "gist_table_xent_workspace": (C.c_int, [C.POINTER(gist_table_xent_desc), C.c_int32,
@@ -588,12 +592,17 @@ def gist_rms_norm_bwd_workspace(n, d):
 
 
 def gist_rms_norm_bwd(ctx, n, d, dy, lddy, dy_store, h, ldh, store, gain, rstd, dsum, ldds, dx, lddx,
-                      dgain, ws):
-    """Gradients of ``gist_rms_norm``: dx (of x and of the residual, with dsum added) and dgain."""
-    _check(_lib.gist_rms_norm_bwd(ctx.handle, int(n), int(d), _ptr(dy), int(lddy), int(dy_store),
-                                  _ptr(h), int(ldh), int(store), _ptr(gain), _ptr(rstd),
-                                  _ptr(dsum), int(ldds), _ptr(dx), int(lddx), _ptr(dgain), _ptr(ws),
-                                  _nbytes(ws)))
+                      dgain, ws, labels=None, n_valid_dev=None):
+    """Gradients of ``gist_rms_norm``: dx (of x and of the residual, with dsum added) and dgain.  With
+    ``labels`` or ``n_valid_dev`` (``gist_rms_norm_bwd_padded``) the rows that
+    ``gist_table_xent`` leaves out for them take no part."""
+    head = (ctx.handle, int(n), int(d), _ptr(dy), int(lddy), int(dy_store), _ptr(h), int(ldh),
+            int(store), _ptr(gain), _ptr(rstd), _ptr(dsum), int(ldds))
+    tail = (_ptr(dx), int(lddx), _ptr(dgain), _ptr(ws), _nbytes(ws))
+    if labels is None and n_valid_dev is None:
+        _check(_lib.gist_rms_norm_bwd(*head, *tail))
+    else:
+        _check(_lib.gist_rms_norm_bwd_padded(*head, _ptr(labels), _ptr(n_valid_dev), *tail))
 
 
 def gist_quantize_rows(ctx, n, d, x, ldx, store, y, ldy, scale):

@@ -1377,7 +1377,7 @@ class TableHead:
         """In place of ``run.loss_and_grad`` after its forward pass: the loss (into ``loss_out``, a
         one-element device tensor, or ``loss``), ``run.dlogits``, which is the residual's gradient
         as well, ``dT`` and ``dgain``.  Rows behind a padded batch's real ones (``n_dev``) and rows
-        with a negative label take no part."""
+        with a negative label take no part, whatever they hold; their ``run.dlogits`` are zero."""
         n, x = self._rows(run, batch, residual)
         b = self._reserve(n)
         d, st = self.d, self.store
@@ -1396,7 +1396,7 @@ class TableHead:
             gain = self._gain
         G.gist_rms_norm_bwd(self.ctx, n, d, b["dy"], d, st, x if residual is None else b["h"], d,
                             G.GIST_STORE_F32, gain, b["rstd"], None, d, run.dlogits, d, self.dgain,
-                            b["norm_ws"])
+                            b["norm_ws"], batch.labels, getattr(batch, "n_dev", None))
         self.logp, self.lse = b["logp"][:n], b["lse"][:n]
 
     def quantise(self):
