@@ -1136,9 +1136,10 @@ class SubGCN:
 
     def adamw(self, params, head=None, weight_decay=0.01, eight=False):
         """An :class:`AdamW` over ``params`` (GAT: the attention vectors without decay) and, with
-        ``head``, its table and gain, which is not decayed.  A head with a loss scale is refused
+        ``head``, its table and gain, which is not decayed; :meth:`step` takes it with that head
+        only.  A head with a loss scale is refused
         (ValueError): its gradients are times that and the layers' are not, so its ``items`` take an
-        :class:`AdamW` of their own and ``grad_scale`` there."""
+        :class:`AdamW` of their own and ``grad_scale`` there, and :meth:`step` one made without a head."""
         if head is not None and head.grad_scale != 1.0:
             raise ValueError("a head with a loss scale needs an AdamW of its own")
         items = []
@@ -1150,7 +1151,7 @@ class SubGCN:
         if head is not None:
             items += head.items(weight_decay)
         opt = AdamW(self.ctx, items, eight=eight, device=self.device)
-        opt.of = (self, [p.data_ptr() for p in params])
+        opt.of = (self, [p.data_ptr() for p in params], head)
         return opt
 
     def step(self, batch, params, lr, adam=None, loss_out=None, muon=None, adamw=None, head=None,
@@ -1160,12 +1161,18 @@ class SubGCN:
         fresh) Muon, ``adamw`` = (optimizer of :meth:`adamw`, step) AdamW, else SGD; more than
         one is refused (ValueError).  With ``head`` the loss is that :class:`TableHead`'s
         (``residual``: rows added to the last layer's output), whose table and gain AdamW
-        steps and the other optimizers leave as they are."""
+        steps and the other optimizers leave as they are; an AdamW not made with it, or made with a
+        head that is not the step's, is refused (ValueError)."""
         if sum(o is not None for o in (adam, muon, adamw)) > 1:
             raise ValueError("one optimizer a step: adam, muon or adamw")
-        if adamw is not None and (adamw[0].of is None or adamw[0].of[0] is not self
-                                  or adamw[0].of[1] != [p.data_ptr() for p in params]):
-            raise ValueError("the AdamW is not this runner's adamw() of these weights")
+        if adamw is not None:
+            of = adamw[0].of
+            if of is None or of[0] is not self or of[1] != [p.data_ptr() for p in params]:
+                raise ValueError("the AdamW is not this runner's adamw() of these weights")
+            # with another head it would step a table that has no gradient of this step, without one leave
+            # the table as it is; a head with a loss scale has an AdamW of its own
+            if of[2] is not (head if head is None or head.grad_scale == 1.0 else None):
+                raise ValueError("the AdamW was not made with the step's head")
         self.forward(batch, params)
         if head is None:
             if residual is not None:
@@ -1243,7 +1250,7 @@ class AdamW:
 
     def __init__(self, ctx, items, eight=False, device="cuda"):
         self.ctx, self.eight = ctx, eight
-        self.of = None         # the runner and the addresses of the weights that SubGCN.adamw made it for
+        self.of = None         # SubGCN.adamw's runner, its weights' addresses and the head
         self.state, self._keep, tensors = [], [], []
         for i, it in enumerate(items):
             W, dW, copy = it["W"], it["dW"], it.get("copy")

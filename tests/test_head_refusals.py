@@ -1,9 +1,22 @@
-"""What the end of a step refuses beyond its arrays: the norm's backward pass with labels.  No GPU
-needed: every check runs on the host before anything touches the device."""
+"""What the end of a step refuses beyond its arrays: the norm's backward pass with labels, and
+optimizers of another head.  No GPU needed: every check runs on the host before
+anything touches the device."""
 
 import pytest
 
-from test_more_refusals import A, B, D, E, F, G, H, I, INVAL, NOMEM, UNSUP, Null, Ws, ctx, refused
+from test_more_refusals import (A, B, D, E, F, G, H, I, INVAL, NOMEM, UNSUP, CpuBatch, Null, Ws, ctx,
+                                refused)
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """The library's device calls, by name, in place of being made."""
+    from paper_2102_10424_amd import step as S
+    made = []
+    for name in ("gist_gcn_layer_fwd", "gist_gcn_layer_bwd", "gist_rms_norm", "gist_rms_norm_bwd",
+                 "gist_table_xent", "gist_softmax_xent", "gist_quantize_rows", "gist_adamw_update"):
+        monkeypatch.setattr(S.G, name, lambda *a, name=name: made.append(name))
+    return made
 
 
 @pytest.mark.parametrize("change,status", [
@@ -17,3 +30,21 @@ def test_rms_norm_bwd_padded(change, status, labels, n_dev):
              dx=F, lddx=4, dgain=H, ws=Ws(need), labels=labels, n_valid_dev=n_dev)
     refused(status, G.gist_rms_norm_bwd, ctx, **{**a, **change})
     refused(INVAL, G.gist_rms_norm_bwd, Null, **a)
+
+
+def test_adamw_belongs_to_its_head(calls):
+    import torch
+    from paper_2102_10424_amd import step as S
+    run, b = S.SubGCN(None, "gcn", [8, 24, 5], 16, device="cpu"), CpuBatch(16)
+    params = [torch.zeros(8, 24), torch.zeros(24, 5)]
+    head, other = (S.TableHead(None, torch.zeros(50, 5), device="cpu") for _ in range(2))
+    with_head, without = run.adamw(params, head), run.adamw(params)
+    scaled = S.TableHead(None, torch.zeros(50, 5), grad_scale=8.0, device="cpu")   # has an AdamW of its own
+    for opt, h in ((with_head, None), (with_head, other), (without, head), (with_head, scaled)):
+        with pytest.raises(ValueError):
+            run.step(b, params, 0.1, adamw=(opt, 1), head=h)
+        assert not calls
+    for opt, h in ((with_head, head), (without, None), (without, scaled)):
+        run.step(b, params, 0.1, adamw=(opt, 1), head=h)
+        assert calls.pop() == "gist_adamw_update"
+        calls.clear()
