@@ -14,7 +14,8 @@ def calls(monkeypatch):
     from paper_2102_10424_amd import step as S
     made = []
     for name in ("gist_gcn_layer_fwd", "gist_gcn_layer_bwd", "gist_rms_norm", "gist_rms_norm_bwd",
-                 "gist_table_xent", "gist_softmax_xent", "gist_quantize_rows", "gist_adamw_update"):
+                 "gist_table_xent", "gist_softmax_xent", "gist_quantize_rows", "gist_adamw_update",
+                 "gist_embed_lookup"):
         monkeypatch.setattr(S.G, name, lambda *a, name=name: made.append(name))
     return made
 
