@@ -1369,6 +1369,8 @@ class TableHead:
         n = batch.rows(run.L)
         if run.widths[-1] != self.d:
             raise ValueError(f"the runner's output width is not the table's {self.d}")
+        if n > run.n_cap:
+            raise ValueError("more rows than any forward pass has had")
         if residual is not None:
             _check_array("residual", residual, torch.float32, n, self.d)
         _check_array("labels", batch.labels, torch.int32, n)

@@ -1,5 +1,5 @@
-"""What the end of a step refuses beyond its arrays: the norm's backward pass with labels, and
-optimizers of another head.  No GPU needed: every check runs on the host before
+"""What the end of a step refuses beyond its arrays: the norm's backward pass with labels,
+optimizers of another head, batches that the runner has no rows for.  No GPU needed: every check runs on the host before
 anything touches the device."""
 
 import pytest
@@ -49,3 +49,23 @@ def test_adamw_belongs_to_its_head(calls):
         run.step(b, params, 0.1, adamw=(opt, 1), head=h)
         assert calls.pop() == "gist_adamw_update"
         calls.clear()
+
+
+@pytest.mark.parametrize("n", [17, 1000])
+def test_more_rows_than_the_runner_has(calls, n):
+    """Its outputs and their gradient end at its capacity."""
+    import torch
+    from paper_2102_10424_amd import step as S
+    run, head = S.SubGCN(None, "gcn", [8, 24, 5], 16, device="cpu"), S.TableHead(None, torch.zeros(50, 5), device="cpu")
+    params, big = [torch.zeros(8, 24), torch.zeros(24, 5)], CpuBatch(n)
+    head.quantise()
+    calls.clear()
+    for f in (lambda: head.score(run, big), lambda: head.score(run, big, eight=True),
+              lambda: head.loss_and_grad(run, big)):
+        with pytest.raises(ValueError):
+            f()
+    assert not calls
+    run.forward(big, params)
+    head.loss_and_grad(run, big)
+    head.score(run, big)
+    assert calls[-1] == "gist_table_xent" and run.dlogits.shape[0] >= n
