@@ -298,10 +298,12 @@ class Context:
         _check(_lib.gist_create(int(device), _P(stream), C.byref(h)))
         self.handle = h
         self.device = device
+        self.stream = stream
         self.captures = 0      # recordings begun on this context
 
     def set_stream(self, stream):
         _check(_lib.gist_set_stream(self.handle, _P(stream)))
+        self.stream = stream
 
     def close(self):
         if self.handle:

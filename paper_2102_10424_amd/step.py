@@ -1,7 +1,7 @@
 """Sub-GCN training step and GIST round, sequenced over the C ABI.
 
 Nothing here computes: each stage is one ``libgist`` call enqueued on the
-context's stream (torch only provides the device buffers).
+context's stream (torch only provides the device buffers, and rounds a table's 16-bit copy).
 
 * :class:`SubGCN` -- ``subTrain`` (Section 2.2): layer forward for every
   layer (eq. (2), or the GAT layer), softmax cross-entropy, layer backward
@@ -1200,12 +1200,17 @@ class LearnedRows:
     of the gather of given ones, ``sgd`` steps the rows that were looked up by
     the input gradient of a ``SubGCN(input_grad=True)``.  ``ids`` are device
     int32 node ids (a batch's node map); ids outside the table are padding.
-    Arrays of another type, with gaps or too few rows are refused (ValueError)."""
+    ``head``: a :class:`TableHead` of the same table; ``sgd`` keeps its 16-bit copy in step.
+    Arrays of another type, with gaps or too few rows, and a head of another table, are
+    refused (ValueError)."""
 
-    def __init__(self, ctx, table, scale=1.0, n_cap=0, device="cuda"):
+    def __init__(self, ctx, table, scale=1.0, n_cap=0, device="cuda", head=None):
         if table.dim() != 2:
             raise ValueError("the table is a matrix")
         _check_array("the table", table, torch.float32, 0)
+        if head is not None and (head.table.data_ptr() != table.data_ptr() or head.table.shape != table.shape):
+            raise ValueError("the head is of another table")
+        self.head = head
         self.ctx, self.table, self.scale, self.device = ctx, table, float(scale), device
         self.N, self.d = table.shape
         self.n_cap = 0
@@ -1235,6 +1240,8 @@ class LearnedRows:
         self._reserve(n)
         G.gist_embed_grad_sgd(self.ctx, n, self.N, self.d, ids, self.scale, dX, self.d, lr,
                               self.table, self.d, self.ws)
+        if self.head is not None:
+            self.head.round_table(self.ctx)
 
 
 _STORE = {torch.float32: G.GIST_STORE_F32, torch.bfloat16: G.GIST_STORE_BF16,
@@ -1297,6 +1304,9 @@ class TableHead:
     ``dtype``: torch.float32 (``product`` GIST_DTYPE_F32 or GIST_DTYPE_BF16_IN), or bfloat16 or
     float16: the normed rows, the table's copy ``table16`` and the gradients ``dT`` are held
     so, and the gradients times ``grad_scale``.  ``scale`` multiplies the logits.
+    An :class:`AdamW` with :meth:`items` keeps ``table16`` in step with the table, and so does a
+    :class:`LearnedRows` made with this head; any other change of the table (weights loaded into it, an
+    optimizer of one's own) wants :meth:`round_table` behind it.
     After a call: ``loss``, ``logp``, ``lse``, and after :meth:`loss_and_grad` ``dT`` and
     ``dgain`` (both times grad_scale) and the runner's ``dlogits`` (as they are).  Arrays of another
     type, with gaps or too short are refused (ValueError)."""
@@ -1407,6 +1417,18 @@ class TableHead:
                             G.GIST_STORE_F32, gain, b["rstd"], None, d, run.dlogits, d, self.dgain,
                             b["norm_ws"], batch.labels, getattr(batch, "n_dev", None))
         self.logp, self.lse = b["logp"][:n], b["lse"][:n]
+
+    def round_table(self, ctx=None):
+        """The 16-bit copy from the table again, on the stream of ``ctx`` (the head's); nothing for
+        an fp32 head.  May be recorded."""
+        if self.table16 is None:
+            return
+        ctx = self.ctx if ctx is None else ctx
+        if not self.table16.is_cuda:
+            self.table16.copy_(self.table)
+            return
+        with torch.cuda.stream(torch.cuda.ExternalStream(ctx.stream, device=ctx.device)):
+            self.table16.copy_(self.table)
 
     def quantise(self):
         """The table in 8 bits for :meth:`score`; again after the table has changed."""

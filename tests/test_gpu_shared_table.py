@@ -1,0 +1,91 @@
+"""One table as learned input rows and as a 16-bit head's classes: what the head scores after the
+rows' step is the table as it is then, eager, on two streams and in a recorded step."""
+
+import numpy as np
+import pytest
+
+from gpu_util import to_dev
+from test_gpu_table_head import C, D, EPS, SCALE, setup
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def G():
+    from paper_2102_10424_amd import gist
+    return gist
+
+
+def make(G, ctx, dtype, seed):
+    """A batch whose inputs are rows of the table that the head scores against."""
+    import torch
+    from paper_2102_10424_amd.step import DeviceBatch, LearnedRows, SubGCN, TableHead
+    csr, n, widths, W, X, T, gain, y = setup("gcn", seed)
+    b = DeviceBatch(csr, to_dev(X), to_dev(y), "cuda")
+    run = SubGCN(ctx, "gcn", widths, n, input_grad=True)
+    head = TableHead(ctx, to_dev(T.copy()), n_cap=n, dtype=dtype, scale=SCALE, eps=EPS)
+    rows = LearnedRows(ctx, head.table, n_cap=n, head=head)
+    ids = to_dev(np.random.default_rng(seed).integers(0, C, n).astype(np.int32))
+    run.prepare(b)
+    head.prepare(n)
+    head.prepare(n, False)
+    return b, run, [to_dev(w.copy()) for w in W], head, rows, ids
+
+
+def step(b, run, params, head, rows, ids):
+    n = b.n
+    rows.lookup(ids, n, b.X)
+    run.forward(b, params)
+    head.loss_and_grad(run, b, b.X)
+    run.backward(b, params)
+    rows.sgd(ids, n, run.dH[0], 0.5)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+def test_score_after_the_rows_step(G, dtype):
+    import torch
+    from paper_2102_10424_amd.step import TableHead
+    side = torch.cuda.Stream()
+    for ctx in (G.Context(0), G.Context(0, stream=side.cuda_stream)):
+        b, run, params, head, rows, ids = made = make(G, ctx, getattr(torch, dtype), 21)
+        torch.cuda.synchronize()
+        before = head.table.clone()
+        for k in range(3):
+            if k == 2:                      # weights from elsewhere
+                torch.cuda.synchronize()
+                head.table.mul_(1.5)
+                torch.cuda.synchronize()
+                head.round_table()
+            step(*made)
+            got = head.score(run, b, b.X)
+            torch.cuda.synchronize()
+            got = {q: v.clone() for q, v in got.items()}
+            fresh = TableHead(ctx, head.table, n_cap=b.n, dtype=getattr(torch, dtype), scale=SCALE, eps=EPS)
+            torch.cuda.synchronize()
+            want = fresh.score(run, b, b.X)
+            torch.cuda.synchronize()
+            assert not torch.equal(head.table, before)
+            assert all(torch.equal(got[q], want[q]) for q in got), k
+            if head.table16 is not None:
+                assert torch.equal(head.table16, head.table.to(head.dtype))
+
+
+def test_recorded(G):
+    """Recorded once, replayed three times beside eager steps of a twin: the same bits."""
+    import torch
+    side = torch.cuda.Stream()
+    ctx, cap = G.Context(0), G.Context(0, stream=side.cuda_stream)
+    twins = [make(G, c, torch.bfloat16, 22) for c in (cap, ctx)]
+    torch.cuda.synchronize()
+    G.gist_capture_begin(cap)
+    try:
+        step(*twins[0])
+    finally:
+        rep = G.gist_capture_end(cap)
+    for k in range(3):
+        G.gist_replay_launch(ctx, rep)
+        step(*twins[1])
+        torch.cuda.synchronize()
+        for a, b in zip(*[(t[3].loss, t[3].table, t[3].table16, t[3].dT) for t in twins]):
+            assert torch.equal(a, b), k
+        assert torch.equal(twins[0][3].table16, twins[0][3].table.bfloat16()), k

@@ -1,6 +1,7 @@
 """What the end of a step refuses beyond its arrays: the norm's backward pass with labels,
-optimizers of another head, batches that the runner has no rows for.  No GPU needed: every check runs on the host before
-anything touches the device."""
+optimizers of another head, batches that the runner has no rows for, learned rows of another
+table; and that the table's copy follows them.  No GPU needed: every check runs on the host
+before anything touches the device."""
 
 import pytest
 
@@ -69,3 +70,31 @@ def test_more_rows_than_the_runner_has(calls, n):
     head.loss_and_grad(run, big)
     head.score(run, big)
     assert calls[-1] == "gist_table_xent" and run.dlogits.shape[0] >= n
+
+
+def test_learned_rows_of_another_table():
+    import torch
+    from paper_2102_10424_amd import step as S
+    T = torch.zeros(50, 5)
+    head = S.TableHead(None, T, dtype=torch.bfloat16, device="cpu")
+    for other in (torch.zeros(50, 5), T[:40], T[1:]):
+        with pytest.raises(ValueError):
+            S.LearnedRows(None, other, head=head, device="cpu")
+    assert S.LearnedRows(None, T, head=head, device="cpu").head is head
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+def test_table_copy_follows(monkeypatch, dtype):
+    """After round_table, and after the learned rows' step, the copy is the table's."""
+    import torch
+    from paper_2102_10424_amd import step as S
+    T = torch.randn(50, 5)
+    head = S.TableHead(None, T, dtype=getattr(torch, dtype), device="cpu")
+    same = lambda: head.table16 is None or torch.equal(head.table16, T.to(head.dtype))
+    T += 1
+    head.round_table()
+    assert same()
+    monkeypatch.setattr(S.G, "gist_embed_grad_sgd", lambda *a: T.mul_(2))
+    rows = S.LearnedRows(None, T, device="cpu", head=head)
+    rows.sgd(torch.zeros(3, dtype=torch.int32), 3, torch.zeros(3, 5), 0.1)
+    assert same()
