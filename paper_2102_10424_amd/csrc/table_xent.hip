@@ -16,7 +16,7 @@
 //             The given class's entries are left out of E: they are most of a
 //             gradient, and p - 1 is small where p is known to bf16 only.  dH adds
 //             (p - 1) t_y in fp32 at its end, dT the rows (p - 1) h through the
-//             learned rows' sums (embed.hip).  Rows with a logit of more than r_v + 30 get
+//             learned rows' sums (embed.hip).  Rows whose largest logit is more than 30 from r_v get
 //             their E again, from lse_v.  Three products of n C d, no more than there are.
 //   gradient, fp16   (whose range would not do) the table piece by piece: the
 //             piece's logits again, as G; then its share of dH and its rows of dT.
@@ -60,7 +60,7 @@ constexpr float kL = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr size_t kPieceBytes = size_t{256} << 20;   // G of one piece, or an fp32 piece's logits
 constexpr size_t kExpBytes = size_t{1} << 30;       // E of one piece
 constexpr int kNoSlot = INT32_MAX;
-constexpr float kFar = 30.f;                        // a row's largest logit above its reference
+constexpr float kFar = 30.f;                        // a row's largest logit from its reference
 constexpr size_t kPartBytes = size_t{64} << 20;     // fp32 partial results beyond one
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -730,7 +730,7 @@ __global__ __launch_bounds__(1024) void join_stats_kernel(int64_t row0, int64_t 
   // far off; then E comes again, from lse, and its given class after it.
   float f = 0.f;
   if (y >= 0) {
-    if (m - ref[row] > kFar) {
+    if (fabsf(m - ref[row]) > kFar) {
       far[row >> 8] = 1;
       ref[row] = l;
     }
@@ -880,7 +880,8 @@ __global__ __launch_bounds__(kBegin) void begin_kernel(Begin a) {
   }
   for (int o = a.lanes >> 1; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
   s *= a.scale;
-  // a reference that is no number would spoil rows whose own logits are; their results are NaN by themselves
+  // a reference that is no number, or none to speak of, would spoil rows whose other logits are; 0 may then lie far
+  // above a row's largest logit, which makes it far as well
   if (lane == 0) a.ref[row] = fabsf(s) < 1e30f ? s : 0.f;
 }
 
