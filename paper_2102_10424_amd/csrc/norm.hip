@@ -14,7 +14,8 @@
 //
 // 8-bit rows: e4m3, the row's largest magnitude at 448, nearest even.  The codes are those of exact
 // arithmetic on h and g (s cancels): 32 bits decide all but those near the middle between two
-// codes, which are decided again in 64 bits (one element in 60,000).  65,537 rows of 2,048 from fp32 take
+// codes, which are decided again in 64 bits (one element in 60,000 with a norm, in 150,000 without; of
+// bf16 rows without one 1 in 200 is a middle itself).  65,537 rows of 2,048 from fp32 take
 // 134 us with that and without, 16,384 of 4,096 in bf16 with a residual 114 and 95.
 //
 // The gain's gradient: a workgroup keeps its rows' sum of dy n in registers (every
@@ -161,19 +162,28 @@ __device__ __forceinline__ float scale_of(float big, float& inv) {
 }
 
 // How far a code's argument is from the middle between two codes, whose 20 lowest bits are
-// 0x80000, in units of its last place: at most 2 kNear if within kNear of it.  32 bits leave an
-// argument off by less: two roundings each of it and of the row's largest, the quotient's and the
-// product's are 6 of 2^-24 relative, 6 places at most.  (Below 2^-6 codes are 2^-9 apart; a code that
-// is one off there is 2^-18 of the row's largest, and left.)
-constexpr unsigned kNear = 8;
-__device__ __forceinline__ unsigned border(float a) { return (__float_as_uint(a) + (0x80000u + kNear)) & 0xfffffu; }
+// 0x80000, in units of its last place, times 2^12: at most 2 kNear if within kNear of it.  32 bits leave
+// an argument off by less: the quotient's and the product's roundings and, with a norm, two each of it and
+// of the row's largest, 2 or 6 of 2^-24 relative, as many places at most.
+template <bool NORM>
+constexpr unsigned kNear = (NORM ? 8u : 3u) << 12;
+template <bool NORM>
+__device__ __forceinline__ unsigned border(float a) { return (__float_as_uint(a) << 12) + (0x80000000u + kNear<NORM>); }
+// Below 2^-6 codes are 2^-9 apart throughout: 32 |a| + 1/2 has their middles where border looks for them
+// (the error is half the places above, and half of one by the addition).  What is larger becomes 1,
+// which is no middle.
+template <bool NORM>
+__device__ __forceinline__ unsigned border_small(float a) {
+  return border<NORM>(__builtin_amdgcn_fmed3f(fmaf(fabsf(a), 32.f, 0.5f), 0.f, 1.f));
+}
 
-// The float whose nearest code is a's.
+// A float whose nearest code is a's: a cut to 24 bits, the last of them set where something was cut off, so
+// that nothing but a middle itself becomes one.
 __device__ __forceinline__ float decided(double a) {
   const float f = static_cast<float>(a);
-  const unsigned u = __float_as_uint(f);
-  if ((u & 0xfffffu) != 0x80000u || static_cast<double>(f) == a) return f;
-  return __uint_as_float(fabs(a) > fabs(static_cast<double>(f)) ? u + 1 : u - 1);
+  const double w = static_cast<double>(f);
+  if (w == a) return f;
+  return __uint_as_float((__float_as_uint(f) - (fabs(w) > fabs(a) ? 1u : 0u)) | 1u);
 }
 
 template <int THREADS>
@@ -241,9 +251,12 @@ __global__ __launch_bounds__(block_of(THREADS), rows_waves(STORE, OUT, THREADS, 
       }
       const float rstd = 1.f / sqrtf(row_sum<THREADS>(s, sh, turn) * inv_d + a.eps);
       if (a.rstd && lane == 0) a.rstd[row] = rstd;
+      int at = lane;
+      // the gain's addresses, kept over the rows, would have registers of the codes spilled
+      if constexpr (OUT == GIST_STORE_E4M3 && STORE != GIST_STORE_F32) asm volatile("" : "+v"(at));
 #pragma unroll
       for (int i = 0; i < CH; ++i) {
-        const int c = (i * THREADS + lane) * V;
+        const int c = (i * THREADS + at) * V;
         if (c >= whole) continue;
         if (a.h) store_as<STORE, V>(a.h, row * a.ldh + c, h[i]);
         float g[V];
@@ -273,21 +286,23 @@ __global__ __launch_bounds__(block_of(THREADS), rows_waves(STORE, OUT, THREADS, 
       float inv;
       const float scale = scale_of(row_max<THREADS>(big, sh, turn), inv);
       if (lane == 0) a.y_scale[row] = scale;
-      unsigned near = ~0u;
+      unsigned near = ~0u, near_small = ~0u;
 #pragma unroll
       for (int i = 0; i < CH; ++i)
 #pragma unroll
         for (int q = 0; q < V; ++q) {
           h[i][q] *= inv;
-          near = min(near, border(h[i][q]));
+          near = min(near, border<NORM>(h[i][q]));
+          near_small = min(near_small, border_small<NORM>(h[i][q]));
         }
       if (TAIL) {
         t[0] *= inv;
-        near = min(near, border(t[0]));
+        near = min(near, border<NORM>(t[0]));
+        near_small = min(near_small, border_small<NORM>(t[0]));
       }
       bool again;
-      if constexpr (THREADS <= 64) again = __any(near <= 2 * kNear);
-      else again = __syncthreads_or(near <= 2 * kNear);
+      if constexpr (THREADS <= 64) again = __any(min(near, near_small) <= 2 * kNear<NORM>);
+      else again = __syncthreads_or(min(near, near_small) <= 2 * kNear<NORM>);
 #pragma unroll
       for (int i = 0; i < CH; ++i) {
         const int c = (i * THREADS + lane) * V;
@@ -298,7 +313,8 @@ __global__ __launch_bounds__(block_of(THREADS), rows_waves(STORE, OUT, THREADS, 
             static_cast<unsigned char>(__builtin_amdgcn_cvt_pk_fp8_f32(t[0], 0.f, 0, false));
       if (again) {
         // the largest is one of those that 32 bits put next to it; then what is near a middle, over
-        // the codes that have been stored
+        // the codes that have been stored; where a thread has a small one near a middle, all of its own (a second
+        // test of every element here took 12 us of 94, 65,537 rows of 2,048 in bf16)
         constexpr float kLargest = kTop * (1.f - 0x1p-20f);
         static_assert(CH * V <= 32, "a bit for each of a thread's elements");
         unsigned large = 0u, close = 0u;
@@ -309,8 +325,10 @@ __global__ __launch_bounds__(block_of(THREADS), rows_waves(STORE, OUT, THREADS, 
             float x = h[i][q];
             asm volatile("" : "+v"(x));   // from h again: no value of the tests above is kept for this
             if (fabsf(x) > kLargest) large |= 1u << (i * V + q);
-            if (border(x) <= 2 * kNear) close |= 1u << (i * V + q);
+            if (border<NORM>(x) <= 2 * kNear<NORM>) close |= 1u << (i * V + q);
           }
+        const bool all = near_small <= 2 * kNear<NORM>;
+        if (all) close = ~0u >> (32 - CH * V);
         auto column = [&](int e) { return (e / V * THREADS + lane) * V + e % V; };
         double big64 = 0.0;
 #pragma unroll 1
@@ -324,8 +342,11 @@ __global__ __launch_bounds__(block_of(THREADS), rows_waves(STORE, OUT, THREADS, 
         };
         if (inv > 0.f) {     // no row of zeros or NaN
 #pragma unroll 1
-          for (; close; close &= close - 1u) again_at(column(__ffs(close) - 1));
-          if (TAIL && tail < a.d && border(t[0]) <= 2 * kNear) again_at(tail);
+          for (; close; close &= close - 1u) {
+            const int c = column(__ffs(close) - 1);
+            if (c < whole) again_at(c);
+          }
+          if (TAIL && tail < a.d && (all || border<NORM>(t[0]) <= 2 * kNear<NORM>)) again_at(tail);
         }
       }
     }
