@@ -633,8 +633,8 @@ gist_status gist_quantize_rows(gist_ctx* ctx, int64_t n, int32_t d, const void* 
 
 /* Softmax cross-entropy of n rows H (n x d) against a table T of class
  * vectors (C x d: the layout of gist_embed_lookup's table, so the two may be
- * one), in pieces of at most 1 GiB of logits or exponentials (256 rows' where that
- * is more):
+ * one), with at most a piece of the n x C logits, or their exponentials, in
+ * memory (the sizes are at `ws` below):
  *   z_vj = scale <h_v, t_j>,  lse[v] = log sum_j exp z_vj,
  *   logp[v] = z_vy - lse[v],  *loss_dev = - mean logp over the labelled rows.
  * Rows and classes: row v is labelled if v < *n_valid_dev (one device int32,
@@ -653,11 +653,17 @@ gist_status gist_quantize_rows(gist_ctx* ctx, int64_t n, int32_t d, const void* 
  *         rounded to bf16, fp32 sums; gradients fp32
  *   GIST_STORE_BF16 / F16 (dtype ignored)    operands as stored, exponentials
  *         rounded to bf16 / fp16, fp32 sums; gradients rounded once to `store`
+ *         (by bf16 products, of fp32 arrays too, dT takes the rows of H times a factor
+ *         each, rounded to bf16 once more)
  *   GIST_STORE_E4M3   h_v = code h_scale[v], t_j = code t_scale[j] (fp32 scales,
  *         NULL for the other stores); no gradients.  fp32 sums of exact products.
  * logp and lse (n fp32 each) may be NULL.  Sums and statistics are fp32.
  * `ws` needs gist_table_xent_workspace() bytes for this descriptor (gradients:
- * whether the call has any).  Results are deterministic.  Errors: GIST_E_INVAL (negative n, C < 1,
+ * whether the call has any): room for operands at any address, 16-bit copies of H and T
+ * among it, and by fp32 products 256 MiB of logits (a row's where that is more); by bf16
+ * products with gradients 1 GiB of exponentials in bf16 (256 rows' where that is more)
+ * and, if the rows take several such pieces, dT in fp32; by fp16 products with gradients
+ * 256 MiB of them in fp16 (256 classes' of all rows where that is more).  Results are deterministic.  Errors: GIST_E_INVAL (negative n, C < 1,
  * d < 1, a leading dimension below d, unknown store or dtype, non-finite scale
  * or grad_scale, NULL H, T or labels with n > 0, NULL loss_dev, one gradient without
  * the other, gradients of E4M3 operands, scales not matching the store,

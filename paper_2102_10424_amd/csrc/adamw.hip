@@ -59,7 +59,8 @@ static_assert(sizeof(Args) <= 4096, "kernel arguments");
 typedef unsigned u32u __attribute__((aligned(1)));
 
 // A mixture of 32 bits: odd multipliers between shifts by about half the word
-// (every step can be undone, so no two inputs meet).
+// (every step can be undone, so no two inputs meet).  Shifts and multipliers are those that
+// C. Wellons found by search ("Prospecting for Hash Functions", 2018) to have the least bias.
 __host__ __device__ __forceinline__ unsigned mix(unsigned x) {
   x ^= x >> 16;
   x *= 0x7feb352du;

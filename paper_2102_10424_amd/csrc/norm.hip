@@ -12,9 +12,9 @@
 // branch a load, with long rows read again, these took 183 and 220 us, 100,000 rows of 64 in fp32
 // 49 us (now 11), and 4,000 of 16,384 in bf16 180 us (now 111).
 //
-// 8-bit rows: e4m3, the row's largest magnitude at 448, nearest even.  The codes are those of exact
-// arithmetic on h and g (s cancels): 32 bits decide all but those near the middle between two
-// codes, which are decided again in 64 bits (one element in 60,000 with a norm, in 150,000 without; of
+// 8-bit rows: e4m3, the row's largest magnitude at 448, nearest even.  The codes are those of 64-bit
+// arithmetic on h and g, h g (448 / the largest) (s cancels): 32 bits decide all but those near the middle between
+// two codes, which are decided again in 64 bits (one element in 60,000 with a norm, in 150,000 without; of
 // bf16 rows without one 1 in 200 is a middle itself).  65,537 rows of 2,048 from fp32 take
 // 134 us with that and without, 16,384 of 4,096 in bf16 with a residual 114 and 95.
 //
@@ -199,7 +199,7 @@ __device__ __forceinline__ double row_max64(double v, double* sh) {
   return v;
 }
 
-// h times the gain, exactly: h from where it has just been stored, since x or the residual may be there.
+// h times the gain in 64 bits: h from where it has just been stored, since x or the residual may be there.
 template <int STORE, bool NORM>
 __device__ __forceinline__ double exact_y(const Fwd& a, int64_t row, int c) {
   float h[1];

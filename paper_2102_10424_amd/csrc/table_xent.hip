@@ -21,13 +21,15 @@
 //   gradient, fp16   (whose range would not do) the table piece by piece: the
 //             piece's logits again, as G; then its share of dH and its rows of dT.
 // E and G are rounded to the operands' type (relative 2^-9 in bf16, 2^-11 in fp16, where
-// G is held times 2^15 so that probabilities down to 2^-29 keep all bits), as matrix
-// instructions want it; everything else is fp32.
+// G is held times 2^15 so that probabilities down to 2^-29 keep all bits), and so are, in bf16, the
+// rows of H times their factors, as matrix instructions want it; everything else is fp32.
 //
-// In bf16 with gradients 8,192 rows of 2,048 against 131,072 classes take 11.7 ms (1,130 TFLOP/s over
-// the three products), of 1,024 against 50,001 classes 2.50 ms; bound by power (1.6 to 1.75
-// GHz, the matrix cores busy 54 to 67% of the time).  One row of 1,024 against 131,072 classes: 58 us,
-// the table's bytes at 4.7 TB/s.
+// In bf16 with gradients 8,192 rows of 2,048 against 131,072 classes take 11.4 to 11.9 ms by the card (1,130
+// TFLOP/s over the three products), of 1,024 against 50,001 classes 2.48 to 2.52 ms.  The matrix cores are busy 49 to
+// 66% and 43 to 58% of the cycles, waves wait 29 to 39% of theirs: the logits' product ends in
+// its exponentials with nothing beside them, and dT's 784 tiles of the smaller one are three
+// rounds of the card and 16 more.  One row of 1,024 against 131,072 classes: 58 us, the table's bytes
+// at 4.7 TB/s.
 //
 // All products have the result's rows in the lanes and its columns in the
 // accumulator's registers: a row's maximum and sum over the classes are then
@@ -1200,7 +1202,9 @@ struct Cut {
 // number of slices with the least time in units of a whole product's tile, a
 // fortieth of it added for every slice (its partial result is written and read).  Uncut, the call of 8,192
 // rows, 50,001 classes, d 1,024 takes 2,996 us in place of 2,504, that of 1,024 rows, 50,000
-// classes, d 2,048 1,271 in place of 807.  Tiles of 256 from a quarter of a round of them on (8,192 rows, 12,000
+// classes, d 2,048 1,271 in place of 807.  With room for 1 GiB of parts, so that dT is cut as
+// well, these take 2,709 and 1,095.  Up to 256 slices in place of 64: 200,000 rows, 41 classes, d 256 446 us (452), in
+// fp16 244 (257), 100,000 rows, 200 classes, d 128 202 (198); all others the same.  Tiles of 256 from a quarter of a round of them on (8,192 rows, 12,000
 // classes, d 1,024: 719 us, 849 by tiles of 128).
 Cut cut_of(int64_t M, int64_t N, int steps) {
   Cut c{};
