@@ -1427,7 +1427,10 @@ class TableHead:
         if not self.table16.is_cuda:
             self.table16.copy_(self.table)
             return
-        with torch.cuda.stream(torch.cuda.ExternalStream(ctx.stream, device=ctx.device)):
+        # torch takes address 0 for no stream given, and makes one
+        stream = torch.cuda.ExternalStream(ctx.stream, device=ctx.device) if ctx.stream else \
+            torch.cuda.default_stream(ctx.device)
+        with torch.cuda.stream(stream):
             self.table16.copy_(self.table)
 
     def quantise(self):
