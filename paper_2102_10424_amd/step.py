@@ -821,6 +821,21 @@ def _grown(need, cap, ctx):
     return max(need, 2 * cap) if _recorded(ctx) else need
 
 
+def _stream(ctx):
+    """The context's stream as torch's (which takes address 0 for none given, and makes one)."""
+    if ctx.stream:
+        return torch.cuda.ExternalStream(ctx.stream, device=ctx.device)
+    return torch.cuda.default_stream(ctx.device)
+
+
+def _filled(ctx, device):
+    """Arrays were filled on torch's current stream: the context's goes on behind that."""
+    if torch.device(device).type == "cuda":
+        current = torch.cuda.current_stream(ctx.device)
+        if current.cuda_stream != (ctx.stream or 0):
+            _stream(ctx).wait_stream(current)
+
+
 def _check_array(name, t, dtype, n, d=None):
     """The kernels take addresses: a tensor of another type, with gaps or too short would be
     read as something else, or past its end."""
@@ -1281,6 +1296,7 @@ class AdamW:
                 st[2] if eight else None, st[3] if eight else None, copy,
                 G.GIST_STORE_BF16 if copy is None else _STORE[copy.dtype]))
         self.tensors = G.adamw_tensors(tensors)
+        _filled(ctx, device)
 
     def step(self, lr, step, betas=(0.9, 0.999), eps=1e-8, fresh=False, grad_scale=1.0, seed=None):
         """Step number ``step`` (from 1); ``fresh`` takes the moments as zero, ``seed`` (default: the
@@ -1334,6 +1350,7 @@ class TableHead:
         self.loss = torch.zeros(1, device=device)
         self.n_cap, self.ws, self.b = 0, {}, None
         self._kept = []        # outgrown buffers that a recorded step may still use
+        _filled(ctx, device)
         if n_cap:
             self._reserve(n_cap)
 
@@ -1427,10 +1444,7 @@ class TableHead:
         if not self.table16.is_cuda:
             self.table16.copy_(self.table)
             return
-        # torch takes address 0 for no stream given, and makes one
-        stream = torch.cuda.ExternalStream(ctx.stream, device=ctx.device) if ctx.stream else \
-            torch.cuda.default_stream(ctx.device)
-        with torch.cuda.stream(stream):
+        with torch.cuda.stream(_stream(ctx)):
             self.table16.copy_(self.table)
 
     def quantise(self):

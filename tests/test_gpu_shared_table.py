@@ -1,5 +1,6 @@
 """One table as learned input rows and as a 16-bit head's classes: what the head scores after the
-rows' step is the table as it is then, eager, on two streams and in a recorded step."""
+rows' step is the table as it is then, eager, on two streams and in a recorded step; heads and
+optimizers made while torch's own stream still has work."""
 
 import numpy as np
 import pytest
@@ -114,3 +115,26 @@ def test_rounded_behind_the_streams_work(G, own_stream, current):
             head.round_table()
         torch.cuda.synchronize()
         assert torch.equal(head.table16, head.table.bfloat16()), k
+
+
+def test_made_while_the_current_stream_works(G):
+    """A head and an AdamW of a context on another stream, used right after they were made: what
+    torch filled for them is there."""
+    import torch
+    from paper_2102_10424_amd.step import AdamW, TableHead
+    side = torch.cuda.Stream()
+    ctx = G.Context(0, stream=side.cuda_stream)
+    table, W, dW = torch.randn(300, 24, device="cuda"), torch.ones(5000, device="cuda"), torch.ones(5000, device="cuda")
+    ids, copy = torch.arange(300, dtype=torch.int32, device="cuda"), torch.empty(300, 24, device="cuda")
+    torch.empty(1 << 22, device="cuda").fill_(float("nan"))      # what is allocated next is not zero
+    torch.cuda.synchronize()
+    for k in range(3):
+        torch.cuda._sleep(20_000_000)      # some 10 ms
+        opt = AdamW(ctx, [dict(W=W, dW=dW)])
+        head = TableHead(ctx, table, dtype=torch.bfloat16)
+        opt.step(0.0, 1)
+        G.gist_embed_lookup(ctx, 300, 300, 24, head.table16, 24, G.GIST_STORE_BF16, ids, 1.0, copy, 24)
+        torch.cuda.synchronize()
+        m, v = opt.state[0]
+        assert bool((m == 1 - torch.tensor(0.9).float().cuda()).all()) and bool((v > 0).all()), k
+        assert torch.equal(copy, table.bfloat16().float()), k
